@@ -33,6 +33,13 @@
  *      hscale_gptq_factor               damped inverse-Cholesky factor (Algorithm 3)
  *      hscale_gptq_hscale               GPTQ with H-Scale as local quantizer (Algorithm 3)
  *
+ * What follows the quantization, which the paper leaves to other programs:
+ *
+ *   3. hscale_project                   the packed weight applied to activations, with low-rank
+ *                                       adapters of many requests beside it (serving, training)
+ *      hscale_project_backward          its gradients, for training the adapters
+ *      hscale_checkpoint_save, _load    activations kept in 8 bits for that backward pass
+ *
  * Equation numbers count the paper's displayed equations in order (Eq. 1 is the
  * effective scale s = s_g * l).
  *
@@ -483,6 +490,77 @@ int hscale_gptq_hscale(const void* w_bf16, int64_t m, int64_t n, const float* U,
                        const float* global_scale, const uint8_t* dead, int32_t block, int32_t down, int32_t up,
                        uint8_t* codes_out, uint8_t* packed_out, void* workspace, size_t workspace_bytes,
                        void* stream);
+
+/*
+ * Activations in 8 bits, kept between the forward and the backward pass of a training step.
+ * A row of x [tokens, n] (bf16, rows ld_x elements apart) is cut into blocks of 32 channels, the
+ * last one shorter.  Each block has a power of two 2^E as its scale, stored as the byte E + 127
+ * in scales [tokens, ceil(n / 32)], and one byte per element in codes [tokens, n].  With
+ * amax = f 2^p the block's largest magnitude, 1 <= f < 2, and E >= -124 always:
+ *   INT8  E = p - 6, code = RNE(x 2^-E) as a signed byte, its magnitude at most 127;
+ *   E4M3  E = p - 8, or p - 7 where f > 1.75, code = the E4M3 byte of x 2^-E (RNE), its
+ *         magnitude at most 448, or 240 with E = 120, where 256 would leave bf16's range.
+ * An element stands for code * 2^E, which is exact in bf16; an element's error is at most half a
+ * step of its grid.  A block with an Inf or NaN has the scale byte 255 and loads as NaN.
+ *
+ * x may have any alignment of 2 bytes, codes and scales any; rows of x on 16 bytes and rows of
+ * codes on 8 are faster.  Any n.  Zero sizes do nothing.
+ */
+typedef enum hscale_checkpoint_format {
+  HSCALE_CHECKPOINT_INT8 = 0,
+  HSCALE_CHECKPOINT_E4M3 = 1
+} hscale_checkpoint_format;
+
+int hscale_checkpoint_save(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, int32_t format,
+                           uint8_t* codes, int64_t ld_codes, uint8_t* scales, int64_t ld_scales, void* stream);
+
+/* x = the values that a checkpoint's elements stand for (exact). */
+int hscale_checkpoint_load(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales,
+                           int64_t tokens, int64_t n, int32_t format, void* x_bf16, int64_t ld_x, void* stream);
+
+/*
+ * A projection by the packed weight with low-rank adapters of many requests beside it:
+ *   y_t = W_hat x_t + alpha_a B_a (A_a x_t),  a = adapter_of[t]
+ * W_hat [m, n] is the dequantized weight of packed [m, n/2], codes [m, n/16] and global_scale.
+ * x [tokens, n] and y [tokens, m] are bf16 with rows ld_x and ld_y elements apart.
+ * a [adapters, rank, n], b [adapters, m, rank] (bf16, contiguous) and alpha [adapters] (fp32) are
+ * the adapters; adapters of a smaller rank are padded with zeros.  adapter_of [tokens] gives each
+ * token's adapter; a value outside [0, adapters) means none, and NULL adapter 0 for every token.
+ * With adapters == 0 the adapter arguments are ignored.
+ *
+ * Sums are fp32 (A_a x_t included), and y is rounded once.  A token's result depends on its own row
+ * and adapter only: an Inf or NaN in another token's row or adapter does not reach it.
+ *
+ * n must be a multiple of 16, rank one of 8 up to 128, adapters at most 65535.  x, y, a and b
+ * are 16-byte aligned, ld_x and ld_y multiples of 8, packed 8-byte aligned.  With n == 0, y is zero.
+ * The workspace (256-byte aligned; none is needed where the query says 0) holds A_a x_t; calls
+ * that may overlap need their own.
+ */
+size_t hscale_project_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t adapters, int64_t rank);
+int hscale_project(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, const uint8_t* packed,
+                   const uint8_t* codes, const float* global_scale, int64_t m, const void* a_bf16,
+                   const void* b_bf16, const float* alpha, int64_t adapters, int64_t rank,
+                   const int32_t* adapter_of, void* y_bf16, int64_t ld_y, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/*
+ * The gradients of hscale_project at x = the values of a checkpoint (x_codes, x_scales, x_format):
+ *   dz_t = alpha_a B_a^T dy_t,  z_t = alpha_a A_a x_t
+ *   dx_t = W_hat^T dy_t + A_a^T dz_t
+ *   da_a = sum of dz_t x_t^T,  db_a = sum of dy_t z_t^T  over the tokens with adapter_of[t] == a
+ * dy [tokens, m] and dx [tokens, n] are bf16 with rows ld_dy and ld_dx elements apart; da and db
+ * (bf16, contiguous) are shaped like a and b, and are zero for an adapter without tokens.  W_hat
+ * is frozen, and has no gradient.  dx, da or db may be NULL: it is then not computed; the checkpoint is
+ * read for da and db only.  Empty sums (tokens or m == 0) write zeros.  The rest is as in
+ * hscale_project; da and db are 16-byte aligned.
+ */
+size_t hscale_project_backward_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t adapters, int64_t rank);
+int hscale_project_backward(const void* dy_bf16, int64_t tokens, int64_t m, int64_t ld_dy, const uint8_t* x_codes,
+                            int64_t ld_x_codes, const uint8_t* x_scales, int64_t ld_x_scales, int32_t x_format,
+                            int64_t n, const uint8_t* packed, const uint8_t* codes, const float* global_scale,
+                            const void* a_bf16, const void* b_bf16, const float* alpha, int64_t adapters,
+                            int64_t rank, const int32_t* adapter_of, void* dx_bf16, int64_t ld_dx, void* da_bf16,
+                            void* db_bf16, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

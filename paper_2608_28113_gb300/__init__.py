@@ -33,7 +33,10 @@ __all__ = [
     "hscale_dequant_residual", "hscale_output_error_workspace_bytes", "hscale_output_error",
     "residual_ld", "hscale_selftest_bounded_wait", "hscale_hessian_full_workspace_bytes",
     "hscale_hessian_full_accumulate", "hscale_gptq_factor_workspace_bytes", "hscale_gptq_factor",
-    "hscale_gptq_workspace_bytes", "hscale_gptq_hscale", "EXPORTED_SYMBOLS",
+    "hscale_gptq_workspace_bytes", "hscale_gptq_hscale",
+    "HSCALE_CHECKPOINT_INT8", "HSCALE_CHECKPOINT_E4M3", "hscale_checkpoint_save", "hscale_checkpoint_load",
+    "hscale_project_workspace_bytes", "hscale_project", "hscale_project_backward_workspace_bytes",
+    "hscale_project_backward", "EXPORTED_SYMBOLS",
 ]
 
 _PKG = pathlib.Path(__file__).resolve().parent
@@ -76,6 +79,14 @@ _SIGNATURES = {
     "hscale_gptq_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _I32]),
     "hscale_gptq_hscale": (ctypes.c_int, [_P, _I64, _I64, _P, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P,
                                           ctypes.c_size_t, _P]),
+    "hscale_checkpoint_save": (ctypes.c_int, [_P, _I64, _I64, _I64, _I32, _P, _I64, _P, _I64, _P]),
+    "hscale_checkpoint_load": (ctypes.c_int, [_P, _I64, _P, _I64, _I64, _I64, _I32, _P, _I64, _P]),
+    "hscale_project_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64]),
+    "hscale_project": (ctypes.c_int, [_P, _I64, _I64, _I64, _P, _P, _P, _I64, _P, _P, _P, _I64, _I64, _P, _P, _I64,
+                                      _P, _SZ, _P]),
+    "hscale_project_backward_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64]),
+    "hscale_project_backward": (ctypes.c_int, [_P, _I64, _I64, _I64, _P, _I64, _P, _I64, _I32, _I64, _P, _P, _P, _P,
+                                               _P, _P, _I64, _I64, _P, _P, _I64, _P, _P, _P, _SZ, _P]),
 }
 EXPORTED_SYMBOLS = tuple(_SIGNATURES)
 
@@ -545,3 +556,145 @@ def hscale_gptq_factor_workspace_bytes(n: int) -> int:
 
 def hscale_gptq_workspace_bytes(m: int, n: int, block: int) -> int:
     return int(load().hscale_gptq_workspace_bytes(int(m), int(n), int(block)))
+
+
+HSCALE_CHECKPOINT_INT8, HSCALE_CHECKPOINT_E4M3 = 0, 1
+
+
+def hscale_checkpoint_save(x: torch.Tensor, fmt: int, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """Activations x (bf16 [tokens, n]) in 8 bits: codes [tokens, n] and one power-of-two scale byte per
+    32 channels, scales [tokens, ceil(n / 32)] (uint8 views with contiguous rows)."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a 2-D view")
+    tokens, n = x.shape
+    ld_x = _row_view(x, "x", torch.bfloat16, tokens, n)
+    ld_c = _row_view(codes, "codes", torch.uint8, tokens, n)
+    ld_s = _row_view(scales, "scales", torch.uint8, tokens, (n + 31) // 32)
+    _check("hscale_checkpoint_save",
+           load().hscale_checkpoint_save(_ptr(x), tokens, n, ld_x, int(fmt), _ptr(codes), ld_c, _ptr(scales), ld_s,
+                                         _stream_ptr(stream)))
+
+
+def hscale_checkpoint_load(codes: torch.Tensor, scales: torch.Tensor, fmt: int, x: torch.Tensor, stream=None) -> None:
+    """x (bf16 [tokens, n]) = the values that a checkpoint stands for."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a 2-D view")
+    tokens, n = x.shape
+    ld_x = _row_view(x, "x", torch.bfloat16, tokens, n)
+    ld_c = _row_view(codes, "codes", torch.uint8, tokens, n)
+    ld_s = _row_view(scales, "scales", torch.uint8, tokens, (n + 31) // 32)
+    _check("hscale_checkpoint_load",
+           load().hscale_checkpoint_load(_ptr(codes), ld_c, _ptr(scales), ld_s, tokens, n, int(fmt), _ptr(x), ld_x,
+                                         _stream_ptr(stream)))
+
+
+def _whole(t: torch.Tensor, name: str, dtype, shape: tuple) -> torch.Tensor:
+    _need(t, dtype, name)
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {list(shape)}")
+    return t
+
+
+def _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens: int, m: int, n: int):
+    """Checks of a packed weight and its adapters; (adapters, rank)."""
+    if n % 16 != 0:
+        raise ValueError("n must be a multiple of 16")
+    _whole(packed, "packed", torch.uint8, (m, n // 2))
+    _whole(codes, "codes", torch.uint8, (m, n // 16))
+    _need(global_scale, torch.float32, "global_scale")
+    if a is None:
+        if b is not None or alpha is not None or adapter_of is not None:
+            raise ValueError("a, b, alpha and adapter_of belong together")
+        return 0, 0
+    _need(a, torch.bfloat16, "a")
+    if a.dim() != 3:
+        raise ValueError("a must be [adapters, rank, n]")
+    adapters, rank = a.shape[0], a.shape[1]
+    _whole(a, "a", torch.bfloat16, (adapters, rank, n))
+    _whole(b, "b", torch.bfloat16, (adapters, m, rank))
+    _whole(alpha, "alpha", torch.float32, (adapters,))
+    if adapter_of is not None:
+        _whole(adapter_of, "adapter_of", torch.int32, (tokens,))
+    return adapters, rank
+
+
+def _project_workspace(workspace, nbytes: int, device):
+    if workspace is None and nbytes > 0:
+        workspace = _workspace(nbytes, device)
+    if workspace is not None:
+        _need(workspace, torch.uint8, "workspace")
+    return workspace, 0 if workspace is None else workspace.numel()
+
+
+def hscale_project_workspace_bytes(tokens: int, m: int, n: int, adapters: int, rank: int) -> int:
+    return int(load().hscale_project_workspace_bytes(int(tokens), int(m), int(n), int(adapters), int(rank)))
+
+
+def hscale_project(x: torch.Tensor, packed: torch.Tensor, codes: torch.Tensor, global_scale: torch.Tensor,
+                   a: torch.Tensor | None, b: torch.Tensor | None, alpha: torch.Tensor | None,
+                   adapter_of: torch.Tensor | None, y: torch.Tensor, workspace: torch.Tensor | None = None,
+                   stream=None) -> None:
+    """y (bf16 [tokens, m]) = x W_hat^T, plus alpha_a B_a A_a x_t with a = adapter_of[t] (int32 [tokens];
+    outside [0, adapters): none; None: adapter 0 for every token).  a [adapters, rank, n] and
+    b [adapters, m, rank] are bf16, alpha fp32 [adapters]; a, b, alpha None: no adapters."""
+    if not isinstance(x, torch.Tensor) or not isinstance(y, torch.Tensor) or x.dim() != 2 or y.dim() != 2:
+        raise ValueError("x and y must be 2-D views")
+    (tokens, n), m = x.shape, y.shape[1]
+    ld_x = _row_view(x, "x", torch.bfloat16, tokens, n)
+    ld_y = _row_view(y, "y", torch.bfloat16, tokens, m)
+    adapters, rank = _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens, m, n)
+    workspace, nbytes = _project_workspace(
+        workspace, load().hscale_project_workspace_bytes(tokens, m, n, adapters, rank) if workspace is None else 0,
+        x.device)
+    _check("hscale_project",
+           load().hscale_project(_ptr(x), tokens, n, _ld8(ld_x, tokens), _ptr(packed), _ptr(codes),
+                                 _ptr(global_scale), m, _ptr(a), _ptr(b), _ptr(alpha), adapters, rank,
+                                 _ptr(adapter_of), _ptr(y), _ld8(ld_y, tokens), _ptr(workspace), nbytes,
+                                 _stream_ptr(stream)))
+
+
+def _ld8(ld: int, rows: int) -> int:
+    """A single row's stride is free: rounded up to the alignment that the library asks for."""
+    return ld if rows > 1 else (ld + 7) // 8 * 8
+
+
+def hscale_project_backward_workspace_bytes(tokens: int, m: int, n: int, adapters: int, rank: int) -> int:
+    return int(load().hscale_project_backward_workspace_bytes(int(tokens), int(m), int(n), int(adapters), int(rank)))
+
+
+def hscale_project_backward(dy: torch.Tensor, x_codes: torch.Tensor | None, x_scales: torch.Tensor | None,
+                            x_format: int, packed: torch.Tensor, codes: torch.Tensor, global_scale: torch.Tensor,
+                            a: torch.Tensor | None, b: torch.Tensor | None, alpha: torch.Tensor | None,
+                            adapter_of: torch.Tensor | None, dx: torch.Tensor | None, da: torch.Tensor | None,
+                            db: torch.Tensor | None, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """The gradients of hscale_project for dy (bf16 [tokens, m]) at the x of a checkpoint (x_codes, x_scales,
+    x_format): dx (bf16 [tokens, n]), da and db (bf16, shaped like a and b); each may be None."""
+    if not isinstance(dy, torch.Tensor) or dy.dim() != 2:
+        raise ValueError("dy must be a 2-D view")
+    _need(packed, torch.uint8, "packed")
+    if packed.dim() != 2:
+        raise ValueError("packed must be [m, n/2]")
+    (tokens, m), n = dy.shape, 2 * packed.shape[1]
+    ld_dy = _row_view(dy, "dy", torch.bfloat16, tokens, m)
+    ld_dx = n if dx is None else _row_view(dx, "dx", torch.bfloat16, tokens, n)
+    adapters, rank = _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens, m, n)
+    if adapters == 0 and (da is not None or db is not None):
+        if a is None:
+            raise ValueError("da and db need adapters")
+    if da is not None:
+        _whole(da, "da", torch.bfloat16, (adapters, rank, n))
+    if db is not None:
+        _whole(db, "db", torch.bfloat16, (adapters, m, rank))
+    ld_c = ld_s = 0
+    if adapters > 0 and (da is not None or db is not None):
+        ld_c = _row_view(x_codes, "x_codes", torch.uint8, tokens, n)
+        ld_s = _row_view(x_scales, "x_scales", torch.uint8, tokens, (n + 31) // 32)
+    workspace, nbytes = _project_workspace(
+        workspace, load().hscale_project_backward_workspace_bytes(tokens, m, n, adapters, rank)
+        if workspace is None else 0, dy.device)
+    _check("hscale_project_backward",
+           load().hscale_project_backward(_ptr(dy), tokens, m, _ld8(ld_dy, tokens), _ptr(x_codes), ld_c,
+                                          _ptr(x_scales), ld_s, int(x_format), n, _ptr(packed), _ptr(codes),
+                                          _ptr(global_scale), _ptr(a), _ptr(b), _ptr(alpha), adapters, rank,
+                                          _ptr(adapter_of), _ptr(dx), _ld8(ld_dx, tokens), _ptr(da), _ptr(db),
+                                          _ptr(workspace), nbytes, _stream_ptr(stream)))

@@ -10,6 +10,7 @@
 
 #include "../../include/hscale.h"
 #include "hscale_internal.h"
+#include "nvfp4_weight.cuh"
 
 namespace hscale {
 
@@ -51,6 +52,61 @@ inline int check_weight(const void* w, int64_t m, int64_t n) {
   if (w == nullptr) return HSCALE_ERR_NULL;
   if (!aligned(w, 16)) return HSCALE_ERR_ALIGN;
   return HSCALE_OK;
+}
+
+// rows of bf16 that the matrix kernels read or write
+inline int check_rows(const void* x, int64_t rows, int64_t cols, int64_t ld) {
+  if (rows < 0 || cols < 0 || ld < cols) return HSCALE_ERR_SHAPE;
+  if (rows == 0 || cols == 0) return HSCALE_OK;
+  if (rows > INT32_MAX || cols > INT32_MAX || rows > INT64_MAX / 2 / ld) return HSCALE_ERR_SHAPE;
+  if (x == nullptr) return HSCALE_ERR_NULL;
+  if (!aligned(x, 16) || ld % 8 != 0) return HSCALE_ERR_ALIGN;
+  return HSCALE_OK;
+}
+
+inline int check_checkpoint(const void* x, int64_t tokens, int64_t n, int64_t ld_x, int32_t format, const uint8_t* codes,
+                            int64_t ld_codes, const uint8_t* scales, int64_t ld_scales) {
+  if (format != HSCALE_CHECKPOINT_INT8 && format != HSCALE_CHECKPOINT_E4M3) return HSCALE_ERR_ARG;
+  if (tokens < 0 || n < 0) return HSCALE_ERR_SHAPE;
+  if (tokens == 0 || n == 0) return HSCALE_OK;
+  if (ld_x < n || ld_codes < n || ld_scales < (n + 31) / 32) return HSCALE_ERR_SHAPE;
+  if (n > INT32_MAX || tokens > INT32_MAX || tokens > INT64_MAX / 2 / ld_x || tokens > INT64_MAX / ld_codes ||
+      tokens > INT64_MAX / ld_scales)
+    return HSCALE_ERR_SHAPE;
+  if (x == nullptr || codes == nullptr || scales == nullptr) return HSCALE_ERR_NULL;
+  if (!aligned(x, 2)) return HSCALE_ERR_ALIGN;
+  return HSCALE_OK;
+}
+
+// the packed weight and the adapters of a projection
+inline int check_projection(int64_t tokens, int64_t m, int64_t n, const uint8_t* packed, const uint8_t* codes,
+                            const float* global_scale, const void* a, const void* b, const float* alpha,
+                            int64_t adapters, int64_t rank, const int32_t* adapter_of) {
+  if (tokens < 0 || m < 0 || n < 0 || n % 16 != 0 || adapters < 0) return HSCALE_ERR_SHAPE;
+  if (tokens > INT32_MAX || m > INT32_MAX || n > INT32_MAX) return HSCALE_ERR_SHAPE;
+  if (adapters > 0 && (rank < 8 || rank > 128 || rank % 8 != 0)) return HSCALE_ERR_SHAPE;
+  if (adapters > 65535) return HSCALE_ERR_SHAPE;
+  if (tokens > 0 && m > 0 && n > 0) {
+    if (packed == nullptr || codes == nullptr || global_scale == nullptr) return HSCALE_ERR_NULL;
+    if (!aligned(packed, 8) || !aligned(global_scale, 4)) return HSCALE_ERR_ALIGN;
+    if (adapters > 0) {
+      if (a == nullptr || b == nullptr || alpha == nullptr) return HSCALE_ERR_NULL;
+      if (!aligned(a, 16) || !aligned(b, 16) || !aligned(alpha, 4) || !aligned(adapter_of, 4)) return HSCALE_ERR_ALIGN;
+    }
+  }
+  return HSCALE_OK;
+}
+
+inline hscale::Adapters as_adapters(const void* a, const void* b, const float* alpha, int64_t adapters, int64_t rank,
+                                    const int32_t* adapter_of) {
+  return {static_cast<const __nv_bfloat16*>(a), static_cast<const __nv_bfloat16*>(b), alpha, adapter_of,
+          (int32_t)adapters, (int32_t)rank};
+}
+
+inline int64_t round256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+inline cudaError_t zero_rows(void* x, int64_t rows, int64_t cols, int64_t ld, cudaStream_t stream) {
+  return cudaMemset2DAsync(x, (size_t)ld * 2, 0, (size_t)cols * 2, (size_t)rows, stream);
 }
 
 }  // namespace
@@ -319,10 +375,6 @@ int hscale_gptq_factor(const float* H, int64_t n, int64_t ld_h, float damp, floa
   return from_cuda(hscale::launch_gptq_factor(H, n, ld_h, damp, U, dead, info, workspace, as_stream(stream)));
 }
 
-namespace {
-inline int64_t round256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
-}  // namespace
-
 // running weights (fp32 m x n) and the bf16 split operands of the update: the errors
 // (m rows of three parts) and U's rows (n rows), each part as wide as the update's K.  Never less than
 // 12 block per row, and that is enough for a call too: its panels then have at most four blocks.
@@ -374,6 +426,98 @@ int hscale_pack_nvfp4(const void* w_bf16, int64_t m, int64_t n, const float* glo
   if (!aligned(packed_out, 8)) return HSCALE_ERR_ALIGN;
   return from_cuda(hscale::launch_pack(w_bf16, m, n, global_scale, codes, packed_out,
                                        as_stream(stream)));
+}
+
+// ---------------------------------------------------------------- 8-bit checkpoints
+int hscale_checkpoint_save(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, int32_t format, uint8_t* codes,
+                           int64_t ld_codes, uint8_t* scales, int64_t ld_scales, void* stream) {
+  const int st = check_checkpoint(x_bf16, tokens, n, ld_x, format, codes, ld_codes, scales, ld_scales);
+  if (st != HSCALE_OK || tokens == 0 || n == 0) return st;
+  return from_cuda(hscale::launch_checkpoint_save(x_bf16, tokens, n, ld_x, format, codes, ld_codes, scales, ld_scales,
+                                                  as_stream(stream)));
+}
+
+int hscale_checkpoint_load(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales,
+                           int64_t tokens, int64_t n, int32_t format, void* x_bf16, int64_t ld_x, void* stream) {
+  const int st = check_checkpoint(x_bf16, tokens, n, ld_x, format, codes, ld_codes, scales, ld_scales);
+  if (st != HSCALE_OK || tokens == 0 || n == 0) return st;
+  return from_cuda(hscale::launch_checkpoint_load(codes, ld_codes, scales, ld_scales, tokens, n, format, x_bf16, ld_x,
+                                                  as_stream(stream)));
+}
+
+// ---------------------------------------------------------------- projection with adapters
+size_t hscale_project_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t adapters, int64_t rank) {
+  (void)m, (void)n;
+  if (tokens <= 0 || adapters <= 0 || rank <= 0) return 0;
+  return (size_t)round256(tokens * rank * 4);
+}
+
+int hscale_project(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, const uint8_t* packed,
+                   const uint8_t* codes, const float* global_scale, int64_t m, const void* a_bf16, const void* b_bf16,
+                   const float* alpha, int64_t adapters, int64_t rank, const int32_t* adapter_of, void* y_bf16,
+                   int64_t ld_y, void* workspace, size_t workspace_bytes, void* stream) {
+  int st = check_projection(tokens, m, n, packed, codes, global_scale, a_bf16, b_bf16, alpha, adapters, rank, adapter_of);
+  if (st == HSCALE_OK) st = check_rows(x_bf16, tokens, n, ld_x);
+  if (st == HSCALE_OK) st = check_rows(y_bf16, tokens, m, ld_y);
+  if (st != HSCALE_OK || tokens == 0 || m == 0) return st;
+  if (n == 0) return from_cuda(zero_rows(y_bf16, tokens, m, ld_y, as_stream(stream)));
+  const size_t need = hscale_project_workspace_bytes(tokens, m, n, adapters, rank);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 256))) return HSCALE_ERR_WORKSPACE;
+  const hscale::Nvfp4Weight w = {packed, codes, global_scale, m, n};
+  const hscale::Adapters ad = as_adapters(a_bf16, b_bf16, alpha, adapters, rank, adapter_of);
+  float* z = static_cast<float*>(workspace);
+  cudaStream_t s = as_stream(stream);
+  if (adapters > 0) {
+    const cudaError_t err = hscale::launch_adapter_down(x_bf16, ld_x, nullptr, 0, tokens, n, ad, z, s);
+    if (err != cudaSuccess) return HSCALE_ERR_CUDA;
+  }
+  return from_cuda(hscale::launch_project(true, x_bf16, tokens, ld_x, w, ad, z, y_bf16, ld_y, s));
+}
+
+size_t hscale_project_backward_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t adapters, int64_t rank) {
+  return 2 * hscale_project_workspace_bytes(tokens, m, n, adapters, rank);
+}
+
+int hscale_project_backward(const void* dy_bf16, int64_t tokens, int64_t m, int64_t ld_dy, const uint8_t* x_codes,
+                            int64_t ld_x_codes, const uint8_t* x_scales, int64_t ld_x_scales, int32_t x_format,
+                            int64_t n, const uint8_t* packed, const uint8_t* codes, const float* global_scale,
+                            const void* a_bf16, const void* b_bf16, const float* alpha, int64_t adapters, int64_t rank,
+                            const int32_t* adapter_of, void* dx_bf16, int64_t ld_dx, void* da_bf16, void* db_bf16,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  int st = check_projection(tokens, m, n, packed, codes, global_scale, a_bf16, b_bf16, alpha, adapters, rank, adapter_of);
+  if (st == HSCALE_OK) st = check_rows(dy_bf16, tokens, m, ld_dy);
+  if (st == HSCALE_OK && dx_bf16 != nullptr) st = check_rows(dx_bf16, tokens, n, ld_dx);
+  const bool grads = adapters > 0 && (da_bf16 != nullptr || db_bf16 != nullptr);
+  if (st == HSCALE_OK && grads) {
+    if (!aligned(da_bf16, 16) || !aligned(db_bf16, 16)) return HSCALE_ERR_ALIGN;
+    st = check_checkpoint(dy_bf16, tokens, n, n, x_format, x_codes, ld_x_codes, x_scales, ld_x_scales);
+  }
+  if (st != HSCALE_OK) return st;
+  cudaStream_t s = as_stream(stream);
+  if (tokens == 0 || m == 0 || n == 0) {
+    // empty sums: the outputs that exist are zero
+    cudaError_t err = cudaSuccess;
+    if (dx_bf16 != nullptr && tokens > 0 && n > 0) err = zero_rows(dx_bf16, tokens, n, ld_dx, s);
+    if (err == cudaSuccess && grads && da_bf16 != nullptr && n > 0) err = cudaMemsetAsync(da_bf16, 0, (size_t)(adapters * rank * n) * 2, s);
+    if (err == cudaSuccess && grads && db_bf16 != nullptr && m > 0) err = cudaMemsetAsync(db_bf16, 0, (size_t)(adapters * rank * m) * 2, s);
+    return from_cuda(err);
+  }
+  const size_t need = hscale_project_backward_workspace_bytes(tokens, m, n, adapters, rank);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 256))) return HSCALE_ERR_WORKSPACE;
+  const hscale::Nvfp4Weight w = {packed, codes, global_scale, m, n};
+  const hscale::Adapters ad = as_adapters(a_bf16, b_bf16, alpha, adapters, rank, adapter_of);
+  const hscale::Checkpoint x = {x_codes, x_scales, ld_x_codes, ld_x_scales};
+  float* z = static_cast<float*>(workspace);
+  float* dz = z + need / 8;
+  cudaError_t err = cudaSuccess;
+  if (adapters > 0) err = hscale::launch_adapter_up_t(dy_bf16, ld_dy, tokens, m, ad, dz, s);
+  if (err == cudaSuccess && dx_bf16 != nullptr) err = hscale::launch_project(false, dy_bf16, tokens, ld_dy, w, ad, dz, dx_bf16, ld_dx, s);
+  if (err == cudaSuccess && grads && da_bf16 != nullptr) err = hscale::launch_adapter_grad_a(x, x_format, tokens, n, ad, dz, da_bf16, s);
+  if (err == cudaSuccess && grads && db_bf16 != nullptr) {
+    err = hscale::launch_adapter_down(nullptr, 0, &x, x_format, tokens, n, ad, z, s);
+    if (err == cudaSuccess) err = hscale::launch_adapter_grad_b(dy_bf16, ld_dy, tokens, m, ad, z, db_bf16, s);
+  }
+  return from_cuda(err);
 }
 
 }  // extern "C"

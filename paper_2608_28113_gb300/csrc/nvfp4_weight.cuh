@@ -1,0 +1,64 @@
+// nvfp4_weight.cuh -- the packed NVFP4 weight and the 8-bit checkpoint as kernels read them.
+#pragma once
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "hscale_device.cuh"
+
+namespace hscale {
+
+// W_hat[f, k] = s_g * E4M3(code[f, k / 16]) * E2M1(nibble[f, k]); n % 16 == 0.
+struct Nvfp4Weight {
+  const uint8_t* packed;      // [m, n / 2], 8-byte aligned
+  const uint8_t* codes;       // [m, n / 16]
+  const float* global_scale;  // device scalar
+  int64_t m, n;
+};
+
+// E4M3 value of a code byte, read as the rest of the library reads codes: sign cleared, in [1, 126].
+__device__ __forceinline__ uint32_t ladder_code(uint32_t c) {
+  return min(max(c & 0x7Fu, 1u), kE4M3MaxCode);
+}
+
+// The low-rank adapters of a call: A [count, rank, n], B [count, m, rank], alpha [count], and the
+// adapter of each token (nullptr: adapter 0 for all).
+struct Adapters {
+  const __nv_bfloat16* a;
+  const __nv_bfloat16* b;
+  const float* alpha;
+  const int32_t* of_token;
+  int32_t count, rank;
+};
+
+// The adapter of token t, or -1 for none.
+__device__ __forceinline__ int adapter_of(const Adapters& ad, int64_t t) {
+  if (ad.count == 0) return -1;
+  if (ad.of_token == nullptr) return 0;
+  const int a = ad.of_token[t];
+  return (unsigned)a < (unsigned)ad.count ? a : -1;
+}
+
+// Activations in 8 bits: codes [tokens, cols] and a power-of-two scale byte per 32 channels.
+constexpr int kCkptBlock = 32;
+constexpr int kCkptInt8 = 0, kCkptE4M3 = 1;
+struct Checkpoint {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  int64_t ld_codes, ld_scales;
+};
+
+// 2^(byte - 127); byte 255 is NaN, and byte 0, which no save writes, 0.
+__device__ __forceinline__ float ckpt_scale(uint32_t byte) {
+  return __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23);
+}
+
+// An element as the value it stands for, in units of its block's scale.
+template <int kFormat>
+__device__ __forceinline__ float ckpt_element(uint32_t code) {
+  if (kFormat == kCkptInt8) return (float)(int)(int8_t)(uint8_t)code;
+  const float v = e4m3_mag(code & 0x7Fu);
+  return (code & 0x80u) ? -v : v;
+}
+
+}  // namespace hscale
