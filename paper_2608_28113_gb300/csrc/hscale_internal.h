@@ -154,6 +154,7 @@ cudaError_t read_output_error_device_error(uint32_t* flags);
 cudaError_t read_update_device_error(uint32_t* flags);
 cudaError_t read_gptq_device_error(uint32_t* flags);
 cudaError_t read_hessian_cluster_device_error(uint32_t* flags);
+cudaError_t read_project_device_error(uint32_t* flags);
 cudaError_t read_selftest_device_error(uint32_t* flags);
 
 // One CTA waits at most `polls` polls on an mbarrier that nothing arrives on.

@@ -1,81 +1,607 @@
-// project.cu -- the product of activations with a packed NVFP4 weight, with each token's adapter added:
+// project.cu -- the product of activations with a packed NVFP4 weight on the tcgen05 tensor cores, with each
+// token's adapter added as the result leaves tensor memory:
 //   y_t  = W_hat x_t + B_a z_t        (forward;  z  = alpha_a A_a x_t,    adapter.cu)
 //   dx_t = W_hat^T dy_t + A_a^T dz_t  (backward; dz = alpha_a B_a^T dy_t, adapter.cu)
 // Accumulated in fp32 and rounded once, to bf16.
+//
+// The weight never exists in bf16 outside shared memory.  E2M1 times E4M3 has at most 6 significant bits, so
+// each weight without s_g is exact in bf16 (2^-7 of it is what the tile holds, see unpack8); s_g is a
+// factor of the accumulator.
+//
+// Tile: 128 outputs (M, the weight) x kN tokens (N), K in blocks of 64.  14 warps:
+//   0      TMA loads of the tokens' tile, K-major, 128-byte swizzle
+//   1      MMAs
+//   2-5    epilogue: tensor memory -> s_g, adapter, bf16 -> out (lane = output, columns = tokens)
+//   6-13   the weight's tile: 16 packed bytes and 2 codes a thread and K block, kept kAhead blocks ahead in
+//          registers, unpacked into the swizzled tile.  Forward (K = n) the tile is K-major, backward
+//          (K = m, outputs = n) the same packed rows make it MN-major, so W is read as it is stored.
+// Each weight is unpacked once per kN tokens: about 2.7 instructions a weight against kN / 64 tensor-core
+// cycles, so at kN = 256 the unpacking hides behind the MMAs.
+//
+// Where the tiles leave SMs idle, a cluster of csize CTAs splits K: each rank accumulates its share, hands the
+// others the columns they own through distributed shared memory, and finishes its own columns, summing in rank
+// order.  With csize 1 the grid is persistent and the epilogue of a tile runs beside the MMAs of the next (two
+// accumulators in tensor memory).
+//
+// The adapter's term is a dot product of `rank` fp32 numbers per result on the epilogue's FMA pipes rather than
+// more K columns of the MMAs: there a token that does not use an adapter would meet it as 0 times its values,
+// and an Inf or NaN in one request's adapter would spoil the others' tokens.
+//
+// Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>
 
 #include "hscale_internal.h"
 #include "nvfp4_weight.cuh"
+#include "tcgen05.cuh"
+#include "tma.cuh"
 
 namespace hscale {
 namespace {
 
-// 64 tokens x 64 outputs a block, 16 of the summed axis a step, 4 x 4 outputs a thread.
-// kForward: out[t, f] over k < n; else out[t, j] over f < m.
-template <bool kForward>
-__global__ void __launch_bounds__(256)
-project_kernel(const uint16_t* __restrict__ v, int64_t tokens, int64_t ld_v, Nvfp4Weight w, Adapters ad, const float* z,
-               __nv_bfloat16* out, int64_t ld_out) {
-  __shared__ float sv[16][65], sw[16][65];
-  const int64_t outs = kForward ? w.m : w.n, depth = kForward ? w.n : w.m;
-  const int64_t t0 = (int64_t)blockIdx.y * 64, o0 = (int64_t)blockIdx.x * 64;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  for (int64_t k0 = 0; k0 < depth; k0 += 16) {
-    for (int i = threadIdx.x; i < 1024; i += 256) {
-      const int k = i & 15, t = i >> 4;
-      sv[k][t] = t0 + t < tokens && k0 + k < depth ? __uint_as_float((uint32_t)v[(t0 + t) * ld_v + k0 + k] << 16) : 0.0f;
-      const int kk = kForward ? k : i >> 6, oo = kForward ? t : i & 63;
-      const int64_t f = kForward ? o0 + oo : k0 + kk, c = kForward ? k0 + kk : o0 + oo;
-      float q = 0.0f;
-      if (f < w.m && c < w.n) {
-        const uint32_t nib = (w.packed[f * (w.n / 2) + c / 2] >> (4 * (c & 1))) & 15u;
-        q = e4m3_mag(ladder_code(w.codes[f * (w.n / 16) + c / 16])) * e2m1_from_raw((nib & 7u) << 22);
-        if (nib & 8u) q = -q;
-      }
-      sw[kk][oo] = q;
-    }
-    __syncthreads();
+constexpr int kBM = 128, kBK = 64;
+constexpr int kThreads = 448;
+constexpr int kUnpackThreads = 256, kUnpackWarp0 = 6;
+constexpr int kAhead = 8;
+constexpr uint32_t kTileABytes = kBM * kBK * 2;  // 16 KB
+constexpr uint32_t kGroupBytes = 64 * kBK * 2;   // MN-major: 64 outputs x 64 rows of K
+
+template <int kN>
+struct Tile {
+  static constexpr int kStages = kN == 256 ? 4 : kN == 128 ? 5 : 6;
+  static constexpr uint32_t kBBytes = kN * kBK * 2;
+  static constexpr uint32_t kStageBytes = kTileABytes + kBBytes;
+  static constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 /* alignment */ + 256 /* barriers */;
+  static constexpr uint32_t kTmemCols = 2 * kN;
+};
+
+__device__ uint32_t g_project_flags = 0;
+
+struct ProjectArgs {
+  Nvfp4Weight w;
+  Adapters ad;
+  const float* z;
+  __nv_bfloat16* out;
+  int64_t tokens, ld_out;
+  int32_t kb_total, tiles_t, tiles_o, csize, chained;
+};
+
+// ---------------------------------------------------------------- weights
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Two code bytes as bf16x2 E4M3 2^119.  A byte shifted to bf16's mantissa and low exponent bits reads as
+// E4M3 2^-120, subnormals included (the formats' subnormal boundaries line up).
+__device__ __forceinline__ uint32_t unpack_codes(uint32_t c2) {
+  uint32_t c = (c2 & 0x7Fu) | ((c2 & 0x7F00u) << 8);
+  c = __vminu2(__vmaxu2(c, 0x00010001u), kE4M3MaxCode * 0x00010001u);
+  return mul_bf16x2(mul_bf16x2(c << 4, 0x7F007F00u /* 2^127 */), 0x77807780u /* 2^112 */);
+}
+
+// Eight nibbles times a scale (bf16x2, both halves): a nibble's magnitude bits at bf16's bits 8-6 read as
+// E2M1 2^-126, so with scales E4M3 2^119 the products are the weights 2^-7, exact.
+__device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t (&r)[4]) {
+  constexpr uint32_t kSign = 0x80008000u, kMag = 0x01C001C0u;
+  const uint32_t up = w << 4;
+  // halves (nibble 0 | 2 at bits 4 | 12, nibble 1 | 3 likewise), and the same of nibbles 4-7
+  const uint32_t a = __byte_perm(up, w, 0x5410), b = __byte_perm(up, w, 0x7632);
+  r[0] = mul_bf16x2(((a << 8) & kSign) | ((a << 2) & kMag), scale);
+  r[1] = mul_bf16x2((a & kSign) | ((a >> 6) & kMag), scale);
+  r[2] = mul_bf16x2(((b << 8) & kSign) | ((b << 2) & kMag), scale);
+  r[3] = mul_bf16x2((b & kSign) | ((b >> 6) & kMag), scale);
+}
+
+__device__ __forceinline__ uint2 ld_v2_ahead(const void* p) {
+  uint2 r;
+  asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ uint4 ld_v4_ahead(const void* p) {
+  uint4 r;
+  asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ uint32_t ld_u16_ahead(const void* p) {
+  uint16_t r;
+  asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(r) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ uint32_t ld_u8_ahead(const void* p) {
+  uint32_t r;
+  asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(r) : "l"(p));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+
+// ---------------------------------------------------------------- epilogue
+// Results of tokens t0 .. t0 + W - 1 and this lane's output o: v (without the adapters' terms) plus each
+// token's adapter, rounded and stored.  The tokens' adapters are uniform over the warp; the lane keeps its 8
+// factors of an adapter while the tokens stay on it.
+template <bool kForward, int W>
+__device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p) {
+  const int64_t outs = kForward ? p.w.m : p.w.n;
+  const bool on = o < outs;
+  int id = -1;
+  if (lane < W && t0 + lane < p.tokens) id = adapter_of(p.ad, t0 + lane);
+  if (__any_sync(0xFFFFFFFFu, id >= 0)) {
+    const int rank = p.ad.rank;
+    for (int r0 = 0; r0 < rank; r0 += 8) {
+      int cur = -1;
+      float f[8];
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
+      for (int j = 0; j < 8; ++j) f[j] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int j = 0; j < W; ++j) {
+        const int a = __shfl_sync(0xFFFFFFFFu, id, j);
+        if (a < 0) continue;
+        if (a != cur) {
+          cur = a;
+          if (on) {
+            if (kForward) {
+              const uint4 q = *reinterpret_cast<const uint4*>(p.ad.b + ((int64_t)a * p.w.m + o) * rank + r0);
+              f[0] = bf16_lo(q.x), f[1] = bf16_hi(q.x), f[2] = bf16_lo(q.y), f[3] = bf16_hi(q.y);
+              f[4] = bf16_lo(q.z), f[5] = bf16_hi(q.z), f[6] = bf16_lo(q.w), f[7] = bf16_hi(q.w);
+            } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sv[k][ty + 16 * i], sw[k][tx + 16 * j], acc[i][j]);
-    __syncthreads();
-  }
-  const float sg = *w.global_scale;
-  for (int i = 0; i < 4; ++i) {
-    const int64_t t = t0 + ty + 16 * i;
-    if (t >= tokens) continue;
-    const int a = adapter_of(ad, t);
-    for (int j = 0; j < 4; ++j) {
-      const int64_t o = o0 + tx + 16 * j;
-      if (o >= outs) continue;
-      float s = acc[i][j] * sg;
-      if (a >= 0) {
-        float low = 0.0f;
-        for (int r = 0; r < ad.rank; ++r) {
-          const int64_t e = kForward ? ((int64_t)a * w.m + o) * ad.rank + r : ((int64_t)a * ad.rank + r) * w.n + o;
-          low = fmaf(z[t * ad.rank + r], __bfloat162float((kForward ? ad.b : ad.a)[e]), low);
+              for (int i = 0; i < 8; ++i) f[i] = __bfloat162float(p.ad.a[((int64_t)a * rank + r0 + i) * p.w.n + o]);
+            }
+          }
         }
-        s += low;
+        const float4* zp = reinterpret_cast<const float4*>(p.z + (t0 + j) * rank + r0);
+        const float4 z0 = zp[0], z1 = zp[1];
+        float s = v[j];
+        s = fmaf(z0.x, f[0], s), s = fmaf(z0.y, f[1], s), s = fmaf(z0.z, f[2], s), s = fmaf(z0.w, f[3], s);
+        s = fmaf(z1.x, f[4], s), s = fmaf(z1.y, f[5], s), s = fmaf(z1.z, f[6], s), s = fmaf(z1.w, f[7], s);
+        v[j] = s;
       }
-      out[t * ld_out + o] = __float2bfloat16_rn(s);
     }
   }
+  if (!on) return;
+  __nv_bfloat16* dst = p.out + t0 * p.ld_out + o;
+#pragma unroll
+  for (int j = 0; j < W; ++j)
+    if (t0 + j < p.tokens) dst[j * p.ld_out] = __float2bfloat16_rn(v[j]);
+}
+
+// Tile t of the persistent order: groups of 8 token tiles, the outputs' tiles along a group, so that the
+// tiles in flight at once share token tiles and weights in L2.
+__device__ __forceinline__ void raster(int t, const ProjectArgs& p, int& tt, int& to) {
+  const int group = t / (8 * p.tiles_o) * 8;
+  const int rows = min(8, p.tiles_t - group);
+  const int within = t - group * p.tiles_o;
+  tt = group + within % rows;
+  to = within / rows;
+}
+
+template <bool kForward, int kN>
+__global__ void __launch_bounds__(kThreads, 1)
+project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ ProjectArgs p) {
+  using T = Tile<kN>;
+  constexpr int kStages = T::kStages;
+  extern __shared__ __align__(16) uint8_t dynamic_smem[];
+  uint8_t* smem = dynamic_smem + ((1024u - (smem_addr(dynamic_smem) & 1023u)) & 1023u);
+  uint8_t* tile_a = smem;
+  uint8_t* tile_b = smem + kStages * kTileABytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kStages * T::kStageBytes);
+  uint64_t* empty = full + kStages;
+  uint64_t* acc_full = empty + kStages;
+  uint64_t* acc_empty = acc_full + 2;
+  uint64_t* mma_done = acc_empty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
+  uint32_t* failed = tmem_slot + 1;
+
+  const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int csize = p.csize;
+  const int crank = csize > 1 ? (int)cluster_rank() : 0;
+  const int tiles = p.tiles_t * p.tiles_o;
+  // csize 1: tiles blockIdx.x, + gridDim.x, ...; else one tile a cluster, K blocks [kb0, kb1) of it
+  const int first = csize > 1 ? (int)blockIdx.x / csize : (int)blockIdx.x;
+  const int step = (int)gridDim.x;
+  const int ntiles = csize > 1 ? 1 : (tiles - first + step - 1) / step;
+  const int kb0 = (int)((int64_t)p.kb_total * crank / csize), kb1 = (int)((int64_t)p.kb_total * (crank + 1) / csize);
+  const int kbs = kb1 - kb0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1 + kUnpackThreads / 32);  // the TMA load and each unpacking warp
+      mbar_init(&empty[s], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], 128);
+    }
+    mbar_init(mma_done, 1);
+    *failed = 0u;
+    mbar_fence_init();
+    prefetch_tensormap(&vmap);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_addr(tmem_slot), T::kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_d = warp_uniform(*tmem_slot);
+
+  // the epilogue's thread: tensor-memory lane, output of a tile
+  const uint32_t quarter = (uint32_t)(warp & 3);
+  const uint32_t lane_base = (quarter * 32u) << 16;
+  const int out_row = (int)quarter * 32 + lane;
+  bool have = true;  // the cluster's partial is complete
+
+  if (warp == 0) {
+    uint64_t policy;
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
+    uint32_t s = 0, parity = 1;
+    bool go = true;
+    for (int i = 0; i < ntiles && go; ++i) {
+      int tt, to;
+      raster(first + i * step, p, tt, to);
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait_warp(&empty[s], parity)) {
+          if (lane == 0) atomicOr(failed, 1u);
+          go = false;
+          break;
+        }
+        if (elect_one()) {
+          mbar_arrive_expect_tx(&full[s], T::kBBytes);
+          tma_load_2d(tile_b + s * T::kBBytes, &vmap, kb * kBK, tt * kN, &full[s], policy);
+        }
+        __syncwarp();
+        if (++s == kStages) {
+          s = 0;
+          parity ^= 1u;
+        }
+      }
+    }
+    // a full barrier also waits for the unpacking warps, whose waits are bounded like this one's
+    ring_drain(full, kStages, s, parity);
+  } else if (warp == 1) {
+    constexpr uint32_t kIdesc = idesc_bf16_f32(kBM, kN) | (kForward ? 0u : 1u << 15);
+    uint32_t s = 0, parity = 0;
+    bool ok = true;
+    for (int i = 0; i < ntiles && ok; ++i) {
+      const uint32_t acc = (uint32_t)i & 1u;
+      if (i >= 2 && !mbar_wait_warp(&acc_empty[acc], (uint32_t)((i >> 1) - 1) & 1u)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after_sync();
+      for (int kb = 0; kb < kbs; ++kb) {
+        if (!mbar_wait_warp(&full[s], parity)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after_sync();
+        if (elect_one()) {
+          const uint32_t a = smem_addr(tile_a + s * kTileABytes), b = smem_addr(tile_b + s * T::kBBytes);
+          const uint64_t ad = kForward ? smem_desc_k_sw128(a) : smem_desc_mn_sw128(a, kGroupBytes);
+          const uint64_t bd = smem_desc_k_sw128(b);
+#pragma unroll
+          for (int kk = 0; kk < kBK / 16; ++kk)
+            umma_bf16(tmem_d + acc * kN, ad + (kForward ? 2 : 128) * kk, bd + 2 * kk, kIdesc, (uint32_t)(kb > 0 || kk > 0));
+          umma_commit(smem_addr(&empty[s]));
+          if (kb + 1 == kbs) umma_commit(smem_addr(&acc_full[acc]));
+        }
+        __syncwarp();
+        if (++s == kStages) {
+          s = 0;
+          parity ^= 1u;
+        }
+      }
+    }
+    if (!ok && lane == 0) atomicOr(failed, 1u);
+    __syncwarp();
+    umma_drain(mma_done);
+  } else if (warp < kUnpackWarp0) {
+    if (csize == 1) {
+      const float scale = *p.w.global_scale * 128.0f;
+      if (p.chained) pdl_wait_primary();  // z
+      for (int i = 0; i < ntiles; ++i) {
+        int tt, to;
+        raster(first + i * step, p, tt, to);
+        const uint32_t acc = (uint32_t)i & 1u;
+        if (!mbar_wait_acc(&acc_full[acc], (uint32_t)(i >> 1) & 1u)) {
+          atomicOr(failed, 1u);
+          break;
+        }
+        tc_fence_after_sync();
+        const int64_t o = (int64_t)to * kBM + out_row;
+#pragma unroll 1
+        for (int c = 0; c < kN; c += 32) {
+          const int64_t t0 = (int64_t)tt * kN + c;
+          uint32_t q[32];
+          tmem_ld_32x32b_x32(tmem_d + acc * kN + lane_base + (uint32_t)c, q);
+          tmem_ld_wait();
+          if (c + 32 == kN) {
+            tc_fence_before_sync();
+            mbar_arrive(&acc_empty[acc]);
+          }
+          if (t0 >= p.tokens) continue;
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(q[j]) * scale;
+          finish<kForward, 32>(v, t0, o, lane, p);
+        }
+      }
+    } else {
+      have = mbar_wait_acc(&acc_full[0], 0u);
+      if (!have) atomicOr(failed, 1u);
+      tc_fence_after_sync();
+    }
+  } else {
+    // ---- the weight's tile.  Thread: row of the tile (forward: output; backward: K), a half of its 64 columns
+    const int tid = (int)threadIdx.x - kUnpackWarp0 * 32;
+    const int group = kForward ? 0 : tid >> 7;  // backward: 64 outputs each
+    const int row = kForward ? tid >> 1 : (tid & 127) >> 1, half = tid & 1;
+    const int64_t m = p.w.m, n = p.w.n;
+    const bool wide = (n & 31) == 0 && ((reinterpret_cast<uintptr_t>(p.w.packed) & 15) | (reinterpret_cast<uintptr_t>(p.w.codes) & 1)) == 0;
+    uint8_t* const dst0 = tile_a + group * kGroupBytes + row * 128;
+    // position of the next block to load
+    int li = 0, lk = kb0;
+    int64_t f = 0, k0 = 0;
+    const int total = ntiles * kbs;
+    auto start_tile = [&]() {
+      int tt, to;
+      raster(first + li * step, p, tt, to);
+      f = kForward ? (int64_t)to * kBM + row : (int64_t)lk * kBK + row;
+      k0 = kForward ? (int64_t)lk * kBK + half * 32 : (int64_t)to * kBM + group * 64 + half * 32;
+    };
+    uint4 ring[kAhead];
+    uint32_t codes[kAhead];
+    auto load = [&](uint4& q, uint32_t& c) {
+      q = make_uint4(0u, 0u, 0u, 0u);
+      c = 0u;
+      if (f < m && k0 < n) {
+        const uint8_t* wp = p.w.packed + f * (n >> 1) + (k0 >> 1);
+        const uint8_t* cp = p.w.codes + f * (n >> 4) + (k0 >> 4);
+        if (wide) {
+          q = ld_v4_ahead(wp);
+          c = ld_u16_ahead(cp);
+        } else {
+          const uint2 lo = ld_v2_ahead(wp);
+          q.x = lo.x, q.y = lo.y;
+          c = ld_u8_ahead(cp);
+          if (k0 + 16 < n) {
+            const uint2 hi = ld_v2_ahead(wp + 8);
+            q.z = hi.x, q.w = hi.y;
+            c |= ld_u8_ahead(cp + 1) << 8;
+          }
+        }
+      }
+      if (kForward) k0 += kBK; else f += kBK;
+      if (++lk == kb1) {
+        lk = kb0;
+        if (++li < ntiles) start_tile();
+      }
+    };
+    start_tile();
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (u < total) load(ring[u], codes[u]);
+    uint32_t s = 0, parity = 1;
+    bool go = true;
+    for (int base = 0; base < total && go; base += kAhead) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (base + u >= total || !go) break;
+        if (!mbar_wait_warp(&empty[s], parity)) {
+          if (lane == 0) atomicOr(failed, 1u);
+          go = false;
+          break;
+        }
+        uint8_t* dst = dst0 + s * kTileABytes;
+        const uint32_t sc = unpack_codes(codes[u]);
+        const uint32_t s0 = __byte_perm(sc, sc, 0x1010), s1 = __byte_perm(sc, sc, 0x3232);
+        const uint32_t w[4] = {ring[u].x, ring[u].y, ring[u].z, ring[u].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t r[4];
+          unpack8(w[i], i < 2 ? s0 : s1, r);
+          *reinterpret_cast<uint4*>(dst + (((half * 4 + i) ^ (row & 7)) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[s]);
+        if (++s == kStages) {
+          s = 0;
+          parity ^= 1u;
+        }
+        if (base + u + kAhead < total) load(ring[u], codes[u]);
+      }
+    }
+  }
+
+  if (csize > 1) {
+    // the ranks' partials: rank d owns columns [d own, (d + 1) own); the ring is free once every rank's MMAs
+    // have completed, and its memory takes [source][column][output]
+    const int own = kN / csize;
+    float* inbox = reinterpret_cast<float*>(smem);
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after_sync();
+    const bool epilogue = warp >= 2 && warp < kUnpackWarp0;
+    int tt, to;
+    raster(first, p, tt, to);
+    if (epilogue) {
+      for (int d = 0; d < csize; ++d) {
+        if (d == crank) continue;
+        const uint32_t base = mapa(smem_addr(inbox + (crank * own) * kBM + out_row), (uint32_t)d);
+        for (int c = 0; c < own; c += 8) {
+          uint32_t q[8];
+          tmem_ld_32x32b_x8(tmem_d + lane_base + (uint32_t)(d * own + c), q);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(base + (uint32_t)((c + j) * kBM * 4)),
+                         "r"(have ? q[j] : 0x7FC00000u)
+                         : "memory");
+        }
+      }
+    }
+    cluster_sync();
+    if (epilogue) {
+      const float scale = *p.w.global_scale * 128.0f;
+      if (p.chained) pdl_wait_primary();  // z
+      const int64_t o = (int64_t)to * kBM + out_row;
+      for (int c = 0; c < own; c += 8) {
+        const int64_t t0 = (int64_t)tt * kN + crank * own + c;
+        uint32_t q[8];
+        tmem_ld_32x32b_x8(tmem_d + lane_base + (uint32_t)(crank * own + c), q);
+        tmem_ld_wait();
+        if (t0 >= p.tokens) continue;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float mine = have ? __uint_as_float(q[j]) : __int_as_float(0x7FC00000);
+          float sum = 0.0f;
+          for (int d = 0; d < csize; ++d)
+            sum += d == crank ? mine : inbox[(d * own + c + j) * kBM + out_row];
+          v[j] = sum * scale;
+        }
+        finish<kForward, 8>(v, t0, o, lane, p);
+      }
+    }
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_d, T::kTmemCols);
+  }
+  if (*failed) {
+    if (threadIdx.x == 0) atomicOr(&g_project_flags, kErrMbarTimeout);
+    if (csize == 1 && warp >= 2 && warp < kUnpackWarp0) {
+      for (int i = 0; i < ntiles; ++i) {
+        int tt, to;
+        raster(first + i * step, p, tt, to);
+        const int64_t o = (int64_t)to * kBM + out_row;
+        for (int64_t t = (int64_t)tt * kN; t < min(p.tokens, (int64_t)(tt + 1) * kN); ++t)
+          if (o < (kForward ? p.w.m : p.w.n)) p.out[t * p.ld_out + o] = __ushort_as_bfloat16(0x7FC0);
+      }
+    }
+  }
+}
+
+template <bool kForward, int kN>
+cudaError_t launch(const void* v, int64_t ld_v, ProjectArgs p, int csize, int sms, cudaStream_t stream) {
+  using T = Tile<kN>;
+  EncodeTiledFn encode = nullptr;
+  cudaError_t err = encode_tiled_fn(&encode);
+  if (err != cudaSuccess) return err;
+  CUtensorMap map;
+  const int64_t depth = kForward ? p.w.n : p.w.m;
+  const cuuint64_t dims[2] = {(cuuint64_t)depth, (cuuint64_t)p.tokens};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld_v * 2};
+  const cuuint32_t box[2] = {(cuuint32_t)kBK, (cuuint32_t)kN};
+  const cuuint32_t estr[2] = {1, 1};
+  if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(v), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
+  auto kernel = project_kernel<kForward, kN>;
+  err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)T::kSmemBytes);
+  if (err != cudaSuccess) return err;
+  p.csize = csize;
+  p.tiles_t = (int32_t)((p.tokens + kN - 1) / kN);
+  const int64_t tiles = (int64_t)p.tiles_t * p.tiles_o;
+  if (tiles * csize > INT32_MAX) return cudaErrorInvalidValue;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(csize > 1 ? tiles * csize : std::min<int64_t>(tiles, sms)), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = T::kSmemBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)csize;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.chained ? 2 : 1;
+  err = cudaLaunchKernelEx(&cfg, kernel, map, p);
+  return err != cudaSuccess ? err : cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_project(bool forward, const void* v, int64_t tokens, int64_t ld_v, const Nvfp4Weight& w, const Adapters& ad,
                            const float* z, void* out, int64_t ld_out, cudaStream_t stream) {
-  const dim3 grid((unsigned)(((forward ? w.m : w.n) + 63) / 64), (unsigned)((tokens + 63) / 64));
-  if (forward)
-    project_kernel<true><<<grid, 256, 0, stream>>>((const uint16_t*)v, tokens, ld_v, w, ad, z, (__nv_bfloat16*)out, ld_out);
-  else
-    project_kernel<false><<<grid, 256, 0, stream>>>((const uint16_t*)v, tokens, ld_v, w, ad, z, (__nv_bfloat16*)out, ld_out);
-  return cudaGetLastError();
+  DeviceInfo info;
+  const cudaError_t err = current_device_info(&info);
+  if (err != cudaSuccess) return err;
+  const int sms = info.sm_count;
+  ProjectArgs p = {};
+  p.w = w, p.ad = ad, p.z = z, p.out = static_cast<__nv_bfloat16*>(out), p.tokens = tokens, p.ld_out = ld_out;
+  p.kb_total = (int32_t)(((forward ? w.n : w.m) + kBK - 1) / kBK);
+  p.tiles_o = (int32_t)(((forward ? w.m : w.n) + kBM - 1) / kBM);
+  p.chained = ad.count > 0;
+  // Tokens a tile and CTAs a tile by an estimate of the time: K blocks in a row on the busiest SM, each the
+  // larger of its unpacking (about 300 cycles) and its MMAs (2 cycles a token), and for a cluster its hand-over
+  // (about 10 blocks).
+  int best_n = 32, best_c = 1;
+  double best = 1e300;
+  for (int kn = 32; kn <= 256; kn *= 2) {
+    if (kn > 32 && kn / 2 >= tokens) break;
+    const double tiles = (double)((tokens + kn - 1) / kn) * p.tiles_o;
+    for (int c = 1; c <= 8 && kn / c >= 8 && c <= p.kb_total; c *= 2) {
+      const double waves = c == 1 ? std::max(1.0, (double)(int64_t)((tiles + sms - 1) / sms))
+                                  : (double)(int64_t)((tiles * c + sms - 1) / sms);
+      const double blocks = waves * ((p.kb_total + c - 1) / c) + (c > 1 ? 10 * waves : 0);
+      const double cost = blocks * std::max(300, 2 * kn);
+      if (cost < best) best = cost, best_n = kn, best_c = c;
+    }
+  }
+  if (forward) {
+    switch (best_n) {
+      case 32: return launch<true, 32>(v, ld_v, p, best_c, sms, stream);
+      case 64: return launch<true, 64>(v, ld_v, p, best_c, sms, stream);
+      case 128: return launch<true, 128>(v, ld_v, p, best_c, sms, stream);
+      default: return launch<true, 256>(v, ld_v, p, best_c, sms, stream);
+    }
+  }
+  switch (best_n) {
+    case 32: return launch<false, 32>(v, ld_v, p, best_c, sms, stream);
+    case 64: return launch<false, 64>(v, ld_v, p, best_c, sms, stream);
+    case 128: return launch<false, 128>(v, ld_v, p, best_c, sms, stream);
+    default: return launch<false, 256>(v, ld_v, p, best_c, sms, stream);
+  }
+}
+
+cudaError_t read_project_device_error(uint32_t* flags) {
+  uint32_t v = 0;
+  cudaError_t err = cudaMemcpyFromSymbol(&v, g_project_flags, sizeof v);
+  if (err != cudaSuccess) return err;
+  *flags = v;
+  if (v) {
+    const uint32_t zero = 0;
+    err = cudaMemcpyToSymbol(g_project_flags, &zero, sizeof zero);
+  }
+  return err;
 }
 
 }  // namespace hscale
