@@ -118,12 +118,7 @@ checkpoint_load_kernel(const uint8_t* __restrict__ codes, int64_t ld_codes, cons
     const float scale = ckpt_scale(scales[row * ld_scales + blk]);
     uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float lo = ckpt_element<kFormat>((q[j >> 1] >> (16 * (j & 1))) & 0xFFu) * scale;
-      const float hi = ckpt_element<kFormat>((q[j >> 1] >> (16 * (j & 1) + 8)) & 0xFFu) * scale;
-      w[j] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(lo)) |
-             (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(hi)) << 16;
-    }
+    for (int j = 0; j < 4; ++j) w[j] = ckpt_values<kFormat>(q[j >> 1] >> (16 * (j & 1)), scale);
     uint16_t* dst = x + row * ld_x + col;
     if (kVec && have == 8) {
       *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);

@@ -53,12 +53,28 @@ __device__ __forceinline__ float ckpt_scale(uint32_t byte) {
   return __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23);
 }
 
-// An element as the value it stands for, in units of its block's scale.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// The two elements in the low 16 bits of `two` as the values they stand for: bf16x2, exact.
 template <int kFormat>
-__device__ __forceinline__ float ckpt_element(uint32_t code) {
-  if (kFormat == kCkptInt8) return (float)(int)(int8_t)(uint8_t)code;
-  const float v = e4m3_mag(code & 0x7Fu);
-  return (code & 0x80u) ? -v : v;
+__device__ __forceinline__ uint32_t ckpt_values(uint32_t two, float scale) {
+  float lo, hi;
+  if constexpr (kFormat == kCkptInt8) {
+    // a byte b ^ 0x80 in the low mantissa bits of 2^23 reads as 2^23 + 128 + b
+    const uint32_t u = two ^ 0x8080u;
+    lo = __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540)) - 8388736.0f;
+    hi = __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7541)) - 8388736.0f;
+  } else {
+    asm("{\n\t.reg .b32 p;\n\t.reg .f16 l, h;\n\tcvt.rn.f16x2.e4m3x2 p, %2;\n\tmov.b32 {l, h}, p;\n\t"
+        "cvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}"
+        : "=f"(lo), "=f"(hi)
+        : "h"((uint16_t)two));
+  }
+  return pack_bf16(lo * scale, hi * scale);
 }
 
 }  // namespace hscale
