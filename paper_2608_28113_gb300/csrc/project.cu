@@ -50,7 +50,7 @@ struct Tile {
   static constexpr int kStages = kN == 256 ? 4 : kN == 128 ? 5 : 6;
   static constexpr uint32_t kBBytes = kN * kBK * 2;
   static constexpr uint32_t kStageBytes = kTileABytes + kBBytes;
-  static constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 /* alignment */ + 256 /* barriers */;
+  static constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 /* alignment */ + 256 /* barriers */ + 4096 /* z */;
   static constexpr uint32_t kTmemCols = 2 * kN;
 };
 
@@ -136,45 +136,86 @@ __device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[
 }
 
 // ---------------------------------------------------------------- epilogue
+// The 8 factors r0 .. r0 + 7 that adapter a has for output o, as 4 x bf16x2: B_a[o, r] (contiguous) or A_a[r, o].
+template <bool kForward>
+__device__ __forceinline__ uint4 factors8(const ProjectArgs& p, int a, int64_t o, int r0, bool on) {
+  uint4 q = make_uint4(0u, 0u, 0u, 0u);
+  if (!on) return q;
+  if (kForward) return ld_nc_v4(p.ad.b + ((int64_t)a * p.w.m + o) * p.ad.rank + r0);
+  uint32_t e[8];
+  const uint16_t* src = reinterpret_cast<const uint16_t*>(p.ad.a) + ((int64_t)a * p.ad.rank + r0) * p.w.n + o;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e[i] = __ldg(src + i * p.w.n);
+  q.x = e[0] | e[1] << 16, q.y = e[2] | e[3] << 16, q.z = e[4] | e[5] << 16, q.w = e[6] | e[7] << 16;
+  return q;
+}
+__device__ __forceinline__ float dot8(const float* z, const float (&f)[8], float s) {
+  const float4 z0 = reinterpret_cast<const float4*>(z)[0], z1 = reinterpret_cast<const float4*>(z)[1];
+  s = fmaf(z0.x, f[0], s), s = fmaf(z0.y, f[1], s), s = fmaf(z0.z, f[2], s), s = fmaf(z0.w, f[3], s);
+  s = fmaf(z1.x, f[4], s), s = fmaf(z1.y, f[5], s), s = fmaf(z1.z, f[6], s), s = fmaf(z1.w, f[7], s);
+  return s;
+}
+__device__ __forceinline__ void unpack_factors(const uint4& q, float (&f)[8]) {
+  f[0] = bf16_lo(q.x), f[1] = bf16_hi(q.x), f[2] = bf16_lo(q.y), f[3] = bf16_hi(q.y);
+  f[4] = bf16_lo(q.z), f[5] = bf16_hi(q.z), f[6] = bf16_lo(q.w), f[7] = bf16_hi(q.w);
+}
+
 // Results of tokens t0 .. t0 + W - 1 and this lane's output o: v (without the adapters' terms) plus each
-// token's adapter, rounded and stored.  The tokens' adapters are uniform over the warp; the lane keeps its 8
-// factors of an adapter while the tokens stay on it.
+// token's adapter, rounded and stored.  zs: 32 x 8 floats of the warp's own.  Eight ranks a pass: each lane
+// fetches its token's z into zs, from where every lane reads all of them; z and factors of the next pass are
+// fetched before the present one's products.  Tokens on one adapter share a lane's 8 factors; otherwise
+// the factors of 8 tokens are fetched at once.  A token without an adapter keeps v as it is (no product by
+// zero: the factors may be Inf or NaN).
 template <bool kForward, int W>
-__device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p) {
-  const int64_t outs = kForward ? p.w.m : p.w.n;
-  const bool on = o < outs;
+__device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p, float* zs) {
+  const bool on = o < (kForward ? p.w.m : p.w.n);
   int id = -1;
   if (lane < W && t0 + lane < p.tokens) id = adapter_of(p.ad, t0 + lane);
-  if (__any_sync(0xFFFFFFFFu, id >= 0)) {
+  const uint32_t with = __ballot_sync(0xFFFFFFFFu, id >= 0);
+  if (with) {
     const int rank = p.ad.rank;
+    const int a0 = __shfl_sync(0xFFFFFFFFu, id, __ffs(with) - 1);
+    const bool one = __all_sync(0xFFFFFFFFu, id < 0 || id == a0);
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4* zp = reinterpret_cast<const float4*>(p.z + (t0 + lane) * rank);
+    float4 z0 = id >= 0 ? zp[0] : zero, z1 = id >= 0 ? zp[1] : zero;
+    uint4 q = one ? factors8<kForward>(p, a0, o, 0, on) : make_uint4(0u, 0u, 0u, 0u);
     for (int r0 = 0; r0 < rank; r0 += 8) {
-      int cur = -1;
+      __syncwarp();
+      if (lane < W) {
+        reinterpret_cast<float4*>(zs)[2 * lane] = z0;
+        reinterpret_cast<float4*>(zs)[2 * lane + 1] = z1;
+      }
+      __syncwarp();
       float f[8];
+      unpack_factors(q, f);
+      if (r0 + 8 < rank) {
+        zp += 2;
+        if (id >= 0) z0 = zp[0], z1 = zp[1];
+        if (one) q = factors8<kForward>(p, a0, o, r0 + 8, on);
+      }
+      if (one) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = 0.0f;
+        for (int j = 0; j < W; ++j) {
+          const float s = dot8(zs + 8 * j, f, v[j]);
+          v[j] = ((with >> j) & 1u) ? s : v[j];
+        }
+      } else {
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const int a = __shfl_sync(0xFFFFFFFFu, id, j);
-        if (a < 0) continue;
-        if (a != cur) {
-          cur = a;
-          if (on) {
-            if (kForward) {
-              const uint4 q = *reinterpret_cast<const uint4*>(p.ad.b + ((int64_t)a * p.w.m + o) * rank + r0);
-              f[0] = bf16_lo(q.x), f[1] = bf16_hi(q.x), f[2] = bf16_lo(q.y), f[3] = bf16_hi(q.y);
-              f[4] = bf16_lo(q.z), f[5] = bf16_hi(q.z), f[6] = bf16_lo(q.w), f[7] = bf16_hi(q.w);
-            } else {
+        for (int j0 = 0; j0 < W; j0 += 8) {
+          uint4 e[8];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) f[i] = __bfloat162float(p.ad.a[((int64_t)a * rank + r0 + i) * p.w.n + o]);
-            }
+          for (int j = 0; j < 8; ++j) {
+            const int a = __shfl_sync(0xFFFFFFFFu, id, j0 + j);
+            e[j] = factors8<kForward>(p, a, o, r0, on && a >= 0);
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            unpack_factors(e[j], f);
+            const float s = dot8(zs + 8 * (j0 + j), f, v[j0 + j]);
+            v[j0 + j] = ((with >> (j0 + j)) & 1u) ? s : v[j0 + j];
           }
         }
-        const float4* zp = reinterpret_cast<const float4*>(p.z + (t0 + j) * rank + r0);
-        const float4 z0 = zp[0], z1 = zp[1];
-        float s = v[j];
-        s = fmaf(z0.x, f[0], s), s = fmaf(z0.y, f[1], s), s = fmaf(z0.z, f[2], s), s = fmaf(z0.w, f[3], s);
-        s = fmaf(z1.x, f[4], s), s = fmaf(z1.y, f[5], s), s = fmaf(z1.z, f[6], s), s = fmaf(z1.w, f[7], s);
-        v[j] = s;
       }
     }
   }
@@ -211,6 +252,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
   uint64_t* mma_done = acc_empty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
   uint32_t* failed = tmem_slot + 1;
+  float* zs = reinterpret_cast<float*>(smem + kStages * T::kStageBytes + 256) + (threadIdx.x >> 5 & 3) * 256;
 
   const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int csize = p.csize;
@@ -344,7 +386,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           float v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(q[j]) * scale;
-          finish<kForward, 32>(v, t0, o, lane, p);
+          finish<kForward, 32>(v, t0, o, lane, p, zs);
         }
       }
     } else {
@@ -483,7 +525,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
             sum += d == crank ? mine : inbox[(d * own + c + j) * kBM + out_row];
           v[j] = sum * scale;
         }
-        finish<kForward, 8>(v, t0, o, lane, p);
+        finish<kForward, 8>(v, t0, o, lane, p, zs);
       }
     }
   }
