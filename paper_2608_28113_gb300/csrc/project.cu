@@ -12,8 +12,9 @@
 //   0      TMA loads of the tokens' tile, K-major, 128-byte swizzle
 //   1      MMAs
 //   2-5    epilogue: tensor memory -> s_g, adapter, bf16 -> out (lane = output, columns = tokens)
-//   6-13   the weight's tile: 16 packed bytes and 2 codes a thread and K block, kept kAhead blocks ahead in
-//          registers, unpacked into the swizzled tile.  Forward (K = n) the tile is K-major, backward
+//   6-13   the weight's tile: two groups of four warps take the K blocks in turn, 32 packed bytes and 4 codes
+//          a thread, kept kAhead of the group's blocks ahead in registers and unpacked into the swizzled tile (the
+//          groups' waits and fences overlap; one group of eight warps was slower).  Forward (K = n) the tile is K-major, backward
 //          (K = m, outputs = n) the same packed rows make it MN-major, so W is read as it is stored.
 // Each weight is unpacked once per kN tokens: about 2.7 instructions a weight against kN / 64 tensor-core
 // cycles, so at kN = 256 the unpacking hides behind the MMAs.
@@ -40,8 +41,8 @@ namespace {
 
 constexpr int kBM = 128, kBK = 64;
 constexpr int kThreads = 448;
-constexpr int kUnpackThreads = 256, kUnpackWarp0 = 6;
-constexpr int kAhead = 8;
+constexpr int kUnpackWarp0 = 6, kUnpackGroups = 2, kGroupThreads = 128;
+constexpr int kAhead = 4;  // blocks of its own that a group has in flight
 constexpr uint32_t kTileABytes = kBM * kBK * 2;  // 16 KB
 constexpr uint32_t kGroupBytes = 64 * kBK * 2;   // MN-major: 64 outputs x 64 rows of K
 
@@ -93,22 +94,23 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t (&r
   r[3] = mul_bf16x2((b & kSign) | ((b >> 6) & kMag), scale);
 }
 
-__device__ __forceinline__ uint2 ld_v2_ahead(const void* p) {
+// Loads that stay where they are written, so that several are in flight.
+__device__ __forceinline__ void ld_32_ahead(const void* p, uint32_t (&r)[8]) {
+  asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "l"(p));
+}
+__device__ __forceinline__ uint2 ld_8_ahead(const void* p) {
   uint2 r;
   asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
   return r;
 }
-__device__ __forceinline__ uint4 ld_v4_ahead(const void* p) {
-  uint4 r;
-  asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+__device__ __forceinline__ uint32_t ld_4_ahead(const void* p) {
+  uint32_t r;
+  asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(r) : "l"(p));
   return r;
 }
-__device__ __forceinline__ uint32_t ld_u16_ahead(const void* p) {
-  uint16_t r;
-  asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(r) : "l"(p));
-  return r;
-}
-__device__ __forceinline__ uint32_t ld_u8_ahead(const void* p) {
+__device__ __forceinline__ uint32_t ld_1_ahead(const void* p) {
   uint32_t r;
   asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(r) : "l"(p));
   return r;
@@ -267,7 +269,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&full[s], 1 + kUnpackThreads / 32);  // the TMA load and each unpacking warp
+      mbar_init(&full[s], 1 + kGroupThreads / 32);  // the TMA load and the unpacking group's warps
       mbar_init(&empty[s], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -395,84 +397,87 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
       tc_fence_after_sync();
     }
   } else {
-    // ---- the weight's tile.  Thread: row of the tile (forward: output; backward: K), a half of its 64 columns
+    // ---- the weight's tile.  Thread: one row of 64 nibbles, K-major an output's, MN-major 64 outputs of a K
     const int tid = (int)threadIdx.x - kUnpackWarp0 * 32;
-    const int group = kForward ? 0 : tid >> 7;  // backward: 64 outputs each
-    const int row = kForward ? tid >> 1 : (tid & 127) >> 1, half = tid & 1;
+    const int who = tid / kGroupThreads;              // takes blocks who, who + kUnpackGroups, ... of the CTA's
+    const int line = tid % kGroupThreads;             // 128-byte line of the tile
+    const int row = kForward ? line : line & 63;
     const int64_t m = p.w.m, n = p.w.n;
-    const bool wide = (n & 31) == 0 && ((reinterpret_cast<uintptr_t>(p.w.packed) & 15) | (reinterpret_cast<uintptr_t>(p.w.codes) & 1)) == 0;
-    uint8_t* const dst0 = tile_a + group * kGroupBytes + row * 128;
+    const bool wide = (n & 63) == 0 && (reinterpret_cast<uintptr_t>(p.w.packed) & 31) == 0 &&
+                      (reinterpret_cast<uintptr_t>(p.w.codes) & 3) == 0;
     // position of the next block to load
-    int li = 0, lk = kb0;
+    int li = -1, lk = kb1;
     int64_t f = 0, k0 = 0;
     const int total = ntiles * kbs;
-    auto start_tile = [&]() {
-      int tt, to;
-      raster(first + li * step, p, tt, to);
-      f = kForward ? (int64_t)to * kBM + row : (int64_t)lk * kBK + row;
-      k0 = kForward ? (int64_t)lk * kBK + half * 32 : (int64_t)to * kBM + group * 64 + half * 32;
+    auto advance = [&](int blocks) {
+      lk += blocks;
+      if (kForward) k0 += blocks * kBK; else f += blocks * kBK;
+      while (lk >= kb1 && li < ntiles) {
+        lk -= kbs;
+        int tt, to;
+        if (++li < ntiles) {
+          raster(first + li * step, p, tt, to);
+          f = kForward ? (int64_t)to * kBM + row : (int64_t)lk * kBK + row;
+          k0 = kForward ? (int64_t)lk * kBK : (int64_t)to * kBM + (line >> 6) * 64;
+        }
+      }
     };
-    uint4 ring[kAhead];
-    uint32_t codes[kAhead];
-    auto load = [&](uint4& q, uint32_t& c) {
-      q = make_uint4(0u, 0u, 0u, 0u);
+    uint32_t ring[kAhead][8], codes[kAhead];
+    auto load = [&](uint32_t (&q)[8], uint32_t& c) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[i] = 0u;
       c = 0u;
       if (f < m && k0 < n) {
         const uint8_t* wp = p.w.packed + f * (n >> 1) + (k0 >> 1);
         const uint8_t* cp = p.w.codes + f * (n >> 4) + (k0 >> 4);
         if (wide) {
-          q = ld_v4_ahead(wp);
-          c = ld_u16_ahead(cp);
+          ld_32_ahead(wp, q);
+          c = ld_4_ahead(cp);
         } else {
-          const uint2 lo = ld_v2_ahead(wp);
-          q.x = lo.x, q.y = lo.y;
-          c = ld_u8_ahead(cp);
-          if (k0 + 16 < n) {
-            const uint2 hi = ld_v2_ahead(wp + 8);
-            q.z = hi.x, q.w = hi.y;
-            c |= ld_u8_ahead(cp + 1) << 8;
-          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (k0 + 16 * i < n) {
+              const uint2 v = ld_8_ahead(wp + 8 * i);
+              q[2 * i] = v.x, q[2 * i + 1] = v.y;
+              c |= ld_1_ahead(cp + i) << (8 * i);
+            }
         }
       }
-      if (kForward) k0 += kBK; else f += kBK;
-      if (++lk == kb1) {
-        lk = kb0;
-        if (++li < ntiles) start_tile();
-      }
+      advance(kUnpackGroups);
     };
-    start_tile();
+    advance(who);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (u < total) load(ring[u], codes[u]);
-    uint32_t s = 0, parity = 1;
+      if (who + u * kUnpackGroups < total) load(ring[u], codes[u]);
+    uint32_t s = (uint32_t)who % kStages, parity = 1;
     bool go = true;
-    for (int base = 0; base < total && go; base += kAhead) {
+    for (int base = who; base < total && go; base += kAhead * kUnpackGroups) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        if (base + u >= total || !go) break;
+        if (base + u * kUnpackGroups >= total || !go) break;
         if (!mbar_wait_warp(&empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
           go = false;
           break;
         }
-        uint8_t* dst = dst0 + s * kTileABytes;
-        const uint32_t sc = unpack_codes(codes[u]);
-        const uint32_t s0 = __byte_perm(sc, sc, 0x1010), s1 = __byte_perm(sc, sc, 0x3232);
-        const uint32_t w[4] = {ring[u].x, ring[u].y, ring[u].z, ring[u].w};
+        uint8_t* dst = tile_a + s * kTileABytes + line * 128;
+        const uint32_t ca = unpack_codes(codes[u] & 0xFFFFu), cb = unpack_codes(codes[u] >> 16);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t c = i < 4 ? ca : cb;
           uint32_t r[4];
-          unpack8(w[i], i < 2 ? s0 : s1, r);
-          *reinterpret_cast<uint4*>(dst + (((half * 4 + i) ^ (row & 7)) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
+          unpack8(ring[u][i], __byte_perm(c, c, (i & 2) ? 0x3232 : 0x1010), r);
+          *reinterpret_cast<uint4*>(dst + ((i ^ (row & 7)) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&full[s]);
-        if (++s == kStages) {
-          s = 0;
+        s += kUnpackGroups;
+        if (s >= kStages) {
+          s -= kStages;
           parity ^= 1u;
         }
-        if (base + u + kAhead < total) load(ring[u], codes[u]);
+        if (base + (u + kAhead) * kUnpackGroups < total) load(ring[u], codes[u]);
       }
     }
   }
