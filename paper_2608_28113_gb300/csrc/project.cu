@@ -24,9 +24,13 @@
 // order.  With csize 1 the grid is persistent and the epilogue of a tile runs beside the MMAs of the next (two
 // accumulators in tensor memory).
 //
-// The adapter's term is a dot product of `rank` fp32 numbers per result on the epilogue's FMA pipes rather than
-// more K columns of the MMAs: there a token that does not use an adapter would meet it as 0 times its values,
-// and an Inf or NaN in one request's adapter would spoil the others' tokens.
+// The adapters' terms.  Tokens are looked at in blocks of 16.  A block whose tokens share one adapter takes its
+// term on the tensor cores: after the weight's K blocks the unpacking warps write the adapter's factors and
+// the tokens' z (as a pair hi + lo of bf16 numbers, so 2^-17 of it is lost) as one more K block for up to 32 ranks,
+// and the MMAs of that block run over the columns of just those token blocks.  The tokens of the other,
+// mixed blocks get theirs in the epilogue, a dot product of `rank` fp32 numbers per result.  Masking a mixed
+// block's z instead would multiply other requests' factors by zero, and an Inf or NaN in one request's adapter
+// would spoil the others' tokens.
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>
@@ -168,11 +172,13 @@ __device__ __forceinline__ void unpack_factors(const uint4& q, float (&f)[8]) {
 // fetched before the present one's products.  Tokens on one adapter share a lane's 8 factors; otherwise
 // the factors of 8 tokens are fetched at once.  A token without an adapter keeps v as it is (no product by
 // zero: the factors may be Inf or NaN).
+// mixed: bit b for the 16 tokens from t0 + 16 b whose terms are added here.
 template <bool kForward, int W>
-__device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p, float* zs) {
+__device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p, uint32_t mixed,
+                                       float* zs) {
   const bool on = o < (kForward ? p.w.m : p.w.n);
   int id = -1;
-  if (lane < W && t0 + lane < p.tokens) id = adapter_of(p.ad, t0 + lane);
+  if (lane < W && t0 + lane < p.tokens && ((mixed >> (lane >> 4)) & 1u)) id = adapter_of(p.ad, t0 + lane);
   const uint32_t with = __ballot_sync(0xFFFFFFFFu, id >= 0);
   if (with) {
     const int rank = p.ad.rank;
@@ -228,6 +234,116 @@ __device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int
     if (t0 + j < p.tokens) dst[j * p.ld_out] = __float2bfloat16_rn(v[j]);
 }
 
+// The adapters of a tile's token blocks (16 tokens each; lane b holds block b's): `same` marks the blocks whose
+// tokens all have adapter `id`, `mixed` those that have adapters otherwise.  Tokens past the end fit any block.
+// All lanes of a warp take part; every role of a CTA finds the same.
+struct TokenBlocks {
+  uint32_t same, mixed;
+  int id;
+};
+template <int kN>
+__device__ __forceinline__ TokenBlocks token_blocks(const ProjectArgs& p, int64_t t0, int lane) {
+  TokenBlocks r = {0u, 0u, -1};
+  if (p.ad.count == 0) return r;
+  if (p.ad.of_token == nullptr) {
+    r.id = 0;
+    const int64_t have = (p.tokens - t0 + 15) >> 4;
+    r.same = have >= kN / 16 ? (1u << (kN / 16)) - 1u : (1u << have) - 1u;
+    return r;
+  }
+  int id[kN / 32];
+#pragma unroll
+  for (int i = 0; i < kN / 32; ++i) {
+    const int64_t t = t0 + 32 * i + lane;
+    id[i] = t < p.tokens ? adapter_of(p.ad, t) : -2;
+  }
+#pragma unroll
+  for (int i = 0; i < kN / 32; ++i) {
+    const int lead = __shfl_sync(0xFFFFFFFFu, id[i], lane & 16);
+    const uint32_t like = __ballot_sync(0xFFFFFFFFu, id[i] == lead || id[i] == -2);
+    const uint32_t some = __ballot_sync(0xFFFFFFFFu, id[i] >= 0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int a = __shfl_sync(0xFFFFFFFFu, lead, 16 * h);
+      const bool same = ((like >> (16 * h)) & 0xFFFFu) == 0xFFFFu && a >= 0;
+      const bool any = ((some >> (16 * h)) & 0xFFFFu) != 0u;
+      const int b = 2 * i + h;
+      r.same |= same ? 1u << b : 0u;
+      r.mixed |= any && !same ? 1u << b : 0u;
+      if (lane == b) r.id = a;
+    }
+  }
+  return r;
+}
+// Takes the next adapter off the blocks in `left`: its blocks, in `a` the adapter.
+__device__ __forceinline__ uint32_t next_adapter(const TokenBlocks& tb, uint32_t& left, int lane, int& a) {
+  a = __shfl_sync(0xFFFFFFFFu, tb.id, __ffs(left) - 1);
+  const uint32_t sel = __ballot_sync(0xFFFFFFFFu, ((left >> lane) & 1u) && tb.id == a);
+  left &= ~sel;
+  return sel;
+}
+// K blocks that the adapters of a tile add: one per adapter and 32 ranks
+constexpr int kRanks = 32;
+__device__ __forceinline__ int adapter_blocks(const ProjectArgs& p, const TokenBlocks& tb, int lane) {
+  uint32_t left = tb.same;
+  int count = 0, a;
+  while (left) {
+    next_adapter(tb, left, lane, a);
+    ++count;
+  }
+  return count * ((p.ad.rank + kRanks - 1) / kRanks);
+}
+// Ranks that each half of such a block's K holds: [factors | factors] times [hi | lo]
+__device__ __forceinline__ int half_ranks(int rank, int r0) { return rank - r0 <= 16 ? 16 : kRanks; }
+
+// Such a block for ranks r0 ..: the 128 threads of a group write the factors of adapter a (as the weight's tile)
+// and the z of the tile's tokens (as the tokens' tile).  z of tokens that do not use the adapter is whatever
+// it is: the MMAs leave their columns alone.
+// The accumulator is in units of 128 s_g: z is divided by it.
+template <bool kForward, int kN>
+__device__ __forceinline__ void adapter_block(const ProjectArgs& p, uint8_t* ta, uint8_t* tb, int64_t t0, int64_t o0, int a, int r0,
+                                           int tid) {
+  const int rank = p.ad.rank, half = half_ranks(rank, r0), hc = half / 8;
+  if (kForward) {
+    const int64_t o = o0 + tid;
+    const __nv_bfloat16* src = p.ad.b + ((int64_t)a * p.w.m + o) * rank + r0;
+    for (int c = 0; c < hc; ++c) {
+      const uint4 q = o < p.w.m && r0 + 8 * c < rank ? ld_nc_v4(src + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
+      *reinterpret_cast<uint4*>(ta + tid * 128 + ((c ^ (tid & 7)) << 4)) = q;
+      *reinterpret_cast<uint4*>(ta + tid * 128 + (((c + hc) ^ (tid & 7)) << 4)) = q;
+    }
+  } else {
+    for (int i = tid; i < half * 16; i += kGroupThreads) {
+      const int r = i >> 4, group = (i >> 3) & 1, c = i & 7;
+      const int64_t o = o0 + group * 64 + c * 8;
+      const uint4 q = o < p.w.n && r0 + r < rank ? ld_nc_v4(p.ad.a + ((int64_t)a * rank + r0 + r) * p.w.n + o)
+                                                 : make_uint4(0u, 0u, 0u, 0u);
+      uint8_t* dst = ta + group * kGroupBytes + r * 128 + ((c ^ (r & 7)) << 4);
+      *reinterpret_cast<uint4*>(dst) = q;
+      *reinterpret_cast<uint4*>(dst + half * 128) = q;
+    }
+  }
+  const float unit = 1.0f / (128.0f * *p.w.global_scale);
+  for (int t = tid; t < kN; t += kGroupThreads) {
+    const float* src = p.z + (t0 + t) * rank + r0;
+    for (int c = 0; c < hc; ++c) {
+      uint32_t hi[4] = {0u, 0u, 0u, 0u}, lo[4] = {0u, 0u, 0u, 0u};
+      if (t0 + t < p.tokens && r0 + 8 * c < rank) {
+        const float4 v0 = reinterpret_cast<const float4*>(src)[2 * c], v1 = reinterpret_cast<const float4*>(src)[2 * c + 1];
+        const float v[8] = {v0.x * unit, v0.y * unit, v0.z * unit, v0.w * unit,
+                            v1.x * unit, v1.y * unit, v1.z * unit, v1.w * unit};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          hi[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+          lo[j] = pack_bf16(v[2 * j] - bf16_lo(hi[j]), v[2 * j + 1] - bf16_hi(hi[j]));
+        }
+      }
+      *reinterpret_cast<uint4*>(tb + t * 128 + ((c ^ (t & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(tb + t * 128 + (((c + hc) ^ (t & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+  }
+}
+
 // Tile t of the persistent order: groups of 8 token tiles, the outputs' tiles along a group, so that the
 // tiles in flight at once share token tiles and weights in L2.
 __device__ __forceinline__ void raster(int t, const ProjectArgs& p, int& tt, int& to) {
@@ -236,6 +352,45 @@ __device__ __forceinline__ void raster(int t, const ProjectArgs& p, int& tt, int
   const int within = t - group * p.tiles_o;
   tt = group + within % rows;
   to = within / rows;
+}
+
+// An unpacking group's progress over the adapters' blocks: the tile they are due for next, how many there have
+// been (both groups count all of them, and take them in turn).
+struct AdapterTurn {
+  int tile, extras;
+  bool waited;  // for z
+};
+// The group's part of the adapters' blocks of tiles turn.tile .. until - 1; false once a wait ran out.
+template <bool kForward, int kN>
+__device__ __noinline__ bool adapter_turn(const ProjectArgs& p, uint8_t* smem, uint64_t* full, uint64_t* empty, AdapterTurn& turn,
+                                          int until, int first, int step, int kbs, int who, int line) {
+  using T = Tile<kN>;
+  const int lane = threadIdx.x & 31;
+  for (; turn.tile < until; ++turn.tile) {
+    int tt, to;
+    raster(first + turn.tile * step, p, tt, to);
+    const TokenBlocks tb = token_blocks<kN>(p, (int64_t)tt * kN, lane);
+    uint32_t left = tb.same;
+    if (left && !turn.waited) {
+      pdl_wait_primary();
+      turn.waited = true;
+    }
+    while (left) {
+      int a;
+      next_adapter(tb, left, lane, a);
+      for (int r0 = 0; r0 < p.ad.rank; r0 += kRanks, ++turn.extras) {
+        if (turn.extras % kUnpackGroups != who) continue;
+        const int pos = (turn.tile + 1) * kbs + turn.extras, s = pos % T::kStages;
+        if (!mbar_wait_warp(&empty[s], ((uint32_t)(pos / T::kStages) & 1u) ^ 1u)) return false;
+        adapter_block<kForward, kN>(p, smem + s * kTileABytes, smem + T::kStages * kTileABytes + s * T::kBBytes,
+                                    (int64_t)tt * kN, (int64_t)to * kBM, a, r0, line);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[s]);
+      }
+    }
+  }
+  return true;
 }
 
 template <bool kForward, int kN>
@@ -266,6 +421,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
   const int ntiles = csize > 1 ? 1 : (tiles - first + step - 1) / step;
   const int kb0 = (int)((int64_t)p.kb_total * crank / csize), kb1 = (int)((int64_t)p.kb_total * (crank + 1) / csize);
   const int kbs = kb1 - kb0;
+  const bool adds = p.ad.count > 0 && crank == csize - 1;  // the adapters' blocks are the last rank's
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -320,11 +476,28 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           parity ^= 1u;
         }
       }
+      // the adapters' blocks are the unpacking warps' alone
+      const int extra = adds && go ? adapter_blocks(p, token_blocks<kN>(p, (int64_t)tt * kN, lane), lane) : 0;
+      for (int e = 0; e < extra; ++e) {
+        if (!mbar_wait_warp(&empty[s], parity)) {
+          if (lane == 0) atomicOr(failed, 1u);
+          go = false;
+          break;
+        }
+        if (elect_one()) mbar_arrive(&full[s]);
+        __syncwarp();
+        if (++s == kStages) {
+          s = 0;
+          parity ^= 1u;
+        }
+      }
     }
     // a full barrier also waits for the unpacking warps, whose waits are bounded like this one's
     ring_drain(full, kStages, s, parity);
   } else if (warp == 1) {
-    constexpr uint32_t kIdesc = idesc_bf16_f32(kBM, kN) | (kForward ? 0u : 1u << 15);
+    constexpr uint32_t kMajor = kForward ? 0u : 1u << 15;
+    constexpr uint32_t kIdesc = idesc_bf16_f32(kBM, kN) | kMajor;
+    constexpr uint32_t kStepA = kForward ? 2 : 128;  // 16 of K further in the descriptor
     uint32_t s = 0, parity = 0;
     bool ok = true;
     for (int i = 0; i < ntiles && ok; ++i) {
@@ -334,6 +507,9 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
         break;
       }
       tc_fence_after_sync();
+      int tt, to;
+      raster(first + i * step, p, tt, to);
+      TokenBlocks tb = {0u, 0u, -1};
       for (int kb = 0; kb < kbs; ++kb) {
         if (!mbar_wait_warp(&full[s], parity)) {
           ok = false;
@@ -346,16 +522,53 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           const uint64_t bd = smem_desc_k_sw128(b);
 #pragma unroll
           for (int kk = 0; kk < kBK / 16; ++kk)
-            umma_bf16(tmem_d + acc * kN, ad + (kForward ? 2 : 128) * kk, bd + 2 * kk, kIdesc, (uint32_t)(kb > 0 || kk > 0));
+            umma_bf16(tmem_d + acc * kN, ad + kStepA * kk, bd + 2 * kk, kIdesc, (uint32_t)(kb > 0 || kk > 0));
           umma_commit(smem_addr(&empty[s]));
-          if (kb + 1 == kbs) umma_commit(smem_addr(&acc_full[acc]));
         }
         __syncwarp();
         if (++s == kStages) {
           s = 0;
           parity ^= 1u;
         }
+        // looked up while the MMAs of a few blocks are under way
+        if (adds && kb == min(3, kbs - 1)) tb = token_blocks<kN>(p, (int64_t)tt * kN, lane);
       }
+      if (ok) {
+        uint32_t left = tb.same;
+        while (left && ok) {
+          int who;
+          const uint32_t sel = next_adapter(tb, left, lane, who);
+          for (int r0 = 0; r0 < p.ad.rank && ok; r0 += kRanks) {
+            if (!mbar_wait_warp(&full[s], parity)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after_sync();
+            const uint32_t a = smem_addr(tile_a + s * kTileABytes), b = smem_addr(tile_b + s * T::kBBytes);
+            const uint64_t ad = kForward ? smem_desc_k_sw128(a) : smem_desc_mn_sw128(a, kGroupBytes);
+            const uint64_t bd = smem_desc_k_sw128(b);
+            const int steps = half_ranks(p.ad.rank, r0) / 8;
+            if (elect_one()) {
+              for (uint32_t runs = sel; runs;) {  // each run of neighbouring blocks
+                const int b0 = __ffs(runs) - 1, len = __ffs(~(runs >> b0)) - 1;
+                runs &= ~(((1u << len) - 1u) << b0);
+                const uint32_t idesc = idesc_bf16_f32(kBM, 0) | kMajor | ((uint32_t)(2 * len) << 17);
+                for (int kk = 0; kk < steps; ++kk)
+                  umma_bf16(tmem_d + acc * kN + 16 * b0, ad + kStepA * kk, bd + 128 * b0 + 2 * kk, idesc, 1u);
+              }
+              umma_commit(smem_addr(&empty[s]));
+            }
+            __syncwarp();
+            if (++s == kStages) {
+              s = 0;
+              parity ^= 1u;
+            }
+          }
+        }
+      }
+      // fires once every MMA issued above has completed
+      if (ok && elect_one()) umma_commit(smem_addr(&acc_full[acc]));
+      __syncwarp();
     }
     if (!ok && lane == 0) atomicOr(failed, 1u);
     __syncwarp();
@@ -374,6 +587,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
         }
         tc_fence_after_sync();
         const int64_t o = (int64_t)to * kBM + out_row;
+        const uint32_t mixed = token_blocks<kN>(p, (int64_t)tt * kN, lane).mixed;
 #pragma unroll 1
         for (int c = 0; c < kN; c += 32) {
           const int64_t t0 = (int64_t)tt * kN + c;
@@ -388,7 +602,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           float v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(q[j]) * scale;
-          finish<kForward, 32>(v, t0, o, lane, p, zs);
+          finish<kForward, 32>(v, t0, o, lane, p, mixed >> (c >> 4), zs);
         }
       }
     } else {
@@ -449,14 +663,24 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
       if (who + u * kUnpackGroups < total) load(ring[u], codes[u]);
+    AdapterTurn turn = {0, 0, p.chained == 0};
+    int tile_end = adds ? kbs : INT32_MAX;  // first block of the next tile, whose turn is behind the adapters'
     uint32_t s = (uint32_t)who % kStages, parity = 1;
     bool go = true;
     for (int base = who; base < total && go; base += kAhead * kUnpackGroups) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        if (base + u * kUnpackGroups >= total || !go) break;
+        const int next = base + u * kUnpackGroups;
+        if (next >= total || !go) break;
+        if (next >= tile_end) {
+          const int tile = next / kbs;
+          tile_end = (tile + 1) * kbs;
+          go = adapter_turn<kForward, kN>(p, smem, full, empty, turn, tile, first, step, kbs, who, line);
+          if (!go) break;
+          s = (uint32_t)(next + turn.extras) % kStages;
+          parity = (((uint32_t)(next + turn.extras) / kStages) & 1u) ^ 1u;
+        }
         if (!mbar_wait_warp(&empty[s], parity)) {
-          if (lane == 0) atomicOr(failed, 1u);
           go = false;
           break;
         }
@@ -480,6 +704,8 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
         if (base + (u + kAhead) * kUnpackGroups < total) load(ring[u], codes[u]);
       }
     }
+    if (go && adds) go = adapter_turn<kForward, kN>(p, smem, full, empty, turn, ntiles, first, step, kbs, who, line);
+    if (!go && lane == 0) atomicOr(failed, 1u);
   }
 
   if (csize > 1) {
@@ -515,6 +741,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
       const float scale = *p.w.global_scale * 128.0f;
       if (p.chained) pdl_wait_primary();  // z
       const int64_t o = (int64_t)to * kBM + out_row;
+      const uint32_t mixed = token_blocks<kN>(p, (int64_t)tt * kN, lane).mixed;
       for (int c = 0; c < own; c += 8) {
         const int64_t t0 = (int64_t)tt * kN + crank * own + c;
         uint32_t q[8];
@@ -530,7 +757,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
             sum += d == crank ? mine : inbox[(d * own + c + j) * kBM + out_row];
           v[j] = sum * scale;
         }
-        finish<kForward, 8>(v, t0, o, lane, p, zs);
+        finish<kForward, 8>(v, t0, o, lane, p, mixed >> ((crank * own + c) >> 4), zs);
       }
     }
   }
