@@ -24,13 +24,14 @@
 // order.  With csize 1 the grid is persistent and the epilogue of a tile runs beside the MMAs of the next (two
 // accumulators in tensor memory).
 //
-// The adapters' terms.  Tokens are looked at in blocks of 16.  A block whose tokens share one adapter takes its
-// term on the tensor cores: after the weight's K blocks the unpacking warps write the adapter's factors and
-// the tokens' z (as a pair hi + lo of bf16 numbers, so 2^-17 of it is lost) as one more K block for up to 32 ranks,
-// and the MMAs of that block run over the columns of just those token blocks.  The tokens of the other,
-// mixed blocks get theirs in the epilogue, a dot product of `rank` fp32 numbers per result.  Masking a mixed
-// block's z instead would multiply other requests' factors by zero, and an Inf or NaN in one request's adapter
-// would spoil the others' tokens.
+// The adapters' terms.  An adapter with enough tokens in a tile takes its term on the tensor cores: after the
+// weight's K blocks the epilogue's warps, idle by then, write its factors and its tokens' z (as a pair hi + lo of
+// bf16 numbers, so 2^-17 of it is lost; zeros for the other tokens) as one more K block per 32 ranks, fetched
+// before the stage is free.  An adapter with few tokens there ("loose": a decoding batch) is cheaper in the epilogue
+// itself, a dot product of `rank` fp32 numbers per result.  Zeros times factors are zeros only while the
+// factors are finite: an output whose factors hold an Inf or NaN is left out of the K block, and the tokens
+// of that adapter get NaN there; so nothing passes from one request's adapter to another's tokens.
+// Which adapters a tile has is found by one warp, two tiles ahead (TileInfo).
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>
@@ -49,13 +50,18 @@ constexpr int kUnpackWarp0 = 6, kUnpackGroups = 2, kGroupThreads = 128;
 constexpr int kAhead = 4;  // blocks of its own that a group has in flight
 constexpr uint32_t kTileABytes = kBM * kBK * 2;  // 16 KB
 constexpr uint32_t kGroupBytes = 64 * kBK * 2;   // MN-major: 64 outputs x 64 rows of K
+constexpr int kInfos = 4;                        // TileInfo of as many tiles
+constexpr uint32_t kInfoBytes = 576;
+constexpr uint32_t kBarBytes = 512;
+constexpr int kGo = 8;                           // tiles whose place in the ring's order is kept: more than it has stages
 
 template <int kN>
 struct Tile {
   static constexpr int kStages = kN == 256 ? 4 : kN == 128 ? 5 : 6;
   static constexpr uint32_t kBBytes = kN * kBK * 2;
   static constexpr uint32_t kStageBytes = kTileABytes + kBBytes;
-  static constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 /* alignment */ + 256 /* barriers */ + 4096 /* z */;
+  static constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 /* alignment */ + kBarBytes + 4096 /* z */ +
+                                         kInfos * kInfoBytes + 1024 /* bad */;
   static constexpr uint32_t kTmemCols = 2 * kN;
 };
 
@@ -172,13 +178,13 @@ __device__ __forceinline__ void unpack_factors(const uint4& q, float (&f)[8]) {
 // fetched before the present one's products.  Tokens on one adapter share a lane's 8 factors; otherwise
 // the factors of 8 tokens are fetched at once.  A token without an adapter keeps v as it is (no product by
 // zero: the factors may be Inf or NaN).
-// mixed: bit b for the 16 tokens from t0 + 16 b whose terms are added here.
+// loose: bit j where token t0 + j's term is added here.
 template <bool kForward, int W>
-__device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p, uint32_t mixed,
+__device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p, uint32_t loose,
                                        float* zs) {
   const bool on = o < (kForward ? p.w.m : p.w.n);
   int id = -1;
-  if (lane < W && t0 + lane < p.tokens && ((mixed >> (lane >> 4)) & 1u)) id = adapter_of(p.ad, t0 + lane);
+  if (lane < W && ((loose >> lane) & 1u)) id = adapter_of(p.ad, t0 + lane);
   const uint32_t with = __ballot_sync(0xFFFFFFFFu, id >= 0);
   if (with) {
     const int rank = p.ad.rank;
@@ -234,114 +240,168 @@ __device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int
     if (t0 + j < p.tokens) dst[j * p.ld_out] = __float2bfloat16_rn(v[j]);
 }
 
-// The adapters of a tile's token blocks (16 tokens each; lane b holds block b's): `same` marks the blocks whose
-// tokens all have adapter `id`, `mixed` those that have adapters otherwise.  Tokens past the end fit any block.
-// All lanes of a warp take part; every role of a CTA finds the same.
-struct TokenBlocks {
-  uint32_t same, mixed;
-  int id;
+constexpr int kRanks = 32;      // ranks a K block of an adapter holds: [factors | factors] times [hi | lo]
+constexpr int kMaxListed = 32;  // adapters of a tile that may take their term on the tensor cores
+// The adapters of a tile of kN <= 256 tokens.
+struct TileInfo {
+  int listed, blocks;            // adapters on the tensor cores, K blocks that they add
+  uint32_t loose[8];             // tokens whose term the epilogue adds
+  int adapter[kMaxListed];
+  uint32_t sel[kMaxListed];      // bit b: the adapter has tokens among 16 b .. 16 b + 15
+  uint8_t index[256];            // a token's place in the list, or 255
 };
+static_assert(sizeof(TileInfo) <= kInfoBytes, "TileInfo's place");
+__device__ __forceinline__ int rank_blocks(int rank) { return (rank + kRanks - 1) / kRanks; }
+__device__ __forceinline__ int half_ranks(int rank, int r0) { return rank - r0 <= 16 ? 16 : kRanks; }
+
+// A K block costs the epilogue's warps about 1500 cycles, a loose token 112 per 8 ranks (eight tokens' factors
+// fetched at once), so an adapter is listed from 14 rank_blocks / (rank / 8) tokens on.
 template <int kN>
-__device__ __forceinline__ TokenBlocks token_blocks(const ProjectArgs& p, int64_t t0, int lane) {
-  TokenBlocks r = {0u, 0u, -1};
-  if (p.ad.count == 0) return r;
-  if (p.ad.of_token == nullptr) {
-    r.id = 0;
-    const int64_t have = (p.tokens - t0 + 15) >> 4;
-    r.same = have >= kN / 16 ? (1u << (kN / 16)) - 1u : (1u << have) - 1u;
-    return r;
-  }
+__device__ __forceinline__ void find_adapters(const ProjectArgs& p, int64_t t0, int lane, TileInfo& info) {
   int id[kN / 32];
+  uint32_t left[kN / 32], loose[kN / 32];
 #pragma unroll
   for (int i = 0; i < kN / 32; ++i) {
     const int64_t t = t0 + 32 * i + lane;
-    id[i] = t < p.tokens ? adapter_of(p.ad, t) : -2;
+    id[i] = t < p.tokens ? adapter_of(p.ad, t) : -1;
   }
 #pragma unroll
   for (int i = 0; i < kN / 32; ++i) {
-    const int lead = __shfl_sync(0xFFFFFFFFu, id[i], lane & 16);
-    const uint32_t like = __ballot_sync(0xFFFFFFFFu, id[i] == lead || id[i] == -2);
-    const uint32_t some = __ballot_sync(0xFFFFFFFFu, id[i] >= 0);
+    left[i] = __ballot_sync(0xFFFFFFFFu, id[i] >= 0);
+    loose[i] = left[i];
+    info.index[32 * i + lane] = 255;
+  }
+  const int enough = (14 * rank_blocks(p.ad.rank) + p.ad.rank / 8 - 1) / (p.ad.rank / 8);
+  int listed = 0;
+  // the first token left over, its adapter, all its tokens
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int a = __shfl_sync(0xFFFFFFFFu, lead, 16 * h);
-      const bool same = ((like >> (16 * h)) & 0xFFFFu) == 0xFFFFu && a >= 0;
-      const bool any = ((some >> (16 * h)) & 0xFFFFu) != 0u;
-      const int b = 2 * i + h;
-      r.same |= same ? 1u << b : 0u;
-      r.mixed |= any && !same ? 1u << b : 0u;
-      if (lane == b) r.id = a;
+  for (int i = 0; i < kN / 32; ++i) {
+    while (left[i] && listed < kMaxListed) {
+      const int a = __shfl_sync(0xFFFFFFFFu, id[i], __ffs(left[i]) - 1);
+      uint32_t of[kN / 32], sel = 0u;
+      int count = 0;
+#pragma unroll
+      for (int k = i; k < kN / 32; ++k) {
+        of[k] = __ballot_sync(0xFFFFFFFFu, id[k] == a);
+        left[k] &= ~of[k];
+        count += __popc(of[k]);
+        sel |= (((of[k] & 0xFFFFu) ? 1u : 0u) | ((of[k] >> 16) ? 2u : 0u)) << (2 * k);
+      }
+      if (count < enough) continue;
+#pragma unroll
+      for (int k = i; k < kN / 32; ++k) {
+        loose[k] &= ~of[k];
+        if ((of[k] >> lane) & 1u) info.index[32 * k + lane] = (uint8_t)listed;
+      }
+      if (lane == 0) info.adapter[listed] = a, info.sel[listed] = sel;
+      ++listed;
     }
   }
-  return r;
+#pragma unroll
+  for (int i = 0; i < kN / 32; ++i)
+    if (lane == i) info.loose[i] = loose[i];
+  if (lane == 0) info.listed = listed, info.blocks = listed * rank_blocks(p.ad.rank);
+  __syncwarp();
 }
-// Takes the next adapter off the blocks in `left`: its blocks, in `a` the adapter.
-__device__ __forceinline__ uint32_t next_adapter(const TokenBlocks& tb, uint32_t& left, int lane, int& a) {
-  a = __shfl_sync(0xFFFFFFFFu, tb.id, __ffs(left) - 1);
-  const uint32_t sel = __ballot_sync(0xFFFFFFFFu, ((left >> lane) & 1u) && tb.id == a);
-  left &= ~sel;
-  return sel;
-}
-// K blocks that the adapters of a tile add: one per adapter and 32 ranks
-constexpr int kRanks = 32;
-__device__ __forceinline__ int adapter_blocks(const ProjectArgs& p, const TokenBlocks& tb, int lane) {
-  uint32_t left = tb.same;
-  int count = 0, a;
-  while (left) {
-    next_adapter(tb, left, lane, a);
-    ++count;
-  }
-  return count * ((p.ad.rank + kRanks - 1) / kRanks);
-}
-// Ranks that each half of such a block's K holds: [factors | factors] times [hi | lo]
-__device__ __forceinline__ int half_ranks(int rank, int r0) { return rank - r0 <= 16 ? 16 : kRanks; }
 
-// Such a block for ranks r0 ..: the 128 threads of a group write the factors of adapter a (as the weight's tile)
-// and the z of the tile's tokens (as the tokens' tile).  z of tokens that do not use the adapter is whatever
-// it is: the MMAs leave their columns alone.
-// The accumulator is in units of 128 s_g: z is divided by it.
-template <bool kForward, int kN>
-__device__ __forceinline__ void adapter_block(const ProjectArgs& p, uint8_t* ta, uint8_t* tb, int64_t t0, int64_t o0, int a, int r0,
-                                           int tid) {
-  const int rank = p.ad.rank, half = half_ranks(rank, r0), hc = half / 8;
-  if (kForward) {
-    const int64_t o = o0 + tid;
-    const __nv_bfloat16* src = p.ad.b + ((int64_t)a * p.w.m + o) * rank + r0;
-    for (int c = 0; c < hc; ++c) {
-      const uint4 q = o < p.w.m && r0 + 8 * c < rank ? ld_nc_v4(src + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
-      *reinterpret_cast<uint4*>(ta + tid * 128 + ((c ^ (tid & 7)) << 4)) = q;
-      *reinterpret_cast<uint4*>(ta + tid * 128 + (((c + hc) ^ (tid & 7)) << 4)) = q;
-    }
-  } else {
-    for (int i = tid; i < half * 16; i += kGroupThreads) {
-      const int r = i >> 4, group = (i >> 3) & 1, c = i & 7;
-      const int64_t o = o0 + group * 64 + c * 8;
-      const uint4 q = o < p.w.n && r0 + r < rank ? ld_nc_v4(p.ad.a + ((int64_t)a * rank + r0 + r) * p.w.n + o)
-                                                 : make_uint4(0u, 0u, 0u, 0u);
-      uint8_t* dst = ta + group * kGroupBytes + r * 128 + ((c ^ (r & 7)) << 4);
-      *reinterpret_cast<uint4*>(dst) = q;
-      *reinterpret_cast<uint4*>(dst + half * 128) = q;
+// Bits of a register's bf16 halves that are Inf or NaN (0xFFFF each).
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return __vcmpeq2(w & 0x7F807F80u, 0x7F807F80u); }
+
+// The K block of ranks r0 .. of the list's adapter e, by the epilogue's 128 threads: the factors (as the weight's
+// tile) and the z of its tokens (as the tokens' tile; the accumulator is in units of 128 s_g, so z is divided by it).
+// Loaded before `acquire` waits for the stage.  bad[output] gets bit e where a factor is Inf or NaN.
+template <bool kForward, int kN, typename Acquire>
+__device__ __forceinline__ bool adapter_block(const ProjectArgs& p, const TileInfo& info, int e, int r0, int64_t t0, int64_t o0,
+                                              int line, float unit, uint32_t* bad, uint8_t* tile_a, uint8_t* tile_b,
+                                              Acquire acquire) {
+  constexpr int kRows = (kN + 127) / 128;
+  const int rank = p.ad.rank, a = info.adapter[e], half = half_ranks(rank, r0), hc = half / 8;
+  uint4 f[4], hi[kRows][4], lo[kRows][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (i >= hc) continue;
+    if (kForward) {
+      if (o0 + line < p.w.m && r0 + 8 * i < rank) f[i] = ld_nc_v4(p.ad.b + ((int64_t)a * p.w.m + o0 + line) * rank + r0 + 8 * i);
+    } else {
+      const int k = line + i * 128, r = k >> 4;  // rank r, outputs 8 (k % 16) ..
+      const int64_t o = o0 + (k & 15) * 8;
+      if (o < p.w.n && r0 + r < rank) f[i] = ld_nc_v4(p.ad.a + ((int64_t)a * rank + r0 + r) * p.w.n + o);
     }
   }
-  const float unit = 1.0f / (128.0f * *p.w.global_scale);
-  for (int t = tid; t < kN; t += kGroupThreads) {
-    const float* src = p.z + (t0 + t) * rank + r0;
-    for (int c = 0; c < hc; ++c) {
-      uint32_t hi[4] = {0u, 0u, 0u, 0u}, lo[4] = {0u, 0u, 0u, 0u};
-      if (t0 + t < p.tokens && r0 + 8 * c < rank) {
-        const float4 v0 = reinterpret_cast<const float4*>(src)[2 * c], v1 = reinterpret_cast<const float4*>(src)[2 * c + 1];
-        const float v[8] = {v0.x * unit, v0.y * unit, v0.z * unit, v0.w * unit,
-                            v1.x * unit, v1.y * unit, v1.z * unit, v1.w * unit};
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int t = line + 128 * k;
+    const bool mine = t < kN && info.index[t < kN ? t : 0] == e;
+    const float4* src = reinterpret_cast<const float4*>(p.z + (t0 + t) * rank + r0);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
+      if (mine && c < hc && r0 + 8 * c < rank) v0 = src[2 * c], v1 = src[2 * c + 1];
+      const float v[8] = {v0.x * unit, v0.y * unit, v0.z * unit, v0.w * unit, v1.x * unit, v1.y * unit, v1.z * unit, v1.w * unit};
+      uint32_t h[4], l[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        h[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+        l[j] = pack_bf16(v[2 * j] - bf16_lo(h[j]), v[2 * j + 1] - bf16_hi(h[j]));
+      }
+      hi[k][c] = make_uint4(h[0], h[1], h[2], h[3]);
+      lo[k][c] = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+  }
+  uint32_t odd = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd |= not_finite(f[i].x) | not_finite(f[i].y) | not_finite(f[i].z) | not_finite(f[i].w);
+  if (odd) {
+    if (kForward) {
+      atomicOr(&bad[line], 1u << e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = make_uint4(0u, 0u, 0u, 0u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t w[4] = {f[i].x, f[i].y, f[i].z, f[i].w};
+        const int o = ((line + i * 128) & 15) * 8;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          hi[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-          lo[j] = pack_bf16(v[2 * j] - bf16_lo(hi[j]), v[2 * j + 1] - bf16_hi(hi[j]));
+          const uint32_t x = not_finite(w[j]);
+          if (x & 0xFFFFu) atomicOr(&bad[o + 2 * j], 1u << e);
+          if (x >> 16) atomicOr(&bad[o + 2 * j + 1], 1u << e);
+          w[j] &= ~x;
         }
+        f[i] = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      *reinterpret_cast<uint4*>(tb + t * 128 + ((c ^ (t & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      *reinterpret_cast<uint4*>(tb + t * 128 + (((c + hc) ^ (t & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
   }
+  int s;
+  if (!acquire(s)) return false;
+  uint8_t* ta = tile_a + s * kTileABytes;
+  uint8_t* tb = tile_b + s * Tile<kN>::kBBytes;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i >= hc) continue;
+    if (kForward) {
+      *reinterpret_cast<uint4*>(ta + line * 128 + ((i ^ (line & 7)) << 4)) = f[i];
+      *reinterpret_cast<uint4*>(ta + line * 128 + (((i + hc) ^ (line & 7)) << 4)) = f[i];
+    } else {
+      const int k = line + i * 128, r = k >> 4, c = k & 7;
+      uint8_t* dst = ta + ((k >> 3) & 1) * kGroupBytes + r * 128 + ((c ^ (r & 7)) << 4);
+      *reinterpret_cast<uint4*>(dst) = f[i];
+      *reinterpret_cast<uint4*>(dst + half * 128) = f[i];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int t = line + 128 * k;
+    if (t >= kN) continue;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if (c >= hc) continue;
+      *reinterpret_cast<uint4*>(tb + t * 128 + ((c ^ (t & 7)) << 4)) = hi[k][c];
+      *reinterpret_cast<uint4*>(tb + t * 128 + (((c + hc) ^ (t & 7)) << 4)) = lo[k][c];
+    }
+  }
+  return true;
 }
 
 // Tile t of the persistent order: groups of 8 token tiles, the outputs' tiles along a group, so that the
@@ -354,44 +414,15 @@ __device__ __forceinline__ void raster(int t, const ProjectArgs& p, int& tt, int
   to = within / rows;
 }
 
-// An unpacking group's progress over the adapters' blocks: the tile they are due for next, how many there have
-// been (both groups count all of them, and take them in turn).
-struct AdapterTurn {
-  int tile, extras;
-  bool waited;  // for z
-};
-// The group's part of the adapters' blocks of tiles turn.tile .. until - 1; false once a wait ran out.
-template <bool kForward, int kN>
-__device__ __noinline__ bool adapter_turn(const ProjectArgs& p, uint8_t* smem, uint64_t* full, uint64_t* empty, AdapterTurn& turn,
-                                          int until, int first, int step, int kbs, int who, int line) {
-  using T = Tile<kN>;
-  const int lane = threadIdx.x & 31;
-  for (; turn.tile < until; ++turn.tile) {
-    int tt, to;
-    raster(first + turn.tile * step, p, tt, to);
-    const TokenBlocks tb = token_blocks<kN>(p, (int64_t)tt * kN, lane);
-    uint32_t left = tb.same;
-    if (left && !turn.waited) {
-      pdl_wait_primary();
-      turn.waited = true;
-    }
-    while (left) {
-      int a;
-      next_adapter(tb, left, lane, a);
-      for (int r0 = 0; r0 < p.ad.rank; r0 += kRanks, ++turn.extras) {
-        if (turn.extras % kUnpackGroups != who) continue;
-        const int pos = (turn.tile + 1) * kbs + turn.extras, s = pos % T::kStages;
-        if (!mbar_wait_warp(&empty[s], ((uint32_t)(pos / T::kStages) & 1u) ^ 1u)) return false;
-        adapter_block<kForward, kN>(p, smem + s * kTileABytes, smem + T::kStages * kTileABytes + s * T::kBBytes,
-                                    (int64_t)tt * kN, (int64_t)to * kBM, a, r0, line);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&full[s]);
-      }
-    }
-  }
-  return true;
+// NaN where this output's factors of the token's adapter were left out of the K block.
+template <int W>
+__device__ __forceinline__ void spoil(uint32_t (&q)[W], uint32_t bad, const uint8_t* index) {
+  if (!__any_sync(0xFFFFFFFFu, bad != 0u)) return;
+#pragma unroll
+  for (int j = 0; j < W; ++j)
+    if (index[j] < kMaxListed && ((bad >> index[j]) & 1u)) q[j] = 0x7FC00000u;
 }
+__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 template <bool kForward, int kN>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -406,10 +437,17 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
   uint64_t* empty = full + kStages;
   uint64_t* acc_full = empty + kStages;
   uint64_t* acc_empty = acc_full + 2;
-  uint64_t* mma_done = acc_empty + 2;
+  uint64_t* info_full = acc_empty + 2;
+  uint64_t* slot = info_full + kInfos;  // a stage is free for an adapter's block
+  uint64_t* go_full = slot + kStages;   // a tile's place in the ring's order is known
+  uint64_t* mma_done = go_full + kGo;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
   uint32_t* failed = tmem_slot + 1;
-  float* zs = reinterpret_cast<float*>(smem + kStages * T::kStageBytes + 256) + (threadIdx.x >> 5 & 3) * 256;
+  int* place = reinterpret_cast<int*>(failed + 1);  // [kGo]
+  float* zs = reinterpret_cast<float*>(smem + kStages * T::kStageBytes + kBarBytes) + (threadIdx.x >> 5 & 3) * 256;
+  uint8_t* info_base = smem + kStages * T::kStageBytes + kBarBytes + 4096;
+  uint32_t* bad = reinterpret_cast<uint32_t*>(info_base + kInfos * kInfoBytes);  // [2][128]
+  auto info_of = [&](int i) -> TileInfo& { return *reinterpret_cast<TileInfo*>(info_base + (i % kInfos) * kInfoBytes); };
 
   const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int csize = p.csize;
@@ -421,17 +459,20 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
   const int ntiles = csize > 1 ? 1 : (tiles - first + step - 1) / step;
   const int kb0 = (int)((int64_t)p.kb_total * crank / csize), kb1 = (int)((int64_t)p.kb_total * (crank + 1) / csize);
   const int kbs = kb1 - kb0;
-  const bool adds = p.ad.count > 0 && crank == csize - 1;  // the adapters' blocks are the last rank's
+  const bool adapters = p.ad.count > 0, adds = adapters && crank == csize - 1;  // the last rank adds the K blocks
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&full[s], 1 + kGroupThreads / 32);  // the TMA load and the unpacking group's warps
       mbar_init(&empty[s], 1);
+      mbar_init(&slot[s], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&acc_full[i], 1);
       mbar_init(&acc_empty[i], 128);
     }
+    for (int i = 0; i < kInfos; ++i) mbar_init(&info_full[i], 1);
+    for (int i = 0; i < kGo; ++i) mbar_init(&go_full[i], 1);
     mbar_init(mma_done, 1);
     *failed = 0u;
     mbar_fence_init();
@@ -451,11 +492,14 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
   const uint32_t lane_base = (quarter * 32u) << 16;
   const int out_row = (int)quarter * 32 + lane;
   bool have = true;  // the cluster's partial is complete
+  // the adapters of the CTA's tile i
+  auto wait_info = [&](int i) { return mbar_wait_warp(&info_full[i % kInfos], (uint32_t)(i / kInfos) & 1u); };
 
   if (warp == 0) {
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
     uint32_t s = 0, parity = 1;
+    int extras = 0;
     bool go = true;
     for (int i = 0; i < ntiles && go; ++i) {
       int tt, to;
@@ -476,20 +520,31 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           parity ^= 1u;
         }
       }
-      // the adapters' blocks are the unpacking warps' alone
-      const int extra = adds && go ? adapter_blocks(p, token_blocks<kN>(p, (int64_t)tt * kN, lane), lane) : 0;
+      // the adapters' blocks are the epilogue warps' alone, which this warp tells when a stage is theirs (they come
+      // from far behind in the ring's order, and the parity of `empty` only tells neighbouring turns apart)
+      if (adds && go && !(go = wait_info(i)) && lane == 0) atomicOr(failed, 1u);
+      const int extra = adds && go ? info_of(i).blocks : 0;
       for (int e = 0; e < extra; ++e) {
         if (!mbar_wait_warp(&empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
           go = false;
           break;
         }
-        if (elect_one()) mbar_arrive(&full[s]);
+        if (elect_one()) {
+          mbar_arrive(&full[s]);
+          mbar_arrive(&slot[s]);
+        }
         __syncwarp();
         if (++s == kStages) {
           s = 0;
           parity ^= 1u;
         }
+      }
+      // the unpacking warps skip them: the next tile's place, told once this warp has come to it
+      extras += extra;
+      if (adds && go && lane == 0) {
+        place[i % kGo] = (i + 1) * kbs + extras;
+        mbar_arrive(&go_full[i % kGo]);
       }
     }
     // a full barrier also waits for the unpacking warps, whose waits are bounded like this one's
@@ -507,9 +562,6 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
         break;
       }
       tc_fence_after_sync();
-      int tt, to;
-      raster(first + i * step, p, tt, to);
-      TokenBlocks tb = {0u, 0u, -1};
       for (int kb = 0; kb < kbs; ++kb) {
         if (!mbar_wait_warp(&full[s], parity)) {
           ok = false;
@@ -530,14 +582,12 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           s = 0;
           parity ^= 1u;
         }
-        // looked up while the MMAs of a few blocks are under way
-        if (adds && kb == min(3, kbs - 1)) tb = token_blocks<kN>(p, (int64_t)tt * kN, lane);
       }
-      if (ok) {
-        uint32_t left = tb.same;
-        while (left && ok) {
-          int who;
-          const uint32_t sel = next_adapter(tb, left, lane, who);
+      if (adds && ok) ok = wait_info(i);
+      if (adds && ok) {
+        const TileInfo& info = info_of(i);
+        for (int e = 0; e < info.listed && ok; ++e) {
+          const uint32_t sel = info.sel[e];
           for (int r0 = 0; r0 < p.ad.rank && ok; r0 += kRanks) {
             if (!mbar_wait_warp(&full[s], parity)) {
               ok = false;
@@ -574,42 +624,79 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
     __syncwarp();
     umma_drain(mma_done);
   } else if (warp < kUnpackWarp0) {
-    if (csize == 1) {
-      const float scale = *p.w.global_scale * 128.0f;
-      if (p.chained) pdl_wait_primary();  // z
-      for (int i = 0; i < ntiles; ++i) {
-        int tt, to;
-        raster(first + i * step, p, tt, to);
-        const uint32_t acc = (uint32_t)i & 1u;
-        if (!mbar_wait_acc(&acc_full[acc], (uint32_t)(i >> 1) & 1u)) {
-          atomicOr(failed, 1u);
-          break;
-        }
-        tc_fence_after_sync();
-        const int64_t o = (int64_t)to * kBM + out_row;
-        const uint32_t mixed = token_blocks<kN>(p, (int64_t)tt * kN, lane).mixed;
-#pragma unroll 1
-        for (int c = 0; c < kN; c += 32) {
-          const int64_t t0 = (int64_t)tt * kN + c;
-          uint32_t q[32];
-          tmem_ld_32x32b_x32(tmem_d + acc * kN + lane_base + (uint32_t)c, q);
-          tmem_ld_wait();
-          if (c + 32 == kN) {
-            tc_fence_before_sync();
-            mbar_arrive(&acc_empty[acc]);
+    const float scale = *p.w.global_scale * 128.0f;
+    const auto find = [&](int i) {
+      if (!adapters || warp != 2 || i >= ntiles) return;
+      int tt, to;
+      raster(first + i * step, p, tt, to);
+      find_adapters<kN>(p, (int64_t)tt * kN, lane, info_of(i));
+      if (lane == 0) mbar_arrive(&info_full[i % kInfos]);
+    };
+    bad[out_row] = bad[128 + out_row] = 0u;
+    find(0);
+    find(1);
+    epilogue_sync();
+    if (p.chained) pdl_wait_primary();  // z
+    int extras = 0;          // the adapters' blocks so far
+    uint32_t slot_turn = 0;  // parity of each stage's next `slot`
+    // a wait that ran out ends the waiting, not the tiles: every warp reaches every barrier
+    for (int i = 0; i < ntiles; ++i) {
+      int tt, to;
+      raster(first + i * step, p, tt, to);
+      const uint32_t acc = (uint32_t)i & 1u;
+      const int64_t o = (int64_t)to * kBM + out_row;
+      const TileInfo& info = info_of(i);
+      uint32_t spoiled = 0u;
+      if (adapters && have) have = wait_info(i);
+      if (adds) {
+        for (int e = 0; have && e < info.listed; ++e)
+          for (int r0 = 0; r0 < p.ad.rank && have; r0 += kRanks, ++extras) {
+            int s = 0;
+            const auto acquire = [&](int& stage) {
+              s = stage = ((i + 1) * kbs + extras) % kStages;
+              const uint32_t parity = (slot_turn >> s) & 1u;
+              slot_turn ^= 1u << s;
+              return mbar_wait_warp(&slot[s], parity);
+            };
+            have = adapter_block<kForward, kN>(p, info, e, r0, (int64_t)tt * kN, (int64_t)to * kBM, out_row, 1.0f / scale,
+                                               bad + acc * 128, tile_a, tile_b, acquire);
+            if (have) {
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&full[s]);
+            }
           }
-          if (t0 >= p.tokens) continue;
-          float v[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(q[j]) * scale;
-          finish<kForward, 32>(v, t0, o, lane, p, mixed >> (c >> 4), zs);
-        }
+        epilogue_sync();
+        spoiled = bad[acc * 128 + out_row];
+        bad[acc * 128 + out_row] = 0u;  // its next use is two tiles on, behind the next tile's barrier
       }
-    } else {
-      have = mbar_wait_acc(&acc_full[0], 0u);
-      if (!have) atomicOr(failed, 1u);
+      if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i >> 1) & 1u));
+      if (!have) continue;
       tc_fence_after_sync();
+      find(i + 2);  // every role is done with tile i - 2, whose place it takes
+      if (csize > 1) {
+        bad[out_row] = spoiled;
+        break;
+      }
+#pragma unroll 1
+      for (int c = 0; c < kN; c += 32) {
+        const int64_t t0 = (int64_t)tt * kN + c;
+        uint32_t q[32];
+        tmem_ld_32x32b_x32(tmem_d + acc * kN + lane_base + (uint32_t)c, q);
+        tmem_ld_wait();
+        if (c + 32 == kN) {
+          tc_fence_before_sync();
+          mbar_arrive(&acc_empty[acc]);
+        }
+        if (t0 >= p.tokens) continue;
+        if (adapters) spoil<32>(q, spoiled, info.index + c);
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(q[j]) * scale;
+        finish<kForward, 32>(v, t0, o, lane, p, adapters ? info.loose[c >> 5] : 0u, zs);
+      }
     }
+    if (!have && lane == 0) atomicOr(failed, 1u);
   } else {
     // ---- the weight's tile.  Thread: one row of 64 nibbles, K-major an output's, MN-major 64 outputs of a K
     const int tid = (int)threadIdx.x - kUnpackWarp0 * 32;
@@ -663,8 +750,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
       if (who + u * kUnpackGroups < total) load(ring[u], codes[u]);
-    AdapterTurn turn = {0, 0, p.chained == 0};
-    int tile_end = adds ? kbs : INT32_MAX;  // first block of the next tile, whose turn is behind the adapters'
+    int tile_end = adds ? kbs : INT32_MAX;  // the first block behind the present tile
     uint32_t s = (uint32_t)who % kStages, parity = 1;
     bool go = true;
     for (int base = who; base < total && go; base += kAhead * kUnpackGroups) {
@@ -673,12 +759,13 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
         const int next = base + u * kUnpackGroups;
         if (next >= total || !go) break;
         if (next >= tile_end) {
-          const int tile = next / kbs;
+          const int tile = next / kbs, before = tile - 1;
           tile_end = (tile + 1) * kbs;
-          go = adapter_turn<kForward, kN>(p, smem, full, empty, turn, tile, first, step, kbs, who, line);
+          go = mbar_wait_warp(&go_full[before % kGo], (uint32_t)(before / kGo) & 1u);
           if (!go) break;
-          s = (uint32_t)(next + turn.extras) % kStages;
-          parity = (((uint32_t)(next + turn.extras) / kStages) & 1u) ^ 1u;
+          const uint32_t pos = (uint32_t)(place[before % kGo] + next - tile * kbs);
+          s = pos % kStages;
+          parity = ((pos / kStages) & 1u) ^ 1u;
         }
         if (!mbar_wait_warp(&empty[s], parity)) {
           go = false;
@@ -704,7 +791,6 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
         if (base + (u + kAhead) * kUnpackGroups < total) load(ring[u], codes[u]);
       }
     }
-    if (go && adds) go = adapter_turn<kForward, kN>(p, smem, full, empty, turn, ntiles, first, step, kbs, who, line);
     if (!go && lane == 0) atomicOr(failed, 1u);
   }
 
@@ -728,6 +814,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           uint32_t q[8];
           tmem_ld_32x32b_x8(tmem_d + lane_base + (uint32_t)(d * own + c), q);
           tmem_ld_wait();
+          if (adds) spoil<8>(q, bad[out_row], info_of(0).index + d * own + c);
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(base + (uint32_t)((c + j) * kBM * 4)),
@@ -739,15 +826,15 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
     cluster_sync();
     if (epilogue) {
       const float scale = *p.w.global_scale * 128.0f;
-      if (p.chained) pdl_wait_primary();  // z
       const int64_t o = (int64_t)to * kBM + out_row;
-      const uint32_t mixed = token_blocks<kN>(p, (int64_t)tt * kN, lane).mixed;
       for (int c = 0; c < own; c += 8) {
         const int64_t t0 = (int64_t)tt * kN + crank * own + c;
         uint32_t q[8];
         tmem_ld_32x32b_x8(tmem_d + lane_base + (uint32_t)(crank * own + c), q);
         tmem_ld_wait();
         if (t0 >= p.tokens) continue;
+        const int col = crank * own + c;
+        if (adds) spoil<8>(q, bad[out_row], info_of(0).index + col);
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -757,7 +844,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
             sum += d == crank ? mine : inbox[(d * own + c + j) * kBM + out_row];
           v[j] = sum * scale;
         }
-        finish<kForward, 8>(v, t0, o, lane, p, mixed >> ((crank * own + c) >> 4), zs);
+        finish<kForward, 8>(v, t0, o, lane, p, adapters && have ? info_of(0).loose[col >> 5] >> (col & 31) : 0u, zs);
       }
     }
   }

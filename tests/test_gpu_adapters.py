@@ -339,6 +339,34 @@ def test_inf_and_nan_stay_in_their_token_and_adapter(t):
     assert torch.equal(da[3], clean_b[1][3]) and torch.equal(db[3], clean_b[2][3])
 
 
+@pytest.mark.parametrize("t, m, n, rank, order", [
+    (64, 200, 512, 16, "mixed"), (300, 200, 512, 16, "mixed"), (300, 264, 272, 64, "mixed"), (700, 130, 400, 8, "runs"),
+    (257, 640, 2048, 24, "runs"), (2000, 384, 256, 40, "mixed")])
+def test_a_broken_adapter_of_many_tokens(t, m, n, rank, order):
+    """One of three adapters holds an Inf and a NaN: the others' tokens keep their bits, its own tokens keep
+    theirs at the outputs that its factors do not spoil."""
+    L = Layer(t, m, n, 3, rank, order, seed=2)
+    clean, clean_b = L.project(), L.backward()
+    on = L.which == 1
+    L.b[1, 7, 2], L.b[1, m - 1, rank - 1] = float("nan"), float("inf")
+    y = L.project()
+    assert torch.equal(y[~on], clean[~on])
+    spoilt = torch.zeros(m, dtype=torch.bool, device=DEV)
+    spoilt[[7, m - 1]] = True
+    assert torch.equal(y[on][:, ~spoilt], clean[on][:, ~spoilt])
+    assert y[on][:, 7].isnan().all() and not y[on][:, m - 1].isfinite().any()
+    L.b[1] = Layer(t, m, n, 3, rank, order, seed=2).b[1]
+    L.a[1, rank - 1, 9], L.a[1, 0, n - 2] = float("-inf"), float("nan")
+    dx, da, db, _ = L.backward()
+    assert torch.equal(dx[~on], clean_b[0][~on])
+    spoilt = torch.zeros(n, dtype=torch.bool, device=DEV)
+    spoilt[[9, n - 2]] = True
+    assert torch.equal(dx[on][:, ~spoilt], clean_b[0][on][:, ~spoilt])
+    assert not dx[on][:, spoilt].isfinite().any()
+    assert torch.equal(da, clean_b[1])  # z alone depends on A
+    assert torch.equal(db[[0, 2]], clean_b[2][[0, 2]])
+
+
 def test_another_stream_and_a_given_workspace():
     L = Layer(70, 300, 512, 5, 16, "mixed")
     want, wantb = L.project(), L.backward()
