@@ -45,15 +45,15 @@ namespace hscale {
 namespace {
 
 constexpr int kBM = 128, kBK = 64;
-constexpr int kThreads = 448;
-constexpr int kUnpackWarp0 = 6, kUnpackGroups = 2, kGroupThreads = 128;
-constexpr int kAhead = 4;  // blocks of its own that a group has in flight
+constexpr int kThreads = 576;
+constexpr int kUnpackWarp0 = 6, kUnpackGroups = 3, kGroupThreads = 128;
+constexpr int kAhead = 3;  // blocks of its own that a group has in flight
 constexpr uint32_t kTileABytes = kBM * kBK * 2;  // 16 KB
 constexpr uint32_t kGroupBytes = 64 * kBK * 2;   // MN-major: 64 outputs x 64 rows of K
 constexpr int kInfos = 4;                        // TileInfo of as many tiles
 constexpr uint32_t kInfoBytes = 576;
 constexpr uint32_t kBarBytes = 512;
-constexpr int kGo = 8;                           // tiles whose place in the ring's order is kept: more than it has stages
+constexpr int kGo = 16;                          // tiles whose place in the ring's order is kept: more than it has stages
 
 template <int kN>
 struct Tile {
@@ -104,26 +104,28 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t (&r
   r[3] = mul_bf16x2((b & kSign) | ((b >> 6) & kMag), scale);
 }
 
-// Loads that stay where they are written, so that several are in flight.
-__device__ __forceinline__ void ld_32_ahead(const void* p, uint32_t (&r)[8]) {
-  asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-               : "l"(p));
+// Loads that stay where they are written, so that several are in flight, and that leave the registers as they are
+// where `on` is false (a branch around a load would have the result moved, and the move waits for it).
+__device__ __forceinline__ void ld_32_ahead(bool on, const void* p, uint32_t (&r)[8]) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %9, 0;\n\t"
+               "@p ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t}"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+               : "l"(p), "r"((uint32_t)on));
 }
-__device__ __forceinline__ uint2 ld_8_ahead(const void* p) {
-  uint2 r;
-  asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
-  return r;
+__device__ __forceinline__ void ld_8_ahead(bool on, const void* p, uint32_t& a, uint32_t& b) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\t@p ld.global.nc.v2.u32 {%0, %1}, [%2];\n\t}"
+               : "+r"(a), "+r"(b)
+               : "l"(p), "r"((uint32_t)on));
 }
-__device__ __forceinline__ uint32_t ld_4_ahead(const void* p) {
-  uint32_t r;
-  asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(r) : "l"(p));
-  return r;
+__device__ __forceinline__ void ld_4_ahead(bool on, const void* p, uint32_t& a) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u32 %0, [%1];\n\t}"
+               : "+r"(a)
+               : "l"(p), "r"((uint32_t)on));
 }
-__device__ __forceinline__ uint32_t ld_1_ahead(const void* p) {
-  uint32_t r;
-  asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(r) : "l"(p));
-  return r;
+__device__ __forceinline__ void ld_1_ahead(bool on, const void* p, uint32_t& a) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u8 %0, [%1];\n\t}"
+               : "+r"(a)
+               : "l"(p), "r"((uint32_t)on));
 }
 
 __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
@@ -706,42 +708,45 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
     const int64_t m = p.w.m, n = p.w.n;
     const bool wide = (n & 63) == 0 && (reinterpret_cast<uintptr_t>(p.w.packed) & 31) == 0 &&
                       (reinterpret_cast<uintptr_t>(p.w.codes) & 3) == 0;
-    // position of the next block to load
-    int li = -1, lk = kb1;
+    // the next block to load: where its 32 bytes and 4 codes are, and K blocks left in its tile
+    int li = -1, left = 0;
     int64_t f = 0, k0 = 0;
+    const uint8_t *wp = nullptr, *cp = nullptr;
+    const int64_t w_step = kUnpackGroups * (kForward ? (int64_t)kBK / 2 : kBK * (n >> 1));
+    const int64_t c_step = kUnpackGroups * (kForward ? (int64_t)kBK / 16 : kBK * (n >> 4));
     const int total = ntiles * kbs;
     auto advance = [&](int blocks) {
-      lk += blocks;
-      if (kForward) k0 += blocks * kBK; else f += blocks * kBK;
-      while (lk >= kb1 && li < ntiles) {
-        lk -= kbs;
-        int tt, to;
-        if (++li < ntiles) {
-          raster(first + li * step, p, tt, to);
-          f = kForward ? (int64_t)to * kBM + row : (int64_t)lk * kBK + row;
-          k0 = kForward ? (int64_t)lk * kBK : (int64_t)to * kBM + (line >> 6) * 64;
-        }
+      left -= blocks;
+      if (left > 0) {
+        if (kForward) k0 += kUnpackGroups * kBK; else f += kUnpackGroups * kBK;
+        wp += w_step, cp += c_step;
+        return;
       }
+      while (left <= 0 && ++li < ntiles) left += kbs;
+      if (li >= ntiles) return;
+      int tt, to;
+      raster(first + li * step, p, tt, to);
+      const int64_t kb = kb1 - left;
+      f = kForward ? (int64_t)to * kBM + row : kb * kBK + row;
+      k0 = kForward ? kb * kBK : (int64_t)to * kBM + (line >> 6) * 64;
+      wp = p.w.packed + f * (n >> 1) + (k0 >> 1);
+      cp = p.w.codes + f * (n >> 4) + (k0 >> 4);
     };
-    uint32_t ring[kAhead][8], codes[kAhead];
-    auto load = [&](uint32_t (&q)[8], uint32_t& c) {
+    uint32_t ring[kAhead][8], codes[kAhead][4];  // codes: one word, or one byte a word
+    auto load = [&](uint32_t (&q)[8], uint32_t (&c)[4]) {
+      const bool on = f < m && k0 < n;
 #pragma unroll
       for (int i = 0; i < 8; ++i) q[i] = 0u;
-      c = 0u;
-      if (f < m && k0 < n) {
-        const uint8_t* wp = p.w.packed + f * (n >> 1) + (k0 >> 1);
-        const uint8_t* cp = p.w.codes + f * (n >> 4) + (k0 >> 4);
-        if (wide) {
-          ld_32_ahead(wp, q);
-          c = ld_4_ahead(cp);
-        } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (k0 + 16 * i < n) {
-              const uint2 v = ld_8_ahead(wp + 8 * i);
-              q[2 * i] = v.x, q[2 * i + 1] = v.y;
-              c |= ld_1_ahead(cp + i) << (8 * i);
-            }
+      for (int i = 0; i < 4; ++i) c[i] = 0u;
+      if (wide) {
+        ld_32_ahead(on, wp, q);
+        ld_4_ahead(on, cp, c[0]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ld_8_ahead(on && k0 + 16 * i < n, wp + 8 * i, q[2 * i], q[2 * i + 1]);
+          ld_1_ahead(on && k0 + 16 * i < n, cp + i, c[i]);
         }
       }
       advance(kUnpackGroups);
@@ -772,7 +777,8 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           break;
         }
         uint8_t* dst = tile_a + s * kTileABytes + line * 128;
-        const uint32_t ca = unpack_codes(codes[u] & 0xFFFFu), cb = unpack_codes(codes[u] >> 16);
+        const uint32_t code = codes[u][0] | codes[u][1] << 8 | codes[u][2] << 16 | codes[u][3] << 24;
+        const uint32_t ca = unpack_codes(code & 0xFFFFu), cb = unpack_codes(code >> 16);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const uint32_t c = i < 4 ? ca : cb;
