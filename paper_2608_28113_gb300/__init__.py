@@ -588,11 +588,31 @@ def hscale_checkpoint_load(codes: torch.Tensor, scales: torch.Tensor, fmt: int, 
                                          _stream_ptr(stream)))
 
 
-def _whole(t: torch.Tensor, name: str, dtype, shape: tuple) -> torch.Tensor:
+def _whole(t: torch.Tensor, name: str, dtype, shape: tuple) -> None:
+    try:
+        if t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous():
+            return
+    except AttributeError:
+        pass
     _need(t, dtype, name)
-    if tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous {list(shape)}")
-    return t
+    raise ValueError(f"{name} must be contiguous {list(shape)}")
+
+
+def _rows(t: torch.Tensor, name: str) -> tuple:
+    """(rows, columns, row stride) of a bf16 [rows, columns] view with contiguous rows.  A single row's stride
+    is free: rounded up to the alignment that the library asks for."""
+    try:
+        if t.dtype is torch.bfloat16 and t.is_cuda:
+            rows, cols = t.shape
+            ld, step = t.stride()
+            if step == 1 or cols <= 1:
+                return rows, cols, ld if rows > 1 else (max(cols, ld) + 7) // 8 * 8
+    except (AttributeError, ValueError):
+        pass
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D view")
+    _need(t, torch.bfloat16, name)
+    raise ValueError(f"{name} must be a 2-D view with contiguous rows")
 
 
 def _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens: int, m: int, n: int):
@@ -609,7 +629,7 @@ def _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens: in
     _need(a, torch.bfloat16, "a")
     if a.dim() != 3:
         raise ValueError("a must be [adapters, rank, n]")
-    adapters, rank = a.shape[0], a.shape[1]
+    adapters, rank, _ = a.shape
     _whole(a, "a", torch.bfloat16, (adapters, rank, n))
     _whole(b, "b", torch.bfloat16, (adapters, m, rank))
     _whole(alpha, "alpha", torch.float32, (adapters,))
@@ -637,25 +657,19 @@ def hscale_project(x: torch.Tensor, packed: torch.Tensor, codes: torch.Tensor, g
     """y (bf16 [tokens, m]) = x W_hat^T, plus alpha_a B_a A_a x_t with a = adapter_of[t] (int32 [tokens];
     outside [0, adapters): none; None: adapter 0 for every token).  a [adapters, rank, n] and
     b [adapters, m, rank] are bf16, alpha fp32 [adapters]; a, b, alpha None: no adapters."""
-    if not isinstance(x, torch.Tensor) or not isinstance(y, torch.Tensor) or x.dim() != 2 or y.dim() != 2:
-        raise ValueError("x and y must be 2-D views")
-    (tokens, n), m = x.shape, y.shape[1]
-    ld_x = _row_view(x, "x", torch.bfloat16, tokens, n)
-    ld_y = _row_view(y, "y", torch.bfloat16, tokens, m)
+    tokens, n, ld_x = _rows(x, "x")
+    y_rows, m, ld_y = _rows(y, "y")
+    if y_rows != tokens:
+        raise ValueError("x and y must have the same number of rows")
     adapters, rank = _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens, m, n)
+    lib = load()
     workspace, nbytes = _project_workspace(
-        workspace, load().hscale_project_workspace_bytes(tokens, m, n, adapters, rank) if workspace is None else 0,
+        workspace, lib.hscale_project_workspace_bytes(tokens, m, n, adapters, rank) if workspace is None else 0,
         x.device)
     _check("hscale_project",
-           load().hscale_project(_ptr(x), tokens, n, _ld8(ld_x, tokens), _ptr(packed), _ptr(codes),
-                                 _ptr(global_scale), m, _ptr(a), _ptr(b), _ptr(alpha), adapters, rank,
-                                 _ptr(adapter_of), _ptr(y), _ld8(ld_y, tokens), _ptr(workspace), nbytes,
-                                 _stream_ptr(stream)))
-
-
-def _ld8(ld: int, rows: int) -> int:
-    """A single row's stride is free: rounded up to the alignment that the library asks for."""
-    return ld if rows > 1 else (ld + 7) // 8 * 8
+           lib.hscale_project(x.data_ptr(), tokens, n, ld_x, packed.data_ptr(), codes.data_ptr(),
+                              global_scale.data_ptr(), m, _ptr(a), _ptr(b), _ptr(alpha), adapters, rank,
+                              _ptr(adapter_of), y.data_ptr(), ld_y, _ptr(workspace), nbytes, _stream_ptr(stream)))
 
 
 def hscale_project_backward_workspace_bytes(tokens: int, m: int, n: int, adapters: int, rank: int) -> int:
@@ -669,14 +683,16 @@ def hscale_project_backward(dy: torch.Tensor, x_codes: torch.Tensor | None, x_sc
                             db: torch.Tensor | None, workspace: torch.Tensor | None = None, stream=None) -> None:
     """The gradients of hscale_project for dy (bf16 [tokens, m]) at the x of a checkpoint (x_codes, x_scales,
     x_format): dx (bf16 [tokens, n]), da and db (bf16, shaped like a and b); each may be None."""
-    if not isinstance(dy, torch.Tensor) or dy.dim() != 2:
-        raise ValueError("dy must be a 2-D view")
+    tokens, m, ld_dy = _rows(dy, "dy")
     _need(packed, torch.uint8, "packed")
     if packed.dim() != 2:
         raise ValueError("packed must be [m, n/2]")
-    (tokens, m), n = dy.shape, 2 * packed.shape[1]
-    ld_dy = _row_view(dy, "dy", torch.bfloat16, tokens, m)
-    ld_dx = n if dx is None else _row_view(dx, "dx", torch.bfloat16, tokens, n)
+    n = 2 * packed.shape[1]
+    ld_dx = n
+    if dx is not None:
+        dx_rows, dx_cols, ld_dx = _rows(dx, "dx")
+        if (dx_rows, dx_cols) != (tokens, n):
+            raise ValueError(f"dx must be a [{tokens}, {n}] view")
     adapters, rank = _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens, m, n)
     if adapters == 0 and (da is not None or db is not None):
         if a is None:
@@ -689,12 +705,13 @@ def hscale_project_backward(dy: torch.Tensor, x_codes: torch.Tensor | None, x_sc
     if adapters > 0 and (da is not None or db is not None):
         ld_c = _row_view(x_codes, "x_codes", torch.uint8, tokens, n)
         ld_s = _row_view(x_scales, "x_scales", torch.uint8, tokens, (n + 31) // 32)
+    lib = load()
     workspace, nbytes = _project_workspace(
-        workspace, load().hscale_project_backward_workspace_bytes(tokens, m, n, adapters, rank)
+        workspace, lib.hscale_project_backward_workspace_bytes(tokens, m, n, adapters, rank)
         if workspace is None else 0, dy.device)
     _check("hscale_project_backward",
-           load().hscale_project_backward(_ptr(dy), tokens, m, _ld8(ld_dy, tokens), _ptr(x_codes), ld_c,
-                                          _ptr(x_scales), ld_s, int(x_format), n, _ptr(packed), _ptr(codes),
-                                          _ptr(global_scale), _ptr(a), _ptr(b), _ptr(alpha), adapters, rank,
-                                          _ptr(adapter_of), _ptr(dx), _ld8(ld_dx, tokens), _ptr(da), _ptr(db),
-                                          _ptr(workspace), nbytes, _stream_ptr(stream)))
+           lib.hscale_project_backward(dy.data_ptr(), tokens, m, ld_dy, _ptr(x_codes), ld_c, _ptr(x_scales), ld_s,
+                                       int(x_format), n, packed.data_ptr(), codes.data_ptr(),
+                                       global_scale.data_ptr(), _ptr(a), _ptr(b), _ptr(alpha), adapters, rank,
+                                       _ptr(adapter_of), _ptr(dx), ld_dx, _ptr(da), _ptr(db), _ptr(workspace),
+                                       nbytes, _stream_ptr(stream)))

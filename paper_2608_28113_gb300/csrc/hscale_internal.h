@@ -147,6 +147,11 @@ cudaError_t launch_adapter_grad_b(const void* dy, int64_t ld_dy, int64_t tokens,
 cudaError_t launch_project(bool forward, const void* v, int64_t tokens, int64_t ld_v, const Nvfp4Weight& w,
                            const Adapters& ad, const float* z, void* out, int64_t ld_out, cudaStream_t stream);
 
+// The forward product for up to kDecodeTokens tokens.
+constexpr int64_t kDecodeTokens = 16;
+cudaError_t launch_project_decode(const void* x, int64_t tokens, int64_t ld_x, const Nvfp4Weight& w, const Adapters& ad,
+                                  const float* z, void* y, int64_t ld_y, cudaStream_t stream);
+
 // Sticky device error flags of each translation unit (bit 0: a bounded wait ran out);
 // cleared on read.
 cudaError_t read_hessian_device_error(uint32_t* flags);

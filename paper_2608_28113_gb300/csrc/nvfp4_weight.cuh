@@ -16,9 +16,48 @@ struct Nvfp4Weight {
   int64_t m, n;
 };
 
-// E4M3 value of a code byte, read as the rest of the library reads codes: sign cleared, in [1, 126].
-__device__ __forceinline__ uint32_t ladder_code(uint32_t c) {
-  return min(max(c & 0x7Fu, 1u), kE4M3MaxCode);
+// Weights as bf16.  E2M1 times E4M3 has at most 6 significant bits, so a weight without s_g is exact in bf16; the
+// kernels hold 2^-7 of it (kWeightUnit) and multiply their sums by 128 s_g.
+constexpr float kWeightUnit = 128.0f;
+
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Two code bytes as bf16x2 E4M3 2^119, read as the rest of the library reads codes: sign cleared, in [1, 126].
+// A byte shifted to bf16's mantissa and low exponent bits reads as
+// E4M3 2^-120, subnormals included (the formats' subnormal boundaries line up).
+__device__ __forceinline__ uint32_t unpack_codes(uint32_t c2) {
+  uint32_t c = (c2 & 0x7Fu) | ((c2 & 0x7F00u) << 8);
+  c = __vminu2(__vmaxu2(c, 0x00010001u), kE4M3MaxCode * 0x00010001u);
+  return mul_bf16x2(mul_bf16x2(c << 4, 0x7F007F00u /* 2^127 */), 0x77807780u /* 2^112 */);
+}
+
+
+// Loads that stay where they are written, so that several are in flight, and that leave the registers as they are
+// where `on` is false (a branch around a load would have the result moved, and the move waits for it).
+__device__ __forceinline__ void ld_32_ahead(bool on, const void* p, uint32_t (&r)[8]) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %9, 0;\n\t"
+               "@p ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t}"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+               : "l"(p), "r"((uint32_t)on));
+}
+__device__ __forceinline__ void ld_8_ahead(bool on, const void* p, uint32_t& a, uint32_t& b) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\t@p ld.global.nc.v2.u32 {%0, %1}, [%2];\n\t}"
+               : "+r"(a), "+r"(b)
+               : "l"(p), "r"((uint32_t)on));
+}
+__device__ __forceinline__ void ld_4_ahead(bool on, const void* p, uint32_t& a) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u32 %0, [%1];\n\t}"
+               : "+r"(a)
+               : "l"(p), "r"((uint32_t)on));
+}
+__device__ __forceinline__ void ld_1_ahead(bool on, const void* p, uint32_t& a) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u8 %0, [%1];\n\t}"
+               : "+r"(a)
+               : "l"(p), "r"((uint32_t)on));
 }
 
 // The low-rank adapters of a call: A [count, rank, n], B [count, m, rank], alpha [count], and the

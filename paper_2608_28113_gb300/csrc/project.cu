@@ -77,20 +77,6 @@ struct ProjectArgs {
 };
 
 // ---------------------------------------------------------------- weights
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-
-// Two code bytes as bf16x2 E4M3 2^119.  A byte shifted to bf16's mantissa and low exponent bits reads as
-// E4M3 2^-120, subnormals included (the formats' subnormal boundaries line up).
-__device__ __forceinline__ uint32_t unpack_codes(uint32_t c2) {
-  uint32_t c = (c2 & 0x7Fu) | ((c2 & 0x7F00u) << 8);
-  c = __vminu2(__vmaxu2(c, 0x00010001u), kE4M3MaxCode * 0x00010001u);
-  return mul_bf16x2(mul_bf16x2(c << 4, 0x7F007F00u /* 2^127 */), 0x77807780u /* 2^112 */);
-}
-
 // Eight nibbles times a scale (bf16x2, both halves): a nibble's magnitude bits at bf16's bits 8-6 read as
 // E2M1 2^-126, so with scales E4M3 2^119 the products are the weights 2^-7, exact.
 __device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t (&r)[4]) {
@@ -102,30 +88,6 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t (&r
   r[1] = mul_bf16x2((a & kSign) | ((a >> 6) & kMag), scale);
   r[2] = mul_bf16x2(((b << 8) & kSign) | ((b << 2) & kMag), scale);
   r[3] = mul_bf16x2((b & kSign) | ((b >> 6) & kMag), scale);
-}
-
-// Loads that stay where they are written, so that several are in flight, and that leave the registers as they are
-// where `on` is false (a branch around a load would have the result moved, and the move waits for it).
-__device__ __forceinline__ void ld_32_ahead(bool on, const void* p, uint32_t (&r)[8]) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %9, 0;\n\t"
-               "@p ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t}"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
-               : "l"(p), "r"((uint32_t)on));
-}
-__device__ __forceinline__ void ld_8_ahead(bool on, const void* p, uint32_t& a, uint32_t& b) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\t@p ld.global.nc.v2.u32 {%0, %1}, [%2];\n\t}"
-               : "+r"(a), "+r"(b)
-               : "l"(p), "r"((uint32_t)on));
-}
-__device__ __forceinline__ void ld_4_ahead(bool on, const void* p, uint32_t& a) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u32 %0, [%1];\n\t}"
-               : "+r"(a)
-               : "l"(p), "r"((uint32_t)on));
-}
-__device__ __forceinline__ void ld_1_ahead(bool on, const void* p, uint32_t& a) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u8 %0, [%1];\n\t}"
-               : "+r"(a)
-               : "l"(p), "r"((uint32_t)on));
 }
 
 __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
@@ -918,6 +880,7 @@ cudaError_t launch(const void* v, int64_t ld_v, ProjectArgs p, int csize, int sm
 
 cudaError_t launch_project(bool forward, const void* v, int64_t tokens, int64_t ld_v, const Nvfp4Weight& w, const Adapters& ad,
                            const float* z, void* out, int64_t ld_out, cudaStream_t stream) {
+  if (forward && tokens <= kDecodeTokens) return launch_project_decode(v, tokens, ld_v, w, ad, z, out, ld_out, stream);
   DeviceInfo info;
   const cudaError_t err = current_device_info(&info);
   if (err != cudaSuccess) return err;

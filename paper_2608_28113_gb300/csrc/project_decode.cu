@@ -1,0 +1,218 @@
+// project_decode.cu -- the packed projection for a few tokens (a decoding batch): y_t = W_hat x_t + B_a z_t.
+//
+// Bound by the weight's bytes and by unpacking them (about 2.4 instructions a weight).  tcgen05 would take
+// 128-row tiles of W through shared memory; here the unpacked weights are the A fragments of warp-level MMAs
+// (m16n8k16) in the registers they were unpacked in.  A CTA takes 16 kMT outputs and its 8 warps split K in blocks
+// of 128: a lane holds 32 consecutive nibbles of each of its rows (16 bytes, one load, the next block's ahead of the
+// present one's products).  The order of K within a block is free, so a word's nibbles are paired as they are
+// cheapest to unpack (0 with 4, 1 with 5, ...), and x is paired alike.  The warps' sums meet in
+// shared memory, in order, where each thread adds its outputs' adapter terms in fp32 and rounds once.
+#include <algorithm>
+
+#include "hscale_internal.h"
+#include "nvfp4_weight.cuh"
+#include "tma.cuh"
+#include "warp_mma.cuh"
+
+namespace hscale {
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+
+struct DecodeArgs {
+  Nvfp4Weight w;
+  Adapters ad;
+  const uint16_t* x;
+  const float* z;
+  __nv_bfloat16* y;
+  int64_t ld_x, ld_y;
+  int32_t tokens, chained;
+  bool wide;  // rows of W are 16-byte and rows of codes 2-byte aligned, n % 32 == 0
+};
+
+// Eight nibbles times a scale (bf16x2, both halves): pairs (0, 4), (1, 5), (2, 6), (3, 7).  A nibble's magnitude bits
+// at bf16's bits 8-6 read as E2M1 2^-126.
+__device__ __forceinline__ void unpack_pairs(uint32_t w, uint32_t scale, uint32_t (&r)[4]) {
+  constexpr uint32_t kSign = 0x80008000u, kMag = 0x01C001C0u;
+  r[0] = mul_bf16x2(((w << 12) & kSign) | ((w << 6) & kMag), scale);
+  r[1] = mul_bf16x2(((w << 8) & kSign) | ((w << 2) & kMag), scale);
+  r[2] = mul_bf16x2(((w << 4) & kSign) | ((w >> 2) & kMag), scale);
+  r[3] = mul_bf16x2((w & kSign) | ((w >> 6) & kMag), scale);
+}
+
+__device__ __forceinline__ void ld_16_ahead(bool on, const void* p, uint32_t (&r)[4]) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3])
+               : "l"(p), "r"((uint32_t)on));
+}
+__device__ __forceinline__ void ld_2_ahead(bool on, const void* p, uint32_t& a) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u16 %0, [%1];\n\t}"
+               : "+r"(a)
+               : "l"(p), "r"((uint32_t)on));
+}
+
+template <int kMT>
+struct Block {
+  uint32_t w[2 * kMT][4], c[2 * kMT], c1[2 * kMT];
+};
+
+template <int kMT>
+__device__ __forceinline__ void load_block(const DecodeArgs& p, int64_t row0, int64_t k, Block<kMT>& b) {
+  const int64_t n = p.w.n;
+#pragma unroll
+  for (int i = 0; i < 2 * kMT; ++i) {
+    const int64_t f = row0 + 8 * i;
+    const bool on = f < p.w.m && k < n;
+    const uint8_t* wp = p.w.packed + f * (n >> 1) + (k >> 1);
+    const uint8_t* cp = p.w.codes + f * (n >> 4) + (k >> 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b.w[i][j] = 0u;
+    b.c[i] = b.c1[i] = 0u;
+    if (p.wide) {
+      ld_16_ahead(on, wp, b.w[i]);
+      ld_2_ahead(on, cp, b.c[i]);
+    } else {
+      const bool on1 = on && k + 16 < n;
+      ld_8_ahead(on, wp, b.w[i][0], b.w[i][1]);
+      ld_1_ahead(on, cp, b.c[i]);
+      ld_8_ahead(on1, wp + 8, b.w[i][2], b.w[i][3]);
+      ld_1_ahead(on1, cp + 1, b.c1[i]);
+    }
+  }
+}
+
+template <int kMT, int kNT>
+__global__ void __launch_bounds__(kThreads, 2) project_decode_kernel(const __grid_constant__ DecodeArgs p) {
+  __shared__ float part[kWarps][8 * kNT][16 * kMT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int64_t n = p.w.n, f0 = (int64_t)blockIdx.x * (16 * kMT);
+  constexpr int kOuts = 16 * kMT * 8 * kNT;
+  // the adapters' rows that the end will need, on their way to L2
+  for (int i = threadIdx.x; i < kOuts; i += kThreads) {
+    const int t = i / (16 * kMT);
+    const int64_t f = f0 + i % (16 * kMT);
+    const int a = t < p.tokens && f < p.w.m ? adapter_of(p.ad, t) : -1;
+    if (a >= 0) {
+      const char* b = reinterpret_cast<const char*>(p.ad.b + ((int64_t)a * p.w.m + f) * p.ad.rank);
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(b));
+      if (p.ad.rank > 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(b + p.ad.rank * 2 - 2));
+    }
+  }
+  float acc[kMT][kNT][4];
+#pragma unroll
+  for (int i = 0; i < kMT; ++i)
+#pragma unroll
+    for (int j = 0; j < kNT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+
+  constexpr int64_t kStep = kWarps * 128;
+  int64_t k = (int64_t)warp * 128 + 32 * q;  // this lane's 32 of the warp's block
+  const int64_t kend = n + 32 * q;           // the block begins below n
+  Block<kMT> ring[2];
+  load_block<kMT>(p, f0 + g, k, ring[0]);
+  while (k < kend) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (k >= kend) break;
+      load_block<kMT>(p, f0 + g, k + kStep, ring[u ^ 1]);
+      Block<kMT>& b = ring[u];
+      uint32_t scale[2 * kMT];
+#pragma unroll
+      for (int i = 0; i < 2 * kMT; ++i) scale[i] = unpack_codes(b.c[i] | b.c1[i] << 8);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t xb[kNT][4];
+#pragma unroll
+        for (int j = 0; j < kNT; ++j) {
+          const int t = 8 * j + g;
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (t < p.tokens && k + 8 * i < n) v = ld_nc_v4(p.x + t * p.ld_x + k + 8 * i);
+          xb[j][0] = __byte_perm(v.x, v.z, 0x5410), xb[j][1] = __byte_perm(v.x, v.z, 0x7632);
+          xb[j][2] = __byte_perm(v.y, v.w, 0x5410), xb[j][3] = __byte_perm(v.y, v.w, 0x7632);
+        }
+#pragma unroll
+        for (int t = 0; t < kMT; ++t) {
+          uint32_t lo[4], hi[4];
+          const uint32_t pick = i < 2 ? 0x1010u : 0x3232u;
+          unpack_pairs(b.w[2 * t][i], __byte_perm(scale[2 * t], 0u, pick), lo);
+          unpack_pairs(b.w[2 * t + 1][i], __byte_perm(scale[2 * t + 1], 0u, pick), hi);
+          const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+#pragma unroll
+          for (int j = 0; j < kNT; ++j) {
+            mma_bf16(acc[t][j], a0, xb[j][0], xb[j][1]);
+            mma_bf16(acc[t][j], a1, xb[j][2], xb[j][3]);
+          }
+        }
+      }
+      k += kStep;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kMT; ++i)
+#pragma unroll
+    for (int j = 0; j < kNT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[warp][8 * j + 2 * q + (e & 1)][16 * i + 8 * (e >> 1) + g] = acc[i][j][e];
+  __syncthreads();
+  const float unit = kWeightUnit * *p.w.global_scale;
+  if (p.chained) pdl_wait_primary();  // z
+  for (int i = threadIdx.x; i < kOuts; i += kThreads) {
+    const int t = i / (16 * kMT), r = i % (16 * kMT);
+    const int64_t f = f0 + r;
+    if (t >= p.tokens || f >= p.w.m) continue;
+    float s = part[0][t][r];
+#pragma unroll
+    for (int v = 1; v < kWarps; ++v) s += part[v][t][r];
+    s *= unit;
+    const int a = adapter_of(p.ad, t);
+    if (a >= 0) {
+      const int rank = p.ad.rank;
+      const __nv_bfloat16* b = p.ad.b + ((int64_t)a * p.w.m + f) * rank;
+      const float4* z = reinterpret_cast<const float4*>(p.z + (int64_t)t * rank);
+      for (int r0 = 0; r0 < rank; r0 += 8) {
+        const uint4 h = ld_nc_v4(b + r0);
+        const float4 z0 = z[r0 / 4], z1 = z[r0 / 4 + 1];
+        s = fmaf(z0.x, bf16_lo(h.x), s), s = fmaf(z0.y, bf16_hi(h.x), s), s = fmaf(z0.z, bf16_lo(h.y), s);
+        s = fmaf(z0.w, bf16_hi(h.y), s), s = fmaf(z1.x, bf16_lo(h.z), s), s = fmaf(z1.y, bf16_hi(h.z), s);
+        s = fmaf(z1.z, bf16_lo(h.w), s), s = fmaf(z1.w, bf16_hi(h.w), s);
+      }
+    }
+    p.y[(int64_t)t * p.ld_y + f] = __float2bfloat16_rn(s);
+  }
+}
+
+template <int kMT, int kNT>
+cudaError_t launch(const DecodeArgs& p, cudaStream_t stream) {
+  auto kernel = project_decode_kernel<kMT, kNT>;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((p.w.m + 16 * kMT - 1) / (16 * kMT)), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.chained ? 1 : 0;
+  const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, p);
+  return err != cudaSuccess ? err : cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_project_decode(const void* x, int64_t tokens, int64_t ld_x, const Nvfp4Weight& w, const Adapters& ad,
+                                  const float* z, void* y, int64_t ld_y, cudaStream_t stream) {
+  DeviceInfo info;
+  const cudaError_t err = current_device_info(&info);
+  if (err != cudaSuccess) return err;
+  DecodeArgs p = {};
+  p.w = w, p.ad = ad, p.x = static_cast<const uint16_t*>(x), p.z = z, p.y = static_cast<__nv_bfloat16*>(y);
+  p.ld_x = ld_x, p.ld_y = ld_y, p.tokens = (int32_t)tokens, p.chained = ad.count > 0;
+  p.wide = w.n % 32 == 0 && reinterpret_cast<uintptr_t>(w.packed) % 16 == 0 && reinterpret_cast<uintptr_t>(w.codes) % 2 == 0;
+  // 32 outputs a CTA (x is read once for them) where that fills the SMs twice, else 16
+  const bool two = (w.m + 31) / 32 >= 2 * info.sm_count;
+  if (tokens <= 8) return two ? launch<2, 1>(p, stream) : launch<1, 1>(p, stream);
+  return two ? launch<2, 2>(p, stream) : launch<1, 2>(p, stream);
+}
+
+}  // namespace hscale
