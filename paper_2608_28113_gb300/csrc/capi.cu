@@ -469,7 +469,7 @@ int hscale_project(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, 
   float* z = static_cast<float*>(workspace);
   cudaStream_t s = as_stream(stream);
   if (adapters > 0) {
-    const cudaError_t err = hscale::launch_adapter_down(x_bf16, ld_x, nullptr, 0, tokens, n, ad, z, s);
+    const cudaError_t err = hscale::launch_adapter_down(x_bf16, ld_x, tokens, n, ad, z, s);
     if (err != cudaSuccess) return HSCALE_ERR_CUDA;
   }
   return from_cuda(hscale::launch_project(true, x_bf16, tokens, ld_x, w, ad, z, y_bf16, ld_y, s));
@@ -511,13 +511,14 @@ int hscale_project_backward(const void* dy_bf16, int64_t tokens, int64_t m, int6
   float* z = static_cast<float*>(workspace);
   float* dz = z + need / 8;
   cudaError_t err = cudaSuccess;
-  if (adapters > 0) err = hscale::launch_adapter_up_t(dy_bf16, ld_dy, tokens, m, ad, dz, s);
-  if (err == cudaSuccess && dx_bf16 != nullptr) err = hscale::launch_project(false, dy_bf16, tokens, ld_dy, w, ad, dz, dx_bf16, ld_dx, s);
-  if (err == cudaSuccess && grads && da_bf16 != nullptr) err = hscale::launch_adapter_grad_a(x, x_format, tokens, n, ad, dz, da_bf16, s);
-  if (err == cudaSuccess && grads && db_bf16 != nullptr) {
-    err = hscale::launch_adapter_down(nullptr, 0, &x, x_format, tokens, n, ad, z, s);
-    if (err == cudaSuccess) err = hscale::launch_adapter_grad_b(dy_bf16, ld_dy, tokens, m, ad, z, db_bf16, s);
-  }
+  const bool want_dz = adapters > 0 && (dx_bf16 != nullptr || da_bf16 != nullptr), want_z = grads && db_bf16 != nullptr;
+  if (want_dz || want_z)
+    err = hscale::launch_adapter_backward(x, x_format, n, dy_bf16, ld_dy, m, tokens, ad, want_z ? z : nullptr,
+                                          want_dz ? dz : nullptr, s);
+  if (err == cudaSuccess && dx_bf16 != nullptr)
+    err = hscale::launch_project(false, dy_bf16, tokens, ld_dy, w, ad, dz, dx_bf16, ld_dx, s);
+  if (err == cudaSuccess && grads)
+    err = hscale::launch_adapter_gradients(x, x_format, n, dy_bf16, ld_dy, m, tokens, ad, z, dz, da_bf16, db_bf16, s);
   return from_cuda(err);
 }
 

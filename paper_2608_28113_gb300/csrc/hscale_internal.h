@@ -131,17 +131,16 @@ cudaError_t launch_checkpoint_save(const void* x, int64_t tokens, int64_t n, int
                                    int64_t ld_codes, uint8_t* scales, int64_t ld_scales, cudaStream_t stream);
 cudaError_t launch_checkpoint_load(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales,
                                    int64_t tokens, int64_t n, int format, void* x, int64_t ld_x, cudaStream_t stream);
-// z[t] = alpha_a A_a x_t of bf16 rows x (ckpt == nullptr) or of a checkpoint's; fp32 [tokens, rank].
-cudaError_t launch_adapter_down(const void* x, int64_t ld_x, const Checkpoint* ckpt, int format, int64_t tokens,
-                                int64_t n, const Adapters& ad, float* z, cudaStream_t stream);
-// dz[t] = alpha_a B_a^T dy_t.
-cudaError_t launch_adapter_up_t(const void* dy, int64_t ld_dy, int64_t tokens, int64_t m, const Adapters& ad, float* dz,
+// z[t] = alpha_a A_a x_t; fp32 [tokens, rank].
+cudaError_t launch_adapter_down(const void* x, int64_t ld_x, int64_t tokens, int64_t n, const Adapters& ad, float* z,
                                 cudaStream_t stream);
-// dA_a = sum dz_t x_t^T and dB_a = sum dy_t z_t^T over the tokens of each adapter.
-cudaError_t launch_adapter_grad_a(const Checkpoint& ckpt, int format, int64_t tokens, int64_t n, const Adapters& ad,
-                                  const float* dz, void* da, cudaStream_t stream);
-cudaError_t launch_adapter_grad_b(const void* dy, int64_t ld_dy, int64_t tokens, int64_t m, const Adapters& ad,
-                                  const float* z, void* db, cudaStream_t stream);
+// z[t] of a checkpoint's x, and dz[t] = alpha_a B_a^T dy_t; either may be nullptr.
+cudaError_t launch_adapter_backward(const Checkpoint& x, int format, int64_t n, const void* dy, int64_t ld_dy, int64_t m,
+                                    int64_t tokens, const Adapters& ad, float* z, float* dz, cudaStream_t stream);
+// dA_a = sum dz_t x_t^T and dB_a = sum dy_t z_t^T over the tokens of each adapter; either may be nullptr.
+cudaError_t launch_adapter_gradients(const Checkpoint& x, int format, int64_t n, const void* dy, int64_t ld_dy, int64_t m,
+                                     int64_t tokens, const Adapters& ad, const float* z, const float* dz, void* da, void* db,
+                                     cudaStream_t stream);
 // out = W_hat v (forward: v [tokens, n], out [tokens, m]) or W_hat^T v (v [tokens, m], out [tokens, n]),
 // plus each token's adapter applied to z.
 cudaError_t launch_project(bool forward, const void* v, int64_t tokens, int64_t ld_v, const Nvfp4Weight& w,

@@ -44,6 +44,11 @@ __device__ __forceinline__ void ld_32_ahead(bool on, const void* p, uint32_t (&r
                : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
                : "l"(p), "r"((uint32_t)on));
 }
+__device__ __forceinline__ void ld_16_ahead(bool on, const void* p, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+               : "+r"(a), "+r"(b), "+r"(c), "+r"(d)
+               : "l"(p), "r"((uint32_t)on));
+}
 __device__ __forceinline__ void ld_8_ahead(bool on, const void* p, uint32_t& a, uint32_t& b) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\t@p ld.global.nc.v2.u32 {%0, %1}, [%2];\n\t}"
                : "+r"(a), "+r"(b)
@@ -51,6 +56,11 @@ __device__ __forceinline__ void ld_8_ahead(bool on, const void* p, uint32_t& a, 
 }
 __device__ __forceinline__ void ld_4_ahead(bool on, const void* p, uint32_t& a) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u32 %0, [%1];\n\t}"
+               : "+r"(a)
+               : "l"(p), "r"((uint32_t)on));
+}
+__device__ __forceinline__ void ld_2_ahead(bool on, const void* p, uint32_t& a) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u16 %0, [%1];\n\t}"
                : "+r"(a)
                : "l"(p), "r"((uint32_t)on));
 }

@@ -40,17 +40,6 @@ __device__ __forceinline__ void unpack_pairs(uint32_t w, uint32_t scale, uint32_
   r[3] = mul_bf16x2((w & kSign) | ((w >> 6) & kMag), scale);
 }
 
-__device__ __forceinline__ void ld_16_ahead(bool on, const void* p, uint32_t (&r)[4]) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3])
-               : "l"(p), "r"((uint32_t)on));
-}
-__device__ __forceinline__ void ld_2_ahead(bool on, const void* p, uint32_t& a) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p ld.global.nc.u16 %0, [%1];\n\t}"
-               : "+r"(a)
-               : "l"(p), "r"((uint32_t)on));
-}
-
 template <int kMT>
 struct Block {
   uint32_t w[2 * kMT][4], c[2 * kMT], c1[2 * kMT];
@@ -69,7 +58,7 @@ __device__ __forceinline__ void load_block(const DecodeArgs& p, int64_t row0, in
     for (int j = 0; j < 4; ++j) b.w[i][j] = 0u;
     b.c[i] = b.c1[i] = 0u;
     if (p.wide) {
-      ld_16_ahead(on, wp, b.w[i]);
+      ld_16_ahead(on, wp, b.w[i][0], b.w[i][1], b.w[i][2], b.w[i][3]);
       ld_2_ahead(on, cp, b.c[i]);
     } else {
       const bool on1 = on && k + 16 < n;
