@@ -65,61 +65,57 @@ struct Rows {
   int64_t ld;
   Checkpoint ckpt;
   int64_t cols;
-  int vec;  // checkpoint: codes that may be copied at once (16, 8 or 1)
+  int vec;     // checkpoint: codes that may be copied at once (16, 8 or 1)
+  bool words;  // checkpoint: the scales of 4 blocks may be copied at once
 
-  // elements [k, k + 8) of row t to dst (16 bytes of bf16, 8 codes), zeros past the end of the row; k % 8 == 0
-  __device__ __forceinline__ void copy(uint8_t* dst, int64_t t, int64_t k, bool on) const {
-    on = on && k < cols;
+  static constexpr int kElement = kFormat < 0 ? 2 : 1;  // bytes
+  __device__ __forceinline__ const uint8_t* row(int64_t t) const {
+    return kFormat < 0 ? reinterpret_cast<const uint8_t*>(x + t * ld) : ckpt.codes + t * ckpt.ld_codes;
+  }
+  __device__ __forceinline__ const uint8_t* scale_row(int64_t t) const { return ckpt.scales + t * ckpt.ld_scales; }
+  // elements [k, k + 8) of a row: how many bytes of them there are (0 where `on` is false)
+  __device__ __forceinline__ int bytes(int64_t k, bool on) const {
+    return on && k < cols ? (int)min((int64_t)8, cols - k) * kElement : 0;
+  }
+  // those elements to dst (16 bytes of bf16, 8 codes), zeros past the end; k % 8 == 0 and inside the row
+  __device__ __forceinline__ void copy(uint8_t* dst, const uint8_t* row, int64_t k, int bytes) const {
     if constexpr (kFormat < 0) {
-      copy_16(dst, on ? x + t * ld + k : x, on ? (int)min((int64_t)16, (cols - k) * 2) : 0);
+      copy_16(dst, row + k * 2, bytes);
+    } else if (vec >= 8) {
+      copy_8(dst, row + k, bytes);
     } else {
-      const uint8_t* p = on ? ckpt.codes + t * ckpt.ld_codes + k : ckpt.codes;
-      if (vec >= 8) {
-        copy_8(dst, p, on ? 8 : 0);  // cols % 16 == 0
-      } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dst[j] = on ? __ldg(p + j) : (uint8_t)0;
-      }
+      for (int j = 0; j < 8; ++j) dst[j] = j < bytes ? __ldg(row + k + j) : (uint8_t)0;
     }
   }
-  __device__ __forceinline__ uint32_t scale(int64_t t, int64_t k, bool on) const {
-    uint32_t r = 0u;
-    if (kFormat >= 0) ld_1_ahead(on && k < cols, ckpt.scales + t * ckpt.ld_scales + k / kCkptBlock, r);
-    return r;
+  // the scale byte of element k's block, in the word at dst: byte number scale_at(k)
+  __device__ __forceinline__ void copy_scale(uint8_t* dst, const uint8_t* scale_row, int64_t k, bool on) const {
+    const int64_t block = k / kCkptBlock;
+    if (words) {
+      copy_4(dst, scale_row + (block & ~(int64_t)3), on ? 4 : 0);
+    } else {
+      *reinterpret_cast<uint32_t*>(dst) = on ? (uint32_t)__ldg(scale_row + block) << (8 * (block & 3)) : 0u;
+    }
+  }
+  static __device__ __forceinline__ uint32_t scale_of(uint32_t word, int64_t k) {
+    return ckpt_scale((word >> (8 * ((uint32_t)(k / kCkptBlock) & 3u))) & 0xFFu);
   }
   // A lane's two groups of 8 of the block of 64 elements from kb, for q = 0 .. 3: where they begin
   static __device__ __forceinline__ int64_t group(int64_t kb, int q, int h) {
     return kFormat < 0 ? kb + 32 * h + 8 * q : kb + 16 * q + 8 * h;
   }
-  // both groups: two slots of bf16, one of codes
-  static constexpr int kSlots = kFormat < 0 ? 2 : 1;
+  // group h of a pair (two slots of bf16, one of codes) as 4 x bf16x2; a checkpoint's values are exact in bf16
   static constexpr int kSlotStep = 512;  // a lane's next slot
-  __device__ __forceinline__ void copy_pair(uint8_t* dst, int64_t t, int64_t kb, int q) const {
-    if constexpr (kFormat < 0) {
-      copy(dst, t, group(kb, q, 0), true);
-      copy(dst + kSlotStep, t, group(kb, q, 1), true);
-    } else {
-      const int64_t k = group(kb, q, 0);
-      if (vec == 16) {
-        copy_16(dst, k < cols ? ckpt.codes + t * ckpt.ld_codes + k : ckpt.codes, k < cols ? 16 : 0);
-      } else {
-        copy(dst, t, k, true);
-        copy(dst + 8, t, k + 8, true);
-      }
-    }
-  }
-  // group h of a pair as 4 x bf16x2; a checkpoint's values are exact in bf16
-  static __device__ __forceinline__ uint4 values_of(const uint8_t* src, int h, uint32_t byte) {
+  static __device__ __forceinline__ uint4 values_of(const uint8_t* src, int h, uint32_t scale) {
     if constexpr (kFormat < 0) {
       return *reinterpret_cast<const uint4*>(src + h * kSlotStep);
     } else {
-      return values(*reinterpret_cast<const uint2*>(src + 8 * h), byte);
+      return values(*reinterpret_cast<const uint2*>(src + 8 * h), scale);
     }
   }
-  static __device__ __forceinline__ uint4 values(uint2 v, uint32_t byte) {
-    const float s = ckpt_scale(byte);
-    return make_uint4(ckpt_values<kFormat>(v.x, s), ckpt_values<kFormat>(v.x >> 16, s), ckpt_values<kFormat>(v.y, s),
-                      ckpt_values<kFormat>(v.y >> 16, s));
+  static __device__ __forceinline__ uint4 values(uint2 v, uint32_t scale) {
+    return make_uint4(ckpt_values<kFormat, 0>(v.x, scale), ckpt_values<kFormat, 1>(v.x, scale),
+                      ckpt_values<kFormat, 0>(v.y, scale), ckpt_values<kFormat, 1>(v.y, scale));
   }
 };
 
@@ -139,29 +135,38 @@ struct Split {
 };
 constexpr int kDepth = 2;  // two CTAs an SM fit
 template <int kMT, int kNT>
-constexpr int ring_bytes() {  // of a warp: the slots of kDepth blocks
+constexpr int ring_bytes() {  // of a warp: the slots of kDepth blocks (16 bytes a lane each)
   return kDepth * (4 * kMT + 2 * kNT) * 512;
 }
 template <int kFormat, bool kDown, int kMT, int kTG, int kNT>
 __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t tokens, const Adapters& ad, float* z,
                                             int64_t tile, const Split& sp, float* part, float* mark, uint8_t* rings) {
   constexpr int kGroup = 16 * kMT, kTok = kTG * kGroup, kSplits = kWarps / kTG;
-  constexpr int kPair = Rows<kFormat>::kSlots * 512, kX = 2 * kMT * kPair, kBlock = kX + 2 * kNT * 512;
+  // a row's slots of a block: bf16 two; a checkpoint one of codes, and for all rows together kMT / 2 of scale words
+  constexpr int kPair = kFormat < 0 ? 1024 : 512, kScales = kFormat < 0 ? 0 : 512, kX = 2 * kMT * kPair + kScales;
+  constexpr int kBlock = kX + 2 * kNT * 512;
+  static_assert(kDepth * kBlock <= ring_bytes<kMT, kNT>(), "a ring's room");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int tg = warp % kTG, split = warp / kTG;
-  const int64_t t0 = tile * kTok, tw = t0 + tg * kGroup;
+  const int64_t t0 = tile * kTok, tw = t0 + tg * kGroup, cols = rows.cols;
   const int rank = ad.rank;
   const int mine = lane < kGroup && tw + lane < tokens ? adapter_of(ad, tw + lane) : -1;
-  const __nv_bfloat16* factors = kDown ? ad.a : ad.b;
   uint8_t* ring = rings + warp * ring_bytes<kMT, kNT>() + lane * 16;
-  int64_t trow[2 * kMT];  // rows past the end are read as the last one; their results have no adapter
+  const uint8_t *trow[2 * kMT], *srow[2 * kMT];  // rows past the end are read as the last one; their results have no adapter
 #pragma unroll
-  for (int i = 0; i < 2 * kMT; ++i) trow[i] = min(tw + 8 * i + g, tokens - 1);
+  for (int i = 0; i < 2 * kMT; ++i) {
+    const int64_t t = min(tw + 8 * i + g, tokens - 1);
+    trow[i] = rows.row(t), srow[i] = rows.scale_row(t);
+  }
   // this warp's blocks of 64: first, first + ways, ...: `count` of them, taken from a place of its own on
-  const int ways = kSplits * sp.csize, blocks = (int)((rows.cols + 63) / 64);
+  const int ways = kSplits * sp.csize, blocks = (int)((cols + 63) / 64);
   const int first = (int)((sp.crank * kSplits + split + tile) % ways);
   const int count = first < blocks ? (blocks - first + ways - 1) / ways : 0;
   const int lead = count > 0 ? (int)((tile / ways) % count) : 0;
+  const auto block_at = [&](int i) {
+    const int at = i + lead;
+    return (int64_t)(first + (at < count ? at : at - count) * ways) * 64;
+  };
   float* out = part + (split * kTok + tg * kGroup) * rank;
   uint32_t left = __ballot_sync(0xFFFFFFFFu, mine >= 0);
   for (int nth = 0; left; ++nth) {
@@ -177,57 +182,66 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
         for (int j = 0; j < kNT; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-      const auto block_at = [&](int i) {
-        const int at = i + lead;
-        return (int64_t)(first + (at < count ? at : at - count) * ways) * 64;
-      };
-      uint32_t byte[2 * kMT];  // the next block's scales
+      // kDown: this lane's row of A's first tile of 8 ranks; else its first row of B, from its ranks on
+      const __nv_bfloat16* factors = kDown ? ad.a + ((int64_t)a * rank + min(r0 + g, rank - 1)) * cols
+                                           : ad.b + ((int64_t)a * cols) * rank + min(r0 + 2 * q, rank - 2);
       const auto fetch = [&](int i) {
         if (i < count) {
           const int64_t kb = block_at(i);
-          uint8_t* dst = ring + i % kDepth * kBlock;
+          uint8_t* dst = ring + (i & (kDepth - 1)) * kBlock;
+          const int64_t k[2] = {Rows<kFormat>::group(kb, q, 0), Rows<kFormat>::group(kb, q, 1)};
+          const int64_t kin[2] = {min(k[0], cols - 1) & ~(int64_t)7, min(k[1], cols - 1) & ~(int64_t)7};  // inside the row
+          const int have[2] = {rows.bytes(k[0], true), rows.bytes(k[1], true)};
 #pragma unroll
-          for (int t = 0; t < 2 * kMT; ++t) rows.copy_pair(dst + t * kPair, trow[t], kb, q);
+          for (int t = 0; t < 2 * kMT; ++t) {
+            uint8_t* slot = dst + t * kPair;
+            if constexpr (kFormat < 0) {
+              rows.copy(slot, trow[t], kin[0], have[0]);
+              rows.copy(slot + 512, trow[t], kin[1], have[1]);
+            } else {
+              if (rows.vec == 16) {
+                copy_16(slot, trow[t] + (kin[0] & ~(int64_t)15), have[0] + have[1]);  // cols % 16 == 0
+              } else {
+                rows.copy(slot, trow[t], kin[0], have[0]);
+                rows.copy(slot + 8, trow[t], kin[1], have[1]);
+              }
+              rows.copy_scale(dst + 2 * kMT * kPair + 4 * t, srow[t], kin[0], have[0] > 0);
+            }
+          }
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int j = 0; j < kNT; ++j) {
               uint8_t* slot = dst + kX + (h * kNT + j) * 512;
-              if (kDown) {
-                const int64_t k = Rows<kFormat>::group(kb, q, h);
-                const int r = r0 + 8 * j + g;
-                const bool on = r < rank && k < rows.cols;
-                copy_16_l1(slot, on ? factors + ((int64_t)a * rank + r) * rows.cols + k : factors, on ? 16 : 0);
+              if constexpr (kDown) {  // cols % 16 == 0
+                const bool on = r0 + 8 * j + g < rank && have[h] > 0;
+                copy_16_l1(slot, factors + (on ? (int64_t)(8 * j) * cols : 0) + kin[h], on ? 16 : 0);
               } else {
                 // register u of the fragment: slots 2 q', 2 q' + 1 are elements 8 q' + 2 u, + 1
-                const int r = r0 + 8 * j + 2 * q;
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                  const int64_t k = kb + 32 * h + (g >> 1) * 8 + 2 * u + (g & 1);
-                  const bool on = r < rank && k < rows.cols;
-                  copy_4(slot + 4 * u, on ? factors + ((int64_t)a * rows.cols + k) * rank + r : factors, on ? 4 : 0);
+                  const int64_t kk = kb + 32 * h + (g >> 1) * 8 + 2 * u + (g & 1);
+                  const bool on = r0 + 8 * j + 2 * q < rank && kk < cols;
+                  copy_4(slot + 4 * u, factors + (on ? kk * rank + 8 * j : 0), on ? 4 : 0);
                 }
               }
             }
         }
         copies_end();
       };
-      const auto fetch_scales = [&](int i) {
-#pragma unroll
-        for (int t = 0; t < 2 * kMT; ++t)
-          byte[t] = rows.scale(trow[t], Rows<kFormat>::group(i < count ? block_at(i) : 0, q, 0), i < count);
-      };
 #pragma unroll
       for (int i = 0; i < kDepth - 1; ++i) fetch(i);
-      if (kFormat >= 0) fetch_scales(0);
       for (int it = 0; it < count; ++it) {
         fetch(it + kDepth - 1);
-        uint32_t now[2 * kMT];
-#pragma unroll
-        for (int t = 0; t < 2 * kMT; ++t) now[t] = kFormat >= 0 ? byte[t] : 0u;
-        if (kFormat >= 0) fetch_scales(it + 1);
         copies_wait<kDepth - 1>();
-        const uint8_t* src = ring + it % kDepth * kBlock;
+        const uint8_t* src = ring + (it & (kDepth - 1)) * kBlock;
+        uint32_t scale[2 * kMT];
+        if constexpr (kFormat >= 0) {
+          const int64_t k = Rows<kFormat>::group(block_at(it), q, 0);
+#pragma unroll
+          for (int t = 0; t < 2 * kMT; ++t)
+            scale[t] = Rows<kFormat>::scale_of(*reinterpret_cast<const uint32_t*>(src + 2 * kMT * kPair + 4 * t), min(k, cols - 1));
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint4 w[kNT];
@@ -238,8 +252,8 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
           }
 #pragma unroll
           for (int i = 0; i < kMT; ++i) {
-            const uint4 lo = Rows<kFormat>::values_of(src + 2 * i * kPair, h, now[2 * i]);
-            const uint4 hi = Rows<kFormat>::values_of(src + (2 * i + 1) * kPair, h, now[2 * i + 1]);
+            const uint4 lo = Rows<kFormat>::values_of(src + 2 * i * kPair, h, scale[2 * i]);
+            const uint4 hi = Rows<kFormat>::values_of(src + (2 * i + 1) * kPair, h, scale[2 * i + 1]);
             const uint32_t a0[4] = {lo.x, hi.x, lo.y, hi.y}, a1[4] = {lo.z, hi.z, lo.w, hi.w};
 #pragma unroll
             for (int j = 0; j < kNT; ++j) {
@@ -367,29 +381,49 @@ cudaError_t launch_shrink(const Rows<kFormat>& x, const Rows<-1>& dy, const Shri
 }
 
 // ---------------------------------------------------------------- dA and dB
-// A CTA (of a cluster of csize that splits the tokens) takes 64 columns of one adapter's gradient and all of
-// the adapter's tokens, 16 at a time and warp, kUnits such units in flight.  As an MMA: M = ranks (z or dz transposed, as a
-// pair hi + lo of bf16 numbers: 2^-17 of a value is lost), N = columns, K = tokens.  A lane loads 8 columns of four
-// tokens and pairs the tokens' halves up into the fragments of 8 column tiles.  The adapter's tokens are found in windows
-// of kWindow: the CTA scans their adapters and lists its own, in order, so an adapter without tokens gets
-// zeros and the sums' order does not depend on anything but the tokens'.
+// A CTA takes 256 columns of one adapter's gradient and the adapter's tokens, in chunks of 128 that the CTAs of a
+// cluster of csize take in turn; 64 columns a warp, kSub sets of four warps that take a chunk's units of 16 tokens in
+// turn.  As an MMA: M = ranks (z or dz transposed, as a pair hi + lo of bf16 numbers: 2^-17 of a value is lost),
+// N = columns, K = tokens.
+//   * The rows: a lane copies 8 columns of four tokens of a unit into its own ring, kUnits units ahead, and pairs
+//     the tokens' halves up into the fragments of 8 column tiles.
+//   * z and a checkpoint's scales are the same for all warps: the CTA copies the next chunk's while it works on the
+//     present one, and turns z into A fragments once, which the warps then read (copied and split by each warp for
+//     itself they took a third of the kernel's time).
+// The adapter's tokens are found in windows of kWindow: the CTA scans their adapters and lists its own, in order, so an
+// adapter without tokens gets zeros and the sums' order does not depend on anything but the tokens'.
 constexpr int kUnits = 3;
-constexpr int kWindow = 4096;
+constexpr int kWindow = 4096, kChunk = 128;
+constexpr int kColumns = 256, kPitch = kColumns + 2;
 struct GradShared {
   uint16_t list[kWindow];
-  int counts[kWarps];
+  int counts[16];
+  alignas(16) uint8_t scales[2][kChunk][8];
 };
-
+// Ranks / 16 of a pass and the sets of warps: 64 ranks take the registers of two sets.
 template <int kRT>
-constexpr int unit_bytes() { return 2048 + kRT * 1024; }
+constexpr int grad_sets() { return kRT == 4 ? 2 : 4; }
+constexpr int kUnitBytes = 2048;  // of rows, in a warp's ring
+template <int kRT>
+constexpr int frag_bytes() { return kChunk / 16 * kRT * 1024; }       // of a chunk: hi and lo, 16 bytes a lane each
+template <int kRT>
+constexpr int zrow_floats() { return 16 * kRT + 4; }                  // a token's z as copied
+template <int kRT>
+constexpr int grad_smem_bytes() {
+  return 4 * grad_sets<kRT>() * kUnits * kUnitBytes + 2 * frag_bytes<kRT>() + kChunk * zrow_floats<kRT>() * 4;
+}
 
 template <int kFormat, bool kRankMajor, int kRT>
 __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tokens, const Adapters& ad, const float* z,
                                           __nv_bfloat16* out, int64_t col0, int a, int r0, int csize, int crank,
-                                          float* part, uint8_t* rings, GradShared& sh) {
+                                          uint8_t* smem, GradShared& sh) {
+  constexpr int kSub = grad_sets<kRT>(), kWarpsG = 4 * kSub, kThreadsG = 32 * kWarpsG;
+  constexpr int kTurns = kChunk / 16 / kSub;  // a warp's units of a chunk
+  constexpr int kZRow = zrow_floats<kRT>();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int sub = warp >> 2;
   const int rank = ad.rank;
-  const int64_t col = col0 + 8 * g;
+  const int64_t cols = rows.cols;
   float acc[kRT][8][4];
 #pragma unroll
   for (int i = 0; i < kRT; ++i)
@@ -397,19 +431,21 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
     for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-
-  // the warp's ring: a unit of 16 tokens is four slots of rows and 8 kRT words of z a lane
-  constexpr int kRow = kFormat < 0 ? 512 : 256, kUnit = 4 * kRow + kRT * 1024;
-  static_assert(kUnit <= unit_bytes<kRT>(), "a unit's place");
-  uint8_t* ring = rings + warp * kUnits * unit_bytes<kRT>();
-  uint8_t* ring_x = ring + lane * (kRow / 32);
-  uint8_t* ring_z = ring + 4 * kRow + lane * 16;
+  // the lane's 8 columns: bytes of them inside the rows, and a place inside
+  const int64_t col = col0 + 64 * (warp & 3) + 8 * g;
+  const int64_t colin = min(col, cols - 1) & ~(int64_t)7;
+  const int colbytes = rows.bytes(col, true);
+  const int block = (int)((colin - col0) / kCkptBlock) & 7;  // a column past the end may take any scale
+  constexpr int kRow = kFormat < 0 ? 512 : 256;
+  uint8_t* ring = smem + warp * kUnits * kUnitBytes + lane * (kRow / 32);
+  uint8_t* frags = smem + kWarpsG * kUnits * kUnitBytes;
+  float* zraw = reinterpret_cast<float*>(frags + 2 * frag_bytes<kRT>());
   for (int64_t w0 = 0; w0 < tokens; w0 += kWindow) {
     int have = (int)min((int64_t)kWindow, tokens - w0);
     if (ad.of_token != nullptr) {
       // warp w lists tokens [w span, ..) of the window behind the warps' before it
-      constexpr int kSpan = kWindow / kWarps;
-      const int span = ((have + kWarps - 1) / kWarps + 31) & ~31;
+      constexpr int kSpan = kWindow / kWarpsG;
+      const int span = ((have + kWarpsG - 1) / kWarpsG + 31) & ~31;
       __syncthreads();
       uint32_t own[kSpan / 32];
       int count = 0;
@@ -424,7 +460,7 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
       __syncthreads();
       int at = 0;
       have = 0;
-      for (int v = 0; v < kWarps; ++v) {
+      for (int v = 0; v < kWarpsG; ++v) {
         if (v == warp) at = have;
         have += sh.counts[v];
       }
@@ -436,92 +472,114 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
       }
       __syncthreads();
     }
-    const int units = (have + 15) >> 4;
-    const int first = crank * kWarps + warp, stride = csize * kWarps;
-    const auto token = [&](int u, int i, bool& on) {  // slots 2 q, 2 q + 1, 2 q + 8, 2 q + 9
-      const int e = 16 * u + 2 * q + (i & 1) + 8 * (i >> 1);
-      on = e < have;
-      return w0 + (on ? (ad.of_token != nullptr ? (int)sh.list[e] : e) : 0);
+    const int all = (have + kChunk - 1) / kChunk, chunks = all > crank ? (all - 1 - crank) / csize + 1 : 0;
+    const auto token = [&](int e) { return w0 + (e < have ? (ad.of_token != nullptr ? (int)sh.list[e] : e) : 0); };
+    // z and scales of this CTA's chunk c
+    const auto fetch_chunk = [&](int c) {
+      const int e0 = (crank + c * csize) * kChunk;
+      for (int i = threadIdx.x; i < kChunk * 4 * kRT; i += kThreadsG) {
+        const int e = e0 + i / (4 * kRT), r = 4 * (i % (4 * kRT));
+        const bool on = e < have && r0 + r < rank;
+        copy_16(zraw + i / (4 * kRT) * kZRow + r, z + token(e) * rank + (on ? r0 + r : 0), on ? 16 : 0);
+      }
+      if constexpr (kFormat >= 0) {
+        const int64_t first = col0 / kCkptBlock, last = (cols + kCkptBlock - 1) / kCkptBlock;
+        for (int i = threadIdx.x; i < kChunk * 2; i += kThreadsG) {
+          const int e = e0 + i / 2, b = 4 * (i % 2);
+          const uint8_t* src = rows.scale_row(token(e)) + first;
+          uint8_t* dst = &sh.scales[c & 1][i / 2][b];
+          if (rows.words) {
+            const bool on = e < have && first + b < last;
+            copy_4(dst, on ? src + b : rows.ckpt.scales, on ? 4 : 0);
+          } else {
+            for (int k = 0; k < 4; ++k) dst[k] = e < have && first + b + k < last ? __ldg(src + b + k) : (uint8_t)0;
+          }
+        }
+      }
     };
-    const auto fetch = [&](int u, int stage) {
-      if (u < units) {
+    // rows of this warp's k-th unit
+    const auto fetch_rows = [&](int k, int stage) {
+      if (k < chunks * kTurns) {
+        const int e0 = (crank + k / kTurns * csize) * kChunk + (sub + k % kTurns * kSub) * 16 + 2 * q;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          bool on;
-          const int64_t t = token(u, i, on);
-          rows.copy(ring_x + stage * unit_bytes<kRT>() + i * kRow, t, col, on);
-#pragma unroll
-          for (int m = 0; m < kRT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int r = r0 + 16 * m + 8 * h + g;
-              const bool have_z = on && r < rank;
-              copy_4(ring_z + stage * unit_bytes<kRT>() + (m * 2 + h) * 512 + 4 * i, have_z ? z + t * rank + r : z, have_z ? 4 : 0);
-            }
+          const int e = e0 + (i & 1) + 8 * (i >> 1);  // slots 2 q, 2 q + 1, 2 q + 8, 2 q + 9
+          rows.copy(ring + stage * kUnitBytes + i * kRow, rows.row(token(e)), colin, e < have ? colbytes : 0);
         }
       }
       copies_end();
     };
-    uint32_t byte[4];  // the next unit's scales
-    const auto fetch_scales = [&](int u) {
+    if (chunks > 0) fetch_chunk(0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bool on = false;
-        const int64_t t = u < units ? token(u, i, on) : 0;
-        byte[i] = rows.scale(t, col, on);
-      }
-    };
+    for (int i = 0; i < kUnits - 1; ++i) fetch_rows(i, i);
+    int stage = 0, k = 0;
+    for (int c = 0; c < chunks; ++c) {
+      // chunk c's copies are older than the latest kUnits - 2 units' (the first chunk's came with the first unit's)
+      copies_wait<kUnits - 2>();
+      __syncthreads();
+      uint8_t* frag = frags + (c & 1) * frag_bytes<kRT>();
+      for (int i = threadIdx.x; i < kChunk / 16 * kRT * 32; i += kThreadsG) {
+        // unit i / (32 kRT), ranks 16 m .., as this lane of the warps will read them: rows fg | fg + 8, slots
+        // (2 fq, 2 fq + 1) | (2 fq + 8, 2 fq + 9)
+        const int l = i & 31, m = i / 32 % kRT, u = i / (32 * kRT), fg = l >> 2, fq = l & 3;
+        const float* src = zraw + (16 * u + 2 * fq) * kZRow + 16 * m + fg;
+        uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int i = 0; i < kUnits - 1; ++i) fetch(first + i * stride, i);
-    if (kFormat >= 0) fetch_scales(first);
-    int stage = 0;
-    for (int u = first; u < units; u += stride) {
-      fetch(u + (kUnits - 1) * stride, stage == 0 ? kUnits - 1 : stage - 1);
-      uint32_t now[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) now[i] = kFormat >= 0 ? byte[i] : 0u;
-      if (kFormat >= 0) fetch_scales(u + stride);
-      copies_wait<kUnits - 1>();
-      uint32_t v[4][4], hi[kRT][4], lo[kRT][4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint4 x;
-        if constexpr (kFormat < 0)
-          x = *reinterpret_cast<const uint4*>(ring_x + stage * unit_bytes<kRT>() + i * kRow);
-        else
-          x = Rows<kFormat>::values(*reinterpret_cast<const uint2*>(ring_x + stage * unit_bytes<kRT>() + i * kRow), now[i]);
-        v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
-      }
-#pragma unroll
-      for (int i = 0; i < kRT; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float4 zq = *reinterpret_cast<const float4*>(ring_z + stage * unit_bytes<kRT>() + (i * 2 + h) * 512);
-          const float zv[4] = {zq.x, zq.y, zq.z, zq.w};
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
-            // rows g | g + 8, slots (2 q, 2 q + 1) | (2 q + 8, 2 q + 9)
-            const uint32_t p = pack_bf16(zv[2 * s], zv[2 * s + 1]);
-            hi[i][2 * s + h] = p;
-            lo[i][2 * s + h] = pack_bf16(zv[2 * s] - bf16_lo(p), zv[2 * s + 1] - bf16_hi(p));
+            const float z0 = src[8 * s * kZRow + 8 * h], z1 = src[(8 * s + 1) * kZRow + 8 * h];
+            const uint32_t p = pack_bf16(z0, z1);
+            hi[2 * s + h] = p;
+            lo[2 * s + h] = pack_bf16(z0 - bf16_lo(p), z1 - bf16_hi(p));
+          }
+        uint4* dst = reinterpret_cast<uint4*>(frag) + (u * kRT + m) * 64 + l;
+        dst[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        dst[32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+      __syncthreads();
+      if (c + 1 < chunks) fetch_chunk(c + 1);
+      for (int turn = 0; turn < kTurns; ++turn, ++k) {
+        fetch_rows(k + kUnits - 1, stage == 0 ? kUnits - 1 : stage - 1);
+        copies_wait<kUnits - 1>();
+        const int u = sub + turn * kSub;
+        if ((crank + c * csize) * kChunk + 16 * u < have) {
+          uint32_t v[4][4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint8_t* src = ring + stage * kUnitBytes + i * kRow;
+            uint4 x;
+            if constexpr (kFormat < 0) {
+              x = *reinterpret_cast<const uint4*>(src);
+            } else {
+              const uint32_t byte = sh.scales[c & 1][16 * u + 2 * q + (i & 1) + 8 * (i >> 1)][block];
+              x = Rows<kFormat>::values(*reinterpret_cast<const uint2*>(src), ckpt_scale(byte));
+            }
+            v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
+          }
+          const uint4* fsrc = reinterpret_cast<const uint4*>(frag) + u * kRT * 64 + lane;
+#pragma unroll
+          for (int i = 0; i < kRT; ++i) {
+            const uint4 h4 = fsrc[64 * i], l4 = fsrc[64 * i + 32];
+            const uint32_t hi[4] = {h4.x, h4.y, h4.z, h4.w}, lo[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t pick = (j & 1) ? 0x7632u : 0x5410u;
+              const uint32_t b0 = __byte_perm(v[0][j >> 1], v[1][j >> 1], pick);
+              const uint32_t b1 = __byte_perm(v[2][j >> 1], v[3][j >> 1], pick);
+              mma_bf16(acc[i][j], hi, b0, b1);
+              mma_bf16(acc[i][j], lo, b0, b1);
+            }
           }
         }
-      stage = stage + 1 == kUnits ? 0 : stage + 1;
-#pragma unroll
-      for (int i = 0; i < kRT; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t pick = (j & 1) ? 0x7632u : 0x5410u;
-          const uint32_t b0 = __byte_perm(v[0][j >> 1], v[1][j >> 1], pick);
-          const uint32_t b1 = __byte_perm(v[2][j >> 1], v[3][j >> 1], pick);
-          mma_bf16(acc[i][j], hi[i], b0, b1);
-          mma_bf16(acc[i][j], lo[i], b0, b1);
-        }
+        stage = stage + 1 == kUnits ? 0 : stage + 1;
+      }
     }
   }
-  // acc[i][j]: ranks 16 i + g (e 0, 1) and + 8 (e 2, 3), N slots 2 q, 2 q + 1 of column tile j, which are
-  // columns 8 (2 q) + j and 8 (2 q + 1) + j.  The warps' partials: [warp][rank][64].
-  constexpr int kSize = 16 * kRT * 64;
+  // acc[i][j]: ranks 16 i + g (e 0, 1) and + 8 (e 2, 3), N slots 2 q, 2 q + 1 of column tile j, which are columns
+  // 8 (2 q) + j and 8 (2 q + 1) + j of the warp's 64.  The sets' partials: [set][rank][column].
+  constexpr int kSize = 16 * kRT * kPitch;
+  float* part = reinterpret_cast<float*>(smem);
   copies_wait<0>();
   __syncthreads();  // the partials take the rings' place
 #pragma unroll
@@ -530,25 +588,27 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
     for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        part[warp * kSize + (16 * i + 8 * (e >> 1) + g) * 64 + 8 * (2 * q + (e & 1)) + j] = acc[i][j][e];
+        part[sub * kSize + (16 * i + 8 * (e >> 1) + g) * kPitch + 64 * (warp & 3) + 8 * (2 * q + (e & 1)) + j] = acc[i][j][e];
   __syncthreads();
-  for (int i = threadIdx.x; i < kSize; i += kThreads) {
+  for (int i = threadIdx.x; i < kSize; i += kThreadsG) {
     float s = part[i];
 #pragma unroll
-    for (int v = 1; v < kWarps; ++v) s += part[v * kSize + i];
+    for (int v = 1; v < kSub; ++v) s += part[v * kSize + i];
     part[i] = s;
   }
   if (csize > 1) cluster_sync(); else __syncthreads();
-  const int share = (kSize + csize - 1) / csize;
-  for (int i = crank * share + threadIdx.x; i < min(kSize, (crank + 1) * share); i += kThreads) {
+  // a rank finishes a share of the columns
+  const int share = (kColumns / 8 + csize - 1) / csize * 8, c0 = crank * share, width = min(share, kColumns - c0);
+  for (int i = threadIdx.x; i < 16 * kRT * width; i += kThreadsG) {
     // dA's rows run along the columns, dB's along the ranks
-    const int e = kRankMajor ? i : (i % (16 * kRT)) * 64 + i / (16 * kRT);
-    const int r = r0 + (e >> 6);
-    const int64_t c = col0 + (e & 63);
-    if (r >= rank || c >= rows.cols) continue;
-    float s = csize > 1 ? ld_cluster(part + e, 0) : part[e];
-    for (int d = 1; d < csize; ++d) s += ld_cluster(part + e, (uint32_t)d);
-    out[kRankMajor ? ((int64_t)a * rank + r) * rows.cols + c : ((int64_t)a * rows.cols + c) * rank + r] = __float2bfloat16_rn(s);
+    const int rr = kRankMajor ? i / width : i % (16 * kRT), cc = c0 + (kRankMajor ? i % width : i / (16 * kRT));
+    const int r = r0 + rr;
+    const int64_t c = col0 + cc;
+    if (r >= rank || c >= cols) continue;
+    const float* src = part + rr * kPitch + cc;
+    float s = csize > 1 ? ld_cluster(src, 0) : *src;
+    for (int d = 1; d < csize; ++d) s += ld_cluster(src, (uint32_t)d);
+    out[kRankMajor ? ((int64_t)a * rank + r) * cols + c : ((int64_t)a * cols + c) * rank + r] = __float2bfloat16_rn(s);
   }
   if (csize > 1) cluster_sync();
 }
@@ -562,17 +622,16 @@ struct GradArgs {
   int csize, tiles_a;
 };
 template <int kFormat, int kRT>
-__global__ void __launch_bounds__(kThreads, 2) grad_kernel(Rows<kFormat> x, Rows<-1> dy, GradArgs p) {
+__global__ void __launch_bounds__(128 * grad_sets<kRT>(), 1) grad_kernel(Rows<kFormat> x, Rows<-1> dy, GradArgs p) {
   extern __shared__ __align__(16) uint8_t grad_smem[];
   __shared__ GradShared sh;
-  float* part = reinterpret_cast<float*>(grad_smem);  // after the rings
   const int crank = p.csize > 1 ? (int)cluster_rank() : 0, tile = blockIdx.x / p.csize, r0 = blockIdx.z * 16 * kRT;
   if (tile < p.tiles_a)
-    grad_tile<kFormat, true, kRT>(x, p.tokens, p.ad, p.dz, p.da, (int64_t)tile * 64, blockIdx.y, r0, p.csize, crank, part,
-                                  grad_smem, sh);
+    grad_tile<kFormat, true, kRT>(x, p.tokens, p.ad, p.dz, p.da, (int64_t)tile * kColumns, blockIdx.y, r0, p.csize, crank, grad_smem,
+                                  sh);
   else
-    grad_tile<-1, false, kRT>(dy, p.tokens, p.ad, p.z, p.db, (int64_t)(tile - p.tiles_a) * 64, blockIdx.y, r0, p.csize, crank,
-                              part, grad_smem, sh);
+    grad_tile<-1, false, kRT>(dy, p.tokens, p.ad, p.z, p.db, (int64_t)(tile - p.tiles_a) * kColumns, blockIdx.y, r0, p.csize,
+                              crank, grad_smem, sh);
 }
 
 template <int kFormat, int kRT>
@@ -581,20 +640,23 @@ cudaError_t launch_grad_of(const Rows<kFormat>& x, const Rows<-1>& dy, GradArgs 
   cudaError_t err = current_device_info(&info);
   if (err != cudaSuccess) return err;
   auto kernel = grad_kernel<kFormat, kRT>;
-  constexpr int kSmem = std::max(kWarps * 16 * kRT * 64 * 4, kWarps * kUnits * unit_bytes<kRT>());
+  constexpr int kSets = grad_sets<kRT>();
+  constexpr int kSmem = std::max(kSets * 16 * kRT * kPitch * 4, grad_smem_bytes<kRT>());
+  static_assert(kSmem + sizeof(GradShared) <= 227 * 1024, "shared memory");
   err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmem);
   if (err != cudaSuccess) return err;
-  p.tiles_a = p.da != nullptr ? (int)((x.cols + 63) / 64) : 0;
-  const int64_t tiles = p.tiles_a + (p.db != nullptr ? (dy.cols + 63) / 64 : 0);
+  p.tiles_a = p.da != nullptr ? (int)((x.cols + kColumns - 1) / kColumns) : 0;
+  const int64_t tiles = p.tiles_a + (p.db != nullptr ? (dy.cols + kColumns - 1) / kColumns : 0);
   const int passes = (p.ad.rank + 16 * kRT - 1) / (16 * kRT);
-  // the tokens split while two CTAs an SM hold all, and a warp of an adapter's share has 16 of them
+  // the tokens split (by up to four: clusters of eight CTAs that fill an SM each leave many SMs out) while a CTA an
+  // SM holds all, and an adapter's share has a chunk of them
   p.csize = 1;
-  while (p.csize < 8 && tiles * p.ad.count * passes * (p.csize + 1) <= 2 * info.sm_count &&
-         p.tokens / p.ad.count > (int64_t)p.csize * kWarps * 16)
+  while (p.csize < 4 && tiles * p.ad.count * passes * (p.csize + 1) <= info.sm_count &&
+         p.tokens / p.ad.count > (int64_t)p.csize * kChunk)
     ++p.csize;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * p.csize), (unsigned)p.ad.count, (unsigned)passes);
-  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.blockDim = dim3(128 * kSets, 1, 1);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -607,13 +669,14 @@ cudaError_t launch_grad_of(const Rows<kFormat>& x, const Rows<-1>& dy, GradArgs 
   return err != cudaSuccess ? err : cudaGetLastError();
 }
 
-Rows<-1> bf16_rows(const void* x, int64_t ld, int64_t cols) { return {static_cast<const uint16_t*>(x), ld, {}, cols, 1}; }
+Rows<-1> bf16_rows(const void* x, int64_t ld, int64_t cols) { return {static_cast<const uint16_t*>(x), ld, {}, cols, 1, false}; }
 
 template <int kFormat>
 Rows<kFormat> ckpt_rows(const Checkpoint& c, int64_t cols) {
   const uintptr_t base = reinterpret_cast<uintptr_t>(c.codes);
   const int vec = base % 16 == 0 && c.ld_codes % 16 == 0 ? 16 : base % 8 == 0 && c.ld_codes % 8 == 0 ? 8 : 1;
-  return {nullptr, 0, c, cols, vec};
+  const bool words = reinterpret_cast<uintptr_t>(c.scales) % 4 == 0 && c.ld_scales % 4 == 0 && cols % 128 == 0;
+  return {nullptr, 0, c, cols, vec, words};
 }
 
 template <int kFormat>
@@ -624,7 +687,8 @@ cudaError_t backward_products(const Checkpoint& c, int64_t n, const Rows<-1>& dy
 template <int kFormat>
 cudaError_t gradients(const Checkpoint& c, int64_t n, const Rows<-1>& dy, const GradArgs& p, cudaStream_t stream) {
   const Rows<kFormat> x = ckpt_rows<kFormat>(c, n);
-  return p.ad.rank <= 16 ? launch_grad_of<kFormat, 1>(x, dy, p, stream) : launch_grad_of<kFormat, 2>(x, dy, p, stream);
+  if (p.ad.rank <= 16) return launch_grad_of<kFormat, 1>(x, dy, p, stream);
+  return p.ad.rank <= 32 ? launch_grad_of<kFormat, 2>(x, dy, p, stream) : launch_grad_of<kFormat, 4>(x, dy, p, stream);
 }
 
 }  // namespace

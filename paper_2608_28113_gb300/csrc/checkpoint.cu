@@ -115,10 +115,9 @@ checkpoint_load_kernel(const uint8_t* __restrict__ codes, int64_t ld_codes, cons
       for (int j = 0; j < 8; ++j)
         if (j < have) q[j >> 2] |= (uint32_t)src[j] << (8 * (j & 3));
     }
-    const float scale = ckpt_scale(scales[row * ld_scales + blk]);
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = ckpt_values<kFormat>(q[j >> 1] >> (16 * (j & 1)), scale);
+    const uint32_t scale = ckpt_scale(scales[row * ld_scales + blk]);
+    const uint32_t w[4] = {ckpt_values<kFormat, 0>(q[0], scale), ckpt_values<kFormat, 1>(q[0], scale),
+                           ckpt_values<kFormat, 0>(q[1], scale), ckpt_values<kFormat, 1>(q[1], scale)};
     uint16_t* dst = x + row * ld_x + col;
     if (kVec && have == 8) {
       *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);

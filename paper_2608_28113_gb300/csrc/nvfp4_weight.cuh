@@ -97,9 +97,9 @@ struct Checkpoint {
   int64_t ld_codes, ld_scales;
 };
 
-// 2^(byte - 127); byte 255 is NaN, and byte 0, which no save writes, 0.
-__device__ __forceinline__ float ckpt_scale(uint32_t byte) {
-  return __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23);
+// 2^(byte - 127) in both halves, exact; byte 255 is NaN, and byte 0, which no save writes, 0.
+__device__ __forceinline__ uint32_t ckpt_scale(uint32_t byte) {
+  return (byte == 255u ? 0x7FC0u : byte << 7) * 0x00010001u;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -108,22 +108,21 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-// The two elements in the low 16 bits of `two` as the values they stand for: bf16x2, exact.
-template <int kFormat>
-__device__ __forceinline__ uint32_t ckpt_values(uint32_t two, float scale) {
-  float lo, hi;
+// Two elements (bytes 2 kPair, 2 kPair + 1 of `four`) as the values they stand for: bf16x2, every step exact.
+template <int kFormat, int kPair>
+__device__ __forceinline__ uint32_t ckpt_values(uint32_t four, uint32_t scale) {
   if constexpr (kFormat == kCkptInt8) {
-    // a byte b ^ 0x80 in the low mantissa bits of 2^23 reads as 2^23 + 128 + b
-    const uint32_t u = two ^ 0x8080u;
-    lo = __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540)) - 8388736.0f;
-    hi = __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7541)) - 8388736.0f;
+    // the low 7 bits u of a byte in the mantissa of 128 read as 128 + u; its sign bit one place further up makes 128 256
+    const uint32_t p = __byte_perm(four, 0u, kPair ? 0x4342 : 0x4140);
+    const uint32_t m = (p & 0x007F007Fu) | 0x43004300u, c = (p & 0x00800080u) | 0x43004300u;
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(c));
+    return mul_bf16x2(r, scale);
   } else {
-    asm("{\n\t.reg .b32 p;\n\t.reg .f16 l, h;\n\tcvt.rn.f16x2.e4m3x2 p, %2;\n\tmov.b32 {l, h}, p;\n\t"
-        "cvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}"
-        : "=f"(lo), "=f"(hi)
-        : "h"((uint16_t)two));
+    // exponent and mantissa moved to bf16's low exponent bits and mantissa read as E4M3 2^-120
+    const uint32_t p = __byte_perm(four, 0u, kPair ? 0x3424 : 0x1404);
+    return mul_bf16x2(mul_bf16x2((p & 0x80008000u) | ((p >> 4) & 0x07F007F0u), 0x7B807B80u /* 2^120 */), scale);
   }
-  return pack_bf16(lo * scale, hi * scale);
 }
 
 }  // namespace hscale
