@@ -26,8 +26,8 @@
 //
 // The adapters' terms.  An adapter with enough tokens in a tile takes its term on the tensor cores: after the
 // weight's K blocks the epilogue's warps, idle by then, write its factors and its tokens' z (as a pair hi + lo of
-// bf16 numbers, so 2^-17 of it is lost; zeros for the other tokens) as one more K block per 32 ranks, fetched
-// before the stage is free.  An adapter with few tokens there ("loose": a decoding batch) is cheaper in the epilogue
+// bf16 numbers, so 2^-17 of it is lost; zeros for the other tokens) as one more K block per 32 ranks or per two or
+// four adapters of fewer ranks, fetched before the stage is free.  An adapter with few tokens there ("loose": a decoding batch) is cheaper in the epilogue
 // itself, a dot product of `rank` fp32 numbers per result.  Zeros times factors are zeros only while the
 // factors are finite: an output whose factors hold an Inf or NaN is left out of the K block, and the tokens
 // of that adapter get NaN there; so nothing passes from one request's adapter to another's tokens.
@@ -53,6 +53,7 @@ constexpr uint32_t kGroupBytes = 64 * kBK * 2;   // MN-major: 64 outputs x 64 ro
 constexpr int kInfos = 4;                        // TileInfo of as many tiles
 constexpr uint32_t kInfoBytes = 576;
 constexpr uint32_t kBarBytes = 512;
+constexpr uint32_t kTurnBytes = 4 * 2048;        // of the epilogue's warps: z, and results on their way out
 constexpr int kGo = 16;                          // tiles whose place in the ring's order is kept: more than it has stages
 
 template <int kN>
@@ -60,7 +61,7 @@ struct Tile {
   static constexpr int kStages = kN == 256 ? 4 : kN == 128 ? 5 : 6;
   static constexpr uint32_t kBBytes = kN * kBK * 2;
   static constexpr uint32_t kStageBytes = kTileABytes + kBBytes;
-  static constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 /* alignment */ + kBarBytes + 4096 /* z */ +
+  static constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 /* alignment */ + kBarBytes + kTurnBytes +
                                          kInfos * kInfoBytes + 1024 /* bad */;
   static constexpr uint32_t kTmemCols = 2 * kN;
 };
@@ -137,7 +138,7 @@ __device__ __forceinline__ void unpack_factors(const uint4& q, float (&f)[8]) {
 }
 
 // Results of tokens t0 .. t0 + W - 1 and this lane's output o: v (without the adapters' terms) plus each
-// token's adapter, rounded and stored.  zs: 32 x 8 floats of the warp's own.  Eight ranks a pass: each lane
+// token's adapter, rounded and stored.  zs: 2 KB of the warp's own.  Eight ranks a pass: each lane
 // fetches its token's z into zs, from where every lane reads all of them; z and factors of the next pass are
 // fetched before the present one's products.  Tokens on one adapter share a lane's 8 factors; otherwise
 // the factors of 8 tokens are fetched at once.  A token without an adapter keeps v as it is (no product by
@@ -197,14 +198,40 @@ __device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int
       }
     }
   }
-  if (!on) return;
-  __nv_bfloat16* dst = p.out + t0 * p.ld_out + o;
+  // Rounded, and turned in zs (pairs of tokens, an output a lane) so that a lane stores 8 outputs of a token at once:
+  // stores of one output a lane kept the epilogue from the next tile's adapters (8192 x 14336 x 4096, rank 16: 806 us,
+  // 727 now)
+  uint32_t* turn = reinterpret_cast<uint32_t*>(zs);
+  __syncwarp();
 #pragma unroll
-  for (int j = 0; j < W; ++j)
-    if (t0 + j < p.tokens) dst[j * p.ld_out] = __float2bfloat16_rn(v[j]);
+  for (int j = 0; j < W / 2; ++j) turn[j * 32 + lane] = pack_bf16(v[2 * j], v[2 * j + 1]);
+  __syncwarp();
+  const int64_t outs = kForward ? p.w.m : p.w.n, first = o - lane;
+#pragma unroll
+  for (int i = lane; i < W * 2; i += 32) {
+    const int pair = i >> 2, group = i & 3;
+    const uint4 a = reinterpret_cast<const uint4*>(turn)[pair * 8 + group * 2];
+    const uint4 b = reinterpret_cast<const uint4*>(turn)[pair * 8 + group * 2 + 1];
+    const int64_t t = t0 + 2 * pair, at = first + 8 * group;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if (t + e >= p.tokens) continue;
+      const uint32_t pick = e ? 0x7632u : 0x5410u;
+      const uint4 r = make_uint4(__byte_perm(a.x, a.y, pick), __byte_perm(a.z, a.w, pick), __byte_perm(b.x, b.y, pick),
+                                 __byte_perm(b.z, b.w, pick));
+      uint16_t* dst = reinterpret_cast<uint16_t*>(p.out) + (t + e) * p.ld_out + at;
+      if (at + 8 <= outs) {
+        *reinterpret_cast<uint4*>(dst) = r;
+      } else {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (at + k < outs) dst[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+      }
+    }
+  }
 }
 
-constexpr int kRanks = 32;      // ranks a K block of an adapter holds: [factors | factors] times [hi | lo]
 constexpr int kMaxListed = 32;  // adapters of a tile that may take their term on the tensor cores
 // The adapters of a tile of kN <= 256 tokens.
 struct TileInfo {
@@ -215,12 +242,19 @@ struct TileInfo {
   uint8_t index[256];            // a token's place in the list, or 255
 };
 static_assert(sizeof(TileInfo) <= kInfoBytes, "TileInfo's place");
-__device__ __forceinline__ int rank_blocks(int rank) { return (rank + kRanks - 1) / kRanks; }
-__device__ __forceinline__ int half_ranks(int rank, int r0) { return rank - r0 <= 16 ? 16 : kRanks; }
+// A K block of the adapters: [factors | factors] times [hi | lo] of 8, 16 or 32 ranks, of as many adapters as fit in
+// 64.
+__device__ __forceinline__ int half_ranks(int rank) { return rank <= 8 ? 8 : rank <= 16 ? 16 : 32; }
+__device__ __forceinline__ int adapters_a_block(int rank) { return rank <= 8 ? 4 : rank <= 16 ? 2 : 1; }
+__device__ __forceinline__ int blocks_of(int listed, int rank) {
+  const int per = adapters_a_block(rank);
+  return (listed + per - 1) / per * ((rank + 31) >> 5);
+}
 
-// A K block costs the epilogue's warps about 1500 cycles, a loose token 112 per 8 ranks (eight tokens' factors
-// fetched at once), so an adapter is listed from 14 rank_blocks / (rank / 8) tokens on.
-template <int kN>
+// A K block costs the epilogue's warps about 1500 cycles; a loose token about 112 cycles per 8 ranks forward, where its
+// factors are 16 bytes an output, and 450 backward, where they are 8 loads (eight tokens' factors fetched at once).  An
+// adapter is listed where its tokens' share would cost more than its part of a K block.
+template <bool kForward, int kN>
 __device__ __forceinline__ void find_adapters(const ProjectArgs& p, int64_t t0, int lane, TileInfo& info) {
   int id[kN / 32];
   uint32_t left[kN / 32], loose[kN / 32];
@@ -235,7 +269,8 @@ __device__ __forceinline__ void find_adapters(const ProjectArgs& p, int64_t t0, 
     loose[i] = left[i];
     info.index[32 * i + lane] = 255;
   }
-  const int enough = (14 * rank_blocks(p.ad.rank) + p.ad.rank / 8 - 1) / (p.ad.rank / 8);
+  const int block = 1500 * ((p.ad.rank + 31) / 32) / adapters_a_block(p.ad.rank), loose_token = (kForward ? 14 : 56) * p.ad.rank;
+  const int enough = (block + loose_token - 1) / loose_token;
   int listed = 0;
   // the first token left over, its adapter, all its tokens
 #pragma unroll
@@ -264,44 +299,53 @@ __device__ __forceinline__ void find_adapters(const ProjectArgs& p, int64_t t0, 
 #pragma unroll
   for (int i = 0; i < kN / 32; ++i)
     if (lane == i) info.loose[i] = loose[i];
-  if (lane == 0) info.listed = listed, info.blocks = listed * rank_blocks(p.ad.rank);
+  if (lane == 0) info.listed = listed, info.blocks = blocks_of(listed, p.ad.rank);
   __syncwarp();
 }
 
 // Bits of a register's bf16 halves that are Inf or NaN (0xFFFF each).
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return __vcmpeq2(w & 0x7F807F80u, 0x7F807F80u); }
 
-// The K block of ranks r0 .. of the list's adapter e, by the epilogue's 128 threads: the factors (as the weight's
-// tile) and the z of its tokens (as the tokens' tile; the accumulator is in units of 128 s_g, so z is divided by it).
-// Loaded before `acquire` waits for the stage.  bad[output] gets bit e where a factor is Inf or NaN.
+// The K block of ranks r0 .. of the list's adapters from e on, by the epilogue's 128 threads: the factors (as the
+// weight's tile) and the z of their tokens (as the tokens' tile; the accumulator is in units of 128 s_g, so z is divided
+// by it), zeros for the other tokens.  Loaded before `acquire` waits for the stage.  bad[output] gets an adapter's bit
+// where a factor is Inf or NaN.
 template <bool kForward, int kN, typename Acquire>
 __device__ __forceinline__ bool adapter_block(const ProjectArgs& p, const TileInfo& info, int e, int r0, int64_t t0, int64_t o0,
                                               int line, float unit, uint32_t* bad, uint8_t* tile_a, uint8_t* tile_b,
                                               Acquire acquire) {
   constexpr int kRows = (kN + 127) / 128;
-  const int rank = p.ad.rank, a = info.adapter[e], half = half_ranks(rank, r0), hc = half / 8;
+  const int rank = p.ad.rank, half = half_ranks(rank), hc = half / 8, per = adapters_a_block(rank);
+  const int hs = rank <= 8 ? 0 : rank <= 16 ? 1 : 2;  // hc = 2^hs
+  // 16-byte piece i of the factors: forward ranks 8 (i % hc) .. of this output, of adapter e + i / hc; backward 8 outputs of
+  // row (line + 128 i) / 16 of the block's 32 rows of factors
+  const auto owner = [&](int i) { return kForward ? i >> hs : (line + i * 128) >> (7 + hs); };
   uint4 f[4], hi[kRows][4], lo[kRows][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     f[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (i >= hc) continue;
+    const int sub = owner(i);
+    if (e + sub >= info.listed) continue;
+    const int64_t a = info.adapter[e + sub];
     if (kForward) {
-      if (o0 + line < p.w.m && r0 + 8 * i < rank) f[i] = ld_nc_v4(p.ad.b + ((int64_t)a * p.w.m + o0 + line) * rank + r0 + 8 * i);
+      const int r = r0 + 8 * (i & (hc - 1));
+      if (o0 + line < p.w.m && r < rank) f[i] = ld_nc_v4(p.ad.b + (a * p.w.m + o0 + line) * rank + r);
     } else {
-      const int k = line + i * 128, r = k >> 4;  // rank r, outputs 8 (k % 16) ..
-      const int64_t o = o0 + (k & 15) * 8;
-      if (o < p.w.n && r0 + r < rank) f[i] = ld_nc_v4(p.ad.a + ((int64_t)a * rank + r0 + r) * p.w.n + o);
+      const int r = r0 + (((line + i * 128) >> 4) & (half - 1));
+      const int64_t o = o0 + (line & 15) * 8;
+      if (o < p.w.n && r < rank) f[i] = ld_nc_v4(p.ad.a + (a * rank + r) * p.w.n + o);
     }
   }
+  int mine[kRows];  // the row's adapter among the block's, or none
 #pragma unroll
   for (int k = 0; k < kRows; ++k) {
-    const int t = line + 128 * k;
-    const bool mine = t < kN && info.index[t < kN ? t : 0] == e;
+    const int t = line + 128 * k, index = info.index[t < kN ? t : 0];
+    mine[k] = t < kN && index >= e && index < e + per ? index - e : -1;  // 255: none
     const float4* src = reinterpret_cast<const float4*>(p.z + (t0 + t) * rank + r0);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
-      if (mine && c < hc && r0 + 8 * c < rank) v0 = src[2 * c], v1 = src[2 * c + 1];
+      if (mine[k] >= 0 && c < hc && r0 + 8 * c < rank) v0 = src[2 * c], v1 = src[2 * c + 1];
       const float v[8] = {v0.x * unit, v0.y * unit, v0.z * unit, v0.w * unit, v1.x * unit, v1.y * unit, v1.z * unit, v1.w * unit};
       uint32_t h[4], l[4];
 #pragma unroll
@@ -313,29 +357,23 @@ __device__ __forceinline__ bool adapter_block(const ProjectArgs& p, const TileIn
       lo[k][c] = make_uint4(l[0], l[1], l[2], l[3]);
     }
   }
-  uint32_t odd = 0u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) odd |= not_finite(f[i].x) | not_finite(f[i].y) | not_finite(f[i].z) | not_finite(f[i].w);
-  if (odd) {
-    if (kForward) {
-      atomicOr(&bad[line], 1u << e);
+  for (int i = 0; i < 4; ++i) {
+    if (!(not_finite(f[i].x) | not_finite(f[i].y) | not_finite(f[i].z) | not_finite(f[i].w))) continue;
+    const uint32_t bit = 1u << (e + owner(i));
+    uint32_t w[4] = {f[i].x, f[i].y, f[i].z, f[i].w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = make_uint4(0u, 0u, 0u, 0u);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t w[4] = {f[i].x, f[i].y, f[i].z, f[i].w};
-        const int o = ((line + i * 128) & 15) * 8;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t x = not_finite(w[j]);
-          if (x & 0xFFFFu) atomicOr(&bad[o + 2 * j], 1u << e);
-          if (x >> 16) atomicOr(&bad[o + 2 * j + 1], 1u << e);
-          w[j] &= ~x;
-        }
-        f[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t x = not_finite(w[j]);
+      if (kForward) {
+        if (x) atomicOr(&bad[line], bit);
+      } else {
+        if (x & 0xFFFFu) atomicOr(&bad[(line & 15) * 8 + 2 * j], bit);
+        if (x >> 16) atomicOr(&bad[(line & 15) * 8 + 2 * j + 1], bit);
       }
+      w[j] &= ~x;
     }
+    f[i] = make_uint4(w[0], w[1], w[2], w[3]);
   }
   int s;
   if (!acquire(s)) return false;
@@ -343,13 +381,14 @@ __device__ __forceinline__ bool adapter_block(const ProjectArgs& p, const TileIn
   uint8_t* tb = tile_b + s * Tile<kN>::kBBytes;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (i >= hc) continue;
+    const int sub = owner(i);
     if (kForward) {
-      *reinterpret_cast<uint4*>(ta + line * 128 + ((i ^ (line & 7)) << 4)) = f[i];
-      *reinterpret_cast<uint4*>(ta + line * 128 + (((i + hc) ^ (line & 7)) << 4)) = f[i];
+      const int c = sub * 2 * hc + (i & (hc - 1));
+      *reinterpret_cast<uint4*>(ta + line * 128 + ((c ^ (line & 7)) << 4)) = f[i];
+      *reinterpret_cast<uint4*>(ta + line * 128 + (((c + hc) ^ (line & 7)) << 4)) = f[i];
     } else {
-      const int k = line + i * 128, r = k >> 4, c = k & 7;
-      uint8_t* dst = ta + ((k >> 3) & 1) * kGroupBytes + r * 128 + ((c ^ (r & 7)) << 4);
+      const int r = sub * 2 * half + (((line + i * 128) >> 4) & (half - 1)), c = line & 7;
+      uint8_t* dst = ta + ((line >> 3) & 1) * kGroupBytes + r * 128 + ((c ^ (r & 7)) << 4);
       *reinterpret_cast<uint4*>(dst) = f[i];
       *reinterpret_cast<uint4*>(dst + half * 128) = f[i];
     }
@@ -358,11 +397,20 @@ __device__ __forceinline__ bool adapter_block(const ProjectArgs& p, const TileIn
   for (int k = 0; k < kRows; ++k) {
     const int t = line + 128 * k;
     if (t >= kN) continue;
+    uint8_t* dst = tb + t * 128;
+    const int at = mine[k] * 2 * hc;  // the row's first 16 bytes that are not zeros
+    if (per > 1) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (mine[k] < 0 || c < at || c >= at + 2 * hc) *reinterpret_cast<uint4*>(dst + ((c ^ (t & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+      if (mine[k] < 0) continue;
+    }
+    const int first = per > 1 ? at : 0;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       if (c >= hc) continue;
-      *reinterpret_cast<uint4*>(tb + t * 128 + ((c ^ (t & 7)) << 4)) = hi[k][c];
-      *reinterpret_cast<uint4*>(tb + t * 128 + (((c + hc) ^ (t & 7)) << 4)) = lo[k][c];
+      *reinterpret_cast<uint4*>(dst + (((first + c) ^ (t & 7)) << 4)) = hi[k][c];
+      *reinterpret_cast<uint4*>(dst + (((first + c + hc) ^ (t & 7)) << 4)) = lo[k][c];
     }
   }
   return true;
@@ -408,8 +456,8 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
   uint32_t* failed = tmem_slot + 1;
   int* place = reinterpret_cast<int*>(failed + 1);  // [kGo]
-  float* zs = reinterpret_cast<float*>(smem + kStages * T::kStageBytes + kBarBytes) + (threadIdx.x >> 5 & 3) * 256;
-  uint8_t* info_base = smem + kStages * T::kStageBytes + kBarBytes + 4096;
+  float* zs = reinterpret_cast<float*>(smem + kStages * T::kStageBytes + kBarBytes) + (threadIdx.x >> 5 & 3) * (kTurnBytes / 16);
+  uint8_t* info_base = smem + kStages * T::kStageBytes + kBarBytes + kTurnBytes;
   uint32_t* bad = reinterpret_cast<uint32_t*>(info_base + kInfos * kInfoBytes);  // [2][128]
   auto info_of = [&](int i) -> TileInfo& { return *reinterpret_cast<TileInfo*>(info_base + (i % kInfos) * kInfoBytes); };
 
@@ -550,9 +598,12 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
       if (adds && ok) ok = wait_info(i);
       if (adds && ok) {
         const TileInfo& info = info_of(i);
-        for (int e = 0; e < info.listed && ok; ++e) {
-          const uint32_t sel = info.sel[e];
-          for (int r0 = 0; r0 < p.ad.rank && ok; r0 += kRanks) {
+        const int per = adapters_a_block(p.ad.rank);
+        for (int e = 0; e < info.listed && ok; e += per) {
+          uint32_t sel = 0u;
+          const int subs = min(per, info.listed - e);
+          for (int k = 0; k < subs; ++k) sel |= info.sel[e + k];
+          for (int r0 = 0; r0 < p.ad.rank && ok; r0 += 32) {
             if (!mbar_wait_warp(&full[s], parity)) {
               ok = false;
               break;
@@ -561,7 +612,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
             const uint32_t a = smem_addr(tile_a + s * kTileABytes), b = smem_addr(tile_b + s * T::kBBytes);
             const uint64_t ad = kForward ? smem_desc_k_sw128(a) : smem_desc_mn_sw128(a, kGroupBytes);
             const uint64_t bd = smem_desc_k_sw128(b);
-            const int steps = half_ranks(p.ad.rank, r0) / 8;
+            const int steps = subs * half_ranks(p.ad.rank) / 8;
             if (elect_one()) {
               for (uint32_t runs = sel; runs;) {  // each run of neighbouring blocks
                 const int b0 = __ffs(runs) - 1, len = __ffs(~(runs >> b0)) - 1;
@@ -593,7 +644,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
       if (!adapters || warp != 2 || i >= ntiles) return;
       int tt, to;
       raster(first + i * step, p, tt, to);
-      find_adapters<kN>(p, (int64_t)tt * kN, lane, info_of(i));
+      find_adapters<kForward, kN>(p, (int64_t)tt * kN, lane, info_of(i));
       if (lane == 0) mbar_arrive(&info_full[i % kInfos]);
     };
     bad[out_row] = bad[128 + out_row] = 0u;
@@ -613,8 +664,8 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
       uint32_t spoiled = 0u;
       if (adapters && have) have = wait_info(i);
       if (adds) {
-        for (int e = 0; have && e < info.listed; ++e)
-          for (int r0 = 0; r0 < p.ad.rank && have; r0 += kRanks, ++extras) {
+        for (int e = 0; have && e < info.listed; e += adapters_a_block(p.ad.rank))
+          for (int r0 = 0; r0 < p.ad.rank && have; r0 += 32, ++extras) {
             int s = 0;
             const auto acquire = [&](int& stage) {
               s = stage = ((i + 1) * kbs + extras) % kStages;
