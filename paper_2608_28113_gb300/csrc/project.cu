@@ -47,7 +47,7 @@ namespace {
 constexpr int kBM = 128, kBK = 64;
 constexpr int kThreads = 576;
 constexpr int kUnpackWarp0 = 6, kUnpackGroups = 3, kGroupThreads = 128;
-constexpr int kAhead = 3;  // blocks of its own that a group has in flight
+constexpr int kAhead = 2;  // blocks of its own that a group has in flight
 constexpr uint32_t kTileABytes = kBM * kBK * 2;  // 16 KB
 constexpr uint32_t kGroupBytes = 64 * kBK * 2;   // MN-major: 64 outputs x 64 rows of K
 constexpr int kInfos = 4;                        // TileInfo of as many tiles
@@ -639,6 +639,8 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
     __syncwarp();
     umma_drain(mma_done);
   } else if (warp < kUnpackWarp0) {
+    // columns at a time: the small tiles' loops need the registers that 32 would take
+    constexpr int kWide = kN >= 128 ? 32 : 16;
     const float scale = *p.w.global_scale * 128.0f;
     const auto find = [&](int i) {
       if (!adapters || warp != 2 || i >= ntiles) return;
@@ -694,21 +696,24 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
         break;
       }
 #pragma unroll 1
-      for (int c = 0; c < kN; c += 32) {
+      for (int c = 0; c < kN; c += kWide) {
         const int64_t t0 = (int64_t)tt * kN + c;
-        uint32_t q[32];
-        tmem_ld_32x32b_x32(tmem_d + acc * kN + lane_base + (uint32_t)c, q);
+        uint32_t q[kWide];
+        if constexpr (kWide == 32)
+          tmem_ld_32x32b_x32(tmem_d + acc * kN + lane_base + (uint32_t)c, q);
+        else
+          tmem_ld_32x32b_x16(tmem_d + acc * kN + lane_base + (uint32_t)c, q);
         tmem_ld_wait();
-        if (c + 32 == kN) {
+        if (c + kWide == kN) {
           tc_fence_before_sync();
           mbar_arrive(&acc_empty[acc]);
         }
         if (t0 >= p.tokens) continue;
-        if (adapters) spoil<32>(q, spoiled, info.index + c);
-        float v[32];
+        if (adapters) spoil<kWide>(q, spoiled, info.index + c);
+        float v[kWide];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(q[j]) * scale;
-        finish<kForward, 32>(v, t0, o, lane, p, adapters ? info.loose[c >> 5] : 0u, zs);
+        for (int j = 0; j < kWide; ++j) v[j] = __uint_as_float(q[j]) * scale;
+        finish<kForward, kWide>(v, t0, o, lane, p, adapters ? info.loose[c >> 5] >> (c & 31) : 0u, zs);
       }
     }
     if (!have && lane == 0) atomicOr(failed, 1u);
