@@ -40,32 +40,35 @@ __device__ __forceinline__ void unpack_pairs(uint32_t w, uint32_t scale, uint32_
   r[3] = mul_bf16x2((w & kSign) | ((w >> 6) & kMag), scale);
 }
 
+// A block's words of a lane's rows and their two codes each
 template <int kMT>
 struct Block {
-  uint32_t w[2 * kMT][4], c[2 * kMT], c1[2 * kMT];
+  uint32_t w[2 * kMT][4], c[2 * kMT];
 };
 
+// Rows past the end of W and tokens past the end of x are read as the last ones, and their results dropped, so only
+// the last block of a row needs bounds.
 template <int kMT>
-__device__ __forceinline__ void load_block(const DecodeArgs& p, int64_t row0, int64_t k, Block<kMT>& b) {
-  const int64_t n = p.w.n;
+__device__ __forceinline__ void load_block(const uint8_t* const (&wp)[2 * kMT], const uint8_t* const (&cp)[2 * kMT], int64_t k,
+                                           int64_t n, bool wide, Block<kMT>& b) {
+  const int64_t wk = k >> 1, ck = k >> 4;
+  if (wide) {
+    const bool on = k < n;  // n % 32 == 0
 #pragma unroll
-  for (int i = 0; i < 2 * kMT; ++i) {
-    const int64_t f = row0 + 8 * i;
-    const bool on = f < p.w.m && k < n;
-    const uint8_t* wp = p.w.packed + f * (n >> 1) + (k >> 1);
-    const uint8_t* cp = p.w.codes + f * (n >> 4) + (k >> 4);
+    for (int i = 0; i < 2 * kMT; ++i) {
+      ld_16_ahead(on, wp[i] + wk, b.w[i][0], b.w[i][1], b.w[i][2], b.w[i][3]);
+      ld_2_ahead(on, cp[i] + ck, b.c[i]);
+    }
+  } else {
+    const bool on = k < n, on1 = k + 16 < n;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b.w[i][j] = 0u;
-    b.c[i] = b.c1[i] = 0u;
-    if (p.wide) {
-      ld_16_ahead(on, wp, b.w[i][0], b.w[i][1], b.w[i][2], b.w[i][3]);
-      ld_2_ahead(on, cp, b.c[i]);
-    } else {
-      const bool on1 = on && k + 16 < n;
-      ld_8_ahead(on, wp, b.w[i][0], b.w[i][1]);
-      ld_1_ahead(on, cp, b.c[i]);
-      ld_8_ahead(on1, wp + 8, b.w[i][2], b.w[i][3]);
-      ld_1_ahead(on1, cp + 1, b.c1[i]);
+    for (int i = 0; i < 2 * kMT; ++i) {
+      uint32_t c0 = 0u, c1 = 0u;
+      ld_8_ahead(on, wp[i] + wk, b.w[i][0], b.w[i][1]);
+      ld_8_ahead(on1, wp[i] + wk + 8, b.w[i][2], b.w[i][3]);
+      ld_1_ahead(on, cp[i] + ck, c0);
+      ld_1_ahead(on1, cp[i] + ck + 1, c1);
+      b.c[i] = c0 | c1 << 8;
     }
   }
 }
@@ -76,17 +79,6 @@ __global__ void __launch_bounds__(kThreads, 2) project_decode_kernel(const __gri
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int64_t n = p.w.n, f0 = (int64_t)blockIdx.x * (16 * kMT);
   constexpr int kOuts = 16 * kMT * 8 * kNT;
-  // the adapters' rows that the end will need, on their way to L2
-  for (int i = threadIdx.x; i < kOuts; i += kThreads) {
-    const int t = i / (16 * kMT);
-    const int64_t f = f0 + i % (16 * kMT);
-    const int a = t < p.tokens && f < p.w.m ? adapter_of(p.ad, t) : -1;
-    if (a >= 0) {
-      const char* b = reinterpret_cast<const char*>(p.ad.b + ((int64_t)a * p.w.m + f) * p.ad.rank);
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(b));
-      if (p.ad.rank > 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(b + p.ad.rank * 2 - 2));
-    }
-  }
   float acc[kMT][kNT][4];
 #pragma unroll
   for (int i = 0; i < kMT; ++i)
@@ -96,29 +88,44 @@ __global__ void __launch_bounds__(kThreads, 2) project_decode_kernel(const __gri
       for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
 
   constexpr int64_t kStep = kWarps * 128;
+  const uint8_t *wp[2 * kMT], *cp[2 * kMT];
+#pragma unroll
+  for (int i = 0; i < 2 * kMT; ++i) {
+    const int64_t f = min(f0 + g + 8 * i, p.w.m - 1);
+    wp[i] = p.w.packed + f * (n >> 1), cp[i] = p.w.codes + f * (n >> 4);
+  }
+  const uint16_t* xp[kNT];
+#pragma unroll
+  for (int j = 0; j < kNT; ++j) xp[j] = p.x + min(8 * j + g, p.tokens - 1) * p.ld_x;
   int64_t k = (int64_t)warp * 128 + 32 * q;  // this lane's 32 of the warp's block
-  const int64_t kend = n + 32 * q;           // the block begins below n
+  // what a block past the end leaves in the ring is multiplied by x's zeros there, and any word is a finite weight
   Block<kMT> ring[2];
-  load_block<kMT>(p, f0 + g, k, ring[0]);
-  while (k < kend) {
+#pragma unroll
+  for (int i = 0; i < 2 * kMT; ++i) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ring[0].w[i][e] = ring[1].w[i][e] = 0u;
+    ring[0].c[i] = ring[1].c[i] = 0u;
+  }
+  load_block<kMT>(wp, cp, k, n, p.wide, ring[0]);
+  for (int64_t kb = (int64_t)warp * 128; kb < n;) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      if (k >= kend) break;
-      load_block<kMT>(p, f0 + g, k + kStep, ring[u ^ 1]);
+      if (kb >= n) break;
+      load_block<kMT>(wp, cp, k + kStep, n, p.wide, ring[u ^ 1]);
       Block<kMT>& b = ring[u];
       uint32_t scale[2 * kMT];
 #pragma unroll
-      for (int i = 0; i < 2 * kMT; ++i) scale[i] = unpack_codes(b.c[i] | b.c1[i] << 8);
+      for (int i = 0; i < 2 * kMT; ++i) scale[i] = unpack_codes(b.c[i]);
+      const bool whole = kb + 128 <= n;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t xb[kNT][4];
 #pragma unroll
         for (int j = 0; j < kNT; ++j) {
-          const int t = 8 * j + g;
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (t < p.tokens && k + 8 * i < n) v = ld_nc_v4(p.x + t * p.ld_x + k + 8 * i);
-          xb[j][0] = __byte_perm(v.x, v.z, 0x5410), xb[j][1] = __byte_perm(v.x, v.z, 0x7632);
-          xb[j][2] = __byte_perm(v.y, v.w, 0x5410), xb[j][3] = __byte_perm(v.y, v.w, 0x7632);
+          uint32_t v[4] = {0u, 0u, 0u, 0u};
+          ld_16_ahead(whole || k + 8 * i < n, xp[j] + k + 8 * i, v[0], v[1], v[2], v[3]);
+          xb[j][0] = __byte_perm(v[0], v[2], 0x5410), xb[j][1] = __byte_perm(v[0], v[2], 0x7632);
+          xb[j][2] = __byte_perm(v[1], v[3], 0x5410), xb[j][3] = __byte_perm(v[1], v[3], 0x7632);
         }
 #pragma unroll
         for (int t = 0; t < kMT; ++t) {
@@ -134,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, 2) project_decode_kernel(const __gri
           }
         }
       }
-      k += kStep;
+      k += kStep, kb += kStep;
     }
   }
 #pragma unroll
@@ -172,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, 2) project_decode_kernel(const __gri
 }
 
 template <int kMT, int kNT>
-cudaError_t launch(const DecodeArgs& p, cudaStream_t stream) {
+cudaError_t launch(const DecodeArgs& p, bool early, cudaStream_t stream) {
   auto kernel = project_decode_kernel<kMT, kNT>;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((p.w.m + 16 * kMT - 1) / (16 * kMT)), 1, 1);
@@ -182,7 +189,7 @@ cudaError_t launch(const DecodeArgs& p, cudaStream_t stream) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = p.chained ? 1 : 0;
+  cfg.numAttrs = early ? 1 : 0;
   const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, p);
   return err != cudaSuccess ? err : cudaGetLastError();
 }
@@ -200,8 +207,12 @@ cudaError_t launch_project_decode(const void* x, int64_t tokens, int64_t ld_x, c
   p.wide = w.n % 32 == 0 && reinterpret_cast<uintptr_t>(w.packed) % 16 == 0 && reinterpret_cast<uintptr_t>(w.codes) % 2 == 0;
   // 32 outputs a CTA (x is read once for them) where that fills the SMs twice, else 16
   const bool two = (w.m + 31) / 32 >= 2 * info.sm_count;
-  if (tokens <= 8) return two ? launch<2, 1>(p, stream) : launch<1, 1>(p, stream);
-  return two ? launch<2, 2>(p, stream) : launch<1, 2>(p, stream);
+  // Beside the kernel that makes z (chained launch) where x fits the L1 that that kernel's shared memory leaves: an SM
+  // keeps its split while a CTA of it is resident (16 tokens of 16 adapters on 28672 x 8192: 94 us beside it, 76
+  // behind it; one token on 4096 x 4096: 13.2 and 16.5)
+  const bool early = p.chained && tokens * w.n <= 8192;
+  if (tokens <= 8) return two ? launch<2, 1>(p, early, stream) : launch<1, 1>(p, early, stream);
+  return two ? launch<2, 2>(p, early, stream) : launch<1, 2>(p, early, stream);
 }
 
 }  // namespace hscale
