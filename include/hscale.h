@@ -503,8 +503,8 @@ int hscale_gptq_hscale(const void* w_bf16, int64_t m, int64_t n, const float* U,
  * An element stands for code * 2^E, which is exact in bf16; an element's error is at most half a
  * step of its grid.  A block with an Inf or NaN has the scale byte 255 and loads as NaN.
  *
- * x may have any alignment of 2 bytes, codes and scales any; rows of x on 16 bytes and rows of
- * codes on 8 are faster.  Any n.  Zero sizes do nothing.
+ * x may have any alignment of 2 bytes, codes and scales any; rows of x and of
+ * codes on 16 are faster.  Any n.  Zero sizes do nothing.
  */
 typedef enum hscale_checkpoint_format {
   HSCALE_CHECKPOINT_INT8 = 0,

@@ -9,8 +9,8 @@
 // exact in bf16: a load is exact, and kernels that read a checkpoint may feed it to bf16 tensor cores.
 // A block that holds Inf or NaN gets the byte 255 and loads as NaN.
 //
-// Bound by HBM: 2 B in and 1 + 1/32 B out per element for a save, the reverse for a load.  Four lanes
-// share a block, 16 bytes of x each.
+// Bound by HBM: 2 B in and 1 + 1/32 B out per element for a save, the reverse for a load.  Two lanes share a block,
+// 16 elements each, and a thread has kUnroll such pieces in flight.
 #include <algorithm>
 
 #include "hscale_internal.h"
@@ -19,7 +19,8 @@
 namespace hscale {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kUnroll = 2;
+constexpr int kPiece = 16;  // elements a lane
 
 // (row, block) of a flat unit index; 32-bit arithmetic where it reaches
 __device__ __forceinline__ void unit_of(int64_t u, int64_t units, int blocks, int64_t& row, int& blk) {
@@ -27,69 +28,90 @@ __device__ __forceinline__ void unit_of(int64_t u, int64_t units, int blocks, in
   blk = (int)(u - row * blocks);
 }
 
-// RNE to INT8 or E4M3 of v = x 2^-E
+// RNE of four values x 2^-E, within +-top, to bytes
 template <int kFormat>
-__device__ __forceinline__ uint32_t encode(float v) {
-  if (kFormat == kCkptInt8) return (uint32_t)(uint8_t)(int8_t)__float2int_rn(v);
-  uint16_t r;  // satfinite: +-448 at most, which no v exceeds
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(v));
-  return r & 0xFFu;
+__device__ __forceinline__ uint32_t encode4(const float (&v)[4], float inv, float top) {
+  float c[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c[j] = fmaxf(fminf(v[j] * inv, top), -top);
+  if (kFormat == kCkptInt8) {
+    // added to 1.5 2^23, a number is rounded to a whole one whose low byte is the code
+    uint32_t b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = __float_as_uint(c[j] + 12582912.0f);
+    return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  }
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(c[1]), "f"(c[0]));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(c[3]), "f"(c[2]));
+  return (uint32_t)lo | (uint32_t)hi << 16;
 }
 
-// kVec: rows of x are 16-byte and rows of codes 8-byte aligned
+// kVec: rows of x and of codes are 16-byte aligned
 template <int kFormat, bool kVec>
 __global__ void __launch_bounds__(kThreads)
 checkpoint_save_kernel(const uint16_t* __restrict__ x, int64_t tokens, int64_t n, int64_t ld_x, int blocks,
                        uint8_t* __restrict__ codes, int64_t ld_codes, uint8_t* __restrict__ scales,
                        int64_t ld_scales) {
   const int64_t units = tokens * blocks;
-  const int64_t lanes = (units * 4 + 31) / 32 * 32;  // whole warps take part in the shuffles
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < lanes; i += (int64_t)gridDim.x * kThreads) {
-    const int64_t u = i >> 2;
-    const bool on = u < units;
-    int64_t row = 0;
-    int blk = 0;
-    if (on) unit_of(u, units, blocks, row, blk);
-    const int64_t col = (int64_t)blk * kCkptBlock + (i & 3) * 8;
-    const int have = on ? (int)max((int64_t)0, min((int64_t)8, n - col)) : 0;
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    const uint16_t* src = x + row * ld_x + col;
-    if (kVec && have == 8) {
-      const uint4 v = ld_stream_v4(src);
-      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-    } else {
+  const int64_t lanes = (units * 2 + 31) / 32 * 32;  // whole warps take part in the shuffles
+  const int64_t step = (int64_t)gridDim.x * kThreads;
+  for (int64_t i0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; i0 < lanes; i0 += step * kUnroll) {
+    uint32_t w[kUnroll][8];
+    int64_t row[kUnroll];
+    int blk[kUnroll], have[kUnroll];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < have) w[j >> 1] |= (uint32_t)src[j] << (16 * (j & 1));
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t i = i0 + u * step;
+      const bool on = (i >> 1) < units;
+      row[u] = 0, blk[u] = 0;
+      if (on) unit_of(i >> 1, units, blocks, row[u], blk[u]);
+      const int64_t col = (int64_t)blk[u] * kCkptBlock + (i & 1) * kPiece;
+      have[u] = on ? (int)max((int64_t)0, min((int64_t)kPiece, n - col)) : 0;
+      const uint16_t* src = x + row[u] * ld_x + col;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[u][j] = 0u;
+      if (kVec) {
+        ld_16_ahead(have[u] >= 8, src, w[u][0], w[u][1], w[u][2], w[u][3]);
+        ld_16_ahead(have[u] == 16, src + 8, w[u][4], w[u][5], w[u][6], w[u][7]);
+      }
+      if (!kVec || (have[u] & 7) != 0) {
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j)
+          if (j < have[u] && (!kVec || j >= (have[u] & ~7))) w[u][j >> 1] |= (uint32_t)src[j] << (16 * (j & 1));
+      }
     }
-    uint32_t amax = 0;  // bf16 bit patterns order as magnitudes; NaN above Inf
 #pragma unroll
-    for (int j = 0; j < 4; ++j) amax = max(amax, max(w[j] & 0x7FFFu, (w[j] >> 16) & 0x7FFFu));
-    amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-    amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-    int e = (int)(amax >> 7) - 127 - (kFormat == kCkptInt8 ? 6 : 8);
-    if (kFormat == kCkptE4M3 && (amax & 0x7Fu) > 0x60u) ++e;
-    e = max(e, -124);
-    const bool finite = amax < 0x7F80u;
-    // INT8: |v 2^-E| <= 127.5, and 127.5 itself would round to the even 128
-    const float top = kFormat == kCkptInt8 ? 127.0f : e == 120 ? 240.0f : 448.0f;
-    const float inv = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : 0.0f;
-    uint32_t q[2] = {0u, 0u};
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t i = i0 + u * step;
+      uint32_t amax = 0;  // bf16 bit patterns order as magnitudes; NaN above Inf
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float v = (j & 1) ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]);
-      const uint32_t c = finite ? encode<kFormat>(fmaxf(fminf(v * inv, top), -top)) : 0u;
-      q[j >> 2] |= c << (8 * (j & 3));
+      for (int j = 0; j < 8; ++j) amax = __vmaxu2(amax, w[u][j] & 0x7FFF7FFFu);
+      amax = max(amax & 0xFFFFu, amax >> 16);
+      amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+      int e = (int)(amax >> 7) - 127 - (kFormat == kCkptInt8 ? 6 : 8);
+      if (kFormat == kCkptE4M3 && (amax & 0x7Fu) > 0x60u) ++e;
+      e = max(e, -124);
+      const bool finite = amax < 0x7F80u;
+      // INT8: |v 2^-E| <= 127.5, and 127.5 itself would round to the even 128
+      const float top = kFormat == kCkptInt8 ? 127.0f : e == 120 ? 240.0f : 448.0f;
+      const float inv = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : 0.0f;
+      uint32_t q[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float v[4] = {bf16_lo(w[u][2 * j]), bf16_hi(w[u][2 * j]), bf16_lo(w[u][2 * j + 1]), bf16_hi(w[u][2 * j + 1])};
+        q[j] = finite ? encode4<kFormat>(v, inv, top) : 0u;
+      }
+      uint8_t* dst = codes + row[u] * ld_codes + (int64_t)blk[u] * kCkptBlock + (i & 1) * kPiece;
+      if (kVec && have[u] == kPiece) {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(q[0], q[1], q[2], q[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j)
+          if (j < have[u]) dst[j] = (uint8_t)(q[j >> 2] >> (8 * (j & 3)));
+      }
+      if ((i & 1) == 0 && (i >> 1) < units) scales[row[u] * ld_scales + blk[u]] = finite ? (uint8_t)(e + 127) : (uint8_t)255;
     }
-    uint8_t* dst = codes + row * ld_codes + col;
-    if (kVec && have == 8) {
-      *reinterpret_cast<uint2*>(dst) = make_uint2(q[0], q[1]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < have) dst[j] = (uint8_t)(q[j >> 2] >> (8 * (j & 3)));
-    }
-    if (on && (i & 3) == 0) scales[row * ld_scales + blk] = finite ? (uint8_t)(e + 127) : (uint8_t)255;
   }
 }
 
@@ -98,45 +120,62 @@ __global__ void __launch_bounds__(kThreads)
 checkpoint_load_kernel(const uint8_t* __restrict__ codes, int64_t ld_codes, const uint8_t* __restrict__ scales,
                        int64_t ld_scales, int64_t tokens, int64_t n, int blocks, uint16_t* __restrict__ x,
                        int64_t ld_x) {
-  const int64_t units = tokens * blocks;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < units * 4; i += (int64_t)gridDim.x * kThreads) {
-    int64_t row;
-    int blk;
-    unit_of(i >> 2, units, blocks, row, blk);
-    const int64_t col = (int64_t)blk * kCkptBlock + (i & 3) * 8;
-    const int have = (int)max((int64_t)0, min((int64_t)8, n - col));
-    const uint8_t* src = codes + row * ld_codes + col;
-    uint32_t q[2] = {0u, 0u};
-    if (kVec && have == 8) {
-      const uint2 v = __ldcs(reinterpret_cast<const uint2*>(src));
-      q[0] = v.x, q[1] = v.y;
-    } else {
+  const int64_t units = tokens * blocks, step = (int64_t)gridDim.x * kThreads;
+  for (int64_t i0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; i0 < units * 2; i0 += step * kUnroll) {
+    uint32_t q[kUnroll][4], byte[kUnroll];
+    int64_t row[kUnroll], col[kUnroll];
+    int have[kUnroll];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < have) q[j >> 2] |= (uint32_t)src[j] << (8 * (j & 3));
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t i = i0 + u * step;
+      const bool on = i < units * 2;
+      int blk = 0;
+      row[u] = 0;
+      if (on) unit_of(i >> 1, units, blocks, row[u], blk);
+      col[u] = (int64_t)blk * kCkptBlock + (i & 1) * kPiece;
+      have[u] = on ? (int)max((int64_t)0, min((int64_t)kPiece, n - col[u])) : 0;
+      const uint8_t* src = codes + row[u] * ld_codes + col[u];
+      byte[u] = 0u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[u][j] = 0u;
+      ld_1_ahead(on, scales + row[u] * ld_scales + blk, byte[u]);
+      if (kVec) ld_16_ahead(have[u] == kPiece, src, q[u][0], q[u][1], q[u][2], q[u][3]);
+      if (!kVec || have[u] < kPiece) {
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j)
+          if (j < have[u]) q[u][j >> 2] |= (uint32_t)src[j] << (8 * (j & 3));
+      }
     }
-    const uint32_t scale = ckpt_scale(scales[row * ld_scales + blk]);
-    const uint32_t w[4] = {ckpt_values<kFormat, 0>(q[0], scale), ckpt_values<kFormat, 1>(q[0], scale),
-                           ckpt_values<kFormat, 0>(q[1], scale), ckpt_values<kFormat, 1>(q[1], scale)};
-    uint16_t* dst = x + row * ld_x + col;
-    if (kVec && have == 8) {
-      *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < have) dst[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+    for (int u = 0; u < kUnroll; ++u) {
+      const uint32_t scale = ckpt_scale(byte[u]);
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[2 * j] = ckpt_values<kFormat, 0>(q[u][j], scale);
+        w[2 * j + 1] = ckpt_values<kFormat, 1>(q[u][j], scale);
+      }
+      uint16_t* dst = x + row[u] * ld_x + col[u];
+      if (kVec && have[u] == kPiece) {
+        reinterpret_cast<uint4*>(dst)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(dst)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j)
+          if (j < have[u]) dst[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+      }
     }
   }
 }
 
 bool rows_aligned(const void* x, int64_t ld_x, const void* codes, int64_t ld_codes) {
-  return reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld_x % 8 == 0 && reinterpret_cast<uintptr_t>(codes) % 8 == 0 &&
-         ld_codes % 8 == 0;
+  return reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld_x % 8 == 0 && reinterpret_cast<uintptr_t>(codes) % 16 == 0 &&
+         ld_codes % 16 == 0;
 }
 
 unsigned grid_of(int64_t tokens, int blocks, int sms) {
-  const int64_t want = (tokens * blocks * 4 + kThreads - 1) / kThreads;
-  return (unsigned)std::min<int64_t>(want, (int64_t)sms * 8);
+  const int64_t want = (tokens * blocks * 2 + kThreads * kUnroll - 1) / (kThreads * kUnroll);
+  return (unsigned)std::max<int64_t>(1, std::min<int64_t>(want, (int64_t)sms * 8));
 }
 
 }  // namespace
