@@ -561,31 +561,38 @@ def hscale_gptq_workspace_bytes(m: int, n: int, block: int) -> int:
 HSCALE_CHECKPOINT_INT8, HSCALE_CHECKPOINT_E4M3 = 0, 1
 
 
-def hscale_checkpoint_save(x: torch.Tensor, fmt: int, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
-    """Activations x (bf16 [tokens, n]) in 8 bits: codes [tokens, n] and one power-of-two scale byte per
-    32 channels, scales [tokens, ceil(n / 32)] (uint8 views with contiguous rows)."""
+def _view_ld(t: torch.Tensor, name: str, dtype, rows: int, cols: int) -> int:
+    """_row_view for the calls whose cost is latency: the usual case in few steps."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.shape == (rows, cols):
+        ld, step = t.stride()
+        if step == 1 and rows > 1:
+            return ld
+    return _row_view(t, name, dtype, rows, cols)
+
+
+def _checkpoint_views(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> tuple:
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         raise ValueError("x must be a 2-D view")
     tokens, n = x.shape
-    ld_x = _row_view(x, "x", torch.bfloat16, tokens, n)
-    ld_c = _row_view(codes, "codes", torch.uint8, tokens, n)
-    ld_s = _row_view(scales, "scales", torch.uint8, tokens, (n + 31) // 32)
+    return (tokens, n, _view_ld(x, "x", torch.bfloat16, tokens, n), _view_ld(codes, "codes", torch.uint8, tokens, n),
+            _view_ld(scales, "scales", torch.uint8, tokens, (n + 31) // 32))
+
+
+def hscale_checkpoint_save(x: torch.Tensor, fmt: int, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """Activations x (bf16 [tokens, n]) in 8 bits: codes [tokens, n] and one power-of-two scale byte per
+    32 channels, scales [tokens, ceil(n / 32)] (uint8 views with contiguous rows)."""
+    tokens, n, ld_x, ld_c, ld_s = _checkpoint_views(x, codes, scales)
     _check("hscale_checkpoint_save",
-           load().hscale_checkpoint_save(_ptr(x), tokens, n, ld_x, int(fmt), _ptr(codes), ld_c, _ptr(scales), ld_s,
-                                         _stream_ptr(stream)))
+           load().hscale_checkpoint_save(x.data_ptr(), tokens, n, ld_x, int(fmt), codes.data_ptr(), ld_c,
+                                         scales.data_ptr(), ld_s, _stream_ptr(stream)))
 
 
 def hscale_checkpoint_load(codes: torch.Tensor, scales: torch.Tensor, fmt: int, x: torch.Tensor, stream=None) -> None:
     """x (bf16 [tokens, n]) = the values that a checkpoint stands for."""
-    if not isinstance(x, torch.Tensor) or x.dim() != 2:
-        raise ValueError("x must be a 2-D view")
-    tokens, n = x.shape
-    ld_x = _row_view(x, "x", torch.bfloat16, tokens, n)
-    ld_c = _row_view(codes, "codes", torch.uint8, tokens, n)
-    ld_s = _row_view(scales, "scales", torch.uint8, tokens, (n + 31) // 32)
+    tokens, n, ld_x, ld_c, ld_s = _checkpoint_views(x, codes, scales)
     _check("hscale_checkpoint_load",
-           load().hscale_checkpoint_load(_ptr(codes), ld_c, _ptr(scales), ld_s, tokens, n, int(fmt), _ptr(x), ld_x,
-                                         _stream_ptr(stream)))
+           load().hscale_checkpoint_load(codes.data_ptr(), ld_c, scales.data_ptr(), ld_s, tokens, n, int(fmt),
+                                         x.data_ptr(), ld_x, _stream_ptr(stream)))
 
 
 def _whole(t: torch.Tensor, name: str, dtype, shape: tuple) -> None:
@@ -703,8 +710,8 @@ def hscale_project_backward(dy: torch.Tensor, x_codes: torch.Tensor | None, x_sc
         _whole(db, "db", torch.bfloat16, (adapters, m, rank))
     ld_c = ld_s = 0
     if adapters > 0 and (da is not None or db is not None):
-        ld_c = _row_view(x_codes, "x_codes", torch.uint8, tokens, n)
-        ld_s = _row_view(x_scales, "x_scales", torch.uint8, tokens, (n + 31) // 32)
+        ld_c = _view_ld(x_codes, "x_codes", torch.uint8, tokens, n)
+        ld_s = _view_ld(x_scales, "x_scales", torch.uint8, tokens, (n + 31) // 32)
     lib = load()
     workspace, nbytes = _project_workspace(
         workspace, lib.hscale_project_backward_workspace_bytes(tokens, m, n, adapters, rank)
