@@ -120,92 +120,139 @@ struct Rows {
 };
 
 // ---------------------------------------------------------------- z and dz
-// A CTA takes kTG groups of 16 kMT tokens; the 8 / kTG warps of a group, and the CTAs of a cluster of csize, split
-// the contracted axis in blocks of 64, kDepth blocks of tokens and factors in flight, each CTA and warp from another place on
-// (all of them reading the same factors at once would queue at one slice of L2).  For each
-// adapter among a group's tokens (in order of their first token) the warps multiply all the group's tokens by it and
-// keep the rows of its own tokens: other rows' results are dropped, never added, so nothing passes from one request to
-// another.  An adapter's factors are read from L2 once per CTA that has it (kTG groups share them through L1), so wide
-// ranks take more tokens a CTA.  Where tokens are few, CTAs `turn` of `turns` share the adapters of the same
-// tokens out.  Warps and ranks are summed in order.
+// A tile is 256 tokens.  Its jobs: 32 tokens (or what is left) of one adapter, wherever in the tile they stand, in order of
+// the adapters' first tokens; so a request's tokens and tokens in any order cost the same, each row is read once, and
+// an adapter's factors once per job.  As an MMA: M = ranks, N = tokens (8 a group, as many groups as the job has),
+// K = the contracted axis in blocks of 64.  CTAs `turn` of `turns` take a tile's jobs in turn; the warps, and the CTAs of a
+// cluster of csize, split K, kDepth blocks in flight each, from different places on (all of them reading the same factors
+// at once would queue at one slice of L2).  Partials are summed in order.
 // kDown: A_a [rank, cols] (contracted axis contiguous); else B_a [cols, rank], whose 8 x 8 blocks are
-// transposed in registers.  kNT: ranks / 8 of one pass.
+// transposed in registers.  kNT: ranks / 8 of a pass.
+constexpr int kTile = 256, kJob = 32;
+constexpr int kDepth = 2;  // two CTAs an SM fit
 struct Split {
   int csize, crank, turns, turn;
 };
-constexpr int kDepth = 2;  // two CTAs an SM fit
-template <int kMT, int kNT>
+struct JobShared {
+  uint16_t token[kJob];  // in the tile
+};
+template <int kNT>
 constexpr int ring_bytes() {  // of a warp: the slots of kDepth blocks (16 bytes a lane each)
-  return kDepth * (4 * kMT + 2 * kNT) * 512;
+  return kDepth * (8 + 2 * kNT) * 512;
 }
-template <int kFormat, bool kDown, int kMT, int kTG, int kNT>
+template <int kNT>
+constexpr int part_bytes() {
+  return kWarps * kJob * 8 * kNT * 4;
+}
+
+template <int kFormat, bool kDown, int kNT>
 __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t tokens, const Adapters& ad, float* z,
-                                            int64_t tile, const Split& sp, float* part, float* mark, uint8_t* rings) {
-  constexpr int kGroup = 16 * kMT, kTok = kTG * kGroup, kSplits = kWarps / kTG;
-  // a row's slots of a block: bf16 two; a checkpoint one of codes, and for all rows together kMT / 2 of scale words
-  constexpr int kPair = kFormat < 0 ? 1024 : 512, kScales = kFormat < 0 ? 0 : 512, kX = 2 * kMT * kPair + kScales;
+                                            int64_t tile, const Split& sp, float* part, JobShared& job, uint8_t* rings) {
+  constexpr int kMR = (kNT + 1) / 2, kPass = 8 * kNT;
+  // a group's slots of a block: bf16 two; a checkpoint one of codes, and for all groups together one of scale words
+  constexpr int kPair = kFormat < 0 ? 1024 : 512, kScales = kFormat < 0 ? 0 : 512, kX = 4 * kPair + kScales;
   constexpr int kBlock = kX + 2 * kNT * 512;
-  static_assert(kDepth * kBlock <= ring_bytes<kMT, kNT>(), "a ring's room");
+  static_assert(kDepth * kBlock <= ring_bytes<kNT>(), "a ring's room");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int tg = warp % kTG, split = warp / kTG;
-  const int64_t t0 = tile * kTok, tw = t0 + tg * kGroup, cols = rows.cols;
+  const int64_t t0 = tile * kTile, cols = rows.cols;
   const int rank = ad.rank;
-  const int mine = lane < kGroup && tw + lane < tokens ? adapter_of(ad, tw + lane) : -1;
-  uint8_t* ring = rings + warp * ring_bytes<kMT, kNT>() + lane * 16;
-  const uint8_t *trow[2 * kMT], *srow[2 * kMT];  // rows past the end are read as the last one; their results have no adapter
-#pragma unroll
-  for (int i = 0; i < 2 * kMT; ++i) {
-    const int64_t t = min(tw + 8 * i + g, tokens - 1);
-    trow[i] = rows.row(t), srow[i] = rows.scale_row(t);
-  }
+  uint8_t* ring = rings + warp * ring_bytes<kNT>() + lane * 16;
   // this warp's blocks of 64: first, first + ways, ...: `count` of them, taken from a place of its own on
-  const int ways = kSplits * sp.csize, blocks = (int)((cols + 63) / 64);
-  const int first = (int)((sp.crank * kSplits + split + tile) % ways);
+  const int ways = kWarps * sp.csize, blocks = (int)((cols + 63) / 64), shift = (int)(tile * sp.turns + sp.turn);
+  const int first = (sp.crank * kWarps + warp + shift) % ways;
   const int count = first < blocks ? (blocks - first + ways - 1) / ways : 0;
-  const int lead = count > 0 ? (int)((tile / ways) % count) : 0;
+  const int lead = count > 0 ? (shift / ways) % count : 0;
   const auto block_at = [&](int i) {
     const int at = i + lead;
     return (int64_t)(first + (at < count ? at : at - count) * ways) * 64;
   };
-  float* out = part + (split * kTok + tg * kGroup) * rank;
-  uint32_t left = __ballot_sync(0xFFFFFFFFu, mine >= 0);
-  for (int nth = 0; left; ++nth) {
-    const int a = __shfl_sync(0xFFFFFFFFu, mine, __ffs(left) - 1);
-    const uint32_t sel = __ballot_sync(0xFFFFFFFFu, mine == a);
-    left &= ~sel;
-    if (nth % sp.turns != sp.turn) continue;
-    for (int r0 = 0; r0 < rank; r0 += 8 * kNT) {
-      float acc[kMT][kNT][4];
+  const int words = (int)min((int64_t)(kTile / 32), (tokens - t0 + 31) / 32);  // of 32 tokens
+  int id[kTile / 32];
+  uint32_t left[kTile / 32], of[kTile / 32];
 #pragma unroll
-      for (int i = 0; i < kMT; ++i)
+  for (int i = 0; i < kTile / 32; ++i) {
+    const int64_t t = t0 + 32 * i + lane;
+    id[i] = t < tokens ? adapter_of(ad, t) : -1;
+  }
 #pragma unroll
-        for (int j = 0; j < kNT; ++j)
+  for (int i = 0; i < kTile / 32; ++i) left[i] = __ballot_sync(0xFFFFFFFFu, id[i] >= 0), of[i] = 0u;
+  int next = 0;                         // the first job of the next adapter
+  int want = sp.turn;                     // the CTA's next job
+  int a = -1, a_first = 0, a_tokens = 0;  // the present adapter, its first job, its tokens
+  for (;; want += sp.turns) {
+    // the adapter that has job `want`
+    bool found = a >= 0 && want < next;
+    while (!found) {
+      a = -1;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+      for (int i = 0; i < kTile / 32; ++i)
+        if (i < words && a < 0 && left[i]) a = __shfl_sync(0xFFFFFFFFu, id[i], __ffs(left[i]) - 1);
+      if (a < 0) break;
+      a_first = next, a_tokens = 0;
+#pragma unroll
+      for (int i = 0; i < kTile / 32; ++i) {
+        if (i >= words) continue;
+        of[i] = __ballot_sync(0xFFFFFFFFu, id[i] == a);
+        left[i] &= ~of[i];
+        a_tokens += __popc(of[i]);
+      }
+      next += (a_tokens + kJob - 1) / kJob;
+      found = want < next;
+    }
+    if (!found) break;  // alike in every warp
+    const int skip = (want - a_first) * kJob, have = min(kJob, a_tokens - skip);
+    if (warp == 0) {
+      int at = -skip;
+#pragma unroll
+      for (int i = 0; i < kTile / 32; ++i) {
+        const int p = at + __popc(of[i] & ((1u << lane) - 1u));
+        if (((of[i] >> lane) & 1u) && p >= 0 && p < kJob) job.token[p] = (uint16_t)(32 * i + lane);
+        at += __popc(of[i]);
+      }
+    }
+    __syncthreads();
+    const int groups = (have + 7) >> 3;
+    const uint8_t *trow[4], *srow[4];
+    bool valid[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      valid[c] = 8 * c + g < have;
+      const int64_t t = t0 + (valid[c] ? (int)job.token[8 * c + g] : 0);
+      trow[c] = rows.row(t), srow[c] = rows.scale_row(t);
+    }
+    for (int r0 = 0; r0 < rank; r0 += kPass) {
+      float acc[kMR][4][4];
+#pragma unroll
+      for (int i = 0; i < kMR; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][c][e] = 0.0f;
       // kDown: this lane's row of A's first tile of 8 ranks; else its first row of B, from its ranks on
       const __nv_bfloat16* factors = kDown ? ad.a + ((int64_t)a * rank + min(r0 + g, rank - 1)) * cols
-                                           : ad.b + ((int64_t)a * cols) * rank + min(r0 + 2 * q, rank - 2);
+                                           : ad.b + (int64_t)a * cols * rank + min(r0 + 2 * q, rank - 2);
       const auto fetch = [&](int i) {
         if (i < count) {
           const int64_t kb = block_at(i);
           uint8_t* dst = ring + (i & (kDepth - 1)) * kBlock;
           const int64_t k[2] = {Rows<kFormat>::group(kb, q, 0), Rows<kFormat>::group(kb, q, 1)};
           const int64_t kin[2] = {min(k[0], cols - 1) & ~(int64_t)7, min(k[1], cols - 1) & ~(int64_t)7};  // inside the row
-          const int have[2] = {rows.bytes(k[0], true), rows.bytes(k[1], true)};
+          const int bytes[2] = {rows.bytes(k[0], true), rows.bytes(k[1], true)};
 #pragma unroll
-          for (int t = 0; t < 2 * kMT; ++t) {
-            uint8_t* slot = dst + t * kPair;
+          for (int c = 0; c < 4; ++c) {
+            if (c >= groups) continue;
+            uint8_t* slot = dst + c * kPair;
             if constexpr (kFormat < 0) {
-              rows.copy(slot, trow[t], kin[0], have[0]);
-              rows.copy(slot + 512, trow[t], kin[1], have[1]);
+              rows.copy(slot, trow[c], kin[0], valid[c] ? bytes[0] : 0);
+              rows.copy(slot + 512, trow[c], kin[1], valid[c] ? bytes[1] : 0);
             } else {
               if (rows.vec == 16) {
-                copy_16(slot, trow[t] + (kin[0] & ~(int64_t)15), have[0] + have[1]);  // cols % 16 == 0
+                copy_16(slot, trow[c] + (kin[0] & ~(int64_t)15), valid[c] ? bytes[0] + bytes[1] : 0);  // cols % 16 == 0
               } else {
-                rows.copy(slot, trow[t], kin[0], have[0]);
-                rows.copy(slot + 8, trow[t], kin[1], have[1]);
+                rows.copy(slot, trow[c], kin[0], valid[c] ? bytes[0] : 0);
+                rows.copy(slot + 8, trow[c], kin[1], valid[c] ? bytes[1] : 0);
               }
-              rows.copy_scale(dst + 2 * kMT * kPair + 4 * t, srow[t], kin[0], have[0] > 0);
+              rows.copy_scale(dst + 4 * kPair + 4 * c, srow[c], kin[0], valid[c] && bytes[0] > 0);
             }
           }
 #pragma unroll
@@ -214,7 +261,7 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
             for (int j = 0; j < kNT; ++j) {
               uint8_t* slot = dst + kX + (h * kNT + j) * 512;
               if constexpr (kDown) {  // cols % 16 == 0
-                const bool on = r0 + 8 * j + g < rank && have[h] > 0;
+                const bool on = r0 + 8 * j + g < rank && bytes[h] > 0;
                 copy_16_l1(slot, factors + (on ? (int64_t)(8 * j) * cols : 0) + kin[h], on ? 16 : 0);
               } else {
                 // register u of the fragment: slots 2 q', 2 q' + 1 are elements 8 q' + 2 u, + 1
@@ -235,72 +282,68 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
         fetch(it + kDepth - 1);
         copies_wait<kDepth - 1>();
         const uint8_t* src = ring + (it & (kDepth - 1)) * kBlock;
-        uint32_t scale[2 * kMT];
+        uint32_t scale[4];
         if constexpr (kFormat >= 0) {
-          const int64_t k = Rows<kFormat>::group(block_at(it), q, 0);
-#pragma unroll
-          for (int t = 0; t < 2 * kMT; ++t)
-            scale[t] = Rows<kFormat>::scale_of(*reinterpret_cast<const uint32_t*>(src + 2 * kMT * kPair + 4 * t), min(k, cols - 1));
+          const int64_t k = min(Rows<kFormat>::group(block_at(it), q, 0), cols - 1);
+          const uint4 words = *reinterpret_cast<const uint4*>(src + 4 * kPair);
+          scale[0] = Rows<kFormat>::scale_of(words.x, k), scale[1] = Rows<kFormat>::scale_of(words.y, k);
+          scale[2] = Rows<kFormat>::scale_of(words.z, k), scale[3] = Rows<kFormat>::scale_of(words.w, k);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          uint4 w[kNT];
+          uint4 w[2 * kMR];
 #pragma unroll
-          for (int j = 0; j < kNT; ++j) {
+          for (int j = 0; j < 2 * kMR; ++j) {
+            w[j] = make_uint4(0u, 0u, 0u, 0u);
+            if (j >= kNT) continue;
             w[j] = *reinterpret_cast<const uint4*>(src + kX + (h * kNT + j) * 512);
             if (!kDown) w[j] = make_uint4(transpose_8x8(w[j].x), transpose_8x8(w[j].y), transpose_8x8(w[j].z), transpose_8x8(w[j].w));
           }
 #pragma unroll
-          for (int i = 0; i < kMT; ++i) {
-            const uint4 lo = Rows<kFormat>::values_of(src + 2 * i * kPair, h, scale[2 * i]);
-            const uint4 hi = Rows<kFormat>::values_of(src + (2 * i + 1) * kPair, h, scale[2 * i + 1]);
-            const uint32_t a0[4] = {lo.x, hi.x, lo.y, hi.y}, a1[4] = {lo.z, hi.z, lo.w, hi.w};
+          for (int c = 0; c < 4; ++c) {
+            if (c >= groups) continue;
+            const uint4 x = Rows<kFormat>::values_of(src + c * kPair, h, scale[c]);
 #pragma unroll
-            for (int j = 0; j < kNT; ++j) {
-              mma_bf16(acc[i][j], a0, w[j].x, w[j].y);
-              mma_bf16(acc[i][j], a1, w[j].z, w[j].w);
+            for (int i = 0; i < kMR; ++i) {
+              const uint32_t a0[4] = {w[2 * i].x, w[2 * i + 1].x, w[2 * i].y, w[2 * i + 1].y};
+              const uint32_t a1[4] = {w[2 * i].z, w[2 * i + 1].z, w[2 * i].w, w[2 * i + 1].w};
+              mma_bf16(acc[i][c], a0, x.x, x.y);
+              mma_bf16(acc[i][c], a1, x.z, x.w);
             }
           }
         }
       }
-      // rows g, g + 8 of each 16; ranks 2 q, 2 q + 1 of each 8
+      // ranks 16 i + g (+ 8), tokens 8 c + 2 q (+ 1): the warps' partials [warp][token][rank of the pass]
+      float* out = part + warp * kJob * kPass;
 #pragma unroll
-      for (int i = 0; i < kMT; ++i)
+      for (int i = 0; i < kMR; ++i)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int t = 16 * i + 8 * e + g;
-          if (!((sel >> t) & 1u)) continue;
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int j = 0; j < kNT; ++j) {
-            const int r = r0 + 8 * j + 2 * q;
-            if (r < rank) *reinterpret_cast<float2*>(out + t * rank + r) = make_float2(acc[i][j][2 * e], acc[i][j][2 * e + 1]);
-          }
-        }
+          for (int e = 0; e < 4; ++e)
+            if (c < groups && 16 * i + 8 * (e >> 1) < kPass)
+              out[(8 * c + 2 * q + (e & 1)) * kPass + 16 * i + 8 * (e >> 1) + g] = acc[i][c][e];
+      __syncthreads();
+      // the warps' partials in order, into the first ones'; then the ranks' in order
+      constexpr int kAll = kJob * kPass;
+      for (int i = threadIdx.x; i < kAll; i += kThreads) {
+        float s = part[i];
+#pragma unroll
+        for (int v = 1; v < kWarps; ++v) s += part[v * kAll + i];
+        part[i] = s;
+      }
+      if (sp.csize > 1) cluster_sync(); else __syncthreads();
+      const int share = kAll / sp.csize;
+      for (int i = sp.crank * share + threadIdx.x; i < (sp.crank + 1) * share; i += kThreads) {
+        const int p = i / kPass, r = r0 + i % kPass;
+        if (p >= have || r >= rank) continue;
+        float s = sp.csize > 1 ? ld_cluster(part + i, 0) : part[i];
+        for (int d = 1; d < sp.csize; ++d) s += ld_cluster(part + i, (uint32_t)d);
+        z[(t0 + job.token[p]) * rank + r] = s * ad.alpha[a];
+      }
+      if (sp.csize > 1) cluster_sync(); else __syncthreads();  // the partials, and the others' shared memory, have been read
     }
-    if (sp.turns > 1) {  // this CTA's tokens
-      if (split == 0 && lane < kGroup && ((sel >> lane) & 1u)) mark[tg * kGroup + lane] = 1.0f;
-    }
   }
-  __syncthreads();
-  // the warps' partials in order, into the first warp's; then the ranks' in order
-  for (int i = threadIdx.x; i < kTok * rank; i += kThreads) {
-    float s = part[i];
-#pragma unroll
-    for (int v = 1; v < kSplits; ++v) s += part[v * kTok * rank + i];
-    part[i] = s;
-  }
-  if (sp.csize > 1) cluster_sync(); else __syncthreads();
-  const int share = (kTok * rank + sp.csize - 1) / sp.csize;
-  for (int i = sp.crank * share + threadIdx.x; i < min(kTok * rank, (sp.crank + 1) * share); i += kThreads) {
-    const int64_t t = t0 + i / rank;
-    if (t >= tokens) continue;
-    const int a = adapter_of(ad, t);
-    if (a < 0 || (sp.turns > 1 && mark[i / rank] == 0.0f)) continue;
-    float s = sp.csize > 1 ? ld_cluster(part + i, 0) : part[i];
-    for (int d = 1; d < sp.csize; ++d) s += ld_cluster(part + i, (uint32_t)d);
-    z[t0 * rank + i] = s * ad.alpha[a];
-  }
-  if (sp.csize > 1) cluster_sync();  // the others' shared memory stays until it has been read
 }
 
 // blockIdx.y: the turns of z (x's rows against A), then those of dz (dy's rows against B), whichever are wanted.
@@ -310,42 +353,37 @@ struct ShrinkArgs {
   float *z, *dz;
   int csize, turns;
 };
-template <int kFormat, int kMT, int kTG, int kNT>
+template <int kFormat, int kNT>
 __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(Rows<kFormat> x, Rows<-1> dy, ShrinkArgs p) {
   extern __shared__ __align__(16) uint8_t shrink_smem[];
-  __shared__ float mark[16 * kMT * kTG];
+  __shared__ JobShared job;
   pdl_launch_dependents();  // the projection's own product needs no z
   const Split sp = {p.csize, p.csize > 1 ? (int)cluster_rank() : 0, p.turns, (int)blockIdx.y % p.turns};
-  float* part = reinterpret_cast<float*>(shrink_smem + kWarps * ring_bytes<kMT, kNT>());
-  if (p.turns > 1) {
-    for (int i = threadIdx.x; i < 16 * kMT * kTG; i += kThreads) mark[i] = 0.0f;
-    __syncthreads();
-  }
+  float* part = reinterpret_cast<float*>(shrink_smem + kWarps * ring_bytes<kNT>());
   const int64_t tile = blockIdx.x / p.csize;
   if (p.z != nullptr && (int)blockIdx.y < p.turns)
-    shrink_tile<kFormat, true, kMT, kTG, kNT>(x, p.tokens, p.ad, p.z, tile, sp, part, mark, shrink_smem);
+    shrink_tile<kFormat, true, kNT>(x, p.tokens, p.ad, p.z, tile, sp, part, job, shrink_smem);
   else if constexpr (kFormat >= 0)  // the forward pass has no dz
-    shrink_tile<-1, false, kMT, kTG, kNT>(dy, p.tokens, p.ad, p.dz, tile, sp, part, mark, shrink_smem);
+    shrink_tile<-1, false, kNT>(dy, p.tokens, p.ad, p.dz, tile, sp, part, job, shrink_smem);
 }
 
-template <int kFormat, int kMT, int kTG, int kNT>
-cudaError_t launch_shrink_of(const Rows<kFormat>& x, const Rows<-1>& dy, ShrinkArgs p, int parts, int sms, cudaStream_t stream) {
-  auto kernel = shrink_kernel<kFormat, kMT, kTG, kNT>;
-  constexpr int kTok = 16 * kMT * kTG;
-  const auto smem_of = [](int rank) { return kWarps * ring_bytes<kMT, kNT>() + kWarps / kTG * kTok * rank * 4; };
-  constexpr int kMostRanks = kNT < 4 ? 8 * kNT : kMT == 1 ? 128 : 64;
-  static_assert(kWarps * ring_bytes<kMT, kNT>() + kWarps / kTG * kTok * kMostRanks * 4 <= 227 * 1024, "shared memory");
-  cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem_of(kMostRanks));
+template <int kFormat, int kNT>
+cudaError_t launch_shrink_of(const Rows<kFormat>& x, const Rows<-1>& dy, ShrinkArgs p, int parts, int jobs, int sms,
+                             cudaStream_t stream) {
+  auto kernel = shrink_kernel<kFormat, kNT>;
+  constexpr int kSmem = kWarps * ring_bytes<kNT>() + part_bytes<kNT>();
+  constexpr int kCtas = kSmem <= 113 * 1024 ? 2 : 1;  // an SM holds
+  cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmem);
   if (err != cudaSuccess) return err;
-  // up to two CTAs an SM: first the contracted axis split (down to one block a warp), then the adapters
-  const int64_t tiles = (p.tokens + kTok - 1) / kTok, cols = std::max(x.cols, dy.cols);
+  // first a CTA for each job, then the contracted axis split (down to one block a warp), while the SMs hold all
+  const int64_t tiles = (p.tokens + kTile - 1) / kTile, cols = std::max(x.cols, dy.cols), room = (int64_t)kCtas * sms;
+  p.turns = (int)std::max<int64_t>(1, std::min<int64_t>(jobs, room / (tiles * parts)));
   p.csize = 1;
-  while (p.csize < 8 && tiles * parts * p.csize * 2 <= 2 * sms && (int64_t)p.csize * (kWarps / kTG) * 64 < cols) p.csize *= 2;
-  p.turns = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)p.ad.count, (int64_t)kTok, 2 * sms / (tiles * parts * p.csize)}));
+  while (p.csize < 8 && tiles * parts * p.turns * p.csize * 2 <= room && (int64_t)p.csize * kWarps * 64 < cols) p.csize *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * p.csize), (unsigned)(parts * p.turns), 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
-  cfg.dynamicSmemBytes = (size_t)smem_of(p.ad.rank);
+  cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -362,22 +400,13 @@ cudaError_t launch_shrink(const Rows<kFormat>& x, const Rows<-1>& dy, const Shri
   DeviceInfo info;
   const cudaError_t err = current_device_info(&info);
   if (err != cudaSuccess) return err;
-  const int sms = info.sm_count;
-  // tokens a CTA: as many as still give two CTAs an SM with the axis split eight ways, up to 32, or 128 for wide
-  // ranks, whose factors weigh more than the tokens
-  const auto fits = [&](int tok) { return p.tokens / tok * 8 * parts >= 2 * sms; };
-  const int rank = p.ad.rank;
-  if (rank > 64) return launch_shrink_of<kFormat, 1, 1, 4>(x, dy, p, parts, sms, stream);  // the partials' room
-  if (rank > 16 && fits(128)) return launch_shrink_of<kFormat, 2, 4, 4>(x, dy, p, parts, sms, stream);
-  if (rank > 16 && fits(64)) return launch_shrink_of<kFormat, 2, 2, 4>(x, dy, p, parts, sms, stream);
-  if (fits(32)) {
-    if (rank <= 8) return launch_shrink_of<kFormat, 2, 1, 1>(x, dy, p, parts, sms, stream);
-    if (rank <= 16) return launch_shrink_of<kFormat, 2, 1, 2>(x, dy, p, parts, sms, stream);
-    return launch_shrink_of<kFormat, 2, 1, 4>(x, dy, p, parts, sms, stream);
-  }
-  if (rank <= 8) return launch_shrink_of<kFormat, 1, 1, 1>(x, dy, p, parts, sms, stream);
-  if (rank <= 16) return launch_shrink_of<kFormat, 1, 1, 2>(x, dy, p, parts, sms, stream);
-  return launch_shrink_of<kFormat, 1, 1, 4>(x, dy, p, parts, sms, stream);
+  const int sms = info.sm_count, rank = p.ad.rank;
+  // jobs that a tile may have: its adapters are not known here
+  const int64_t tok = std::min<int64_t>(p.tokens, kTile);
+  const int jobs = (int)std::min<int64_t>(tok, (tok + kJob - 1) / kJob + std::min<int64_t>(p.ad.count, tok) - 1);
+  if (rank <= 8) return launch_shrink_of<kFormat, 1>(x, dy, p, parts, jobs, sms, stream);
+  if (rank <= 16) return launch_shrink_of<kFormat, 2>(x, dy, p, parts, jobs, sms, stream);
+  return launch_shrink_of<kFormat, 4>(x, dy, p, parts, jobs, sms, stream);
 }
 
 // ---------------------------------------------------------------- dA and dB
