@@ -88,31 +88,22 @@ struct Rows {
       for (int j = 0; j < 8; ++j) dst[j] = j < bytes ? __ldg(row + k + j) : (uint8_t)0;
     }
   }
-  // the scale byte of element k's block, in the word at dst: byte number scale_at(k)
-  __device__ __forceinline__ void copy_scale(uint8_t* dst, const uint8_t* scale_row, int64_t k, bool on) const {
+  // the scale bytes of the two blocks from element k on (k % 64 == 0), in the word at dst as scale_of finds them
+  __device__ __forceinline__ void copy_scales(uint8_t* dst, const uint8_t* scale_row, int64_t k, bool on) const {
     const int64_t block = k / kCkptBlock;
     if (words) {
       copy_4(dst, scale_row + (block & ~(int64_t)3), on ? 4 : 0);
     } else {
-      *reinterpret_cast<uint32_t*>(dst) = on ? (uint32_t)__ldg(scale_row + block) << (8 * (block & 3)) : 0u;
+      uint32_t two = 0u;
+      if (on) two = (uint32_t)__ldg(scale_row + block);
+      if (on && k + kCkptBlock < cols) two |= (uint32_t)__ldg(scale_row + block + 1) << 8;
+      *reinterpret_cast<uint32_t*>(dst) = two << (8 * (block & 3));
     }
   }
   static __device__ __forceinline__ uint32_t scale_of(uint32_t word, int64_t k) {
     return ckpt_scale((word >> (8 * ((uint32_t)(k / kCkptBlock) & 3u))) & 0xFFu);
   }
-  // A lane's two groups of 8 of the block of 64 elements from kb, for q = 0 .. 3: where they begin
-  static __device__ __forceinline__ int64_t group(int64_t kb, int q, int h) {
-    return kFormat < 0 ? kb + 32 * h + 8 * q : kb + 16 * q + 8 * h;
-  }
-  // group h of a pair (two slots of bf16, one of codes) as 4 x bf16x2; a checkpoint's values are exact in bf16
-  static constexpr int kSlotStep = 512;  // a lane's next slot
-  static __device__ __forceinline__ uint4 values_of(const uint8_t* src, int h, uint32_t scale) {
-    if constexpr (kFormat < 0) {
-      return *reinterpret_cast<const uint4*>(src + h * kSlotStep);
-    } else {
-      return values(*reinterpret_cast<const uint2*>(src + 8 * h), scale);
-    }
-  }
+  // 8 codes as 4 x bf16x2; a checkpoint's values are exact in bf16
   static __device__ __forceinline__ uint4 values(uint2 v, uint32_t scale) {
     return make_uint4(ckpt_values<kFormat, 0>(v.x, scale), ckpt_values<kFormat, 1>(v.x, scale),
                       ckpt_values<kFormat, 0>(v.y, scale), ckpt_values<kFormat, 1>(v.y, scale));
@@ -135,10 +126,12 @@ struct Split {
 };
 struct JobShared {
   uint16_t token[kJob];  // in the tile
+  const uint8_t* row[kJob];
+  const uint8_t* scale_row[kJob];
 };
 template <int kNT>
-constexpr int ring_bytes() {  // of a warp: the slots of kDepth blocks (16 bytes a lane each)
-  return kDepth * (8 + 2 * kNT) * 512;
+constexpr int ring_bytes() {  // of a warp, for kDepth blocks: the tokens' 128 bytes each (or 64 and a scale word), the factors
+  return kDepth * (kJob * 128 + 1024 * kNT);
 }
 template <int kNT>
 constexpr int part_bytes() {
@@ -149,14 +142,15 @@ template <int kFormat, bool kDown, int kNT>
 __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t tokens, const Adapters& ad, float* z,
                                             int64_t tile, const Split& sp, float* part, JobShared& job, uint8_t* rings) {
   constexpr int kMR = (kNT + 1) / 2, kPass = 8 * kNT;
-  // a group's slots of a block: bf16 two; a checkpoint one of codes, and for all groups together one of scale words
-  constexpr int kPair = kFormat < 0 ? 1024 : 512, kScales = kFormat < 0 ? 0 : 512, kX = 4 * kPair + kScales;
-  constexpr int kBlock = kX + 2 * kNT * 512;
+  // a block: the tokens' rows of kRowBytes, a checkpoint's scale words, the factors
+  constexpr int kRowBytes = kFormat < 0 ? 128 : 64, kX = kJob * kRowBytes + (kFormat < 0 ? 0 : 128);
+  constexpr int kBlock = kX + 1024 * kNT;
+  constexpr int kOdd = kFormat < 0 ? 4 : 1;  // odd rows of A: pieces elsewhere than the even rows' of the same reads
   static_assert(kDepth * kBlock <= ring_bytes<kNT>(), "a ring's room");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int64_t t0 = tile * kTile, cols = rows.cols;
   const int rank = ad.rank;
-  uint8_t* ring = rings + warp * ring_bytes<kNT>() + lane * 16;
+  uint8_t* ring = rings + warp * ring_bytes<kNT>();
   // this warp's blocks of 64: first, first + ways, ...: `count` of them, taken from a place of its own on
   const int ways = kWarps * sp.csize, blocks = (int)((cols + 63) / 64), shift = (int)(tile * sp.turns + sp.turn);
   const int first = (sp.crank * kWarps + warp + shift) % ways;
@@ -211,15 +205,12 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
       }
     }
     __syncthreads();
-    const int groups = (have + 7) >> 3;
-    const uint8_t *trow[4], *srow[4];
-    bool valid[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      valid[c] = 8 * c + g < have;
-      const int64_t t = t0 + (valid[c] ? (int)job.token[8 * c + g] : 0);
-      trow[c] = rows.row(t), srow[c] = rows.scale_row(t);
+    if (threadIdx.x < kJob) {  // places past the job's tokens copy nothing
+      const int64_t t = t0 + ((int)threadIdx.x < have ? (int)job.token[threadIdx.x] : 0);
+      job.row[threadIdx.x] = rows.row(t), job.scale_row[threadIdx.x] = rows.scale_row(t);
     }
+    __syncthreads();
+    const int groups = (have + 7) >> 3;
     for (int r0 = 0; r0 < rank; r0 += kPass) {
       float acc[kMR][4][4];
 #pragma unroll
@@ -228,66 +219,79 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
         for (int c = 0; c < 4; ++c)
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[i][c][e] = 0.0f;
-      // kDown: this lane's row of A's first tile of 8 ranks; else its first row of B, from its ranks on
-      const __nv_bfloat16* factors = kDown ? ad.a + ((int64_t)a * rank + min(r0 + g, rank - 1)) * cols
-                                           : ad.b + (int64_t)a * cols * rank + min(r0 + 2 * q, rank - 2);
+      const __nv_bfloat16* factors = kDown ? ad.a + ((int64_t)a * rank + r0) * cols : ad.b + (int64_t)a * cols * rank + r0;
+      // One block's copies, 16 bytes a lane, whole rows at a time: a row's 16-byte pieces stand in its 128 (64) bytes as the
+      // reads below have them free of bank conflicts.
       const auto fetch = [&](int i) {
         if (i < count) {
           const int64_t kb = block_at(i);
           uint8_t* dst = ring + (i & (kDepth - 1)) * kBlock;
-          const int64_t k[2] = {Rows<kFormat>::group(kb, q, 0), Rows<kFormat>::group(kb, q, 1)};
-          const int64_t kin[2] = {min(k[0], cols - 1) & ~(int64_t)7, min(k[1], cols - 1) & ~(int64_t)7};  // inside the row
-          const int bytes[2] = {rows.bytes(k[0], true), rows.bytes(k[1], true)};
+          if constexpr (kFormat < 0) {
+            const int piece = lane & 7;
+            const int64_t k = kb + 8 * piece, kin = min(k, cols - 1) & ~(int64_t)7;
+            const int bytes = rows.bytes(k, true);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (c >= groups) continue;
-            uint8_t* slot = dst + c * kPair;
-            if constexpr (kFormat < 0) {
-              rows.copy(slot, trow[c], kin[0], valid[c] ? bytes[0] : 0);
-              rows.copy(slot + 512, trow[c], kin[1], valid[c] ? bytes[1] : 0);
-            } else {
+            for (int n = 0; n < 8; ++n) {
+              if (n >= 2 * groups) continue;
+              const int p = 4 * n + (lane >> 3);
+              copy_16(dst + p * 128 + ((piece ^ ((p & 1) << 2)) << 4), job.row[p] + kin * 2, p < have ? bytes : 0);
+            }
+          } else {
+            const int piece = lane & 3;
+            const int64_t k = kb + 16 * piece, kin = min(k, cols - 1) & ~(int64_t)15;
+            const int bytes = k < cols ? 16 : 0;  // cols % 16 == 0
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              if (n >= groups) continue;
+              const int p = 8 * n + (lane >> 2);
+              uint8_t* slot = dst + p * 64 + (piece << 4);
               if (rows.vec == 16) {
-                copy_16(slot, trow[c] + (kin[0] & ~(int64_t)15), valid[c] ? bytes[0] + bytes[1] : 0);  // cols % 16 == 0
+                copy_16(slot, job.row[p] + kin, p < have ? bytes : 0);
               } else {
-                rows.copy(slot, trow[c], kin[0], valid[c] ? bytes[0] : 0);
-                rows.copy(slot + 8, trow[c], kin[1], valid[c] ? bytes[1] : 0);
+                rows.copy(slot, job.row[p], kin, p < have ? bytes / 2 : 0);
+                rows.copy(slot + 8, job.row[p], kin + 8, p < have ? bytes / 2 : 0);
               }
-              rows.copy_scale(dst + 4 * kPair + 4 * c, srow[c], kin[0], valid[c] && bytes[0] > 0);
+            }
+            // the two blocks of 32 of a token: one word
+            rows.copy_scales(dst + kJob * 64 + 4 * lane, job.scale_row[lane], kb, lane < have);
+          }
+          if constexpr (kDown) {
+            const int piece = lane & 7;
+            const int64_t k = kb + 8 * piece;
+#pragma unroll
+            for (int n = 0; n < 2 * kNT; ++n) {  // cols % 16 == 0
+              const int r = 4 * n + (lane >> 3);
+              const bool on = r0 + r < rank && k < cols;
+              copy_16_l1(dst + kX + r * 128 + ((piece ^ ((r & 1) * kOdd)) << 4), factors + (on ? (int64_t)r * cols + k : 0), on ? 16 : 0);
+            }
+          } else {
+#pragma unroll
+            for (int n = 0; n < 2 * kNT; ++n) {
+              const int at = 32 * n + lane, kk = at / kNT, c = at % kNT, v = (kk >> 3) & 3;
+              const bool on = kb + kk < cols && r0 + 8 * c < rank;
+              const int swizzle = kNT == 4 ? v : kNT == 2 ? (v & 1) | (v & 2) << 1 : v << 1;
+              copy_16_l1(dst + kX + ((at ^ swizzle) << 4), factors + (on ? (kb + kk) * rank + 8 * c : 0), on ? 16 : 0);
             }
           }
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < kNT; ++j) {
-              uint8_t* slot = dst + kX + (h * kNT + j) * 512;
-              if constexpr (kDown) {  // cols % 16 == 0
-                const bool on = r0 + 8 * j + g < rank && bytes[h] > 0;
-                copy_16_l1(slot, factors + (on ? (int64_t)(8 * j) * cols : 0) + kin[h], on ? 16 : 0);
-              } else {
-                // register u of the fragment: slots 2 q', 2 q' + 1 are elements 8 q' + 2 u, + 1
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                  const int64_t kk = kb + 32 * h + (g >> 1) * 8 + 2 * u + (g & 1);
-                  const bool on = r0 + 8 * j + 2 * q < rank && kk < cols;
-                  copy_4(slot + 4 * u, factors + (on ? kk * rank + 8 * j : 0), on ? 4 : 0);
-                }
-              }
-            }
         }
         copies_end();
       };
 #pragma unroll
       for (int i = 0; i < kDepth - 1; ++i) fetch(i);
       for (int it = 0; it < count; ++it) {
+        __syncwarp();  // the stage's last reads
         fetch(it + kDepth - 1);
         copies_wait<kDepth - 1>();
+        __syncwarp();  // every lane's copies
         const uint8_t* src = ring + (it & (kDepth - 1)) * kBlock;
         uint32_t scale[4];
         if constexpr (kFormat >= 0) {
-          const int64_t k = min(Rows<kFormat>::group(block_at(it), q, 0), cols - 1);
-          const uint4 words = *reinterpret_cast<const uint4*>(src + 4 * kPair);
-          scale[0] = Rows<kFormat>::scale_of(words.x, k), scale[1] = Rows<kFormat>::scale_of(words.y, k);
-          scale[2] = Rows<kFormat>::scale_of(words.z, k), scale[3] = Rows<kFormat>::scale_of(words.w, k);
+          const int64_t kb = block_at(it);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t word = *reinterpret_cast<const uint32_t*>(src + kJob * 64 + 4 * (8 * c + g));
+            scale[c] = Rows<kFormat>::scale_of(word, kb + 16 * q);
+          }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -296,13 +300,26 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
           for (int j = 0; j < 2 * kMR; ++j) {
             w[j] = make_uint4(0u, 0u, 0u, 0u);
             if (j >= kNT) continue;
-            w[j] = *reinterpret_cast<const uint4*>(src + kX + (h * kNT + j) * 512);
-            if (!kDown) w[j] = make_uint4(transpose_8x8(w[j].x), transpose_8x8(w[j].y), transpose_8x8(w[j].z), transpose_8x8(w[j].w));
+            if constexpr (kDown) {
+              // the tokens' groups of 8: bf16 from 32 h + 8 q on, a checkpoint's from 16 q + 8 h on
+              const int piece = kFormat < 0 ? 4 * h + q : 2 * q + h;
+              w[j] = *reinterpret_cast<const uint4*>(src + kX + (8 * j + g) * 128 + ((piece ^ ((g & 1) * kOdd)) << 4));
+            } else {
+              // register u: slots 2 q', 2 q' + 1 are elements 8 q' + 2 u, + 1 of the half
+              const int u = lane >> 3, r = lane & 7, kk = 32 * h + (r >> 1) * 8 + 2 * u + (r & 1), v = (kk >> 3) & 3;
+              const int swizzle = kNT == 4 ? v : kNT == 2 ? (v & 1) | (v & 2) << 1 : v << 1;
+              w[j] = load_transposed_x4(smem_addr(src + kX + (((kk * kNT + j) ^ swizzle) << 4)));
+            }
           }
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             if (c >= groups) continue;
-            const uint4 x = Rows<kFormat>::values_of(src + c * kPair, h, scale[c]);
+            const int p = 8 * c + g;
+            uint4 x;
+            if constexpr (kFormat < 0)
+              x = *reinterpret_cast<const uint4*>(src + p * 128 + (((4 * h + q) ^ ((p & 1) << 2)) << 4));
+            else
+              x = Rows<kFormat>::values(*reinterpret_cast<const uint2*>(src + p * 64 + 16 * q + 8 * h), scale[c]);
 #pragma unroll
             for (int i = 0; i < kMR; ++i) {
               const uint32_t a0[4] = {w[2 * i].x, w[2 * i + 1].x, w[2 * i].y, w[2 * i + 1].y};
@@ -313,6 +330,8 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
           }
         }
       }
+      copies_wait<0>();
+      __syncwarp();
       // ranks 16 i + g (+ 8), tokens 8 c + 2 q (+ 1): the warps' partials [warp][token][rank of the pass]
       float* out = part + warp * kJob * kPass;
 #pragma unroll
@@ -351,37 +370,47 @@ struct ShrinkArgs {
   Adapters ad;
   int64_t tokens;
   float *z, *dz;
-  int csize, turns;
+  int csize, turns_z, turns_dz;
 };
 template <int kFormat, int kNT>
 __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(Rows<kFormat> x, Rows<-1> dy, ShrinkArgs p) {
   extern __shared__ __align__(16) uint8_t shrink_smem[];
   __shared__ JobShared job;
   pdl_launch_dependents();  // the projection's own product needs no z
-  const Split sp = {p.csize, p.csize > 1 ? (int)cluster_rank() : 0, p.turns, (int)blockIdx.y % p.turns};
+  const bool is_z = (int)blockIdx.y < p.turns_z;
+  const Split sp = {p.csize, p.csize > 1 ? (int)cluster_rank() : 0, is_z ? p.turns_z : p.turns_dz,
+                    (int)blockIdx.y - (is_z ? 0 : p.turns_z)};
   float* part = reinterpret_cast<float*>(shrink_smem + kWarps * ring_bytes<kNT>());
   const int64_t tile = blockIdx.x / p.csize;
-  if (p.z != nullptr && (int)blockIdx.y < p.turns)
+  if (is_z)
     shrink_tile<kFormat, true, kNT>(x, p.tokens, p.ad, p.z, tile, sp, part, job, shrink_smem);
   else if constexpr (kFormat >= 0)  // the forward pass has no dz
     shrink_tile<-1, false, kNT>(dy, p.tokens, p.ad, p.dz, tile, sp, part, job, shrink_smem);
 }
 
 template <int kFormat, int kNT>
-cudaError_t launch_shrink_of(const Rows<kFormat>& x, const Rows<-1>& dy, ShrinkArgs p, int parts, int jobs, int sms,
-                             cudaStream_t stream) {
+cudaError_t launch_shrink_of(const Rows<kFormat>& x, const Rows<-1>& dy, ShrinkArgs p, int jobs, int sms, cudaStream_t stream) {
   auto kernel = shrink_kernel<kFormat, kNT>;
   constexpr int kSmem = kWarps * ring_bytes<kNT>() + part_bytes<kNT>();
   constexpr int kCtas = kSmem <= 113 * 1024 ? 2 : 1;  // an SM holds
   cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmem);
   if (err != cudaSuccess) return err;
-  // first a CTA for each job, then the contracted axis split (down to one block a warp), while the SMs hold all
+  // first a CTA for each job, z's and dz's by the length of their sums, then the contracted axis split (down to one block a
+  // warp), while the SMs hold all
   const int64_t tiles = (p.tokens + kTile - 1) / kTile, cols = std::max(x.cols, dy.cols), room = (int64_t)kCtas * sms;
-  p.turns = (int)std::max<int64_t>(1, std::min<int64_t>(jobs, room / (tiles * parts)));
+  const int64_t slots = std::max<int64_t>(1, room / tiles);
+  p.turns_z = p.turns_dz = 0;
+  if (p.z != nullptr && p.dz != nullptr) {
+    p.turns_z = (int)std::max<int64_t>(1, std::min<int64_t>(jobs, slots * x.cols / (x.cols + dy.cols)));
+    p.turns_dz = (int)std::max<int64_t>(1, std::min<int64_t>(jobs, slots - p.turns_z));
+  } else {
+    (p.z != nullptr ? p.turns_z : p.turns_dz) = (int)std::min<int64_t>(jobs, slots);
+  }
+  const int turns = p.turns_z + p.turns_dz;
   p.csize = 1;
-  while (p.csize < 8 && tiles * parts * p.turns * p.csize * 2 <= room && (int64_t)p.csize * kWarps * 64 < cols) p.csize *= 2;
+  while (p.csize < 8 && tiles * turns * p.csize * 2 <= room && (int64_t)p.csize * kWarps * 64 < cols) p.csize *= 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * p.csize), (unsigned)(parts * p.turns), 1);
+  cfg.gridDim = dim3((unsigned)(tiles * p.csize), (unsigned)turns, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = stream;
@@ -396,7 +425,7 @@ cudaError_t launch_shrink_of(const Rows<kFormat>& x, const Rows<-1>& dy, ShrinkA
 }
 
 template <int kFormat>
-cudaError_t launch_shrink(const Rows<kFormat>& x, const Rows<-1>& dy, const ShrinkArgs& p, int parts, cudaStream_t stream) {
+cudaError_t launch_shrink(const Rows<kFormat>& x, const Rows<-1>& dy, const ShrinkArgs& p, cudaStream_t stream) {
   DeviceInfo info;
   const cudaError_t err = current_device_info(&info);
   if (err != cudaSuccess) return err;
@@ -404,9 +433,9 @@ cudaError_t launch_shrink(const Rows<kFormat>& x, const Rows<-1>& dy, const Shri
   // jobs that a tile may have: its adapters are not known here
   const int64_t tok = std::min<int64_t>(p.tokens, kTile);
   const int jobs = (int)std::min<int64_t>(tok, (tok + kJob - 1) / kJob + std::min<int64_t>(p.ad.count, tok) - 1);
-  if (rank <= 8) return launch_shrink_of<kFormat, 1>(x, dy, p, parts, jobs, sms, stream);
-  if (rank <= 16) return launch_shrink_of<kFormat, 2>(x, dy, p, parts, jobs, sms, stream);
-  return launch_shrink_of<kFormat, 4>(x, dy, p, parts, jobs, sms, stream);
+  if (rank <= 8) return launch_shrink_of<kFormat, 1>(x, dy, p, jobs, sms, stream);
+  if (rank <= 16) return launch_shrink_of<kFormat, 2>(x, dy, p, jobs, sms, stream);
+  return launch_shrink_of<kFormat, 4>(x, dy, p, jobs, sms, stream);
 }
 
 // ---------------------------------------------------------------- dA and dB
@@ -710,8 +739,7 @@ Rows<kFormat> ckpt_rows(const Checkpoint& c, int64_t cols) {
 
 template <int kFormat>
 cudaError_t backward_products(const Checkpoint& c, int64_t n, const Rows<-1>& dy, const ShrinkArgs& p, cudaStream_t stream) {
-  const int parts = (p.z != nullptr) + (p.dz != nullptr);
-  return launch_shrink<kFormat>(ckpt_rows<kFormat>(c, n), dy, p, parts, stream);
+  return launch_shrink<kFormat>(ckpt_rows<kFormat>(c, n), dy, p, stream);
 }
 template <int kFormat>
 cudaError_t gradients(const Checkpoint& c, int64_t n, const Rows<-1>& dy, const GradArgs& p, cudaStream_t stream) {
@@ -724,13 +752,13 @@ cudaError_t gradients(const Checkpoint& c, int64_t n, const Rows<-1>& dy, const 
 
 cudaError_t launch_adapter_down(const void* x, int64_t ld_x, int64_t tokens, int64_t n, const Adapters& ad, float* z,
                                 cudaStream_t stream) {
-  const ShrinkArgs p = {ad, tokens, z, nullptr, 1, 1};
-  return launch_shrink<-1>(bf16_rows(x, ld_x, n), bf16_rows(nullptr, 0, 0), p, 1, stream);
+  const ShrinkArgs p = {ad, tokens, z, nullptr, 1, 1, 0};
+  return launch_shrink<-1>(bf16_rows(x, ld_x, n), bf16_rows(nullptr, 0, 0), p, stream);
 }
 
 cudaError_t launch_adapter_backward(const Checkpoint& x, int format, int64_t n, const void* dy, int64_t ld_dy, int64_t m,
                                     int64_t tokens, const Adapters& ad, float* z, float* dz, cudaStream_t stream) {
-  const ShrinkArgs p = {ad, tokens, z, dz, 1, 1};
+  const ShrinkArgs p = {ad, tokens, z, dz, 1, 1, 1};
   const Rows<-1> rows = bf16_rows(dy, ld_dy, m);
   return format == kCkptE4M3 ? backward_products<kCkptE4M3>(x, n, rows, p, stream)
                              : backward_products<kCkptInt8>(x, n, rows, p, stream);

@@ -13,10 +13,14 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 8 x 8 bf16 block: lane (g, q) gives row g, columns 2 q, 2 q + 1 and gets rows 2 q, 2 q + 1 of column g.
-__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
-  uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+// 8 x 8 bf16 blocks (rows of 16 bytes) from shared memory, transposed: lane 8 u + r gives the address of row r of block u;
+// lane (g, q) gets rows 2 q, 2 q + 1 of column g of each of the four.
+__device__ __forceinline__ uint4 load_transposed_x4(uint32_t saddr) {
+  uint4 r;
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "r"(saddr)
+               : "memory");
   return r;
 }
 
