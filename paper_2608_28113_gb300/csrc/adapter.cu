@@ -119,7 +119,7 @@ struct Rows {
 // at once would queue at one slice of L2).  Partials are summed in order.
 // kDown: A_a [rank, cols] (contracted axis contiguous); else B_a [cols, rank], whose 8 x 8 blocks are
 // transposed in registers.  kNT: ranks / 8 of a pass.
-constexpr int kTile = 256, kJob = 32;
+constexpr int kTile = 256, kJob = 32, kByToken = 64;
 constexpr int kDepth = 2;  // two CTAs an SM fit
 struct Split {
   int csize, crank, turns, turn;
@@ -170,38 +170,63 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
   }
 #pragma unroll
   for (int i = 0; i < kTile / 32; ++i) left[i] = __ballot_sync(0xFFFFFFFFu, id[i] >= 0), of[i] = 0u;
-  int next = 0;                         // the first job of the next adapter
-  int want = sp.turn;                     // the CTA's next job
-  int a = -1, a_first = 0, a_tokens = 0;  // the present adapter, its first job, its tokens
-  for (;; want += sp.turns) {
-    // the adapter that has job `want`
-    bool found = a >= 0 && want < next;
-    while (!found) {
-      a = -1;
+  int a = -1, a_tokens = 0, skip = 0;  // the present adapter, its tokens, those before the present job
+  const auto take = [&](int who) {  // the tokens of an adapter
+    a = who, a_tokens = 0;
+#pragma unroll
+    for (int i = 0; i < kTile / 32; ++i) {
+      if (i >= words) continue;
+      of[i] = __ballot_sync(0xFFFFFFFFu, id[i] == who);
+      a_tokens += __popc(of[i]);
+    }
+  };
+  // Up to 64 tokens, whose adapters may all differ: token `at` is the CTA's if it is its adapter's first, with all (two at
+  // most) of the adapter's jobs.  Else the adapters are gone through in order, and their jobs counted.
+  const bool by_token = tokens <= kByToken;
+  int at = sp.turn;  // the next token, or the next job
+  int next = 0, a_first = 0;  // the first jobs of the next and the present adapter
+  const auto next_job = [&]() {
+    if (by_token) {
+      if (a >= 0 && skip + kJob < a_tokens) {
+        skip += kJob;
+        return true;
+      }
+      for (; at < (int)tokens; at += sp.turns) {
+        const int who = at < 32 ? __shfl_sync(0xFFFFFFFFu, id[0], at) : __shfl_sync(0xFFFFFFFFu, id[1], at - 32);
+        if (who < 0) continue;
+        take(who);
+        if ((of[0] ? __ffs(of[0]) - 1 : 31 + __ffs(of[1])) != at) continue;
+        at += sp.turns;
+        skip = 0;
+        return true;
+      }
+      return false;
+    }
+    while (a < 0 || at >= next) {
+      int who = -1;
 #pragma unroll
       for (int i = 0; i < kTile / 32; ++i)
-        if (i < words && a < 0 && left[i]) a = __shfl_sync(0xFFFFFFFFu, id[i], __ffs(left[i]) - 1);
-      if (a < 0) break;
-      a_first = next, a_tokens = 0;
+        if (i < words && who < 0 && left[i]) who = __shfl_sync(0xFFFFFFFFu, id[i], __ffs(left[i]) - 1);
+      if (who < 0) return false;
+      take(who);
 #pragma unroll
-      for (int i = 0; i < kTile / 32; ++i) {
-        if (i >= words) continue;
-        of[i] = __ballot_sync(0xFFFFFFFFu, id[i] == a);
-        left[i] &= ~of[i];
-        a_tokens += __popc(of[i]);
-      }
+      for (int i = 0; i < kTile / 32; ++i) left[i] &= ~of[i];
+      a_first = next;
       next += (a_tokens + kJob - 1) / kJob;
-      found = want < next;
     }
-    if (!found) break;  // alike in every warp
-    const int skip = (want - a_first) * kJob, have = min(kJob, a_tokens - skip);
+    skip = (at - a_first) * kJob;
+    at += sp.turns;
+    return true;
+  };
+  while (next_job()) {  // alike in every warp
+    const int have = min(kJob, a_tokens - skip);
     if (warp == 0) {
-      int at = -skip;
+      int before = -skip;
 #pragma unroll
       for (int i = 0; i < kTile / 32; ++i) {
-        const int p = at + __popc(of[i] & ((1u << lane) - 1u));
+        const int p = before + __popc(of[i] & ((1u << lane) - 1u));
         if (((of[i] >> lane) & 1u) && p >= 0 && p < kJob) job.token[p] = (uint16_t)(32 * i + lane);
-        at += __popc(of[i]);
+        before += __popc(of[i]);
       }
     }
     __syncthreads();
@@ -432,7 +457,9 @@ cudaError_t launch_shrink(const Rows<kFormat>& x, const Rows<-1>& dy, const Shri
   const int sms = info.sm_count, rank = p.ad.rank;
   // jobs that a tile may have: its adapters are not known here
   const int64_t tok = std::min<int64_t>(p.tokens, kTile);
-  const int jobs = (int)std::min<int64_t>(tok, (tok + kJob - 1) / kJob + std::min<int64_t>(p.ad.count, tok) - 1);
+  const int jobs = p.tokens <= kByToken && p.ad.count > 1
+                       ? (int)tok
+                       : (int)std::min<int64_t>(tok, (tok + kJob - 1) / kJob + std::min<int64_t>(p.ad.count, tok) - 1);
   if (rank <= 8) return launch_shrink_of<kFormat, 1>(x, dy, p, jobs, sms, stream);
   if (rank <= 16) return launch_shrink_of<kFormat, 2>(x, dy, p, jobs, sms, stream);
   return launch_shrink_of<kFormat, 4>(x, dy, p, jobs, sms, stream);
