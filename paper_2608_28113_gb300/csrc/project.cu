@@ -58,11 +58,14 @@ constexpr int kGo = 16;                          // tiles whose place in the rin
 
 template <int kN>
 struct Tile {
+  // a small batch's loose terms are made beside the MMAs and kept (14336 x 4096, 64 tokens of 64 adapters: 53 -> 49.5 us)
+  static constexpr bool kStash = kN <= 64;
   static constexpr int kStages = kN == 256 ? 4 : kN == 128 ? 5 : 6;
   static constexpr uint32_t kBBytes = kN * kBK * 2;
   static constexpr uint32_t kStageBytes = kTileABytes + kBBytes;
   static constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 /* alignment */ + kBarBytes + kTurnBytes +
-                                         kInfos * kInfoBytes + 1024 /* bad */;
+                                         kInfos * kInfoBytes + 1024 /* bad */ + (kStash ? kN * kBM * 4 : 0);
+
   static constexpr uint32_t kTmemCols = 2 * kN;
 };
 
@@ -137,15 +140,14 @@ __device__ __forceinline__ void unpack_factors(const uint4& q, float (&f)[8]) {
   f[4] = bf16_lo(q.z), f[5] = bf16_hi(q.z), f[6] = bf16_lo(q.w), f[7] = bf16_hi(q.w);
 }
 
-// Results of tokens t0 .. t0 + W - 1 and this lane's output o: v (without the adapters' terms) plus each
-// token's adapter, rounded and stored.  zs: 2 KB of the warp's own.  Eight ranks a pass: each lane
+// Tokens t0 .. t0 + W - 1 and this lane's output o: each loose token's adapter added to v.  zs: 2 KB of the warp's own.  Eight ranks a pass: each lane
 // fetches its token's z into zs, from where every lane reads all of them; z and factors of the next pass are
 // fetched before the present one's products.  Tokens on one adapter share a lane's 8 factors; otherwise
 // the factors of 8 tokens are fetched at once.  A token without an adapter keeps v as it is (no product by
 // zero: the factors may be Inf or NaN).
 // loose: bit j where token t0 + j's term is added here.
 template <bool kForward, int W>
-__device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p, uint32_t loose,
+__device__ __forceinline__ void add_loose(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p, uint32_t loose,
                                        float* zs) {
   const bool on = o < (kForward ? p.w.m : p.w.n);
   int id = -1;
@@ -198,6 +200,11 @@ __device__ __forceinline__ void finish(float (&v)[W], int64_t t0, int64_t o, int
       }
     }
   }
+}
+
+// v rounded and stored.
+template <bool kForward, int W>
+__device__ __forceinline__ void store(const float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p, float* zs) {
   // Rounded, and turned in zs (pairs of tokens, an output a lane) so that a lane stores 8 outputs of a token at once:
   // stores of one output a lane kept the epilogue from the next tile's adapters (8192 x 14336 x 4096, rank 16: 806 us,
   // 727 now)
@@ -459,6 +466,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
   float* zs = reinterpret_cast<float*>(smem + kStages * T::kStageBytes + kBarBytes) + (threadIdx.x >> 5 & 3) * (kTurnBytes / 16);
   uint8_t* info_base = smem + kStages * T::kStageBytes + kBarBytes + kTurnBytes;
   uint32_t* bad = reinterpret_cast<uint32_t*>(info_base + kInfos * kInfoBytes);  // [2][128]
+  float* stash = reinterpret_cast<float*>(bad + 256);                             // [kN][128]
   auto info_of = [&](int i) -> TileInfo& { return *reinterpret_cast<TileInfo*>(info_base + (i % kInfos) * kInfoBytes); };
 
   const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -687,6 +695,20 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
         spoiled = bad[acc * 128 + out_row];
         bad[acc * 128 + out_row] = 0u;  // its next use is two tiles on, behind the next tile's barrier
       }
+      if (T::kStash && adapters && have) {
+        // this rank's columns; eight at a time, whose factors are fetched at once
+        const int own = kN / csize;
+#pragma unroll 1
+        for (int c = crank * own; c < (crank + 1) * own; c += 8) {
+          const uint32_t loose = info.loose[c >> 5] >> (c & 31) & 0xFFu;
+          float v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+          if (loose) add_loose<kForward, 8>(v, (int64_t)tt * kN + c, o, lane, p, loose, zs);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) stash[(c + j) * kBM + out_row] = v[j];
+        }
+      }
       if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i >> 1) & 1u));
       if (!have) continue;
       tc_fence_after_sync();
@@ -712,8 +734,10 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
         if (adapters) spoil<kWide>(q, spoiled, info.index + c);
         float v[kWide];
 #pragma unroll
-        for (int j = 0; j < kWide; ++j) v[j] = __uint_as_float(q[j]) * scale;
-        finish<kForward, kWide>(v, t0, o, lane, p, adapters ? info.loose[c >> 5] >> (c & 31) : 0u, zs);
+        for (int j = 0; j < kWide; ++j)
+          v[j] = T::kStash && adapters ? fmaf(__uint_as_float(q[j]), scale, stash[(c + j) * kBM + out_row]) : __uint_as_float(q[j]) * scale;
+        if (!T::kStash && adapters) add_loose<kForward, kWide>(v, t0, o, lane, p, info.loose[c >> 5] >> (c & 31), zs);
+        store<kForward, kWide>(v, t0, o, lane, p, zs);
       }
     }
     if (!have && lane == 0) atomicOr(failed, 1u);
@@ -866,9 +890,10 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           float sum = 0.0f;
           for (int d = 0; d < csize; ++d)
             sum += d == crank ? mine : inbox[(d * own + c + j) * kBM + out_row];
-          v[j] = sum * scale;
+          v[j] = T::kStash && adapters && have ? fmaf(sum, scale, stash[(col + j) * kBM + out_row]) : sum * scale;
         }
-        finish<kForward, 8>(v, t0, o, lane, p, adapters && have ? info_of(0).loose[col >> 5] >> (col & 31) : 0u, zs);
+        if (!T::kStash && adapters && have) add_loose<kForward, 8>(v, t0, o, lane, p, info_of(0).loose[col >> 5] >> (col & 31), zs);
+        store<kForward, 8>(v, t0, o, lane, p, zs);
       }
     }
   }
