@@ -140,7 +140,8 @@ constexpr int part_bytes() {
 
 template <int kFormat, bool kDown, int kNT>
 __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t tokens, const Adapters& ad, float* z,
-                                            int64_t tile, const Split& sp, float* part, JobShared& job, uint8_t* rings) {
+                                            uint32_t* z_split, float unit, int64_t tile, const Split& sp, float* part,
+                                            JobShared& job, uint8_t* rings) {
   constexpr int kMR = (kNT + 1) / 2, kPass = 8 * kNT;
   // a block: the tokens' rows of kRowBytes, a checkpoint's scale words, the factors
   constexpr int kRowBytes = kFormat < 0 ? 128 : 64, kX = kJob * kRowBytes + (kFormat < 0 ? 0 : 128);
@@ -383,7 +384,14 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
         if (p >= have || r >= rank) continue;
         float s = sp.csize > 1 ? ld_cluster(part + i, 0) : part[i];
         for (int d = 1; d < sp.csize; ++d) s += ld_cluster(part + i, (uint32_t)d);
-        z[(t0 + job.token[p]) * rank + r] = s * ad.alpha[a];
+        s *= ad.alpha[a];
+        const int64_t at = (t0 + job.token[p]) * rank + r;
+        z[at] = s;
+        if (z_split != nullptr) {
+          const float v = s * unit;
+          const uint32_t hi = pack_bf16(v, 0.0f);
+          z_split[at] = hi | pack_bf16(0.0f, v - bf16_lo(hi));
+        }
       }
       if (sp.csize > 1) cluster_sync(); else __syncthreads();  // the partials, and the others' shared memory, have been read
     }
@@ -394,7 +402,9 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
 struct ShrinkArgs {
   Adapters ad;
   int64_t tokens;
+  const float* global_scale;
   float *z, *dz;
+  uint32_t *z_split, *dz_split;
   int csize, turns_z, turns_dz;
 };
 template <int kFormat, int kNT>
@@ -407,10 +417,11 @@ __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(Rows<kFormat> x, Ro
                     (int)blockIdx.y - (is_z ? 0 : p.turns_z)};
   float* part = reinterpret_cast<float*>(shrink_smem + kWarps * ring_bytes<kNT>());
   const int64_t tile = blockIdx.x / p.csize;
+  const float unit = 1.0f / (kWeightUnit * *p.global_scale);
   if (is_z)
-    shrink_tile<kFormat, true, kNT>(x, p.tokens, p.ad, p.z, tile, sp, part, job, shrink_smem);
+    shrink_tile<kFormat, true, kNT>(x, p.tokens, p.ad, p.z, p.z_split, unit, tile, sp, part, job, shrink_smem);
   else if constexpr (kFormat >= 0)  // the forward pass has no dz
-    shrink_tile<-1, false, kNT>(dy, p.tokens, p.ad, p.dz, tile, sp, part, job, shrink_smem);
+    shrink_tile<-1, false, kNT>(dy, p.tokens, p.ad, p.dz, p.dz_split, unit, tile, sp, part, job, shrink_smem);
 }
 
 template <int kFormat, int kNT>
@@ -777,15 +788,16 @@ cudaError_t gradients(const Checkpoint& c, int64_t n, const Rows<-1>& dy, const 
 
 }  // namespace
 
-cudaError_t launch_adapter_down(const void* x, int64_t ld_x, int64_t tokens, int64_t n, const Adapters& ad, float* z,
-                                cudaStream_t stream) {
-  const ShrinkArgs p = {ad, tokens, z, nullptr, 1, 1, 0};
+cudaError_t launch_adapter_down(const void* x, int64_t ld_x, int64_t tokens, int64_t n, const Adapters& ad,
+                                const float* global_scale, float* z, uint32_t* z_split, cudaStream_t stream) {
+  const ShrinkArgs p = {ad, tokens, global_scale, z, nullptr, z_split, nullptr, 1, 1, 0};
   return launch_shrink<-1>(bf16_rows(x, ld_x, n), bf16_rows(nullptr, 0, 0), p, stream);
 }
 
 cudaError_t launch_adapter_backward(const Checkpoint& x, int format, int64_t n, const void* dy, int64_t ld_dy, int64_t m,
-                                    int64_t tokens, const Adapters& ad, float* z, float* dz, cudaStream_t stream) {
-  const ShrinkArgs p = {ad, tokens, z, dz, 1, 1, 1};
+                                    int64_t tokens, const Adapters& ad, const float* global_scale, float* z, float* dz,
+                                    uint32_t* dz_split, cudaStream_t stream) {
+  const ShrinkArgs p = {ad, tokens, global_scale, z, dz, nullptr, dz_split, 1, 1, 1};
   const Rows<-1> rows = bf16_rows(dy, ld_dy, m);
   return format == kCkptE4M3 ? backward_products<kCkptE4M3>(x, n, rows, p, stream)
                              : backward_products<kCkptInt8>(x, n, rows, p, stream);

@@ -450,7 +450,7 @@ int hscale_checkpoint_load(const uint8_t* codes, int64_t ld_codes, const uint8_t
 size_t hscale_project_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t adapters, int64_t rank) {
   (void)m, (void)n;
   if (tokens <= 0 || adapters <= 0 || rank <= 0) return 0;
-  return (size_t)round256(tokens * rank * 4);
+  return 2 * (size_t)round256(tokens * rank * 4);  // z and z_split
 }
 
 int hscale_project(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, const uint8_t* packed,
@@ -467,16 +467,19 @@ int hscale_project(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, 
   const hscale::Nvfp4Weight w = {packed, codes, global_scale, m, n};
   const hscale::Adapters ad = as_adapters(a_bf16, b_bf16, alpha, adapters, rank, adapter_of);
   float* z = static_cast<float*>(workspace);
+  uint32_t* z_split = reinterpret_cast<uint32_t*>(z + need / 8);
   cudaStream_t s = as_stream(stream);
   if (adapters > 0) {
-    const cudaError_t err = hscale::launch_adapter_down(x_bf16, ld_x, tokens, n, ad, z, s);
+    const cudaError_t err = hscale::launch_adapter_down(x_bf16, ld_x, tokens, n, ad, global_scale, z, z_split, s);
     if (err != cudaSuccess) return HSCALE_ERR_CUDA;
   }
-  return from_cuda(hscale::launch_project(true, x_bf16, tokens, ld_x, w, ad, z, y_bf16, ld_y, s));
+  return from_cuda(hscale::launch_project(true, x_bf16, tokens, ld_x, w, ad, z, z_split, y_bf16, ld_y, s));
 }
 
 size_t hscale_project_backward_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t adapters, int64_t rank) {
-  return 2 * hscale_project_workspace_bytes(tokens, m, n, adapters, rank);
+  (void)m, (void)n;
+  if (tokens <= 0 || adapters <= 0 || rank <= 0) return 0;
+  return 3 * (size_t)round256(tokens * rank * 4);  // z, dz and dz_split
 }
 
 int hscale_project_backward(const void* dy_bf16, int64_t tokens, int64_t m, int64_t ld_dy, const uint8_t* x_codes,
@@ -509,14 +512,15 @@ int hscale_project_backward(const void* dy_bf16, int64_t tokens, int64_t m, int6
   const hscale::Adapters ad = as_adapters(a_bf16, b_bf16, alpha, adapters, rank, adapter_of);
   const hscale::Checkpoint x = {x_codes, x_scales, ld_x_codes, ld_x_scales};
   float* z = static_cast<float*>(workspace);
-  float* dz = z + need / 8;
+  float* dz = z + need / 12;
+  uint32_t* dz_split = reinterpret_cast<uint32_t*>(dz + need / 12);
   cudaError_t err = cudaSuccess;
   const bool want_dz = adapters > 0 && (dx_bf16 != nullptr || da_bf16 != nullptr), want_z = grads && db_bf16 != nullptr;
   if (want_dz || want_z)
-    err = hscale::launch_adapter_backward(x, x_format, n, dy_bf16, ld_dy, m, tokens, ad, want_z ? z : nullptr,
-                                          want_dz ? dz : nullptr, s);
+    err = hscale::launch_adapter_backward(x, x_format, n, dy_bf16, ld_dy, m, tokens, ad, global_scale, want_z ? z : nullptr,
+                                          want_dz ? dz : nullptr, want_dz ? dz_split : nullptr, s);
   if (err == cudaSuccess && dx_bf16 != nullptr)
-    err = hscale::launch_project(false, dy_bf16, tokens, ld_dy, w, ad, dz, dx_bf16, ld_dx, s);
+    err = hscale::launch_project(false, dy_bf16, tokens, ld_dy, w, ad, dz, dz_split, dx_bf16, ld_dx, s);
   if (err == cudaSuccess && grads)
     err = hscale::launch_adapter_gradients(x, x_format, n, dy_bf16, ld_dy, m, tokens, ad, z, dz, da_bf16, db_bf16, s);
   return from_cuda(err);

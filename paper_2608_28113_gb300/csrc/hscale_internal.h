@@ -131,12 +131,14 @@ cudaError_t launch_checkpoint_save(const void* x, int64_t tokens, int64_t n, int
                                    int64_t ld_codes, uint8_t* scales, int64_t ld_scales, cudaStream_t stream);
 cudaError_t launch_checkpoint_load(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales,
                                    int64_t tokens, int64_t n, int format, void* x, int64_t ld_x, cudaStream_t stream);
-// z[t] = alpha_a A_a x_t; fp32 [tokens, rank].
-cudaError_t launch_adapter_down(const void* x, int64_t ld_x, int64_t tokens, int64_t n, const Adapters& ad, float* z,
-                                cudaStream_t stream);
-// z[t] of a checkpoint's x, and dz[t] = alpha_a B_a^T dy_t; either may be nullptr.
+// z[t] = alpha_a A_a x_t; fp32 [tokens, rank].  z_split: z / (128 s_g) as a pair of bf16 numbers, hi | lo << 16, for the
+// projection's tensor cores.
+cudaError_t launch_adapter_down(const void* x, int64_t ld_x, int64_t tokens, int64_t n, const Adapters& ad,
+                                const float* global_scale, float* z, uint32_t* z_split, cudaStream_t stream);
+// z[t] of a checkpoint's x, and dz[t] = alpha_a B_a^T dy_t with its dz_split; z or dz and dz_split may be nullptr.
 cudaError_t launch_adapter_backward(const Checkpoint& x, int format, int64_t n, const void* dy, int64_t ld_dy, int64_t m,
-                                    int64_t tokens, const Adapters& ad, float* z, float* dz, cudaStream_t stream);
+                                    int64_t tokens, const Adapters& ad, const float* global_scale, float* z, float* dz,
+                                    uint32_t* dz_split, cudaStream_t stream);
 // dA_a = sum dz_t x_t^T and dB_a = sum dy_t z_t^T over the tokens of each adapter; either may be nullptr.
 cudaError_t launch_adapter_gradients(const Checkpoint& x, int format, int64_t n, const void* dy, int64_t ld_dy, int64_t m,
                                      int64_t tokens, const Adapters& ad, const float* z, const float* dz, void* da, void* db,
@@ -144,7 +146,8 @@ cudaError_t launch_adapter_gradients(const Checkpoint& x, int format, int64_t n,
 // out = W_hat v (forward: v [tokens, n], out [tokens, m]) or W_hat^T v (v [tokens, m], out [tokens, n]),
 // plus each token's adapter applied to z.
 cudaError_t launch_project(bool forward, const void* v, int64_t tokens, int64_t ld_v, const Nvfp4Weight& w,
-                           const Adapters& ad, const float* z, void* out, int64_t ld_out, cudaStream_t stream);
+                           const Adapters& ad, const float* z, const uint32_t* z_split, void* out, int64_t ld_out,
+                           cudaStream_t stream);
 
 // The forward product for up to kDecodeTokens tokens.
 constexpr int64_t kDecodeTokens = 16;

@@ -38,11 +38,10 @@ __device__ __forceinline__ uint32_t unpack_codes(uint32_t c2) {
 
 // Loads that stay where they are written, so that several are in flight, and that leave the registers as they are
 // where `on` is false (a branch around a load would have the result moved, and the move waits for it).
-__device__ __forceinline__ void ld_32_ahead(bool on, const void* p, uint32_t (&r)[8]) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %9, 0;\n\t"
-               "@p ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t}"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
-               : "l"(p), "r"((uint32_t)on));
+__device__ __forceinline__ void ld_32_ahead(const void* p, uint32_t (&r)[8]) {
+  asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "l"(p));
 }
 __device__ __forceinline__ void ld_16_ahead(bool on, const void* p, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"

@@ -75,6 +75,7 @@ struct ProjectArgs {
   Nvfp4Weight w;
   Adapters ad;
   const float* z;
+  const uint32_t* z_split;
   __nv_bfloat16* out;
   int64_t tokens, ld_out;
   int32_t kb_total, tiles_t, tiles_o, csize, chained;
@@ -314,12 +315,12 @@ __device__ __forceinline__ void find_adapters(const ProjectArgs& p, int64_t t0, 
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return __vcmpeq2(w & 0x7F807F80u, 0x7F807F80u); }
 
 // The K block of ranks r0 .. of the list's adapters from e on, by the epilogue's 128 threads: the factors (as the
-// weight's tile) and the z of their tokens (as the tokens' tile; the accumulator is in units of 128 s_g, so z is divided
-// by it), zeros for the other tokens.  Loaded before `acquire` waits for the stage.  bad[output] gets an adapter's bit
+// weight's tile) and the z of their tokens (as the tokens' tile; z_split: the accumulator is in units of 128 s_g), zeros
+// for the other tokens.  Loaded before `acquire` waits for the stage.  bad[output] gets an adapter's bit
 // where a factor is Inf or NaN.
 template <bool kForward, int kN, typename Acquire>
 __device__ __forceinline__ bool adapter_block(const ProjectArgs& p, const TileInfo& info, int e, int r0, int64_t t0, int64_t o0,
-                                              int line, float unit, uint32_t* bad, uint8_t* tile_a, uint8_t* tile_b,
+                                              int line, uint32_t* bad, uint8_t* tile_a, uint8_t* tile_b,
                                               Acquire acquire) {
   constexpr int kRows = (kN + 127) / 128;
   const int rank = p.ad.rank, half = half_ranks(rank), hc = half / 8, per = adapters_a_block(rank);
@@ -348,20 +349,15 @@ __device__ __forceinline__ bool adapter_block(const ProjectArgs& p, const TileIn
   for (int k = 0; k < kRows; ++k) {
     const int t = line + 128 * k, index = info.index[t < kN ? t : 0];
     mine[k] = t < kN && index >= e && index < e + per ? index - e : -1;  // 255: none
-    const float4* src = reinterpret_cast<const float4*>(p.z + (t0 + t) * rank + r0);
+    const uint4* src = reinterpret_cast<const uint4*>(p.z_split + (t0 + t) * rank + r0);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
+      uint4 v0 = make_uint4(0u, 0u, 0u, 0u), v1 = v0;
       if (mine[k] >= 0 && c < hc && r0 + 8 * c < rank) v0 = src[2 * c], v1 = src[2 * c + 1];
-      const float v[8] = {v0.x * unit, v0.y * unit, v0.z * unit, v0.w * unit, v1.x * unit, v1.y * unit, v1.z * unit, v1.w * unit};
-      uint32_t h[4], l[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        h[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-        l[j] = pack_bf16(v[2 * j] - bf16_lo(h[j]), v[2 * j + 1] - bf16_hi(h[j]));
-      }
-      hi[k][c] = make_uint4(h[0], h[1], h[2], h[3]);
-      lo[k][c] = make_uint4(l[0], l[1], l[2], l[3]);
+      hi[k][c] = make_uint4(__byte_perm(v0.x, v0.y, 0x5410), __byte_perm(v0.z, v0.w, 0x5410), __byte_perm(v1.x, v1.y, 0x5410),
+                            __byte_perm(v1.z, v1.w, 0x5410));
+      lo[k][c] = make_uint4(__byte_perm(v0.x, v0.y, 0x7632), __byte_perm(v0.z, v0.w, 0x7632), __byte_perm(v1.x, v1.y, 0x7632),
+                            __byte_perm(v1.z, v1.w, 0x7632));
     }
   }
 #pragma unroll
@@ -683,7 +679,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
               slot_turn ^= 1u << s;
               return mbar_wait_warp(&slot[s], parity);
             };
-            have = adapter_block<kForward, kN>(p, info, e, r0, (int64_t)tt * kN, (int64_t)to * kBM, out_row, 1.0f / scale,
+            have = adapter_block<kForward, kN>(p, info, e, r0, (int64_t)tt * kN, (int64_t)to * kBM, out_row,
                                                bad + acc * 128, tile_a, tile_b, acquire);
             if (have) {
               fence_proxy_async_smem();
@@ -753,7 +749,9 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
     // the next block to load: where its 32 bytes and 4 codes are, and K blocks left in its tile
     int li = -1, left = 0;
     int64_t f = 0, k0 = 0;
-    const uint8_t *wp = nullptr, *cp = nullptr;
+    // Blocks past W's edges are read inside it: outputs past the end are not stored, and past the end of K the tokens'
+    // tile is zeros, which any weight, a finite number, leaves zeros.
+    const uint8_t *wp = nullptr, *cp = nullptr, *last_w = nullptr, *last_c = nullptr;
     const int64_t w_step = kUnpackGroups * (kForward ? (int64_t)kBK / 2 : kBK * (n >> 1));
     const int64_t c_step = kUnpackGroups * (kForward ? (int64_t)kBK / 16 : kBK * (n >> 4));
     const int total = ntiles * kbs;
@@ -762,6 +760,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
       if (left > 0) {
         if (kForward) k0 += kUnpackGroups * kBK; else f += kUnpackGroups * kBK;
         wp += w_step, cp += c_step;
+        if (!kForward && f >= m) wp = last_w, cp = last_c;
         return;
       }
       while (left <= 0 && ++li < ntiles) left += kbs;
@@ -771,24 +770,22 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
       const int64_t kb = kb1 - left;
       f = kForward ? (int64_t)to * kBM + row : kb * kBK + row;
       k0 = kForward ? kb * kBK : (int64_t)to * kBM + (line >> 6) * 64;
-      wp = p.w.packed + f * (n >> 1) + (k0 >> 1);
-      cp = p.w.codes + f * (n >> 4) + (k0 >> 4);
+      const int64_t fin = min(f, m - 1), kin = min(k0, (n - 1) & ~(int64_t)63);
+      wp = p.w.packed + fin * (n >> 1) + (kin >> 1);
+      cp = p.w.codes + fin * (n >> 4) + (kin >> 4);
+      last_w = p.w.packed + (m - 1) * (n >> 1) + (kin >> 1), last_c = p.w.codes + (m - 1) * (n >> 4) + (kin >> 4);
     };
-    uint32_t ring[kAhead][8], codes[kAhead][4];  // codes: one word, or one byte a word
+    uint32_t ring[kAhead][8], codes[kAhead][4] = {};  // codes: one word, or one byte a word
     auto load = [&](uint32_t (&q)[8], uint32_t (&c)[4]) {
-      const bool on = f < m && k0 < n;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q[i] = 0u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c[i] = 0u;
       if (wide) {
-        ld_32_ahead(on, wp, q);
-        ld_4_ahead(on, cp, c[0]);
+        ld_32_ahead(wp, q);
+        ld_4_ahead(true, cp, c[0]);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          ld_8_ahead(on && k0 + 16 * i < n, wp + 8 * i, q[2 * i], q[2 * i + 1]);
-          ld_1_ahead(on && k0 + 16 * i < n, cp + i, c[i]);
+          c[i] = q[2 * i] = q[2 * i + 1] = 0u;
+          ld_8_ahead(k0 + 16 * i < n, wp + 8 * i, q[2 * i], q[2 * i + 1]);
+          ld_1_ahead(k0 + 16 * i < n, cp + i, c[i]);
         }
       }
       advance(kUnpackGroups);
@@ -819,7 +816,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
           break;
         }
         uint8_t* dst = tile_a + s * kTileABytes + line * 128;
-        const uint32_t code = codes[u][0] | codes[u][1] << 8 | codes[u][2] << 16 | codes[u][3] << 24;
+        const uint32_t code = wide ? codes[u][0] : codes[u][0] | codes[u][1] << 8 | codes[u][2] << 16 | codes[u][3] << 24;
         const uint32_t ca = unpack_codes(code & 0xFFFFu), cb = unpack_codes(code >> 16);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -960,14 +957,14 @@ cudaError_t launch(const void* v, int64_t ld_v, ProjectArgs p, int csize, int sm
 }  // namespace
 
 cudaError_t launch_project(bool forward, const void* v, int64_t tokens, int64_t ld_v, const Nvfp4Weight& w, const Adapters& ad,
-                           const float* z, void* out, int64_t ld_out, cudaStream_t stream) {
+                           const float* z, const uint32_t* z_split, void* out, int64_t ld_out, cudaStream_t stream) {
   if (forward && tokens <= kDecodeTokens) return launch_project_decode(v, tokens, ld_v, w, ad, z, out, ld_out, stream);
   DeviceInfo info;
   const cudaError_t err = current_device_info(&info);
   if (err != cudaSuccess) return err;
   const int sms = info.sm_count;
   ProjectArgs p = {};
-  p.w = w, p.ad = ad, p.z = z, p.out = static_cast<__nv_bfloat16*>(out), p.tokens = tokens, p.ld_out = ld_out;
+  p.w = w, p.ad = ad, p.z = z, p.z_split = z_split, p.out = static_cast<__nv_bfloat16*>(out), p.tokens = tokens, p.ld_out = ld_out;
   p.kb_total = (int32_t)(((forward ? w.n : w.m) + kBK - 1) / kBK);
   p.tiles_o = (int32_t)(((forward ? w.m : w.n) + kBM - 1) / kBM);
   p.chained = ad.count > 0;
