@@ -644,7 +644,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
     umma_drain(mma_done);
   } else if (warp < kUnpackWarp0) {
     // columns at a time: the small tiles' loops need the registers that 32 would take
-    constexpr int kWide = kN >= 128 ? 32 : 16;
+    constexpr int kWide = kN == 256 || (!kForward && kN == 128) ? 32 : 16;
     const float scale = *p.w.global_scale * 128.0f;
     const auto find = [&](int i) {
       if (!adapters || warp != 2 || i >= ntiles) return;
