@@ -624,22 +624,38 @@ def _rows(t: torch.Tensor, name: str) -> tuple:
 
 def _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens: int, m: int, n: int):
     """Checks of a packed weight and its adapters; (adapters, rank)."""
+    u8, f32, bf16 = torch.uint8, torch.float32, torch.bfloat16
+    try:  # the usual case, whose cost a small call feels
+        if (n % 16 == 0 and packed.dtype is u8 and codes.dtype is u8 and global_scale.dtype is f32
+                and packed.shape == (m, n // 2) and codes.shape == (m, n // 16)
+                and packed.is_contiguous() and codes.is_contiguous()
+                and packed.is_cuda and codes.is_cuda and global_scale.is_cuda and a is not None):
+            adapters, rank, width = a.shape
+            if (a.dtype is bf16 and b.dtype is bf16 and alpha.dtype is f32 and width == n
+                    and b.shape == (adapters, m, rank) and alpha.shape == (adapters,)
+                    and a.is_contiguous() and b.is_contiguous() and alpha.is_contiguous()
+                    and a.is_cuda and b.is_cuda and alpha.is_cuda
+                    and (adapter_of is None or (adapter_of.dtype is torch.int32 and adapter_of.shape == (tokens,)
+                                                and adapter_of.is_contiguous() and adapter_of.is_cuda))):
+                return adapters, rank
+    except (AttributeError, ValueError):
+        pass
     if n % 16 != 0:
         raise ValueError("n must be a multiple of 16")
-    _whole(packed, "packed", torch.uint8, (m, n // 2))
-    _whole(codes, "codes", torch.uint8, (m, n // 16))
-    _need(global_scale, torch.float32, "global_scale")
+    _whole(packed, "packed", u8, (m, n // 2))
+    _whole(codes, "codes", u8, (m, n // 16))
+    _need(global_scale, f32, "global_scale")
     if a is None:
         if b is not None or alpha is not None or adapter_of is not None:
             raise ValueError("a, b, alpha and adapter_of belong together")
         return 0, 0
-    _need(a, torch.bfloat16, "a")
+    _need(a, bf16, "a")
     if a.dim() != 3:
         raise ValueError("a must be [adapters, rank, n]")
     adapters, rank, _ = a.shape
-    _whole(a, "a", torch.bfloat16, (adapters, rank, n))
-    _whole(b, "b", torch.bfloat16, (adapters, m, rank))
-    _whole(alpha, "alpha", torch.float32, (adapters,))
+    _whole(a, "a", bf16, (adapters, rank, n))
+    _whole(b, "b", bf16, (adapters, m, rank))
+    _whole(alpha, "alpha", f32, (adapters,))
     if adapter_of is not None:
         _whole(adapter_of, "adapter_of", torch.int32, (tokens,))
     return adapters, rank
@@ -669,14 +685,22 @@ def hscale_project(x: torch.Tensor, packed: torch.Tensor, codes: torch.Tensor, g
     if y_rows != tokens:
         raise ValueError("x and y must have the same number of rows")
     adapters, rank = _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens, m, n)
-    lib = load()
-    workspace, nbytes = _project_workspace(
-        workspace, lib.hscale_project_workspace_bytes(tokens, m, n, adapters, rank) if workspace is None else 0,
-        x.device)
-    _check("hscale_project",
-           lib.hscale_project(x.data_ptr(), tokens, n, ld_x, packed.data_ptr(), codes.data_ptr(),
-                              global_scale.data_ptr(), m, _ptr(a), _ptr(b), _ptr(alpha), adapters, rank,
-                              _ptr(adapter_of), y.data_ptr(), ld_y, _ptr(workspace), nbytes, _stream_ptr(stream)))
+    lib = _lib or load()
+    if workspace is None:
+        nbytes = lib.hscale_project_workspace_bytes(tokens, m, n, adapters, rank)
+        workspace = _workspace(nbytes, x.device) if nbytes else None
+    nbytes = 0
+    if workspace is not None:
+        _need(workspace, torch.uint8, "workspace")
+        nbytes = workspace.numel()
+    status = lib.hscale_project(
+        x.data_ptr(), tokens, n, ld_x, packed.data_ptr(), codes.data_ptr(), global_scale.data_ptr(), m,
+        None if a is None else a.data_ptr(), None if b is None else b.data_ptr(),
+        None if alpha is None else alpha.data_ptr(), adapters, rank,
+        None if adapter_of is None else adapter_of.data_ptr(), y.data_ptr(), ld_y,
+        None if workspace is None else workspace.data_ptr(), nbytes, _stream_ptr(stream))
+    if status:
+        raise HScaleError("hscale_project", status)
 
 
 def hscale_project_backward_workspace_bytes(tokens: int, m: int, n: int, adapters: int, rank: int) -> int:

@@ -507,7 +507,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
   const uint32_t quarter = (uint32_t)(warp & 3);
   const uint32_t lane_base = (quarter * 32u) << 16;
   const int out_row = (int)quarter * 32 + lane;
-  bool have = true;  // the cluster's partial is complete
+  bool have = true;  // of the epilogue's warps: no wait has run out
   // the adapters of the CTA's tile i
   auto wait_info = [&](int i) { return mbar_wait_warp(&info_full[i % kInfos], (uint32_t)(i / kInfos) & 1u); };
 
@@ -840,22 +840,25 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
   }
 
   if (csize > 1) {
-    // the ranks' partials: rank d owns columns [d own, (d + 1) own); the ring is free once every rank's MMAs
-    // have completed, and its memory takes [source][column][output]
-    const int own = kN / csize;
+    // The ranks' partials: rank d owns columns [d own, (d + 1) own); the ring is free once every rank's MMAs
+    // have completed, and its memory takes [source][column][output].  All warps but the first two take part, four to a
+    // quarter of tensor memory, eight columns in turn (the epilogue's four alone took 20 us for 256 columns).
+    const int own = kN / csize, share = (warp - 2) >> 2;
     float* inbox = reinterpret_cast<float*>(smem);
+    float* turn = reinterpret_cast<float*>(smem + kN * kBM * 4) + (warp - 2) * (kTurnBytes / 16);
+    static_assert(kN * kBM * 4 + (kThreads / 32 - 2) * (kTurnBytes / 4) <= kStages * T::kStageBytes, "the ring's room");
     tc_fence_before_sync();
     __syncthreads();
+    const bool complete = *failed == 0u;
     cluster_sync();
     tc_fence_after_sync();
-    const bool epilogue = warp >= 2 && warp < kUnpackWarp0;
     int tt, to;
     raster(first, p, tt, to);
-    if (epilogue) {
+    if (warp >= 2) {
       for (int d = 0; d < csize; ++d) {
         if (d == crank) continue;
         const uint32_t base = mapa(smem_addr(inbox + (crank * own) * kBM + out_row), (uint32_t)d);
-        for (int c = 0; c < own; c += 8) {
+        for (int c = 8 * share; c < own; c += 32) {
           uint32_t q[8];
           tmem_ld_32x32b_x8(tmem_d + lane_base + (uint32_t)(d * own + c), q);
           tmem_ld_wait();
@@ -863,34 +866,39 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(base + (uint32_t)((c + j) * kBM * 4)),
-                         "r"(have ? q[j] : 0x7FC00000u)
+                         "r"(complete ? q[j] : 0x7FC00000u)
                          : "memory");
         }
       }
     }
     cluster_sync();
-    if (epilogue) {
+    if (warp >= 2) {
       const float scale = *p.w.global_scale * 128.0f;
+      if (p.chained) pdl_wait_primary();  // z
       const int64_t o = (int64_t)to * kBM + out_row;
-      for (int c = 0; c < own; c += 8) {
+      for (int c = 8 * share; c < own; c += 32) {
         const int64_t t0 = (int64_t)tt * kN + crank * own + c;
+        const int col = crank * own + c;
         uint32_t q[8];
-        tmem_ld_32x32b_x8(tmem_d + lane_base + (uint32_t)(crank * own + c), q);
+        tmem_ld_32x32b_x8(tmem_d + lane_base + (uint32_t)col, q);
         tmem_ld_wait();
         if (t0 >= p.tokens) continue;
-        const int col = crank * own + c;
         if (adds) spoil<8>(q, bad[out_row], info_of(0).index + col);
         float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float mine = have ? __uint_as_float(q[j]) : __int_as_float(0x7FC00000);
-          float sum = 0.0f;
-          for (int d = 0; d < csize; ++d)
-            sum += d == crank ? mine : inbox[(d * own + c + j) * kBM + out_row];
-          v[j] = T::kStash && adapters && have ? fmaf(sum, scale, stash[(col + j) * kBM + out_row]) : sum * scale;
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        for (int d = 0; d < csize; ++d) {
+          const float* src = inbox + (d * own + c) * kBM + out_row;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            v[j] += d != crank ? src[j * kBM] : complete ? __uint_as_float(q[j]) : __int_as_float(0x7FC00000);
         }
-        if (!T::kStash && adapters && have) add_loose<kForward, 8>(v, t0, o, lane, p, info_of(0).loose[col >> 5] >> (col & 31), zs);
-        store<kForward, 8>(v, t0, o, lane, p, zs);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          v[j] = T::kStash && adapters && complete ? fmaf(v[j], scale, stash[(col + j) * kBM + out_row]) : v[j] * scale;
+        if (!T::kStash && adapters && complete)
+          add_loose<kForward, 8>(v, t0, o, lane, p, info_of(0).loose[col >> 5] >> (col & 31), turn);
+        store<kForward, 8>(v, t0, o, lane, p, turn);
       }
     }
   }
@@ -968,19 +976,20 @@ cudaError_t launch_project(bool forward, const void* v, int64_t tokens, int64_t 
   p.kb_total = (int32_t)(((forward ? w.n : w.m) + kBK - 1) / kBK);
   p.tiles_o = (int32_t)(((forward ? w.m : w.n) + kBM - 1) / kBM);
   p.chained = ad.count > 0;
-  // Tokens a tile and CTAs a tile by an estimate of the time: K blocks in a row on the busiest SM, each the
-  // larger of its unpacking (about 300 cycles) and its MMAs (2 cycles a token), and for a cluster its hand-over
-  // (about 10 blocks).
+  // Tokens a tile and CTAs a tile by an estimate of the time: a wave's start and end, and its K blocks one after
+  // another, as fitted to measurements (us, 64 tokens on 4096 x 4096 with 1, 2, 4 CTAs a tile: 22.1, 15.6, 12.0; 256:
+  // 64 tokens a tile 22.6, 128 by two CTAs 18.2; 512 on 4096 x 14336: 83.0 with 128 a tile, 55.3 with 256 by two CTAs).
+  // One CTA a tile is persistent and starts once.  Clusters of eight leave a sixth of the SMs out.
+  constexpr double kStart[4] = {9.0, 9.0, 11.0, 14.0}, kBlock[4] = {0.20, 0.21, 0.27, 0.34};  // 32, 64, 128, 256 tokens
   int best_n = 32, best_c = 1;
   double best = 1e300;
-  for (int kn = 32; kn <= 256; kn *= 2) {
+  for (int i = 0, kn = 32; kn <= 256; ++i, kn *= 2) {
     if (kn > 32 && kn / 2 >= tokens) break;
-    const double tiles = (double)((tokens + kn - 1) / kn) * p.tiles_o;
+    const int64_t tiles = (tokens + kn - 1) / kn * p.tiles_o;
     for (int c = 1; c <= 8 && kn / c >= 8 && c <= p.kb_total; c *= 2) {
-      const double waves = c == 1 ? std::max(1.0, (double)(int64_t)((tiles + sms - 1) / sms))
-                                  : (double)(int64_t)((tiles * c + sms - 1) / sms);
-      const double blocks = waves * ((p.kb_total + c - 1) / c) + (c > 1 ? 10 * waves : 0);
-      const double cost = blocks * std::max(300, 2 * kn);
+      const int64_t room = c == 8 ? sms * 5 / 6 : sms, waves = (tiles * c + room - 1) / room;
+      const double blocks = (double)((p.kb_total + c - 1) / c);
+      const double cost = (c == 1 ? kStart[i] : waves * kStart[i]) + waves * blocks * kBlock[i];
       if (cost < best) best = cost, best_n = kn, best_c = c;
     }
   }
