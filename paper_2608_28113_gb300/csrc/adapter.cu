@@ -119,12 +119,13 @@ struct Rows {
 // at once would queue at one slice of L2).  Partials are summed in order.
 // kDown: A_a [rank, cols] (contracted axis contiguous); else B_a [cols, rank], whose 8 x 8 blocks are
 // transposed in registers.  kNT: ranks / 8 of a pass.
-constexpr int kTile = 256, kJob = 32, kByToken = 64;
+constexpr int kTile = 256, kJob = 32;
 constexpr int kDepth = 2;  // two CTAs an SM fit
 struct Split {
   int csize, crank, turns, turn;
 };
 struct JobShared {
+  int adapter;
   uint16_t token[kJob];  // in the tile
   const uint8_t* row[kJob];
   const uint8_t* scale_row[kJob];
@@ -136,6 +137,68 @@ constexpr int ring_bytes() {  // of a warp, for kDepth blocks: the tokens' 128 b
 template <int kNT>
 constexpr int part_bytes() {
   return kWarps * kJob * 8 * kNT * 4;
+}
+
+// What the CTA's threads, one a token of the tile, tell each other of the tokens' adapters.
+struct TileScratch {
+  alignas(16) int2 seen[kTile];  // the adapters of warp w's tokens, in the order of their first ones, from 32 w on; their tokens
+  int first_job[kTile];     // of those whose first token in the tile is this warp's
+  int adapters[kWarps], jobs[kWarps];
+};
+static_assert(kTile == kThreads && sizeof(TileScratch) <= part_bytes<1>(), "a token a thread");
+
+// (job, place in it) of this thread's token, whose adapter is id; (-1, 0) without one.  Jobs are numbered in the order of the
+// adapters' first tokens.  Every thread of the CTA calls.  (Each warp going through the adapters for itself, with
+// eight ballots each, took dx of 2048 tokens on 32 adapters 8 us longer.)
+__device__ __forceinline__ int2 place_token(int id, int words, int warp, int lane, TileScratch& sh, int& jobs) {
+  const uint32_t before = (1u << lane) - 1u;
+  const uint32_t alike = __match_any_sync(0xFFFFFFFFu, id);
+  const int leader = __ffs(alike) - 1;
+  const bool leads = id >= 0 && leader == lane;
+  const uint32_t leaders = __ballot_sync(0xFFFFFFFFu, leads);
+  const int entry = 32 * warp + __popc(leaders & before);
+  // behind a word's adapters, entries of none
+  sh.seen[leads ? entry : 32 * warp + __popc(leaders) + __popc(~leaders & before)] = leads ? make_int2(id, __popc(alike)) : make_int2(-2, 0);
+  if (lane == 0) sh.adapters[warp] = __popc(leaders);
+  __syncthreads();
+  int ahead = 0, total = 0, first = -1;  // the adapter's tokens in earlier warps, in all, and its first entry
+  for (int w = 0; w < words; ++w) {
+    const int end = 32 * w + sh.adapters[w];
+    int hit = -1, held = 0;
+    for (int k = 32 * w; k < end; k += 4) {
+      const int4 e0 = *reinterpret_cast<const int4*>(&sh.seen[k]), e1 = *reinterpret_cast<const int4*>(&sh.seen[k + 2]);
+      if (e0.x == id) hit = k, held = e0.y;
+      if (e0.z == id) hit = k + 1, held = e0.w;
+      if (e1.x == id) hit = k + 2, held = e1.y;
+      if (e1.z == id) hit = k + 3, held = e1.w;
+    }
+    if (first < 0) first = hit;
+    if (w < warp) ahead += held;
+    total += held;
+  }
+  const bool opens = leads && first == entry;
+  const int own = opens ? (total + kJob - 1) / kJob : 0;
+  int sum = own;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+    if (lane >= d) sum += v;
+  }
+  if (lane == 31) sh.jobs[warp] = sum;
+  __syncthreads();
+  int base = 0;
+  jobs = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w >= words) break;
+    if (w == warp) base = jobs;
+    jobs += sh.jobs[w];
+  }
+  if (opens) sh.first_job[entry] = base + sum - own;
+  __syncthreads();
+  if (id < 0) return make_int2(-1, 0);
+  const int at = ahead + __popc(alike & before);
+  return make_int2(sh.first_job[first] + at / kJob, at % kJob);
 }
 
 template <int kFormat, bool kDown, int kNT>
@@ -161,81 +224,23 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
     const int at = i + lead;
     return (int64_t)(first + (at < count ? at : at - count) * ways) * 64;
   };
-  const int words = (int)min((int64_t)(kTile / 32), (tokens - t0 + 31) / 32);  // of 32 tokens
-  int id[kTile / 32];
-  uint32_t left[kTile / 32], of[kTile / 32];
-#pragma unroll
-  for (int i = 0; i < kTile / 32; ++i) {
-    const int64_t t = t0 + 32 * i + lane;
-    id[i] = t < tokens ? adapter_of(ad, t) : -1;
-  }
-#pragma unroll
-  for (int i = 0; i < kTile / 32; ++i) left[i] = __ballot_sync(0xFFFFFFFFu, id[i] >= 0), of[i] = 0u;
-  int a = -1, a_tokens = 0, skip = 0;  // the present adapter, its tokens, those before the present job
-  const auto take = [&](int who) {  // the tokens of an adapter
-    a = who, a_tokens = 0;
-#pragma unroll
-    for (int i = 0; i < kTile / 32; ++i) {
-      if (i >= words) continue;
-      of[i] = __ballot_sync(0xFFFFFFFFu, id[i] == who);
-      a_tokens += __popc(of[i]);
+  // A thread's token: its job, and its place in it.
+  const int words = (int)min((int64_t)kWarps, (tokens - t0 + 31) / 32);  // of 32 tokens
+  const int64_t mine = t0 + threadIdx.x;
+  const int id = mine < tokens ? adapter_of(ad, mine) : -1;
+  int jobs;
+  const int2 slot = place_token(id, words, warp, lane, reinterpret_cast<TileScratch&>(*part), jobs);
+  for (int at = sp.turn; at < jobs; at += sp.turns) {
+    if (slot.x == at) {
+      job.token[slot.y] = (uint16_t)threadIdx.x;
+      job.row[slot.y] = rows.row(mine), job.scale_row[slot.y] = rows.scale_row(mine);
+      if (slot.y == 0) job.adapter = id;
     }
-  };
-  // Up to 64 tokens, whose adapters may all differ: token `at` is the CTA's if it is its adapter's first, with all (two at
-  // most) of the adapter's jobs.  Else the adapters are gone through in order, and their jobs counted.
-  const bool by_token = tokens <= kByToken;
-  int at = sp.turn;  // the next token, or the next job
-  int next = 0, a_first = 0;  // the first jobs of the next and the present adapter
-  const auto next_job = [&]() {
-    if (by_token) {
-      if (a >= 0 && skip + kJob < a_tokens) {
-        skip += kJob;
-        return true;
-      }
-      for (; at < (int)tokens; at += sp.turns) {
-        const int who = at < 32 ? __shfl_sync(0xFFFFFFFFu, id[0], at) : __shfl_sync(0xFFFFFFFFu, id[1], at - 32);
-        if (who < 0) continue;
-        take(who);
-        if ((of[0] ? __ffs(of[0]) - 1 : 31 + __ffs(of[1])) != at) continue;
-        at += sp.turns;
-        skip = 0;
-        return true;
-      }
-      return false;
-    }
-    while (a < 0 || at >= next) {
-      int who = -1;
-#pragma unroll
-      for (int i = 0; i < kTile / 32; ++i)
-        if (i < words && who < 0 && left[i]) who = __shfl_sync(0xFFFFFFFFu, id[i], __ffs(left[i]) - 1);
-      if (who < 0) return false;
-      take(who);
-#pragma unroll
-      for (int i = 0; i < kTile / 32; ++i) left[i] &= ~of[i];
-      a_first = next;
-      next += (a_tokens + kJob - 1) / kJob;
-    }
-    skip = (at - a_first) * kJob;
-    at += sp.turns;
-    return true;
-  };
-  while (next_job()) {  // alike in every warp
-    const int have = min(kJob, a_tokens - skip);
-    if (warp == 0) {
-      int before = -skip;
-#pragma unroll
-      for (int i = 0; i < kTile / 32; ++i) {
-        const int p = before + __popc(of[i] & ((1u << lane) - 1u));
-        if (((of[i] >> lane) & 1u) && p >= 0 && p < kJob) job.token[p] = (uint16_t)(32 * i + lane);
-        before += __popc(of[i]);
-      }
-    }
+    const int have = __syncthreads_count(slot.x == at);
+    if ((int)threadIdx.x >= have && threadIdx.x < kJob)  // places past the job's tokens copy nothing
+      job.row[threadIdx.x] = rows.row(t0), job.scale_row[threadIdx.x] = rows.scale_row(t0);
     __syncthreads();
-    if (threadIdx.x < kJob) {  // places past the job's tokens copy nothing
-      const int64_t t = t0 + ((int)threadIdx.x < have ? (int)job.token[threadIdx.x] : 0);
-      job.row[threadIdx.x] = rows.row(t), job.scale_row[threadIdx.x] = rows.scale_row(t);
-    }
-    __syncthreads();
+    const int a = job.adapter;
     const int groups = (have + 7) >> 3;
     for (int r0 = 0; r0 < rank; r0 += kPass) {
       float acc[kMR][4][4];
@@ -468,9 +473,7 @@ cudaError_t launch_shrink(const Rows<kFormat>& x, const Rows<-1>& dy, const Shri
   const int sms = info.sm_count, rank = p.ad.rank;
   // jobs that a tile may have: its adapters are not known here
   const int64_t tok = std::min<int64_t>(p.tokens, kTile);
-  const int jobs = p.tokens <= kByToken && p.ad.count > 1
-                       ? (int)tok
-                       : (int)std::min<int64_t>(tok, (tok + kJob - 1) / kJob + std::min<int64_t>(p.ad.count, tok) - 1);
+  const int jobs = (int)std::min<int64_t>(tok, (tok + kJob - 1) / kJob + std::min<int64_t>(p.ad.count, tok) - 1);
   if (rank <= 8) return launch_shrink_of<kFormat, 1>(x, dy, p, jobs, sms, stream);
   if (rank <= 16) return launch_shrink_of<kFormat, 2>(x, dy, p, jobs, sms, stream);
   // more ranks a pass read the rows fewer times, but leave room for one CTA an SM: bf16 rows gain (4096 tokens x 14336, rank
@@ -498,24 +501,23 @@ struct GradShared {
   int counts[16];
   alignas(16) uint8_t scales[2][kChunk][8];
 };
-// Ranks / 16 of a pass and the sets of warps: 64 ranks take the registers of two sets.
-template <int kRT>
-constexpr int grad_sets() { return kRT == 4 ? 2 : 4; }
+// Sets of warps: four and one CTA an SM, or two and two CTAs (more than 32 ranks: two and one, whose registers they take).
+constexpr int grad_ctas(int rt, int sets) { return rt == 4 ? 1 : 4 / sets; }  // an SM holds
 constexpr int kUnitBytes = 2048;  // of rows, in a warp's ring
 template <int kRT>
 constexpr int frag_bytes() { return kChunk / 16 * kRT * 1024; }       // of a chunk: hi and lo, 16 bytes a lane each
 template <int kRT>
 constexpr int zrow_floats() { return 16 * kRT + 4; }                  // a token's z as copied
-template <int kRT>
+template <int kRT, int kSets>
 constexpr int grad_smem_bytes() {
-  return 4 * grad_sets<kRT>() * kUnits * kUnitBytes + 2 * frag_bytes<kRT>() + kChunk * zrow_floats<kRT>() * 4;
+  return 4 * kSets * kUnits * kUnitBytes + 2 * frag_bytes<kRT>() + kChunk * zrow_floats<kRT>() * 4;
 }
 
-template <int kFormat, bool kRankMajor, int kRT>
+template <int kFormat, bool kRankMajor, int kRT, int kSub>
 __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tokens, const Adapters& ad, const float* z,
                                           __nv_bfloat16* out, int64_t col0, int a, int r0, int csize, int crank,
                                           uint8_t* smem, GradShared& sh) {
-  constexpr int kSub = grad_sets<kRT>(), kWarpsG = 4 * kSub, kThreadsG = 32 * kWarpsG;
+  constexpr int kWarpsG = 4 * kSub, kThreadsG = 32 * kWarpsG;
   constexpr int kTurns = kChunk / 16 / kSub;  // a warp's units of a chunk
   constexpr int kZRow = zrow_floats<kRT>();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
@@ -538,6 +540,7 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
   uint8_t* ring = smem + warp * kUnits * kUnitBytes + lane * (kRow / 32);
   uint8_t* frags = smem + kWarpsG * kUnits * kUnitBytes;
   float* zraw = reinterpret_cast<float*>(frags + 2 * frag_bytes<kRT>());
+  bool any = false;  // tokens; alike in a cluster
   for (int64_t w0 = 0; w0 < tokens; w0 += kWindow) {
     int have = (int)min((int64_t)kWindow, tokens - w0);
     if (ad.of_token != nullptr) {
@@ -570,6 +573,7 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
       }
       __syncthreads();
     }
+    any |= have > 0;
     const int all = (have + kChunk - 1) / kChunk, chunks = all > crank ? (all - 1 - crank) / csize + 1 : 0;
     const auto token = [&](int e) { return w0 + (e < have ? (ad.of_token != nullptr ? (int)sh.list[e] : e) : 0); };
     // z and scales of this CTA's chunk c
@@ -678,23 +682,25 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
   // 8 (2 q) + j and 8 (2 q + 1) + j of the warp's 64.  The sets' partials: [set][rank][column].
   constexpr int kSize = 16 * kRT * kPitch;
   float* part = reinterpret_cast<float*>(smem);
-  copies_wait<0>();
-  __syncthreads();  // the partials take the rings' place
-#pragma unroll
-  for (int i = 0; i < kRT; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        part[sub * kSize + (16 * i + 8 * (e >> 1) + g) * kPitch + 64 * (warp & 3) + 8 * (2 * q + (e & 1)) + j] = acc[i][j][e];
-  __syncthreads();
-  for (int i = threadIdx.x; i < kSize; i += kThreadsG) {
-    float s = part[i];
-#pragma unroll
-    for (int v = 1; v < kSub; ++v) s += part[v * kSize + i];
-    part[i] = s;
+  if (any) {
+    copies_wait<0>();
+    __syncthreads();  // the partials take the rings' place
+  #pragma unroll
+    for (int i = 0; i < kRT; ++i)
+  #pragma unroll
+      for (int j = 0; j < 8; ++j)
+  #pragma unroll
+        for (int e = 0; e < 4; ++e)
+          part[sub * kSize + (16 * i + 8 * (e >> 1) + g) * kPitch + 64 * (warp & 3) + 8 * (2 * q + (e & 1)) + j] = acc[i][j][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < kSize; i += kThreadsG) {
+      float s = part[i];
+  #pragma unroll
+      for (int v = 1; v < kSub; ++v) s += part[v * kSize + i];
+      part[i] = s;
+    }
+    if (csize > 1) cluster_sync(); else __syncthreads();
   }
-  if (csize > 1) cluster_sync(); else __syncthreads();
   // a rank finishes a share of the columns
   const int share = (kColumns / 8 + csize - 1) / csize * 8, c0 = crank * share, width = min(share, kColumns - c0);
   for (int i = threadIdx.x; i < 16 * kRT * width; i += kThreadsG) {
@@ -703,9 +709,12 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
     const int r = r0 + rr;
     const int64_t c = col0 + cc;
     if (r >= rank || c >= cols) continue;
-    const float* src = part + rr * kPitch + cc;
-    float s = csize > 1 ? ld_cluster(src, 0) : *src;
-    for (int d = 1; d < csize; ++d) s += ld_cluster(src, (uint32_t)d);
+    float s = 0.0f;
+    if (any) {
+      const float* src = part + rr * kPitch + cc;
+      s = csize > 1 ? ld_cluster(src, 0) : *src;
+      for (int d = 1; d < csize; ++d) s += ld_cluster(src, (uint32_t)d);
+    }
     out[kRankMajor ? ((int64_t)a * rank + r) * cols + c : ((int64_t)a * cols + c) * rank + r] = __float2bfloat16_rn(s);
   }
   if (csize > 1) cluster_sync();
@@ -719,37 +728,32 @@ struct GradArgs {
   __nv_bfloat16 *da, *db;
   int csize, tiles_a;
 };
-template <int kFormat, int kRT>
-__global__ void __launch_bounds__(128 * grad_sets<kRT>(), 1) grad_kernel(Rows<kFormat> x, Rows<-1> dy, GradArgs p) {
+template <int kFormat, int kRT, int kSets>
+__global__ void __launch_bounds__(128 * kSets, grad_ctas(kRT, kSets)) grad_kernel(Rows<kFormat> x, Rows<-1> dy, GradArgs p) {
   extern __shared__ __align__(16) uint8_t grad_smem[];
   __shared__ GradShared sh;
   const int crank = p.csize > 1 ? (int)cluster_rank() : 0, tile = blockIdx.x / p.csize, r0 = blockIdx.z * 16 * kRT;
   if (tile < p.tiles_a)
-    grad_tile<kFormat, true, kRT>(x, p.tokens, p.ad, p.dz, p.da, (int64_t)tile * kColumns, blockIdx.y, r0, p.csize, crank, grad_smem,
+    grad_tile<kFormat, true, kRT, kSets>(x, p.tokens, p.ad, p.dz, p.da, (int64_t)tile * kColumns, blockIdx.y, r0, p.csize, crank, grad_smem,
                                   sh);
   else
-    grad_tile<-1, false, kRT>(dy, p.tokens, p.ad, p.z, p.db, (int64_t)(tile - p.tiles_a) * kColumns, blockIdx.y, r0, p.csize,
+    grad_tile<-1, false, kRT, kSets>(dy, p.tokens, p.ad, p.z, p.db, (int64_t)(tile - p.tiles_a) * kColumns, blockIdx.y, r0, p.csize,
                               crank, grad_smem, sh);
 }
 
-template <int kFormat, int kRT>
-cudaError_t launch_grad_of(const Rows<kFormat>& x, const Rows<-1>& dy, GradArgs p, cudaStream_t stream) {
-  DeviceInfo info;
-  cudaError_t err = current_device_info(&info);
+template <int kFormat, int kRT, int kSets>
+cudaError_t launch_grad_of(const Rows<kFormat>& x, const Rows<-1>& dy, GradArgs p, int64_t tiles, int passes, int sms,
+                           cudaStream_t stream) {
+  auto kernel = grad_kernel<kFormat, kRT, kSets>;
+  constexpr int kCtas = grad_ctas(kRT, kSets);
+  constexpr int kSmem = std::max(kSets * 16 * kRT * kPitch * 4, grad_smem_bytes<kRT, kSets>());
+  static_assert(kCtas * (kSmem + sizeof(GradShared) + 1024) <= 228 * 1024, "shared memory");
+  cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmem);
   if (err != cudaSuccess) return err;
-  auto kernel = grad_kernel<kFormat, kRT>;
-  constexpr int kSets = grad_sets<kRT>();
-  constexpr int kSmem = std::max(kSets * 16 * kRT * kPitch * 4, grad_smem_bytes<kRT>());
-  static_assert(kSmem + sizeof(GradShared) <= 227 * 1024, "shared memory");
-  err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmem);
-  if (err != cudaSuccess) return err;
-  p.tiles_a = p.da != nullptr ? (int)((x.cols + kColumns - 1) / kColumns) : 0;
-  const int64_t tiles = p.tiles_a + (p.db != nullptr ? (dy.cols + kColumns - 1) / kColumns : 0);
-  const int passes = (p.ad.rank + 16 * kRT - 1) / (16 * kRT);
   // the tokens split (by up to four: clusters of eight CTAs that fill an SM each leave many SMs out) while a CTA an
   // SM holds all, and an adapter's share has a chunk of them
   p.csize = 1;
-  while (p.csize < 4 && tiles * p.ad.count * passes * (p.csize + 1) <= info.sm_count &&
+  while (p.csize < 4 && tiles * p.ad.count * passes * (p.csize + 1) <= kCtas * sms &&
          p.tokens / p.ad.count > (int64_t)p.csize * kChunk)
     ++p.csize;
   cudaLaunchConfig_t cfg = {};
@@ -765,6 +769,24 @@ cudaError_t launch_grad_of(const Rows<kFormat>& x, const Rows<-1>& dy, GradArgs 
   cfg.numAttrs = 1;
   err = cudaLaunchKernelEx(&cfg, kernel, x, dy, p);
   return err != cudaSuccess ? err : cudaGetLastError();
+}
+
+template <int kFormat, int kRT>
+cudaError_t launch_grad(const Rows<kFormat>& x, const Rows<-1>& dy, GradArgs p, cudaStream_t stream) {
+  DeviceInfo info;
+  const cudaError_t err = current_device_info(&info);
+  if (err != cudaSuccess) return err;
+  p.tiles_a = p.da != nullptr ? (int)((x.cols + kColumns - 1) / kColumns) : 0;
+  const int64_t tiles = p.tiles_a + (p.db != nullptr ? (dy.cols + kColumns - 1) / kColumns : 0);
+  const int passes = (p.ad.rank + 16 * kRT - 1) / (16 * kRT), sms = info.sm_count;
+  if constexpr (kRT == 4) {
+    return launch_grad_of<kFormat, kRT, 2>(x, dy, p, tiles, passes, sms, stream);
+  } else {
+    // with more CTAs than SMs, two an SM (2048 tokens on 32 adapters, 1024 x 4096: 62 -> 52 us); with fewer, each the faster
+    // the more warps it has (300 tokens on 4, 2048 x 2048: 25.7 us and 24.7)
+    return tiles * p.ad.count * passes > sms ? launch_grad_of<kFormat, kRT, 2>(x, dy, p, tiles, passes, sms, stream)
+                                             : launch_grad_of<kFormat, kRT, 4>(x, dy, p, tiles, passes, sms, stream);
+  }
 }
 
 Rows<-1> bf16_rows(const void* x, int64_t ld, int64_t cols) { return {static_cast<const uint16_t*>(x), ld, {}, cols, 1, false}; }
@@ -784,8 +806,8 @@ cudaError_t backward_products(const Checkpoint& c, int64_t n, const Rows<-1>& dy
 template <int kFormat>
 cudaError_t gradients(const Checkpoint& c, int64_t n, const Rows<-1>& dy, const GradArgs& p, cudaStream_t stream) {
   const Rows<kFormat> x = ckpt_rows<kFormat>(c, n);
-  if (p.ad.rank <= 16) return launch_grad_of<kFormat, 1>(x, dy, p, stream);
-  return p.ad.rank <= 32 ? launch_grad_of<kFormat, 2>(x, dy, p, stream) : launch_grad_of<kFormat, 4>(x, dy, p, stream);
+  if (p.ad.rank <= 16) return launch_grad<kFormat, 1>(x, dy, p, stream);
+  return p.ad.rank <= 32 ? launch_grad<kFormat, 2>(x, dy, p, stream) : launch_grad<kFormat, 4>(x, dy, p, stream);
 }
 
 }  // namespace

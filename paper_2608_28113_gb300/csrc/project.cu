@@ -262,51 +262,63 @@ __device__ __forceinline__ int blocks_of(int listed, int rank) {
 // A K block costs the epilogue's warps about 1500 cycles; a loose token about 112 cycles per 8 ranks forward, where its
 // factors are 16 bytes an output, and 450 backward, where they are 8 loads (eight tokens' factors fetched at once).  An
 // adapter is listed where its tokens' share would cost more than its part of a K block.
+// One pass over the words of 32 tokens: each token's place among the tile's adapters, in order of their first tokens,
+// then the choice (a pass over the tokens for each adapter took 32 adapters 11 us a tile).  seen: 2 KB of the warp's own.
 template <bool kForward, int kN>
-__device__ __forceinline__ void find_adapters(const ProjectArgs& p, int64_t t0, int lane, TileInfo& info) {
-  int id[kN / 32];
-  uint32_t left[kN / 32], loose[kN / 32];
+__device__ __forceinline__ void find_adapters(const ProjectArgs& p, int64_t t0, int lane, TileInfo& info, int* seen) {
+  constexpr int kWords = kN / 32;
+  int* held = seen + 256;  // of each adapter seen: its tokens << 16 | its bits of sel; then its place in the list
+  int at[kWords];          // a token's place in seen, or none
+  int id[kWords];
 #pragma unroll
-  for (int i = 0; i < kN / 32; ++i) {
+  for (int i = 0; i < kWords; ++i) {
     const int64_t t = t0 + 32 * i + lane;
     id[i] = t < p.tokens ? adapter_of(p.ad, t) : -1;
   }
+  int count = 0;  // seen
+  __syncwarp();
 #pragma unroll
-  for (int i = 0; i < kN / 32; ++i) {
-    left[i] = __ballot_sync(0xFFFFFFFFu, id[i] >= 0);
-    loose[i] = left[i];
-    info.index[32 * i + lane] = 255;
+  for (int i = 0; i < kWords; ++i) {
+    at[i] = -1;
+#pragma unroll 4
+    for (int k = 0; k < count; ++k)
+      if (seen[k] == id[i]) at[i] = k;  // none is negative
+    const uint32_t alike = __match_any_sync(0xFFFFFFFFu, id[i]);
+    const bool leads = id[i] >= 0 && __ffs(alike) - 1 == lane;
+    const uint32_t fresh = __ballot_sync(0xFFFFFFFFu, leads && at[i] < 0);
+    if (leads) {
+      const int value = __popc(alike) << 16 | ((alike & 0xFFFFu ? 1 : 0) | (alike >> 16 ? 2 : 0)) << (2 * i);
+      if (at[i] < 0) {
+        at[i] = count + __popc(fresh & ((1u << lane) - 1u));
+        seen[at[i]] = id[i], held[at[i]] = value;
+      } else {
+        held[at[i]] += value;  // another word's bits
+      }
+    }
+    at[i] = __shfl_sync(0xFFFFFFFFu, at[i], __ffs(alike) - 1);
+    count += __popc(fresh);
+    __syncwarp();
   }
   const int block = 1500 * ((p.ad.rank + 31) / 32) / adapters_a_block(p.ad.rank), loose_token = (kForward ? 14 : 56) * p.ad.rank;
   const int enough = (block + loose_token - 1) / loose_token;
   int listed = 0;
-  // the first token left over, its adapter, all its tokens
-#pragma unroll
-  for (int i = 0; i < kN / 32; ++i) {
-    while (left[i] && listed < kMaxListed) {
-      const int a = __shfl_sync(0xFFFFFFFFu, id[i], __ffs(left[i]) - 1);
-      uint32_t of[kN / 32], sel = 0u;
-      int count = 0;
-#pragma unroll
-      for (int k = i; k < kN / 32; ++k) {
-        of[k] = __ballot_sync(0xFFFFFFFFu, id[k] == a);
-        left[k] &= ~of[k];
-        count += __popc(of[k]);
-        sel |= (((of[k] & 0xFFFFu) ? 1u : 0u) | ((of[k] >> 16) ? 2u : 0u)) << (2 * k);
-      }
-      if (count < enough) continue;
-#pragma unroll
-      for (int k = i; k < kN / 32; ++k) {
-        loose[k] &= ~of[k];
-        if ((of[k] >> lane) & 1u) info.index[32 * k + lane] = (uint8_t)listed;
-      }
-      if (lane == 0) info.adapter[listed] = a, info.sel[listed] = sel;
-      ++listed;
-    }
+  for (int k0 = 0; k0 < count; k0 += 32) {
+    const int k = k0 + lane, value = k < count ? held[k] : 0;
+    const uint32_t take = __ballot_sync(0xFFFFFFFFu, k < count && value >> 16 >= enough);
+    const int place = listed + __popc(take & ((1u << lane) - 1u));
+    const bool on = ((take >> lane) & 1u) && place < kMaxListed;
+    if (on) info.adapter[place] = seen[k], info.sel[place] = (uint32_t)value & 0xFFFFu;
+    if (k < count) held[k] = on ? place : 255;
+    listed = min(listed + __popc(take), kMaxListed);
   }
+  __syncwarp();
 #pragma unroll
-  for (int i = 0; i < kN / 32; ++i)
-    if (lane == i) info.loose[i] = loose[i];
+  for (int i = 0; i < kWords; ++i) {
+    const int place = at[i] >= 0 ? held[at[i]] : 255;
+    info.index[32 * i + lane] = (uint8_t)place;
+    const uint32_t loose = __ballot_sync(0xFFFFFFFFu, at[i] >= 0 && place == 255);
+    if (lane == i) info.loose[i] = loose;
+  }
   if (lane == 0) info.listed = listed, info.blocks = blocks_of(listed, p.ad.rank);
   __syncwarp();
 }
@@ -650,7 +662,7 @@ project_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__
       if (!adapters || warp != 2 || i >= ntiles) return;
       int tt, to;
       raster(first + i * step, p, tt, to);
-      find_adapters<kForward, kN>(p, (int64_t)tt * kN, lane, info_of(i));
+      find_adapters<kForward, kN>(p, (int64_t)tt * kN, lane, info_of(i), reinterpret_cast<int*>(zs));
       if (lane == 0) mbar_arrive(&info_full[i % kInfos]);
     };
     bad[out_row] = bad[128 + out_row] = 0u;
