@@ -120,7 +120,7 @@ struct Rows {
 // kDown: A_a [rank, cols] (contracted axis contiguous); else B_a [cols, rank], whose 8 x 8 blocks are
 // transposed in registers.  kNT: ranks / 8 of a pass.
 constexpr int kTile = 256, kJob = 32;
-constexpr int kDepth = 2;  // two CTAs an SM fit
+constexpr int kDepth = 2;
 struct Split {
   int csize, crank, turns, turn;
 };
@@ -130,9 +130,9 @@ struct JobShared {
   const uint8_t* row[kJob];
   const uint8_t* scale_row[kJob];
 };
-template <int kNT>
-constexpr int ring_bytes() {  // of a warp, for kDepth blocks: the tokens' 128 bytes each (or 64 and a scale word), the factors
-  return kDepth * (kJob * 128 + 1024 * kNT);
+template <int kFormat, int kNT>
+constexpr int block_bytes() {  // of a warp's ring: the tokens' rows of 128 bytes (a checkpoint's 64 and a scale word), the factors
+  return kJob * (kFormat < 0 ? 128 : 68) + 1024 * kNT;
 }
 template <int kNT>
 constexpr int part_bytes() {
@@ -203,18 +203,16 @@ __device__ __forceinline__ int2 place_token(int id, int words, int warp, int lan
 
 template <int kFormat, bool kDown, int kNT>
 __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t tokens, const Adapters& ad, float* z,
-                                            uint32_t* z_split, float unit, int64_t tile, const Split& sp, float* part,
-                                            JobShared& job, uint8_t* rings) {
+                                            uint32_t* z_split, float unit, int64_t tile, const Split& sp, JobShared& job,
+                                            uint8_t* smem) {
   constexpr int kMR = (kNT + 1) / 2, kPass = 8 * kNT;
-  // a block: the tokens' rows of kRowBytes, a checkpoint's scale words, the factors
-  constexpr int kRowBytes = kFormat < 0 ? 128 : 64, kX = kJob * kRowBytes + (kFormat < 0 ? 0 : 128);
-  constexpr int kBlock = kX + 1024 * kNT;
+  constexpr int kX = kJob * (kFormat < 0 ? 128 : 68), kBlock = block_bytes<kFormat, kNT>();
   constexpr int kOdd = kFormat < 0 ? 4 : 1;  // odd rows of A: pieces elsewhere than the even rows' of the same reads
-  static_assert(kDepth * kBlock <= ring_bytes<kNT>(), "a ring's room");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int64_t t0 = tile * kTile, cols = rows.cols;
   const int rank = ad.rank;
-  uint8_t* ring = rings + warp * ring_bytes<kNT>();
+  uint8_t* ring = smem + warp * kDepth * kBlock;
+  float* part = reinterpret_cast<float*>(smem);  // the warps' partials take the rings' place
   // this warp's blocks of 64: first, first + ways, ...: `count` of them, taken from a place of its own on
   const int ways = kWarps * sp.csize, blocks = (int)((cols + 63) / 64), shift = (int)(tile * sp.turns + sp.turn);
   const int first = (sp.crank * kWarps + warp + shift) % ways;
@@ -362,7 +360,7 @@ __device__ __forceinline__ void shrink_tile(const Rows<kFormat>& rows, int64_t t
         }
       }
       copies_wait<0>();
-      __syncwarp();
+      __syncthreads();
       // ranks 16 i + g (+ 8), tokens 8 c + 2 q (+ 1): the warps' partials [warp][token][rank of the pass]
       float* out = part + warp * kJob * kPass;
 #pragma unroll
@@ -412,6 +410,12 @@ struct ShrinkArgs {
   uint32_t *z_split, *dz_split;
   int csize, turns_z, turns_dz;
 };
+constexpr int dz_ranks(int kNT) { return std::min(kNT, 2); }  // so that two CTAs fit an SM
+template <int kFormat, int kNT>
+constexpr int shrink_smem_bytes() {
+  return std::max({kWarps * kDepth * block_bytes<kFormat, kNT>(), kFormat < 0 ? 0 : kWarps * kDepth * block_bytes<-1, dz_ranks(kNT)>(),
+                   part_bytes<kNT>()});
+}
 template <int kFormat, int kNT>
 __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(Rows<kFormat> x, Rows<-1> dy, ShrinkArgs p) {
   extern __shared__ __align__(16) uint8_t shrink_smem[];
@@ -420,19 +424,18 @@ __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(Rows<kFormat> x, Ro
   const bool is_z = (int)blockIdx.y < p.turns_z;
   const Split sp = {p.csize, p.csize > 1 ? (int)cluster_rank() : 0, is_z ? p.turns_z : p.turns_dz,
                     (int)blockIdx.y - (is_z ? 0 : p.turns_z)};
-  float* part = reinterpret_cast<float*>(shrink_smem + kWarps * ring_bytes<kNT>());
   const int64_t tile = blockIdx.x / p.csize;
   const float unit = 1.0f / (kWeightUnit * *p.global_scale);
   if (is_z)
-    shrink_tile<kFormat, true, kNT>(x, p.tokens, p.ad, p.z, p.z_split, unit, tile, sp, part, job, shrink_smem);
+    shrink_tile<kFormat, true, kNT>(x, p.tokens, p.ad, p.z, p.z_split, unit, tile, sp, job, shrink_smem);
   else if constexpr (kFormat >= 0)  // the forward pass has no dz
-    shrink_tile<-1, false, kNT>(dy, p.tokens, p.ad, p.dz, p.dz_split, unit, tile, sp, part, job, shrink_smem);
+    shrink_tile<-1, false, dz_ranks(kNT)>(dy, p.tokens, p.ad, p.dz, p.dz_split, unit, tile, sp, job, shrink_smem);
 }
 
 template <int kFormat, int kNT>
 cudaError_t launch_shrink_of(const Rows<kFormat>& x, const Rows<-1>& dy, ShrinkArgs p, int jobs, int sms, cudaStream_t stream) {
   auto kernel = shrink_kernel<kFormat, kNT>;
-  constexpr int kSmem = kWarps * ring_bytes<kNT>() + part_bytes<kNT>();
+  constexpr int kSmem = shrink_smem_bytes<kFormat, kNT>();
   constexpr int kCtas = kSmem <= 113 * 1024 ? 2 : 1;  // an SM holds
   cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmem);
   if (err != cudaSuccess) return err;
@@ -476,9 +479,10 @@ cudaError_t launch_shrink(const Rows<kFormat>& x, const Rows<-1>& dy, const Shri
   const int jobs = (int)std::min<int64_t>(tok, (tok + kJob - 1) / kJob + std::min<int64_t>(p.ad.count, tok) - 1);
   if (rank <= 8) return launch_shrink_of<kFormat, 1>(x, dy, p, jobs, sms, stream);
   if (rank <= 16) return launch_shrink_of<kFormat, 2>(x, dy, p, jobs, sms, stream);
-  // more ranks a pass read the rows fewer times, but leave room for one CTA an SM: bf16 rows gain (4096 tokens x 14336, rank
-  // 64: 167 us and 150), the backward pass does not (358 and 378)
-  return launch_shrink_of<kFormat, kFormat < 0 ? 4 : 2>(x, dy, p, jobs, sms, stream);
+  // 32 ranks a pass of bf16 rows leave room for one CTA an SM, and gain all the same (4096 tokens x 14336, rank 64: 167 us
+  // at 16 ranks a pass and two CTAs, 150); z of a checkpoint takes 32, two CTAs fit (z, dz, dA and dB of 4096 x (4096 x
+  // 14336), rank 64: 311 us at 16 ranks, 258)
+  return launch_shrink_of<kFormat, 4>(x, dy, p, jobs, sms, stream);
 }
 
 // ---------------------------------------------------------------- dA and dB
