@@ -528,13 +528,15 @@ int hscale_checkpoint_load(const uint8_t* codes, int64_t ld_codes, const uint8_t
  * token's adapter; a value outside [0, adapters) means none, and NULL adapter 0 for every token.
  * With adapters == 0 the adapter arguments are ignored.
  *
- * Sums are fp32 (A_a x_t included), and y is rounded once.  A token's result depends on its own row
- * and adapter only: an Inf or NaN in another token's row or adapter does not reach it.
+ * Sums are fp32 (A_a x_t included), and y is rounded once; A_a x_t may enter the second product as
+ * a pair of bf16 numbers, which lose 2^-17 of it (of an Inf there, NaN is left).  A token's result depends
+ * on its own row and adapter only: an Inf or NaN in another token's row or adapter does not reach it.
+ * Where its adapter's own values are not finite, NaN may stand for an Inf.  Equal calls give equal bits.
  *
  * n must be a multiple of 16, rank one of 8 up to 128, adapters at most 65535.  x, y, a and b
  * are 16-byte aligned, ld_x and ld_y multiples of 8, packed 8-byte aligned.  With n == 0, y is zero.
- * The workspace (256-byte aligned; none is needed where the query says 0) holds A_a x_t; calls
- * that may overlap need their own.
+ * The workspace (256-byte aligned; none is needed where the query says 0) holds A_a x_t,
+ * as fp32 and as its pair; calls that may overlap need their own.
  */
 size_t hscale_project_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t adapters, int64_t rank);
 int hscale_project(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, const uint8_t* packed,

@@ -3,11 +3,17 @@
 //   dA = sum_t dz_t x_t^T      dB = sum_t dy_t z_t^T          over the tokens of each adapter
 // z and dz are fp32 [tokens, rank]; rows of tokens without an adapter are left as they are.
 //
-// All four read long rows of activations once and multiply them by something narrow (`rank` wide), so they
-// are bound by HBM, and their tiles are too thin for tcgen05 (N = rank, or K = the tokens of one adapter): they
-// run on warp-level MMAs (m16n8k16, bf16 operands, fp32 sums) whose fragments come straight from global
-// memory.  The order of a contracted axis is free, so a lane takes 16 consecutive bytes of a row and calls
-// its 8 elements whatever slots of K the fragment layout gives it, on both operands alike.
+// All four multiply long rows of activations by something narrow (`rank` wide), grouped by the tokens' adapters: tiles
+// too thin for tcgen05 (N = rank, or K = the tokens of one adapter).  They run on warp-level MMAs (m16n8k16,
+// bf16 operands, fp32 sums); a warp's operands come through a ring of its own in shared memory by asynchronous copies, so
+// warps wait for no one but themselves until their sums meet.  The order of a contracted axis is free, so a lane takes
+// 16 consecutive bytes of a row and calls its 8 elements whatever slots of K the fragment layout gives it, on both
+// operands alike.
+//
+// The bytes (each row once) would take a tenth of the time that they do: few ranks are bound by the latency of the copies
+// and of each launch's start and end, many ranks by L2, from where a job's factors and the rows of each
+// pass come again, and by the MMAs.  Under a profiler, one GB300: z and dz of 8192 tokens, 4096 x 4096, rank 16: 35 us, dA
+// and dB 59; of 4096 tokens, 4096 x 14336, rank 64: 118 and 186.
 #include <algorithm>
 
 #include "hscale_internal.h"

@@ -8,27 +8,34 @@
 // each weight without s_g is exact in bf16 (2^-7 of it is what the tile holds, see unpack8); s_g is a
 // factor of the accumulator.
 //
-// Tile: 128 outputs (M, the weight) x kN tokens (N), K in blocks of 64.  14 warps:
+// Tile: 128 outputs (M, the weight) x kN tokens (N), K in blocks of 64.  18 warps:
 //   0      TMA loads of the tokens' tile, K-major, 128-byte swizzle
 //   1      MMAs
 //   2-5    epilogue: tensor memory -> s_g, adapter, bf16 -> out (lane = output, columns = tokens)
-//   6-13   the weight's tile: two groups of four warps take the K blocks in turn, 32 packed bytes and 4 codes
+//   6-17   the weight's tile: three groups of four warps take the K blocks in turn, 32 packed bytes and 4 codes
 //          a thread, kept kAhead of the group's blocks ahead in registers and unpacked into the swizzled tile (the
-//          groups' waits and fences overlap; one group of eight warps was slower).  Forward (K = n) the tile is K-major, backward
-//          (K = m, outputs = n) the same packed rows make it MN-major, so W is read as it is stored.
+//          groups' waits and fences overlap; all warps on one block was slower).  Forward (K = n) the tile is K-major,
+//          backward (K = m, outputs = n) the same packed rows make it MN-major, so W is read as it is stored.
 // Each weight is unpacked once per kN tokens: about 2.7 instructions a weight against kN / 64 tensor-core
 // cycles, so at kN = 256 the unpacking hides behind the MMAs.
 //
+// What bounds it.  Many tokens: the tensor cores, 0.80 of the measured bf16 rate (8192 tokens, 14336 x 4096: 650 us without
+// adapters, 1.48 PFLOP/s); the rest is the ring's four stages, whose hand-over the unpacking warps' issue and shared-memory
+// writes delay.  Few tokens: the K blocks' chain, 0.2-0.34 us each whatever the rate (launch_project's estimate).
+//
 // Where the tiles leave SMs idle, a cluster of csize CTAs splits K: each rank accumulates its share, hands the
-// others the columns they own through distributed shared memory, and finishes its own columns, summing in rank
-// order.  With csize 1 the grid is persistent and the epilogue of a tile runs beside the MMAs of the next (two
-// accumulators in tensor memory).
+// others the columns they own through distributed shared memory (all warps but two take part), and finishes its own
+// columns, summing in rank order.  With csize 1 the grid is persistent and the epilogue of a tile runs beside the MMAs
+// of the next (two accumulators in tensor memory).
 //
 // The adapters' terms.  An adapter with enough tokens in a tile takes its term on the tensor cores: after the
 // weight's K blocks the epilogue's warps, idle by then, write its factors and its tokens' z (as a pair hi + lo of
 // bf16 numbers, so 2^-17 of it is lost; zeros for the other tokens) as one more K block per 32 ranks or per two or
-// four adapters of fewer ranks, fetched before the stage is free.  An adapter with few tokens there ("loose": a decoding batch) is cheaper in the epilogue
-// itself, a dot product of `rank` fp32 numbers per result.  Zeros times factors are zeros only while the
+// four adapters of fewer ranks, fetched before the stage is free.  A block takes them 0.8 us (load, write, fence), so 16
+// adapters in requests cost 8192 tokens 20-35 us, and 32 adapters in any order cost 2048 tokens 35 us.  An adapter
+// with few tokens there ("loose": a decoding batch) is cheaper in the epilogue itself, a dot product of `rank` fp32
+// numbers per result; these are bound by the four warps' instructions (64 tokens of 64 adapters, 14336 x 4096: 35.5 us
+// in the kernel, 23.5 without adapters).  Zeros times factors are zeros only while the
 // factors are finite: an output whose factors hold an Inf or NaN is left out of the K block, and the tokens
 // of that adapter get NaN there; so nothing passes from one request's adapter to another's tokens.
 // Which adapters a tile has is found by one warp, two tiles ahead (TileInfo).
@@ -141,12 +148,11 @@ __device__ __forceinline__ void unpack_factors(const uint4& q, float (&f)[8]) {
   f[4] = bf16_lo(q.z), f[5] = bf16_hi(q.z), f[6] = bf16_lo(q.w), f[7] = bf16_hi(q.w);
 }
 
-// Tokens t0 .. t0 + W - 1 and this lane's output o: each loose token's adapter added to v.  zs: 2 KB of the warp's own.  Eight ranks a pass: each lane
-// fetches its token's z into zs, from where every lane reads all of them; z and factors of the next pass are
-// fetched before the present one's products.  Tokens on one adapter share a lane's 8 factors; otherwise
-// the factors of 8 tokens are fetched at once.  A token without an adapter keeps v as it is (no product by
-// zero: the factors may be Inf or NaN).
-// loose: bit j where token t0 + j's term is added here.
+// Tokens t0 .. t0 + W - 1 and this lane's output o: each loose token's adapter added to v.  loose: bit j where token
+// t0 + j's term is added here.  zs: 2 KB of the warp's own.  Eight ranks a pass: each lane fetches its token's z into zs,
+// from where every lane reads all of them; z and factors of the next pass are fetched before the present one's
+// products.  Tokens on one adapter share a lane's 8 factors; otherwise the factors of 8 tokens are fetched at once.
+// A token without an adapter keeps v as it is (no product by zero: the factors may be Inf or NaN).
 template <bool kForward, int W>
 __device__ __forceinline__ void add_loose(float (&v)[W], int64_t t0, int64_t o, int lane, const ProjectArgs& p, uint32_t loose,
                                        float* zs) {
