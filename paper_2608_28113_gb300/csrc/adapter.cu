@@ -13,7 +13,7 @@
 // The bytes (each row once) would take a tenth of the time that they do: few ranks are bound by the latency of the copies
 // and of each launch's start and end, many ranks by L2, from where a job's factors and the rows of each
 // pass come again, and by the MMAs.  Under a profiler, one GB300: z and dz of 8192 tokens, 4096 x 4096, rank 16: 35 us, dA
-// and dB 59; of 4096 tokens, 4096 x 14336, rank 64: 118 and 186.
+// and dB 59; of 4096 tokens, 4096 x 14336, rank 64: 137 and 191.
 #include <algorithm>
 
 #include "hscale_internal.h"
