@@ -93,3 +93,68 @@ def test_projection_of_a_starved_block(starved, monkeypatch, t, m, n):  # noqa: 
     for c in range(0, m, 128):
         part = lost[:, c:c + 128]
         assert torch.equal(part.all(1), part.any(1))
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("rank", [8, 32, 64])
+@pytest.mark.parametrize("lead, pad, scale_lead, scale_pad", [(8, 8, 0, 0), (1, 3, 0, 0), (0, 0, 1, 2), (5, 4, 3, 1)])
+def test_checkpoint_rows_at_any_address(fmt, rank, lead, pad, scale_lead, scale_pad):
+    """The gradients read codes and scales at any address, and get the same bits as from aligned ones."""
+    t, m, n, count = 150, 96, 400, 3
+    packed, codes, sg, a, b, alpha = layer(m, n, count, rank, seed=4)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    ids = torch.randint(-1, count, (t,), generator=g, device=DEV).to(I32)
+    dy = torch.randn(t, m, generator=g, device=DEV).to(BF16)
+    q, s = torch.empty(t, n, dtype=U8, device=DEV), torch.empty(t, (n + 31) // 32, dtype=U8, device=DEV)
+    hs.hscale_checkpoint_save(torch.randn(t, n, generator=g, device=DEV).to(BF16), fmt, q, s)
+
+    def gradients(q, s):
+        dx = torch.empty(t, n, dtype=BF16, device=DEV)
+        da, db = torch.empty_like(a), torch.empty_like(b)
+        hs.hscale_project_backward(dy, q, s, fmt, packed, codes, sg, a, b, alpha, ids, dx, da, db)
+        return dx, da, db
+
+    def moved(v, lead, pad):
+        rows, cols = v.shape
+        wide = torch.randint(256, (lead + rows * (cols + pad),), generator=g, device=DEV, dtype=U8)
+        view = wide[lead:].view(rows, cols + pad)[:, :cols]
+        view.copy_(v)
+        return view
+
+    for got, want in zip(gradients(moved(q, lead, pad), moved(s, scale_lead, scale_pad)), gradients(q, s)):
+        assert torch.equal(got, want) and want.float().abs().max() > 0
+
+
+@pytest.mark.parametrize("t, order", [(7, "any"), (64, "each its own"), (257, "any"), (700, "runs"), (520, "rare")])
+def test_gradients_of_many_adapters(t, order):
+    """More adapters than a tile lists or an SM has CTAs, most of them with few tokens or none, against the formulas in 64
+    bits.  Tolerance: dA and dB are rounded once to bf16, at most 2^-8 of a value.  Before that, in units of the terms'
+    summed magnitudes: z and dz are fp32 sums of at most 272 terms (272 2^-24) that enter as pairs (2^-17), and the
+    tokens, at most 520 of an adapter, are summed in fp32 (520 2^-23): together less than 2^-13."""
+    m, n, count, rank = 136, 272, 300, 8
+    packed, codes, sg, a, b, alpha = layer(m, n, count, rank, seed=6)
+    g = torch.Generator(device=DEV).manual_seed(7)
+    ids = {"any": torch.randint(-1, count, (t,), generator=g, device=DEV),
+           "each its own": torch.randperm(count, generator=g, device=DEV)[:t],
+           "runs": torch.arange(t, device=DEV) // 3 % count,
+           "rare": torch.where(torch.arange(t, device=DEV) % 97 == 0, torch.arange(t, device=DEV) % count, count - 1)}[order].to(I32)
+    dy = torch.randn(t, m, generator=g, device=DEV).to(BF16)
+    q, s = torch.empty(t, n, dtype=U8, device=DEV), torch.empty(t, (n + 31) // 32, dtype=U8, device=DEV)
+    x = torch.empty(t, n, dtype=BF16, device=DEV)
+    hs.hscale_checkpoint_save(torch.randn(t, n, generator=g, device=DEV).to(BF16), 0, q, s)
+    hs.hscale_checkpoint_load(q, s, 0, x)
+    da, db = torch.empty_like(a), torch.empty_like(b)
+    hs.hscale_project_backward(dy, q, s, 0, packed, codes, sg, a, b, alpha, ids, None, da, db)
+    on = (ids >= 0).nonzero()[:, 0]
+    who, xd, dyd = ids[on].long(), x[on].to(F64), dy[on].to(F64)
+    ad, bd = a.to(F64)[who], b.to(F64)[who]
+    z, dz = torch.einsum("trn,tn->tr", ad, xd), torch.einsum("tmr,tm->tr", bd, dyd)
+    for got, left, right, inner in ((da, dz, xd, torch.einsum("tmr,tm->tr", bd.abs(), dyd.abs())),
+                                    (db, dyd, z, torch.einsum("trn,tn->tr", ad.abs(), xd.abs()))):
+        want = torch.zeros(got.shape, dtype=F64, device=DEV).index_add_(0, who, left[:, :, None] * right[:, None, :])
+        size_l, size_r = (inner, right.abs()) if got is da else (left.abs(), inner)
+        size = torch.zeros(got.shape, dtype=F64, device=DEV).index_add_(0, who, size_l[:, :, None] * size_r[:, None, :])
+        assert bool(((got.to(F64) - want).abs() <= want.abs() / 2**8 + size / 2**13).all())
+        idle = torch.ones(count, dtype=torch.bool, device=DEV)
+        idle[who] = False
+        assert not got[idle].any()
