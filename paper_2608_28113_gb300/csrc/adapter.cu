@@ -703,31 +703,41 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
         for (int e = 0; e < 4; ++e)
           part[sub * kSize + (16 * i + 8 * (e >> 1) + g) * kPitch + 64 * (warp & 3) + 8 * (2 * q + (e & 1)) + j] = acc[i][j][e];
     __syncthreads();
-    for (int i = threadIdx.x; i < kSize; i += kThreadsG) {
-      float s = part[i];
-  #pragma unroll
-      for (int v = 1; v < kSub; ++v) s += part[v * kSize + i];
-      part[i] = s;
-    }
-    if (csize > 1) cluster_sync(); else __syncthreads();
   }
-  // a rank finishes a share of the columns
-  const int share = (kColumns / 8 + csize - 1) / csize * 8, c0 = crank * share, width = min(share, kColumns - c0);
-  for (int i = threadIdx.x; i < 16 * kRT * width; i += kThreadsG) {
-    // dA's rows run along the columns, dB's along the ranks
-    const int rr = kRankMajor ? i / width : i % (16 * kRT), cc = c0 + (kRankMajor ? i % width : i / (16 * kRT));
-    const int r = r0 + rr;
-    const int64_t c = col0 + cc;
-    if (r >= rank || c >= cols) continue;
-    float s = 0.0f;
-    if (any) {
-      const float* src = part + rr * kPitch + cc;
-      s = csize > 1 ? ld_cluster(src, 0) : *src;
-      for (int d = 1; d < csize; ++d) s += ld_cluster(src, (uint32_t)d);
+  // `width` columns from c0 on; value(at): the sum at `at` of a partial
+  const auto finish = [&](int c0, int width, auto value) {
+    for (int i = threadIdx.x; i < 16 * kRT * width; i += kThreadsG) {
+      // dA's rows run along the columns, dB's along the ranks
+      const int rr = kRankMajor ? i / width : i % (16 * kRT), cc = c0 + (kRankMajor ? i % width : i / (16 * kRT));
+      const int r = r0 + rr;
+      const int64_t c = col0 + cc;
+      if (r >= rank || c >= cols) continue;
+      const float s = any ? value(rr * kPitch + cc) : 0.0f;
+      out[kRankMajor ? ((int64_t)a * rank + r) * cols + c : ((int64_t)a * cols + c) * rank + r] = __float2bfloat16_rn(s);
     }
-    out[kRankMajor ? ((int64_t)a * rank + r) * cols + c : ((int64_t)a * cols + c) * rank + r] = __float2bfloat16_rn(s);
+  };
+  const auto sum_sets = [&](int at) {
+    float s = part[at];
+#pragma unroll
+    for (int v = 1; v < kSub; ++v) s += part[v * kSize + at];
+    return s;
+  };
+  if (csize == 1) {
+    finish(0, kColumns, sum_sets);
+    return;
   }
-  if (csize > 1) cluster_sync();
+  // a rank of the cluster finishes a share of the columns
+  if (any) {
+    for (int i = threadIdx.x; i < kSize; i += kThreadsG) part[i] = sum_sets(i);
+    cluster_sync();
+  }
+  const int share = (kColumns / 8 + csize - 1) / csize * 8, c0 = crank * share;
+  finish(c0, min(share, kColumns - c0), [&](int at) {
+    float s = ld_cluster(part + at, 0);
+    for (int d = 1; d < csize; ++d) s += ld_cluster(part + at, (uint32_t)d);
+    return s;
+  });
+  cluster_sync();
 }
 
 // blockIdx.x / csize: the column tiles of dA (tiles_a of them), then those of dB.
