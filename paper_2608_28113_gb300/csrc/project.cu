@@ -19,7 +19,7 @@
 // Each weight is unpacked once per kN tokens: about 2.7 instructions a weight against kN / 64 tensor-core
 // cycles, so at kN = 256 the unpacking hides behind the MMAs.
 //
-// What bounds it.  Many tokens: the tensor cores, 0.80 of the measured bf16 rate (8192 tokens, 14336 x 4096: 650 us without
+// What bounds it.  Many tokens: the tensor cores, 0.78 of the measured bf16 rate (8192 tokens, 14336 x 4096: 650 us without
 // adapters, 1.48 PFLOP/s); the rest is the ring's four stages, whose hand-over the unpacking warps' issue and shared-memory
 // writes delay.  Few tokens: the K blocks' chain, 0.2-0.34 us each whatever the rate (launch_project's estimate).
 //
