@@ -553,7 +553,9 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
   bool any = false;  // tokens; alike in a cluster
   for (int64_t w0 = 0; w0 < tokens; w0 += kWindow) {
     int have = (int)min((int64_t)kWindow, tokens - w0);
-    if (ad.of_token != nullptr) {
+    if (ad.of_token == nullptr) {
+      if (a != 0) have = 0;  // all tokens are adapter 0's
+    } else {
       // warp w lists tokens [w span, ..) of the window behind the warps' before it
       constexpr int kSpan = kWindow / kWarpsG;
       const int span = ((have + kWarpsG - 1) / kWarpsG + 31) & ~31;
