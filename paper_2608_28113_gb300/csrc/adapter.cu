@@ -552,6 +552,7 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
   float* zraw = reinterpret_cast<float*>(frags + 2 * frag_bytes<kRT>());
   bool any = false;  // tokens; alike in a cluster
   for (int64_t w0 = 0; w0 < tokens; w0 += kWindow) {
+    __syncthreads();  // every warp has read the list and the scales of the window before
     int have = (int)min((int64_t)kWindow, tokens - w0);
     if (ad.of_token == nullptr) {
       if (a != 0) have = 0;  // all tokens are adapter 0's
@@ -559,7 +560,6 @@ __device__ __forceinline__ void grad_tile(const Rows<kFormat>& rows, int64_t tok
       // warp w lists tokens [w span, ..) of the window behind the warps' before it
       constexpr int kSpan = kWindow / kWarpsG;
       const int span = ((have + kWarpsG - 1) / kWarpsG + 31) & ~31;
-      __syncthreads();
       uint32_t own[kSpan / 32];
       int count = 0;
 #pragma unroll

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2608_28113_gb300 as hs
-from test_gpu_adapters import Layer, check
+from test_gpu_adapters import BF16, DEV, F64, I32, Layer, check, gen
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,26 @@ def test_adapters_without_tokens_get_zeros(t, m, n, count, rank, fmt):
     check(da, wa, sa, t + m, 2.0 ** -16)
     check(db, wb, sb, t + n, 2.0 ** -16)
     assert not da[1:].any() and not db[1:].any()
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("t, m, n", [(9000, 5120, 5120), (8200, 9984, 256)])
+def test_windows_of_tokens_follow_one_another(t, m, n, fmt):
+    """Tokens are taken in windows of 4096, here by clusters of three, whose CTAs end a window on different chunks.  The
+    tokens' magnitudes differ by powers of two, so that one token's scales on another's elements show.  dA and dB
+    against the formulas in 64 bits (the tolerances of test_gpu_adapters), the bits of a call that names adapter 0 for each
+    token, and the same bits again."""
+    L = Layer(t, m, n, 1, 16, None, fmt=fmt)
+    L.x.mul_(torch.exp2(torch.randint(-12, 13, (t, 1), generator=gen("magnitudes", t, fmt), device=DEV)).to(BF16))
+    dx, da, db, held = L.backward()
+    x, dy, a, b, alpha = held.to(F64), L.dy.to(F64), L.a[0].to(F64), L.b[0].to(F64), L.alpha[0].to(F64)
+    dz, z = alpha * dy @ b, alpha * x @ a.T
+    check(da[0], dz.T @ x, (alpha * dy.abs() @ b.abs()).T @ x.abs(), t + m, 2.0 ** -16)
+    check(db[0], dy.T @ z, dy.abs().T @ (alpha * x.abs() @ a.abs().T), t + n, 2.0 ** -16)
+    for _ in range(4):
+        again = L.backward()
+        assert torch.equal(again[1], da) and torch.equal(again[2], db)
+    L.ids = torch.zeros(t, dtype=I32, device=DEV)
+    named = L.backward()
+    for got, want in zip(named[:3], (dx, da, db)):
+        assert torch.equal(got, want)
