@@ -438,6 +438,9 @@ __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(Rows<kFormat> x, Ro
     shrink_tile<-1, false, dz_ranks(kNT)>(dy, p.tokens, p.ad, p.dz, p.dz_split, unit, tile, sp, job, shrink_smem);
 }
 
+// Adapters that tokens may be on: the work is dealt out for these.
+int64_t used_adapters(const Adapters& ad) { return ad.of_token == nullptr ? std::min(ad.count, 1) : ad.count; }
+
 template <int kFormat, int kNT>
 cudaError_t launch_shrink_of(const Rows<kFormat>& x, const Rows<-1>& dy, ShrinkArgs p, int jobs, int sms, cudaStream_t stream) {
   auto kernel = shrink_kernel<kFormat, kNT>;
@@ -482,7 +485,7 @@ cudaError_t launch_shrink(const Rows<kFormat>& x, const Rows<-1>& dy, const Shri
   const int sms = info.sm_count, rank = p.ad.rank;
   // jobs that a tile may have: its adapters are not known here
   const int64_t tok = std::min<int64_t>(p.tokens, kTile);
-  const int jobs = (int)std::min<int64_t>(tok, (tok + kJob - 1) / kJob + std::min<int64_t>(p.ad.count, tok) - 1);
+  const int jobs = (int)std::min<int64_t>(tok, (tok + kJob - 1) / kJob + std::min<int64_t>(used_adapters(p.ad), tok) - 1);
   if (rank <= 8) return launch_shrink_of<kFormat, 1>(x, dy, p, jobs, sms, stream);
   if (rank <= 16) return launch_shrink_of<kFormat, 2>(x, dy, p, jobs, sms, stream);
   // 32 ranks a pass of bf16 rows leave room for one CTA an SM, and gain all the same (4096 tokens x 14336, rank 64: 167 us
@@ -774,9 +777,9 @@ cudaError_t launch_grad_of(const Rows<kFormat>& x, const Rows<-1>& dy, GradArgs 
   if (err != cudaSuccess) return err;
   // the tokens split (by up to four: clusters of eight CTAs that fill an SM each leave many SMs out) while a CTA an
   // SM holds all, and an adapter's share has a chunk of them
+  const int64_t used = used_adapters(p.ad);
   p.csize = 1;
-  while (p.csize < 4 && tiles * p.ad.count * passes * (p.csize + 1) <= kCtas * sms &&
-         p.tokens / p.ad.count > (int64_t)p.csize * kChunk)
+  while (p.csize < 4 && tiles * used * passes * (p.csize + 1) <= kCtas * sms && p.tokens / used > (int64_t)p.csize * kChunk)
     ++p.csize;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * p.csize), (unsigned)p.ad.count, (unsigned)passes);
@@ -806,8 +809,8 @@ cudaError_t launch_grad(const Rows<kFormat>& x, const Rows<-1>& dy, GradArgs p, 
   } else {
     // with more CTAs than SMs, two an SM (2048 tokens on 32 adapters, 1024 x 4096: 62 -> 52 us); with fewer, each the faster
     // the more warps it has (300 tokens on 4, 2048 x 2048: 25.7 us and 24.7)
-    return tiles * p.ad.count * passes > sms ? launch_grad_of<kFormat, kRT, 2>(x, dy, p, tiles, passes, sms, stream)
-                                             : launch_grad_of<kFormat, kRT, 4>(x, dy, p, tiles, passes, sms, stream);
+    return tiles * used_adapters(p.ad) * passes > sms ? launch_grad_of<kFormat, kRT, 2>(x, dy, p, tiles, passes, sms, stream)
+                                                     : launch_grad_of<kFormat, kRT, 4>(x, dy, p, tiles, passes, sms, stream);
   }
 }
 

@@ -54,3 +54,14 @@ def test_windows_of_tokens_follow_one_another(t, m, n, fmt):
     named = L.backward()
     for got, want in zip(named[:3], (dx, da, db)):
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("t, m, n, rank, fmt", [(2000, 2048, 2048, 64, 0), (1000, 1024, 4096, 16, 1), (200, 4096, 4096, 8, 0)])
+def test_adapters_without_tokens_change_nothing(t, m, n, rank, fmt):
+    """However many adapters there are beside adapter 0, its gradients are dealt out, and summed, alike: the same bits."""
+    L = Layer(t, m, n, 40, rank, None, fmt=fmt)
+    y, (dx, da, db, _) = L.project(), L.backward()
+    L.count, L.a, L.b, L.alpha = 1, L.a[:1].contiguous(), L.b[:1].contiguous(), L.alpha[:1].contiguous()
+    alone = L.backward()
+    assert torch.equal(L.project(), y) and torch.equal(alone[0], dx)
+    assert torch.equal(alone[1][0], da[0]) and torch.equal(alone[2][0], db[0])
