@@ -482,8 +482,17 @@ def hscale_output_error(x: torch.Tensor, dw2: torch.Tensor, m: int, out_sum: tor
                                       _stream_ptr(stream)))
 
 
-def _workspace(nbytes: int, device) -> torch.Tensor:
-    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+def _workspace(nbytes: int, device, stream) -> torch.Tensor:
+    """Scratch memory of a call on `stream`.  It is given back when the call returns, with its kernels still to run: so it
+    is that stream's memory, which goes to later work on that stream alone."""
+    nbytes = max(int(nbytes), 256)
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream_ptr(stream)  # 0 and 1 (cudaStreamLegacy): the default stream
+        stream = torch.cuda.default_stream(device) if handle <= 1 else torch.cuda.ExternalStream(handle, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def hscale_hessian_full_accumulate(x: torch.Tensor, H: torch.Tensor, workspace: torch.Tensor | None = None,
@@ -498,7 +507,7 @@ def hscale_hessian_full_accumulate(x: torch.Tensor, H: torch.Tensor, workspace: 
     tokens, n = x.shape
     direct = x.data_ptr() % 16 == 0 and x.stride(0) % 8 == 0
     if workspace is None and not direct:
-        workspace = _workspace(load().hscale_hessian_full_workspace_bytes(tokens, n), x.device)
+        workspace = _workspace(load().hscale_hessian_full_workspace_bytes(tokens, n), x.device, stream)
     _check("hscale_hessian_full_accumulate",
            load().hscale_hessian_full_accumulate(_ptr(x), tokens, n, x.stride(0), _ptr(H), H.stride(0),
                                                  _ptr(workspace) if workspace is not None else None,
@@ -521,7 +530,7 @@ def hscale_gptq_factor(H: torch.Tensor, damp: float, U: torch.Tensor, dead: torc
         nbytes = load().hscale_gptq_factor_workspace_bytes(n)
         if nbytes == 0:
             raise HScaleError("hscale_gptq_factor_workspace_bytes", 5)
-        workspace = _workspace(nbytes, H.device)
+        workspace = _workspace(nbytes, H.device, stream)
     _check("hscale_gptq_factor",
            load().hscale_gptq_factor(_ptr(H), n, H.stride(0), float(damp), _ptr(U), _ptr(dead), _ptr(info),
                                      _ptr(workspace), workspace.numel(), _stream_ptr(stream)))
@@ -539,7 +548,7 @@ def hscale_gptq_hscale(w: torch.Tensor, U: torch.Tensor, h: torch.Tensor, global
         raise ValueError("w must be a contiguous 2-D tensor")
     m, n = w.shape
     if workspace is None:
-        workspace = _workspace(load().hscale_gptq_workspace_bytes(m, n, block), w.device)
+        workspace = _workspace(load().hscale_gptq_workspace_bytes(m, n, block), w.device, stream)
     _check("hscale_gptq_hscale",
            load().hscale_gptq_hscale(_ptr(w), m, n, _ptr(U), _ptr(h), _ptr(global_scale), _ptr(dead), int(block),
                                      int(down), int(up), _ptr(codes_out), _ptr(packed_out), _ptr(workspace),
@@ -661,9 +670,9 @@ def _projection(packed, codes, global_scale, a, b, alpha, adapter_of, tokens: in
     return adapters, rank
 
 
-def _project_workspace(workspace, nbytes: int, device):
+def _project_workspace(workspace, nbytes: int, device, stream):
     if workspace is None and nbytes > 0:
-        workspace = _workspace(nbytes, device)
+        workspace = _workspace(nbytes, device, stream)
     if workspace is not None:
         _need(workspace, torch.uint8, "workspace")
     return workspace, 0 if workspace is None else workspace.numel()
@@ -688,7 +697,7 @@ def hscale_project(x: torch.Tensor, packed: torch.Tensor, codes: torch.Tensor, g
     lib = _lib or load()
     if workspace is None:
         nbytes = lib.hscale_project_workspace_bytes(tokens, m, n, adapters, rank)
-        workspace = _workspace(nbytes, x.device) if nbytes else None
+        workspace = _workspace(nbytes, x.device, stream) if nbytes else None
     nbytes = 0
     if workspace is not None:
         _need(workspace, torch.uint8, "workspace")
@@ -739,7 +748,7 @@ def hscale_project_backward(dy: torch.Tensor, x_codes: torch.Tensor | None, x_sc
     lib = load()
     workspace, nbytes = _project_workspace(
         workspace, lib.hscale_project_backward_workspace_bytes(tokens, m, n, adapters, rank)
-        if workspace is None else 0, dy.device)
+        if workspace is None else 0, dy.device, stream)
     _check("hscale_project_backward",
            lib.hscale_project_backward(dy.data_ptr(), tokens, m, ld_dy, _ptr(x_codes), ld_c, _ptr(x_scales), ld_s,
                                        int(x_format), n, packed.data_ptr(), codes.data_ptr(),
