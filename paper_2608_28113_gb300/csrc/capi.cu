@@ -64,15 +64,22 @@ inline int check_rows(const void* x, int64_t rows, int64_t cols, int64_t ld) {
   return HSCALE_OK;
 }
 
-inline int check_checkpoint(const void* x, int64_t tokens, int64_t n, int64_t ld_x, int32_t format, const uint8_t* codes,
-                            int64_t ld_codes, const uint8_t* scales, int64_t ld_scales) {
+// a checkpoint's format, sizes and strides
+inline int check_codes(int64_t tokens, int64_t n, int32_t format, int64_t ld_codes, int64_t ld_scales) {
   if (format != HSCALE_CHECKPOINT_INT8 && format != HSCALE_CHECKPOINT_E4M3) return HSCALE_ERR_ARG;
   if (tokens < 0 || n < 0) return HSCALE_ERR_SHAPE;
   if (tokens == 0 || n == 0) return HSCALE_OK;
-  if (ld_x < n || ld_codes < n || ld_scales < (n + 31) / 32) return HSCALE_ERR_SHAPE;
-  if (n > INT32_MAX || tokens > INT32_MAX || tokens > INT64_MAX / 2 / ld_x || tokens > INT64_MAX / ld_codes ||
-      tokens > INT64_MAX / ld_scales)
+  if (ld_codes < n || ld_scales < (n + 31) / 32) return HSCALE_ERR_SHAPE;
+  if (n > INT32_MAX || tokens > INT32_MAX || tokens > INT64_MAX / ld_codes || tokens > INT64_MAX / ld_scales)
     return HSCALE_ERR_SHAPE;
+  return HSCALE_OK;
+}
+
+inline int check_checkpoint(const void* x, int64_t tokens, int64_t n, int64_t ld_x, int32_t format, const uint8_t* codes,
+                            int64_t ld_codes, const uint8_t* scales, int64_t ld_scales) {
+  const int st = check_codes(tokens, n, format, ld_codes, ld_scales);
+  if (st != HSCALE_OK || tokens == 0 || n == 0) return st;
+  if (ld_x < n || tokens > INT64_MAX / 2 / ld_x) return HSCALE_ERR_SHAPE;
   if (x == nullptr || codes == nullptr || scales == nullptr) return HSCALE_ERR_NULL;
   if (!aligned(x, 2)) return HSCALE_ERR_ALIGN;
   return HSCALE_OK;
@@ -494,7 +501,9 @@ int hscale_project_backward(const void* dy_bf16, int64_t tokens, int64_t m, int6
   const bool grads = adapters > 0 && (da_bf16 != nullptr || db_bf16 != nullptr);
   if (st == HSCALE_OK && grads) {
     if (!aligned(da_bf16, 16) || !aligned(db_bf16, 16)) return HSCALE_ERR_ALIGN;
-    st = check_checkpoint(dy_bf16, tokens, n, n, x_format, x_codes, ld_x_codes, x_scales, ld_x_scales);
+    st = check_codes(tokens, n, x_format, ld_x_codes, ld_x_scales);
+    const bool read = tokens > 0 && m > 0 && n > 0;
+    if (st == HSCALE_OK && read && (x_codes == nullptr || x_scales == nullptr)) return HSCALE_ERR_NULL;
   }
   if (st != HSCALE_OK) return st;
   cudaStream_t s = as_stream(stream);
