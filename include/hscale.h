@@ -529,7 +529,8 @@ int hscale_checkpoint_load(const uint8_t* codes, int64_t ld_codes, const uint8_t
  * With adapters == 0 the adapter arguments are ignored.
  *
  * Sums are fp32 (A_a x_t included), and y is rounded once; A_a x_t may enter the second product as
- * a pair of bf16 numbers, which lose 2^-17 of it (of an Inf there, NaN is left).  A token's result depends
+ * a pair of bf16 numbers, which lose 2^-17 of it (of an Inf there, NaN is left).  They are held in units of
+ * 128 global_scale, in which they have to stay within fp32's range; a global_scale may be 0.  A token's result depends
  * on its own row and adapter only: an Inf or NaN in another token's row or adapter does not reach it.
  * Where its adapter's own values are not finite, NaN may stand for an Inf.  Equal calls give equal bits.
  *

@@ -267,7 +267,8 @@ __device__ __forceinline__ int blocks_of(int listed, int rank) {
 
 // A K block costs the epilogue's warps about 1500 cycles; a loose token about 112 cycles per 8 ranks forward, where its
 // factors are 16 bytes an output, and 450 backward, where they are 8 loads (eight tokens' factors fetched at once).  An
-// adapter is listed where its tokens' share would cost more than its part of a K block.
+// adapter is listed where its tokens' share would cost more than its part of a K block.  None is where the
+// accumulator's unit is so far from 1 that z in it may leave fp32's range (a global scale of 0 among them).
 // One pass over the words of 32 tokens: each token's place among the tile's adapters, in order of their first tokens,
 // then the choice (a pass over the tokens for each adapter took 32 adapters 11 us a tile).  seen: 2 KB of the warp's own.
 template <bool kForward, int kN>
@@ -306,7 +307,9 @@ __device__ __forceinline__ void find_adapters(const ProjectArgs& p, int64_t t0, 
     __syncwarp();
   }
   const int block = 1500 * ((p.ad.rank + 31) / 32) / adapters_a_block(p.ad.rank), loose_token = (kForward ? 14 : 56) * p.ad.rank;
-  const int enough = (block + loose_token - 1) / loose_token;
+  const float unit = fabsf(*p.w.global_scale * kWeightUnit);  // read again: a register over the tile's loops costs more
+  const bool in_range = unit >= 0x1p-64f && unit <= 0x1p64f;
+  const int enough = in_range ? (block + loose_token - 1) / loose_token : INT32_MAX;
   int listed = 0;
   for (int k0 = 0; k0 < count; k0 += 32) {
     const int k = k0 + lane, value = k < count ? held[k] : 0;
