@@ -503,8 +503,9 @@ int hscale_gptq_hscale(const void* w_bf16, int64_t m, int64_t n, const float* U,
  * An element stands for code * 2^E, which is exact in bf16; an element's error is at most half a
  * step of its grid.  A block with an Inf or NaN has the scale byte 255 and loads as NaN.
  *
- * x may have any alignment of 2 bytes, codes and scales any; rows of x and of
- * codes on 16 are faster.  Any n.  Zero sizes do nothing.
+ * x may have any alignment of 2 bytes, codes and scales any.  Where a row of x or of codes does not
+ * begin on 16 bytes both go element by element: a save takes 4.5 times as long, a load 9 times; so give
+ * codes a row length that is a multiple of 16.  Any n.  Zero sizes do nothing.
  */
 typedef enum hscale_checkpoint_format {
   HSCALE_CHECKPOINT_INT8 = 0,
@@ -529,9 +530,10 @@ int hscale_checkpoint_load(const uint8_t* codes, int64_t ld_codes, const uint8_t
  * With adapters == 0 the adapter arguments are ignored.
  *
  * Sums are fp32 (A_a x_t included), and y is rounded once; A_a x_t may enter the second product as
- * a pair of bf16 numbers, which lose 2^-17 of it (of an Inf there, NaN is left).  They are held in units of
- * 128 global_scale, in which they have to stay within fp32's range; a global_scale may be 0.  A token's result depends
- * on its own row and adapter only: an Inf or NaN in another token's row or adapter does not reach it.
+ * a pair of bf16 numbers, which lose 2^-17 of it (of an Inf there, NaN is left).  The sums are held in units of
+ * 128 global_scale, and overflow where they leave fp32's range in these; a global_scale of 0 is allowed.
+ * A token's value depends on its own row and adapter only: an Inf or NaN in another token's row or adapter does not
+ * reach it.  Its last bits may depend on the other tokens too, by whose number and adapters the sums are split.
  * Where its adapter's own values are not finite, NaN may stand for an Inf.  Equal calls give equal bits.
  *
  * n must be a multiple of 16, rank one of 8 up to 128, adapters at most 65535.  x, y, a and b

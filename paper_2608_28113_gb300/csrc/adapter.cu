@@ -515,6 +515,7 @@ struct GradShared {
   alignas(16) uint8_t scales[2][kChunk][8];
 };
 // Sets of warps: four and one CTA an SM, or two and two CTAs (more than 32 ranks: two and one, whose registers they take).
+// 17 to 32 ranks take all 128 registers and spill (36 bytes stored and 88 loaded with two sets, 4 and 8 with four).
 constexpr int grad_ctas(int rt, int sets) { return rt == 4 ? 1 : 4 / sets; }  // an SM holds
 constexpr int kUnitBytes = 2048;  // of rows, in a warp's ring
 template <int kRT>

@@ -10,8 +10,9 @@
 // A block that holds Inf or NaN gets the byte 255 and loads as NaN.
 //
 // 2 B in and 1 + 1/32 B out per element for a save, the reverse for a load: one pass, 4.7 TB/s over both at 8192 x 4096.  A load
-// is bound by HBM, a save by its integer instructions (70 % of their rate under a profiler).  Two lanes share a
-// block, 16 elements each, and a thread has kUnroll such pieces in flight.
+// is bound by HBM, a save by its integer instructions (64 % of their pipe's rate under a profiler, HBM at 42 %).  Two lanes
+// share a block, 16 elements each, and a thread has kUnroll such pieces in flight.  Rows off 16 bytes (kVec false) go element
+// by element: 8192 x 4104 with contiguous rows of codes 94 us saved and 178 loaded, 21 and 21 with rows of 4112.
 #include <algorithm>
 #include <type_traits>
 

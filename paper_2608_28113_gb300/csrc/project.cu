@@ -40,6 +40,9 @@
 // of that adapter get NaN there; so nothing passes from one request's adapter to another's tokens.
 // Which adapters a tile has is found by one warp, two tiles ahead (TileInfo).
 //
+// 576 threads leave 96 registers each: the large tiles' instances spill (bytes stored and loaded, by the compiler: 256 tokens
+// backward 136 and 68, 128 backward 108 and 56, 256 forward 28 and 20, 128 forward 20 and 28), the others do not.
+//
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>
 
@@ -1000,7 +1003,8 @@ cudaError_t launch_project(bool forward, const void* v, int64_t tokens, int64_t 
   // Tokens a tile and CTAs a tile by an estimate of the time: a wave's start and end, and its K blocks one after
   // another, as fitted to measurements (us, 64 tokens on 4096 x 4096 with 1, 2, 4 CTAs a tile: 22.1, 15.6, 12.0; 256:
   // 64 tokens a tile 22.6, 128 by two CTAs 18.2; 512 on 4096 x 14336: 83.0 with 128 a tile, 55.3 with 256 by two CTAs).
-  // One CTA a tile is persistent and starts once.  Clusters of eight leave a sixth of the SMs out.
+  // One CTA a tile is persistent and starts once.  Clusters of eight leave a sixth of the SMs out.  The adapters' K blocks are
+  // not in it (which a tile has is known on the GPU only): 32 adapters in any order add 8 to the 16 of a 1024-row weight's dx.
   constexpr double kStart[4] = {9.0, 9.0, 11.0, 14.0}, kBlock[4] = {0.20, 0.21, 0.27, 0.34};  // 32, 64, 128, 256 tokens
   int best_n = 32, best_c = 1;
   double best = 1e300;

@@ -208,8 +208,10 @@ cudaError_t launch_project_decode(const void* x, int64_t tokens, int64_t ld_x, c
   // 32 outputs a CTA (x is read once for them) where that fills the SMs twice, else 16
   const bool two = (w.m + 31) / 32 >= 2 * info.sm_count;
   // Beside the kernel that makes z (chained launch) where x fits the L1 that that kernel's shared memory leaves: an SM
-  // keeps its split while a CTA of it is resident (16 tokens of 16 adapters on 28672 x 8192: 94 us beside it, 76
-  // behind it; one token on 4096 x 4096: 13.2 and 16.5)
+  // keeps its split while a CTA of it is resident.  In a graph, 16 adapters of rank 16, beside it and behind it: one token on
+  // 4096 x 4096 7.6 and 11.0 us, 16 tokens on 28672 x 8192 92 and 67.  The bound lies below all that lose: 28672 x 8192
+  // does from 3 tokens on (52.6 and 48.1), while 4096 x 4096 would still gain at 8 (11.7 and 12.6), 14336 x 4096 too
+  // (20.4 and 24.2) and 4096 x 14336 at 4 (18.7 and 24.8).
   const bool early = p.chained && tokens * w.n <= 8192;
   if (tokens <= 8) return two ? launch<2, 1>(p, early, stream) : launch<1, 1>(p, early, stream);
   return two ? launch<2, 2>(p, early, stream) : launch<1, 2>(p, early, stream);
