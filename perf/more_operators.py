@@ -205,6 +205,7 @@ def prepare(case, seed):
         s["norm"] = torch.empty(1, dtype=F32, device=_dev())
         if own:
             import paper_2608_28113_gb300 as hs
+            s["lists"] = hs.hscale_tensors(s["grads"]), hs.hscale_tensors(s["out"])
             s["ws"] = torch.empty(hs.hscale_grad_norm_workspace_bytes(), dtype=U8, device=_dev())
         return s
     t, e, k = case["tokens"], case["experts"], case["k"]
@@ -362,7 +363,7 @@ def run(s):
         hs.hscale_route_backward(s["logits"], s["ids"], s["weights"], s["dweights"], case["renormalize"], s["dlogits"])
         return {"dlogits": s["dlogits"]}
     if kind == "clip":
-        hs.hscale_grad_clip(s["grads"], s["max_norm"], s["norm"], s["out"], s["ws"])
+        hs.hscale_grad_clip(s["lists"][0], s["max_norm"], s["norm"], s["lists"][1], s["ws"])
         return {"norm": s["norm"], "grads": s["buffer"]}
     act = ACTIVATIONS[case["activation"]]
     if kind == "experts":
