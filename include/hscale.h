@@ -39,6 +39,9 @@
  *                                       adapters of many requests beside it (serving, training)
  *      hscale_project_backward          its gradients, for training the adapters
  *      hscale_checkpoint_save, _load    activations kept in 8 bits for that backward pass
+ *   4. hscale_route, _route_backward    a mixture of experts: the choice of each token's experts
+ *      hscale_experts, _backward        the layer of experts with packed weights, and its gradients
+ *   5. hscale_grad_norm, hscale_grad_clip   the norm over many gradients, and clipping by it
  *
  * Equation numbers count the paper's displayed equations in order (Eq. 1 is the
  * effective scale s = s_g * l).
@@ -566,6 +569,91 @@ int hscale_project_backward(const void* dy_bf16, int64_t tokens, int64_t m, int6
                             const void* a_bf16, const void* b_bf16, const float* alpha, int64_t adapters,
                             int64_t rank, const int32_t* adapter_of, void* dx_bf16, int64_t ld_dx, void* da_bf16,
                             void* db_bf16, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Element types of the calls that take several. */
+typedef enum hscale_type { HSCALE_BF16 = 0, HSCALE_F32 = 1, HSCALE_F16 = 2 } hscale_type;
+
+/*
+ * The router of a mixture of experts: of each token's logits [tokens, experts] (bf16 or fp32, rows ld_logits elements
+ * apart) the k largest, in descending order and the lowest index first among equal ones: ids [tokens, k], and
+ *   weights_j = p_j with p = softmax(logits), or (renormalize) p_j / sum of the chosen p     (fp32 [tokens, k]).
+ * A logit of -Inf or NaN is an expert that is off: never chosen, p = 0; +Inf counts as the largest finite number, and
+ * the type's lowest number as any other.  Where fewer than k experts are on, the rest of ids is -1 and of weights 0.
+ * experts at most 1024, k at most 32.  Logits may have any alignment of their type.
+ */
+int hscale_route(const void* logits, int32_t type, int64_t tokens, int64_t experts, int64_t ld_logits, int64_t k,
+                 int32_t renormalize, int32_t* ids, float* weights, void* stream);
+
+/*
+ * The gradient of hscale_route's weights: dlogits [tokens, experts] (the type of logits) of dweights (fp32 [tokens, k]),
+ * with the ids and weights that hscale_route gave:
+ *   renormalize:  dlogits_e = w_j (dw_j - sum_i w_i dw_i) where e = ids_j, 0 elsewhere (logits are not read, may be NULL)
+ *   else:         dlogits_e = p_e ([e = ids_j] dw_j - sum_i w_i dw_i)
+ * An id outside [0, experts) has no term, whatever its weight and dweight; one that a token has twice has both.
+ */
+int hscale_route_backward(const void* logits, int32_t type, int64_t tokens, int64_t experts, int64_t ld_logits,
+                          const int32_t* ids, const float* weights, const float* dweights, int64_t k, int32_t renormalize,
+                          void* dlogits, int64_t ld_dlogits, void* stream);
+
+/* act(g) = g s(g), or g s(2 sqrt(2 / pi) (g + 0.044715 g^3)), with s the logistic function. */
+typedef enum hscale_activation { HSCALE_ACT_SILU = 0, HSCALE_ACT_GELU_TANH = 1 } hscale_activation;
+
+/*
+ * A layer of experts whose weights are packed:
+ *   y_t = sum_j w_tj D_e (act(G_e x_t) * (U_e x_t)),  e = ids[t, j], j < k
+ * G, U [experts, inner, n] and D [experts, n, inner] are NVFP4, each matrix as hscale_refine_scales writes it: packed
+ * [experts, rows, cols/2], codes [experts, rows, cols/16] and a global scale each, scale [experts].  x and y [tokens, n]
+ * are bf16 with rows ld_x and ld_y elements apart; ids and weights [tokens, k] are contiguous.  An id outside
+ * [0, experts) has no term, whatever its weight; a token without experts gets zeros.
+ *
+ * Sums are fp32 and y is rounded once.  act(G x) * (U x) is rounded to 16 bits before the second product: to bf16, or
+ * (few tokens) to fp16 under a power of two of its row; a few tokens' x is held in fp16 under a power of two of its
+ * row, which changes elements below 2^-30 of the row's largest alone.  A token's value depends on its own row and
+ * experts only, an Inf or NaN elsewhere does not reach it; its last bits may depend on how many tokens there are.  Where its own
+ * values are not finite, NaN may stand for an Inf.  Equal calls give equal bits.
+ *
+ * n and inner are multiples of 16, experts at most 1024, k at most 32.  x and y are 16-byte aligned, ld_x and ld_y
+ * multiples of 8, packed weights 8-byte aligned.  With inner == 0, y is zero.  The workspace is 256-byte aligned; calls
+ * that may overlap need their own.
+ */
+size_t hscale_experts_workspace_bytes(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts);
+int hscale_experts(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, const int32_t* ids, const float* weights,
+                   int64_t k, const uint8_t* gate_packed, const uint8_t* gate_codes, const float* gate_scale,
+                   const uint8_t* up_packed, const uint8_t* up_codes, const float* up_scale, const uint8_t* down_packed,
+                   const uint8_t* down_codes, const float* down_scale, int64_t experts, int64_t inner, int32_t activation,
+                   void* y_bf16, int64_t ld_y, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The gradients of hscale_experts for dy (bf16 [tokens, n], rows ld_dy elements apart):
+ *   dh = D_e^T dy_t,  dweights_tj = h . dh  (fp32 [tokens, k]; 0 for an id that is none),
+ *   dx_t = sum_j w_tj (G_e^T (dh * u * act'(g)) + U_e^T (dh * act(g)))  (bf16, rows ld_dx elements apart)
+ * with g = G_e x_t, u = U_e x_t and h = act(g) * u made again from x.  The weights are frozen, and have no gradient.
+ * dx or dweights may be NULL: it is then not computed.  dh and the factors beside it are fp32, their products are rounded to bf16
+ * before G_e^T and U_e^T.  The rest is as in hscale_experts.
+ */
+size_t hscale_experts_backward_workspace_bytes(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts);
+int hscale_experts_backward(const void* dy_bf16, int64_t tokens, int64_t n, int64_t ld_dy, const void* x_bf16, int64_t ld_x,
+                            const int32_t* ids, const float* weights, int64_t k, const uint8_t* gate_packed,
+                            const uint8_t* gate_codes, const float* gate_scale, const uint8_t* up_packed,
+                            const uint8_t* up_codes, const float* up_scale, const uint8_t* down_packed,
+                            const uint8_t* down_codes, const float* down_scale, int64_t experts, int64_t inner,
+                            int32_t activation, void* dx_bf16, int64_t ld_dx, float* dweights, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * The 2-norm over many tensors, *norm = sqrt(sum of the squares of all their elements), and the tensors scaled to it:
+ *   out_i = tensors_i * min(1, max_norm / norm)
+ * tensors, out, sizes (elements) and types (hscale_type) are HOST arrays of `count`; what tensors and out point to is on
+ * the device, contiguous and aligned to its type (to 16 bytes: faster).  out == NULL scales in place; out_i has the type of
+ * tensors_i.  Where the norm is not finite nothing is scaled (out_i = tensors_i): the caller sees it in *norm.  Squares that
+ * leave fp32's range are not lost; the sum is fp64 across CTAs, and equal calls give equal bits.  count == 0: the norm
+ * is 0.  The arrays are read before the call returns, so a captured call keeps what they held.
+ */
+size_t hscale_grad_norm_workspace_bytes(void);
+int hscale_grad_norm(const void* const* tensors, const int64_t* sizes, const int32_t* types, int64_t count, float* norm,
+                     void* workspace, size_t workspace_bytes, void* stream);
+int hscale_grad_clip(const void* const* tensors, const int64_t* sizes, const int32_t* types, int64_t count, float max_norm,
+                     float* norm, void* const* out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

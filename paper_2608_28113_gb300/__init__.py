@@ -36,7 +36,10 @@ __all__ = [
     "hscale_gptq_workspace_bytes", "hscale_gptq_hscale",
     "HSCALE_CHECKPOINT_INT8", "HSCALE_CHECKPOINT_E4M3", "hscale_checkpoint_save", "hscale_checkpoint_load",
     "hscale_project_workspace_bytes", "hscale_project", "hscale_project_backward_workspace_bytes",
-    "hscale_project_backward", "EXPORTED_SYMBOLS",
+    "hscale_project_backward",
+    "HSCALE_ACT_SILU", "HSCALE_ACT_GELU_TANH", "hscale_route", "hscale_route_backward", "hscale_experts_workspace_bytes",
+    "hscale_experts", "hscale_experts_backward_workspace_bytes", "hscale_experts_backward", "TensorList", "hscale_tensors",
+    "hscale_grad_norm_workspace_bytes", "hscale_grad_norm", "hscale_grad_clip", "EXPORTED_SYMBOLS",
 ]
 
 _PKG = pathlib.Path(__file__).resolve().parent
@@ -87,6 +90,17 @@ _SIGNATURES = {
     "hscale_project_backward_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64]),
     "hscale_project_backward": (ctypes.c_int, [_P, _I64, _I64, _I64, _P, _I64, _P, _I64, _I32, _I64, _P, _P, _P, _P,
                                                _P, _P, _I64, _I64, _P, _P, _I64, _P, _P, _P, _SZ, _P]),
+    "hscale_route": (ctypes.c_int, [_P, _I32, _I64, _I64, _I64, _I64, _I32, _P, _P, _P]),
+    "hscale_route_backward": (ctypes.c_int, [_P, _I32, _I64, _I64, _I64, _P, _P, _P, _I64, _I32, _P, _I64, _P]),
+    "hscale_experts_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64]),
+    "hscale_experts": (ctypes.c_int, [_P, _I64, _I64, _I64, _P, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64,
+                                      _I32, _P, _I64, _P, _SZ, _P]),
+    "hscale_experts_backward_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64]),
+    "hscale_experts_backward": (ctypes.c_int, [_P, _I64, _I64, _I64, _P, _I64, _P, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P,
+                                               _P, _I64, _I64, _I32, _P, _I64, _P, _P, _SZ, _P]),
+    "hscale_grad_norm_workspace_bytes": (_SZ, []),
+    "hscale_grad_norm": (ctypes.c_int, [_P, _P, _P, _I64, _P, _P, _SZ, _P]),
+    "hscale_grad_clip": (ctypes.c_int, [_P, _P, _P, _I64, ctypes.c_float, _P, _P, _P, _SZ, _P]),
 }
 EXPORTED_SYMBOLS = tuple(_SIGNATURES)
 
@@ -755,3 +769,214 @@ def hscale_project_backward(dy: torch.Tensor, x_codes: torch.Tensor | None, x_sc
                                        global_scale.data_ptr(), _ptr(a), _ptr(b), _ptr(alpha), adapters, rank,
                                        _ptr(adapter_of), _ptr(dx), ld_dx, _ptr(da), _ptr(db), _ptr(workspace),
                                        nbytes, _stream_ptr(stream)))
+
+
+# ---------------------------------------------------------------- mixtures of experts
+HSCALE_ACT_SILU, HSCALE_ACT_GELU_TANH = 0, 1
+_TYPES = {torch.bfloat16: 0, torch.float32: 1, torch.float16: 2}
+
+
+def _here(t: torch.Tensor, name: str) -> None:
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
+
+
+def _logits(t: torch.Tensor, name: str) -> tuple:
+    """(tokens, experts, row stride, type) of a bf16 or fp32 [tokens, experts] view with contiguous rows."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D view")
+    if t.dtype not in (torch.bfloat16, torch.float32) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor of dtype torch.bfloat16 or torch.float32")
+    tokens, experts = t.shape
+    if experts > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must be a 2-D view with contiguous rows")
+    _here(t, name)
+    return tokens, experts, t.stride(0) if tokens > 1 else max(experts, t.stride(0)), _TYPES[t.dtype]
+
+
+def _routing(ids: torch.Tensor, weights: torch.Tensor, tokens: int) -> int:
+    """k of ids (int32) and weights (fp32) [tokens, k]."""
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise ValueError("ids must be [tokens, k]")
+    k = ids.shape[1]
+    _whole(ids, "ids", torch.int32, (tokens, k))
+    _whole(weights, "weights", torch.float32, (tokens, k))
+    return k
+
+
+def hscale_route(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, renormalize: bool, stream=None) -> None:
+    """The k largest of each token's logits (bf16 or fp32 [tokens, experts]), ties to the lowest index: ids (int32
+    [tokens, k]) and weights (fp32 [tokens, k]), softmax(logits) there, or that divided by its sum over the chosen
+    ones (renormalize).  -Inf and NaN are experts that are off; where too few are on, ids are -1 and weights 0."""
+    tokens, experts, ld, kind = _logits(logits, "logits")
+    k = _routing(ids, weights, tokens)
+    _check("hscale_route", load().hscale_route(logits.data_ptr(), kind, tokens, experts, ld, k, int(bool(renormalize)),
+                                               ids.data_ptr(), weights.data_ptr(), _stream_ptr(stream)))
+
+
+def hscale_route_backward(logits: torch.Tensor | None, ids: torch.Tensor, weights: torch.Tensor, dweights: torch.Tensor,
+                          renormalize: bool, dlogits: torch.Tensor, stream=None) -> None:
+    """dlogits (like logits) of dweights (fp32 [tokens, k]), with the ids and weights that hscale_route gave.  logits may
+    be None where the weights are renormalized."""
+    tokens, experts, ld_out, kind = _logits(dlogits, "dlogits")
+    ld = experts
+    if logits is not None:
+        rows, cols, ld, logits_kind = _logits(logits, "logits")
+        if (rows, cols, logits_kind) != (tokens, experts, kind):
+            raise ValueError("logits and dlogits must have the same shape and dtype")
+    elif not renormalize:
+        raise ValueError("logits are needed where the weights are not renormalized")
+    k = _routing(ids, weights, tokens)
+    _whole(dweights, "dweights", torch.float32, (tokens, k))
+    _check("hscale_route_backward",
+           load().hscale_route_backward(_ptr(logits), kind, tokens, experts, ld, ids.data_ptr(), weights.data_ptr(),
+                                        dweights.data_ptr(), k, int(bool(renormalize)), dlogits.data_ptr(), ld_out,
+                                        _stream_ptr(stream)))
+
+
+def _expert_matrices(gate: tuple, up: tuple, down: tuple, n: int) -> tuple:
+    """Checks of (packed, codes, scale) of each matrix; (experts, inner, the nine pointers)."""
+    u8, f32 = torch.uint8, torch.float32
+    packed = gate[0]
+    if not isinstance(packed, torch.Tensor) or packed.dim() != 3:
+        raise ValueError("gate's packed weight must be [experts, inner, n/2]")
+    experts, inner, _ = packed.shape
+    if n % 16 != 0 or inner % 16 != 0:
+        raise ValueError("n and inner must be multiples of 16")
+    pointers = []
+    for name, (p, c, s), rows, cols in (("gate", gate, inner, n), ("up", up, inner, n), ("down", down, n, inner)):
+        _whole(p, name + "'s packed weight", u8, (experts, rows, cols // 2))
+        _whole(c, name + "'s codes", u8, (experts, rows, cols // 16))
+        _whole(s, name + "'s scale", f32, (experts,))
+        pointers += [p.data_ptr(), c.data_ptr(), s.data_ptr()]
+    return experts, inner, pointers
+
+
+def hscale_experts_workspace_bytes(tokens: int, k: int, n: int, inner: int, experts: int) -> int:
+    return int(load().hscale_experts_workspace_bytes(int(tokens), int(k), int(n), int(inner), int(experts)))
+
+
+def hscale_experts(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, gate: tuple, up: tuple, down: tuple,
+                   activation: int, y: torch.Tensor, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """y_t (bf16 [tokens, n]) = sum_j weights[t, j] D (act(G x_t) * (U x_t)) of expert ids[t, j] (int32 [tokens, k]; outside
+    [0, experts): none).  gate, up and down are (packed, codes, scale) of G, U [experts, inner, n] and D [experts, n,
+    inner]: packed uint8 [experts, rows, cols/2], codes uint8 [experts, rows, cols/16], scale fp32 [experts]."""
+    tokens, n, ld_x = _rows(x, "x")
+    y_rows, y_cols, ld_y = _rows(y, "y")
+    if (y_rows, y_cols) != (tokens, n):
+        raise ValueError("x and y must have the same shape")
+    _here(x, "x")
+    k = _routing(ids, weights, tokens)
+    experts, inner, pointers = _expert_matrices(gate, up, down, n)
+    lib = _lib or load()
+    workspace, nbytes = _project_workspace(
+        workspace, lib.hscale_experts_workspace_bytes(tokens, k, n, inner, experts) if workspace is None else 0, x.device, stream)
+    _check("hscale_experts",
+           lib.hscale_experts(x.data_ptr(), tokens, n, ld_x, ids.data_ptr(), weights.data_ptr(), k, *pointers, experts, inner,
+                              int(activation), y.data_ptr(), ld_y, _ptr(workspace), nbytes, _stream_ptr(stream)))
+
+
+def hscale_experts_backward_workspace_bytes(tokens: int, k: int, n: int, inner: int, experts: int) -> int:
+    return int(load().hscale_experts_backward_workspace_bytes(int(tokens), int(k), int(n), int(inner), int(experts)))
+
+
+def hscale_experts_backward(dy: torch.Tensor, x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, gate: tuple,
+                            up: tuple, down: tuple, activation: int, dx: torch.Tensor | None,
+                            dweights: torch.Tensor | None, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """The gradients of hscale_experts for dy (bf16 [tokens, n]): dx (bf16 [tokens, n]) and dweights (fp32 [tokens, k]); each
+    may be None."""
+    tokens, n, ld_dy = _rows(dy, "dy")
+    x_rows, x_cols, ld_x = _rows(x, "x")
+    if (x_rows, x_cols) != (tokens, n):
+        raise ValueError("x and dy must have the same shape")
+    ld_dx = n
+    if dx is not None:
+        dx_rows, dx_cols, ld_dx = _rows(dx, "dx")
+        if (dx_rows, dx_cols) != (tokens, n):
+            raise ValueError(f"dx must be a [{tokens}, {n}] view")
+    _here(dy, "dy")
+    k = _routing(ids, weights, tokens)
+    if dweights is not None:
+        _whole(dweights, "dweights", torch.float32, (tokens, k))
+    experts, inner, pointers = _expert_matrices(gate, up, down, n)
+    lib = _lib or load()
+    workspace, nbytes = _project_workspace(
+        workspace, lib.hscale_experts_backward_workspace_bytes(tokens, k, n, inner, experts) if workspace is None else 0,
+        dy.device, stream)
+    _check("hscale_experts_backward",
+           lib.hscale_experts_backward(dy.data_ptr(), tokens, n, ld_dy, x.data_ptr(), ld_x, ids.data_ptr(), weights.data_ptr(), k,
+                                       *pointers, experts, inner, int(activation), _ptr(dx), ld_dx, _ptr(dweights),
+                                       _ptr(workspace), nbytes, _stream_ptr(stream)))
+
+
+# ---------------------------------------------------------------- gradients
+class TensorList:
+    """Tensors of a call that takes many, checked once: a program that keeps its gradients' memory keeps this beside
+    them.  It holds the tensors; whoever moves one (``.data``, ``set_``) makes a new list."""
+
+    def __init__(self, tensors):
+        self.tensors = tuple(tensors)
+        for t in self.tensors:
+            if not isinstance(t, torch.Tensor) or t.dtype not in _TYPES or not t.is_cuda:
+                raise TypeError("tensors must be CUDA tensors of dtype bfloat16, float16 or float32")
+            if not t.is_contiguous():
+                raise ValueError("tensors must be contiguous")
+        count = len(self.tensors)
+        self.device = self.tensors[0].get_device() if count else None
+        if any(t.get_device() != self.device for t in self.tensors):
+            raise ValueError("tensors must be on one device")
+        pointers, sizes = [t.data_ptr() for t in self.tensors], [t.numel() for t in self.tensors]
+        self.pointers = (ctypes.c_void_p * count)(*pointers)
+        self.sizes = (ctypes.c_int64 * count)(*sizes)
+        self.types = (ctypes.c_int32 * count)(*[_TYPES[t.dtype] for t in self.tensors])
+        self.shape = tuple(zip(sizes, self.types))
+        spans = sorted((p, p + s * t.element_size()) for p, s, t in zip(pointers, sizes, self.tensors) if s)
+        self.disjoint = all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def hscale_tensors(tensors) -> TensorList:
+    """The tensors (or a TensorList) as a TensorList."""
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+
+
+def _grad_arguments(tensors, norm, workspace, stream) -> tuple:
+    tensors = hscale_tensors(tensors)
+    _need(norm, torch.float32, "norm")
+    if norm.numel() < 1:
+        raise ValueError("norm must hold one float32")
+    _here(norm, "norm")
+    if len(tensors) and tensors.device != norm.get_device():
+        raise ValueError("tensors and norm must be on one device")
+    lib = _lib or load()
+    workspace, nbytes = _project_workspace(workspace, lib.hscale_grad_norm_workspace_bytes() if workspace is None else 0,
+                                           norm.device, stream)
+    return lib, tensors, workspace, nbytes
+
+
+def hscale_grad_norm_workspace_bytes() -> int:
+    return int(load().hscale_grad_norm_workspace_bytes())
+
+
+def hscale_grad_norm(tensors, norm: torch.Tensor, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """norm (fp32 [1]) = the 2-norm over all elements of the tensors (bf16, fp16 and fp32; a list or a TensorList)."""
+    lib, tensors, workspace, nbytes = _grad_arguments(tensors, norm, workspace, stream)
+    _check("hscale_grad_norm", lib.hscale_grad_norm(tensors.pointers, tensors.sizes, tensors.types, len(tensors),
+                                                    norm.data_ptr(), _ptr(workspace), nbytes, _stream_ptr(stream)))
+
+
+def hscale_grad_clip(tensors, max_norm: float, norm: torch.Tensor, out=None, workspace: torch.Tensor | None = None,
+                     stream=None) -> None:
+    """norm as hscale_grad_norm, and out_i = tensors_i * min(1, max_norm / norm) (out None: in place).  Where the norm is not
+    finite nothing is scaled."""
+    lib, tensors, workspace, nbytes = _grad_arguments(tensors, norm, workspace, stream)
+    into = tensors if out is None else hscale_tensors(out)
+    if into.shape != tensors.shape or into.device != tensors.device:
+        raise ValueError("out must have the tensors' sizes, dtypes and device")
+    if not into.disjoint:
+        raise ValueError("tensors that are written must not overlap")
+    _check("hscale_grad_clip", lib.hscale_grad_clip(tensors.pointers, tensors.sizes, tensors.types, len(tensors),
+                                                    float(max_norm), norm.data_ptr(), None if out is None else into.pointers,
+                                                    _ptr(workspace), nbytes, _stream_ptr(stream)))

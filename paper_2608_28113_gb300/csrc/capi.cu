@@ -137,7 +137,7 @@ int hscale_abi_version(void) { return 4; }
 
 int hscale_device_error_flags(uint32_t* flags) {
   if (flags == nullptr) return HSCALE_ERR_NULL;
-  uint32_t a = 0, b = 0, c = 0, d = 0, e = 0, f = 0, g = 0;
+  uint32_t a = 0, b = 0, c = 0, d = 0, e = 0, f = 0, g = 0, i = 0, j = 0;
   cudaError_t err = hscale::read_hessian_device_error(&a);
   if (err == cudaSuccess) err = hscale::read_output_error_device_error(&b);
   if (err == cudaSuccess) err = hscale::read_selftest_device_error(&c);
@@ -145,7 +145,9 @@ int hscale_device_error_flags(uint32_t* flags) {
   if (err == cudaSuccess) err = hscale::read_gptq_device_error(&e);
   if (err == cudaSuccess) err = hscale::read_hessian_cluster_device_error(&f);
   if (err == cudaSuccess) err = hscale::read_project_device_error(&g);
-  *flags = a | b | c | d | e | f | g;
+  if (err == cudaSuccess) err = hscale::read_experts_device_error(&i);
+  if (err == cudaSuccess) err = hscale::read_experts_backward_device_error(&j);
+  *flags = a | b | c | d | e | f | g | i | j;
   return from_cuda(err);
 }
 

@@ -1,0 +1,586 @@
+// experts.cu -- a layer of experts with packed NVFP4 weights on the tcgen05 tensor cores:
+//   y_t = sum_j w_tj D_e (act(G_e x_t) * (U_e x_t)),  e = ids[t, j]
+// Five steps, each launched while the one before it ends: the slots (token, j) are grouped by expert; their x is laid out
+// in that order; the first product makes h = act(G x) * (U x), rounded to bf16 (the second product's operand: its error
+// is of the size of y's own rounding); the second makes w D h of each slot in fp32; a token's slots are added up in
+// order and rounded once.
+//
+// The products.  Tile: 256 rows of weights as two halves of 128 (128 rows of G and the same 128 of U, or 256 rows of
+// D) x up to kN slots of one expert, K in blocks of 64.  18 warps:
+//   0      TMA loads of the slots' tile, K-major, 128-byte swizzle
+//   1      MMAs
+//   2-5    epilogue (lane = row of weights, columns = slots)
+//   6-17   the weights: three groups of four warps take the halves' blocks in turn.  A thread has one row, 32 packed
+//          bytes and 4 codes of it a block, kept kAhead blocks ahead in registers, and writes 64 bf16 weights into
+//          tensor memory, from where the MMAs take their A operand: shared memory, which both operands would
+//          saturate, holds the slots' tile alone.
+// E2M1 times E4M3 has at most 6 significant bits: a weight without its global scale is exact in bf16.
+//
+// Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
+#include <algorithm>
+
+#include "chained_launch.h"
+#include "experts.cuh"
+#include "hscale_internal.h"
+#include "tcgen05.cuh"
+#include "tma.cuh"
+
+namespace hscale {
+namespace {
+
+__device__ uint32_t g_experts_flags = 0;
+
+// ---------------------------------------------------------------- grouping
+constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
+
+// A stable counting sort by one CTA: each warp counts a run of slots, the warps' counts are summed up expert by
+// expert, and each warp then places its run.  Integers only: equal calls give equal plans.
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __restrict__ ids, int64_t slots, int experts, int width,
+                                                            Plan plan) {
+  extern __shared__ int32_t counts[];  // [kPlanWarps][experts], then each expert's first position
+  int32_t* first = counts + kPlanWarps * experts;
+  __shared__ int32_t warp_total[kPlanWarps], warp_chunks[kPlanWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t run = (slots + kPlanWarps - 1) / kPlanWarps, s0 = warp * run, s1 = min(slots, s0 + run);
+  for (int i = threadIdx.x; i < kPlanWarps * experts; i += kPlanThreads) counts[i] = 0;
+  __syncthreads();
+  int32_t* mine = counts + warp * experts;
+  for (int64_t s = s0; s < s1; s += 32) {
+    const int id = s + lane < s1 ? ids[s + lane] : -1;
+    const bool on = (unsigned)id < (unsigned)experts;
+    const uint32_t alike = __match_any_sync(0xFFFFFFFFu, on ? id : -1);
+    if (on && __ffs(alike) - 1 == lane) mine[id] += __popc(alike);
+    __syncwarp();
+  }
+  __syncthreads();
+  // expert e = threadIdx.x (at most 1024): its slots, then the experts' first positions and first chunks
+  int total = 0;
+  if ((int)threadIdx.x < experts) {
+    for (int w = 0; w < kPlanWarps; ++w) {
+      const int c = counts[w * experts + threadIdx.x];
+      counts[w * experts + threadIdx.x] = total;
+      total += c;
+    }
+  }
+  const int pieces = (total + width - 1) / width;
+  int at = total, chunk = pieces;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int a = __shfl_up_sync(0xFFFFFFFFu, at, d), b = __shfl_up_sync(0xFFFFFFFFu, chunk, d);
+    if (lane >= d) at += a, chunk += b;
+  }
+  if (lane == 31) warp_total[warp] = at, warp_chunks[warp] = chunk;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) at += warp_total[w], chunk += warp_chunks[w];
+  if (threadIdx.x == kPlanThreads - 1) plan.header[0] = chunk, plan.header[1] = at;
+  at -= total, chunk -= pieces;
+  if ((int)threadIdx.x < experts) {
+    first[threadIdx.x] = at;
+    // chunks of nearly the same size, whole 16s
+    const int each = pieces ? ((total + pieces - 1) / pieces + 15) / 16 * 16 : 0;
+    for (int c = 0; c < pieces; ++c) {
+      const int from = min(total, c * each), to = min(total, from + each);
+      plan.chunks[chunk + c] = {(int32_t)threadIdx.x, at + from, to - from, 0};
+    }
+  }
+  __syncthreads();
+  for (int64_t s = s0; s < s1; s += 32) {
+    const int id = s + lane < s1 ? ids[s + lane] : -1;
+    const bool on = (unsigned)id < (unsigned)experts;
+    const uint32_t alike = __match_any_sync(0xFFFFFFFFu, on ? id : -1);
+    if (on) plan.slot_of[first[id] + mine[id] + __popc(alike & ((1u << lane) - 1u))] = (int32_t)(s + lane);
+    __syncwarp();
+    if (on && __ffs(alike) - 1 == lane) mine[id] += __popc(alike);
+    __syncwarp();
+  }
+}
+
+// out[pos] = x of position pos's token; 16 bytes a thread.
+__global__ void __launch_bounds__(256) gather_kernel(const uint4* x, int64_t ld, int64_t pieces, int k, Plan plan,
+                                                     uint4* out) {
+  pdl_wait_primary();
+  const int64_t pos = blockIdx.x;
+  if (pos >= plan.header[1]) return;
+  const int64_t token = plan.slot_of[pos] / k;
+  for (int64_t i = threadIdx.x; i < pieces; i += 256) out[pos * pieces + i] = x[token * ld + i];
+}
+
+// out_t = the sum of the token's slots' rows, in order; four columns a thread.
+__global__ void __launch_bounds__(256) combine_kernel(const float* part, const int32_t* ids, int64_t tokens, int k,
+                                                      int experts, int64_t n, __nv_bfloat16* out, int64_t ld) {
+  pdl_wait_primary();
+  const int64_t per = n / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= tokens * per) return;
+  const int64_t t = i / per, c = (i - t * per) * 4;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int j = 0; j < k; ++j) {
+    if ((unsigned)ids[t * k + j] >= (unsigned)experts) continue;
+    const float4 v = *reinterpret_cast<const float4*>(part + (t * k + j) * n + c);
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  uint2 r;
+  r.x = pack_bf16(s.x, s.y), r.y = pack_bf16(s.z, s.w);
+  *reinterpret_cast<uint2*>(out + t * ld + c) = r;
+}
+
+// ---------------------------------------------------------------- the products
+constexpr int kBM = 128, kBK = 64, kHalves = 2;
+constexpr int kThreads = 576;
+constexpr int kUnpackWarp0 = 6, kUnpackGroups = 3;
+constexpr int kAhead = 3;  // blocks of its own that a group has in flight
+constexpr int kModeHidden = 0, kModeRaw = 1, kModeDown = 2;
+constexpr uint32_t kTurnBytes = 4 * 2048;
+
+template <int kN>
+struct Tile {
+  static constexpr int kStages = 4;
+  static constexpr int kAccs = kN <= 64 ? 2 : 1;
+  static constexpr uint32_t kBBytes = kN * kBK * 2;
+  static constexpr uint32_t kSmemBytes = kStages * kBBytes + 1024 /* alignment */ + 256 /* barriers */ + kTurnBytes;
+  static constexpr uint32_t kAcc = kHalves * kN;                // columns of an accumulator
+  static constexpr uint32_t kA0 = kAccs * kAcc;                 // the weights' first column
+  static constexpr uint32_t kAStage = kHalves * kBK / 2;
+  static_assert(kA0 + kStages * kAStage <= 512, "tensor memory");
+};
+
+struct GemmArgs {
+  ExpertMatrix a, b;  // the tile's halves
+  int64_t rows, cols;  // of an expert's matrix
+  int32_t kb_total, tiles_o, tile_rows;  // tile_rows: between the tiles' first rows
+  int32_t activation;
+  Plan plan;
+  const float* weights;
+  void* out;
+};
+
+__device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t* r) {
+  constexpr uint32_t kSign = 0x80008000u, kMag = 0x01C001C0u;
+  const uint32_t up = w << 4;
+  const uint32_t a = __byte_perm(up, w, 0x5410), b = __byte_perm(up, w, 0x7632);
+  r[0] = mul_bf16x2(((a << 8) & kSign) | ((a << 2) & kMag), scale);
+  r[1] = mul_bf16x2((a & kSign) | ((a >> 6) & kMag), scale);
+  r[2] = mul_bf16x2(((b << 8) & kSign) | ((b << 2) & kMag), scale);
+  r[3] = mul_bf16x2((b & kSign) | ((b >> 6) & kMag), scale);
+}
+
+// D[tmem] (+)= A[tmem] * B[smem]^T: A's row in its lane, two elements of K a column.
+__device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+template <int kMode, int kN>
+__global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ GemmArgs p) {
+  using T = Tile<kN>;
+  constexpr int kStages = T::kStages, kAccs = T::kAccs;
+  extern __shared__ __align__(16) uint8_t dynamic_smem[];
+  uint8_t* smem = dynamic_smem + ((1024u - (smem_addr(dynamic_smem) & 1023u)) & 1023u);
+  uint8_t* tile_b = smem;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kStages * T::kBBytes);
+  uint64_t* empty = full + kStages;
+  uint64_t* acc_full = empty + kStages;
+  uint64_t* acc_empty = acc_full + kAccs;
+  uint64_t* mma_done = acc_empty + kAccs;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
+  uint32_t* failed = tmem_slot + 1;
+  uint32_t* turn = reinterpret_cast<uint32_t*>(smem + kStages * T::kBBytes + 256) + (threadIdx.x >> 5 & 3) * (kTurnBytes / 16);
+
+  const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1 + kHalves * 4);  // the TMA load and the warps of the halves' groups
+      mbar_init(&empty[s], 1);
+    }
+    for (int i = 0; i < kAccs; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], 128);
+    }
+    mbar_init(mma_done, 1);
+    *failed = 0u;
+    mbar_fence_init();
+    prefetch_tensormap(&vmap);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_addr(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = warp_uniform(*tmem_slot);
+  pdl_wait_primary();  // the plan and the slots' tile
+
+  const int tiles = p.plan.header[0] * p.tiles_o, step = (int)gridDim.x, first = (int)blockIdx.x;
+  const int ntiles = tiles > first ? (tiles - first + step - 1) / step : 0;
+  const int kbs = p.kb_total;
+  const uint32_t quarter = (uint32_t)(warp & 3), lane_base = (quarter * 32u) << 16;
+  const int row_in_half = (int)quarter * 32 + lane;
+
+  if (warp == 0) {
+    uint64_t policy;
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
+    uint32_t s = 0, parity = 1;
+    bool go = true;
+    for (int i = 0; i < ntiles && go; ++i) {
+      const Chunk c = p.plan.chunks[(first + i * step) / p.tiles_o];
+      for (int kb = 0; kb < kbs; ++kb) {
+        if (!mbar_wait_warp(&empty[s], parity)) {
+          if (lane == 0) atomicOr(failed, 1u);
+          go = false;
+          break;
+        }
+        if (elect_one()) {
+          mbar_arrive_expect_tx(&full[s], T::kBBytes);
+          tma_load_2d(tile_b + s * T::kBBytes, &vmap, kb * kBK, c.first, &full[s], policy);
+        }
+        __syncwarp();
+        if (++s == kStages) s = 0, parity ^= 1u;
+      }
+    }
+    ring_drain(full, kStages, s, parity);
+  } else if (warp == 1) {
+    uint32_t s = 0, parity = 0;
+    bool ok = true;
+    for (int i = 0; i < ntiles && ok; ++i) {
+      const Chunk c = p.plan.chunks[(first + i * step) / p.tiles_o];
+      const uint32_t idesc = warp_uniform(idesc_bf16_f32(kBM, (uint32_t)((c.count + 15) & ~15)));
+      const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc;
+      if (i >= kAccs && !mbar_wait_warp(&acc_empty[acc], (uint32_t)(i / kAccs - 1) & 1u)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after_sync();
+      for (int kb = 0; kb < kbs; ++kb) {
+        if (!mbar_wait_warp(&full[s], parity)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after_sync();
+        if (elect_one()) {
+          const uint64_t bd = smem_desc_k_sw128(smem_addr(tile_b + s * T::kBBytes));
+          const uint32_t a = tmem + T::kA0 + s * T::kAStage;
+#pragma unroll
+          for (int half = 0; half < kHalves; ++half)
+#pragma unroll
+            for (int kk = 0; kk < kBK / 16; ++kk)
+              umma_bf16_ts(d + half * kN, a + half * (kBK / 2) + 8 * kk, bd + 2 * kk, idesc, (uint32_t)(kb > 0 || kk > 0));
+          umma_commit(smem_addr(&empty[s]));
+        }
+        __syncwarp();
+        if (++s == kStages) s = 0, parity ^= 1u;
+      }
+      if (ok && elect_one()) umma_commit(smem_addr(&acc_full[acc]));
+      __syncwarp();
+    }
+    if (!ok && lane == 0) atomicOr(failed, 1u);
+    __syncwarp();
+    umma_drain(mma_done);
+  } else if (warp < kUnpackWarp0) {
+    bool have = true;
+    for (int i = 0; i < ntiles; ++i) {
+      const int t = first + i * step;
+      const Chunk c = p.plan.chunks[t / p.tiles_o];
+      const int64_t o0 = (int64_t)(t % p.tiles_o) * p.tile_rows, o = o0 + row_in_half;
+      const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc + lane_base;
+      const float scale_a = p.a.scale[c.expert] * kWeightUnit, scale_b = p.b.scale[c.expert] * kWeightUnit;
+      if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i / kAccs) & 1u));
+      tc_fence_after_sync();
+#pragma unroll 1
+      for (int j0 = 0; j0 < kN; j0 += 16) {
+        if (j0 >= c.count) break;
+        uint32_t a[16], b[16];
+        tmem_ld_32x32b_x16(d + (uint32_t)j0, a);
+        tmem_ld_32x32b_x16(d + (uint32_t)(kN + j0), b);
+        tmem_ld_wait();
+        if (j0 + 16 >= c.count) {
+          tc_fence_before_sync();
+          mbar_arrive(&acc_empty[acc]);
+        }
+        const int left = min(16, c.count - j0);
+        float va[16], vb[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          va[j] = have ? __uint_as_float(a[j]) * scale_a : __int_as_float(0x7FC00000);
+          vb[j] = have ? __uint_as_float(b[j]) * scale_b : __int_as_float(0x7FC00000);
+        }
+        if constexpr (kMode == kModeHidden) {
+          // rounded and turned, so that a lane stores 8 outputs of a slot at once
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            turn[j * 32 + lane] = pack_bf16(activate_fast(p.activation, va[2 * j]) * vb[2 * j],
+                                            activate_fast(p.activation, va[2 * j + 1]) * vb[2 * j + 1]);
+          __syncwarp();
+          const int pair = lane >> 2;
+          const uint4 q0 = reinterpret_cast<const uint4*>(turn)[2 * lane], q1 = reinterpret_cast<const uint4*>(turn)[2 * lane + 1];
+          const int64_t at = o0 + quarter * 32 + (lane & 3) * 8;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t pick = e ? 0x7632u : 0x5410u;
+            const uint4 r = make_uint4(__byte_perm(q0.x, q0.y, pick), __byte_perm(q0.z, q0.w, pick), __byte_perm(q1.x, q1.y, pick),
+                                       __byte_perm(q1.z, q1.w, pick));
+            // rows are a multiple of 16: 8 outputs are all there or none is
+            if (2 * pair + e < left && at < p.rows)
+              *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + (int64_t)(c.first + j0 + 2 * pair + e) * p.rows + at) = r;
+          }
+        } else if constexpr (kMode == kModeRaw) {
+          float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * 2 * p.rows + o;
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (j < left && o < p.rows) out[(int64_t)j * 2 * p.rows] = va[j], out[(int64_t)(2 * j + 1) * p.rows] = vb[j];
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            if (j >= left) break;
+            const int slot = p.plan.slot_of[c.first + j0 + j];
+            const float w = p.weights[slot];
+            float* out = static_cast<float*>(p.out) + (int64_t)slot * p.rows + o;
+            if (o < p.rows) out[0] = w * va[j];
+            if (o + kBM < p.rows) out[kBM] = w * vb[j];
+          }
+        }
+      }
+    }
+    if (!have && lane == 0) atomicOr(failed, 1u);
+  } else {
+    const int group = (warp - kUnpackWarp0) >> 2;
+    const int64_t cols = p.cols, half_cols = cols >> 1, code_cols = cols >> 4;
+    const bool wide = (cols & 63) == 0 && ((reinterpret_cast<uintptr_t>(p.a.packed) | reinterpret_cast<uintptr_t>(p.b.packed)) & 31) == 0 &&
+                      ((reinterpret_cast<uintptr_t>(p.a.codes) | reinterpret_cast<uintptr_t>(p.b.codes)) & 3) == 0;
+    // job j: half j % 2 of K block j / 2, over the CTA's tiles; this group's are group, group + 3, ...
+    const int per_tile = kHalves * kbs;
+    const int64_t total = (int64_t)ntiles * per_tile;
+    // the next job to load
+    int li = -1, lj = 0;
+    const uint8_t *wp[2] = {nullptr, nullptr}, *cp[2] = {nullptr, nullptr};
+    uint32_t ring[kAhead][8], codes[kAhead][4];
+    auto seek = [&]() {  // li, lj inside a tile; its rows
+      while (lj >= per_tile || li < 0) {
+        if (li >= 0) lj -= per_tile;
+        ++li;
+        if (li >= ntiles) return;
+        if (lj >= per_tile) continue;
+        const int t = first + li * step;
+        const int64_t e = p.plan.chunks[t / p.tiles_o].expert, o0 = (int64_t)(t % p.tiles_o) * p.tile_rows;
+        // rows past the end are read as the last one, and not stored
+        const int64_t ra = e * p.rows + min(o0 + row_in_half, p.rows - 1);
+        const int64_t rb = e * p.rows + min(o0 + row_in_half + (kMode == kModeDown ? kBM : 0), p.rows - 1);
+        wp[0] = p.a.packed + ra * half_cols, cp[0] = p.a.codes + ra * code_cols;
+        wp[1] = p.b.packed + rb * half_cols, cp[1] = p.b.codes + rb * code_cols;
+      }
+    };
+    auto load = [&](uint32_t (&q)[8], uint32_t (&c)[4]) {
+      const int64_t k0 = (int64_t)(lj >> 1) * kBK;
+      const uint8_t* w = ((lj & 1) ? wp[1] : wp[0]) + (k0 >> 1);
+      const uint8_t* code = ((lj & 1) ? cp[1] : cp[0]) + (k0 >> 4);
+      if (wide) {
+        ld_32_ahead(w, q);
+        ld_4_ahead(true, code, c[0]);
+      } else {
+        // blocks past the end of K are zeros; so is the slots' tile there
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          c[i] = q[2 * i] = q[2 * i + 1] = 0u;
+          ld_8_ahead(k0 + 16 * i < cols, w + 8 * i, q[2 * i], q[2 * i + 1]);
+          ld_1_ahead(k0 + 16 * i < cols, code + i, c[i]);
+        }
+      }
+      lj += kUnpackGroups;
+      seek();
+    };
+    lj = group;
+    seek();
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) codes[u][i] = 0u;
+      if (li < ntiles) load(ring[u], codes[u]);
+    }
+    bool go = true;
+    for (int64_t base = group; base < total && go; base += kAhead * kUnpackGroups) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int64_t job = base + u * kUnpackGroups;
+        if (job >= total || !go) break;
+        const uint32_t block = (uint32_t)(job >> 1), s = block % kStages, parity = ((block / kStages) & 1u) ^ 1u;
+        if (!mbar_wait_warp(&empty[s], parity)) {
+          go = false;
+          break;
+        }
+        tc_fence_after_sync();
+        const uint32_t dst = tmem + T::kA0 + s * T::kAStage + (uint32_t)(job & 1) * (kBK / 2) + lane_base;
+        const uint32_t code = wide ? codes[u][0] : codes[u][0] | codes[u][1] << 8 | codes[u][2] << 16 | codes[u][3] << 24;
+        const uint32_t ca = unpack_codes(code & 0xFFFFu), cb = unpack_codes(code >> 16);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t r[16];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            unpack8(ring[u][4 * h + i], __byte_perm(h ? cb : ca, 0u, (i & 2) ? 0x3232 : 0x1010), r + 4 * i);
+          tmem_st_32x32b_x16(dst + 16 * h, r);
+        }
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[s]);
+        if (li < ntiles) load(ring[u], codes[u]);
+      }
+    }
+    if (!go && lane == 0) atomicOr(failed, 1u);
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+  if (threadIdx.x == 0 && *failed) atomicOr(&g_experts_flags, kErrMbarTimeout);
+}
+
+cudaError_t slots_map(CUtensorMap* map, const void* v, int64_t cols, int64_t rows, int width) {
+  EncodeTiledFn encode = nullptr;
+  const cudaError_t err = encode_tiled_fn(&encode);
+  if (err != cudaSuccess) return err;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)cols * 2};
+  const cuuint32_t box[2] = {(cuuint32_t)kBK, (cuuint32_t)width};
+  const cuuint32_t estr[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(v), dims, strides, box, estr,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+
+template <int kMode, int kN>
+cudaError_t launch_gemm_n(const void* v, int64_t slots, const GemmArgs& p, int64_t most_tiles, int sms, cudaStream_t stream) {
+  CUtensorMap map;
+  cudaError_t err = slots_map(&map, v, p.cols, slots, kN);
+  if (err != cudaSuccess) return err;
+  auto kernel = gemm_kernel<kMode, kN>;
+  err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)Tile<kN>::kSmemBytes);
+  if (err != cudaSuccess) return err;
+  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map, p);
+}
+template <int kMode>
+cudaError_t launch_gemm(int width, const void* v, int64_t slots, GemmArgs p, int64_t chunks, int sms, cudaStream_t stream) {
+  p.tile_rows = kMode == kModeDown ? 2 * kBM : kBM;
+  p.tiles_o = (int32_t)((p.rows + p.tile_rows - 1) / p.tile_rows);
+  p.kb_total = (int32_t)((p.cols + kBK - 1) / kBK);
+  const int64_t tiles = chunks * p.tiles_o;
+  if (tiles > INT32_MAX) return cudaErrorInvalidValue;
+  switch (width) {
+    case 32: return launch_gemm_n<kMode, 32>(v, slots, p, tiles, sms, stream);
+    case 64: return launch_gemm_n<kMode, 64>(v, slots, p, tiles, sms, stream);
+    default: return launch_gemm_n<kMode, 128>(v, slots, p, tiles, sms, stream);
+  }
+}
+
+inline int64_t round256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+}  // namespace
+
+// Slots a tile: as many as an expert has on average, so that a tile's weights serve them all.
+int experts_width(int64_t slots, int64_t experts) {
+  const int64_t each = (slots + experts - 1) / experts;
+  return each <= 24 ? 32 : each <= 56 ? 64 : 128;
+}
+
+int64_t experts_plan_bytes(int64_t slots, int64_t experts) {
+  return 256 + round256(plan_chunks(slots, experts, 32) * (int64_t)sizeof(Chunk)) + round256(slots * 4);
+}
+
+Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts) {
+  uint8_t* p = static_cast<uint8_t*>(workspace);
+  Plan plan;
+  plan.header = reinterpret_cast<int32_t*>(p);
+  plan.chunks = reinterpret_cast<Chunk*>(p + 256);
+  plan.slot_of = reinterpret_cast<int32_t*>(p + 256 + round256(plan_chunks(slots, experts, 32) * (int64_t)sizeof(Chunk)));
+  return plan;
+}
+
+cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, const Plan& plan, cudaStream_t stream) {
+  const int smem = (int)((kPlanWarps + 1) * experts * 4);
+  // set once, for every call's size
+  const cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void*>(plan_kernel), (kPlanWarps + 1) * (int)kRouteExperts * 4);
+  if (err != cudaSuccess) return err;
+  plan_kernel<<<1, kPlanThreads, smem, stream>>>(r.ids, r.tokens * r.k, (int)experts, width, plan);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_experts_gather(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out,
+                                  cudaStream_t stream) {
+  return launch_chained(gather_kernel, dim3((unsigned)(r.tokens * r.k)), 256, 0, stream, static_cast<const uint4*>(x), ld / 8, n / 8,
+                        r.k, plan, static_cast<uint4*>(out));
+}
+
+cudaError_t launch_experts_combine(const float* part, const Routing& r, int64_t experts, int64_t n, void* out, int64_t ld,
+                                   cudaStream_t stream) {
+  const int64_t threads = r.tokens * (n / 4);
+  return launch_chained(combine_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, stream, part, r.ids, r.tokens, r.k,
+                        (int)experts, n, static_cast<__nv_bfloat16*>(out), ld);
+}
+
+// g and u of every position, fp32 [positions, 2, inner].
+cudaError_t launch_experts_raw(const void* xs, int64_t slots, const Experts& w, const Plan& plan, int width, float* raw,
+                               cudaStream_t stream) {
+  DeviceInfo info;
+  const cudaError_t err = current_device_info(&info);
+  if (err != cudaSuccess) return err;
+  GemmArgs p = {};
+  p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan, p.out = raw;
+  return launch_gemm<kModeRaw>(width, xs, slots, p, plan_chunks(slots, w.count, width), info.sm_count, stream);
+}
+
+int64_t experts_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
+  const int64_t slots = tokens * k;
+  return experts_plan_bytes(slots, experts) + round256(slots * n * 2) + round256(slots * inner * 2) + round256(slots * n * 4);
+}
+
+cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const Experts& w, void* y, int64_t ld_y, void* workspace,
+                           cudaStream_t stream) {
+  DeviceInfo info;
+  cudaError_t err = current_device_info(&info);
+  if (err != cudaSuccess) return err;
+  const int64_t slots = r.tokens * r.k;
+  const int width = experts_width(slots, w.count);
+  const Plan plan = experts_plan_at(workspace, slots, w.count);
+  uint8_t* xs = static_cast<uint8_t*>(workspace) + experts_plan_bytes(slots, w.count);
+  uint8_t* h = xs + round256(slots * w.n * 2);
+  float* part = reinterpret_cast<float*>(h + round256(slots * w.inner * 2));
+  const int64_t chunks = plan_chunks(slots, w.count, width);
+  if ((err = launch_experts_plan(r, w.count, width, plan, stream)) != cudaSuccess) return err;
+  if ((err = launch_experts_gather(x, ld_x, w.n, r, plan, xs, stream)) != cudaSuccess) return err;
+  GemmArgs p = {};
+  p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan, p.out = h;
+  if ((err = launch_gemm<kModeHidden>(width, xs, slots, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
+  p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.weights = r.weights, p.out = part;
+  if ((err = launch_gemm<kModeDown>(width, h, slots, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
+  return launch_experts_combine(part, r, w.count, w.n, y, ld_y, stream);
+}
+
+cudaError_t read_experts_device_error(uint32_t* flags) {
+  uint32_t v = 0;
+  cudaError_t err = cudaMemcpyFromSymbol(&v, g_experts_flags, sizeof v);
+  if (err != cudaSuccess) return err;
+  *flags = v;
+  if (v) {
+    const uint32_t zero = 0;
+    err = cudaMemcpyToSymbol(g_experts_flags, &zero, sizeof zero);
+  }
+  return err;
+}
+
+}  // namespace hscale

@@ -154,6 +154,47 @@ constexpr int64_t kDecodeTokens = 16;
 cudaError_t launch_project_decode(const void* x, int64_t tokens, int64_t ld_x, const Nvfp4Weight& w, const Adapters& ad,
                                   const float* z, void* y, int64_t ld_y, cudaStream_t stream);
 
+// The router and its gradient (route.cu); sizes are positive, experts <= kRouteExperts, k <= 32.
+constexpr int64_t kRouteExperts = 1024;
+cudaError_t launch_route(bool bf16, const void* logits, int64_t tokens, int64_t experts, int64_t ld, int64_t k,
+                         bool renormalize, int32_t* ids, float* weights, cudaStream_t stream);
+cudaError_t launch_route_backward(bool bf16, const void* logits, int64_t tokens, int64_t experts, int64_t ld,
+                                  const int32_t* ids, const float* weights, const float* dweights, int64_t k,
+                                  bool renormalize, void* dlogits, int64_t ld_out, cudaStream_t stream);
+
+// The experts' layer (experts.cuh: the structures; experts.cu, experts_backward.cu).  Sizes are positive, arguments
+// validated.
+struct Experts;
+struct Routing;
+struct Plan;
+int64_t experts_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts);
+cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const Experts& w, void* y, int64_t ld_y,
+                           void* workspace, cudaStream_t stream);
+int64_t experts_backward_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts);
+// dx or dweights may be nullptr
+cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const Routing& r,
+                                    const Experts& w, void* dx, int64_t ld_dx, float* dweights, void* workspace,
+                                    cudaStream_t stream);
+// Their steps: slots a tile; the plan's memory; the plan; rows of x in its order (contiguous); g and u of each position (fp32
+// [positions, 2, inner]); a token's slots' rows (fp32, contiguous) added up.
+int experts_width(int64_t slots, int64_t experts);
+int64_t experts_plan_bytes(int64_t slots, int64_t experts);
+Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts);
+cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, const Plan& plan, cudaStream_t stream);
+cudaError_t launch_experts_gather(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out,
+                                  cudaStream_t stream);
+cudaError_t launch_experts_raw(const void* xs, int64_t slots, const Experts& w, const Plan& plan, int width, float* raw,
+                               cudaStream_t stream);
+cudaError_t launch_experts_combine(const float* part, const Routing& r, int64_t experts, int64_t n, void* out, int64_t ld,
+                                   cudaStream_t stream);
+
+// The norm over tensors and, with clip, the tensors scaled into out (nullptr: in place); host arrays.
+// parts: kGradParts doubles.
+constexpr int kGradParts = 1024;
+constexpr int kGradBF16 = 0, kGradF32 = 1, kGradF16 = 2;
+cudaError_t launch_grad_norm(const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types,
+                             int64_t count, bool clip, float max_norm, float* norm, double* parts, cudaStream_t stream);
+
 // Sticky device error flags of each translation unit (bit 0: a bounded wait ran out);
 // cleared on read.
 cudaError_t read_hessian_device_error(uint32_t* flags);
@@ -162,6 +203,8 @@ cudaError_t read_update_device_error(uint32_t* flags);
 cudaError_t read_gptq_device_error(uint32_t* flags);
 cudaError_t read_hessian_cluster_device_error(uint32_t* flags);
 cudaError_t read_project_device_error(uint32_t* flags);
+cudaError_t read_experts_device_error(uint32_t* flags);
+cudaError_t read_experts_backward_device_error(uint32_t* flags);
 cudaError_t read_selftest_device_error(uint32_t* flags);
 
 // One CTA waits at most `polls` polls on an mbarrier that nothing arrives on.
