@@ -30,8 +30,11 @@ namespace {
 
 __device__ uint32_t g_experts_flags = 0;
 
+constexpr int kSpreadKept = 4;  // 16-byte pieces of a row that a thread keeps in registers: 8192 columns
+
 // ---------------------------------------------------------------- grouping
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
+constexpr int kPlanAhead = 8;  // ids a lane has in flight: one at a time, 32768 slots took 56 us
 
 // A stable counting sort by one CTA: each warp counts a run of slots, the warps' counts are summed up expert by
 // expert, and each warp then places its run.  Integers only: equal calls give equal plans.
@@ -45,12 +48,16 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
   for (int i = threadIdx.x; i < kPlanWarps * experts; i += kPlanThreads) counts[i] = 0;
   __syncthreads();
   int32_t* mine = counts + warp * experts;
-  for (int64_t s = s0; s < s1; s += 32) {
-    const int id = s + lane < s1 ? ids[s + lane] : -1;
-    const bool on = (unsigned)id < (unsigned)experts;
-    const uint32_t alike = __match_any_sync(0xFFFFFFFFu, on ? id : -1);
-    if (on && __ffs(alike) - 1 == lane) mine[id] += __popc(alike);
-    __syncwarp();
+  for (int64_t s = s0; s < s1; s += 32 * kPlanAhead) {
+    int id[kPlanAhead];
+#pragma unroll
+    for (int u = 0; u < kPlanAhead; ++u) id[u] = s + 32 * u + lane < s1 ? ids[s + 32 * u + lane] : -1;
+#pragma unroll
+    for (int u = 0; u < kPlanAhead; ++u) {
+      if (s + 32 * u >= s1) break;
+      const bool on = (unsigned)id[u] < (unsigned)experts;
+      if (on) atomicAdd(&mine[id[u]], 1);  // the warp's own, whole numbers
+    }
   }
   __syncthreads();
   // expert e = threadIdx.x (at most 1024): its slots, then the experts' first positions and first chunks
@@ -84,39 +91,89 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
     }
   }
   __syncthreads();
-  for (int64_t s = s0; s < s1; s += 32) {
-    const int id = s + lane < s1 ? ids[s + lane] : -1;
-    const bool on = (unsigned)id < (unsigned)experts;
-    const uint32_t alike = __match_any_sync(0xFFFFFFFFu, on ? id : -1);
-    if (on) plan.slot_of[first[id] + mine[id] + __popc(alike & ((1u << lane) - 1u))] = (int32_t)(s + lane);
-    __syncwarp();
-    if (on && __ffs(alike) - 1 == lane) mine[id] += __popc(alike);
-    __syncwarp();
+  for (int64_t s = s0; s < s1; s += 32 * kPlanAhead) {
+    int id[kPlanAhead];
+#pragma unroll
+    for (int u = 0; u < kPlanAhead; ++u) id[u] = s + 32 * u + lane < s1 ? ids[s + 32 * u + lane] : -1;
+#pragma unroll
+    for (int u = 0; u < kPlanAhead; ++u) {
+      if (s + 32 * u >= s1) break;
+      const bool on = (unsigned)id[u] < (unsigned)experts;
+      const uint32_t alike = __match_any_sync(0xFFFFFFFFu, on ? id[u] : -1);
+      int pos = -1;
+      if (on) {
+        pos = first[id[u]] + mine[id[u]] + __popc(alike & ((1u << lane) - 1u));
+        plan.slot_of[pos] = (int32_t)(s + 32 * u + lane);
+      }
+      if (s + 32 * u + lane < s1) plan.pos_of[s + 32 * u + lane] = pos;
+      __syncwarp();
+      if (on && __ffs(alike) - 1 == lane) mine[id[u]] += __popc(alike);
+      __syncwarp();
+    }
   }
 }
 
-// out[pos] = x of position pos's token; 16 bytes a thread.
-__global__ void __launch_bounds__(256) gather_kernel(const uint4* x, int64_t ld, int64_t pieces, int k, Plan plan,
-                                                     uint4* out) {
+// A token's row in fp16 (experts.cuh) to the positions of its slots, with the row's amax; a row of h begins with none.
+__global__ void __launch_bounds__(256) spread_kernel(const uint4* x, int64_t ld, int64_t pieces, int k, Plan plan, uint4* out,
+                                                     uint32_t* amax, uint32_t* h_amax) {
+  __shared__ uint32_t warp_max[8];
   pdl_wait_primary();
-  const int64_t pos = blockIdx.x;
-  if (pos >= plan.header[1]) return;
-  const int64_t token = plan.slot_of[pos] / k;
-  for (int64_t i = threadIdx.x; i < pieces; i += 256) out[pos * pieces + i] = x[token * ld + i];
+  const int64_t t = blockIdx.x;
+  const uint4* row = x + t * ld;
+  uint4 kept[kSpreadKept];
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < kSpreadKept; ++i) {
+    const int64_t at = threadIdx.x + 256 * i;
+    if (at < pieces) m = max(m, amax_bf16(kept[i] = row[at]));
+  }
+  for (int64_t at = threadIdx.x + 256 * kSpreadKept; at < pieces; at += 256) m = max(m, amax_bf16(row[at]));
+  m = __reduce_max_sync(0xFFFFFFFFu, m);
+  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, warp_max[i]);
+  const float down = exp2_int(-row_exponent(m));
+#pragma unroll
+  for (int i = 0; i < kSpreadKept; ++i) kept[i] = bf16_to_f16(kept[i], down);
+  for (int j = 0; j < k; ++j) {
+    const int64_t pos = plan.pos_of[t * k + j];
+    if (pos < 0) continue;
+    if (threadIdx.x == 0) {
+      amax[pos] = m;
+      if (h_amax != nullptr) h_amax[pos] = 0u;
+    }
+    uint4* to = out + pos * pieces;
+#pragma unroll
+    for (int i = 0; i < kSpreadKept; ++i)
+      if (threadIdx.x + 256 * i < pieces) to[threadIdx.x + 256 * i] = kept[i];
+    for (int64_t at = threadIdx.x + 256 * kSpreadKept; at < pieces; at += 256) to[at] = bf16_to_f16(row[at], down);
+  }
 }
 
-// out_t = the sum of the token's slots' rows, in order; four columns a thread.
-__global__ void __launch_bounds__(256) combine_kernel(const float* part, const int32_t* ids, int64_t tokens, int k,
-                                                      int experts, int64_t n, __nv_bfloat16* out, int64_t ld) {
+// h, bf16, to fp16 in place (experts.cuh), 16 bytes a thread.
+__global__ void __launch_bounds__(256) convert_kernel(uint4* h, int64_t pieces, Plan plan, const uint32_t* amax) {
+  pdl_wait_primary();
+  const int64_t total = plan.header[1] * pieces;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256)
+    h[i] = bf16_to_f16(h[i], exp2_int(-row_exponent(amax[i / pieces])));
+}
+
+// out_t = the sum of the token's slots' rows times their weights (nullptr: 1), in order; four columns a thread.
+__global__ void __launch_bounds__(256) combine_kernel(const float* part, Plan plan, const float* weights, int64_t tokens, int k, int64_t n,
+                                                      __nv_bfloat16* out, int64_t ld) {
   pdl_wait_primary();
   const int64_t per = n / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= tokens * per) return;
   const int64_t t = i / per, c = (i - t * per) * 4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
   for (int j = 0; j < k; ++j) {
-    if ((unsigned)ids[t * k + j] >= (unsigned)experts) continue;
-    const float4 v = *reinterpret_cast<const float4*>(part + (t * k + j) * n + c);
-    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    const int64_t pos = plan.pos_of[t * k + j];
+    if (pos < 0) continue;
+    const float w = weights == nullptr ? 1.0f : weights[t * k + j];
+    const float4 v = *reinterpret_cast<const float4*>(part + pos * n + c);
+    s.x = fmaf(w, v.x, s.x), s.y = fmaf(w, v.y, s.y), s.z = fmaf(w, v.z, s.z), s.w = fmaf(w, v.w, s.w);
   }
   uint2 r;
   r.x = pack_bf16(s.x, s.y), r.y = pack_bf16(s.z, s.w);
@@ -125,18 +182,22 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* part, const i
 
 // ---------------------------------------------------------------- the products
 constexpr int kBM = 128, kBK = 64, kHalves = 2;
-constexpr int kThreads = 576;
-constexpr int kUnpackWarp0 = 6, kUnpackGroups = 3;
-constexpr int kAhead = 3;  // blocks of its own that a group has in flight
+constexpr int kEpilogueWarp0 = 2, kUnpackWarp0 = 6, kUnpackWarps = 16, kWeightsWarp = 22;
+constexpr int kThreads = 768;
 constexpr int kModeHidden = 0, kModeRaw = 1, kModeDown = 2;
 constexpr uint32_t kTurnBytes = 4 * 2048;
+constexpr int kStages = 4;              // unpacked blocks and blocks of the slots' tile
+constexpr int kPackedStages = 14;       // packed blocks: 112 KB on their way or here
+constexpr uint32_t kHalfBytes = kBM * kBK / 2, kPackedBytes = kHalves * kHalfBytes;
+constexpr int kCodesAhead = 8;          // blocks of its own whose codes a thread has on their way
+constexpr uint32_t kCodeBytes = kCodesAhead * kUnpackWarps * 32 * 4;
 
 template <int kN>
 struct Tile {
-  static constexpr int kStages = 4;
   static constexpr int kAccs = kN <= 64 ? 2 : 1;
   static constexpr uint32_t kBBytes = kN * kBK * 2;
-  static constexpr uint32_t kSmemBytes = kStages * kBBytes + 1024 /* alignment */ + 256 /* barriers */ + kTurnBytes;
+  static constexpr uint32_t kSmemBytes =
+      kStages * kBBytes + kPackedStages * kPackedBytes + 1024 /* alignment */ + 512 /* barriers */ + kCodeBytes + kTurnBytes;
   static constexpr uint32_t kAcc = kHalves * kN;                // columns of an accumulator
   static constexpr uint32_t kA0 = kAccs * kAcc;                 // the weights' first column
   static constexpr uint32_t kAStage = kHalves * kBK / 2;
@@ -148,23 +209,24 @@ struct GemmArgs {
   int64_t rows, cols;  // of an expert's matrix
   int32_t kb_total, tiles_o, tile_rows;  // tile_rows: between the tiles' first rows
   int32_t activation;
+  bool bulk;  // the packed weights can be loaded by TMA, and their codes four at a time
   Plan plan;
-  const float* weights;
+  const uint32_t* amax;  // of each position's row of the slots' tile
+  uint32_t* h_amax;      // of each position's h
   void* out;
 };
 
-__device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t* r) {
-  constexpr uint32_t kSign = 0x80008000u, kMag = 0x01C001C0u;
-  const uint32_t up = w << 4;
-  const uint32_t a = __byte_perm(up, w, 0x5410), b = __byte_perm(up, w, 0x7632);
-  r[0] = mul_bf16x2(((a << 8) & kSign) | ((a << 2) & kMag), scale);
-  r[1] = mul_bf16x2((a & kSign) | ((a >> 6) & kMag), scale);
-  r[2] = mul_bf16x2(((b << 8) & kSign) | ((b << 2) & kMag), scale);
-  r[3] = mul_bf16x2((b & kSign) | ((b >> 6) & kMag), scale);
+__device__ __forceinline__ void copy_4_async(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
 }
 
 // D[tmem] (+)= A[tmem] * B[smem]^T: A's row in its lane, two elements of K a column.
-__device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void umma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
@@ -182,26 +244,38 @@ __device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_
 }
 
 template <int kMode, int kN>
-__global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ GemmArgs p) {
+__global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap vmap,
+                                                           const __grid_constant__ CUtensorMap amap,
+                                                           const __grid_constant__ CUtensorMap bmap,
+                                                           const __grid_constant__ GemmArgs p) {
   using T = Tile<kN>;
-  constexpr int kStages = T::kStages, kAccs = T::kAccs;
+  constexpr int kAccs = T::kAccs;
   extern __shared__ __align__(16) uint8_t dynamic_smem[];
   uint8_t* smem = dynamic_smem + ((1024u - (smem_addr(dynamic_smem) & 1023u)) & 1023u);
   uint8_t* tile_b = smem;
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kStages * T::kBBytes);
+  uint8_t* packed = smem + kStages * T::kBBytes;
+  uint8_t* rest = packed + kPackedStages * kPackedBytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(rest);
   uint64_t* empty = full + kStages;
   uint64_t* acc_full = empty + kStages;
   uint64_t* acc_empty = acc_full + kAccs;
-  uint64_t* mma_done = acc_empty + kAccs;
+  uint64_t* packed_full = acc_empty + kAccs;
+  uint64_t* packed_empty = packed_full + kPackedStages;
+  uint64_t* mma_done = packed_empty + kPackedStages;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
   uint32_t* failed = tmem_slot + 1;
-  uint32_t* turn = reinterpret_cast<uint32_t*>(smem + kStages * T::kBBytes + 256) + (threadIdx.x >> 5 & 3) * (kTurnBytes / 16);
+  uint32_t* turn = reinterpret_cast<uint32_t*>(rest + 512) + (threadIdx.x >> 5 & 3) * (kTurnBytes / 16);
+  uint32_t* code_ring = reinterpret_cast<uint32_t*>(rest + 512 + kTurnBytes);
 
   const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&full[s], 1 + kHalves * 4);  // the TMA load and the warps of the halves' groups
       mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < kPackedStages; ++s) {
+      mbar_init(&packed_full[s], 1);
+      mbar_init(&packed_empty[s], kHalves * 4);
     }
     for (int i = 0; i < kAccs; ++i) {
       mbar_init(&acc_full[i], 1);
@@ -211,6 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
     *failed = 0u;
     mbar_fence_init();
     prefetch_tensormap(&vmap);
+    if (p.bulk) prefetch_tensormap(&amap), prefetch_tensormap(&bmap);
   }
   if (warp == 1) {
     tmem_alloc(smem_addr(tmem_slot), 512);
@@ -255,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
     bool ok = true;
     for (int i = 0; i < ntiles && ok; ++i) {
       const Chunk c = p.plan.chunks[(first + i * step) / p.tiles_o];
-      const uint32_t idesc = warp_uniform(idesc_bf16_f32(kBM, (uint32_t)((c.count + 15) & ~15)));
+      const uint32_t idesc = warp_uniform(idesc_f16_f32(kBM, (uint32_t)((c.count + 15) & ~15)));
       const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc;
       if (i >= kAccs && !mbar_wait_warp(&acc_empty[acc], (uint32_t)(i / kAccs - 1) & 1u)) {
         ok = false;
@@ -275,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
           for (int half = 0; half < kHalves; ++half)
 #pragma unroll
             for (int kk = 0; kk < kBK / 16; ++kk)
-              umma_bf16_ts(d + half * kN, a + half * (kBK / 2) + 8 * kk, bd + 2 * kk, idesc, (uint32_t)(kb > 0 || kk > 0));
+              umma_f16_ts(d + half * kN, a + half * (kBK / 2) + 8 * kk, bd + 2 * kk, idesc, (uint32_t)(kb > 0 || kk > 0));
           umma_commit(smem_addr(&empty[s]));
         }
         __syncwarp();
@@ -294,12 +369,15 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
       const Chunk c = p.plan.chunks[t / p.tiles_o];
       const int64_t o0 = (int64_t)(t % p.tiles_o) * p.tile_rows, o = o0 + row_in_half;
       const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc + lane_base;
-      const float scale_a = p.a.scale[c.expert] * kWeightUnit, scale_b = p.b.scale[c.expert] * kWeightUnit;
+      const float scale_a = p.a.scale[c.expert], scale_b = p.b.scale[c.expert];
       if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i / kAccs) & 1u));
       tc_fence_after_sync();
 #pragma unroll 1
       for (int j0 = 0; j0 < kN; j0 += 16) {
         if (j0 >= c.count) break;
+        const int left = min(16, c.count - j0);
+        // lane j: the power of two of slot j's row
+        const float my_up = lane < left ? exp2_int(row_exponent(p.amax[c.first + j0 + lane])) : 0.0f;
         uint32_t a[16], b[16];
         tmem_ld_32x32b_x16(d + (uint32_t)j0, a);
         tmem_ld_32x32b_x16(d + (uint32_t)(kN + j0), b);
@@ -308,12 +386,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
           tc_fence_before_sync();
           mbar_arrive(&acc_empty[acc]);
         }
-        const int left = min(16, c.count - j0);
         float va[16], vb[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          va[j] = have ? __uint_as_float(a[j]) * scale_a : __int_as_float(0x7FC00000);
-          vb[j] = have ? __uint_as_float(b[j]) * scale_b : __int_as_float(0x7FC00000);
+          const float up = __shfl_sync(0xFFFFFFFFu, my_up, j);
+          va[j] = have ? __uint_as_float(a[j]) * (scale_a * up) : __int_as_float(0x7FC00000);
+          vb[j] = have ? __uint_as_float(b[j]) * (scale_b * up) : __int_as_float(0x7FC00000);
         }
         if constexpr (kMode == kModeHidden) {
           // rounded and turned, so that a lane stores 8 outputs of a slot at once
@@ -332,8 +410,13 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
             const uint4 r = make_uint4(__byte_perm(q0.x, q0.y, pick), __byte_perm(q0.z, q0.w, pick), __byte_perm(q1.x, q1.y, pick),
                                        __byte_perm(q1.z, q1.w, pick));
             // rows are a multiple of 16: 8 outputs are all there or none is
-            if (2 * pair + e < left && at < p.rows)
-              *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + (int64_t)(c.first + j0 + 2 * pair + e) * p.rows + at) = r;
+            const bool on = 2 * pair + e < left && at < p.rows;
+            const int64_t pos = c.first + j0 + 2 * pair + e;
+            if (on) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + pos * p.rows + at) = r;
+            uint32_t m = on ? amax_bf16(r) : 0u;
+            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+            if (on && (lane & 3) == 0) atomicMax(&p.h_amax[pos], m);
           }
         } else if constexpr (kMode == kModeRaw) {
           float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * 2 * p.rows + o;
@@ -341,104 +424,143 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
           for (int j = 0; j < 16; ++j)
             if (j < left && o < p.rows) out[(int64_t)j * 2 * p.rows] = va[j], out[(int64_t)(2 * j + 1) * p.rows] = vb[j];
         } else {
+          float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * p.rows + o;
+          const bool on_a = o < p.rows, on_b = o + kBM < p.rows;
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            if (j >= left) break;
-            const int slot = p.plan.slot_of[c.first + j0 + j];
-            const float w = p.weights[slot];
-            float* out = static_cast<float*>(p.out) + (int64_t)slot * p.rows + o;
-            if (o < p.rows) out[0] = w * va[j];
-            if (o + kBM < p.rows) out[kBM] = w * vb[j];
+            if (j < left && on_a) out[j * p.rows] = va[j];
+            if (j < left && on_b) out[j * p.rows + kBM] = vb[j];
           }
         }
       }
     }
     if (!have && lane == 0) atomicOr(failed, 1u);
-  } else {
-    const int group = (warp - kUnpackWarp0) >> 2;
+  } else if (warp < kUnpackWarp0 + kUnpackWarps) {
+    // group: the half it unpacks, of every other K block
+    const int group = (warp - kUnpackWarp0) >> 2, half = group & 1;
+    const ExpertMatrix& w = half ? p.b : p.a;
     const int64_t cols = p.cols, half_cols = cols >> 1, code_cols = cols >> 4;
-    const bool wide = (cols & 63) == 0 && ((reinterpret_cast<uintptr_t>(p.a.packed) | reinterpret_cast<uintptr_t>(p.b.packed)) & 31) == 0 &&
-                      ((reinterpret_cast<uintptr_t>(p.a.codes) | reinterpret_cast<uintptr_t>(p.b.codes)) & 3) == 0;
-    // job j: half j % 2 of K block j / 2, over the CTA's tiles; this group's are group, group + 3, ...
-    const int per_tile = kHalves * kbs;
-    const int64_t total = (int64_t)ntiles * per_tile;
-    // the next job to load
-    int li = -1, lj = 0;
-    const uint8_t *wp[2] = {nullptr, nullptr}, *cp[2] = {nullptr, nullptr};
-    uint32_t ring[kAhead][8], codes[kAhead][4];
-    auto seek = [&]() {  // li, lj inside a tile; its rows
-      while (lj >= per_tile || li < 0) {
-        if (li >= 0) lj -= per_tile;
-        ++li;
-        if (li >= ntiles) return;
-        if (lj >= per_tile) continue;
-        const int t = first + li * step;
-        const int64_t e = p.plan.chunks[t / p.tiles_o].expert, o0 = (int64_t)(t % p.tiles_o) * p.tile_rows;
-        // rows past the end are read as the last one, and not stored
-        const int64_t ra = e * p.rows + min(o0 + row_in_half, p.rows - 1);
-        const int64_t rb = e * p.rows + min(o0 + row_in_half + (kMode == kModeDown ? kBM : 0), p.rows - 1);
-        wp[0] = p.a.packed + ra * half_cols, cp[0] = p.a.codes + ra * code_cols;
-        wp[1] = p.b.packed + rb * half_cols, cp[1] = p.b.codes + rb * code_cols;
-      }
+    const int64_t row_in_tile = row_in_half + (kMode == kModeDown && half ? kBM : 0);
+    // rows past the end are read as the last one, or by TMA as what is behind it, and not stored
+    const auto row_of = [&](int i) {
+      const int t = first + i * step;
+      return (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows +
+             min((int64_t)(t % p.tiles_o) * p.tile_rows + row_in_tile, p.rows - 1);
     };
-    auto load = [&](uint32_t (&q)[8], uint32_t (&c)[4]) {
-      const int64_t k0 = (int64_t)(lj >> 1) * kBK;
-      const uint8_t* w = ((lj & 1) ? wp[1] : wp[0]) + (k0 >> 1);
-      const uint8_t* code = ((lj & 1) ? cp[1] : cp[0]) + (k0 >> 4);
-      if (wide) {
-        ld_32_ahead(w, q);
-        ld_4_ahead(true, code, c[0]);
-      } else {
-        // blocks past the end of K are zeros; so is the slots' tile there
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          c[i] = q[2 * i] = q[2 * i + 1] = 0u;
-          ld_8_ahead(k0 + 16 * i < cols, w + 8 * i, q[2 * i], q[2 * i + 1]);
-          ld_1_ahead(k0 + 16 * i < cols, code + i, c[i]);
+    const int total = ntiles * kbs;
+    // block b: kb of tile i.  The codes' copies are kCodesAhead blocks of the group ahead.
+    int i = 0, kb = group >> 1, ci = 0, ckb = group >> 1;
+    int64_t row = 0, code_row = 0;
+    const uint32_t code_slot = smem_addr(code_ring + (threadIdx.x - kUnpackWarp0 * 32));
+    const auto code_copy = [&](int turn_of) {
+      if (ci < ntiles) {
+        copy_4_async(code_slot + (uint32_t)turn_of * (kUnpackWarps * 32 * 4), w.codes + code_row * code_cols + (ckb << 2));
+        ckb += 2;
+        if (ckb >= kbs) {
+          while (ckb >= kbs) ckb -= kbs, ++ci;
+          if (ci < ntiles) code_row = row_of(ci);
         }
       }
-      lj += kUnpackGroups;
-      seek();
+      copies_commit();
     };
-    lj = group;
-    seek();
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) codes[u][i] = 0u;
-      if (li < ntiles) load(ring[u], codes[u]);
-    }
+    while (kb >= kbs) kb -= kbs, ++i;
+    ckb = kb, ci = i;
+    if (i < ntiles) row = code_row = row_of(i);
+    if (p.bulk)
+      for (int u = 0; u < kCodesAhead - 1; ++u) code_copy(u);
     bool go = true;
-    for (int64_t base = group; base < total && go; base += kAhead * kUnpackGroups) {
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int64_t job = base + u * kUnpackGroups;
-        if (job >= total || !go) break;
-        const uint32_t block = (uint32_t)(job >> 1), s = block % kStages, parity = ((block / kStages) & 1u) ^ 1u;
-        if (!mbar_wait_warp(&empty[s], parity)) {
+    uint32_t ps = (uint32_t)(group >> 1), parity_p = 0;
+    int turn_of = 0;
+    for (int b = group >> 1; b < total && go; b += 2) {
+      uint32_t q[8], code;
+      if (p.bulk) {
+        code_copy(turn_of == 0 ? kCodesAhead - 1 : turn_of - 1);
+        if (!mbar_wait_warp(&packed_full[ps], parity_p)) {
           go = false;
           break;
         }
-        tc_fence_after_sync();
-        const uint32_t dst = tmem + T::kA0 + s * T::kAStage + (uint32_t)(job & 1) * (kBK / 2) + lane_base;
-        const uint32_t code = wide ? codes[u][0] : codes[u][0] | codes[u][1] << 8 | codes[u][2] << 16 | codes[u][3] << 24;
-        const uint32_t ca = unpack_codes(code & 0xFFFFu), cb = unpack_codes(code >> 16);
+        // 16-byte pieces as TMA's 32-byte swizzle leaves them: swapped in every other four rows
+        const uint8_t* src = packed + ps * kPackedBytes + half * kHalfBytes + row_in_half * 32;
+        const int swap = (row_in_half >> 2) & 1;
+        const uint4 v0 = *reinterpret_cast<const uint4*>(src + 16 * swap), v1 = *reinterpret_cast<const uint4*>(src + 16 - 16 * swap);
+        q[0] = v0.x, q[1] = v0.y, q[2] = v0.z, q[3] = v0.w, q[4] = v1.x, q[5] = v1.y, q[6] = v1.z, q[7] = v1.w;
+        copies_wait<kCodesAhead - 1>();
+        code = code_ring[turn_of * (kUnpackWarps * 32) + threadIdx.x - kUnpackWarp0 * 32];
+        if (++turn_of == kCodesAhead) turn_of = 0;
+      } else {
+        // blocks past the end of K are zeros; so is the slots' tile there
+        const uint8_t *wp = w.packed + row * half_cols + ((int64_t)kb << 5), *cp = w.codes + row * code_cols + ((int64_t)kb << 2);
+        uint32_t c[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t r[16];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            unpack8(ring[u][4 * h + i], __byte_perm(h ? cb : ca, 0u, (i & 2) ? 0x3232 : 0x1010), r + 4 * i);
-          tmem_st_32x32b_x16(dst + 16 * h, r);
+        for (int e = 0; e < 4; ++e) {
+          c[e] = q[2 * e] = q[2 * e + 1] = 0u;
+          const bool on = (int64_t)kb * kBK + 16 * e < cols;
+          ld_8_ahead(on, wp + 8 * e, q[2 * e], q[2 * e + 1]);
+          ld_1_ahead(on, cp + e, c[e]);
         }
-        tmem_st_wait();
-        tc_fence_before_sync();
+        code = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+      }
+      const uint32_t s = (uint32_t)b % kStages, parity = (((uint32_t)b / kStages) & 1u) ^ 1u;
+      if (!mbar_wait_warp(&empty[s], parity)) {
+        go = false;
+        break;
+      }
+      tc_fence_after_sync();
+      const uint32_t dst = tmem + T::kA0 + s * T::kAStage + (uint32_t)half * (kBK / 2) + lane_base;
+      uint32_t ca, cb;
+      codes_f16(code, ca, cb);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t r[16];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) unpack_f16(q[4 * h + e], __byte_perm(h ? cb : ca, 0u, (e & 2) ? 0x3232 : 0x1010), r + 4 * e);
+        tmem_st_32x32b_x16(dst + 16 * h, r);
+      }
+      if (p.bulk) {
+        // only now have the loads' values been used: an arrival does not wait for loads still under way
         __syncwarp();
-        if (lane == 0) mbar_arrive(&full[s]);
-        if (li < ntiles) load(ring[u], codes[u]);
+        if (lane == 0) mbar_arrive(&packed_empty[ps]);
+        ps += 2;
+        if (ps >= kPackedStages) ps -= kPackedStages, parity_p ^= 1u;
+      }
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&full[s]);
+      kb += 2;
+      if (kb >= kbs) {
+        while (kb >= kbs) kb -= kbs, ++i;
+        if (!p.bulk && i < ntiles) row = row_of(i);
       }
     }
+    copies_wait<0>();
     if (!go && lane == 0) atomicOr(failed, 1u);
+  } else if (warp == kWeightsWarp && p.bulk) {
+    // the packed weights; an expert's other chunks read them again, from L2
+    uint64_t policy;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+    uint32_t s = 0, parity = 1;
+    bool go = true;
+    for (int i = 0; i < ntiles && go; ++i) {
+      const int t = first + i * step;
+      const int row = (int)((int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + (int64_t)(t % p.tiles_o) * p.tile_rows);
+      for (int kb = 0; kb < kbs; ++kb) {
+        if (!mbar_wait_warp(&packed_empty[s], parity)) {
+          if (lane == 0) atomicOr(failed, 1u);
+          go = false;
+          break;
+        }
+        if (elect_one()) {
+          mbar_arrive_expect_tx(&packed_full[s], kPackedBytes);
+          tma_load_2d(packed + s * kPackedBytes, &amap, kb * (kBK / 2), row, &packed_full[s], policy);
+          tma_load_2d(packed + s * kPackedBytes + kHalfBytes, &bmap, kb * (kBK / 2), row + (kMode == kModeDown ? kBM : 0),
+                      &packed_full[s], policy);
+        }
+        __syncwarp();
+        if (++s == kPackedStages) s = 0, parity ^= 1u;
+      }
+    }
+    ring_drain(packed_full, kPackedStages, s, parity);
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -464,27 +586,52 @@ cudaError_t slots_map(CUtensorMap* map, const void* v, int64_t cols, int64_t row
              : cudaErrorInvalidValue;
 }
 
+// Packed bytes [rows, bytes] in boxes of 32 x 128.
+cudaError_t packed_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t rows) {
+  EncodeTiledFn encode = nullptr;
+  const cudaError_t err = encode_tiled_fn(&encode);
+  if (err != cudaSuccess) return err;
+  const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)bytes};
+  const cuuint32_t box[2] = {(cuuint32_t)kBK / 2, (cuuint32_t)kBM};
+  const cuuint32_t estr[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(v), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+
 template <int kMode, int kN>
-cudaError_t launch_gemm_n(const void* v, int64_t slots, const GemmArgs& p, int64_t most_tiles, int sms, cudaStream_t stream) {
-  CUtensorMap map;
+cudaError_t launch_gemm_n(const void* v, int64_t slots, int64_t experts, GemmArgs p, int64_t most_tiles, int sms, cudaStream_t stream) {
+  CUtensorMap map, amap, bmap;
   cudaError_t err = slots_map(&map, v, p.cols, slots, kN);
   if (err != cudaSuccess) return err;
+  const auto at = [](const void* q, uintptr_t a) { return reinterpret_cast<uintptr_t>(q) % a == 0; };
+  p.bulk = p.cols % kBK == 0 && at(p.a.packed, 16) && at(p.b.packed, 16) && at(p.a.codes, 4) && at(p.b.codes, 4) &&
+           experts * p.rows + 2 * kBM <= INT32_MAX;
+  amap = bmap = map;
+  if (p.bulk) {
+    if ((err = packed_map(&amap, p.a.packed, p.cols / 2, experts * p.rows)) != cudaSuccess) return err;
+    if ((err = packed_map(&bmap, p.b.packed, p.cols / 2, experts * p.rows)) != cudaSuccess) return err;
+  }
   auto kernel = gemm_kernel<kMode, kN>;
   err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)Tile<kN>::kSmemBytes);
   if (err != cudaSuccess) return err;
-  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map, p);
+  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map, amap,
+                        bmap, p);
 }
 template <int kMode>
-cudaError_t launch_gemm(int width, const void* v, int64_t slots, GemmArgs p, int64_t chunks, int sms, cudaStream_t stream) {
+cudaError_t launch_gemm(int width, const void* v, int64_t slots, int64_t experts, GemmArgs p, int64_t chunks, int sms,
+                        cudaStream_t stream) {
   p.tile_rows = kMode == kModeDown ? 2 * kBM : kBM;
   p.tiles_o = (int32_t)((p.rows + p.tile_rows - 1) / p.tile_rows);
   p.kb_total = (int32_t)((p.cols + kBK - 1) / kBK);
   const int64_t tiles = chunks * p.tiles_o;
-  if (tiles > INT32_MAX) return cudaErrorInvalidValue;
+  if (tiles * p.kb_total > INT32_MAX) return cudaErrorInvalidValue;
   switch (width) {
-    case 32: return launch_gemm_n<kMode, 32>(v, slots, p, tiles, sms, stream);
-    case 64: return launch_gemm_n<kMode, 64>(v, slots, p, tiles, sms, stream);
-    default: return launch_gemm_n<kMode, 128>(v, slots, p, tiles, sms, stream);
+    case 32: return launch_gemm_n<kMode, 32>(v, slots, experts, p, tiles, sms, stream);
+    case 64: return launch_gemm_n<kMode, 64>(v, slots, experts, p, tiles, sms, stream);
+    default: return launch_gemm_n<kMode, 128>(v, slots, experts, p, tiles, sms, stream);
   }
 }
 
@@ -499,7 +646,7 @@ int experts_width(int64_t slots, int64_t experts) {
 }
 
 int64_t experts_plan_bytes(int64_t slots, int64_t experts) {
-  return 256 + round256(plan_chunks(slots, experts, 32) * (int64_t)sizeof(Chunk)) + round256(slots * 4);
+  return 256 + round256(plan_chunks(slots, experts, 32) * (int64_t)sizeof(Chunk)) + 2 * round256(slots * 4);
 }
 
 Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts) {
@@ -507,7 +654,9 @@ Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts) {
   Plan plan;
   plan.header = reinterpret_cast<int32_t*>(p);
   plan.chunks = reinterpret_cast<Chunk*>(p + 256);
-  plan.slot_of = reinterpret_cast<int32_t*>(p + 256 + round256(plan_chunks(slots, experts, 32) * (int64_t)sizeof(Chunk)));
+  p += 256 + round256(plan_chunks(slots, experts, 32) * (int64_t)sizeof(Chunk));
+  plan.slot_of = reinterpret_cast<int32_t*>(p);
+  plan.pos_of = reinterpret_cast<int32_t*>(p + round256(slots * 4));
   return plan;
 }
 
@@ -520,33 +669,33 @@ cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, co
   return cudaGetLastError();
 }
 
-cudaError_t launch_experts_gather(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out,
-                                  cudaStream_t stream) {
-  return launch_chained(gather_kernel, dim3((unsigned)(r.tokens * r.k)), 256, 0, stream, static_cast<const uint4*>(x), ld / 8, n / 8,
-                        r.k, plan, static_cast<uint4*>(out));
+cudaError_t launch_experts_spread(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out, uint32_t* amax,
+                                  uint32_t* h_amax, cudaStream_t stream) {
+  return launch_chained(spread_kernel, dim3((unsigned)r.tokens), 256, 0, stream, static_cast<const uint4*>(x), ld / 8, n / 8, r.k, plan,
+                        static_cast<uint4*>(out), amax, h_amax);
 }
 
-cudaError_t launch_experts_combine(const float* part, const Routing& r, int64_t experts, int64_t n, void* out, int64_t ld,
-                                   cudaStream_t stream) {
+cudaError_t launch_experts_combine(const float* part, const Routing& r, const float* weights, const Plan& plan, int64_t n, void* out,
+                                   int64_t ld, cudaStream_t stream) {
   const int64_t threads = r.tokens * (n / 4);
-  return launch_chained(combine_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, stream, part, r.ids, r.tokens, r.k,
-                        (int)experts, n, static_cast<__nv_bfloat16*>(out), ld);
+  return launch_chained(combine_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, stream, part, plan, weights, r.tokens, r.k, n,
+                        static_cast<__nv_bfloat16*>(out), ld);
 }
 
-// g and u of every position, fp32 [positions, 2, inner].
-cudaError_t launch_experts_raw(const void* xs, int64_t slots, const Experts& w, const Plan& plan, int width, float* raw,
-                               cudaStream_t stream) {
+cudaError_t launch_experts_raw(const void* xs, const uint32_t* amax, int64_t slots, const Experts& w, const Plan& plan, int width,
+                               float* raw, cudaStream_t stream) {
   DeviceInfo info;
   const cudaError_t err = current_device_info(&info);
   if (err != cudaSuccess) return err;
   GemmArgs p = {};
-  p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan, p.out = raw;
-  return launch_gemm<kModeRaw>(width, xs, slots, p, plan_chunks(slots, w.count, width), info.sm_count, stream);
+  p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan, p.amax = amax, p.out = raw;
+  return launch_gemm<kModeRaw>(width, xs, slots, w.count, p, plan_chunks(slots, w.count, width), info.sm_count, stream);
 }
 
 int64_t experts_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
   const int64_t slots = tokens * k;
-  return experts_plan_bytes(slots, experts) + round256(slots * n * 2) + round256(slots * inner * 2) + round256(slots * n * 4);
+  return experts_plan_bytes(slots, experts) + 2 * round256(slots * 4) + round256(slots * n * 2) + round256(slots * inner * 2) +
+         round256(slots * n * 4);
 }
 
 cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const Experts& w, void* y, int64_t ld_y, void* workspace,
@@ -557,18 +706,25 @@ cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const 
   const int64_t slots = r.tokens * r.k;
   const int width = experts_width(slots, w.count);
   const Plan plan = experts_plan_at(workspace, slots, w.count);
-  uint8_t* xs = static_cast<uint8_t*>(workspace) + experts_plan_bytes(slots, w.count);
+  uint8_t* at = static_cast<uint8_t*>(workspace) + experts_plan_bytes(slots, w.count);
+  uint32_t* amax = reinterpret_cast<uint32_t*>(at);
+  uint32_t* h_amax = reinterpret_cast<uint32_t*>(at + round256(slots * 4));
+  uint8_t* xs = at + 2 * round256(slots * 4);
   uint8_t* h = xs + round256(slots * w.n * 2);
   float* part = reinterpret_cast<float*>(h + round256(slots * w.inner * 2));
   const int64_t chunks = plan_chunks(slots, w.count, width);
   if ((err = launch_experts_plan(r, w.count, width, plan, stream)) != cudaSuccess) return err;
-  if ((err = launch_experts_gather(x, ld_x, w.n, r, plan, xs, stream)) != cudaSuccess) return err;
+  if ((err = launch_experts_spread(x, ld_x, w.n, r, plan, xs, amax, h_amax, stream)) != cudaSuccess) return err;
   GemmArgs p = {};
-  p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan, p.out = h;
-  if ((err = launch_gemm<kModeHidden>(width, xs, slots, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
-  p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.weights = r.weights, p.out = part;
-  if ((err = launch_gemm<kModeDown>(width, h, slots, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
-  return launch_experts_combine(part, r, w.count, w.n, y, ld_y, stream);
+  p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan;
+  p.amax = amax, p.h_amax = h_amax, p.out = h;
+  if ((err = launch_gemm<kModeHidden>(width, xs, slots, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
+  const int64_t blocks = std::min<int64_t>(8 * info.sm_count, (slots * (w.inner / 8) + 255) / 256);
+  err = launch_chained(convert_kernel, dim3((unsigned)blocks), 256, 0, stream, reinterpret_cast<uint4*>(h), w.inner / 8, plan, h_amax);
+  if (err != cudaSuccess) return err;
+  p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.amax = h_amax, p.out = part;
+  if ((err = launch_gemm<kModeDown>(width, h, slots, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
+  return launch_experts_combine(part, r, r.weights, plan, w.n, y, ld_y, stream);
 }
 
 cudaError_t read_experts_device_error(uint32_t* flags) {

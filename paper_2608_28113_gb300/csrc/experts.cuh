@@ -3,6 +3,7 @@
 #pragma once
 #include <cstdint>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include "hscale_device.cuh"
@@ -40,7 +41,7 @@ struct Chunk {
 struct Plan {
   int32_t* header;  // chunks, positions
   Chunk* chunks;
-  int32_t* slot_of;
+  int32_t *slot_of, *pos_of;  // pos_of: -1 for a slot without an expert
 };
 inline __host__ __device__ int64_t plan_chunks(int64_t slots, int64_t experts, int64_t width) {
   return (slots < experts ? slots : experts) + slots / width;
@@ -62,6 +63,51 @@ __device__ __forceinline__ float2 activate(int kind, float g) {
   const float s = q >= 0.0f ? part : other, rest = q >= 0.0f ? other : part;
   const float slope = rest > 0.0f ? g * dq * s * rest : 0.0f;  // rest or s may be 0 where dq is infinite
   return make_float2(g * s, s > 0.0f ? s + slope : 0.0f);
+}
+
+// Weights as fp16: E2M1 times E4M3 has at most 6 significant bits, from 2^-10 to 2688, so a weight without its global
+// scale is exact.  The card converts two nibbles in one instruction, and to fp16 only: 85 weights a cycle and
+// SM with their scales, against 43 by the bit operations that make bf16.
+
+// Four code bytes as two pairs of fp16, read as the rest of the library reads codes: sign cleared, in [1, 126] (byte
+// 127, NaN, is left by the minimum).
+__device__ __forceinline__ void codes_f16(uint32_t c4, uint32_t& lo, uint32_t& hi) {
+  c4 &= 0x7F7F7F7Fu;
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t"
+      "min.f16x2 %0, %0, %3;\n\tmin.f16x2 %1, %1, %3;\n\tmax.f16x2 %0, %0, %4;\n\tmax.f16x2 %1, %1, %4;\n\t}"
+      : "=&r"(lo), "=&r"(hi)
+      : "r"(c4), "r"(0x5F005F00u /* 448 */), "r"(0x18001800u /* 2^-9 */));
+}
+// Eight nibbles times a scale (both halves), pairs (0, 1), (2, 3), (4, 5), (6, 7).
+__device__ __forceinline__ void unpack_f16(uint32_t w, uint32_t scale, uint32_t* r) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t.reg .b32 p, q, s, t;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 p, a;\n\tcvt.rn.f16x2.e2m1x2 q, b;\n\tcvt.rn.f16x2.e2m1x2 s, c;\n\tcvt.rn.f16x2.e2m1x2 t, d;\n\t"
+      "mul.rn.f16x2 %0, p, %5;\n\tmul.rn.f16x2 %1, q, %5;\n\tmul.rn.f16x2 %2, s, %5;\n\tmul.rn.f16x2 %3, t, %5;\n\t}"
+      : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3])
+      : "r"(w), "r"(scale));
+}
+
+// The slots' operand is fp16 too, under a power of two of its row: with amax (the bits of the row's largest bf16
+// magnitude, 2^p <= amax < 2^(p + 1)) elements are held as v 2^-E, E = p - 14, so the largest is below 2^15.  fp16 has
+// 24 binades below 2^0 and bf16's 8 bits fit its 11: an element loses bits only where it is below 2^-31 of the largest, and
+// 2^-40 of the largest at most.  E >= -112: bf16's smallest numbers are still exact then.  A row with an Inf or NaN is taken as
+// it is.
+__device__ __forceinline__ int row_exponent(uint32_t amax) {
+  return amax >= 0x7F80u ? 0 : max((int)(amax >> 7) - 127 - 14, -112);
+}
+__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
+// two bf16 numbers times 2^-E as fp16
+__device__ __forceinline__ uint32_t bf16_to_f16(uint32_t v, float down) {
+  const __half2 h = __floats2half2_rn(bf16_lo(v) * down, bf16_hi(v) * down);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint4 bf16_to_f16(const uint4& v, float down) {
+  return make_uint4(bf16_to_f16(v.x, down), bf16_to_f16(v.y, down), bf16_to_f16(v.z, down), bf16_to_f16(v.w, down));
+}
+// the largest magnitude of eight bf16 numbers, as bits
+__device__ __forceinline__ uint32_t amax_bf16(const uint4& v) {
+  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+  return max(m & 0xFFFFu, m >> 16);
 }
 
 }  // namespace hscale

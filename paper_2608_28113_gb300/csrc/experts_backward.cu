@@ -49,6 +49,7 @@ struct BackArgs {
   int32_t activation;
   Plan plan;
   const float* weights;
+  const uint32_t* amax;      // of each position's dy
   const float* raw;          // g and u, [positions, 2, cols]
   const float *gate_scale, *up_scale;
   __nv_bfloat16* factors;    // [positions, 2, cols], or nullptr
@@ -178,7 +179,8 @@ __global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant
     bool ok = true;
     for (int i = 0; i < ntiles && ok; ++i) {
       const Chunk c = p.plan.chunks[(first + i * step) / p.tiles_o];
-      const uint32_t idesc = warp_uniform(idesc_bf16_f32(kBM, (uint32_t)((c.count + 15) & ~15)) | 1u << 15);
+      const uint32_t idesc = warp_uniform((kMode == kModeHidden ? idesc_f16_f32(kBM, (uint32_t)((c.count + 15) & ~15))
+                                                                   : idesc_bf16_f32(kBM, (uint32_t)((c.count + 15) & ~15))) | 1u << 15);
       const uint32_t acc = (uint32_t)i & 1u, d = tmem + acc * T::kAcc;
       if (i >= 2 && !mbar_wait_warp(&acc_empty[acc], (uint32_t)((i >> 1) - 1) & 1u)) {
         ok = false;
@@ -218,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant
       const int t = first + i * step, to = t % p.tiles_o;
       const Chunk c = p.plan.chunks[t / p.tiles_o];
       const uint32_t acc = (uint32_t)i & 1u, d = tmem + acc * T::kAcc + lane_base;
-      const float scale = kMode == kModeHidden ? p.a.scale[c.expert] * kWeightUnit : kWeightUnit;
+      const float scale = kMode == kModeHidden ? p.a.scale[c.expert] : kWeightUnit;
       if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i >> 1) & 1u));
       tc_fence_after_sync();
 #pragma unroll 1
@@ -237,10 +239,11 @@ __global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant
           }
           const int left = min(16, c.count - j0);
           const int64_t pos = c.first + j0;
-          const int my_slot = lane < left ? p.plan.slot_of[pos + lane] : 0;
           if constexpr (kMode == kModeHidden) {
+            const int my_slot = lane < left ? p.plan.slot_of[pos + lane] : 0;
             const float sg = p.gate_scale[c.expert], su = p.up_scale[c.expert];
             const float my_w = lane < left ? p.weights[my_slot] : 0.0f;
+            const float my_up = lane < left ? exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
             float dg[16], du[16];
             const float* raw = p.raw + pos * 2 * p.cols + o;
 #pragma unroll
@@ -251,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant
             float dot[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-              const float dh = have ? __uint_as_float(a[j]) * scale : nan, w = __shfl_sync(0xFFFFFFFFu, my_w, j);
+              const float dh = have ? __uint_as_float(a[j]) * (scale * __shfl_sync(0xFFFFFFFFu, my_up, j)) : nan, w = __shfl_sync(0xFFFFFFFFu, my_w, j);
               const float2 act = activate(p.activation, dg[j]);
               const float u = du[j];
               dot[j] = j < left && on ? dh * (act.x * u) : 0.0f;
@@ -271,8 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant
           } else {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-              const int slot = __shfl_sync(0xFFFFFFFFu, my_slot, j);
-              if (j < left && on) p.part[(int64_t)slot * p.cols + o] = have ? __uint_as_float(a[j]) * scale : nan;
+              if (j < left && on) p.part[(pos + j) * p.cols + o] = have ? __uint_as_float(a[j]) * scale : nan;
             }
           }
         }
@@ -335,11 +337,19 @@ __global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant
         }
         uint8_t* dst = tile_a + s * T::kABytes + (uint32_t)(job & 1) * kHalfBytes + line * 128;
         const uint32_t code = wide ? codes[u][0] : codes[u][0] | codes[u][1] << 8 | codes[u][2] << 16 | codes[u][3] << 24;
-        const uint32_t ca = unpack_codes(code & 0xFFFFu), cb = unpack_codes(code >> 16);
+        uint32_t ca, cb;
+        if constexpr (kMode == kModeHidden)
+          codes_f16(code, ca, cb);
+        else
+          ca = unpack_codes(code & 0xFFFFu), cb = unpack_codes(code >> 16);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           uint32_t r[4];
-          unpack8(ring[u][i], __byte_perm(i < 4 ? ca : cb, 0u, (i & 2) ? 0x3232 : 0x1010), r);
+          const uint32_t scale = __byte_perm(i < 4 ? ca : cb, 0u, (i & 2) ? 0x3232 : 0x1010);
+          if constexpr (kMode == kModeHidden)
+            unpack_f16(ring[u][i], scale, r);
+          else
+            unpack8(ring[u][i], scale, r);
           *reinterpret_cast<uint4*>(dst + ((i ^ (row & 7)) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
         }
         fence_proxy_async_smem();
@@ -413,7 +423,7 @@ inline int64_t dot_parts(int64_t inner) { return (inner + kHalves * kBM - 1) / (
 int64_t experts_backward_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
   const int64_t slots = tokens * k;
   // x and dy in order, whose place the slots' parts of dx take afterwards; g and u; the factors; the dots
-  return experts_plan_bytes(slots, experts) + 2 * round256(slots * n * 2) + round256(slots * inner * 8) + round256(slots * inner * 4) +
+  return experts_plan_bytes(slots, experts) + 2 * round256(slots * 4) + 2 * round256(slots * n * 2) + round256(slots * inner * 8) + round256(slots * inner * 4) +
          round256(dot_parts(inner) * slots * 4);
 }
 
@@ -425,18 +435,20 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   const int64_t slots = r.tokens * r.k;
   const int width = experts_width(slots, w.count);
   const Plan plan = experts_plan_at(workspace, slots, w.count);
-  uint8_t* xs = static_cast<uint8_t*>(workspace) + experts_plan_bytes(slots, w.count);
+  uint32_t* amax = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + experts_plan_bytes(slots, w.count));
+  uint32_t* dy_amax = amax + round256(slots * 4) / 4;
+  uint8_t* xs = reinterpret_cast<uint8_t*>(dy_amax) + round256(slots * 4);
   uint8_t* dys = xs + round256(slots * w.n * 2);
   uint8_t* raw = dys + round256(slots * w.n * 2);
   uint8_t* factors = raw + round256(slots * w.inner * 8);
   uint8_t* dots = factors + round256(slots * w.inner * 4);
   const int64_t chunks = plan_chunks(slots, w.count, width);
   if ((err = launch_experts_plan(r, w.count, width, plan, stream)) != cudaSuccess) return err;
-  if ((err = launch_experts_gather(x, ld_x, w.n, r, plan, xs, stream)) != cudaSuccess) return err;
-  if ((err = launch_experts_gather(dy, ld_dy, w.n, r, plan, dys, stream)) != cudaSuccess) return err;
-  if ((err = launch_experts_raw(xs, slots, w, plan, width, reinterpret_cast<float*>(raw), stream)) != cudaSuccess) return err;
+  if ((err = launch_experts_spread(x, ld_x, w.n, r, plan, xs, amax, nullptr, stream)) != cudaSuccess) return err;
+  if ((err = launch_experts_spread(dy, ld_dy, w.n, r, plan, dys, dy_amax, nullptr, stream)) != cudaSuccess) return err;
+  if ((err = launch_experts_raw(xs, amax, slots, w, plan, width, reinterpret_cast<float*>(raw), stream)) != cudaSuccess) return err;
   BackArgs p = {};
-  p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.activation = w.activation, p.plan = plan, p.weights = r.weights;
+  p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.activation = w.activation, p.plan = plan, p.weights = r.weights, p.amax = dy_amax;
   p.raw = reinterpret_cast<const float*>(raw), p.gate_scale = w.gate.scale, p.up_scale = w.up.scale, p.slots = slots;
   p.factors = dx != nullptr ? reinterpret_cast<__nv_bfloat16*>(factors) : nullptr;
   p.dots = dweights != nullptr ? reinterpret_cast<float*>(dots) : nullptr;
@@ -444,7 +456,7 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   if (dx != nullptr) {
     p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.part = reinterpret_cast<float*>(xs);
     if ((err = launch_back<kModeInput>(width, factors, 2, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
-    if ((err = launch_experts_combine(p.part, r, w.count, w.n, dx, ld_dx, stream)) != cudaSuccess) return err;
+    if ((err = launch_experts_combine(p.part, r, nullptr, plan, w.n, dx, ld_dx, stream)) != cudaSuccess) return err;
   }
   if (dweights == nullptr) return cudaSuccess;
   return launch_chained(dweights_kernel, dim3((unsigned)((slots + 255) / 256)), 256, 0, stream, reinterpret_cast<const float*>(dots),

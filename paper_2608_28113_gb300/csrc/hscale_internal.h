@@ -175,18 +175,19 @@ int64_t experts_backward_workspace(int64_t tokens, int64_t k, int64_t n, int64_t
 cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const Routing& r,
                                     const Experts& w, void* dx, int64_t ld_dx, float* dweights, void* workspace,
                                     cudaStream_t stream);
-// Their steps: slots a tile; the plan's memory; the plan; rows of x in its order (contiguous); g and u of each position (fp32
-// [positions, 2, inner]); a token's slots' rows (fp32, contiguous) added up.
+// Their steps: slots a tile; the plan's memory; the plan; rows of x in its order (fp16 under a power of two of each row's
+// amax, contiguous); g and u of each position (fp32 [positions, 2, inner]); a token's slots' rows (fp32, contiguous) times
+// their weights (nullptr: 1) added up.
 int experts_width(int64_t slots, int64_t experts);
 int64_t experts_plan_bytes(int64_t slots, int64_t experts);
 Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts);
 cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, const Plan& plan, cudaStream_t stream);
-cudaError_t launch_experts_gather(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out,
-                                  cudaStream_t stream);
-cudaError_t launch_experts_raw(const void* xs, int64_t slots, const Experts& w, const Plan& plan, int width, float* raw,
-                               cudaStream_t stream);
-cudaError_t launch_experts_combine(const float* part, const Routing& r, int64_t experts, int64_t n, void* out, int64_t ld,
-                                   cudaStream_t stream);
+cudaError_t launch_experts_spread(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out,
+                                  uint32_t* amax, uint32_t* h_amax, cudaStream_t stream);
+cudaError_t launch_experts_raw(const void* xs, const uint32_t* amax, int64_t slots, const Experts& w, const Plan& plan,
+                               int width, float* raw, cudaStream_t stream);
+cudaError_t launch_experts_combine(const float* part, const Routing& r, const float* weights, const Plan& plan, int64_t n,
+                                   void* out, int64_t ld, cudaStream_t stream);
 
 // The norm over tensors and, with clip, the tensors scaled into out (nullptr: in place); host arrays.
 // parts: kGradParts doubles.
