@@ -182,26 +182,34 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* part, Plan pl
 
 // ---------------------------------------------------------------- the products
 constexpr int kBM = 128, kBK = 64, kHalves = 2;
-constexpr int kEpilogueWarp0 = 2, kUnpackWarp0 = 6, kUnpackWarps = 16, kWeightsWarp = 22;
+constexpr int kEpilogueWarp0 = 2, kUnpackWarp0 = 6, kUnpackWarps = 16, kWeightsWarp0 = 22;
 constexpr int kThreads = 768;
 constexpr int kModeHidden = 0, kModeRaw = 1, kModeDown = 2;
-constexpr uint32_t kTurnBytes = 4 * 2048;
 constexpr int kStages = 4;              // unpacked blocks and blocks of the slots' tile
-constexpr int kPackedStages = 14;       // packed blocks: 112 KB on their way or here
-constexpr uint32_t kHalfBytes = kBM * kBK / 2, kPackedBytes = kHalves * kHalfBytes;
-constexpr int kCodesAhead = 8;          // blocks of its own whose codes a thread has on their way
-constexpr uint32_t kCodeBytes = kCodesAhead * kUnpackWarps * 32 * 4;
+// A packed block: kQuad blocks of K of the tile's rows, 128 bytes a row, and 16 bytes of their codes (20 where they are
+// copied as whole words from any address).
+constexpr int kQuad = 4;
+constexpr uint32_t kRowBytes = kQuad * kBK / 2, kCodeRow = 20;
+constexpr uint32_t kHalfBytes = kBM * kRowBytes, kHalfCodes = kBM * kCodeRow;
+constexpr uint32_t kPackedBytes = kHalves * (kHalfBytes + kHalfCodes);
+// How the packed weights come: read where they are unpacked (codes at an odd address), by two warps' asynchronous
+// copies (rows that TMA cannot have), by TMA.
+constexpr int kDirect = 0, kCopies = 1, kBulk = 2;
 
 template <int kN>
 struct Tile {
   static constexpr int kAccs = kN <= 64 ? 2 : 1;
+  static constexpr bool kHelp = kAccs == 1;  // the unpacking warps take part in the epilogue
+  static constexpr int kPackedStages = kN <= 64 ? 5 : 3;
+  static constexpr int kEpilogueWarps = kHelp ? 4 + kUnpackWarps : 4;
   static constexpr uint32_t kBBytes = kN * kBK * 2;
-  static constexpr uint32_t kSmemBytes =
-      kStages * kBBytes + kPackedStages * kPackedBytes + 1024 /* alignment */ + 512 /* barriers */ + kCodeBytes + kTurnBytes;
+  static constexpr uint32_t kTurnBytes = kEpilogueWarps * 1024;
+  static constexpr uint32_t kSmemBytes = kStages * kBBytes + kPackedStages * kPackedBytes + 1024 /* alignment */ + 512 /* barriers */ + kTurnBytes;
   static constexpr uint32_t kAcc = kHalves * kN;                // columns of an accumulator
   static constexpr uint32_t kA0 = kAccs * kAcc;                 // the weights' first column
   static constexpr uint32_t kAStage = kHalves * kBK / 2;
   static_assert(kA0 + kStages * kAStage <= 512, "tensor memory");
+  static_assert(kSmemBytes <= 232448, "shared memory");
 };
 
 struct GemmArgs {
@@ -209,20 +217,24 @@ struct GemmArgs {
   int64_t rows, cols;  // of an expert's matrix
   int32_t kb_total, tiles_o, tile_rows;  // tile_rows: between the tiles' first rows
   int32_t activation;
-  bool bulk;  // the packed weights can be loaded by TMA, and their codes four at a time
+  int32_t path;  // kDirect, kCopies or kBulk
+  int64_t all_rows;  // of all experts
   Plan plan;
   const uint32_t* amax;  // of each position's row of the slots' tile
   uint32_t* h_amax;      // of each position's h
   void* out;
 };
 
-__device__ __forceinline__ void copy_4_async(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+// Asynchronous copies of 4 or 8 bytes, of which `bytes` are read and the rest zeros.
+__device__ __forceinline__ void copy_4_async(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft>
-__device__ __forceinline__ void copies_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+__device__ __forceinline__ void copy_8_async(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// Arrives, as one of the barrier's count, once this thread's copies so far have landed.
+__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 
 // D[tmem] (+)= A[tmem] * B[smem]^T: A's row in its lane, two elements of K a column.
@@ -244,17 +256,17 @@ __device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_
 }
 
 template <int kMode, int kN>
-__global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap vmap,
-                                                           const __grid_constant__ CUtensorMap amap,
-                                                           const __grid_constant__ CUtensorMap bmap,
-                                                           const __grid_constant__ GemmArgs p) {
+__global__ void __launch_bounds__(kThreads, 1)
+gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
+            const __grid_constant__ CUtensorMap acodes, const __grid_constant__ CUtensorMap bcodes, const __grid_constant__ GemmArgs p) {
   using T = Tile<kN>;
-  constexpr int kAccs = T::kAccs;
+  constexpr int kAccs = T::kAccs, kPackedStages = T::kPackedStages;
   extern __shared__ __align__(16) uint8_t dynamic_smem[];
   uint8_t* smem = dynamic_smem + ((1024u - (smem_addr(dynamic_smem) & 1023u)) & 1023u);
   uint8_t* tile_b = smem;
-  uint8_t* packed = smem + kStages * T::kBBytes;
-  uint8_t* rest = packed + kPackedStages * kPackedBytes;
+  uint8_t* packed = smem + kStages * T::kBBytes;                                    // [stages][halves]
+  uint8_t* packed_codes = packed + kPackedStages * kHalves * kHalfBytes;            // [stages][halves]
+  uint8_t* rest = packed_codes + kPackedStages * kHalves * kHalfCodes;
   uint64_t* full = reinterpret_cast<uint64_t*>(rest);
   uint64_t* empty = full + kStages;
   uint64_t* acc_full = empty + kStages;
@@ -264,8 +276,6 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
   uint64_t* mma_done = packed_empty + kPackedStages;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
   uint32_t* failed = tmem_slot + 1;
-  uint32_t* turn = reinterpret_cast<uint32_t*>(rest + 512) + (threadIdx.x >> 5 & 3) * (kTurnBytes / 16);
-  uint32_t* code_ring = reinterpret_cast<uint32_t*>(rest + 512 + kTurnBytes);
 
   const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -274,18 +284,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
       mbar_init(&empty[s], 1);
     }
     for (int s = 0; s < kPackedStages; ++s) {
-      mbar_init(&packed_full[s], 1);
-      mbar_init(&packed_empty[s], kHalves * 4);
+      mbar_init(&packed_full[s], p.path == kCopies ? 2 * 32 : 1);
+      mbar_init(&packed_empty[s], kUnpackWarps);
     }
     for (int i = 0; i < kAccs; ++i) {
       mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], 128);
+      mbar_init(&acc_empty[i], T::kEpilogueWarps);
     }
     mbar_init(mma_done, 1);
     *failed = 0u;
     mbar_fence_init();
     prefetch_tensormap(&vmap);
-    if (p.bulk) prefetch_tensormap(&amap), prefetch_tensormap(&bmap);
+    if (p.path == kBulk) prefetch_tensormap(&amap), prefetch_tensormap(&bmap), prefetch_tensormap(&acodes), prefetch_tensormap(&bcodes);
   }
   if (warp == 1) {
     tmem_alloc(smem_addr(tmem_slot), 512);
@@ -299,9 +309,82 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
 
   const int tiles = p.plan.header[0] * p.tiles_o, step = (int)gridDim.x, first = (int)blockIdx.x;
   const int ntiles = tiles > first ? (tiles - first + step - 1) / step : 0;
-  const int kbs = p.kb_total;
+  const int kbs = p.kb_total, quads = (kbs + kQuad - 1) / kQuad;
   const uint32_t quarter = (uint32_t)(warp & 3), lane_base = (quarter * 32u) << 16;
   const int row_in_half = (int)quarter * 32 + lane;
+  bool have = true;  // of the warps of the epilogue: no wait for an accumulator has run out
+
+  // The epilogue of the CTA's tile i: 16 slots a time, those of this warp (one of T::kEpilogueWarps / 4 of its quarter).
+  const auto finish = [&](int i, int who, uint32_t* turn) {
+    constexpr int kWorkers = T::kEpilogueWarps / 4;
+    const int t = first + i * step;
+    const Chunk c = p.plan.chunks[t / p.tiles_o];
+    const int64_t o0 = (int64_t)(t % p.tiles_o) * p.tile_rows, o = o0 + row_in_half;
+    const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc + lane_base;
+    const float scale_a = p.a.scale[c.expert], scale_b = p.b.scale[c.expert];
+    const float nan = __int_as_float(0x7FC00000);
+    if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i / kAccs) & 1u));
+    tc_fence_after_sync();
+#pragma unroll 1
+    for (int j0 = 16 * who; j0 < c.count; j0 += 16 * kWorkers) {
+      const int left = min(16, c.count - j0);
+      // lane j: the power of two of slot j's row
+      const float my_up = lane < left ? exp2_int(row_exponent(p.amax[c.first + j0 + lane])) : 0.0f;
+      uint32_t a[16], b[16];
+      tmem_ld_32x32b_x16(d + (uint32_t)j0, a);
+      tmem_ld_32x32b_x16(d + (uint32_t)(kN + j0), b);
+      tmem_ld_wait();
+      if constexpr (kMode == kModeHidden) {
+        // rounded and turned, so that a lane stores 8 outputs of a slot at once
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float h[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float up = __shfl_sync(0xFFFFFFFFu, my_up, 2 * j + e);
+            h[e] = activate_fast(p.activation, __uint_as_float(a[2 * j + e]) * (scale_a * up)) *
+                   (__uint_as_float(b[2 * j + e]) * (scale_b * up));
+          }
+          turn[j * 32 + lane] = have ? pack_bf16(h[0], h[1]) : 0x7FC07FC0u;
+        }
+        __syncwarp();
+        const int pair = lane >> 2;
+        const uint4 q0 = reinterpret_cast<const uint4*>(turn)[2 * lane], q1 = reinterpret_cast<const uint4*>(turn)[2 * lane + 1];
+        const int64_t at = o0 + quarter * 32 + (lane & 3) * 8;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t pick = e ? 0x7632u : 0x5410u;
+          const uint4 r = make_uint4(__byte_perm(q0.x, q0.y, pick), __byte_perm(q0.z, q0.w, pick), __byte_perm(q1.x, q1.y, pick),
+                                     __byte_perm(q1.z, q1.w, pick));
+          // rows are a multiple of 16: 8 outputs are all there or none is
+          const bool on = 2 * pair + e < left && at < p.rows;
+          const int64_t pos = c.first + j0 + 2 * pair + e;
+          if (on) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + pos * p.rows + at) = r;
+          uint32_t m = on ? amax_bf16(r) : 0u;
+          m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+          m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+          if (on && (lane & 3) == 0) atomicMax(&p.h_amax[pos], m);
+        }
+      } else {
+        // 32 outputs of a slot side by side: raw [position][2][rows], or the part of y [position][rows]
+        const int64_t stride = kMode == kModeRaw ? 2 * p.rows : p.rows, second = kMode == kModeRaw ? p.rows : kBM;
+        float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * stride + o;
+        const bool on_a = o < p.rows, on_b = kMode == kModeRaw ? on_a : o + kBM < p.rows;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float up = __shfl_sync(0xFFFFFFFFu, my_up, j);
+          if (j < left && on_a) out[0] = have ? __uint_as_float(a[j]) * (scale_a * up) : nan;
+          if (j < left && on_b) out[second] = have ? __uint_as_float(b[j]) * (scale_b * up) : nan;
+          out += stride;
+        }
+      }
+    }
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+  };
+  const auto turn_at = [&](int worker) { return reinterpret_cast<uint32_t*>(rest + 512 + worker * 1024); };
 
   if (warp == 0) {
     uint64_t policy;
@@ -363,179 +446,111 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
     __syncwarp();
     umma_drain(mma_done);
   } else if (warp < kUnpackWarp0) {
-    bool have = true;
-    for (int i = 0; i < ntiles; ++i) {
-      const int t = first + i * step;
-      const Chunk c = p.plan.chunks[t / p.tiles_o];
-      const int64_t o0 = (int64_t)(t % p.tiles_o) * p.tile_rows, o = o0 + row_in_half;
-      const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc + lane_base;
-      const float scale_a = p.a.scale[c.expert], scale_b = p.b.scale[c.expert];
-      if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i / kAccs) & 1u));
-      tc_fence_after_sync();
-#pragma unroll 1
-      for (int j0 = 0; j0 < kN; j0 += 16) {
-        if (j0 >= c.count) break;
-        const int left = min(16, c.count - j0);
-        // lane j: the power of two of slot j's row
-        const float my_up = lane < left ? exp2_int(row_exponent(p.amax[c.first + j0 + lane])) : 0.0f;
-        uint32_t a[16], b[16];
-        tmem_ld_32x32b_x16(d + (uint32_t)j0, a);
-        tmem_ld_32x32b_x16(d + (uint32_t)(kN + j0), b);
-        tmem_ld_wait();
-        if (j0 + 16 >= c.count) {
-          tc_fence_before_sync();
-          mbar_arrive(&acc_empty[acc]);
-        }
-        float va[16], vb[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float up = __shfl_sync(0xFFFFFFFFu, my_up, j);
-          va[j] = have ? __uint_as_float(a[j]) * (scale_a * up) : __int_as_float(0x7FC00000);
-          vb[j] = have ? __uint_as_float(b[j]) * (scale_b * up) : __int_as_float(0x7FC00000);
-        }
-        if constexpr (kMode == kModeHidden) {
-          // rounded and turned, so that a lane stores 8 outputs of a slot at once
-          __syncwarp();
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            turn[j * 32 + lane] = pack_bf16(activate_fast(p.activation, va[2 * j]) * vb[2 * j],
-                                            activate_fast(p.activation, va[2 * j + 1]) * vb[2 * j + 1]);
-          __syncwarp();
-          const int pair = lane >> 2;
-          const uint4 q0 = reinterpret_cast<const uint4*>(turn)[2 * lane], q1 = reinterpret_cast<const uint4*>(turn)[2 * lane + 1];
-          const int64_t at = o0 + quarter * 32 + (lane & 3) * 8;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t pick = e ? 0x7632u : 0x5410u;
-            const uint4 r = make_uint4(__byte_perm(q0.x, q0.y, pick), __byte_perm(q0.z, q0.w, pick), __byte_perm(q1.x, q1.y, pick),
-                                       __byte_perm(q1.z, q1.w, pick));
-            // rows are a multiple of 16: 8 outputs are all there or none is
-            const bool on = 2 * pair + e < left && at < p.rows;
-            const int64_t pos = c.first + j0 + 2 * pair + e;
-            if (on) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + pos * p.rows + at) = r;
-            uint32_t m = on ? amax_bf16(r) : 0u;
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-            if (on && (lane & 3) == 0) atomicMax(&p.h_amax[pos], m);
-          }
-        } else if constexpr (kMode == kModeRaw) {
-          float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * 2 * p.rows + o;
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (j < left && o < p.rows) out[(int64_t)j * 2 * p.rows] = va[j], out[(int64_t)(2 * j + 1) * p.rows] = vb[j];
-        } else {
-          float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * p.rows + o;
-          const bool on_a = o < p.rows, on_b = o + kBM < p.rows;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            if (j < left && on_a) out[j * p.rows] = va[j];
-            if (j < left && on_b) out[j * p.rows + kBM] = vb[j];
-          }
-        }
-      }
-    }
+    for (int i = 0; i < ntiles; ++i) finish(i, 0, turn_at(warp - kEpilogueWarp0));
     if (!have && lane == 0) atomicOr(failed, 1u);
-  } else if (warp < kUnpackWarp0 + kUnpackWarps) {
+  } else if (warp < kWeightsWarp0) {
     // group: the half it unpacks, of every other K block
-    const int group = (warp - kUnpackWarp0) >> 2, half = group & 1;
+    const int group = (warp - kUnpackWarp0) >> 2, half = group & 1, odd = group >> 1;
     const ExpertMatrix& w = half ? p.b : p.a;
     const int64_t cols = p.cols, half_cols = cols >> 1, code_cols = cols >> 4;
-    const int64_t row_in_tile = row_in_half + (kMode == kModeDown && half ? kBM : 0);
-    // rows past the end are read as the last one, or by TMA as what is behind it, and not stored
-    const auto row_of = [&](int i) {
-      const int t = first + i * step;
-      return (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows +
-             min((int64_t)(t % p.tiles_o) * p.tile_rows + row_in_tile, p.rows - 1);
-    };
-    const int total = ntiles * kbs;
-    // block b: kb of tile i.  The codes' copies are kCodesAhead blocks of the group ahead.
-    int i = 0, kb = group >> 1, ci = 0, ckb = group >> 1;
-    int64_t row = 0, code_row = 0;
-    const uint32_t code_slot = smem_addr(code_ring + (threadIdx.x - kUnpackWarp0 * 32));
-    const auto code_copy = [&](int turn_of) {
-      if (ci < ntiles) {
-        copy_4_async(code_slot + (uint32_t)turn_of * (kUnpackWarps * 32 * 4), w.codes + code_row * code_cols + (ckb << 2));
-        ckb += 2;
-        if (ckb >= kbs) {
-          while (ckb >= kbs) ckb -= kbs, ++ci;
-          if (ci < ntiles) code_row = row_of(ci);
-        }
-      }
-      copies_commit();
-    };
-    while (kb >= kbs) kb -= kbs, ++i;
-    ckb = kb, ci = i;
-    if (i < ntiles) row = code_row = row_of(i);
-    if (p.bulk)
-      for (int u = 0; u < kCodesAhead - 1; ++u) code_copy(u);
+    const int row_in_tile = row_in_half + (kMode == kModeDown && half ? kBM : 0);
+    const uint32_t src = smem_addr(packed + half * kHalfBytes + row_in_half * kRowBytes), swizzle = (uint32_t)row_in_half & 7u;
+    const uint32_t code_src = smem_addr(packed_codes + half * kHalfCodes);
+    uint32_t* turn = turn_at(T::kHelp ? 4 + warp - kUnpackWarp0 : 0);
     bool go = true;
-    uint32_t ps = (uint32_t)(group >> 1), parity_p = 0;
-    int turn_of = 0;
-    for (int b = group >> 1; b < total && go; b += 2) {
-      uint32_t q[8], code;
-      if (p.bulk) {
-        code_copy(turn_of == 0 ? kCodesAhead - 1 : turn_of - 1);
-        if (!mbar_wait_warp(&packed_full[ps], parity_p)) {
-          go = false;
-          break;
+    uint32_t stage = 0, parity_p = 0, block0 = 0;  // block0: of the tile's first K block
+    for (int i = 0; i < ntiles; ++i, block0 += (uint32_t)kbs) {
+      int64_t row = 0;
+      uint32_t shift = 0;  // bits that a row's codes begin into a word
+      if (p.path != kBulk) {
+        // rows past the end are read as the last one, or as what is behind it, and not stored
+        const int t = first + i * step;
+        const int64_t in_tile = (int64_t)(t % p.tiles_o) * p.tile_rows + row_in_tile;
+        row = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows;
+        if (p.path == kCopies)
+          shift = (uint32_t)((row + in_tile) * code_cols & 3) * 8;
+        else
+          row += min(in_tile, p.rows - 1);
+      }
+      for (int quad = 0; quad < quads && go; ++quad) {
+        uint32_t code[2] = {0u, 0u};
+        if (p.path != kDirect) {
+          if (!mbar_wait_warp(&packed_full[stage], parity_p)) {
+            go = false;
+            break;
+          }
+          const uint32_t at = code_src + stage * (kHalves * kHalfCodes) + row_in_half * (p.path == kBulk ? 16u : kCodeRow);
+          if (p.path == kBulk) {
+            uint32_t c[4];
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]) : "r"(at));
+            code[0] = odd ? c[1] : c[0], code[1] = odd ? c[3] : c[2];
+          } else {
+            uint32_t c[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(c[e]) : "r"(at + 4 * (odd + e)));
+            code[0] = __funnelshift_r(c[0], c[1], shift), code[1] = __funnelshift_r(c[2], c[3], shift);
+          }
         }
-        // 16-byte pieces as TMA's 32-byte swizzle leaves them: swapped in every other four rows
-        const uint8_t* src = packed + ps * kPackedBytes + half * kHalfBytes + row_in_half * 32;
-        const int swap = (row_in_half >> 2) & 1;
-        const uint4 v0 = *reinterpret_cast<const uint4*>(src + 16 * swap), v1 = *reinterpret_cast<const uint4*>(src + 16 - 16 * swap);
-        q[0] = v0.x, q[1] = v0.y, q[2] = v0.z, q[3] = v0.w, q[4] = v1.x, q[5] = v1.y, q[6] = v1.z, q[7] = v1.w;
-        copies_wait<kCodesAhead - 1>();
-        code = code_ring[turn_of * (kUnpackWarps * 32) + threadIdx.x - kUnpackWarp0 * 32];
-        if (++turn_of == kCodesAhead) turn_of = 0;
-      } else {
-        // blocks past the end of K are zeros; so is the slots' tile there
-        const uint8_t *wp = w.packed + row * half_cols + ((int64_t)kb << 5), *cp = w.codes + row * code_cols + ((int64_t)kb << 2);
-        uint32_t c[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          c[e] = q[2 * e] = q[2 * e + 1] = 0u;
-          const bool on = (int64_t)kb * kBK + 16 * e < cols;
-          ld_8_ahead(on, wp + 8 * e, q[2 * e], q[2 * e + 1]);
-          ld_1_ahead(on, cp + e, c[e]);
+        for (int u = 0; u < 2; ++u) {
+          const int in_quad = odd + 2 * u, kb = kQuad * quad + in_quad;
+          if (kb >= kbs || !go) break;
+          uint32_t q[8];
+          if (p.path != kDirect) {
+            const uint32_t from = src + stage * (kHalves * kHalfBytes);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                           : "=r"(q[4 * e]), "=r"(q[4 * e + 1]), "=r"(q[4 * e + 2]), "=r"(q[4 * e + 3])
+                           : "r"(from + ((((uint32_t)(2 * in_quad + e)) ^ swizzle) << 4)));
+          } else {
+            // blocks past the end of K are zeros; so is the slots' tile there
+            const uint8_t *wp = w.packed + row * half_cols + ((int64_t)kb << 5), *cp = w.codes + row * code_cols + ((int64_t)kb << 2);
+            uint32_t c[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              c[e] = q[2 * e] = q[2 * e + 1] = 0u;
+              const bool on = (int64_t)kb * kBK + 16 * e < cols;
+              ld_8_ahead(on, wp + 8 * e, q[2 * e], q[2 * e + 1]);
+              ld_1_ahead(on, cp + e, c[e]);
+            }
+            code[u] = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+          }
+          const uint32_t block = block0 + (uint32_t)kb, s = block % kStages;
+          if (!mbar_wait_warp(&empty[s], ((block / kStages) & 1u) ^ 1u)) {
+            go = false;
+            break;
+          }
+          tc_fence_after_sync();
+          const uint32_t dst = tmem + T::kA0 + s * T::kAStage + (uint32_t)half * (kBK / 2) + lane_base;
+          uint32_t ca, cb;
+          codes_f16(code[u], ca, cb);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t r[16];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) unpack_f16(q[4 * h + e], __byte_perm(h ? cb : ca, 0u, (e & 2) ? 0x3232 : 0x1010), r + 4 * e);
+            tmem_st_32x32b_x16(dst + 16 * h, r);
+          }
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&full[s]);
         }
-        code = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
-      }
-      const uint32_t s = (uint32_t)b % kStages, parity = (((uint32_t)b / kStages) & 1u) ^ 1u;
-      if (!mbar_wait_warp(&empty[s], parity)) {
-        go = false;
-        break;
-      }
-      tc_fence_after_sync();
-      const uint32_t dst = tmem + T::kA0 + s * T::kAStage + (uint32_t)half * (kBK / 2) + lane_base;
-      uint32_t ca, cb;
-      codes_f16(code, ca, cb);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t r[16];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) unpack_f16(q[4 * h + e], __byte_perm(h ? cb : ca, 0u, (e & 2) ? 0x3232 : 0x1010), r + 4 * e);
-        tmem_st_32x32b_x16(dst + 16 * h, r);
-      }
-      if (p.bulk) {
-        // only now have the loads' values been used: an arrival does not wait for loads still under way
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&packed_empty[ps]);
-        ps += 2;
-        if (ps >= kPackedStages) ps -= kPackedStages, parity_p ^= 1u;
-      }
-      tmem_st_wait();
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&full[s]);
-      kb += 2;
-      if (kb >= kbs) {
-        while (kb >= kbs) kb -= kbs, ++i;
-        if (!p.bulk && i < ntiles) row = row_of(i);
+        if (p.path != kDirect && go) {
+          // only now have the loads' values been used: an arrival does not wait for loads still under way (one right behind
+          // them had TMA overwrite rows that were being read)
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&packed_empty[stage]);
+          if (++stage == kPackedStages) stage = 0, parity_p ^= 1u;
+        }
+        // the tile before, once this one's first blocks are there for the MMAs
+        if (T::kHelp && quad == 0 && i > 0) finish(i - 1, 1 + group, turn);
       }
     }
-    copies_wait<0>();
-    if (!go && lane == 0) atomicOr(failed, 1u);
-  } else if (warp == kWeightsWarp && p.bulk) {
+    if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + group, turn);
+    if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
+  } else if (p.path == kBulk && warp == kWeightsWarp0) {
     // the packed weights; an expert's other chunks read them again, from L2
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
@@ -543,24 +558,70 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_kernel(const __grid_constant
     bool go = true;
     for (int i = 0; i < ntiles && go; ++i) {
       const int t = first + i * step;
-      const int row = (int)((int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + (int64_t)(t % p.tiles_o) * p.tile_rows);
-      for (int kb = 0; kb < kbs; ++kb) {
+      const int row_a = (int)((int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + (int64_t)(t % p.tiles_o) * p.tile_rows);
+      const int row_b = row_a + (kMode == kModeDown ? kBM : 0);
+      for (int quad = 0; quad < quads; ++quad) {
         if (!mbar_wait_warp(&packed_empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
           go = false;
           break;
         }
         if (elect_one()) {
-          mbar_arrive_expect_tx(&packed_full[s], kPackedBytes);
-          tma_load_2d(packed + s * kPackedBytes, &amap, kb * (kBK / 2), row, &packed_full[s], policy);
-          tma_load_2d(packed + s * kPackedBytes + kHalfBytes, &bmap, kb * (kBK / 2), row + (kMode == kModeDown ? kBM : 0),
-                      &packed_full[s], policy);
+          uint8_t *to = packed + s * (kHalves * kHalfBytes), *codes_to = packed_codes + s * (kHalves * kHalfCodes);
+          mbar_arrive_expect_tx(&packed_full[s], kHalves * (kHalfBytes + kBM * 16));
+          tma_load_2d(to, &amap, quad * (int)kRowBytes, row_a, &packed_full[s], policy);
+          tma_load_2d(codes_to, &acodes, quad * 16, row_a, &packed_full[s], policy);
+          tma_load_2d(to + kHalfBytes, &bmap, quad * (int)kRowBytes, row_b, &packed_full[s], policy);
+          tma_load_2d(codes_to + kHalfCodes, &bcodes, quad * 16, row_b, &packed_full[s], policy);
         }
         __syncwarp();
         if (++s == kPackedStages) s = 0, parity ^= 1u;
       }
     }
     ring_drain(packed_full, kPackedStages, s, parity);
+  } else if (p.path == kCopies) {
+    // one half a warp: 16 lanes a row of 128 bytes, then four (five, with the word that the last codes end in) a row's codes
+    const int half = warp - kWeightsWarp0;
+    const ExpertMatrix& w = half ? p.b : p.a;
+    const int64_t half_cols = p.cols >> 1, code_cols = p.cols >> 4, code_end = p.all_rows * code_cols;
+    uint32_t s = 0, parity = 1;
+    bool go = true;
+    for (int i = 0; i < ntiles && go; ++i) {
+      const int t = first + i * step;
+      const int64_t row0 = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + (int64_t)(t % p.tiles_o) * p.tile_rows +
+                           (kMode == kModeDown && half ? kBM : 0);
+      for (int quad = 0; quad < quads; ++quad) {
+        if (!mbar_wait_warp(&packed_empty[s], parity)) {
+          if (lane == 0) atomicOr(failed, 1u);
+          go = false;
+          break;
+        }
+        const uint32_t to = smem_addr(packed + s * (kHalves * kHalfBytes) + half * kHalfBytes);
+        const uint32_t codes_to = smem_addr(packed_codes + s * (kHalves * kHalfCodes) + half * kHalfCodes);
+        const int64_t at = (int64_t)quad * kRowBytes + (lane & 15) * 8;
+        const uint32_t bytes = at < half_cols ? 8u : 0u;
+        int64_t row = row0 + (lane >> 4);
+        const uint8_t* src = w.packed + row * half_cols + at;
+#pragma unroll 8
+        for (int r = 0; r < kBM; r += 2, row += 2, src += 2 * half_cols) {
+          const uint32_t in_half = (uint32_t)(r + (lane >> 4));
+          const bool on = bytes && row < p.all_rows;
+          copy_8_async(to + in_half * kRowBytes + ((((uint32_t)(lane & 15) >> 1) ^ (in_half & 7u)) << 4) + (lane & 1) * 8, on ? src : w.packed,
+                       on ? 8u : 0u);
+        }
+        for (int r = lane; r < kBM; r += 32) {
+          const int64_t word = ((row0 + r) * code_cols + (int64_t)quad * 16) & ~(int64_t)3;
+#pragma unroll
+          for (int e = 0; e < 5; ++e) {
+            const int64_t left = code_end - (word + 4 * e);
+            copy_4_async(codes_to + r * kCodeRow + 4 * e, left > 0 ? w.codes + word + 4 * e : w.codes, left <= 0 ? 0u : left < 4 ? (uint32_t)left : 4u);
+          }
+        }
+        copies_arrive(&packed_full[s]);
+        if (++s == kPackedStages) s = 0, parity ^= 1u;
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -586,39 +647,45 @@ cudaError_t slots_map(CUtensorMap* map, const void* v, int64_t cols, int64_t row
              : cudaErrorInvalidValue;
 }
 
-// Packed bytes [rows, bytes] in boxes of 32 x 128.
-cudaError_t packed_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t rows) {
+// Bytes [rows, bytes] in boxes of `width` x 128.
+cudaError_t bytes_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t rows, uint32_t width) {
   EncodeTiledFn encode = nullptr;
   const cudaError_t err = encode_tiled_fn(&encode);
   if (err != cudaSuccess) return err;
   const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)bytes};
-  const cuuint32_t box[2] = {(cuuint32_t)kBK / 2, (cuuint32_t)kBM};
+  const cuuint32_t box[2] = {width, (cuuint32_t)kBM};
   const cuuint32_t estr[2] = {1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(v), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+                width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? cudaSuccess
              : cudaErrorInvalidValue;
 }
 
 template <int kMode, int kN>
 cudaError_t launch_gemm_n(const void* v, int64_t slots, int64_t experts, GemmArgs p, int64_t most_tiles, int sms, cudaStream_t stream) {
-  CUtensorMap map, amap, bmap;
+  CUtensorMap map;
   cudaError_t err = slots_map(&map, v, p.cols, slots, kN);
   if (err != cudaSuccess) return err;
   const auto at = [](const void* q, uintptr_t a) { return reinterpret_cast<uintptr_t>(q) % a == 0; };
-  p.bulk = p.cols % kBK == 0 && at(p.a.packed, 16) && at(p.b.packed, 16) && at(p.a.codes, 4) && at(p.b.codes, 4) &&
-           experts * p.rows + 2 * kBM <= INT32_MAX;
-  amap = bmap = map;
-  if (p.bulk) {
-    if ((err = packed_map(&amap, p.a.packed, p.cols / 2, experts * p.rows)) != cudaSuccess) return err;
-    if ((err = packed_map(&bmap, p.b.packed, p.cols / 2, experts * p.rows)) != cudaSuccess) return err;
+  p.all_rows = experts * p.rows;
+  // TMA wants rows of whole 16 bytes, codes too, and rows that an int counts
+  const bool bulk = p.cols % 256 == 0 && at(p.a.packed, 16) && at(p.b.packed, 16) && at(p.a.codes, 16) && at(p.b.codes, 16) &&
+                    p.all_rows + 2 * kBM <= INT32_MAX;
+  p.path = bulk ? kBulk : at(p.a.codes, 4) && at(p.b.codes, 4) ? kCopies : kDirect;
+  CUtensorMap maps[4] = {map, map, map, map};
+  if (bulk) {
+    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, 128)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, 128)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[3], p.b.codes, p.cols / 16, p.all_rows, 16)) != cudaSuccess) return err;
   }
   auto kernel = gemm_kernel<kMode, kN>;
   err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)Tile<kN>::kSmemBytes);
   if (err != cudaSuccess) return err;
-  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map, amap,
-                        bmap, p);
+  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map,
+                        maps[0], maps[1], maps[2], maps[3], p);
 }
 template <int kMode>
 cudaError_t launch_gemm(int width, const void* v, int64_t slots, int64_t experts, GemmArgs p, int64_t chunks, int sms,
@@ -629,6 +696,7 @@ cudaError_t launch_gemm(int width, const void* v, int64_t slots, int64_t experts
   const int64_t tiles = chunks * p.tiles_o;
   if (tiles * p.kb_total > INT32_MAX) return cudaErrorInvalidValue;
   switch (width) {
+    case 16: return launch_gemm_n<kMode, 16>(v, slots, experts, p, tiles, sms, stream);
     case 32: return launch_gemm_n<kMode, 32>(v, slots, experts, p, tiles, sms, stream);
     case 64: return launch_gemm_n<kMode, 64>(v, slots, experts, p, tiles, sms, stream);
     default: return launch_gemm_n<kMode, 128>(v, slots, experts, p, tiles, sms, stream);
@@ -642,11 +710,11 @@ inline int64_t round256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // Slots a tile: as many as an expert has on average, so that a tile's weights serve them all.
 int experts_width(int64_t slots, int64_t experts) {
   const int64_t each = (slots + experts - 1) / experts;
-  return each <= 24 ? 32 : each <= 56 ? 64 : 128;
+  return each <= 10 ? 16 : each <= 24 ? 32 : each <= 56 ? 64 : 128;
 }
 
 int64_t experts_plan_bytes(int64_t slots, int64_t experts) {
-  return 256 + round256(plan_chunks(slots, experts, 32) * (int64_t)sizeof(Chunk)) + 2 * round256(slots * 4);
+  return 256 + round256(plan_chunks(slots, experts, 16) * (int64_t)sizeof(Chunk)) + 2 * round256(slots * 4);
 }
 
 Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts) {
@@ -654,7 +722,7 @@ Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts) {
   Plan plan;
   plan.header = reinterpret_cast<int32_t*>(p);
   plan.chunks = reinterpret_cast<Chunk*>(p + 256);
-  p += 256 + round256(plan_chunks(slots, experts, 32) * (int64_t)sizeof(Chunk));
+  p += 256 + round256(plan_chunks(slots, experts, 16) * (int64_t)sizeof(Chunk));
   plan.slot_of = reinterpret_cast<int32_t*>(p);
   plan.pos_of = reinterpret_cast<int32_t*>(p + round256(slots * 4));
   return plan;

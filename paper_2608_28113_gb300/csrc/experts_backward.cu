@@ -433,7 +433,7 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   cudaError_t err = current_device_info(&info);
   if (err != cudaSuccess) return err;
   const int64_t slots = r.tokens * r.k;
-  const int width = experts_width(slots, w.count);
+  const int width = std::max(32, experts_width(slots, w.count));
   const Plan plan = experts_plan_at(workspace, slots, w.count);
   uint32_t* amax = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + experts_plan_bytes(slots, w.count));
   uint32_t* dy_amax = amax + round256(slots * 4) / 4;
