@@ -38,11 +38,12 @@ constexpr int kPlanAhead = 8;  // ids a lane has in flight: one at a time, 32768
 
 // A stable counting sort by one CTA: each warp counts a run of slots, the warps' counts are summed up expert by
 // expert, and each warp then places its run.  Integers only: equal calls give equal plans.
+// wide: chunks of another width over the same positions (its chunks and their number alone; nullptr: none).
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __restrict__ ids, int64_t slots, int experts, int width,
-                                                            Plan plan) {
+                                                            Plan plan, int wide_width, Plan wide) {
   extern __shared__ int32_t counts[];  // [kPlanWarps][experts], then each expert's first position
   int32_t* first = counts + kPlanWarps * experts;
-  __shared__ int32_t warp_total[kPlanWarps], warp_chunks[kPlanWarps];
+  __shared__ int32_t warp_total[kPlanWarps], warp_chunks[kPlanWarps], warp_wide[kPlanWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t run = (slots + kPlanWarps - 1) / kPlanWarps, s0 = warp * run, s1 = min(slots, s0 + run);
   for (int i = threadIdx.x; i < kPlanWarps * experts; i += kPlanThreads) counts[i] = 0;
@@ -69,26 +70,33 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
       total += c;
     }
   }
-  const int pieces = (total + width - 1) / width;
-  int at = total, chunk = pieces;
+  const int pieces = (total + width - 1) / width, wide_pieces = (total + wide_width - 1) / wide_width;
+  int at = total, chunk = pieces, wide_chunk = wide_pieces;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int a = __shfl_up_sync(0xFFFFFFFFu, at, d), b = __shfl_up_sync(0xFFFFFFFFu, chunk, d);
-    if (lane >= d) at += a, chunk += b;
+    const int a = __shfl_up_sync(0xFFFFFFFFu, at, d), b = __shfl_up_sync(0xFFFFFFFFu, chunk, d), c = __shfl_up_sync(0xFFFFFFFFu, wide_chunk, d);
+    if (lane >= d) at += a, chunk += b, wide_chunk += c;
   }
-  if (lane == 31) warp_total[warp] = at, warp_chunks[warp] = chunk;
+  if (lane == 31) warp_total[warp] = at, warp_chunks[warp] = chunk, warp_wide[warp] = wide_chunk;
   __syncthreads();
-  for (int w = 0; w < warp; ++w) at += warp_total[w], chunk += warp_chunks[w];
-  if (threadIdx.x == kPlanThreads - 1) plan.header[0] = chunk, plan.header[1] = at;
-  at -= total, chunk -= pieces;
+  for (int w = 0; w < warp; ++w) at += warp_total[w], chunk += warp_chunks[w], wide_chunk += warp_wide[w];
+  if (threadIdx.x == kPlanThreads - 1) {
+    plan.header[0] = chunk, plan.header[1] = at;
+    if (wide.header != nullptr) wide.header[0] = wide_chunk;
+  }
+  at -= total, chunk -= pieces, wide_chunk -= wide_pieces;
   if ((int)threadIdx.x < experts) {
     first[threadIdx.x] = at;
     // chunks of nearly the same size, whole 16s
-    const int each = pieces ? ((total + pieces - 1) / pieces + 15) / 16 * 16 : 0;
-    for (int c = 0; c < pieces; ++c) {
-      const int from = min(total, c * each), to = min(total, from + each);
-      plan.chunks[chunk + c] = {(int32_t)threadIdx.x, at + from, to - from, 0};
-    }
+    const auto cut = [&](int n, Chunk* to) {
+      const int each = n ? ((total + n - 1) / n + 15) / 16 * 16 : 0;
+      for (int c = 0; c < n; ++c) {
+        const int from = min(total, c * each), end = min(total, from + each);
+        to[c] = {(int32_t)threadIdx.x, at + from, end - from, 0};
+      }
+    };
+    cut(pieces, plan.chunks + chunk);
+    if (wide.header != nullptr) cut(wide_pieces, wide.chunks + wide_chunk);
   }
   __syncthreads();
   for (int64_t s = s0; s < s1; s += 32 * kPlanAhead) {
@@ -224,18 +232,6 @@ struct GemmArgs {
   uint32_t* h_amax;      // of each position's h
   void* out;
 };
-
-// Asynchronous copies of 4 or 8 bytes, of which `bytes` are read and the rest zeros.
-__device__ __forceinline__ void copy_4_async(uint32_t dst, const void* src, uint32_t bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copy_8_async(uint32_t dst, const void* src, uint32_t bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-// Arrives, as one of the barrier's count, once this thread's copies so far have landed.
-__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
 
 // D[tmem] (+)= A[tmem] * B[smem]^T: A's row in its lane, two elements of K a column.
 __device__ __forceinline__ void umma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -617,7 +613,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
             copy_4_async(codes_to + r * kCodeRow + 4 * e, left > 0 ? w.codes + word + 4 * e : w.codes, left <= 0 ? 0u : left < 4 ? (uint32_t)left : 4u);
           }
         }
-        copies_arrive(&packed_full[s]);
+        copies_arrive(smem_addr(&packed_full[s]));
         if (++s == kPackedStages) s = 0, parity ^= 1u;
       }
     }
@@ -647,22 +643,6 @@ cudaError_t slots_map(CUtensorMap* map, const void* v, int64_t cols, int64_t row
              : cudaErrorInvalidValue;
 }
 
-// Bytes [rows, bytes] in boxes of `width` x 128.
-cudaError_t bytes_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t rows, uint32_t width) {
-  EncodeTiledFn encode = nullptr;
-  const cudaError_t err = encode_tiled_fn(&encode);
-  if (err != cudaSuccess) return err;
-  const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)bytes};
-  const cuuint32_t box[2] = {width, (cuuint32_t)kBM};
-  const cuuint32_t estr[2] = {1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(v), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
-             ? cudaSuccess
-             : cudaErrorInvalidValue;
-}
-
 template <int kMode, int kN>
 cudaError_t launch_gemm_n(const void* v, int64_t slots, int64_t experts, GemmArgs p, int64_t most_tiles, int sms, cudaStream_t stream) {
   CUtensorMap map;
@@ -676,10 +656,10 @@ cudaError_t launch_gemm_n(const void* v, int64_t slots, int64_t experts, GemmArg
   p.path = bulk ? kBulk : at(p.a.codes, 4) && at(p.b.codes, 4) ? kCopies : kDirect;
   CUtensorMap maps[4] = {map, map, map, map};
   if (bulk) {
-    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, 128)) != cudaSuccess) return err;
-    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, 128)) != cudaSuccess) return err;
-    if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16)) != cudaSuccess) return err;
-    if ((err = bytes_map(&maps[3], p.b.codes, p.cols / 16, p.all_rows, 16)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, 128, kBM)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, 128, kBM)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16, kBM)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[3], p.b.codes, p.cols / 16, p.all_rows, 16, kBM)) != cudaSuccess) return err;
   }
   auto kernel = gemm_kernel<kMode, kN>;
   err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)Tile<kN>::kSmemBytes);
@@ -707,6 +687,22 @@ inline int64_t round256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 }  // namespace
 
+// Bytes [rows, bytes] in boxes of `width` x `height`.
+cudaError_t bytes_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t rows, uint32_t width, uint32_t height) {
+  EncodeTiledFn encode = nullptr;
+  const cudaError_t err = encode_tiled_fn(&encode);
+  if (err != cudaSuccess) return err;
+  const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)bytes};
+  const cuuint32_t box[2] = {width, height};
+  const cuuint32_t estr[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(v), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+
 // Slots a tile: as many as an expert has on average, so that a tile's weights serve them all.
 int experts_width(int64_t slots, int64_t experts) {
   const int64_t each = (slots + experts - 1) / experts;
@@ -714,7 +710,7 @@ int experts_width(int64_t slots, int64_t experts) {
 }
 
 int64_t experts_plan_bytes(int64_t slots, int64_t experts) {
-  return 256 + round256(plan_chunks(slots, experts, 16) * (int64_t)sizeof(Chunk)) + 2 * round256(slots * 4);
+  return 256 + 2 * round256(plan_chunks(slots, experts, 16) * (int64_t)sizeof(Chunk)) + 2 * round256(slots * 4);
 }
 
 Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts) {
@@ -722,18 +718,28 @@ Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts) {
   Plan plan;
   plan.header = reinterpret_cast<int32_t*>(p);
   plan.chunks = reinterpret_cast<Chunk*>(p + 256);
-  p += 256 + round256(plan_chunks(slots, experts, 16) * (int64_t)sizeof(Chunk));
+  p += 256 + 2 * round256(plan_chunks(slots, experts, 16) * (int64_t)sizeof(Chunk));
   plan.slot_of = reinterpret_cast<int32_t*>(p);
   plan.pos_of = reinterpret_cast<int32_t*>(p + round256(slots * 4));
   return plan;
 }
 
-cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, const Plan& plan, cudaStream_t stream) {
+Plan experts_wide_plan(const Plan& plan, int64_t slots, int64_t experts) {
+  Plan wide = plan;
+  wide.header = plan.header + 2;
+  wide.chunks = reinterpret_cast<Chunk*>(reinterpret_cast<uint8_t*>(plan.chunks) +
+                                         round256(plan_chunks(slots, experts, 16) * (int64_t)sizeof(Chunk)));
+  return wide;
+}
+
+cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, const Plan& plan, int wide_width, const Plan* wide,
+                                cudaStream_t stream) {
   const int smem = (int)((kPlanWarps + 1) * experts * 4);
   // set once, for every call's size
   const cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void*>(plan_kernel), (kPlanWarps + 1) * (int)kRouteExperts * 4);
   if (err != cudaSuccess) return err;
-  plan_kernel<<<1, kPlanThreads, smem, stream>>>(r.ids, r.tokens * r.k, (int)experts, width, plan);
+  plan_kernel<<<1, kPlanThreads, smem, stream>>>(r.ids, r.tokens * r.k, (int)experts, width, plan, wide_width,
+                                                    wide != nullptr ? *wide : Plan{});
   return cudaGetLastError();
 }
 
@@ -781,7 +787,7 @@ cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const 
   uint8_t* h = xs + round256(slots * w.n * 2);
   float* part = reinterpret_cast<float*>(h + round256(slots * w.inner * 2));
   const int64_t chunks = plan_chunks(slots, w.count, width);
-  if ((err = launch_experts_plan(r, w.count, width, plan, stream)) != cudaSuccess) return err;
+  if ((err = launch_experts_plan(r, w.count, width, plan, width, nullptr, stream)) != cudaSuccess) return err;
   if ((err = launch_experts_spread(x, ld_x, w.n, r, plan, xs, amax, h_amax, stream)) != cudaSuccess) return err;
   GemmArgs p = {};
   p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan;

@@ -55,14 +55,27 @@ __device__ __forceinline__ float activate_fast(int kind, float g) {
   const float q = kind == kActSilu ? g : 1.5957691216057308f * fmaf(0.044715f * g * g, g, g);
   return __fdividef(g, 1.0f + __expf(-q));
 }
-// act(g) and its derivative, in fp32 throughout.
+// act(g) and its derivative in fp32: the exponential of a number that is not positive and the quotient are off by a few
+// 2^-23 (of 1, the derivative; of max(1, |g|), the activation).
 __device__ __forceinline__ float2 activate(int kind, float g) {
   const float q = kind == kActSilu ? g : 1.5957691216057308f * fmaf(0.044715f * g * g, g, g);
   const float dq = kind == kActSilu ? 1.0f : 1.5957691216057308f * fmaf(0.134145f * g, g, 1.0f);
-  const float e = expf(-fabsf(q)), part = 1.0f / (1.0f + e), other = e * part;
+  const float e = __expf(-fabsf(q)), part = __fdividef(1.0f, 1.0f + e), other = e * part;
   const float s = q >= 0.0f ? part : other, rest = q >= 0.0f ? other : part;
-  const float slope = rest > 0.0f ? g * dq * s * rest : 0.0f;  // rest or s may be 0 where dq is infinite
-  return make_float2(g * s, s > 0.0f ? s + slope : 0.0f);
+  const float slope = other > 0.0f ? g * dq * s * rest : 0.0f;  // other may be 0 where dq is infinite
+  return make_float2(g * s, s + slope);
+}
+
+// Asynchronous copies of 4 or 8 bytes, of which `bytes` are read and the rest zeros.
+__device__ __forceinline__ void copy_4_async(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_8_async(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// Arrives, as one of the barrier's count, once this thread's copies so far have landed.
+__device__ __forceinline__ void copies_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
 // Weights as fp16: E2M1 times E4M3 has at most 6 significant bits, from 2^-10 to 2688, so a weight without its global

@@ -7,9 +7,12 @@
 //
 // The transposed products.  Tile: 256 outputs (columns of the weights) as two halves of 128 x up to kN slots, K in blocks
 // of 64 rows.  The packed rows, unpacked as they are stored, make the weights' tile MN-major in shared memory
-// (tensor memory would take it K-major only).  18 warps, as in the forward pass: TMA loads of the slots' tile, MMAs,
-// epilogue, and three groups of four that unpack the halves' blocks in turn: a thread has 64 outputs of a row of K.
-// Bound by shared memory, which carries both operands: at 128 slots some 875 cycles a K block against 512 of MMAs.
+// (tensor memory would take it K-major only).  24 warps, as in the forward pass: TMA loads of the slots' tile, MMAs,
+// four of the epilogue, two groups of eight that unpack every other K block (a thread: 64 outputs of a row of
+// K), and two that fetch the packed blocks.
+// Bound by shared memory, which carries both operands, the packed blocks and the unpacking: of 128 bytes a
+// cycle, a K block takes some 1010 cycles at 128 slots against 512 of MMAs, and 1416 at 256 against 1024; so an expert
+// with enough slots takes 256 a tile, and the unpacking warps then take part in its epilogue.
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>
@@ -26,26 +29,37 @@ namespace {
 __device__ uint32_t g_experts_backward_flags = 0;
 
 constexpr int kBM = 128, kBK = 64, kHalves = 2;
-constexpr int kThreads = 576;
-constexpr int kUnpackWarp0 = 6, kUnpackGroups = 3;
-constexpr int kAhead = 2;  // blocks of its own that a group has in flight
+constexpr int kEpilogueWarp0 = 2, kUnpackWarp0 = 6, kUnpackWarps = 16, kWeightsWarp0 = 22;
+constexpr int kThreads = 768;
 constexpr int kModeHidden = 0, kModeInput = 1;
 constexpr uint32_t kGroupBytes = 64 * kBK * 2;  // 64 outputs x 64 rows of K
 constexpr uint32_t kHalfBytes = 2 * kGroupBytes;
-constexpr uint32_t kTurnBytes = 4 * 2048;
+// A packed block: 64 rows of K, 128 bytes (256 outputs) each, and 16 bytes of their codes (20 where they are copied
+// as whole words from any address).
+constexpr uint32_t kRowBytes = kHalves * kBM / 2, kCodeRow = 20;
+constexpr uint32_t kPackedBytes = kBK * kRowBytes, kCodeBytes = kBK * kCodeRow;
+constexpr int kDirect = 0, kCopies = 1, kBulk = 2;  // how the packed weights come (experts.cu)
 
 template <int kN>
 struct Tile {
-  static constexpr int kStages = kN == 128 ? 4 : 5;
+  static constexpr int kStages = kN == 256 ? 2 : kN == 128 ? 3 : 4;
+  static constexpr int kPackedStages = 6;
+  static constexpr int kAccs = kN == 256 ? 1 : 2;
+  static constexpr bool kHelp = kAccs == 1;  // the unpacking warps take part in the epilogue
+  static constexpr int kEpilogueWarps = kHelp ? 4 + kUnpackWarps : 4;
   static constexpr uint32_t kABytes = kHalves * kHalfBytes, kBBytes = kN * kBK * 2;
-  static constexpr uint32_t kSmemBytes = kStages * (kABytes + kBBytes) + 1024 /* alignment */ + 256 /* barriers */ + kTurnBytes;
-  static constexpr uint32_t kAcc = kHalves * kN, kTmemCols = 2 * kAcc;
+  static constexpr uint32_t kTurnBytes = kEpilogueWarps * 512;
+  static constexpr uint32_t kSmemBytes = kStages * (kABytes + kBBytes) + kPackedStages * (kPackedBytes + kCodeBytes) + 1024 /* alignment */ +
+                                         512 /* barriers */ + kTurnBytes;
+  static constexpr uint32_t kAcc = kHalves * kN, kTmemCols = kAccs * kAcc;
+  static_assert(kSmemBytes <= 232448, "shared memory");
 };
 
 struct BackArgs {
   ExpertMatrix a, b;    // the weights of the first and the second half of K (down twice where there is one)
   int64_t rows, cols;   // of an expert's matrix: K and the outputs
-  int32_t kb_part, parts, tiles_o;
+  int32_t kb_part, parts, tiles_o, path;
+  int64_t all_rows;  // of all experts
   int32_t activation;
   Plan plan;
   const float* weights;
@@ -68,10 +82,10 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t (&r
   r[3] = mul_bf16x2((b & kSign) | ((b >> 6) & kMag), scale);
 }
 
-// 16 columns' sums over a warp's lanes: lane l, even, has that of column_of(l).
-__device__ __forceinline__ float sum_columns(float (&v)[16], int lane) {
+// Eight columns' sums over a warp's lanes: every lane has that of column_of(lane).
+__device__ __forceinline__ float sum_columns(float (&v)[8], int lane) {
 #pragma unroll
-  for (int n = 8, d = 16; n > 0; n >>= 1, d >>= 1) {
+  for (int n = 4, d = 16; n > 0; n >>= 1, d >>= 1) {
     const bool upper = (lane & d) != 0;
 #pragma unroll
     for (int j = 0; j < n; ++j) {
@@ -79,62 +93,77 @@ __device__ __forceinline__ float sum_columns(float (&v)[16], int lane) {
       v[j] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, d);
     }
   }
+  v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], 2);
   return v[0] + __shfl_xor_sync(0xFFFFFFFFu, v[0], 1);
 }
-__device__ __forceinline__ int column_of(int lane) { return (lane >> 1 & 8) | (lane >> 1 & 4) | (lane >> 1 & 2) | (lane >> 1 & 1); }
+__device__ __forceinline__ int column_of(int lane) { return lane >> 2; }
 
-// 16 slots of 32 outputs (a slot's in neighbouring lanes) rounded and stored, 8 outputs a lane.
-__device__ __forceinline__ void store_rows(const float (&v)[16], uint32_t* turn, __nv_bfloat16* out, int64_t stride, int64_t at0,
+// Eight slots of 32 outputs (a slot's in neighbouring lanes) rounded and stored, 8 outputs of a slot a lane.
+__device__ __forceinline__ void store_rows(const float (&v)[8], uint32_t* turn, __nv_bfloat16* out, int64_t stride, int64_t at0,
                                            int64_t cols, int left, int lane) {
   __syncwarp();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) turn[j * 32 + lane] = pack_bf16(v[2 * j], v[2 * j + 1]);
+  for (int j = 0; j < 4; ++j) turn[j * 32 + lane] = pack_bf16(v[2 * j], v[2 * j + 1]);
   __syncwarp();
-  const int pair = lane >> 2;
-  const uint4 q0 = reinterpret_cast<const uint4*>(turn)[2 * lane], q1 = reinterpret_cast<const uint4*>(turn)[2 * lane + 1];
+  const int odd = lane >> 4, j = 2 * ((lane >> 2) & 3) + odd;
+  const uint4 q0 = reinterpret_cast<const uint4*>(turn)[2 * (lane & 15)], q1 = reinterpret_cast<const uint4*>(turn)[2 * (lane & 15) + 1];
+  const uint32_t pick = odd ? 0x7632u : 0x5410u;
+  const uint4 r = make_uint4(__byte_perm(q0.x, q0.y, pick), __byte_perm(q0.z, q0.w, pick), __byte_perm(q1.x, q1.y, pick),
+                             __byte_perm(q1.z, q1.w, pick));
   const int64_t at = at0 + (lane & 3) * 8;
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const uint32_t pick = e ? 0x7632u : 0x5410u;
-    const uint4 r = make_uint4(__byte_perm(q0.x, q0.y, pick), __byte_perm(q0.z, q0.w, pick), __byte_perm(q1.x, q1.y, pick),
-                               __byte_perm(q1.z, q1.w, pick));
-    // cols is a multiple of 16: 8 outputs are all there or none is
-    if (2 * pair + e < left && at < cols) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(out) + (2 * pair + e) * stride + at) = r;
-  }
+  // cols is a multiple of 16: 8 outputs are all there or none is
+  if (j < left && at < cols) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(out) + j * stride + at) = r;
+}
+
+__device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
 }
 
 template <int kMode, int kN>
-__global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ BackArgs p) {
+__global__ void __launch_bounds__(kThreads, 1)
+back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
+            const __grid_constant__ CUtensorMap acodes, const __grid_constant__ CUtensorMap bcodes, const __grid_constant__ BackArgs p) {
   using T = Tile<kN>;
-  constexpr int kStages = T::kStages;
+  constexpr int kStages = T::kStages, kPackedStages = T::kPackedStages, kAccs = T::kAccs;
   extern __shared__ __align__(16) uint8_t dynamic_smem[];
   uint8_t* smem = dynamic_smem + ((1024u - (smem_addr(dynamic_smem) & 1023u)) & 1023u);
   uint8_t* tile_a = smem;
   uint8_t* tile_b = smem + kStages * T::kABytes;
-  uint8_t* rest = tile_b + kStages * T::kBBytes;
+  uint8_t* packed = tile_b + kStages * T::kBBytes;
+  uint8_t* packed_codes = packed + kPackedStages * kPackedBytes;
+  uint8_t* rest = packed_codes + kPackedStages * kCodeBytes;
   uint64_t* full = reinterpret_cast<uint64_t*>(rest);
   uint64_t* empty = full + kStages;
   uint64_t* acc_full = empty + kStages;
-  uint64_t* acc_empty = acc_full + 2;
-  uint64_t* mma_done = acc_empty + 2;
+  uint64_t* acc_empty = acc_full + kAccs;
+  uint64_t* packed_full = acc_empty + kAccs;
+  uint64_t* packed_empty = packed_full + kPackedStages;
+  uint64_t* mma_done = packed_empty + kPackedStages;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
   uint32_t* failed = tmem_slot + 1;
-  uint32_t* turn = reinterpret_cast<uint32_t*>(rest + 256) + (threadIdx.x >> 5 & 3) * (kTurnBytes / 16);
 
   const int warp = (int)warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&full[s], 1 + kHalves * 4);  // the TMA load and the warps of the halves' groups
+      mbar_init(&full[s], 1 + kUnpackWarps / 2);  // the TMA load and the warps of a group
       mbar_init(&empty[s], 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int s = 0; s < kPackedStages; ++s) {
+      mbar_init(&packed_full[s], p.path == kCopies ? 2 * 32 : 1);
+      mbar_init(&packed_empty[s], kUnpackWarps / 2);
+    }
+    for (int i = 0; i < kAccs; ++i) {
       mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], 128);
+      mbar_init(&acc_empty[i], T::kEpilogueWarps);
     }
     mbar_init(mma_done, 1);
     *failed = 0u;
     mbar_fence_init();
     prefetch_tensormap(&vmap);
+    if (p.path == kBulk) prefetch_tensormap(&amap), prefetch_tensormap(&bmap), prefetch_tensormap(&acodes), prefetch_tensormap(&bcodes);
   }
   if (warp == 1) {
     tmem_alloc(smem_addr(tmem_slot), T::kTmemCols);
@@ -150,6 +179,83 @@ __global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant
   const int ntiles = tiles > first ? (tiles - first + step - 1) / step : 0;
   const int kbs = p.kb_part * p.parts;
   const uint32_t quarter = (uint32_t)(warp & 3), lane_base = (quarter * 32u) << 16;
+  bool have = true;  // of the warps of the epilogue: no wait for an accumulator has run out
+
+  // The epilogue of the CTA's tile i: eight slots of a half a time, those of this warp.
+  const auto finish = [&](int i, int who, uint32_t* turn) {
+    constexpr int kWorkers = T::kEpilogueWarps / 4;
+    const int t = first + i * step, to = t % p.tiles_o;
+    const Chunk c = p.plan.chunks[t / p.tiles_o];
+    const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc + lane_base;
+    const float scale = kMode == kModeHidden ? p.a.scale[c.expert] : kWeightUnit;
+    const float sg = kMode == kModeHidden ? p.gate_scale[c.expert] : 0.0f, su = kMode == kModeHidden ? p.up_scale[c.expert] : 0.0f;
+    const float nan = __int_as_float(0x7FC00000);
+    const int each = (c.count + 7) / 8, pieces = kHalves * each;
+    float g[8], u[8];
+    const auto fetch = [&](int piece) {
+      if (kMode != kModeHidden || piece >= pieces) return;
+      const int half = piece >= each ? 1 : 0, j0 = (piece - half * each) * 8;
+      const int64_t o = (int64_t)to * (kHalves * kBM) + half * kBM + quarter * 32 + lane;
+      const float* raw = p.raw + (int64_t)(c.first + j0) * 2 * p.cols + o;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool on = j0 + j < c.count && o < p.cols;
+        g[j] = on ? raw[0] : 0.0f;
+        u[j] = on ? raw[p.cols] : 0.0f;
+        raw += 2 * p.cols;
+      }
+    };
+    fetch(who);
+    if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i / kAccs) & 1u));
+    tc_fence_after_sync();
+#pragma unroll 1
+    for (int piece = who; piece < pieces; piece += kWorkers) {
+      const int half = piece >= each ? 1 : 0, j0 = (piece - half * each) * 8, left = min(8, c.count - j0);
+      const int64_t at0 = (int64_t)to * (kHalves * kBM) + half * kBM + quarter * 32, o = at0 + lane, pos = c.first + j0;
+      const bool on = o < p.cols;
+      uint32_t a[8];
+      tmem_ld_32x32b_x8(d + (uint32_t)(half * kN + j0), a);
+      if constexpr (kMode == kModeHidden) {
+        // lane j: slot j's weight, and the power of two of its row of dy
+        const float my_w = lane < left ? p.weights[p.plan.slot_of[pos + lane]] : 0.0f;
+        const float my_up = lane < left ? scale * exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
+        tmem_ld_wait();
+        float dot[8], dg[8], du[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float up = __shfl_sync(0xFFFFFFFFu, my_up, j), w = __shfl_sync(0xFFFFFFFFu, my_w, j);
+          const float dh = have ? __uint_as_float(a[j]) * up : nan;
+          const float2 act = activate(p.activation, g[j]);
+          dot[j] = j < left && on ? dh * (act.x * u[j]) : 0.0f;
+          dg[j] = w * dh * u[j] * act.y * sg;
+          du[j] = w * dh * act.x * su;
+        }
+        fetch(piece + kWorkers);
+        if (p.factors != nullptr) {
+          __nv_bfloat16* out = p.factors + pos * 2 * p.cols;
+          store_rows(dg, turn, out, 2 * p.cols, at0, p.cols, left, lane);
+          store_rows(du, turn, out + p.cols, 2 * p.cols, at0, p.cols, left, lane);
+        }
+        if (p.dots != nullptr) {
+          const float s = sum_columns(dot, lane);
+          const int j = column_of(lane);
+          if ((lane & 3) == 0 && j < left) p.dots[((int64_t)(to * kHalves + half) * 4 + quarter) * p.slots + pos + j] = s;
+        }
+      } else {
+        tmem_ld_wait();
+        float* out = p.part + pos * p.cols + o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (j < left && on) *out = have ? __uint_as_float(a[j]) * scale : nan;
+          out += p.cols;
+        }
+      }
+    }
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+  };
+  const auto turn_at = [&](int worker) { return reinterpret_cast<uint32_t*>(rest + 512 + worker * 512); };
 
   if (warp == 0) {
     uint64_t policy;
@@ -179,10 +285,10 @@ __global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant
     bool ok = true;
     for (int i = 0; i < ntiles && ok; ++i) {
       const Chunk c = p.plan.chunks[(first + i * step) / p.tiles_o];
-      const uint32_t idesc = warp_uniform((kMode == kModeHidden ? idesc_f16_f32(kBM, (uint32_t)((c.count + 15) & ~15))
-                                                                   : idesc_bf16_f32(kBM, (uint32_t)((c.count + 15) & ~15))) | 1u << 15);
-      const uint32_t acc = (uint32_t)i & 1u, d = tmem + acc * T::kAcc;
-      if (i >= 2 && !mbar_wait_warp(&acc_empty[acc], (uint32_t)((i >> 1) - 1) & 1u)) {
+      const uint32_t slots = (uint32_t)((c.count + 15) & ~15);
+      const uint32_t idesc = warp_uniform((kMode == kModeHidden ? idesc_f16_f32(kBM, slots) : idesc_bf16_f32(kBM, slots)) | 1u << 15);
+      const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc;
+      if (i >= kAccs && !mbar_wait_warp(&acc_empty[acc], (uint32_t)(i / kAccs - 1) & 1u)) {
         ok = false;
         break;
       }
@@ -214,151 +320,164 @@ __global__ void __launch_bounds__(kThreads, 1) back_kernel(const __grid_constant
     __syncwarp();
     umma_drain(mma_done);
   } else if (warp < kUnpackWarp0) {
-    bool have = true;
-    const float nan = __int_as_float(0x7FC00000);
-    for (int i = 0; i < ntiles; ++i) {
-      const int t = first + i * step, to = t % p.tiles_o;
-      const Chunk c = p.plan.chunks[t / p.tiles_o];
-      const uint32_t acc = (uint32_t)i & 1u, d = tmem + acc * T::kAcc + lane_base;
-      const float scale = kMode == kModeHidden ? p.a.scale[c.expert] : kWeightUnit;
-      if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i >> 1) & 1u));
-      tc_fence_after_sync();
-#pragma unroll 1
-      for (int half = 0; half < kHalves; ++half) {
-        const int64_t at0 = (int64_t)to * (kHalves * kBM) + half * kBM + quarter * 32, o = at0 + lane;
-        const bool on = o < p.cols;
-#pragma unroll 1
-        for (int j0 = 0; j0 < kN; j0 += 16) {
-          if (j0 >= c.count) break;
-          uint32_t a[16];
-          tmem_ld_32x32b_x16(d + (uint32_t)(half * kN + j0), a);
-          tmem_ld_wait();
-          if (half == kHalves - 1 && j0 + 16 >= c.count) {
-            tc_fence_before_sync();
-            mbar_arrive(&acc_empty[acc]);
-          }
-          const int left = min(16, c.count - j0);
-          const int64_t pos = c.first + j0;
-          if constexpr (kMode == kModeHidden) {
-            const int my_slot = lane < left ? p.plan.slot_of[pos + lane] : 0;
-            const float sg = p.gate_scale[c.expert], su = p.up_scale[c.expert];
-            const float my_w = lane < left ? p.weights[my_slot] : 0.0f;
-            const float my_up = lane < left ? exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
-            float dg[16], du[16];
-            const float* raw = p.raw + pos * 2 * p.cols + o;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              dg[j] = j < left && on ? raw[(int64_t)(2 * j) * p.cols] : 0.0f;
-              du[j] = j < left && on ? raw[(int64_t)(2 * j + 1) * p.cols] : 0.0f;
-            }
-            float dot[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const float dh = have ? __uint_as_float(a[j]) * (scale * __shfl_sync(0xFFFFFFFFu, my_up, j)) : nan, w = __shfl_sync(0xFFFFFFFFu, my_w, j);
-              const float2 act = activate(p.activation, dg[j]);
-              const float u = du[j];
-              dot[j] = j < left && on ? dh * (act.x * u) : 0.0f;
-              dg[j] = w * dh * u * act.y * sg;
-              du[j] = w * dh * act.x * su;
-            }
-            if (p.factors != nullptr) {
-              __nv_bfloat16* out = p.factors + pos * 2 * p.cols;
-              store_rows(dg, turn, out, 2 * p.cols, at0, p.cols, left, lane);
-              store_rows(du, turn, out + p.cols, 2 * p.cols, at0, p.cols, left, lane);
-            }
-            if (p.dots != nullptr) {
-              const float s = sum_columns(dot, lane);
-              const int j = column_of(lane);
-              if ((lane & 1) == 0 && j < left) p.dots[((int64_t)(to * kHalves + half) * 4 + quarter) * p.slots + pos + j] = s;
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              if (j < left && on) p.part[(pos + j) * p.cols + o] = have ? __uint_as_float(a[j]) * scale : nan;
-            }
-          }
-        }
-      }
-    }
+    for (int i = 0; i < ntiles; ++i) finish(i, 0, turn_at(warp - kEpilogueWarp0));
     if (!have && lane == 0) atomicOr(failed, 1u);
-  } else {
-    // a thread: 64 outputs of one row of K
-    const int tid = (int)threadIdx.x - kUnpackWarp0 * 32;
-    const int group = tid >> 7, line = tid & 127, row = line & 63;
+  } else if (warp < kWeightsWarp0) {
+    // group: every other K block; a thread: 64 outputs (`part64` of four) of one row of K
+    const int group = (warp - kUnpackWarp0) >> 3, line = ((warp - kUnpackWarp0) & 7) * 32 + lane, row = line & 63, part64 = line >> 6;
     const int64_t cols = p.cols, half_cols = cols >> 1, code_cols = cols >> 4;
-    const bool wide = (cols & 63) == 0 && ((reinterpret_cast<uintptr_t>(p.a.packed) | reinterpret_cast<uintptr_t>(p.b.packed)) & 31) == 0 &&
-                      ((reinterpret_cast<uintptr_t>(p.a.codes) | reinterpret_cast<uintptr_t>(p.b.codes)) & 3) == 0;
-    // job j: half j % 2 of K block j / 2, over the CTA's tiles; this group's are group, group + 3, ...
-    const int per_tile = kHalves * kbs;
-    const int64_t total = (int64_t)ntiles * per_tile;
-    int li = 0, lj = group;  // the next job to load
-    uint32_t ring[kAhead][8], codes[kAhead][4];
-    auto load = [&](uint32_t (&q)[8], uint32_t (&c)[4]) {
-      while (lj >= per_tile) lj -= per_tile, ++li;
-      if (li >= ntiles) return;
-      const int t = first + li * step, block = lj >> 1, part = block >= p.kb_part ? 1 : 0;
-      const int64_t e = p.plan.chunks[t / p.tiles_o].expert;
-      const int64_t o0 = (int64_t)(t % p.tiles_o) * (kHalves * kBM) + (lj & 1) * kBM + (line >> 6) * 64;
-      // rows past the end of K are read as the last one (the slots' tile is zeros there), outputs past the end as
-      // the last 64 or as zeros, and not stored
-      const int64_t f = e * p.rows + min((int64_t)(block - part * p.kb_part) * kBK + row, p.rows - 1);
-      const int64_t oin = min(o0, (cols - 1) & ~(int64_t)63);
-      const uint8_t* w = (part ? p.b.packed : p.a.packed) + f * half_cols + (oin >> 1);
-      const uint8_t* code = (part ? p.b.codes : p.a.codes) + f * code_cols + (oin >> 4);
-      if (wide) {
-        ld_32_ahead(w, q);
-        ld_4_ahead(true, code, c[0]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          c[i] = q[2 * i] = q[2 * i + 1] = 0u;
-          ld_8_ahead(o0 + 16 * i < cols, w + 8 * i, q[2 * i], q[2 * i + 1]);
-          ld_1_ahead(o0 + 16 * i < cols, code + i, c[i]);
-        }
-      }
-      lj += kUnpackGroups;
-    };
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) codes[u][i] = 0u;
-      load(ring[u], codes[u]);
-    }
+    const uint32_t swizzle = (uint32_t)row & 7u;
+    uint32_t* turn = turn_at(T::kHelp ? 4 + warp - kUnpackWarp0 : 0);
     bool go = true;
-    for (int64_t base = group; base < total && go; base += kAhead * kUnpackGroups) {
+    // blocks of all tiles, one after another: this group's are group, group + 2, ...
+    int kb = group;
+    uint32_t block = (uint32_t)group;
+    for (int i = 0; i < ntiles && go; ++i, kb -= kbs) {
+      const int t = first + i * step;
+      const int64_t e = p.plan.chunks[t / p.tiles_o].expert, o0 = (int64_t)(t % p.tiles_o) * (kHalves * kBM) + part64 * 64;
+      const int64_t row0 = e * p.rows + row;
+      // bits that a row's codes begin into a word: the same for rows 64 apart
+      const uint32_t shift = p.path == kCopies ? (uint32_t)(row0 * code_cols & 3) * 8 : 0u;
+      int done = 0;
+      for (; kb < kbs && go; kb += 2, block += 2) {
+        const uint32_t ps = block % kPackedStages, parity_p = (block / kPackedStages) & 1u;
+        uint32_t q[8], code;
+        if (p.path != kDirect) {
+          if (!mbar_wait_warp(&packed_full[ps], parity_p)) {
+            go = false;
+            break;
+          }
+          const uint32_t from = smem_addr(packed + ps * kPackedBytes + row * kRowBytes);
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int64_t job = base + u * kUnpackGroups;
-        if (job >= total || !go) break;
-        const uint32_t block = (uint32_t)(job >> 1), s = block % kStages, parity = ((block / kStages) & 1u) ^ 1u;
-        if (!mbar_wait_warp(&empty[s], parity)) {
+          for (int h = 0; h < 2; ++h)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(q[4 * h]), "=r"(q[4 * h + 1]), "=r"(q[4 * h + 2]), "=r"(q[4 * h + 3])
+                         : "r"(from + ((((uint32_t)(2 * part64 + h)) ^ swizzle) << 4)));
+          const uint32_t at = smem_addr(packed_codes + ps * kCodeBytes) + row * (p.path == kBulk ? 16u : kCodeRow) + 4 * part64;
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(code) : "r"(at));
+          if (p.path == kCopies) {
+            uint32_t more;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(more) : "r"(at + 4));
+            code = __funnelshift_r(code, more, shift);
+          }
+        } else {
+          // rows past the end of K are read as the last one (the slots' tile is zeros there), outputs past the end are zeros, and not
+          // stored
+          const int part = kb >= p.kb_part ? 1 : 0;
+          const int64_t f = e * p.rows + min((int64_t)(kb - part * p.kb_part) * kBK + row, p.rows - 1);
+          const uint8_t *wp = (part ? p.b.packed : p.a.packed) + f * half_cols + (o0 >> 1),
+                        *cp = (part ? p.b.codes : p.a.codes) + f * code_cols + (o0 >> 4);
+          uint32_t c[4];
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            c[h] = q[2 * h] = q[2 * h + 1] = 0u;
+            ld_8_ahead(o0 + 16 * h < cols, wp + 8 * h, q[2 * h], q[2 * h + 1]);
+            ld_1_ahead(o0 + 16 * h < cols, cp + h, c[h]);
+          }
+          code = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+        }
+        const uint32_t s = block % kStages;
+        if (!mbar_wait_warp(&empty[s], ((block / kStages) & 1u) ^ 1u)) {
           go = false;
           break;
         }
-        uint8_t* dst = tile_a + s * T::kABytes + (uint32_t)(job & 1) * kHalfBytes + line * 128;
-        const uint32_t code = wide ? codes[u][0] : codes[u][0] | codes[u][1] << 8 | codes[u][2] << 16 | codes[u][3] << 24;
+        uint8_t* dst = tile_a + s * T::kABytes + part64 * kGroupBytes + row * 128;
         uint32_t ca, cb;
         if constexpr (kMode == kModeHidden)
           codes_f16(code, ca, cb);
         else
           ca = unpack_codes(code & 0xFFFFu), cb = unpack_codes(code >> 16);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int h = 0; h < 8; ++h) {
           uint32_t r[4];
-          const uint32_t scale = __byte_perm(i < 4 ? ca : cb, 0u, (i & 2) ? 0x3232 : 0x1010);
+          const uint32_t scale = __byte_perm(h < 4 ? ca : cb, 0u, (h & 2) ? 0x3232 : 0x1010);
           if constexpr (kMode == kModeHidden)
-            unpack_f16(ring[u][i], scale, r);
+            unpack_f16(q[h], scale, r);
           else
-            unpack8(ring[u][i], scale, r);
-          *reinterpret_cast<uint4*>(dst + ((i ^ (row & 7)) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
+            unpack8(q[h], scale, r);
+          *reinterpret_cast<uint4*>(dst + (((uint32_t)h ^ swizzle) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&full[s]);
-        load(ring[u], codes[u]);
+        if (lane == 0) {
+          mbar_arrive(&full[s]);
+          if (p.path != kDirect) mbar_arrive(&packed_empty[ps]);  // the loads' values have been used
+        }
+        // the tile before, once this one's first blocks are there for the MMAs
+        if (T::kHelp && done++ == 0 && i > 0) finish(i - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
+      }
+      // (a tile of one K block has none of this group's)
+      if (T::kHelp && done == 0 && i > 0 && go) finish(i - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
+    }
+    if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
+    if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
+  } else if (p.path == kBulk && warp == kWeightsWarp0) {
+    uint64_t policy;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+    uint32_t s = 0, parity = 1;
+    bool go = true;
+    for (int i = 0; i < ntiles && go; ++i) {
+      const int t = first + i * step, to = t % p.tiles_o;
+      const int row0 = (int)((int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows);
+      for (int kb = 0; kb < kbs; ++kb) {
+        if (!mbar_wait_warp(&packed_empty[s], parity)) {
+          if (lane == 0) atomicOr(failed, 1u);
+          go = false;
+          break;
+        }
+        if (elect_one()) {
+          const bool second = kb >= p.kb_part;
+          const int row = row0 + (kb - (second ? p.kb_part : 0)) * kBK;
+          mbar_arrive_expect_tx(&packed_full[s], kPackedBytes + kBK * 16);
+          tma_load_2d(packed + s * kPackedBytes, second ? &bmap : &amap, to * (int)kRowBytes, row, &packed_full[s], policy);
+          tma_load_2d(packed_codes + s * kCodeBytes, second ? &bcodes : &acodes, to * 16, row, &packed_full[s], policy);
+        }
+        __syncwarp();
+        if (++s == kPackedStages) s = 0, parity ^= 1u;
       }
     }
-    if (!go && lane == 0) atomicOr(failed, 1u);
+    ring_drain(packed_full, kPackedStages, s, parity);
+  } else if (p.path == kCopies) {
+    // 32 rows of K a warp: 16 lanes a row of 128 bytes, then a lane a row's five words of codes
+    const int who = warp - kWeightsWarp0;
+    const int64_t half_cols = p.cols >> 1, code_cols = p.cols >> 4, code_end = p.all_rows * code_cols;
+    uint32_t s = 0, parity = 1;
+    bool go = true;
+    for (int i = 0; i < ntiles && go; ++i) {
+      const int t = first + i * step, to = t % p.tiles_o;
+      const int64_t row0 = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + 32 * who;
+      const int64_t at = (int64_t)to * kRowBytes + (lane & 15) * 8;
+      for (int kb = 0; kb < kbs; ++kb) {
+        if (!mbar_wait_warp(&packed_empty[s], parity)) {
+          if (lane == 0) atomicOr(failed, 1u);
+          go = false;
+          break;
+        }
+        const bool second = kb >= p.kb_part;
+        const ExpertMatrix& w = second ? p.b : p.a;
+        const int64_t row1 = row0 + (int64_t)(kb - (second ? p.kb_part : 0)) * kBK;
+        const uint32_t to_packed = smem_addr(packed + s * kPackedBytes), to_codes = smem_addr(packed_codes + s * kCodeBytes);
+        int64_t row = row1 + (lane >> 4);
+        const uint8_t* src = w.packed + row * half_cols + at;
+#pragma unroll 8
+        for (int r = 0; r < 32; r += 2, row += 2, src += 2 * half_cols) {
+          const uint32_t in = (uint32_t)(32 * who + r + (lane >> 4));
+          const bool on = at < half_cols && row < p.all_rows;
+          copy_8_async(to_packed + in * kRowBytes + ((((uint32_t)(lane & 15) >> 1) ^ (in & 7u)) << 4) + (lane & 1) * 8, on ? src : w.packed,
+                       on ? 8u : 0u);
+        }
+        const int64_t word = ((row1 + lane) * code_cols + (int64_t)to * 16) & ~(int64_t)3;
+#pragma unroll
+        for (int h = 0; h < 5; ++h) {
+          const int64_t left = code_end - (word + 4 * h);
+          copy_4_async(to_codes + (32 * who + lane) * kCodeRow + 4 * h, left > 0 ? w.codes + word + 4 * h : w.codes,
+                       left <= 0 ? 0u : left < 4 ? (uint32_t)left : 4u);
+        }
+        copies_arrive(smem_addr(&packed_full[s]));
+        if (++s == kPackedStages) s = 0, parity ^= 1u;
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -384,7 +503,8 @@ __global__ void __launch_bounds__(256) dweights_kernel(const float* dots, int pa
 }
 
 template <int kMode, int kN>
-cudaError_t launch_back_n(const void* v, int64_t depth, int parts, const BackArgs& p, int64_t most_tiles, int sms, cudaStream_t stream) {
+cudaError_t launch_back_n(const void* v, int64_t depth, int64_t experts, BackArgs p, int64_t most_tiles, int sms, cudaStream_t stream) {
+  const int parts = p.parts;
   EncodeTiledFn encode = nullptr;
   cudaError_t err = encode_tiled_fn(&encode);
   if (err != cudaSuccess) return err;
@@ -396,26 +516,47 @@ cudaError_t launch_back_n(const void* v, int64_t depth, int parts, const BackArg
   if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(v), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
+  const auto at = [](const void* q, uintptr_t a) { return reinterpret_cast<uintptr_t>(q) % a == 0; };
+  p.all_rows = experts * p.rows;
+  // TMA wants rows of whole 16 bytes, codes too, and rows that an int counts
+  const bool bulk = p.cols % 256 == 0 && at(p.a.packed, 16) && at(p.b.packed, 16) && at(p.a.codes, 16) && at(p.b.codes, 16) &&
+                    p.all_rows + 2 * kBM <= INT32_MAX;
+  p.path = bulk ? kBulk : at(p.a.codes, 4) && at(p.b.codes, 4) ? kCopies : kDirect;
+  CUtensorMap maps[4] = {map, map, map, map};
+  if (bulk) {
+    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, 128, kBK)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, 128, kBK)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16, kBK)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[3], p.b.codes, p.cols / 16, p.all_rows, 16, kBK)) != cudaSuccess) return err;
+  }
   auto kernel = back_kernel<kMode, kN>;
   err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)Tile<kN>::kSmemBytes);
   if (err != cudaSuccess) return err;
-  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map, p);
+  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map,
+                        maps[0], maps[1], maps[2], maps[3], p);
 }
 template <int kMode>
-cudaError_t launch_back(int width, const void* v, int parts, BackArgs p, int64_t chunks, int sms, cudaStream_t stream) {
+cudaError_t launch_back(int width, const void* v, int parts, int64_t experts, BackArgs p, int64_t chunks, int sms,
+                        cudaStream_t stream) {
   p.parts = parts;
   p.kb_part = (int32_t)((p.rows + kBK - 1) / kBK);
   p.tiles_o = (int32_t)((p.cols + kHalves * kBM - 1) / (kHalves * kBM));
   const int64_t tiles = chunks * p.tiles_o;
-  if (tiles > INT32_MAX) return cudaErrorInvalidValue;
+  if (tiles * p.kb_part * parts > INT32_MAX) return cudaErrorInvalidValue;
   switch (width) {
-    case 32: return launch_back_n<kMode, 32>(v, p.rows, parts, p, tiles, sms, stream);
-    case 64: return launch_back_n<kMode, 64>(v, p.rows, parts, p, tiles, sms, stream);
-    default: return launch_back_n<kMode, 128>(v, p.rows, parts, p, tiles, sms, stream);
+    case 32: return launch_back_n<kMode, 32>(v, p.rows, experts, p, tiles, sms, stream);
+    case 64: return launch_back_n<kMode, 64>(v, p.rows, experts, p, tiles, sms, stream);
+    case 128: return launch_back_n<kMode, 128>(v, p.rows, experts, p, tiles, sms, stream);
+    default: return launch_back_n<kMode, 256>(v, p.rows, experts, p, tiles, sms, stream);
   }
 }
 
 inline int64_t round256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+// Slots a tile of the transposed products.
+inline int back_width(int64_t slots, int64_t experts) {
+  const int64_t each = (slots + experts - 1) / experts;
+  return each <= 24 ? 32 : each <= 56 ? 64 : each <= 144 ? 128 : 256;
+}
 inline int64_t dot_parts(int64_t inner) { return (inner + kHalves * kBM - 1) / (kHalves * kBM) * kHalves * 4; }
 
 }  // namespace
@@ -433,7 +574,7 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   cudaError_t err = current_device_info(&info);
   if (err != cudaSuccess) return err;
   const int64_t slots = r.tokens * r.k;
-  const int width = std::max(32, experts_width(slots, w.count));
+  const int width = experts_width(slots, w.count), wide_width = back_width(slots, w.count);
   const Plan plan = experts_plan_at(workspace, slots, w.count);
   uint32_t* amax = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + experts_plan_bytes(slots, w.count));
   uint32_t* dy_amax = amax + round256(slots * 4) / 4;
@@ -442,20 +583,21 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   uint8_t* raw = dys + round256(slots * w.n * 2);
   uint8_t* factors = raw + round256(slots * w.inner * 8);
   uint8_t* dots = factors + round256(slots * w.inner * 4);
-  const int64_t chunks = plan_chunks(slots, w.count, width);
-  if ((err = launch_experts_plan(r, w.count, width, plan, stream)) != cudaSuccess) return err;
+  const Plan wide = experts_wide_plan(plan, slots, w.count);
+  const int64_t chunks = plan_chunks(slots, w.count, wide_width);
+  if ((err = launch_experts_plan(r, w.count, width, plan, wide_width, &wide, stream)) != cudaSuccess) return err;
   if ((err = launch_experts_spread(x, ld_x, w.n, r, plan, xs, amax, nullptr, stream)) != cudaSuccess) return err;
   if ((err = launch_experts_spread(dy, ld_dy, w.n, r, plan, dys, dy_amax, nullptr, stream)) != cudaSuccess) return err;
   if ((err = launch_experts_raw(xs, amax, slots, w, plan, width, reinterpret_cast<float*>(raw), stream)) != cudaSuccess) return err;
   BackArgs p = {};
-  p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.activation = w.activation, p.plan = plan, p.weights = r.weights, p.amax = dy_amax;
+  p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.activation = w.activation, p.plan = wide, p.weights = r.weights, p.amax = dy_amax;
   p.raw = reinterpret_cast<const float*>(raw), p.gate_scale = w.gate.scale, p.up_scale = w.up.scale, p.slots = slots;
   p.factors = dx != nullptr ? reinterpret_cast<__nv_bfloat16*>(factors) : nullptr;
   p.dots = dweights != nullptr ? reinterpret_cast<float*>(dots) : nullptr;
-  if ((err = launch_back<kModeHidden>(width, dys, 1, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
+  if ((err = launch_back<kModeHidden>(wide_width, dys, 1, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
   if (dx != nullptr) {
     p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.part = reinterpret_cast<float*>(xs);
-    if ((err = launch_back<kModeInput>(width, factors, 2, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
+    if ((err = launch_back<kModeInput>(wide_width, factors, 2, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
     if ((err = launch_experts_combine(p.part, r, nullptr, plan, w.n, dx, ld_dx, stream)) != cudaSuccess) return err;
   }
   if (dweights == nullptr) return cudaSuccess;

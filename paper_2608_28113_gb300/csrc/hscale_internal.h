@@ -179,9 +179,14 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
 // amax, contiguous); g and u of each position (fp32 [positions, 2, inner]); a token's slots' rows (fp32, contiguous) times
 // their weights (nullptr: 1) added up.
 int experts_width(int64_t slots, int64_t experts);
+// Bytes [rows, bytes] in TMA boxes of width (128: swizzled, or 16) x height.
+cudaError_t bytes_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t rows, uint32_t width, uint32_t height);
 int64_t experts_plan_bytes(int64_t slots, int64_t experts);
 Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts);
-cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, const Plan& plan, cudaStream_t stream);
+// (a second list of chunks, of another width, over the same positions: experts_wide_plan's, or nullptr)
+Plan experts_wide_plan(const Plan& plan, int64_t slots, int64_t experts);
+cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, const Plan& plan, int wide_width,
+                                const Plan* wide, cudaStream_t stream);
 cudaError_t launch_experts_spread(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out,
                                   uint32_t* amax, uint32_t* h_amax, cudaStream_t stream);
 cudaError_t launch_experts_raw(const void* xs, const uint32_t* amax, int64_t slots, const Experts& w, const Plan& plan,
