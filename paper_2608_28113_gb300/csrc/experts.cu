@@ -197,12 +197,10 @@ constexpr int kStages = 4;              // unpacked blocks and blocks of the slo
 // A packed block: kQuad blocks of K of the tile's rows, 128 bytes a row, and 16 bytes of their codes (20 where they are
 // copied as whole words from any address).
 constexpr int kQuad = 4;
-constexpr uint32_t kRowBytes = kQuad * kBK / 2, kCodeRow = 20;
+constexpr uint32_t kRowBytes = kPackedRow;
+static_assert(kRowBytes == kQuad * kBK / 2, "a packed stage's rows");
 constexpr uint32_t kHalfBytes = kBM * kRowBytes, kHalfCodes = kBM * kCodeRow;
 constexpr uint32_t kPackedBytes = kHalves * (kHalfBytes + kHalfCodes);
-// How the packed weights come: read where they are unpacked (codes at an odd address), by two warps' asynchronous
-// copies (rows that TMA cannot have), by TMA.
-constexpr int kDirect = 0, kCopies = 1, kBulk = 2;
 
 template <int kN>
 struct Tile {
@@ -225,7 +223,7 @@ struct GemmArgs {
   int64_t rows, cols;  // of an expert's matrix
   int32_t kb_total, tiles_o, tile_rows;  // tile_rows: between the tiles' first rows
   int32_t activation;
-  int32_t path;  // kDirect, kCopies or kBulk
+  int32_t path;  // packed_path
   int64_t all_rows;  // of all experts
   Plan plan;
   const uint32_t* amax;  // of each position's row of the slots' tile
@@ -280,7 +278,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       mbar_init(&empty[s], 1);
     }
     for (int s = 0; s < kPackedStages; ++s) {
-      mbar_init(&packed_full[s], p.path == kCopies ? 2 * 32 : 1);
+      mbar_init(&packed_full[s], (p.path == kCopies || p.path == kMixed ? 2 * 32 : 0) + (p.path >= kMixed ? 1 : 0));
       mbar_init(&packed_empty[s], kUnpackWarps);
     }
     for (int i = 0; i < kAccs; ++i) {
@@ -291,7 +289,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     *failed = 0u;
     mbar_fence_init();
     prefetch_tensormap(&vmap);
-    if (p.path == kBulk) prefetch_tensormap(&amap), prefetch_tensormap(&bmap), prefetch_tensormap(&acodes), prefetch_tensormap(&bcodes);
+    if (p.path >= kMixed) prefetch_tensormap(&amap), prefetch_tensormap(&bmap);
+    if (p.path == kBulk) prefetch_tensormap(&acodes), prefetch_tensormap(&bcodes);
   }
   if (warp == 1) {
     tmem_alloc(smem_addr(tmem_slot), 512);
@@ -463,7 +462,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         const int t = first + i * step;
         const int64_t in_tile = (int64_t)(t % p.tiles_o) * p.tile_rows + row_in_tile;
         row = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows;
-        if (p.path == kCopies)
+        if (p.path != kDirect)
           shift = (uint32_t)((row + in_tile) * code_cols & 3) * 8;
         else
           row += min(in_tile, p.rows - 1);
@@ -546,78 +545,47 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     }
     if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + group, turn);
     if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
-  } else if (p.path == kBulk && warp == kWeightsWarp0) {
+  } else if (p.path != kDirect && (warp == kWeightsWarp0 || p.path != kBulk)) {
     // the packed weights; an expert's other chunks read them again, from L2
+    const int half = warp - kWeightsWarp0;  // whose copies are this warp's
+    const ExpertMatrix& w = half ? p.b : p.a;
+    const bool loads = p.path >= kMixed && half == 0, copies = p.path != kBulk;
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
     uint32_t s = 0, parity = 1;
     bool go = true;
     for (int i = 0; i < ntiles && go; ++i) {
       const int t = first + i * step;
-      const int row_a = (int)((int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + (int64_t)(t % p.tiles_o) * p.tile_rows);
-      const int row_b = row_a + (kMode == kModeDown ? kBM : 0);
+      const int64_t row_a = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + (int64_t)(t % p.tiles_o) * p.tile_rows;
+      const int64_t row_b = row_a + (kMode == kModeDown ? kBM : 0), row = half ? row_b : row_a;
       for (int quad = 0; quad < quads; ++quad) {
         if (!mbar_wait_warp(&packed_empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
           go = false;
           break;
         }
-        if (elect_one()) {
-          uint8_t *to = packed + s * (kHalves * kHalfBytes), *codes_to = packed_codes + s * (kHalves * kHalfCodes);
-          mbar_arrive_expect_tx(&packed_full[s], kHalves * (kHalfBytes + kBM * 16));
-          tma_load_2d(to, &amap, quad * (int)kRowBytes, row_a, &packed_full[s], policy);
-          tma_load_2d(codes_to, &acodes, quad * 16, row_a, &packed_full[s], policy);
-          tma_load_2d(to + kHalfBytes, &bmap, quad * (int)kRowBytes, row_b, &packed_full[s], policy);
-          tma_load_2d(codes_to + kHalfCodes, &bcodes, quad * 16, row_b, &packed_full[s], policy);
-        }
-        __syncwarp();
-        if (++s == kPackedStages) s = 0, parity ^= 1u;
-      }
-    }
-    ring_drain(packed_full, kPackedStages, s, parity);
-  } else if (p.path == kCopies) {
-    // one half a warp: 16 lanes a row of 128 bytes, then four (five, with the word that the last codes end in) a row's codes
-    const int half = warp - kWeightsWarp0;
-    const ExpertMatrix& w = half ? p.b : p.a;
-    const int64_t half_cols = p.cols >> 1, code_cols = p.cols >> 4, code_end = p.all_rows * code_cols;
-    uint32_t s = 0, parity = 1;
-    bool go = true;
-    for (int i = 0; i < ntiles && go; ++i) {
-      const int t = first + i * step;
-      const int64_t row0 = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + (int64_t)(t % p.tiles_o) * p.tile_rows +
-                           (kMode == kModeDown && half ? kBM : 0);
-      for (int quad = 0; quad < quads; ++quad) {
-        if (!mbar_wait_warp(&packed_empty[s], parity)) {
-          if (lane == 0) atomicOr(failed, 1u);
-          go = false;
-          break;
-        }
-        const uint32_t to = smem_addr(packed + s * (kHalves * kHalfBytes) + half * kHalfBytes);
-        const uint32_t codes_to = smem_addr(packed_codes + s * (kHalves * kHalfCodes) + half * kHalfCodes);
-        const int64_t at = (int64_t)quad * kRowBytes + (lane & 15) * 8;
-        const uint32_t bytes = at < half_cols ? 8u : 0u;
-        int64_t row = row0 + (lane >> 4);
-        const uint8_t* src = w.packed + row * half_cols + at;
-#pragma unroll 8
-        for (int r = 0; r < kBM; r += 2, row += 2, src += 2 * half_cols) {
-          const uint32_t in_half = (uint32_t)(r + (lane >> 4));
-          const bool on = bytes && row < p.all_rows;
-          copy_8_async(to + in_half * kRowBytes + ((((uint32_t)(lane & 15) >> 1) ^ (in_half & 7u)) << 4) + (lane & 1) * 8, on ? src : w.packed,
-                       on ? 8u : 0u);
-        }
-        for (int r = lane; r < kBM; r += 32) {
-          const int64_t word = ((row0 + r) * code_cols + (int64_t)quad * 16) & ~(int64_t)3;
-#pragma unroll
-          for (int e = 0; e < 5; ++e) {
-            const int64_t left = code_end - (word + 4 * e);
-            copy_4_async(codes_to + r * kCodeRow + 4 * e, left > 0 ? w.codes + word + 4 * e : w.codes, left <= 0 ? 0u : left < 4 ? (uint32_t)left : 4u);
+        uint8_t *to = packed + s * (kHalves * kHalfBytes), *codes_to = packed_codes + s * (kHalves * kHalfCodes);
+        if (loads && elect_one()) {
+          mbar_arrive_expect_tx(&packed_full[s], kHalves * (kHalfBytes + (p.path == kBulk ? kBM * 16 : 0)));
+          tma_load_2d(to, &amap, quad * (int)kRowBytes, (int)row_a, &packed_full[s], policy);
+          tma_load_2d(to + kHalfBytes, &bmap, quad * (int)kRowBytes, (int)row_b, &packed_full[s], policy);
+          if (p.path == kBulk) {
+            tma_load_2d(codes_to, &acodes, quad * 16, (int)row_a, &packed_full[s], policy);
+            tma_load_2d(codes_to + kHalfCodes, &bcodes, quad * 16, (int)row_b, &packed_full[s], policy);
           }
         }
-        copies_arrive(smem_addr(&packed_full[s]));
+        __syncwarp();
+        if (copies) {
+          if (p.path == kCopies)
+            copy_packed<kBM>(w.packed, p.cols >> 1, p.all_rows, row, (int64_t)quad * kRowBytes, smem_addr(to + half * kHalfBytes), 0, lane);
+          copy_codes<kBM>(w.codes, p.cols >> 4, p.all_rows, row, (int64_t)quad * 16, smem_addr(codes_to + half * kHalfCodes), 0, lane);
+          copies_arrive(smem_addr(&packed_full[s]));
+        }
         if (++s == kPackedStages) s = 0, parity ^= 1u;
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    ring_drain(packed_full, kPackedStages, s, parity);
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -648,16 +616,14 @@ cudaError_t launch_gemm_n(const void* v, int64_t slots, int64_t experts, GemmArg
   CUtensorMap map;
   cudaError_t err = slots_map(&map, v, p.cols, slots, kN);
   if (err != cudaSuccess) return err;
-  const auto at = [](const void* q, uintptr_t a) { return reinterpret_cast<uintptr_t>(q) % a == 0; };
   p.all_rows = experts * p.rows;
-  // TMA wants rows of whole 16 bytes, codes too, and rows that an int counts
-  const bool bulk = p.cols % 256 == 0 && at(p.a.packed, 16) && at(p.b.packed, 16) && at(p.a.codes, 16) && at(p.b.codes, 16) &&
-                    p.all_rows + 2 * kBM <= INT32_MAX;
-  p.path = bulk ? kBulk : at(p.a.codes, 4) && at(p.b.codes, 4) ? kCopies : kDirect;
+  p.path = packed_path(p.a, p.b, p.cols, p.all_rows);
   CUtensorMap maps[4] = {map, map, map, map};
-  if (bulk) {
-    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, 128, kBM)) != cudaSuccess) return err;
-    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, 128, kBM)) != cudaSuccess) return err;
+  if (p.path >= kMixed) {
+    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, kRowBytes, kBM)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, kRowBytes, kBM)) != cudaSuccess) return err;
+  }
+  if (p.path == kBulk) {
     if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16, kBM)) != cudaSuccess) return err;
     if ((err = bytes_map(&maps[3], p.b.codes, p.cols / 16, p.all_rows, 16, kBM)) != cudaSuccess) return err;
   }

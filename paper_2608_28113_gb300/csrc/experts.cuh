@@ -78,6 +78,83 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// How a product's packed weights come: read where they are unpacked (codes at an odd address), by two warps'
+// asynchronous copies (rows that TMA cannot have: they want whole 16 bytes), the codes that way and the rest by TMA, all
+// by TMA.  The copies of everything had 16 tokens of 64 experts, 4096 x 2048, take 2.3 times as long as TMA.
+constexpr int kDirect = 0, kCopies = 1, kMixed = 2, kBulk = 3;
+constexpr uint32_t kPackedRow = 128, kCodeRow = 20;  // bytes of a row in a stage: 256 weights, and their codes' words
+
+// kRows rows of 128 bytes, from byte `from` of row `row` on, to rows first, first + 1, ... of a stage whose 16-byte
+// pieces are swizzled as TMA does.  By a warp, 8 bytes a lane; first % 8 == 0.  Bytes past a row's end are zeros.
+template <int kRows>
+__device__ __forceinline__ void copy_packed(const uint8_t* packed, int64_t half_cols, int64_t all_rows, int64_t row, int64_t from,
+                                            uint32_t stage, int first, int lane) {
+  const int sub = lane >> 4, piece = lane & 15;
+  const bool on = from + piece * 8 < half_cols;
+  const uint8_t* src = on ? packed + (row + sub) * half_cols + from + piece * 8 : packed;
+  const int64_t step = on ? 2 * half_cols : 0;
+  uint32_t to[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    to[i] = stage + (uint32_t)(first + 2 * i + sub) * kPackedRow + (((uint32_t)(piece >> 1) ^ (uint32_t)(2 * i + sub)) << 4) + (piece & 1) * 8;
+  if (row + kRows <= all_rows) {
+#pragma unroll 4
+    for (int r = 0; r < kRows; r += 8)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        copy_8_async(to[i] + r * kPackedRow, src, on ? 8u : 0u);
+        src += step;
+      }
+  } else {
+    for (int r = 0; r < kRows; r += 8)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool there = on && row + r + 2 * i + sub < all_rows;
+        copy_8_async(to[i] + r * kPackedRow, there ? src : packed, there ? 8u : 0u);
+        src += step;
+      }
+  }
+}
+// The words that the codes from byte `from` of these rows on are in: four, and the one that they end in.  (A row's
+// codes may begin inside a word; eight rows further it is the same place in the word.)
+template <int kRows>
+__device__ __forceinline__ void copy_codes(const uint8_t* codes, int64_t code_cols, int64_t all_rows, int64_t row, int64_t from,
+                                           uint32_t stage, int first, int lane) {
+  const int64_t end = all_rows * code_cols;
+  if ((row + kRows - 1) * code_cols + from + 20 <= end) {
+    const uint8_t* src = codes + (((row + (lane >> 2)) * code_cols + from) & ~(int64_t)3) + 4 * (lane & 3);
+    const uint32_t to = stage + (uint32_t)(first + (lane >> 2)) * kCodeRow + 4 * (lane & 3);
+#pragma unroll 4
+    for (int r = 0; r < kRows; r += 8) {
+      copy_4_async(to + r * kCodeRow, src, 4u);
+      src += 8 * code_cols;
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; r += 32)
+      copy_4_async(stage + (uint32_t)(first + r + lane) * kCodeRow + 16,
+                   codes + (((row + r + lane) * code_cols + from) & ~(int64_t)3) + 16, 4u);
+  } else {
+    for (int r = lane; r < kRows; r += 32) {
+      const int64_t word = ((row + r) * code_cols + from) & ~(int64_t)3;
+#pragma unroll
+      for (int e = 0; e < 5; ++e) {
+        const int64_t left = end - (word + 4 * e);
+        copy_4_async(stage + (uint32_t)(first + r) * kCodeRow + 4 * e, left > 0 ? codes + word + 4 * e : codes,
+                     left <= 0 ? 0u : left < 4 ? (uint32_t)left : 4u);
+      }
+    }
+  }
+}
+// The path for matrices a and b: a product's rows are `cols` long, all_rows of them.
+inline int packed_path(const ExpertMatrix& a, const ExpertMatrix& b, int64_t cols, int64_t all_rows) {
+  const auto both = [](const void* p, const void* q, uintptr_t n) {
+    return reinterpret_cast<uintptr_t>(p) % n == 0 && reinterpret_cast<uintptr_t>(q) % n == 0;
+  };
+  if (!both(a.codes, b.codes, 4)) return kDirect;
+  if (cols % 32 != 0 || !both(a.packed, b.packed, 16) || all_rows > INT32_MAX - 512) return kCopies;
+  return cols % 256 == 0 && both(a.codes, b.codes, 16) ? kBulk : kMixed;
+}
+
 // Weights as fp16: E2M1 times E4M3 has at most 6 significant bits, from 2^-10 to 2688, so a weight without its global
 // scale is exact.  The card converts two nibbles in one instruction, and to fp16 only: 85 weights a cycle and
 // SM with their scales, against 43 by the bit operations that make bf16.

@@ -36,9 +36,9 @@ constexpr uint32_t kGroupBytes = 64 * kBK * 2;  // 64 outputs x 64 rows of K
 constexpr uint32_t kHalfBytes = 2 * kGroupBytes;
 // A packed block: 64 rows of K, 128 bytes (256 outputs) each, and 16 bytes of their codes (20 where they are copied
 // as whole words from any address).
-constexpr uint32_t kRowBytes = kHalves * kBM / 2, kCodeRow = 20;
+constexpr uint32_t kRowBytes = kPackedRow;
+static_assert(kRowBytes == kHalves * kBM / 2, "a packed stage's rows");
 constexpr uint32_t kPackedBytes = kBK * kRowBytes, kCodeBytes = kBK * kCodeRow;
-constexpr int kDirect = 0, kCopies = 1, kBulk = 2;  // how the packed weights come (experts.cu)
 
 template <int kN>
 struct Tile {
@@ -152,7 +152,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       mbar_init(&empty[s], 1);
     }
     for (int s = 0; s < kPackedStages; ++s) {
-      mbar_init(&packed_full[s], p.path == kCopies ? 2 * 32 : 1);
+      mbar_init(&packed_full[s], (p.path == kCopies || p.path == kMixed ? 2 * 32 : 0) + (p.path >= kMixed ? 1 : 0));
       mbar_init(&packed_empty[s], kUnpackWarps / 2);
     }
     for (int i = 0; i < kAccs; ++i) {
@@ -163,7 +163,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     *failed = 0u;
     mbar_fence_init();
     prefetch_tensormap(&vmap);
-    if (p.path == kBulk) prefetch_tensormap(&amap), prefetch_tensormap(&bmap), prefetch_tensormap(&acodes), prefetch_tensormap(&bcodes);
+    if (p.path >= kMixed) prefetch_tensormap(&amap), prefetch_tensormap(&bmap);
+    if (p.path == kBulk) prefetch_tensormap(&acodes), prefetch_tensormap(&bcodes);
   }
   if (warp == 1) {
     tmem_alloc(smem_addr(tmem_slot), T::kTmemCols);
@@ -337,7 +338,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       const int64_t e = p.plan.chunks[t / p.tiles_o].expert, o0 = (int64_t)(t % p.tiles_o) * (kHalves * kBM) + part64 * 64;
       const int64_t row0 = e * p.rows + row;
       // bits that a row's codes begin into a word: the same for rows 64 apart
-      const uint32_t shift = p.path == kCopies ? (uint32_t)(row0 * code_cols & 3) * 8 : 0u;
+      const uint32_t shift = p.path == kCopies || p.path == kMixed ? (uint32_t)(row0 * code_cols & 3) * 8 : 0u;
       int done = 0;
       for (; kb < kbs && go; kb += 2, block += 2) {
         const uint32_t ps = block % kPackedStages, parity_p = (block / kPackedStages) & 1u;
@@ -355,7 +356,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
                          : "r"(from + ((((uint32_t)(2 * part64 + h)) ^ swizzle) << 4)));
           const uint32_t at = smem_addr(packed_codes + ps * kCodeBytes) + row * (p.path == kBulk ? 16u : kCodeRow) + 4 * part64;
           asm volatile("ld.shared.u32 %0, [%1];" : "=r"(code) : "r"(at));
-          if (p.path == kCopies) {
+          if (p.path != kBulk) {
             uint32_t more;
             asm volatile("ld.shared.u32 %0, [%1];" : "=r"(more) : "r"(at + 4));
             code = __funnelshift_r(code, more, shift);
@@ -411,42 +412,16 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     }
     if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
     if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
-  } else if (p.path == kBulk && warp == kWeightsWarp0) {
+  } else if (p.path != kDirect && (warp == kWeightsWarp0 || p.path != kBulk)) {
+    const int who = warp - kWeightsWarp0;  // whose copies are 32 of the 64 rows
+    const bool loads = p.path >= kMixed && who == 0, copies = p.path != kBulk;
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
     uint32_t s = 0, parity = 1;
     bool go = true;
     for (int i = 0; i < ntiles && go; ++i) {
       const int t = first + i * step, to = t % p.tiles_o;
-      const int row0 = (int)((int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows);
-      for (int kb = 0; kb < kbs; ++kb) {
-        if (!mbar_wait_warp(&packed_empty[s], parity)) {
-          if (lane == 0) atomicOr(failed, 1u);
-          go = false;
-          break;
-        }
-        if (elect_one()) {
-          const bool second = kb >= p.kb_part;
-          const int row = row0 + (kb - (second ? p.kb_part : 0)) * kBK;
-          mbar_arrive_expect_tx(&packed_full[s], kPackedBytes + kBK * 16);
-          tma_load_2d(packed + s * kPackedBytes, second ? &bmap : &amap, to * (int)kRowBytes, row, &packed_full[s], policy);
-          tma_load_2d(packed_codes + s * kCodeBytes, second ? &bcodes : &acodes, to * 16, row, &packed_full[s], policy);
-        }
-        __syncwarp();
-        if (++s == kPackedStages) s = 0, parity ^= 1u;
-      }
-    }
-    ring_drain(packed_full, kPackedStages, s, parity);
-  } else if (p.path == kCopies) {
-    // 32 rows of K a warp: 16 lanes a row of 128 bytes, then a lane a row's five words of codes
-    const int who = warp - kWeightsWarp0;
-    const int64_t half_cols = p.cols >> 1, code_cols = p.cols >> 4, code_end = p.all_rows * code_cols;
-    uint32_t s = 0, parity = 1;
-    bool go = true;
-    for (int i = 0; i < ntiles && go; ++i) {
-      const int t = first + i * step, to = t % p.tiles_o;
-      const int64_t row0 = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + 32 * who;
-      const int64_t at = (int64_t)to * kRowBytes + (lane & 15) * 8;
+      const int64_t row0 = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows;
       for (int kb = 0; kb < kbs; ++kb) {
         if (!mbar_wait_warp(&packed_empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
@@ -454,30 +429,26 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           break;
         }
         const bool second = kb >= p.kb_part;
-        const ExpertMatrix& w = second ? p.b : p.a;
-        const int64_t row1 = row0 + (int64_t)(kb - (second ? p.kb_part : 0)) * kBK;
-        const uint32_t to_packed = smem_addr(packed + s * kPackedBytes), to_codes = smem_addr(packed_codes + s * kCodeBytes);
-        int64_t row = row1 + (lane >> 4);
-        const uint8_t* src = w.packed + row * half_cols + at;
-#pragma unroll 8
-        for (int r = 0; r < 32; r += 2, row += 2, src += 2 * half_cols) {
-          const uint32_t in = (uint32_t)(32 * who + r + (lane >> 4));
-          const bool on = at < half_cols && row < p.all_rows;
-          copy_8_async(to_packed + in * kRowBytes + ((((uint32_t)(lane & 15) >> 1) ^ (in & 7u)) << 4) + (lane & 1) * 8, on ? src : w.packed,
-                       on ? 8u : 0u);
+        const int64_t row = row0 + (int64_t)(kb - (second ? p.kb_part : 0)) * kBK;
+        uint8_t *packed_to = packed + s * kPackedBytes, *codes_to = packed_codes + s * kCodeBytes;
+        if (loads && elect_one()) {
+          mbar_arrive_expect_tx(&packed_full[s], kPackedBytes + (p.path == kBulk ? kBK * 16 : 0));
+          tma_load_2d(packed_to, second ? &bmap : &amap, to * (int)kRowBytes, (int)row, &packed_full[s], policy);
+          if (p.path == kBulk) tma_load_2d(codes_to, second ? &bcodes : &acodes, to * 16, (int)row, &packed_full[s], policy);
         }
-        const int64_t word = ((row1 + lane) * code_cols + (int64_t)to * 16) & ~(int64_t)3;
-#pragma unroll
-        for (int h = 0; h < 5; ++h) {
-          const int64_t left = code_end - (word + 4 * h);
-          copy_4_async(to_codes + (32 * who + lane) * kCodeRow + 4 * h, left > 0 ? w.codes + word + 4 * h : w.codes,
-                       left <= 0 ? 0u : left < 4 ? (uint32_t)left : 4u);
+        __syncwarp();
+        if (copies) {
+          const ExpertMatrix& w = second ? p.b : p.a;
+          if (p.path == kCopies)
+            copy_packed<32>(w.packed, p.cols >> 1, p.all_rows, row + 32 * who, (int64_t)to * kRowBytes, smem_addr(packed_to), 32 * who, lane);
+          copy_codes<32>(w.codes, p.cols >> 4, p.all_rows, row + 32 * who, (int64_t)to * 16, smem_addr(codes_to), 32 * who, lane);
+          copies_arrive(smem_addr(&packed_full[s]));
         }
-        copies_arrive(smem_addr(&packed_full[s]));
         if (++s == kPackedStages) s = 0, parity ^= 1u;
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    ring_drain(packed_full, kPackedStages, s, parity);
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -516,16 +487,14 @@ cudaError_t launch_back_n(const void* v, int64_t depth, int64_t experts, BackArg
   if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(v), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  const auto at = [](const void* q, uintptr_t a) { return reinterpret_cast<uintptr_t>(q) % a == 0; };
   p.all_rows = experts * p.rows;
-  // TMA wants rows of whole 16 bytes, codes too, and rows that an int counts
-  const bool bulk = p.cols % 256 == 0 && at(p.a.packed, 16) && at(p.b.packed, 16) && at(p.a.codes, 16) && at(p.b.codes, 16) &&
-                    p.all_rows + 2 * kBM <= INT32_MAX;
-  p.path = bulk ? kBulk : at(p.a.codes, 4) && at(p.b.codes, 4) ? kCopies : kDirect;
+  p.path = packed_path(p.a, p.b, p.cols, p.all_rows);
   CUtensorMap maps[4] = {map, map, map, map};
-  if (bulk) {
-    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, 128, kBK)) != cudaSuccess) return err;
-    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, 128, kBK)) != cudaSuccess) return err;
+  if (p.path >= kMixed) {
+    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, kRowBytes, kBK)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, kRowBytes, kBK)) != cudaSuccess) return err;
+  }
+  if (p.path == kBulk) {
     if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16, kBK)) != cudaSuccess) return err;
     if ((err = bytes_map(&maps[3], p.b.codes, p.cols / 16, p.all_rows, 16, kBK)) != cudaSuccess) return err;
   }

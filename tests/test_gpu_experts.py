@@ -52,7 +52,7 @@ def layer(t, n, inner, count, k, seed=0, pad=8, none=0.1, skew=0):
 # tokens, n, inner, experts, k
 SIZES = [(1, 16, 16, 1, 1), (1, 64, 32, 4, 2), (1, 512, 256, 16, 8), (3, 80, 48, 5, 3), (37, 272, 144, 12, 3), (64, 128, 128, 64, 8),
          (130, 512, 256, 8, 2), (300, 256, 400, 3, 2), (600, 64, 80, 2, 1), (45, 1040, 528, 40, 4), (9, 2048, 64, 1024, 32),
-         (70, 144, 1040, 7, 5)]
+         (70, 144, 1040, 7, 5), (1100, 320, 192, 2, 2), (640, 256, 512, 1, 1)]
 
 
 def clean(w):
@@ -213,6 +213,29 @@ def test_streams_and_graphs(t):
     assert torch.equal(y1, run(*args, 0))
     dx, dw = backward(dy, *args, 0)
     assert torch.equal(dx1, dx) and torch.equal(dw1, dw)
+
+
+def moved(weight, packed_by, codes_by):
+    """The same weight at other addresses: bytes behind a multiple of 256."""
+    out = []
+    for t, by in zip(weight[:2], (packed_by, codes_by)):
+        room = torch.empty(t.numel() + by, dtype=U8, device=DEV)
+        room[by:] = t.reshape(-1)
+        out.append(room[by:].view(t.shape))
+    return out[0], out[1], weight[2]
+
+
+@pytest.mark.parametrize("t, n, inner", [(5, 256, 512), (150, 512, 256), (5, 96, 160), (150, 320, 96), (150, 272, 176), (1100, 256, 272)])
+@pytest.mark.parametrize("packed_by, codes_by", [(8, 0), (16, 4), (8, 4), (0, 1), (24, 6)])
+def test_weights_at_any_address(t, n, inner, packed_by, codes_by):
+    """Each way that the packed weights come to be unpacked gives the same bits."""
+    x, ids, w, gate, up, down = layer(t, n, inner, 4, 2, seed=21)
+    dy, _ = rows(t, n, 0, torch.Generator().manual_seed(2))
+    want, (want_dx, want_dw) = run(x, ids, w, gate, up, down, 0), backward(dy, x, ids, w, gate, up, down, 0)
+    other = [moved(m, packed_by, codes_by) for m in (gate, up, down)]
+    assert torch.equal(run(x, ids, w, *other, 0), want)
+    dx, dw = backward(dy, x, ids, w, *other, 0)
+    assert torch.equal(dx, want_dx) and torch.equal(dw, want_dw)
 
 
 def test_two_calls_at_once():
