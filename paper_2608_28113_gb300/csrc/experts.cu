@@ -44,6 +44,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
   extern __shared__ int32_t counts[];  // [kPlanWarps][experts], then each expert's first position
   int32_t* first = counts + kPlanWarps * experts;
   __shared__ int32_t warp_total[kPlanWarps], warp_chunks[kPlanWarps], warp_wide[kPlanWarps];
+  pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t run = (slots + kPlanWarps - 1) / kPlanWarps, s0 = warp * run, s1 = min(slots, s0 + run);
   for (int i = threadIdx.x; i < kPlanWarps * experts; i += kPlanThreads) counts[i] = 0;
@@ -126,6 +127,7 @@ __global__ void __launch_bounds__(256) spread_kernel(const uint4* x, int64_t ld,
                                                      uint32_t* amax, uint32_t* h_amax) {
   __shared__ uint32_t warp_max[8];
   pdl_wait_primary();
+  pdl_launch_dependents();
   const int64_t t = blockIdx.x;
   const uint4* row = x + t * ld;
   uint4 kept[kSpreadKept];
@@ -161,6 +163,7 @@ __global__ void __launch_bounds__(256) spread_kernel(const uint4* x, int64_t ld,
 
 // h, bf16, to fp16 in place (experts.cuh), 16 bytes a thread.
 __global__ void __launch_bounds__(256) convert_kernel(uint4* h, int64_t pieces, Plan plan, const uint32_t* amax) {
+  pdl_launch_dependents();  // the second product's weights may come; it waits for this kernel before it reads h
   pdl_wait_primary();
   const int64_t total = plan.header[1] * pieces;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256)
@@ -193,7 +196,6 @@ constexpr int kBM = 128, kBK = 64, kHalves = 2;
 constexpr int kEpilogueWarp0 = 2, kUnpackWarp0 = 6, kUnpackWarps = 16, kWeightsWarp0 = 22;
 constexpr int kThreads = 768;
 constexpr int kModeHidden = 0, kModeRaw = 1, kModeDown = 2;
-constexpr int kStages = 4;              // unpacked blocks and blocks of the slots' tile
 // A packed block: kQuad blocks of K of the tile's rows, 128 bytes a row, and 16 bytes of their codes (20 where they are
 // copied as whole words from any address).
 constexpr int kQuad = 4;
@@ -204,6 +206,7 @@ constexpr uint32_t kPackedBytes = kHalves * (kHalfBytes + kHalfCodes);
 
 template <int kN>
 struct Tile {
+  static constexpr int kStages = kN <= 32 ? 6 : 4;  // unpacked blocks and blocks of the slots' tile
   static constexpr int kAccs = kN <= 64 ? 2 : 1;
   static constexpr bool kHelp = kAccs == 1;  // the unpacking warps take part in the epilogue
   static constexpr int kPackedStages = kN <= 64 ? 5 : 3;
@@ -254,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
             const __grid_constant__ CUtensorMap acodes, const __grid_constant__ CUtensorMap bcodes, const __grid_constant__ GemmArgs p) {
   using T = Tile<kN>;
-  constexpr int kAccs = T::kAccs, kPackedStages = T::kPackedStages;
+  constexpr int kStages = T::kStages, kAccs = T::kAccs, kPackedStages = T::kPackedStages;
   extern __shared__ __align__(16) uint8_t dynamic_smem[];
   uint8_t* smem = dynamic_smem + ((1024u - (smem_addr(dynamic_smem) & 1023u)) & 1023u);
   uint8_t* tile_b = smem;
@@ -300,7 +303,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = warp_uniform(*tmem_slot);
-  pdl_wait_primary();  // the plan and the slots' tile
+  // The plan is there: the kernel that this one may run beside has waited for it.  What that kernel writes (the slots'
+  // tile, and the rows' amax) is waited for where it is read; the weights begin to come meanwhile.
 
   const int tiles = p.plan.header[0] * p.tiles_o, step = (int)gridDim.x, first = (int)blockIdx.x;
   const int ntiles = tiles > first ? (tiles - first + step - 1) / step : 0;
@@ -382,6 +386,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   const auto turn_at = [&](int worker) { return reinterpret_cast<uint32_t*>(rest + 512 + worker * 1024); };
 
   if (warp == 0) {
+    pdl_wait_primary();
+    pdl_launch_dependents();
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
     uint32_t s = 0, parity = 1;
@@ -441,6 +447,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     __syncwarp();
     umma_drain(mma_done);
   } else if (warp < kUnpackWarp0) {
+    pdl_wait_primary();
     for (int i = 0; i < ntiles; ++i) finish(i, 0, turn_at(warp - kEpilogueWarp0));
     if (!have && lane == 0) atomicOr(failed, 1u);
   } else if (warp < kWeightsWarp0) {
@@ -540,9 +547,13 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           if (++stage == kPackedStages) stage = 0, parity_p ^= 1u;
         }
         // the tile before, once this one's first blocks are there for the MMAs
-        if (T::kHelp && quad == 0 && i > 0) finish(i - 1, 1 + group, turn);
+        if (T::kHelp && quad == 0 && i > 0) {
+          if (i == 1) pdl_wait_primary();
+          finish(i - 1, 1 + group, turn);
+        }
       }
     }
+    if (T::kHelp && ntiles == 1) pdl_wait_primary();
     if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + group, turn);
     if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
   } else if (p.path != kDirect && (warp == kWeightsWarp0 || p.path != kBulk)) {

@@ -175,6 +175,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   tc_fence_after_sync();
   const uint32_t tmem = warp_uniform(*tmem_slot);
   pdl_wait_primary();  // the plan, the slots' tile, g and u
+  pdl_launch_dependents();
 
   const int tiles = p.plan.header[0] * p.tiles_o, step = (int)gridDim.x, first = (int)blockIdx.x;
   const int ntiles = tiles > first ? (tiles - first + step - 1) / step : 0;
