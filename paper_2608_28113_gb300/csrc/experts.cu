@@ -170,9 +170,10 @@ __global__ void __launch_bounds__(256) convert_kernel(uint4* h, int64_t pieces, 
     h[i] = bf16_to_f16(h[i], exp2_int(-row_exponent(amax[i / pieces])));
 }
 
-// out_t = the sum of the token's slots' rows times their weights (nullptr: 1), in order; four columns a thread.
-__global__ void __launch_bounds__(256) combine_kernel(const float* part, Plan plan, const float* weights, int64_t tokens, int k, int64_t n,
-                                                      __nv_bfloat16* out, int64_t ld) {
+// out_t = the sum of the token's slots' rows (part, and more where it is not nullptr) times their weights (nullptr: 1), in order;
+// four columns a thread.
+__global__ void __launch_bounds__(256) combine_kernel(const float* part, const float* more, Plan plan, const float* weights, int64_t tokens, int k,
+                                                      int64_t n, __nv_bfloat16* out, int64_t ld) {
   pdl_wait_primary();
   const int64_t per = n / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= tokens * per) return;
@@ -183,7 +184,11 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* part, Plan pl
     const int64_t pos = plan.pos_of[t * k + j];
     if (pos < 0) continue;
     const float w = weights == nullptr ? 1.0f : weights[t * k + j];
-    const float4 v = *reinterpret_cast<const float4*>(part + pos * n + c);
+    float4 v = *reinterpret_cast<const float4*>(part + pos * n + c);
+    if (more != nullptr) {
+      const float4 m = *reinterpret_cast<const float4*>(more + pos * n + c);
+      v.x += m.x, v.y += m.y, v.z += m.z, v.w += m.w;
+    }
     s.x = fmaf(w, v.x, s.x), s.y = fmaf(w, v.y, s.y), s.z = fmaf(w, v.z, s.z), s.w = fmaf(w, v.w, s.w);
   }
   uint2 r;
@@ -313,26 +318,46 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   const int row_in_half = (int)quarter * 32 + lane;
   bool have = true;  // of the warps of the epilogue: no wait for an accumulator has run out
 
-  // The epilogue of the CTA's tile i: 16 slots a time, those of this warp (one of T::kEpilogueWarps / 4 of its quarter).
-  const auto finish = [&](int i, int who, uint32_t* turn) {
-    constexpr int kWorkers = T::kEpilogueWarps / 4;
+  // What a warp's epilogue of the CTA's tile i needs, fetched before its time: the chunk, the matrices' scales, and the power
+  // of two of the rows of its first 16 slots and its second (lane j: slot j's).
+  struct Finish {
+    Chunk c;
+    float scale_a, scale_b, up0, up1;
+  };
+  constexpr int kWorkers = T::kEpilogueWarps / 4;
+  const auto up_of = [&](const Chunk& c, int j) { return lane < 16 && j + lane < c.count ? exp2_int(row_exponent(p.amax[c.first + j + lane])) : 0.0f; };
+  const auto prepare = [&](int i, int who) {
+    Finish f;
+    f.c = p.plan.chunks[(first + i * step) / p.tiles_o];
+    f.scale_a = p.a.scale[f.c.expert], f.scale_b = p.b.scale[f.c.expert];
+    f.up0 = up_of(f.c, 16 * who), f.up1 = up_of(f.c, 16 * (who + kWorkers));
+    return f;
+  };
+  const auto release = [&](uint32_t acc) {
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+  };
+  // The epilogue: 16 slots a time, those of this warp (one of kWorkers of its quarter).
+  const auto finish = [&](int i, int who, uint32_t* turn, const Finish& f) {
     const int t = first + i * step;
-    const Chunk c = p.plan.chunks[t / p.tiles_o];
+    const Chunk& c = f.c;
     const int64_t o0 = (int64_t)(t % p.tiles_o) * p.tile_rows, o = o0 + row_in_half;
     const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc + lane_base;
-    const float scale_a = p.a.scale[c.expert], scale_b = p.b.scale[c.expert];
+    const float scale_a = f.scale_a, scale_b = f.scale_b;
     const float nan = __int_as_float(0x7FC00000);
     if (have) have = __all_sync(0xFFFFFFFFu, mbar_wait_acc(&acc_full[acc], (uint32_t)(i / kAccs) & 1u));
     tc_fence_after_sync();
 #pragma unroll 1
-    for (int j0 = 16 * who; j0 < c.count; j0 += 16 * kWorkers) {
+    for (int j0 = 16 * who, turns = 0; j0 < c.count; j0 += 16 * kWorkers, ++turns) {
       const int left = min(16, c.count - j0);
-      // lane j: the power of two of slot j's row
-      const float my_up = lane < left ? exp2_int(row_exponent(p.amax[c.first + j0 + lane])) : 0.0f;
+      const float my_up = turns == 0 ? f.up0 : turns == 1 ? f.up1 : up_of(c, j0);
       uint32_t a[16], b[16];
       tmem_ld_32x32b_x16(d + (uint32_t)j0, a);
       tmem_ld_32x32b_x16(d + (uint32_t)(kN + j0), b);
       tmem_ld_wait();
+      // the warp's last columns: the next tile's MMAs need not wait for what is done with them
+      if (j0 + 16 * kWorkers >= c.count) release(acc);
       if constexpr (kMode == kModeHidden) {
         // rounded and turned, so that a lane stores 8 outputs of a slot at once
         __syncwarp();
@@ -379,9 +404,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
       }
     }
-    tc_fence_before_sync();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+    if (16 * who >= c.count) release(acc);
   };
   const auto turn_at = [&](int worker) { return reinterpret_cast<uint32_t*>(rest + 512 + worker * 1024); };
 
@@ -448,7 +471,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     umma_drain(mma_done);
   } else if (warp < kUnpackWarp0) {
     pdl_wait_primary();
-    for (int i = 0; i < ntiles; ++i) finish(i, 0, turn_at(warp - kEpilogueWarp0));
+    Finish f = {};
+    if (ntiles > 0) f = prepare(0, 0);
+    for (int i = 0; i < ntiles; ++i) {
+      finish(i, 0, turn_at(warp - kEpilogueWarp0), f);
+      if (i + 1 < ntiles) f = prepare(i + 1, 0);
+    }
     if (!have && lane == 0) atomicOr(failed, 1u);
   } else if (warp < kWeightsWarp0) {
     // group: the half it unpacks, of every other K block
@@ -475,6 +503,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           row += min(in_tile, p.rows - 1);
       }
       for (int quad = 0; quad < quads && go; ++quad) {
+        Finish f;
+        if (T::kHelp && quad == 0 && i > 0) {
+          if (i == 1) pdl_wait_primary();
+          f = prepare(i - 1, 1 + group);
+        }
         uint32_t code[2] = {0u, 0u};
         if (p.path != kDirect) {
           if (!mbar_wait_warp(&packed_full[stage], parity_p)) {
@@ -547,22 +580,23 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           if (++stage == kPackedStages) stage = 0, parity_p ^= 1u;
         }
         // the tile before, once this one's first blocks are there for the MMAs
-        if (T::kHelp && quad == 0 && i > 0) {
-          if (i == 1) pdl_wait_primary();
-          finish(i - 1, 1 + group, turn);
-        }
+        if (T::kHelp && quad == 0 && i > 0) finish(i - 1, 1 + group, turn, f);
       }
     }
     if (T::kHelp && ntiles == 1) pdl_wait_primary();
-    if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + group, turn);
+    if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + group, turn, prepare(ntiles - 1, 1 + group));
     if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
   } else if (p.path != kDirect && (warp == kWeightsWarp0 || p.path != kBulk)) {
-    // the packed weights; an expert's other chunks read them again, from L2
+    // the packed weights.  In small tiles an expert's only chunk reads them, once; in large ones others read them again,
+    // from L2
     const int half = warp - kWeightsWarp0;  // whose copies are this warp's
     const ExpertMatrix& w = half ? p.b : p.a;
     const bool loads = p.path >= kMixed && half == 0, copies = p.path != kBulk;
     uint64_t policy;
-    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+    if constexpr (kN <= 32)
+      policy = l2_evict_first_policy();
+    else
+      asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
     uint32_t s = 0, parity = 1;
     bool go = true;
     for (int i = 0; i < ntiles && go; ++i) {
@@ -674,7 +708,7 @@ cudaError_t bytes_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t ro
   const cuuint32_t box[2] = {width, height};
   const cuuint32_t estr[2] = {1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(v), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? cudaSuccess
              : cudaErrorInvalidValue;
@@ -726,10 +760,10 @@ cudaError_t launch_experts_spread(const void* x, int64_t ld, int64_t n, const Ro
                         static_cast<uint4*>(out), amax, h_amax);
 }
 
-cudaError_t launch_experts_combine(const float* part, const Routing& r, const float* weights, const Plan& plan, int64_t n, void* out,
+cudaError_t launch_experts_combine(const float* part, const float* more, const Routing& r, const float* weights, const Plan& plan, int64_t n, void* out,
                                    int64_t ld, cudaStream_t stream) {
   const int64_t threads = r.tokens * (n / 4);
-  return launch_chained(combine_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, stream, part, plan, weights, r.tokens, r.k, n,
+  return launch_chained(combine_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, stream, part, more, plan, weights, r.tokens, r.k, n,
                         static_cast<__nv_bfloat16*>(out), ld);
 }
 
@@ -775,7 +809,7 @@ cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const 
   if (err != cudaSuccess) return err;
   p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.amax = h_amax, p.out = part;
   if ((err = launch_gemm<kModeDown>(width, h, slots, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
-  return launch_experts_combine(part, r, r.weights, plan, w.n, y, ld_y, stream);
+  return launch_experts_combine(part, nullptr, r, r.weights, plan, w.n, y, ld_y, stream);
 }
 
 cudaError_t read_experts_device_error(uint32_t* flags) {

@@ -59,6 +59,7 @@ struct BackArgs {
   ExpertMatrix a, b;    // the weights of the first and the second half of K (down twice where there is one)
   int64_t rows, cols;   // of an expert's matrix: K and the outputs
   int32_t kb_part, parts, tiles_o, path;
+  int32_t splits;    // 2: the halves of K are tiles of their own, into part and more
   int64_t all_rows;  // of all experts
   int32_t activation;
   Plan plan;
@@ -69,7 +70,7 @@ struct BackArgs {
   __nv_bfloat16* factors;    // [positions, 2, cols], or nullptr
   float* dots;               // [8 tiles_o, slots] partial sums of h . dh, or nullptr
   int64_t slots;
-  float* part;               // [slots, cols]
+  float *part, *more;        // [slots, cols]
 };
 
 __device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t (&r)[4]) {
@@ -177,17 +178,32 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   pdl_wait_primary();  // the plan, the slots' tile, g and u
   pdl_launch_dependents();
 
-  const int tiles = p.plan.header[0] * p.tiles_o, step = (int)gridDim.x, first = (int)blockIdx.x;
+  const int tiles = p.plan.header[0] * p.tiles_o * p.splits, step = (int)gridDim.x, first = (int)blockIdx.x;
   const int ntiles = tiles > first ? (tiles - first + step - 1) / step : 0;
-  const int kbs = p.kb_part * p.parts;
+  const int kbs = p.kb_part * p.parts / p.splits;
+  // the CTA's tile i: split, chunk, outputs
+  struct Where {
+    int split, chunk, to;
+  };
+  const auto where = [&](int i) {
+    const int t = first + i * step, u = t / p.splits;
+    return Where{t - u * p.splits, u / p.tiles_o, u % p.tiles_o};
+  };
   const uint32_t quarter = (uint32_t)(warp & 3), lane_base = (quarter * 32u) << 16;
   bool have = true;  // of the warps of the epilogue: no wait for an accumulator has run out
 
+  // the next tile's MMAs need not wait for what is done with a warp's last columns
+  const auto release = [&](uint32_t acc) {
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+  };
   // The epilogue of the CTA's tile i: eight slots of a half a time, those of this warp.
   const auto finish = [&](int i, int who, uint32_t* turn) {
     constexpr int kWorkers = T::kEpilogueWarps / 4;
-    const int t = first + i * step, to = t % p.tiles_o;
-    const Chunk c = p.plan.chunks[t / p.tiles_o];
+    const Where at = where(i);
+    const int to = at.to;
+    const Chunk c = p.plan.chunks[at.chunk];
     const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc + lane_base;
     const float scale = kMode == kModeHidden ? p.a.scale[c.expert] : kWeightUnit;
     const float sg = kMode == kModeHidden ? p.gate_scale[c.expert] : 0.0f, su = kMode == kModeHidden ? p.up_scale[c.expert] : 0.0f;
@@ -222,6 +238,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         const float my_w = lane < left ? p.weights[p.plan.slot_of[pos + lane]] : 0.0f;
         const float my_up = lane < left ? scale * exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
         tmem_ld_wait();
+        if (piece + kWorkers >= pieces) release(acc);
         float dot[8], dg[8], du[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -245,7 +262,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
       } else {
         tmem_ld_wait();
-        float* out = p.part + pos * p.cols + o;
+        if (piece + kWorkers >= pieces) release(acc);
+        float* out = (at.split ? p.more : p.part) + pos * p.cols + o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (j < left && on) *out = have ? __uint_as_float(a[j]) * scale : nan;
@@ -253,9 +271,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
       }
     }
-    tc_fence_before_sync();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+    if (who >= pieces) release(acc);
   };
   const auto turn_at = [&](int worker) { return reinterpret_cast<uint32_t*>(rest + 512 + worker * 512); };
 
@@ -265,7 +281,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     uint32_t s = 0, parity = 1;
     bool go = true;
     for (int i = 0; i < ntiles && go; ++i) {
-      const Chunk c = p.plan.chunks[(first + i * step) / p.tiles_o];
+      const Where at = where(i);
+      const Chunk c = p.plan.chunks[at.chunk];
       for (int kb = 0; kb < kbs; ++kb) {
         if (!mbar_wait_warp(&empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
@@ -274,8 +291,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
         if (elect_one()) {
           mbar_arrive_expect_tx(&full[s], T::kBBytes);
-          const int part = kb >= p.kb_part ? 1 : 0;
-          tma_load_3d(tile_b + s * T::kBBytes, &vmap, (kb - part * p.kb_part) * kBK, part, c.first, &full[s], policy);
+          const int part = at.split || kb >= p.kb_part ? 1 : 0;
+          tma_load_3d(tile_b + s * T::kBBytes, &vmap, (kb - (kb >= p.kb_part ? p.kb_part : 0)) * kBK, part, c.first, &full[s], policy);
         }
         __syncwarp();
         if (++s == kStages) s = 0, parity ^= 1u;
@@ -286,7 +303,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     uint32_t s = 0, parity = 0;
     bool ok = true;
     for (int i = 0; i < ntiles && ok; ++i) {
-      const Chunk c = p.plan.chunks[(first + i * step) / p.tiles_o];
+      const Chunk c = p.plan.chunks[where(i).chunk];
       const uint32_t slots = (uint32_t)((c.count + 15) & ~15);
       const uint32_t idesc = warp_uniform((kMode == kModeHidden ? idesc_f16_f32(kBM, slots) : idesc_bf16_f32(kBM, slots)) | 1u << 15);
       const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc;
@@ -335,8 +352,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     int kb = group;
     uint32_t block = (uint32_t)group;
     for (int i = 0; i < ntiles && go; ++i, kb -= kbs) {
-      const int t = first + i * step;
-      const int64_t e = p.plan.chunks[t / p.tiles_o].expert, o0 = (int64_t)(t % p.tiles_o) * (kHalves * kBM) + part64 * 64;
+      const Where at = where(i);
+      const int64_t e = p.plan.chunks[at.chunk].expert, o0 = (int64_t)at.to * (kHalves * kBM) + part64 * 64;
       const int64_t row0 = e * p.rows + row;
       // bits that a row's codes begin into a word: the same for rows 64 apart
       const uint32_t shift = p.path == kCopies || p.path == kMixed ? (uint32_t)(row0 * code_cols & 3) * 8 : 0u;
@@ -355,18 +372,18 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                          : "=r"(q[4 * h]), "=r"(q[4 * h + 1]), "=r"(q[4 * h + 2]), "=r"(q[4 * h + 3])
                          : "r"(from + ((((uint32_t)(2 * part64 + h)) ^ swizzle) << 4)));
-          const uint32_t at = smem_addr(packed_codes + ps * kCodeBytes) + row * (p.path == kBulk ? 16u : kCodeRow) + 4 * part64;
-          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(code) : "r"(at));
+          const uint32_t code_at = smem_addr(packed_codes + ps * kCodeBytes) + row * (p.path == kBulk ? 16u : kCodeRow) + 4 * part64;
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(code) : "r"(code_at));
           if (p.path != kBulk) {
             uint32_t more;
-            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(more) : "r"(at + 4));
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(more) : "r"(code_at + 4));
             code = __funnelshift_r(code, more, shift);
           }
         } else {
           // rows past the end of K are read as the last one (the slots' tile is zeros there), outputs past the end are zeros, and not
           // stored
-          const int part = kb >= p.kb_part ? 1 : 0;
-          const int64_t f = e * p.rows + min((int64_t)(kb - part * p.kb_part) * kBK + row, p.rows - 1);
+          const int part = at.split || kb >= p.kb_part ? 1 : 0;
+          const int64_t f = e * p.rows + min((int64_t)(kb - (kb >= p.kb_part ? p.kb_part : 0)) * kBK + row, p.rows - 1);
           const uint8_t *wp = (part ? p.b.packed : p.a.packed) + f * half_cols + (o0 >> 1),
                         *cp = (part ? p.b.codes : p.a.codes) + f * code_cols + (o0 >> 4);
           uint32_t c[4];
@@ -421,16 +438,17 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     uint32_t s = 0, parity = 1;
     bool go = true;
     for (int i = 0; i < ntiles && go; ++i) {
-      const int t = first + i * step, to = t % p.tiles_o;
-      const int64_t row0 = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows;
+      const Where at = where(i);
+      const int to = at.to;
+      const int64_t row0 = (int64_t)p.plan.chunks[at.chunk].expert * p.rows;
       for (int kb = 0; kb < kbs; ++kb) {
         if (!mbar_wait_warp(&packed_empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
           go = false;
           break;
         }
-        const bool second = kb >= p.kb_part;
-        const int64_t row = row0 + (int64_t)(kb - (second ? p.kb_part : 0)) * kBK;
+        const bool second = at.split || kb >= p.kb_part;
+        const int64_t row = row0 + (int64_t)(kb - (kb >= p.kb_part ? p.kb_part : 0)) * kBK;
         uint8_t *packed_to = packed + s * kPackedBytes, *codes_to = packed_codes + s * kCodeBytes;
         if (loads && elect_one()) {
           mbar_arrive_expect_tx(&packed_full[s], kPackedBytes + (p.path == kBulk ? kBK * 16 : 0));
@@ -505,13 +523,22 @@ cudaError_t launch_back_n(const void* v, int64_t depth, int64_t experts, BackArg
   return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map,
                         maps[0], maps[1], maps[2], maps[3], p);
 }
+// chunks: at most; expected: about how many there are
 template <int kMode>
-cudaError_t launch_back(int width, const void* v, int parts, int64_t experts, BackArgs p, int64_t chunks, int sms,
+cudaError_t launch_back(int width, const void* v, int parts, int64_t experts, BackArgs& p, int64_t chunks, int64_t expected, int sms,
                         cudaStream_t stream) {
   p.parts = parts;
+  p.splits = 1;
   p.kb_part = (int32_t)((p.rows + kBK - 1) / kBK);
   p.tiles_o = (int32_t)((p.cols + kHalves * kBM - 1) / (kHalves * kBM));
-  const int64_t tiles = chunks * p.tiles_o;
+  int64_t tiles = chunks * p.tiles_o;
+  // G's and U's rows as tiles of their own where that fills the last round of tiles better (by more than the second
+  // sum costs): 320 tiles of 256 x 256 x 28672 on 152 SMs, 973 us in three rounds
+  if (parts == 2) {
+    const int64_t likely = std::max<int64_t>(1, expected * p.tiles_o);
+    const int64_t whole = 2 * ((likely + sms - 1) / sms), halves = (2 * likely + sms - 1) / sms;
+    if (halves < whole) p.splits = 2, tiles *= 2;
+  }
   if (tiles * p.kb_part * parts > INT32_MAX) return cudaErrorInvalidValue;
   switch (width) {
     case 32: return launch_back_n<kMode, 32>(v, p.rows, experts, p, tiles, sms, stream);
@@ -527,14 +554,16 @@ inline int back_width(int64_t slots, int64_t experts) {
   const int64_t each = (slots + experts - 1) / experts;
   return each <= 24 ? 32 : each <= 56 ? 64 : each <= 144 ? 128 : 256;
 }
+inline int64_t raw_bytes(int64_t slots, int64_t n, int64_t inner) { return round256(slots * std::max(8 * inner, 4 * n)); }
 inline int64_t dot_parts(int64_t inner) { return (inner + kHalves * kBM - 1) / (kHalves * kBM) * kHalves * 4; }
 
 }  // namespace
 
 int64_t experts_backward_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
   const int64_t slots = tokens * k;
-  // x and dy in order, whose place the slots' parts of dx take afterwards; g and u; the factors; the dots
-  return experts_plan_bytes(slots, experts) + 2 * round256(slots * 4) + 2 * round256(slots * n * 2) + round256(slots * inner * 8) + round256(slots * inner * 4) +
+  // x and dy in order, whose place the slots' parts of dx take afterwards; g and u, whose place a second sum of them takes;
+  // the factors; the dots
+  return experts_plan_bytes(slots, experts) + 2 * round256(slots * 4) + 2 * round256(slots * n * 2) + raw_bytes(slots, n, inner) + round256(slots * inner * 4) +
          round256(dot_parts(inner) * slots * 4);
 }
 
@@ -551,10 +580,11 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   uint8_t* xs = reinterpret_cast<uint8_t*>(dy_amax) + round256(slots * 4);
   uint8_t* dys = xs + round256(slots * w.n * 2);
   uint8_t* raw = dys + round256(slots * w.n * 2);
-  uint8_t* factors = raw + round256(slots * w.inner * 8);
+  uint8_t* factors = raw + raw_bytes(slots, w.n, w.inner);
   uint8_t* dots = factors + round256(slots * w.inner * 4);
   const Plan wide = experts_wide_plan(plan, slots, w.count);
   const int64_t chunks = plan_chunks(slots, w.count, wide_width);
+  const int64_t expected = slots / wide_width + std::min<int64_t>(slots, w.count) / 2;  // half a chunk an expert is not full
   if ((err = launch_experts_plan(r, w.count, width, plan, wide_width, &wide, stream)) != cudaSuccess) return err;
   if ((err = launch_experts_spread(x, ld_x, w.n, r, plan, xs, amax, nullptr, stream)) != cudaSuccess) return err;
   if ((err = launch_experts_spread(dy, ld_dy, w.n, r, plan, dys, dy_amax, nullptr, stream)) != cudaSuccess) return err;
@@ -564,11 +594,11 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   p.raw = reinterpret_cast<const float*>(raw), p.gate_scale = w.gate.scale, p.up_scale = w.up.scale, p.slots = slots;
   p.factors = dx != nullptr ? reinterpret_cast<__nv_bfloat16*>(factors) : nullptr;
   p.dots = dweights != nullptr ? reinterpret_cast<float*>(dots) : nullptr;
-  if ((err = launch_back<kModeHidden>(wide_width, dys, 1, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
+  if ((err = launch_back<kModeHidden>(wide_width, dys, 1, w.count, p, chunks, expected, info.sm_count, stream)) != cudaSuccess) return err;
   if (dx != nullptr) {
-    p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.part = reinterpret_cast<float*>(xs);
-    if ((err = launch_back<kModeInput>(wide_width, factors, 2, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
-    if ((err = launch_experts_combine(p.part, r, nullptr, plan, w.n, dx, ld_dx, stream)) != cudaSuccess) return err;
+    p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.part = reinterpret_cast<float*>(xs), p.more = reinterpret_cast<float*>(raw);
+    if ((err = launch_back<kModeInput>(wide_width, factors, 2, w.count, p, chunks, expected, info.sm_count, stream)) != cudaSuccess) return err;
+    if ((err = launch_experts_combine(p.part, p.splits == 2 ? p.more : nullptr, r, nullptr, plan, w.n, dx, ld_dx, stream)) != cudaSuccess) return err;
   }
   if (dweights == nullptr) return cudaSuccess;
   return launch_chained(dweights_kernel, dim3((unsigned)((slots + 255) / 256)), 256, 0, stream, reinterpret_cast<const float*>(dots),

@@ -6,8 +6,10 @@
 // -Inf and NaN are experts that are switched off: never chosen, p = 0.  +Inf counts as the largest finite number.
 //
 // One warp a token, its logits in registers (up to 1024).  A choice is two warp-wide integer reductions: the largest key
-// (a float's bits, ordered as integers) and the lowest index that has it.  Bound by latency: 16384 tokens of 256
-// bf16 logits are 9.4 MB, 1.4 us at the card's bandwidth.  Sums and exponentials are fp32.
+// (a float's bits, ordered as integers) and the lowest index that has it.  Up to 256 bf16 logits go another way: a
+// logit's 16 bits and its index make one word, each lane sorts its eight, and a choice is one reduction over the
+// lanes' first ones (16384 tokens of 256, k 8: 17.5 us before, ROUTE_US now).  Bound by these instructions: the same are
+// 9.4 MB, 1.4 us at the card's bandwidth.  Sums and exponentials are fp32.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -104,6 +106,89 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const T* __restrict__ l
   }
 }
 
+// ---------------------------------------------------------------- up to 256 bf16 logits
+// A logit and its index as one word: larger logits have larger words, of equal ones the lower index; 0: an expert that
+// is off.
+__device__ __forceinline__ uint32_t word_of(uint32_t bits, int e) {
+  if (bits == 0x8000u) bits = 0u;                                      // -0
+  if ((bits & 0x7FFFu) > 0x7F80u || bits == 0xFF80u) return 0u;        // NaN, -Inf
+  const uint32_t key = (bits & 0x8000u) ? ~bits & 0xFFFFu : min(bits, 0x7F7Fu) | 0x8000u;
+  return key << 16 | (uint32_t)(0xFFFF - e);
+}
+__device__ __forceinline__ float value_of_word(uint32_t w) {
+  const uint32_t key = w >> 16;
+  return __uint_as_float((key & 0x8000u ? key & 0x7FFFu : ~key & 0xFFFFu) << 16);
+}
+__device__ __forceinline__ void order(uint32_t& a, uint32_t& b) {  // the larger first
+  const uint32_t hi = max(a, b), lo = min(a, b);
+  a = hi, b = lo;
+}
+template <int kPer>
+__device__ __forceinline__ void sort_words(uint32_t (&w)[kPer]) {
+  if constexpr (kPer == 2) order(w[0], w[1]);
+  if constexpr (kPer >= 4) {
+#pragma unroll
+    for (int o = 0; o < kPer; o += 4) {
+      order(w[o], w[o + 1]), order(w[o + 2], w[o + 3]);
+      order(w[o], w[o + 2]), order(w[o + 1], w[o + 3]);
+      order(w[o + 1], w[o + 2]);
+    }
+  }
+  if constexpr (kPer == 8) {  // two sorted fours merged (odd-even)
+    order(w[0], w[4]), order(w[1], w[5]), order(w[2], w[6]), order(w[3], w[7]);
+    order(w[2], w[4]), order(w[3], w[5]);
+    order(w[1], w[2]), order(w[3], w[4]), order(w[5], w[6]);
+  }
+}
+
+template <int kPer>
+__global__ void __launch_bounds__(kThreads) route_words_kernel(const uint16_t* __restrict__ logits, int64_t tokens, int experts,
+                                                               int64_t ld, int k, bool renormalize, int32_t* __restrict__ ids,
+                                                               float* __restrict__ weights) {
+  const int64_t t = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (t >= tokens) return;
+  const uint16_t* row = logits + t * ld;
+  uint32_t w[kPer];
+  const int e0 = lane * kPer;
+  if (kPer == 8 && (reinterpret_cast<uintptr_t>(row) & 15) == 0 && e0 + 8 <= experts) {
+    const uint4 v = *reinterpret_cast<const uint4*>(row + e0);
+    const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) w[i] = word_of((q[i / 2] >> (16 * (i & 1))) & 0xFFFFu, e0 + i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) w[i] = e0 + i < experts ? word_of(row[e0 + i], e0 + i) : 0u;
+  }
+  sort_words<kPer>(w);
+  uint32_t mine = 0u;  // lane j: the j-th choice
+  float top = 0.0f, total = 0.0f;
+  for (int j = 0; j < k; ++j) {
+    const uint32_t best = __reduce_max_sync(kAll, w[0]);
+    if (j == 0) {
+      top = value_of_word(best);
+      if (!renormalize) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) s += w[i] ? expf(value_of_word(w[i]) - top) : 0.0f;
+        total = warp_sum(s);
+      }
+    }
+    if (best == 0u) break;  // no expert is left
+    if (lane == j) mine = best;
+    const bool taken = w[0] == best;
+#pragma unroll
+    for (int i = 0; i + 1 < kPer; ++i) w[i] = taken ? w[i + 1] : w[i];
+    w[kPer - 1] = taken ? 0u : w[kPer - 1];
+  }
+  const float p = mine ? expf(value_of_word(mine) - top) : 0.0f;
+  if (renormalize) total = warp_sum(p);
+  if (lane < k) {
+    ids[t * k + lane] = mine ? 0xFFFF - (int)(mine & 0xFFFFu) : -1;
+    weights[t * k + lane] = mine ? p / total : 0.0f;
+  }
+}
+
 template <typename T, int kPer>
 __global__ void __launch_bounds__(kThreads)
 route_backward_kernel(const T* logits, int64_t tokens, int experts, int64_t ld, const int32_t* __restrict__ ids,
@@ -161,6 +246,13 @@ cudaError_t launch(const void* logits, int64_t tokens, int64_t experts, int64_t 
                    const float* dweights, int64_t k, bool renormalize, int32_t* ids, float* weights, void* dlogits,
                    int64_t ld_out, cudaStream_t stream) {
   const unsigned grid = (unsigned)((tokens + kWarps - 1) / kWarps);
+  if constexpr (kPer <= 8 && sizeof(T) == 2) {
+    if (dlogits == nullptr) {
+      route_words_kernel<kPer><<<grid, kThreads, 0, stream>>>(static_cast<const uint16_t*>(logits), tokens, (int)experts, ld, (int)k,
+                                                              renormalize, ids, weights);
+      return cudaGetLastError();
+    }
+  }
   if (dlogits == nullptr)
     route_kernel<T, kPer><<<grid, kThreads, 0, stream>>>(static_cast<const T*>(logits), tokens, (int)experts, ld, (int)k,
                                                          renormalize, ids, weights);
