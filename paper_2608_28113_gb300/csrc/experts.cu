@@ -206,15 +206,15 @@ constexpr int kModeHidden = 0, kModeRaw = 1, kModeDown = 2;
 constexpr int kQuad = 4;
 constexpr uint32_t kRowBytes = kPackedRow;
 static_assert(kRowBytes == kQuad * kBK / 2, "a packed stage's rows");
-constexpr uint32_t kHalfBytes = kBM * kRowBytes, kHalfCodes = kBM * kCodeRow;
+constexpr uint32_t kHalfBytes = kBM * kPairRow, kHalfCodes = kBM * kCodeRow;
 constexpr uint32_t kPackedBytes = kHalves * (kHalfBytes + kHalfCodes);
 
 template <int kN>
 struct Tile {
-  static constexpr int kStages = kN <= 32 ? 6 : 4;  // unpacked blocks and blocks of the slots' tile
+  static constexpr int kStages = 4;  // unpacked blocks and blocks of the slots' tile
   static constexpr int kAccs = kN <= 64 ? 2 : 1;
   static constexpr bool kHelp = kAccs == 1;  // the unpacking warps take part in the epilogue
-  static constexpr int kPackedStages = kN <= 64 ? 5 : 3;
+  static constexpr int kPackedStages = kN <= 32 ? 5 : kN == 64 ? 4 : 3;
   static constexpr int kEpilogueWarps = kHelp ? 4 + kUnpackWarps : 4;
   static constexpr uint32_t kBBytes = kN * kBK * 2;
   static constexpr uint32_t kTurnBytes = kEpilogueWarps * 1024;
@@ -286,7 +286,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       mbar_init(&empty[s], 1);
     }
     for (int s = 0; s < kPackedStages; ++s) {
-      mbar_init(&packed_full[s], (p.path == kCopies || p.path == kMixed ? 2 * 32 : 0) + (p.path >= kMixed ? 1 : 0));
+      mbar_init(&packed_full[s], (p.path == kBulk ? 0 : 2 * 32) + (p.path >= kMixed ? 1 : 0));
       mbar_init(&packed_empty[s], kUnpackWarps);
     }
     for (int i = 0; i < kAccs; ++i) {
@@ -484,7 +484,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     const ExpertMatrix& w = half ? p.b : p.a;
     const int64_t cols = p.cols, half_cols = cols >> 1, code_cols = cols >> 4;
     const int row_in_tile = row_in_half + (kMode == kModeDown && half ? kBM : 0);
-    const uint32_t src = smem_addr(packed + half * kHalfBytes + row_in_half * kRowBytes), swizzle = (uint32_t)row_in_half & 7u;
+    const uint32_t src = smem_addr(packed + half * kHalfBytes);
     const uint32_t code_src = smem_addr(packed_codes + half * kHalfCodes);
     uint32_t* turn = turn_at(T::kHelp ? 4 + warp - kUnpackWarp0 : 0);
     bool go = true;
@@ -532,12 +532,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           if (kb >= kbs || !go) break;
           uint32_t q[8];
           if (p.path != kDirect) {
-            const uint32_t from = src + stage * (kHalves * kHalfBytes);
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                           : "=r"(q[4 * e]), "=r"(q[4 * e + 1]), "=r"(q[4 * e + 2]), "=r"(q[4 * e + 3])
-                           : "r"(from + ((((uint32_t)(2 * in_quad + e)) ^ swizzle) << 4)));
+            read_packed(q, src + stage * (kHalves * kHalfBytes), row_in_half, kBM, 2 * in_quad, p.path == kPairs);
           } else {
             // blocks past the end of K are zeros; so is the slots' tile there
             const uint8_t *wp = w.packed + row * half_cols + ((int64_t)kb << 5), *cp = w.codes + row * code_cols + ((int64_t)kb << 2);
@@ -611,9 +606,19 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
         uint8_t *to = packed + s * (kHalves * kHalfBytes), *codes_to = packed_codes + s * (kHalves * kHalfCodes);
         if (loads && elect_one()) {
-          mbar_arrive_expect_tx(&packed_full[s], kHalves * (kHalfBytes + (p.path == kBulk ? kBM * 16 : 0)));
-          tma_load_2d(to, &amap, quad * (int)kRowBytes, (int)row_a, &packed_full[s], policy);
-          tma_load_2d(to + kHalfBytes, &bmap, quad * (int)kRowBytes, (int)row_b, &packed_full[s], policy);
+          if (p.path == kPairs) {
+            // the even rows of each half, then the odd ones, which begin row_bytes further
+            const int x = quad * (int)kRowBytes, odd_x = (int)(p.cols >> 1) - 8 + x;
+            mbar_arrive_expect_tx(&packed_full[s], kHalves * kBM * kPairRow);
+            tma_load_2d(to, &amap, x, (int)(row_a >> 1), &packed_full[s], policy);
+            tma_load_2d(to + kHalfBytes / 2, &amap, odd_x, (int)(row_a >> 1), &packed_full[s], policy);
+            tma_load_2d(to + kHalfBytes, &bmap, x, (int)(row_b >> 1), &packed_full[s], policy);
+            tma_load_2d(to + kHalfBytes + kHalfBytes / 2, &bmap, odd_x, (int)(row_b >> 1), &packed_full[s], policy);
+          } else {
+            mbar_arrive_expect_tx(&packed_full[s], kHalves * kBM * (kRowBytes + (p.path == kBulk ? 16 : 0)));
+            tma_load_2d(to, &amap, quad * (int)kRowBytes, (int)row_a, &packed_full[s], policy);
+            tma_load_2d(to + kHalfBytes, &bmap, quad * (int)kRowBytes, (int)row_b, &packed_full[s], policy);
+          }
           if (p.path == kBulk) {
             tma_load_2d(codes_to, &acodes, quad * 16, (int)row_a, &packed_full[s], policy);
             tma_load_2d(codes_to + kHalfCodes, &bcodes, quad * 16, (int)row_b, &packed_full[s], policy);
@@ -665,8 +670,11 @@ cudaError_t launch_gemm_n(const void* v, int64_t slots, int64_t experts, GemmArg
   p.path = packed_path(p.a, p.b, p.cols, p.all_rows);
   CUtensorMap maps[4] = {map, map, map, map};
   if (p.path >= kMixed) {
-    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, kRowBytes, kBM)) != cudaSuccess) return err;
-    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, kRowBytes, kBM)) != cudaSuccess) return err;
+    const bool pairs = p.path == kPairs;
+    const int64_t bytes = pairs ? p.cols : p.cols / 2, rows = pairs ? p.all_rows / 2 : p.all_rows;
+    const uint32_t width = pairs ? kPairRow : kRowBytes, height = pairs ? kBM / 2 : kBM;
+    if ((err = bytes_map(&maps[0], p.a.packed, bytes, rows, width, height)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[1], p.b.packed, bytes, rows, width, height)) != cudaSuccess) return err;
   }
   if (p.path == kBulk) {
     if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16, kBM)) != cudaSuccess) return err;

@@ -78,11 +78,33 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// How a product's packed weights come: read where they are unpacked (codes at an odd address), by two warps'
-// asynchronous copies (rows that TMA cannot have: they want whole 16 bytes), the codes that way and the rest by TMA, all
-// by TMA.  The copies of everything had 16 tokens of 64 experts, 4096 x 2048, take 2.3 times as long as TMA.
-constexpr int kDirect = 0, kCopies = 1, kMixed = 2, kBulk = 3;
-constexpr uint32_t kPackedRow = 128, kCodeRow = 20;  // bytes of a row in a stage: 256 weights, and their codes' words
+// How a product's packed weights come to shared memory, a row's 128 bytes (256 weights) a stage:
+//   kBulk    by TMA, their codes too (rows of codes of whole 16 bytes);
+//   kMixed   by TMA, the codes by two warps' asynchronous copies;
+//   kPairs   as kMixed, where a row is 8 bytes more than whole 16s, which TMA cannot step by: two rows are one of its
+//            rows.  The odd ones begin 8 bytes into a piece of 16: their boxes begin 8 bytes earlier, and all are 144 wide;
+//   kCopies  by the two warps' copies too (weights at an address of 8 bytes);
+//   kDirect  not at all, they are read where they are unpacked (codes at an odd address).
+// 16 tokens of 64 experts, 4096 x 2048, first product: 101 us, 118 (kMixed), 184 (kCopies).
+constexpr int kDirect = 0, kCopies = 1, kMixed = 2, kPairs = 3, kBulk = 4;
+constexpr uint32_t kPackedRow = 128, kPairRow = 144, kCodeRow = 20;  // bytes of a row in a stage, and its codes' words
+
+// A lane's 32 bytes, the 16-byte pieces `piece` and `piece` + 1 of row `row` of `rows` (swizzled as TMA does; pairs: even
+// rows first).
+__device__ __forceinline__ void read_packed(uint32_t (&q)[8], uint32_t stage, int row, int rows, int piece, bool pairs) {
+  if (!pairs) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(q[4 * e]), "=r"(q[4 * e + 1]), "=r"(q[4 * e + 2]), "=r"(q[4 * e + 3])
+                   : "r"(stage + (uint32_t)row * kPackedRow + ((((uint32_t)(piece + e)) ^ ((uint32_t)row & 7u)) << 4)));
+  } else {
+    const uint32_t from = stage + (uint32_t)((row & 1) * (rows >> 1) + (row >> 1)) * kPairRow + (row & 1) * 8 + piece * 16;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(q[2 * e]), "=r"(q[2 * e + 1]) : "r"(from + 8 * e));
+  }
+}
 
 // kRows rows of 128 bytes, from byte `from` of row `row` on, to rows first, first + 1, ... of a stage whose 16-byte
 // pieces are swizzled as TMA does.  By a warp, 8 bytes a lane; first % 8 == 0.  Bytes past a row's end are zeros.
@@ -151,7 +173,8 @@ inline int packed_path(const ExpertMatrix& a, const ExpertMatrix& b, int64_t col
     return reinterpret_cast<uintptr_t>(p) % n == 0 && reinterpret_cast<uintptr_t>(q) % n == 0;
   };
   if (!both(a.codes, b.codes, 4)) return kDirect;
-  if (cols % 32 != 0 || !both(a.packed, b.packed, 16) || all_rows > INT32_MAX - 512) return kCopies;
+  if (!both(a.packed, b.packed, 16) || all_rows > INT32_MAX - 512) return kCopies;
+  if (cols % 32 != 0) return kPairs;
   return cols % 256 == 0 && both(a.codes, b.codes, 16) ? kBulk : kMixed;
 }
 

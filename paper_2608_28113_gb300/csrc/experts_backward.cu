@@ -38,7 +38,7 @@ constexpr uint32_t kHalfBytes = 2 * kGroupBytes;
 // as whole words from any address).
 constexpr uint32_t kRowBytes = kPackedRow;
 static_assert(kRowBytes == kHalves * kBM / 2, "a packed stage's rows");
-constexpr uint32_t kPackedBytes = kBK * kRowBytes, kCodeBytes = kBK * kCodeRow;
+constexpr uint32_t kPackedBytes = kBK * kPairRow, kCodeBytes = kBK * kCodeRow;
 
 template <int kN>
 struct Tile {
@@ -153,7 +153,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       mbar_init(&empty[s], 1);
     }
     for (int s = 0; s < kPackedStages; ++s) {
-      mbar_init(&packed_full[s], (p.path == kCopies || p.path == kMixed ? 2 * 32 : 0) + (p.path >= kMixed ? 1 : 0));
+      mbar_init(&packed_full[s], (p.path == kBulk ? 0 : 2 * 32) + (p.path >= kMixed ? 1 : 0));
       mbar_init(&packed_empty[s], kUnpackWarps / 2);
     }
     for (int i = 0; i < kAccs; ++i) {
@@ -345,7 +345,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     // group: every other K block; a thread: 64 outputs (`part64` of four) of one row of K
     const int group = (warp - kUnpackWarp0) >> 3, line = ((warp - kUnpackWarp0) & 7) * 32 + lane, row = line & 63, part64 = line >> 6;
     const int64_t cols = p.cols, half_cols = cols >> 1, code_cols = cols >> 4;
-    const uint32_t swizzle = (uint32_t)row & 7u;
+    const uint32_t swizzle = (uint32_t)row & 7u;  // of the unpacked tile
     uint32_t* turn = turn_at(T::kHelp ? 4 + warp - kUnpackWarp0 : 0);
     bool go = true;
     // blocks of all tiles, one after another: this group's are group, group + 2, ...
@@ -356,7 +356,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       const int64_t e = p.plan.chunks[at.chunk].expert, o0 = (int64_t)at.to * (kHalves * kBM) + part64 * 64;
       const int64_t row0 = e * p.rows + row;
       // bits that a row's codes begin into a word: the same for rows 64 apart
-      const uint32_t shift = p.path == kCopies || p.path == kMixed ? (uint32_t)(row0 * code_cols & 3) * 8 : 0u;
+      const uint32_t shift = p.path != kDirect && p.path != kBulk ? (uint32_t)(row0 * code_cols & 3) * 8 : 0u;
       int done = 0;
       for (; kb < kbs && go; kb += 2, block += 2) {
         const uint32_t ps = block % kPackedStages, parity_p = (block / kPackedStages) & 1u;
@@ -366,12 +366,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
             go = false;
             break;
           }
-          const uint32_t from = smem_addr(packed + ps * kPackedBytes + row * kRowBytes);
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(q[4 * h]), "=r"(q[4 * h + 1]), "=r"(q[4 * h + 2]), "=r"(q[4 * h + 3])
-                         : "r"(from + ((((uint32_t)(2 * part64 + h)) ^ swizzle) << 4)));
+          read_packed(q, smem_addr(packed + ps * kPackedBytes), row, kBK, 2 * part64, p.path == kPairs);
           const uint32_t code_at = smem_addr(packed_codes + ps * kCodeBytes) + row * (p.path == kBulk ? 16u : kCodeRow) + 4 * part64;
           asm volatile("ld.shared.u32 %0, [%1];" : "=r"(code) : "r"(code_at));
           if (p.path != kBulk) {
@@ -451,8 +446,16 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         const int64_t row = row0 + (int64_t)(kb - (kb >= p.kb_part ? p.kb_part : 0)) * kBK;
         uint8_t *packed_to = packed + s * kPackedBytes, *codes_to = packed_codes + s * kCodeBytes;
         if (loads && elect_one()) {
-          mbar_arrive_expect_tx(&packed_full[s], kPackedBytes + (p.path == kBulk ? kBK * 16 : 0));
-          tma_load_2d(packed_to, second ? &bmap : &amap, to * (int)kRowBytes, (int)row, &packed_full[s], policy);
+          const CUtensorMap* map = second ? &bmap : &amap;
+          if (p.path == kPairs) {
+            // the even rows, then the odd ones, which begin row_bytes further
+            mbar_arrive_expect_tx(&packed_full[s], kBK * kPairRow);
+            tma_load_2d(packed_to, map, to * (int)kRowBytes, (int)(row >> 1), &packed_full[s], policy);
+            tma_load_2d(packed_to + kPackedBytes / 2, map, (int)(p.cols >> 1) - 8 + to * (int)kRowBytes, (int)(row >> 1), &packed_full[s], policy);
+          } else {
+            mbar_arrive_expect_tx(&packed_full[s], kBK * (kRowBytes + (p.path == kBulk ? 16 : 0)));
+            tma_load_2d(packed_to, map, to * (int)kRowBytes, (int)row, &packed_full[s], policy);
+          }
           if (p.path == kBulk) tma_load_2d(codes_to, second ? &bcodes : &acodes, to * 16, (int)row, &packed_full[s], policy);
         }
         __syncwarp();
@@ -510,8 +513,11 @@ cudaError_t launch_back_n(const void* v, int64_t depth, int64_t experts, BackArg
   p.path = packed_path(p.a, p.b, p.cols, p.all_rows);
   CUtensorMap maps[4] = {map, map, map, map};
   if (p.path >= kMixed) {
-    if ((err = bytes_map(&maps[0], p.a.packed, p.cols / 2, p.all_rows, kRowBytes, kBK)) != cudaSuccess) return err;
-    if ((err = bytes_map(&maps[1], p.b.packed, p.cols / 2, p.all_rows, kRowBytes, kBK)) != cudaSuccess) return err;
+    const bool pairs = p.path == kPairs;
+    const int64_t bytes = pairs ? p.cols : p.cols / 2, rows = pairs ? p.all_rows / 2 : p.all_rows;
+    const uint32_t width = pairs ? kPairRow : kRowBytes, height = pairs ? kBK / 2 : kBK;
+    if ((err = bytes_map(&maps[0], p.a.packed, bytes, rows, width, height)) != cudaSuccess) return err;
+    if ((err = bytes_map(&maps[1], p.b.packed, bytes, rows, width, height)) != cudaSuccess) return err;
   }
   if (p.path == kBulk) {
     if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16, kBK)) != cudaSuccess) return err;

@@ -179,7 +179,7 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
 // amax, contiguous); g and u of each position (fp32 [positions, 2, inner]); a token's slots' rows (fp32, contiguous; and those of
 // `more`, or nullptr) times their weights (nullptr: 1) added up.
 int experts_width(int64_t slots, int64_t experts);
-// Bytes [rows, bytes] in TMA boxes of width (128: swizzled, or 16) x height.
+// Bytes [rows, bytes] in TMA boxes of width (128: swizzled) x height.
 cudaError_t bytes_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t rows, uint32_t width, uint32_t height);
 int64_t experts_plan_bytes(int64_t slots, int64_t experts);
 Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts);
