@@ -211,10 +211,10 @@ constexpr uint32_t kPackedBytes = kHalves * (kHalfBytes + kHalfCodes);
 
 template <int kN>
 struct Tile {
-  static constexpr int kStages = 4;  // unpacked blocks and blocks of the slots' tile
+  static constexpr int kStages = kN <= 32 ? 6 : 4;  // unpacked blocks and blocks of the slots' tile
   static constexpr int kAccs = kN <= 64 ? 2 : 1;
   static constexpr bool kHelp = kAccs == 1;  // the unpacking warps take part in the epilogue
-  static constexpr int kPackedStages = kN <= 32 ? 5 : kN == 64 ? 4 : 3;
+  static constexpr int kPackedStages = kN == 16 ? 5 : kN <= 64 ? 4 : 3;
   static constexpr int kEpilogueWarps = kHelp ? 4 + kUnpackWarps : 4;
   static constexpr uint32_t kBBytes = kN * kBK * 2;
   static constexpr uint32_t kTurnBytes = kEpilogueWarps * 1024;
@@ -257,7 +257,9 @@ __device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_
       : "memory");
 }
 
-template <int kMode, int kN>
+// kPath: how the packed rows are read: kBulk, kMixed (kCopies too), kPairs or kDirect.  (A branch on it in the unpacking
+// cost a decoding batch 7%.)
+template <int kMode, int kN, int kPath>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
             const __grid_constant__ CUtensorMap acodes, const __grid_constant__ CUtensorMap bcodes, const __grid_constant__ GemmArgs p) {
@@ -488,20 +490,23 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     const uint32_t code_src = smem_addr(packed_codes + half * kHalfCodes);
     uint32_t* turn = turn_at(T::kHelp ? 4 + warp - kUnpackWarp0 : 0);
     bool go = true;
-    uint32_t stage = 0, parity_p = 0, block0 = 0;  // block0: of the tile's first K block
-    for (int i = 0; i < ntiles; ++i, block0 += (uint32_t)kbs) {
+    // the packed stage that is read next; the stage of unpacked blocks that this group writes next
+    uint32_t stage = 0, parity_p = 0, slot = (uint32_t)odd, parity = 1;
+    const uint32_t tmem_a = tmem + T::kA0 + (uint32_t)half * (kBK / 2) + lane_base;
+    for (int i = 0; i < ntiles && go; ++i) {
       int64_t row = 0;
       uint32_t shift = 0;  // bits that a row's codes begin into a word
-      if (p.path != kBulk) {
+      if constexpr (kPath != kBulk) {
         // rows past the end are read as the last one, or as what is behind it, and not stored
         const int t = first + i * step;
         const int64_t in_tile = (int64_t)(t % p.tiles_o) * p.tile_rows + row_in_tile;
         row = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows;
-        if (p.path != kDirect)
+        if (kPath != kDirect)
           shift = (uint32_t)((row + in_tile) * code_cols & 3) * 8;
         else
           row += min(in_tile, p.rows - 1);
       }
+      int kb = odd;
       for (int quad = 0; quad < quads && go; ++quad) {
         Finish f;
         if (T::kHelp && quad == 0 && i > 0) {
@@ -509,18 +514,18 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           f = prepare(i - 1, 1 + group);
         }
         uint32_t code[2] = {0u, 0u};
-        if (p.path != kDirect) {
+        const uint32_t from = src + stage * (kHalves * kHalfBytes);
+        if constexpr (kPath != kDirect) {
           if (!mbar_wait_warp(&packed_full[stage], parity_p)) {
             go = false;
             break;
           }
-          const uint32_t at = code_src + stage * (kHalves * kHalfCodes) + row_in_half * (p.path == kBulk ? 16u : kCodeRow);
-          if (p.path == kBulk) {
-            uint32_t c[4];
+          const uint32_t at = code_src + stage * (kHalves * kHalfCodes) + row_in_half * (kPath == kBulk ? 16u : kCodeRow);
+          uint32_t c[4];
+          if constexpr (kPath == kBulk) {
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]) : "r"(at));
             code[0] = odd ? c[1] : c[0], code[1] = odd ? c[3] : c[2];
           } else {
-            uint32_t c[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(c[e]) : "r"(at + 4 * (odd + e)));
             code[0] = __funnelshift_r(c[0], c[1], shift), code[1] = __funnelshift_r(c[2], c[3], shift);
@@ -528,11 +533,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const int in_quad = odd + 2 * u, kb = kQuad * quad + in_quad;
           if (kb >= kbs || !go) break;
           uint32_t q[8];
-          if (p.path != kDirect) {
-            read_packed(q, src + stage * (kHalves * kHalfBytes), row_in_half, kBM, 2 * in_quad, p.path == kPairs);
+          if constexpr (kPath != kDirect) {
+            read_packed(q, from, row_in_half, kBM, 2 * (odd + 2 * u), kPath == kPairs);
           } else {
             // blocks past the end of K are zeros; so is the slots' tile there
             const uint8_t *wp = w.packed + row * half_cols + ((int64_t)kb << 5), *cp = w.codes + row * code_cols + ((int64_t)kb << 2);
@@ -546,13 +550,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
             }
             code[u] = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
           }
-          const uint32_t block = block0 + (uint32_t)kb, s = block % kStages;
-          if (!mbar_wait_warp(&empty[s], ((block / kStages) & 1u) ^ 1u)) {
+          if (!mbar_wait_warp(&empty[slot], parity)) {
             go = false;
             break;
           }
           tc_fence_after_sync();
-          const uint32_t dst = tmem + T::kA0 + s * T::kAStage + (uint32_t)half * (kBK / 2) + lane_base;
+          const uint32_t dst = tmem_a + slot * T::kAStage;
           uint32_t ca, cb;
           codes_f16(code[u], ca, cb);
 #pragma unroll
@@ -565,9 +568,14 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           tmem_st_wait();
           tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&full[s]);
+          if (lane == 0) mbar_arrive(&full[slot]);
+          // this group's next block, two further, or in the next tile
+          const int ahead = kb + 2 < kbs ? 2 : kbs - kb + odd;
+          kb += 2;
+          slot += (uint32_t)ahead;
+          while (slot >= kStages) slot -= kStages, parity ^= 1u;
         }
-        if (p.path != kDirect && go) {
+        if (kPath != kDirect && go) {
           // only now have the loads' values been used: an arrival does not wait for loads still under way (one right behind
           // them had TMA overwrite rows that were being read)
           __syncwarp();
@@ -576,6 +584,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
         // the tile before, once this one's first blocks are there for the MMAs
         if (T::kHelp && quad == 0 && i > 0) finish(i - 1, 1 + group, turn, f);
+      }
+      if (odd >= kbs) {  // a tile of one block has none for the odd groups
+        slot += (uint32_t)kbs;
+        while (slot >= kStages) slot -= kStages, parity ^= 1u;
       }
     }
     if (T::kHelp && ntiles == 1) pdl_wait_primary();
@@ -606,7 +618,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
         uint8_t *to = packed + s * (kHalves * kHalfBytes), *codes_to = packed_codes + s * (kHalves * kHalfCodes);
         if (loads && elect_one()) {
-          if (p.path == kPairs) {
+          if (kPath == kPairs) {
             // the even rows of each half, then the odd ones, which begin row_bytes further
             const int x = quad * (int)kRowBytes, odd_x = (int)(p.cols >> 1) - 8 + x;
             mbar_arrive_expect_tx(&packed_full[s], kHalves * kBM * kPairRow);
@@ -680,11 +692,18 @@ cudaError_t launch_gemm_n(const void* v, int64_t slots, int64_t experts, GemmArg
     if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16, kBM)) != cudaSuccess) return err;
     if ((err = bytes_map(&maps[3], p.b.codes, p.cols / 16, p.all_rows, 16, kBM)) != cudaSuccess) return err;
   }
-  auto kernel = gemm_kernel<kMode, kN>;
-  err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)Tile<kN>::kSmemBytes);
-  if (err != cudaSuccess) return err;
-  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map,
-                        maps[0], maps[1], maps[2], maps[3], p);
+  const auto launch = [&](auto kernel) {
+    const cudaError_t set = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)Tile<kN>::kSmemBytes);
+    if (set != cudaSuccess) return set;
+    return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map,
+                          maps[0], maps[1], maps[2], maps[3], p);
+  };
+  switch (p.path) {
+    case kBulk: return launch(gemm_kernel<kMode, kN, kBulk>);
+    case kPairs: return launch(gemm_kernel<kMode, kN, kPairs>);
+    case kDirect: return launch(gemm_kernel<kMode, kN, kDirect>);
+    default: return launch(gemm_kernel<kMode, kN, kMixed>);
+  }
 }
 template <int kMode>
 cudaError_t launch_gemm(int width, const void* v, int64_t slots, int64_t experts, GemmArgs p, int64_t chunks, int sms,

@@ -123,7 +123,7 @@ __device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[
                : "memory");
 }
 
-template <int kMode, int kN>
+template <int kMode, int kN, bool kPairRows>
 __global__ void __launch_bounds__(kThreads, 1)
 back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
             const __grid_constant__ CUtensorMap acodes, const __grid_constant__ CUtensorMap bcodes, const __grid_constant__ BackArgs p) {
@@ -366,7 +366,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
             go = false;
             break;
           }
-          read_packed(q, smem_addr(packed + ps * kPackedBytes), row, kBK, 2 * part64, p.path == kPairs);
+          read_packed(q, smem_addr(packed + ps * kPackedBytes), row, kBK, 2 * part64, kPairRows);
           const uint32_t code_at = smem_addr(packed_codes + ps * kCodeBytes) + row * (p.path == kBulk ? 16u : kCodeRow) + 4 * part64;
           asm volatile("ld.shared.u32 %0, [%1];" : "=r"(code) : "r"(code_at));
           if (p.path != kBulk) {
@@ -447,7 +447,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         uint8_t *packed_to = packed + s * kPackedBytes, *codes_to = packed_codes + s * kCodeBytes;
         if (loads && elect_one()) {
           const CUtensorMap* map = second ? &bmap : &amap;
-          if (p.path == kPairs) {
+          if (kPairRows) {
             // the even rows, then the odd ones, which begin row_bytes further
             mbar_arrive_expect_tx(&packed_full[s], kBK * kPairRow);
             tma_load_2d(packed_to, map, to * (int)kRowBytes, (int)(row >> 1), &packed_full[s], policy);
@@ -523,11 +523,13 @@ cudaError_t launch_back_n(const void* v, int64_t depth, int64_t experts, BackArg
     if ((err = bytes_map(&maps[2], p.a.codes, p.cols / 16, p.all_rows, 16, kBK)) != cudaSuccess) return err;
     if ((err = bytes_map(&maps[3], p.b.codes, p.cols / 16, p.all_rows, 16, kBK)) != cudaSuccess) return err;
   }
-  auto kernel = back_kernel<kMode, kN>;
-  err = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)Tile<kN>::kSmemBytes);
-  if (err != cudaSuccess) return err;
-  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map,
-                        maps[0], maps[1], maps[2], maps[3], p);
+  const auto launch = [&](auto kernel) {
+    const cudaError_t set = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), (int)Tile<kN>::kSmemBytes);
+    if (set != cudaSuccess) return set;
+    return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(most_tiles, sms)), kThreads, (int)Tile<kN>::kSmemBytes, stream, map,
+                          maps[0], maps[1], maps[2], maps[3], p);
+  };
+  return p.path == kPairs ? launch(back_kernel<kMode, kN, true>) : launch(back_kernel<kMode, kN, false>);
 }
 // chunks: at most; expected: about how many there are
 template <int kMode>
