@@ -36,17 +36,77 @@ constexpr int kSpreadKept = 4;  // 16-byte pieces of a row that a thread keeps i
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
 constexpr int kPlanAhead = 8;  // ids a lane has in flight: one at a time, 32768 slots took 56 us
 
-// A stable counting sort by one CTA: each warp counts a run of slots, the warps' counts are summed up expert by
-// expert, and each warp then places its run.  Integers only: equal calls give equal plans.
+constexpr int64_t kPlanSlots = 4096;  // of a CTA, where there are more
+
+// An expert's chunks: nearly the same size, whole 16s.
+__device__ __forceinline__ void cut(int expert, int first, int total, int pieces, Chunk* to) {
+  const int each = pieces ? ((total + pieces - 1) / pieces + 15) / 16 * 16 : 0;
+  for (int c = 0; c < pieces; ++c) {
+    const int from = min(total, c * each), end = min(total, from + each);
+    to[c] = {expert, first + from, end - from, 0};
+  }
+}
+
+// The slots of each expert in each run of kPlanSlots slots: counts [runs][experts].
+__global__ void __launch_bounds__(kPlanThreads) count_kernel(const int32_t* __restrict__ ids, int64_t slots, int experts,
+                                                             int32_t* __restrict__ counts) {
+  __shared__ int32_t mine[kRouteExperts];
+  pdl_launch_dependents();
+  for (int e = threadIdx.x; e < experts; e += kPlanThreads) mine[e] = 0;
+  __syncthreads();
+  const int64_t s0 = (int64_t)blockIdx.x * kPlanSlots, s1 = min(slots, s0 + kPlanSlots);
+  for (int64_t s = s0 + threadIdx.x; s < s1; s += kPlanThreads) {
+    const int id = ids[s];
+    if ((unsigned)id < (unsigned)experts) atomicAdd(&mine[id], 1);  // whole numbers
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < experts; e += kPlanThreads) counts[(int64_t)blockIdx.x * experts + e] = mine[e];
+}
+
+// A stable counting sort: each warp counts a run of slots, the warps' counts are summed up expert by expert, and each
+// warp then places its run.  By one CTA, or a CTA for each run of count_kernel's (run_counts; one CTA alone took 32768 slots 36 us).
+// Integers only: equal calls give equal plans.
 // wide: chunks of another width over the same positions (its chunks and their number alone; nullptr: none).
-__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __restrict__ ids, int64_t slots, int experts, int width,
-                                                            Plan plan, int wide_width, Plan wide) {
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* ids, int64_t slots, int experts, int width, Plan plan,
+                                                            int wide_width, Plan wide, const int32_t* run_counts) {
   extern __shared__ int32_t counts[];  // [kPlanWarps][experts], then each expert's first position
   int32_t* first = counts + kPlanWarps * experts;
   __shared__ int32_t warp_total[kPlanWarps], warp_chunks[kPlanWarps], warp_wide[kPlanWarps];
+  if (run_counts != nullptr) pdl_wait_primary();
   pdl_launch_dependents();
+  if (slots <= 32) {
+    // a warp's: an expert's place by the slots of lower ones
+    if (threadIdx.x >= 32) return;
+    const int lane = threadIdx.x, id = lane < slots ? ids[lane] : -1;
+    const bool on = (unsigned)id < (unsigned)experts;
+    const uint32_t alike = __match_any_sync(0xFFFFFFFFu, on ? id : -1), below = (1u << lane) - 1u;
+    const bool leads = on && (alike & below) == 0u;
+    const int total = __popc(alike), pieces = leads ? (total + width - 1) / width : 0;
+    const int wide_pieces = leads ? (total + wide_width - 1) / wide_width : 0;
+    int at = 0, chunk = 0, wide_chunk = 0, chunks = 0, wide_chunks = 0;
+    for (int j = 0; j < (int)slots; ++j) {
+      const int other = __shfl_sync(0xFFFFFFFFu, on ? id : INT32_MAX, j), n = __shfl_sync(0xFFFFFFFFu, pieces, j),
+                w = __shfl_sync(0xFFFFFFFFu, wide_pieces, j);
+      if (other < id) ++at, chunk += n, wide_chunk += w;
+      chunks += n, wide_chunks += w;
+    }
+    if (on) plan.slot_of[at + __popc(alike & below)] = lane;
+    if (lane < slots) plan.pos_of[lane] = on ? at + __popc(alike & below) : -1;
+    if (leads) {
+      cut(id, at, total, pieces, plan.chunks + chunk);
+      if (wide.header != nullptr) cut(id, at, total, wide_pieces, wide.chunks + wide_chunk);
+    }
+    const uint32_t placed = __ballot_sync(0xFFFFFFFFu, on);
+    if (lane == 0) {
+      plan.header[0] = chunks, plan.header[1] = __popc(placed);
+      if (wide.header != nullptr) wide.header[0] = wide_chunks;
+    }
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t run = (slots + kPlanWarps - 1) / kPlanWarps, s0 = warp * run, s1 = min(slots, s0 + run);
+  const int64_t begin = run_counts != nullptr ? blockIdx.x * kPlanSlots : 0;
+  const int64_t stop = run_counts != nullptr ? min(slots, begin + kPlanSlots) : slots;
+  const int64_t run = (stop - begin + kPlanWarps - 1) / kPlanWarps, s0 = begin + warp * run, s1 = min(stop, s0 + run);
   for (int i = threadIdx.x; i < kPlanWarps * experts; i += kPlanThreads) counts[i] = 0;
   __syncthreads();
   int32_t* mine = counts + warp * experts;
@@ -63,12 +123,20 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
   }
   __syncthreads();
   // expert e = threadIdx.x (at most 1024): its slots, then the experts' first positions and first chunks
-  int total = 0;
+  int total = 0, before = 0;  // before: in the runs before this CTA's
   if ((int)threadIdx.x < experts) {
     for (int w = 0; w < kPlanWarps; ++w) {
       const int c = counts[w * experts + threadIdx.x];
       counts[w * experts + threadIdx.x] = total;
       total += c;
+    }
+    if (run_counts != nullptr) {
+      total = 0;
+      for (int g = 0; g < (int)gridDim.x; ++g) {
+        const int c = run_counts[(int64_t)g * experts + threadIdx.x];
+        if (g < (int)blockIdx.x) before += c;
+        total += c;
+      }
     }
   }
   const int pieces = (total + width - 1) / width, wide_pieces = (total + wide_width - 1) / wide_width;
@@ -81,23 +149,17 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* __res
   if (lane == 31) warp_total[warp] = at, warp_chunks[warp] = chunk, warp_wide[warp] = wide_chunk;
   __syncthreads();
   for (int w = 0; w < warp; ++w) at += warp_total[w], chunk += warp_chunks[w], wide_chunk += warp_wide[w];
-  if (threadIdx.x == kPlanThreads - 1) {
+  if (threadIdx.x == kPlanThreads - 1 && blockIdx.x == 0) {
     plan.header[0] = chunk, plan.header[1] = at;
     if (wide.header != nullptr) wide.header[0] = wide_chunk;
   }
   at -= total, chunk -= pieces, wide_chunk -= wide_pieces;
   if ((int)threadIdx.x < experts) {
-    first[threadIdx.x] = at;
-    // chunks of nearly the same size, whole 16s
-    const auto cut = [&](int n, Chunk* to) {
-      const int each = n ? ((total + n - 1) / n + 15) / 16 * 16 : 0;
-      for (int c = 0; c < n; ++c) {
-        const int from = min(total, c * each), end = min(total, from + each);
-        to[c] = {(int32_t)threadIdx.x, at + from, end - from, 0};
-      }
-    };
-    cut(pieces, plan.chunks + chunk);
-    if (wide.header != nullptr) cut(wide_pieces, wide.chunks + wide_chunk);
+    first[threadIdx.x] = at + before;
+    if (blockIdx.x == 0) {
+      cut((int)threadIdx.x, at, total, pieces, plan.chunks + chunk);
+      if (wide.header != nullptr) cut((int)threadIdx.x, at, total, wide_pieces, wide.chunks + wide_chunk);
+    }
   }
   __syncthreads();
   for (int64_t s = s0; s < s1; s += 32 * kPlanAhead) {
@@ -747,8 +809,11 @@ int experts_width(int64_t slots, int64_t experts) {
   return each <= 10 ? 16 : each <= 24 ? 32 : each <= 56 ? 64 : 128;
 }
 
+static int64_t plan_runs(int64_t slots) { return (slots + kPlanSlots - 1) / kPlanSlots; }
+
 int64_t experts_plan_bytes(int64_t slots, int64_t experts) {
-  return 256 + 2 * round256(plan_chunks(slots, experts, 16) * (int64_t)sizeof(Chunk)) + 2 * round256(slots * 4);
+  return 256 + 2 * round256(plan_chunks(slots, experts, 16) * (int64_t)sizeof(Chunk)) + 2 * round256(slots * 4) +
+         round256(plan_runs(slots) * experts * 4);
 }
 
 Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts) {
@@ -776,9 +841,17 @@ cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, co
   // set once, for every call's size
   const cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void*>(plan_kernel), (kPlanWarps + 1) * (int)kRouteExperts * 4);
   if (err != cudaSuccess) return err;
-  plan_kernel<<<1, kPlanThreads, smem, stream>>>(r.ids, r.tokens * r.k, (int)experts, width, plan, wide_width,
-                                                    wide != nullptr ? *wide : Plan{});
-  return cudaGetLastError();
+  const int64_t slots = r.tokens * r.k, runs = plan_runs(slots);
+  const Plan none = {}, &second = wide != nullptr ? *wide : none;
+  if (runs == 1) {
+    plan_kernel<<<1, kPlanThreads, smem, stream>>>(r.ids, slots, (int)experts, width, plan, wide_width, second, nullptr);
+    return cudaGetLastError();
+  }
+  int32_t* counts = plan.pos_of + round256(slots * 4) / 4;
+  count_kernel<<<(unsigned)runs, kPlanThreads, 0, stream>>>(r.ids, slots, (int)experts, counts);
+  if (const cudaError_t count = cudaGetLastError(); count != cudaSuccess) return count;
+  return launch_chained(plan_kernel, dim3((unsigned)runs), kPlanThreads, smem, stream, r.ids, slots, (int)experts, width, plan, wide_width,
+                        second, static_cast<const int32_t*>(counts));
 }
 
 cudaError_t launch_experts_spread(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out, uint32_t* amax,

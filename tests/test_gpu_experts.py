@@ -52,7 +52,7 @@ def layer(t, n, inner, count, k, seed=0, pad=8, none=0.1, skew=0):
 # tokens, n, inner, experts, k
 SIZES = [(1, 16, 16, 1, 1), (1, 64, 32, 4, 2), (1, 512, 256, 16, 8), (3, 80, 48, 5, 3), (37, 272, 144, 12, 3), (64, 128, 128, 64, 8),
          (130, 512, 256, 8, 2), (300, 256, 400, 3, 2), (600, 64, 80, 2, 1), (45, 1040, 528, 40, 4), (9, 2048, 64, 1024, 32),
-         (70, 144, 1040, 7, 5), (1100, 320, 192, 2, 2), (640, 256, 512, 1, 1)]
+         (70, 144, 1040, 7, 5), (1100, 320, 192, 2, 2), (640, 256, 512, 1, 1), (1300, 64, 48, 40, 8)]
 
 
 def clean(w):
