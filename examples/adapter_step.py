@@ -3,13 +3,14 @@ them.
 
 1. Calibration and quantization: h = diag(X^T X) over calibration tokens, RTN codes, the H-Scale search.
 2. Training steps of one low-rank adapter beside the frozen packed weight, against the layer's bf16 weight: the
-   activations are kept in 8 bits between the forward and the backward pass.
+   activations are kept in 8 bits between the forward and the backward pass; the gradients are clipped by their norm.
 3. Serving: one decoding batch whose tokens belong to different adapters (the trained one, another, none).
 
     python examples/adapter_step.py
 """
 from __future__ import annotations
 
+import math
 import os
 import sys
 
@@ -35,7 +36,7 @@ def quantize(w: torch.Tensor, x: torch.Tensor, k: int = 4):
 
 
 def run(m: int = 512, n: int = 1024, tokens: int = 2048, rank: int = 16, steps: int = 30, rate: float = 5e-4, seed: int = 0,
-        device: str = "cuda"):
+        device: str = "cuda", max_norm: float = math.inf):
     """Losses of the training steps (mean squared error to the unquantized layer), and the served outputs.
 
     The rate is Adam's step for an element of A or B. B starts at zero and has to reach about (error of a weight) /
@@ -58,6 +59,8 @@ def run(m: int = 512, n: int = 1024, tokens: int = 2048, rank: int = 16, steps: 
     ids = torch.zeros(tokens, dtype=torch.int32, device=device)  # adapter 0 is trained
     master = [a.float(), b.float()]
     moments = [(torch.zeros_like(t), torch.zeros_like(t)) for t in master]
+    gradients = hs.hscale_tensors([da, db])
+    norm = torch.empty(1, dtype=torch.float32, device=device)
     losses = []
     for step in range(1, steps + 1):
         hs.hscale_project(x, packed, codes, sg, a, b, alpha, ids, y, workspace)
@@ -67,6 +70,7 @@ def run(m: int = 512, n: int = 1024, tokens: int = 2048, rank: int = 16, steps: 
         dy = (error * (2.0 / error.numel())).to(torch.bfloat16)
         hs.hscale_project_backward(dy, held, held_scales, hs.HSCALE_CHECKPOINT_INT8, packed, codes, sg, a, b, alpha, ids, None,
                                    da, db, workspace)
+        hs.hscale_grad_clip(gradients, max_norm, norm)
         for t, grad, param, (first, second) in zip(master, (da, db), (a, b), moments):
             first.lerp_(grad.float(), 0.1)
             second.lerp_(grad.float() ** 2, 0.01)
