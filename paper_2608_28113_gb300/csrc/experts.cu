@@ -18,6 +18,7 @@
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>
+#include <type_traits>
 
 #include "chained_launch.h"
 #include "experts.cuh"
@@ -185,13 +186,22 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* ids, 
 }
 
 // A token's row in fp16 (experts.cuh) to the positions of its slots, with the row's amax; a row of h begins with none.
-__global__ void __launch_bounds__(256) spread_kernel(const uint4* x, int64_t ld, int64_t pieces, int k, Plan plan, uint4* out,
-                                                     uint32_t* amax, uint32_t* h_amax) {
+// gridDim.y of them: of x, and of the backward pass's dy.
+struct Spread {
+  const uint4* x;
+  int64_t ld;
+  uint4* out;
+  uint32_t* amax;
+};
+__global__ void __launch_bounds__(256) spread_kernel(Spread first, Spread second, int64_t pieces, int k, Plan plan, uint32_t* h_amax) {
   __shared__ uint32_t warp_max[8];
   pdl_wait_primary();
   pdl_launch_dependents();
+  const Spread& s = blockIdx.y ? second : first;
+  uint4* out = s.out;
+  uint32_t* amax = s.amax;
   const int64_t t = blockIdx.x;
-  const uint4* row = x + t * ld;
+  const uint4* row = s.x + t * s.ld;
   uint4 kept[kSpreadKept];
   uint32_t m = 0u;
 #pragma unroll
@@ -233,29 +243,51 @@ __global__ void __launch_bounds__(256) convert_kernel(uint4* h, int64_t pieces, 
 }
 
 // out_t = the sum of the token's slots' rows (part, and more where it is not nullptr) times their weights (nullptr: 1), in order;
-// four columns a thread.
-__global__ void __launch_bounds__(256) combine_kernel(const float* part, const float* more, Plan plan, const float* weights, int64_t tokens, int k,
-                                                      int64_t n, __nv_bfloat16* out, int64_t ld) {
+// four columns a thread.  The threads behind them, where there are dots: dweights of each slot, the sum of its position's `parts` partial
+// sums, in order, and 0 of a slot without an expert.
+struct Combine {
+  const float *part, *more, *weights;
+  __nv_bfloat16* out;
+  int64_t n, ld, tokens;
+  int32_t k;
+  const float* dots;
+  int32_t parts;
+  float* dweights;
+};
+__global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ Combine c, Plan plan) {
   pdl_wait_primary();
-  const int64_t per = n / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= tokens * per) return;
-  const int64_t t = i / per, c = (i - t * per) * 4;
+  const int64_t per = c.out != nullptr ? c.n / 4 : 0;
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= c.tokens * per) {
+    i -= c.tokens * per;
+    const int64_t slots = c.tokens * c.k;
+    if (c.dots == nullptr || i >= slots) return;
+    if (plan.pos_of[i] < 0) c.dweights[i] = 0.0f;
+    if (i >= plan.header[1]) return;
+    // position i's, so that a warp's are side by side
+    float s = 0.0f;
+#pragma unroll 8
+    for (int q = 0; q < c.parts; ++q) s += c.dots[(int64_t)q * slots + i];
+    c.dweights[plan.slot_of[i]] = s;
+    return;
+  }
+  const int64_t t = i / per, col = (i - t * per) * 4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int j = 0; j < k; ++j) {
-    const int64_t pos = plan.pos_of[t * k + j];
+  for (int j = 0; j < c.k; ++j) {
+    const int64_t pos = plan.pos_of[t * c.k + j];
     if (pos < 0) continue;
-    const float w = weights == nullptr ? 1.0f : weights[t * k + j];
-    float4 v = *reinterpret_cast<const float4*>(part + pos * n + c);
-    if (more != nullptr) {
-      const float4 m = *reinterpret_cast<const float4*>(more + pos * n + c);
+    const float w = c.weights == nullptr ? 1.0f : c.weights[t * c.k + j];
+    float4 v = *reinterpret_cast<const float4*>(c.part + pos * c.n + col);
+    if (c.more != nullptr) {
+      const float4 m = *reinterpret_cast<const float4*>(c.more + pos * c.n + col);
       v.x += m.x, v.y += m.y, v.z += m.z, v.w += m.w;
     }
     s.x = fmaf(w, v.x, s.x), s.y = fmaf(w, v.y, s.y), s.z = fmaf(w, v.z, s.z), s.w = fmaf(w, v.w, s.w);
   }
   uint2 r;
   r.x = pack_bf16(s.x, s.y), r.y = pack_bf16(s.z, s.w);
-  *reinterpret_cast<uint2*>(out + t * ld + c) = r;
+  *reinterpret_cast<uint2*>(c.out + t * c.ld + col) = r;
 }
 
 // ---------------------------------------------------------------- the products
@@ -425,17 +457,22 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       if constexpr (kMode == kModeHidden) {
         // rounded and turned, so that a lane stores 8 outputs of a slot at once
         __syncwarp();
+        const float my_a = have ? my_up * scale_a : nan, my_b = my_up * scale_b;
+        const auto hidden = [&](auto kind) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float h[2];
+          for (int j = 0; j < 8; ++j) {
+            float h[2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float up = __shfl_sync(0xFFFFFFFFu, my_up, 2 * j + e);
-            h[e] = activate_fast(p.activation, __uint_as_float(a[2 * j + e]) * (scale_a * up)) *
-                   (__uint_as_float(b[2 * j + e]) * (scale_b * up));
+            for (int e = 0; e < 2; ++e)
+              h[e] = activate_fast<decltype(kind)::value>(__uint_as_float(a[2 * j + e]) * __shfl_sync(0xFFFFFFFFu, my_a, 2 * j + e)) *
+                     (__uint_as_float(b[2 * j + e]) * __shfl_sync(0xFFFFFFFFu, my_b, 2 * j + e));
+            turn[j * 32 + lane] = pack_bf16(h[0], h[1]);
           }
-          turn[j * 32 + lane] = have ? pack_bf16(h[0], h[1]) : 0x7FC07FC0u;
-        }
+        };
+        if (p.activation == kActSilu)
+          hidden(std::integral_constant<int, kActSilu>{});
+        else
+          hidden(std::integral_constant<int, kActGeluTanh>{});
         __syncwarp();
         const int pair = lane >> 2;
         const uint4 q0 = reinterpret_cast<const uint4*>(turn)[2 * lane], q1 = reinterpret_cast<const uint4*>(turn)[2 * lane + 1];
@@ -454,17 +491,26 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
           if (on && (lane & 3) == 0) atomicMax(&p.h_amax[pos], m);
         }
-      } else {
-        // 32 outputs of a slot side by side: raw [position][2][rows], or the part of y [position][rows]
-        const int64_t stride = kMode == kModeRaw ? 2 * p.rows : p.rows, second = kMode == kModeRaw ? p.rows : kBM;
-        float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * stride + o;
-        const bool on_a = o < p.rows, on_b = kMode == kModeRaw ? on_a : o + kBM < p.rows;
+      } else if constexpr (kMode == kModeRaw) {
+        // 32 outputs of a slot side by side, g with u
+        float2* out = static_cast<float2*>(p.out) + (int64_t)(c.first + j0) * p.rows + o;
+        const bool on = o < p.rows;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const float up = __shfl_sync(0xFFFFFFFFu, my_up, j);
-          if (j < left && on_a) out[0] = have ? __uint_as_float(a[j]) * (scale_a * up) : nan;
-          if (j < left && on_b) out[second] = have ? __uint_as_float(b[j]) * (scale_b * up) : nan;
-          out += stride;
+          const float up = have ? __shfl_sync(0xFFFFFFFFu, my_up, j) : nan;
+          if (j < left && on) *out = make_float2(__uint_as_float(a[j]) * (scale_a * up), __uint_as_float(b[j]) * (scale_b * up));
+          out += p.rows;
+        }
+      } else {
+        // 32 outputs of a slot side by side
+        float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * p.rows + o;
+        const bool on_a = o < p.rows, on_b = o + kBM < p.rows;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float up = have ? __shfl_sync(0xFFFFFFFFu, my_up, j) : nan;
+          if (j < left && on_a) out[0] = __uint_as_float(a[j]) * (scale_a * up);
+          if (j < left && on_b) out[kBM] = __uint_as_float(b[j]) * (scale_b * up);
+          out += p.rows;
         }
       }
     }
@@ -854,17 +900,19 @@ cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, co
                         second, static_cast<const int32_t*>(counts));
 }
 
-cudaError_t launch_experts_spread(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out, uint32_t* amax,
-                                  uint32_t* h_amax, cudaStream_t stream) {
-  return launch_chained(spread_kernel, dim3((unsigned)r.tokens), 256, 0, stream, static_cast<const uint4*>(x), ld / 8, n / 8, r.k, plan,
-                        static_cast<uint4*>(out), amax, h_amax);
+cudaError_t launch_experts_spread(const void* x, int64_t ld, void* out, uint32_t* amax, const void* dy, int64_t ld_dy, void* dy_out,
+                                  uint32_t* dy_amax, int64_t n, const Routing& r, const Plan& plan, uint32_t* h_amax, cudaStream_t stream) {
+  const Spread first = {static_cast<const uint4*>(x), ld / 8, static_cast<uint4*>(out), amax};
+  const Spread second = {static_cast<const uint4*>(dy), ld_dy / 8, static_cast<uint4*>(dy_out), dy_amax};
+  return launch_chained(spread_kernel, dim3((unsigned)r.tokens, dy != nullptr ? 2 : 1), 256, 0, stream, first, second, n / 8, r.k, plan,
+                        h_amax);
 }
 
-cudaError_t launch_experts_combine(const float* part, const float* more, const Routing& r, const float* weights, const Plan& plan, int64_t n, void* out,
-                                   int64_t ld, cudaStream_t stream) {
-  const int64_t threads = r.tokens * (n / 4);
-  return launch_chained(combine_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, stream, part, more, plan, weights, r.tokens, r.k, n,
-                        static_cast<__nv_bfloat16*>(out), ld);
+cudaError_t launch_experts_combine(const float* part, const float* more, const Routing& r, const float* weights, const Plan& plan, int64_t n,
+                                   void* out, int64_t ld, const float* dots, int parts, float* dweights, cudaStream_t stream) {
+  const Combine c = {part, more, weights, static_cast<__nv_bfloat16*>(out), n, ld, r.tokens, r.k, dots, parts, dweights};
+  const int64_t threads = (out != nullptr ? r.tokens * (n / 4) : 0) + (dots != nullptr ? r.tokens * r.k : 0);
+  return launch_chained(combine_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, stream, c, plan);
 }
 
 cudaError_t launch_experts_raw(const void* xs, const uint32_t* amax, int64_t slots, const Experts& w, const Plan& plan, int width,
@@ -899,7 +947,7 @@ cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const 
   float* part = reinterpret_cast<float*>(h + round256(slots * w.inner * 2));
   const int64_t chunks = plan_chunks(slots, w.count, width);
   if ((err = launch_experts_plan(r, w.count, width, plan, width, nullptr, stream)) != cudaSuccess) return err;
-  if ((err = launch_experts_spread(x, ld_x, w.n, r, plan, xs, amax, h_amax, stream)) != cudaSuccess) return err;
+  if ((err = launch_experts_spread(x, ld_x, xs, amax, nullptr, 0, nullptr, nullptr, w.n, r, plan, h_amax, stream)) != cudaSuccess) return err;
   GemmArgs p = {};
   p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan;
   p.amax = amax, p.h_amax = h_amax, p.out = h;
@@ -909,7 +957,7 @@ cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const 
   if (err != cudaSuccess) return err;
   p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.amax = h_amax, p.out = part;
   if ((err = launch_gemm<kModeDown>(width, h, slots, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
-  return launch_experts_combine(part, nullptr, r, r.weights, plan, w.n, y, ld_y, stream);
+  return launch_experts_combine(part, nullptr, r, r.weights, plan, w.n, y, ld_y, nullptr, 0, nullptr, stream);
 }
 
 cudaError_t read_experts_device_error(uint32_t* flags) {

@@ -51,19 +51,21 @@ constexpr int kActSilu = 0, kActGeluTanh = 1;
 
 // act(g) = g s(q) with s the logistic function and q = g (silu) or 2 sqrt(2 / pi) (g + 0.044715 g^3) (the tanh form of
 // gelu); approximate exponential and quotient (some 2^-20), for values that are rounded to 16 bits next.
-__device__ __forceinline__ float activate_fast(int kind, float g) {
-  const float q = kind == kActSilu ? g : 1.5957691216057308f * fmaf(0.044715f * g * g, g, g);
+template <int kKind>
+__device__ __forceinline__ float activate_fast(float g) {
+  const float q = kKind == kActSilu ? g : 1.5957691216057308f * fmaf(0.044715f * g * g, g, g);
   return __fdividef(g, 1.0f + __expf(-q));
 }
 // act(g) and its derivative in fp32: the exponential of a number that is not positive and the quotient are off by a few
 // 2^-23 (of 1, the derivative; of max(1, |g|), the activation).
-__device__ __forceinline__ float2 activate(int kind, float g) {
-  const float q = kind == kActSilu ? g : 1.5957691216057308f * fmaf(0.044715f * g * g, g, g);
-  const float dq = kind == kActSilu ? 1.0f : 1.5957691216057308f * fmaf(0.134145f * g, g, 1.0f);
+template <int kKind>
+__device__ __forceinline__ float2 activate(float g) {
+  const float q = kKind == kActSilu ? g : 1.5957691216057308f * fmaf(0.044715f * g * g, g, g);
   const float e = __expf(-fabsf(q)), part = __fdividef(1.0f, 1.0f + e), other = e * part;
-  const float s = q >= 0.0f ? part : other, rest = q >= 0.0f ? other : part;
-  const float slope = other > 0.0f ? g * dq * s * rest : 0.0f;  // other may be 0 where dq is infinite
-  return make_float2(g * s, s + slope);
+  const float s = q >= 0.0f ? part : other, a = g * s;
+  if (kKind == kActSilu) return make_float2(a, fmaf(a, q >= 0.0f ? other : part, s));  // part other = s (1 - s)
+  const float dq = 1.5957691216057308f * fmaf(0.134145f * g, g, 1.0f);
+  return make_float2(a, s + (other > 0.0f ? g * dq * (part * other) : 0.0f));  // other may be 0 where dq is infinite
 }
 
 // Asynchronous copies of 4 or 8 bytes, of which `bytes` are read and the rest zeros.

@@ -16,6 +16,7 @@
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>
+#include <type_traits>
 
 #include "chained_launch.h"
 #include "experts.cuh"
@@ -65,7 +66,7 @@ struct BackArgs {
   Plan plan;
   const float* weights;
   const uint32_t* amax;      // of each position's dy
-  const float* raw;          // g and u, [positions, 2, cols]
+  const float2* raw;         // g and u, [positions, cols]
   const float *gate_scale, *up_scale;
   __nv_bfloat16* factors;    // [positions, 2, cols], or nullptr
   float* dots;               // [8 tiles_o, slots] partial sums of h . dh, or nullptr
@@ -175,8 +176,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = warp_uniform(*tmem_slot);
-  pdl_wait_primary();  // the plan, the slots' tile, g and u
-  pdl_launch_dependents();
+  // The plan is there: the kernel that this one may run beside has waited for it.  What that kernel writes (the slots'
+  // tile, g and u) is waited for where it is read; the weights begin to come meanwhile.
 
   const int tiles = p.plan.header[0] * p.tiles_o * p.splits, step = (int)gridDim.x, first = (int)blockIdx.x;
   const int ntiles = tiles > first ? (tiles - first + step - 1) / step : 0;
@@ -214,13 +215,12 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       if (kMode != kModeHidden || piece >= pieces) return;
       const int half = piece >= each ? 1 : 0, j0 = (piece - half * each) * 8;
       const int64_t o = (int64_t)to * (kHalves * kBM) + half * kBM + quarter * 32 + lane;
-      const float* raw = p.raw + (int64_t)(c.first + j0) * 2 * p.cols + o;
+      const float2* raw = p.raw + (int64_t)(c.first + j0) * p.cols + o;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const bool on = j0 + j < c.count && o < p.cols;
-        g[j] = on ? raw[0] : 0.0f;
-        u[j] = on ? raw[p.cols] : 0.0f;
-        raw += 2 * p.cols;
+        const float2 v = j0 + j < c.count && o < p.cols ? *raw : make_float2(0.0f, 0.0f);
+        g[j] = v.x, u[j] = v.y;
+        raw += p.cols;
       }
     };
     fetch(who);
@@ -234,21 +234,27 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       uint32_t a[8];
       tmem_ld_32x32b_x8(d + (uint32_t)(half * kN + j0), a);
       if constexpr (kMode == kModeHidden) {
-        // lane j: slot j's weight, and the power of two of its row of dy
-        const float my_w = lane < left ? p.weights[p.plan.slot_of[pos + lane]] : 0.0f;
-        const float my_up = lane < left ? scale * exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
+        // lane j: slot j's weight times G's and U's scales, and the power of two of its row of dy times D's
+        const float my_w = lane < left ? p.weights[p.plan.slot_of[pos + lane]] : 0.0f, my_g = my_w * sg, my_u = my_w * su;
+        const float my_up = !have ? nan : lane < left ? scale * exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
         tmem_ld_wait();
         if (piece + kWorkers >= pieces) release(acc);
         float dot[8], dg[8], du[8];
+        // (outputs past the end have g = u = 0, and are not stored)
+        const auto factors = [&](auto kind) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float up = __shfl_sync(0xFFFFFFFFu, my_up, j), w = __shfl_sync(0xFFFFFFFFu, my_w, j);
-          const float dh = have ? __uint_as_float(a[j]) * up : nan;
-          const float2 act = activate(p.activation, g[j]);
-          dot[j] = j < left && on ? dh * (act.x * u[j]) : 0.0f;
-          dg[j] = w * dh * u[j] * act.y * sg;
-          du[j] = w * dh * act.x * su;
-        }
+          for (int j = 0; j < 8; ++j) {
+            const float dh = __uint_as_float(a[j]) * __shfl_sync(0xFFFFFFFFu, my_up, j);
+            const float2 act = activate<decltype(kind)::value>(g[j]);
+            dot[j] = dh * (act.x * u[j]);
+            dg[j] = dh * __shfl_sync(0xFFFFFFFFu, my_g, j) * (u[j] * act.y);
+            du[j] = dh * __shfl_sync(0xFFFFFFFFu, my_u, j) * act.x;
+          }
+        };
+        if (p.activation == kActSilu)
+          factors(std::integral_constant<int, kActSilu>{});
+        else
+          factors(std::integral_constant<int, kActGeluTanh>{});
         fetch(piece + kWorkers);
         if (p.factors != nullptr) {
           __nv_bfloat16* out = p.factors + pos * 2 * p.cols;
@@ -276,6 +282,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   const auto turn_at = [&](int worker) { return reinterpret_cast<uint32_t*>(rest + 512 + worker * 512); };
 
   if (warp == 0) {
+    pdl_wait_primary();
+    pdl_launch_dependents();
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
     uint32_t s = 0, parity = 1;
@@ -339,6 +347,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     __syncwarp();
     umma_drain(mma_done);
   } else if (warp < kUnpackWarp0) {
+    pdl_wait_primary();
     for (int i = 0; i < ntiles; ++i) finish(i, 0, turn_at(warp - kEpilogueWarp0));
     if (!have && lane == 0) atomicOr(failed, 1u);
   } else if (warp < kWeightsWarp0) {
@@ -418,11 +427,14 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           if (p.path != kDirect) mbar_arrive(&packed_empty[ps]);  // the loads' values have been used
         }
         // the tile before, once this one's first blocks are there for the MMAs
+        if (T::kHelp && done == 0 && i == 1) pdl_wait_primary();
         if (T::kHelp && done++ == 0 && i > 0) finish(i - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
       }
       // (a tile of one K block has none of this group's)
+      if (T::kHelp && done == 0 && i == 1) pdl_wait_primary();
       if (T::kHelp && done == 0 && i > 0 && go) finish(i - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
     }
+    if (T::kHelp && ntiles == 1) pdl_wait_primary();
     if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
     if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
   } else if (p.path != kDirect && (warp == kWeightsWarp0 || p.path != kBulk)) {
@@ -479,20 +491,6 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     tmem_dealloc(tmem, T::kTmemCols);
   }
   if (threadIdx.x == 0 && *failed) atomicOr(&g_experts_backward_flags, kErrMbarTimeout);
-}
-
-// dweights of each slot: the sum of its position's partial sums, in order; 0 for a slot without an expert.
-__global__ void __launch_bounds__(256) dweights_kernel(const float* dots, int parts, int64_t slots, const int32_t* ids,
-                                                       int experts, Plan plan, float* dweights) {
-  pdl_wait_primary();
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= slots) return;
-  if ((unsigned)ids[i] >= (unsigned)experts) dweights[i] = 0.0f;
-  if (i < plan.header[1]) {
-    float s = 0.0f;
-    for (int q = 0; q < parts; ++q) s += dots[(int64_t)q * slots + i];
-    dweights[plan.slot_of[i]] = s;
-  }
 }
 
 template <int kMode, int kN>
@@ -594,23 +592,21 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   const int64_t chunks = plan_chunks(slots, w.count, wide_width);
   const int64_t expected = slots / wide_width + std::min<int64_t>(slots, w.count) / 2;  // half a chunk an expert is not full
   if ((err = launch_experts_plan(r, w.count, width, plan, wide_width, &wide, stream)) != cudaSuccess) return err;
-  if ((err = launch_experts_spread(x, ld_x, w.n, r, plan, xs, amax, nullptr, stream)) != cudaSuccess) return err;
-  if ((err = launch_experts_spread(dy, ld_dy, w.n, r, plan, dys, dy_amax, nullptr, stream)) != cudaSuccess) return err;
+  err = launch_experts_spread(x, ld_x, xs, amax, dy, ld_dy, dys, dy_amax, w.n, r, plan, nullptr, stream);
+  if (err != cudaSuccess) return err;
   if ((err = launch_experts_raw(xs, amax, slots, w, plan, width, reinterpret_cast<float*>(raw), stream)) != cudaSuccess) return err;
   BackArgs p = {};
   p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.activation = w.activation, p.plan = wide, p.weights = r.weights, p.amax = dy_amax;
-  p.raw = reinterpret_cast<const float*>(raw), p.gate_scale = w.gate.scale, p.up_scale = w.up.scale, p.slots = slots;
+  p.raw = reinterpret_cast<const float2*>(raw), p.gate_scale = w.gate.scale, p.up_scale = w.up.scale, p.slots = slots;
   p.factors = dx != nullptr ? reinterpret_cast<__nv_bfloat16*>(factors) : nullptr;
   p.dots = dweights != nullptr ? reinterpret_cast<float*>(dots) : nullptr;
   if ((err = launch_back<kModeHidden>(wide_width, dys, 1, w.count, p, chunks, expected, info.sm_count, stream)) != cudaSuccess) return err;
   if (dx != nullptr) {
     p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.part = reinterpret_cast<float*>(xs), p.more = reinterpret_cast<float*>(raw);
     if ((err = launch_back<kModeInput>(wide_width, factors, 2, w.count, p, chunks, expected, info.sm_count, stream)) != cudaSuccess) return err;
-    if ((err = launch_experts_combine(p.part, p.splits == 2 ? p.more : nullptr, r, nullptr, plan, w.n, dx, ld_dx, stream)) != cudaSuccess) return err;
   }
-  if (dweights == nullptr) return cudaSuccess;
-  return launch_chained(dweights_kernel, dim3((unsigned)((slots + 255) / 256)), 256, 0, stream, reinterpret_cast<const float*>(dots),
-                        (int)dot_parts(w.inner), slots, r.ids, w.count, plan, dweights);
+  return launch_experts_combine(p.part, p.splits == 2 ? p.more : nullptr, r, nullptr, plan, w.n, dx, ld_dx, p.dots, (int)dot_parts(w.inner),
+                                dweights, stream);
 }
 
 cudaError_t read_experts_backward_device_error(uint32_t* flags) {

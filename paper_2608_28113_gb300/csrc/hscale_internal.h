@@ -176,8 +176,9 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
                                     const Experts& w, void* dx, int64_t ld_dx, float* dweights, void* workspace,
                                     cudaStream_t stream);
 // Their steps: slots a tile; the plan's memory; the plan; rows of x in its order (fp16 under a power of two of each row's
-// amax, contiguous); g and u of each position (fp32 [positions, 2, inner]); a token's slots' rows (fp32, contiguous; and those of
-// `more`, or nullptr) times their weights (nullptr: 1) added up.
+// amax, contiguous; dy's too, or nullptr); g and u of each position (fp32 [positions, inner, 2]); a token's slots' rows (fp32, contiguous; and those of
+// `more`, or nullptr) times their weights (nullptr: 1) added up (out nullptr: not), and dweights of the
+// dots' `parts` partial sums (nullptr: not).
 int experts_width(int64_t slots, int64_t experts);
 // Bytes [rows, bytes] in TMA boxes of width (128: swizzled) x height.
 cudaError_t bytes_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t rows, uint32_t width, uint32_t height);
@@ -187,12 +188,14 @@ Plan experts_plan_at(void* workspace, int64_t slots, int64_t experts);
 Plan experts_wide_plan(const Plan& plan, int64_t slots, int64_t experts);
 cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, const Plan& plan, int wide_width,
                                 const Plan* wide, cudaStream_t stream);
-cudaError_t launch_experts_spread(const void* x, int64_t ld, int64_t n, const Routing& r, const Plan& plan, void* out,
-                                  uint32_t* amax, uint32_t* h_amax, cudaStream_t stream);
+cudaError_t launch_experts_spread(const void* x, int64_t ld, void* out, uint32_t* amax, const void* dy, int64_t ld_dy,
+                                  void* dy_out, uint32_t* dy_amax, int64_t n, const Routing& r, const Plan& plan,
+                                  uint32_t* h_amax, cudaStream_t stream);
 cudaError_t launch_experts_raw(const void* xs, const uint32_t* amax, int64_t slots, const Experts& w, const Plan& plan,
                                int width, float* raw, cudaStream_t stream);
-cudaError_t launch_experts_combine(const float* part, const float* more, const Routing& r, const float* weights, const Plan& plan, int64_t n,
-                                   void* out, int64_t ld, cudaStream_t stream);
+cudaError_t launch_experts_combine(const float* part, const float* more, const Routing& r, const float* weights,
+                                   const Plan& plan, int64_t n, void* out, int64_t ld, const float* dots, int parts,
+                                   float* dweights, cudaStream_t stream);
 
 // The norm over tensors and, with clip, the tensors scaled into out (nullptr: in place); host arrays.
 // parts: kGradParts doubles.
