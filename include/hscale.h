@@ -606,11 +606,11 @@ typedef enum hscale_activation { HSCALE_ACT_SILU = 0, HSCALE_ACT_GELU_TANH = 1 }
  * are bf16 with rows ld_x and ld_y elements apart; ids and weights [tokens, k] are contiguous.  An id outside
  * [0, experts) has no term, whatever its weight; a token without experts gets zeros.
  *
- * Sums are fp32 and y is rounded once.  act(G x) * (U x) is rounded to 16 bits before the second product: to bf16, or
- * (few tokens) to fp16 under a power of two of its row; a few tokens' x is held in fp16 under a power of two of its
- * row, which changes elements below 2^-30 of the row's largest alone.  A token's value depends on its own row and
- * experts only, an Inf or NaN elsewhere does not reach it; its last bits may depend on how many tokens there are.  Where its own
- * values are not finite, NaN may stand for an Inf.  Equal calls give equal bits.
+ * Sums are fp32 and y is rounded once; act(G x) * (U x) is rounded to bf16 before the second product.  The products' operands are
+ * held in fp16 under a power of two of each row: an element loses bits only where it is below 2^-31 of its row's largest,
+ * and 2^-40 of that at most.  A token's value depends on its own row and experts only, an Inf or NaN elsewhere does not
+ * reach it.  Where its own values are not finite, NaN may stand for an Inf.  Equal calls give equal bits, and a token's do
+ * not depend on the batch that it is in.
  *
  * n and inner are multiples of 16, experts at most 1024, k at most 32.  x and y are 16-byte aligned, ld_x and ld_y
  * multiples of 8, packed weights 8-byte aligned.  With inner == 0, y is zero.  The workspace is 256-byte aligned; calls

@@ -1,20 +1,29 @@
 // experts.cu -- a layer of experts with packed NVFP4 weights on the tcgen05 tensor cores:
 //   y_t = sum_j w_tj D_e (act(G_e x_t) * (U_e x_t)),  e = ids[t, j]
-// Five steps, each launched while the one before it ends: the slots (token, j) are grouped by expert; their x is laid out
-// in that order; the first product makes h = act(G x) * (U x), rounded to bf16 (the second product's operand: its error
-// is of the size of y's own rounding); the second makes w D h of each slot in fp32; a token's slots are added up in
-// order and rounded once.
+// Steps, each launched while the one before it runs: the slots (token, j) are grouped by expert; their x is laid out in that
+// order, in fp16 (experts.cuh); the first product makes h = act(G x) * (U x), rounded to bf16 (its error is of the size
+// of y's own rounding); h becomes fp16 under a power of two of its row, exactly; the second product makes D h of each
+// slot in fp32; a token's slots are weighted and added up in order, and rounded once.
 //
 // The products.  Tile: 256 rows of weights as two halves of 128 (128 rows of G and the same 128 of U, or 256 rows of
-// D) x up to kN slots of one expert, K in blocks of 64.  18 warps:
+// D) x up to kN slots of one expert, K in blocks of 64.  24 warps:
 //   0      TMA loads of the slots' tile, K-major, 128-byte swizzle
 //   1      MMAs
 //   2-5    epilogue (lane = row of weights, columns = slots)
-//   6-17   the weights: three groups of four warps take the halves' blocks in turn.  A thread has one row, 32 packed
-//          bytes and 4 codes of it a block, kept kAhead blocks ahead in registers, and writes 64 bf16 weights into
-//          tensor memory, from where the MMAs take their A operand: shared memory, which both operands would
-//          saturate, holds the slots' tile alone.
-// E2M1 times E4M3 has at most 6 significant bits: a weight without its global scale is exact in bf16.
+//   6-21   unpacking: a group of four for each half and every other block; a thread has one row, and writes 64 fp16
+//          weights a block into tensor memory, from where the MMAs take their A operand: shared memory, which both
+//          operands would saturate, holds the slots' tile and the packed rows alone
+//   22-23  the packed rows, 256 columns a stage, as many stages ahead as fit (experts.cuh: how they come)
+// A block's 16384 weights cost the unpacking warps some 1200 instructions, 300 cycles at best; its bytes take 390 cycles at the
+// card's bandwidth, its MMAs 512 at 128 slots.  So few slots are bound by memory (16 tokens of 64 experts, 4096 x 2048, k 8:
+// 164 us, 4.8 TB/s of weights; 5.4 TB/s is what the loads alone reach), many by the tensor cores (32768 slots: 1.65 PFLOP/s
+// in the first product, 1.45 in the second, whose K is half as long; the rest is the epilogue, for which tensor memory has
+// no second accumulator at 128 slots: the unpacking warps take part in it).  One token: latency, of six launches one
+// behind another and of each product's first loads.
+//
+// A packed stage is given back only when its values have been used: an arrival right behind the loads had TMA
+// overwrite rows that were still being read.  The plan is complete before a product's kernel may start, so its weights come
+// while the kernel before it still runs.
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>

@@ -1,9 +1,9 @@
 // experts_backward.cu -- the gradients of a layer of experts with packed NVFP4 weights:
 //   dh = D_e^T dy_t,  dw = h . dh,  dx_t = sum_j w_tj (G_e^T (dh u act'(g)) + U_e^T (dh act(g)))
-// The slots are grouped as in the forward pass (experts.cu), x and dy laid out in that order, and g and u made again in
-// fp32.  Two products by transposed weights follow: the first (K = n) makes dh and, as it leaves tensor memory, dw and the two factors
-// of dx, rounded to bf16 with G's and U's global scales in them; the second (K = G's rows, then U's) makes each slot's
-// part of dx in fp32; a token's slots are added up in order and rounded once.
+// The slots are grouped as in the forward pass (experts.cu), x and dy laid out in that order in fp16, and g and u made again
+// in fp32.  Two products by transposed weights follow: the first (K = n) makes dh and, as it leaves tensor memory, dw's partial sums
+// and the two factors of dx, rounded to bf16 with G's and U's global scales in them; the second (K = G's rows, then U's)
+// makes each slot's part of dx in fp32; a token's slots are added up in order and rounded once.
 //
 // The transposed products.  Tile: 256 outputs (columns of the weights) as two halves of 128 x up to kN slots, K in blocks
 // of 64 rows.  The packed rows, unpacked as they are stored, make the weights' tile MN-major in shared memory
@@ -12,7 +12,9 @@
 // K), and two that fetch the packed blocks.
 // Bound by shared memory, which carries both operands, the packed blocks and the unpacking: of 128 bytes a
 // cycle, a K block takes some 1010 cycles at 128 slots against 512 of MMAs, and 1416 at 256 against 1024; so an expert
-// with enough slots takes 256 a tile, and the unpacking warps then take part in its epilogue.
+// with enough slots takes 256 a tile, and the unpacking warps then take part in its epilogue.  4096 slots of 8 experts,
+// 4096 x 14336: first product 550 us (0.87 PFLOP/s; 28 % of it the epilogue, whose 65536 numbers a tile are some 45
+// instructions each), second 836 us (1.15 PFLOP/s), g and u 600 us (1.6 PFLOP/s).
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>

@@ -271,3 +271,13 @@ def test_small_sizes_and_refusals():
             hs.hscale_experts(a["x"], a["ids"], a["w"], a["gate"], a["up"], a["down"], a["activation"], a["y"])
     with pytest.raises(hs.HScaleError):
         hs.hscale_experts(x, ids, w, gate, up, down, 0, y, torch.empty(256, dtype=U8, device=DEV))
+
+
+def test_a_tokens_bits_do_not_depend_on_its_batch():
+    args = layer(900, 448, 208, 5, 2, seed=31)
+    x, ids, w, gate, up, down = args
+    whole = run(*args, 0)
+    for start, count in ((0, 1), (17, 12), (100, 90), (300, 400)):
+        part = slice(start, start + count)
+        got = run(x[part], ids[part].contiguous(), w[part].contiguous(), gate, up, down, 0)
+        assert torch.equal(got, whole[part])
