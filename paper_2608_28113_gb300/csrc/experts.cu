@@ -333,6 +333,7 @@ struct GemmArgs {
   ExpertMatrix a, b;  // the tile's halves
   int64_t rows, cols;  // of an expert's matrix
   int32_t kb_total, tiles_o, tile_rows;  // tile_rows: between the tiles' first rows
+  int32_t segments, kb_segment;          // of kModeRaw: K's segments, and their K blocks (whole stages; the last has fewer)
   int32_t activation;
   int32_t path;  // packed_path
   int64_t all_rows;  // of all experts
@@ -416,9 +417,15 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   // The plan is there: the kernel that this one may run beside has waited for it.  What that kernel writes (the slots'
   // tile, and the rows' amax) is waited for where it is read; the weights begin to come meanwhile.
 
+  // The CTA's tile i.  In kModeRaw a tile's segments of K are tiles one after another, each summed up from zero and added to
+  // what the ones before left: the tensor cores cut off a sum's low bits at each step of 16 (of 256 steps of random numbers
+  // 1e-6 of it is lost, of positive ones 5e-6), and g and u are wanted as exact as fp32 sums are.
+  const int segments = kMode == kModeRaw ? p.segments : 1;
   const int tiles = p.plan.header[0] * p.tiles_o, step = (int)gridDim.x, first = (int)blockIdx.x;
-  const int ntiles = tiles > first ? (tiles - first + step - 1) / step : 0;
-  const int kbs = p.kb_total, quads = (kbs + kQuad - 1) / kQuad;
+  const int ntiles = tiles > first ? (tiles - first + step - 1) / step * segments : 0;
+  const auto tile_of = [&](int i) { return first + (kMode == kModeRaw ? i / segments : i) * step; };
+  const auto kb_first = [&](int i) { return kMode == kModeRaw ? i % segments * p.kb_segment : 0; };
+  const auto kb_count = [&](int i) { return kMode == kModeRaw ? min(p.kb_segment, p.kb_total - kb_first(i)) : p.kb_total; };
   const uint32_t quarter = (uint32_t)(warp & 3), lane_base = (quarter * 32u) << 16;
   const int row_in_half = (int)quarter * 32 + lane;
   bool have = true;  // of the warps of the epilogue: no wait for an accumulator has run out
@@ -433,7 +440,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   const auto up_of = [&](const Chunk& c, int j) { return lane < 16 && j + lane < c.count ? exp2_int(row_exponent(p.amax[c.first + j + lane])) : 0.0f; };
   const auto prepare = [&](int i, int who) {
     Finish f;
-    f.c = p.plan.chunks[(first + i * step) / p.tiles_o];
+    f.c = p.plan.chunks[tile_of(i) / p.tiles_o];
     f.scale_a = p.a.scale[f.c.expert], f.scale_b = p.b.scale[f.c.expert];
     f.up0 = up_of(f.c, 16 * who), f.up1 = up_of(f.c, 16 * (who + kWorkers));
     return f;
@@ -445,7 +452,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   };
   // The epilogue: 16 slots a time, those of this warp (one of kWorkers of its quarter).
   const auto finish = [&](int i, int who, uint32_t* turn, const Finish& f) {
-    const int t = first + i * step;
+    const int t = tile_of(i);
     const Chunk& c = f.c;
     const int64_t o0 = (int64_t)(t % p.tiles_o) * p.tile_rows, o = o0 + row_in_half;
     const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc + lane_base;
@@ -504,12 +511,26 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         // 32 outputs of a slot side by side, g with u
         float2* out = static_cast<float2*>(p.out) + (int64_t)(c.first + j0) * p.rows + o;
         const bool on = o < p.rows;
+        const auto put = [&](auto add) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float up = have ? __shfl_sync(0xFFFFFFFFu, my_up, j) : nan;
-          if (j < left && on) *out = make_float2(__uint_as_float(a[j]) * (scale_a * up), __uint_as_float(b[j]) * (scale_b * up));
-          out += p.rows;
-        }
+          for (int j0 = 0; j0 < 16; j0 += 8) {
+            float2 before[8];  // all on their way before the first store
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              before[j] = decltype(add)::value && j0 + j < left && on ? out[(j0 + j) * p.rows] : make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float up = __shfl_sync(0xFFFFFFFFu, my_up, j0 + j), upn = have ? up : nan;
+              if (j0 + j < left && on)
+                out[(j0 + j) * p.rows] = make_float2(fmaf(__uint_as_float(a[j0 + j]), scale_a * upn, before[j].x),
+                                                     fmaf(__uint_as_float(b[j0 + j]), scale_b * upn, before[j].y));
+            }
+          }
+        };
+        if (kb_first(i) > 0)
+          put(std::true_type{});
+        else
+          put(std::false_type{});
       } else {
         // 32 outputs of a slot side by side
         float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * p.rows + o;
@@ -535,7 +556,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     uint32_t s = 0, parity = 1;
     bool go = true;
     for (int i = 0; i < ntiles && go; ++i) {
-      const Chunk c = p.plan.chunks[(first + i * step) / p.tiles_o];
+      const Chunk c = p.plan.chunks[tile_of(i) / p.tiles_o];
+      const int kb0 = kb_first(i), kbs = kb_count(i);
       for (int kb = 0; kb < kbs; ++kb) {
         if (!mbar_wait_warp(&empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
@@ -544,7 +566,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
         if (elect_one()) {
           mbar_arrive_expect_tx(&full[s], T::kBBytes);
-          tma_load_2d(tile_b + s * T::kBBytes, &vmap, kb * kBK, c.first, &full[s], policy);
+          tma_load_2d(tile_b + s * T::kBBytes, &vmap, (kb0 + kb) * kBK, c.first, &full[s], policy);
         }
         __syncwarp();
         if (++s == kStages) s = 0, parity ^= 1u;
@@ -555,7 +577,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     uint32_t s = 0, parity = 0;
     bool ok = true;
     for (int i = 0; i < ntiles && ok; ++i) {
-      const Chunk c = p.plan.chunks[(first + i * step) / p.tiles_o];
+      const Chunk c = p.plan.chunks[tile_of(i) / p.tiles_o];
+      const int kbs = kb_count(i);
       const uint32_t idesc = warp_uniform(idesc_f16_f32(kBM, (uint32_t)((c.count + 15) & ~15)));
       const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc;
       if (i >= kAccs && !mbar_wait_warp(&acc_empty[acc], (uint32_t)(i / kAccs - 1) & 1u)) {
@@ -611,11 +634,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     uint32_t stage = 0, parity_p = 0, slot = (uint32_t)odd, parity = 1;
     const uint32_t tmem_a = tmem + T::kA0 + (uint32_t)half * (kBK / 2) + lane_base;
     for (int i = 0; i < ntiles && go; ++i) {
+      const int kb0 = kb_first(i), kbs = kb_count(i), quads = (kbs + kQuad - 1) / kQuad;
       int64_t row = 0;
       uint32_t shift = 0;  // bits that a row's codes begin into a word
       if constexpr (kPath != kBulk) {
         // rows past the end are read as the last one, or as what is behind it, and not stored
-        const int t = first + i * step;
+        const int t = tile_of(i);
         const int64_t in_tile = (int64_t)(t % p.tiles_o) * p.tile_rows + row_in_tile;
         row = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows;
         if (kPath != kDirect)
@@ -656,12 +680,13 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
             read_packed(q, from, row_in_half, kBM, 2 * (odd + 2 * u), kPath == kPairs);
           } else {
             // blocks past the end of K are zeros; so is the slots' tile there
-            const uint8_t *wp = w.packed + row * half_cols + ((int64_t)kb << 5), *cp = w.codes + row * code_cols + ((int64_t)kb << 2);
+            const uint8_t *wp = w.packed + row * half_cols + ((int64_t)(kb0 + kb) << 5);
+            const uint8_t* cp = w.codes + row * code_cols + ((int64_t)(kb0 + kb) << 2);
             uint32_t c[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               c[e] = q[2 * e] = q[2 * e + 1] = 0u;
-              const bool on = (int64_t)kb * kBK + 16 * e < cols;
+              const bool on = (int64_t)(kb0 + kb) * kBK + 16 * e < cols;
               ld_8_ahead(on, wp + 8 * e, q[2 * e], q[2 * e + 1]);
               ld_1_ahead(on, cp + e, c[e]);
             }
@@ -724,10 +749,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     uint32_t s = 0, parity = 1;
     bool go = true;
     for (int i = 0; i < ntiles && go; ++i) {
-      const int t = first + i * step;
+      const int t = tile_of(i), quad0 = kb_first(i) / kQuad, quads = quad0 + (kb_count(i) + kQuad - 1) / kQuad;
       const int64_t row_a = (int64_t)p.plan.chunks[t / p.tiles_o].expert * p.rows + (int64_t)(t % p.tiles_o) * p.tile_rows;
       const int64_t row_b = row_a + (kMode == kModeDown ? kBM : 0), row = half ? row_b : row_a;
-      for (int quad = 0; quad < quads; ++quad) {
+      for (int quad = quad0; quad < quads; ++quad) {
         if (!mbar_wait_warp(&packed_empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
           go = false;
@@ -828,6 +853,12 @@ cudaError_t launch_gemm(int width, const void* v, int64_t slots, int64_t experts
   p.tile_rows = kMode == kModeDown ? 2 * kBM : kBM;
   p.tiles_o = (int32_t)((p.rows + p.tile_rows - 1) / p.tile_rows);
   p.kb_total = (int32_t)((p.cols + kBK - 1) / kBK);
+  // sqrt(cols / 1024) segments: two of 4096 columns, which lose 4e-7 of random sums and 1.0e-6 in one, and cost a training step
+  // 5 %.  More would gain little beside dh, whose sums are whole.
+  int wanted = 1;
+  while (kMode == kModeRaw && (int64_t)wanted * wanted * 1024 < p.cols) ++wanted;
+  p.kb_segment = ((p.kb_total + wanted - 1) / wanted + kQuad - 1) / kQuad * kQuad;
+  p.segments = (p.kb_total + p.kb_segment - 1) / p.kb_segment;
   const int64_t tiles = chunks * p.tiles_o;
   if (tiles * p.kb_total > INT32_MAX) return cudaErrorInvalidValue;
   switch (width) {
