@@ -418,8 +418,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   // tile, and the rows' amax) is waited for where it is read; the weights begin to come meanwhile.
 
   // The CTA's tile i.  In kModeRaw a tile's segments of K are tiles one after another, each summed up from zero and added to
-  // what the ones before left: the tensor cores cut off a sum's low bits at each step of 16 (of 256 steps of random numbers
-  // 1e-6 of it is lost, of positive ones 5e-6), and g and u are wanted as exact as fp32 sums are.
+  // what the ones before left (gate_up_segments).
   const int segments = kMode == kModeRaw ? p.segments : 1;
   const int tiles = p.plan.header[0] * p.tiles_o, step = (int)gridDim.x, first = (int)blockIdx.x;
   const int ntiles = tiles > first ? (tiles - first + step - 1) / step * segments : 0;
@@ -511,26 +510,20 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         // 32 outputs of a slot side by side, g with u
         float2* out = static_cast<float2*>(p.out) + (int64_t)(c.first + j0) * p.rows + o;
         const bool on = o < p.rows;
-        const auto put = [&](auto add) {
+        const bool add = kb_first(i) > 0;
 #pragma unroll
-          for (int j0 = 0; j0 < 16; j0 += 8) {
-            float2 before[8];  // all on their way before the first store
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              before[j] = decltype(add)::value && j0 + j < left && on ? out[(j0 + j) * p.rows] : make_float2(0.0f, 0.0f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float up = __shfl_sync(0xFFFFFFFFu, my_up, j0 + j), upn = have ? up : nan;
-              if (j0 + j < left && on)
-                out[(j0 + j) * p.rows] = make_float2(fmaf(__uint_as_float(a[j0 + j]), scale_a * upn, before[j].x),
-                                                     fmaf(__uint_as_float(b[j0 + j]), scale_b * upn, before[j].y));
-            }
+        for (int j = 0; j < 16; ++j) {
+          const float up = __shfl_sync(0xFFFFFFFFu, my_up, j), upn = have ? up : nan;
+          const float vg = __uint_as_float(a[j]) * (scale_a * upn), vu = __uint_as_float(b[j]) * (scale_b * upn);
+          if (j < left && on) {
+            // to what this thread wrote there before, in that order: no other adds
+            if (add)
+              asm volatile("red.relaxed.gpu.global.add.v2.f32 [%0], {%1, %2};" ::"l"(out), "f"(vg), "f"(vu) : "memory");
+            else
+              *out = make_float2(vg, vu);
           }
-        };
-        if (kb_first(i) > 0)
-          put(std::true_type{});
-        else
-          put(std::false_type{});
+          out += p.rows;
+        }
       } else {
         // 32 outputs of a slot side by side
         float* out = static_cast<float*>(p.out) + (int64_t)(c.first + j0) * p.rows + o;
@@ -853,10 +846,7 @@ cudaError_t launch_gemm(int width, const void* v, int64_t slots, int64_t experts
   p.tile_rows = kMode == kModeDown ? 2 * kBM : kBM;
   p.tiles_o = (int32_t)((p.rows + p.tile_rows - 1) / p.tile_rows);
   p.kb_total = (int32_t)((p.cols + kBK - 1) / kBK);
-  // sqrt(cols / 1024) segments: two of 4096 columns, which lose 4e-7 of random sums and 1.0e-6 in one, and cost a training step
-  // 5 %.  More would gain little beside dh, whose sums are whole.
-  int wanted = 1;
-  while (kMode == kModeRaw && (int64_t)wanted * wanted * 1024 < p.cols) ++wanted;
+  const int wanted = kMode == kModeRaw ? gate_up_segments(p.cols) : 1;
   p.kb_segment = ((p.kb_total + wanted - 1) / wanted + kQuad - 1) / kQuad * kQuad;
   p.segments = (p.kb_total + p.kb_segment - 1) / p.kb_segment;
   const int64_t tiles = chunks * p.tiles_o;

@@ -13,8 +13,9 @@
 // Bound by shared memory, which carries both operands, the packed blocks and the unpacking: of 128 bytes a
 // cycle, a K block takes some 1010 cycles at 128 slots against 512 of MMAs, and 1416 at 256 against 1024; so an expert
 // with enough slots takes 256 a tile, and the unpacking warps then take part in its epilogue.  4096 slots of 8 experts,
-// 4096 x 14336: first product 550 us (0.87 PFLOP/s; 28 % of it the epilogue, whose 65536 numbers a tile are some 45
-// instructions each), second 836 us (1.15 PFLOP/s), g and u 600 us (1.6 PFLOP/s).
+// 4096 x 14336: first product 737 us (550 without segments of K, 28 % of it the epilogue, whose 65536 numbers a tile are
+// some 45 instructions each; a segment more writes and reads dh in L2, with no second accumulator to go on with), second
+// 868 us (1.1 PFLOP/s), g and u 735 us (600 without segments).
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>
@@ -62,6 +63,8 @@ struct BackArgs {
   ExpertMatrix a, b;    // the weights of the first and the second half of K (down twice where there is one)
   int64_t rows, cols;   // of an expert's matrix: K and the outputs
   int32_t kb_part, parts, tiles_o, path;
+  int32_t segments, kb_segment;  // of kModeHidden: K's segments, and their K blocks (the last has fewer)
+  float* held;       // [positions, cols]: dh of the segments before
   int32_t splits;    // 2: the halves of K are tiles of their own, into part and more
   int64_t all_rows;  // of all experts
   int32_t activation;
@@ -182,14 +185,18 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   // tile, g and u) is waited for where it is read; the weights begin to come meanwhile.
 
   const int tiles = p.plan.header[0] * p.tiles_o * p.splits, step = (int)gridDim.x, first = (int)blockIdx.x;
-  const int ntiles = tiles > first ? (tiles - first + step - 1) / step : 0;
-  const int kbs = p.kb_part * p.parts / p.splits;
+  // in kModeHidden a tile's segments of K are tiles one after another (hidden_segments)
+  const int segments = kMode == kModeHidden ? p.segments : 1;
+  const int ntiles = tiles > first ? (tiles - first + step - 1) / step * segments : 0;
+  const int kb_all = p.kb_part * p.parts / p.splits;
+  const auto kb_first = [&](int i) { return kMode == kModeHidden ? i % segments * p.kb_segment : 0; };
+  const auto kb_count = [&](int i) { return kMode == kModeHidden ? min(p.kb_segment, kb_all - kb_first(i)) : kb_all; };
   // the CTA's tile i: split, chunk, outputs
   struct Where {
     int split, chunk, to;
   };
   const auto where = [&](int i) {
-    const int t = first + i * step, u = t / p.splits;
+    const int t = first + (kMode == kModeHidden ? i / segments : i) * step, u = t / p.splits;
     return Where{t - u * p.splits, u / p.tiles_o, u % p.tiles_o};
   };
   const uint32_t quarter = (uint32_t)(warp & 3), lane_base = (quarter * 32u) << 16;
@@ -212,9 +219,11 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     const float sg = kMode == kModeHidden ? p.gate_scale[c.expert] : 0.0f, su = kMode == kModeHidden ? p.up_scale[c.expert] : 0.0f;
     const float nan = __int_as_float(0x7FC00000);
     const int each = (c.count + 7) / 8, pieces = kHalves * each;
+    const int segment = kMode == kModeHidden ? i % segments : 0;
+    const bool last = segment == segments - 1;
     float g[8], u[8];
     const auto fetch = [&](int piece) {
-      if (kMode != kModeHidden || piece >= pieces) return;
+      if (kMode != kModeHidden || piece >= pieces || !last) return;
       const int half = piece >= each ? 1 : 0, j0 = (piece - half * each) * 8;
       const int64_t o = (int64_t)to * (kHalves * kBM) + half * kBM + quarter * 32 + lane;
       const float2* raw = p.raw + (int64_t)(c.first + j0) * p.cols + o;
@@ -235,12 +244,34 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       const bool on = o < p.cols;
       uint32_t a[8];
       tmem_ld_32x32b_x8(d + (uint32_t)(half * kN + j0), a);
-      if constexpr (kMode == kModeHidden) {
-        // lane j: slot j's weight times G's and U's scales, and the power of two of its row of dy times D's
-        const float my_w = lane < left ? p.weights[p.plan.slot_of[pos + lane]] : 0.0f, my_g = my_w * sg, my_u = my_w * su;
+      if (kMode == kModeHidden && segments > 1) {
+        // the segment's dh to what the thread left there of those before
+        float* held = p.held + pos * p.cols + o;
+        float before[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) before[j] = segment > 0 && j < left && on ? held[j * p.cols] : 0.0f;
         const float my_up = !have ? nan : lane < left ? scale * exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
         tmem_ld_wait();
         if (piece + kWorkers >= pieces) release(acc);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float dh = fmaf(__uint_as_float(a[j]), __shfl_sync(0xFFFFFFFFu, my_up, j), before[j]);
+          if (last)
+            a[j] = __float_as_uint(dh);
+          else if (j < left && on)
+            held[j * p.cols] = dh;
+        }
+        if (!last) continue;
+      }
+      if constexpr (kMode == kModeHidden) {
+        // lane j: slot j's weight times G's and U's scales, and the power of two of its row of dy times D's
+        const float my_w = lane < left ? p.weights[p.plan.slot_of[pos + lane]] : 0.0f, my_g = my_w * sg, my_u = my_w * su;
+        float my_up = 1.0f;
+        if (segments == 1) {
+          my_up = !have ? nan : lane < left ? scale * exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
+          tmem_ld_wait();
+          if (piece + kWorkers >= pieces) release(acc);
+        }
         float dot[8], dg[8], du[8];
         // (outputs past the end have g = u = 0, and are not stored)
         const auto factors = [&](auto kind) {
@@ -293,7 +324,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     for (int i = 0; i < ntiles && go; ++i) {
       const Where at = where(i);
       const Chunk c = p.plan.chunks[at.chunk];
-      for (int kb = 0; kb < kbs; ++kb) {
+      const int kb1 = kb_first(i) + kb_count(i);
+      for (int kb = kb_first(i); kb < kb1; ++kb) {
         if (!mbar_wait_warp(&empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
           go = false;
@@ -314,6 +346,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     bool ok = true;
     for (int i = 0; i < ntiles && ok; ++i) {
       const Chunk c = p.plan.chunks[where(i).chunk];
+      const int kbs = kb_count(i);
       const uint32_t slots = (uint32_t)((c.count + 15) & ~15);
       const uint32_t idesc = warp_uniform((kMode == kModeHidden ? idesc_f16_f32(kBM, slots) : idesc_bf16_f32(kBM, slots)) | 1u << 15);
       const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc;
@@ -362,7 +395,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     // blocks of all tiles, one after another: this group's are group, group + 2, ...
     int kb = group;
     uint32_t block = (uint32_t)group;
-    for (int i = 0; i < ntiles && go; ++i, kb -= kbs) {
+    for (int i = 0; i < ntiles && go; kb -= kb_count(i), ++i) {
+      const int kbs = kb_count(i), kb0 = kb_first(i);
       const Where at = where(i);
       const int64_t e = p.plan.chunks[at.chunk].expert, o0 = (int64_t)at.to * (kHalves * kBM) + part64 * 64;
       const int64_t row0 = e * p.rows + row;
@@ -389,7 +423,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           // rows past the end of K are read as the last one (the slots' tile is zeros there), outputs past the end are zeros, and not
           // stored
           const int part = at.split || kb >= p.kb_part ? 1 : 0;
-          const int64_t f = e * p.rows + min((int64_t)(kb - (kb >= p.kb_part ? p.kb_part : 0)) * kBK + row, p.rows - 1);
+          const int64_t f = e * p.rows + min((int64_t)(kb0 + kb - (kb >= p.kb_part ? p.kb_part : 0)) * kBK + row, p.rows - 1);
           const uint8_t *wp = (part ? p.b.packed : p.a.packed) + f * half_cols + (o0 >> 1),
                         *cp = (part ? p.b.codes : p.a.codes) + f * code_cols + (o0 >> 4);
           uint32_t c[4];
@@ -450,7 +484,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       const Where at = where(i);
       const int to = at.to;
       const int64_t row0 = (int64_t)p.plan.chunks[at.chunk].expert * p.rows;
-      for (int kb = 0; kb < kbs; ++kb) {
+      const int kb1 = kb_first(i) + kb_count(i);
+      for (int kb = kb_first(i); kb < kb1; ++kb) {
         if (!mbar_wait_warp(&packed_empty[s], parity)) {
           if (lane == 0) atomicOr(failed, 1u);
           go = false;
@@ -536,8 +571,11 @@ template <int kMode>
 cudaError_t launch_back(int width, const void* v, int parts, int64_t experts, BackArgs& p, int64_t chunks, int64_t expected, int sms,
                         cudaStream_t stream) {
   p.parts = parts;
-  p.splits = 1;
   p.kb_part = (int32_t)((p.rows + kBK - 1) / kBK);
+  p.splits = 1;
+  const int wanted = kMode == kModeHidden ? hidden_segments(p.rows) : 1;
+  p.kb_segment = (p.kb_part + wanted - 1) / wanted;
+  p.segments = (p.kb_part + p.kb_segment - 1) / p.kb_segment;
   p.tiles_o = (int32_t)((p.cols + kHalves * kBM - 1) / (kHalves * kBM));
   int64_t tiles = chunks * p.tiles_o;
   // G's and U's rows as tiles of their own where that fills the last round of tiles better (by more than the second
@@ -563,6 +601,7 @@ inline int back_width(int64_t slots, int64_t experts) {
   return each <= 24 ? 32 : each <= 56 ? 64 : each <= 144 ? 128 : 256;
 }
 inline int64_t raw_bytes(int64_t slots, int64_t n, int64_t inner) { return round256(slots * std::max(8 * inner, 4 * n)); }
+inline int64_t held_bytes(int64_t slots, int64_t n, int64_t inner) { return hidden_segments(n) > 1 ? round256(slots * inner * 4) : 0; }
 inline int64_t dot_parts(int64_t inner) { return (inner + kHalves * kBM - 1) / (kHalves * kBM) * kHalves * 4; }
 
 }  // namespace
@@ -570,9 +609,9 @@ inline int64_t dot_parts(int64_t inner) { return (inner + kHalves * kBM - 1) / (
 int64_t experts_backward_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
   const int64_t slots = tokens * k;
   // x and dy in order, whose place the slots' parts of dx take afterwards; g and u, whose place a second sum of them takes;
-  // the factors; the dots
+  // the factors; the dots; dh of K's segments before the last
   return experts_plan_bytes(slots, experts) + 2 * round256(slots * 4) + 2 * round256(slots * n * 2) + raw_bytes(slots, n, inner) + round256(slots * inner * 4) +
-         round256(dot_parts(inner) * slots * 4);
+         round256(dot_parts(inner) * slots * 4) + held_bytes(slots, n, inner);
 }
 
 cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const Routing& r, const Experts& w,
@@ -602,6 +641,7 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   p.raw = reinterpret_cast<const float2*>(raw), p.gate_scale = w.gate.scale, p.up_scale = w.up.scale, p.slots = slots;
   p.factors = dx != nullptr ? reinterpret_cast<__nv_bfloat16*>(factors) : nullptr;
   p.dots = dweights != nullptr ? reinterpret_cast<float*>(dots) : nullptr;
+  p.held = reinterpret_cast<float*>(dots + round256(dot_parts(w.inner) * slots * 4));
   if ((err = launch_back<kModeHidden>(wide_width, dys, 1, w.count, p, chunks, expected, info.sm_count, stream)) != cudaSuccess) return err;
   if (dx != nullptr) {
     p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.part = reinterpret_cast<float*>(xs), p.more = reinterpret_cast<float*>(raw);

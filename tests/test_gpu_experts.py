@@ -114,6 +114,28 @@ def test_experts_backward(t, n, inner, count, k, kind):
     assert hs.hscale_device_error_flags() == 0
 
 
+@pytest.mark.parametrize("t, n, inner, count, k", [(90, 4176, 272, 3, 2), (20, 5632, 144, 6, 2), (700, 8192, 80, 2, 2), (40, 1424, 528, 2, 3)])
+@pytest.mark.parametrize("packed_by, codes_by", [(0, 0), (8, 4), (16, 1)])
+def test_backward_of_long_rows(t, n, inner, count, k, packed_by, codes_by):
+    """g, u and dh are summed in parts: dweights is as exact from long rows as from short ones."""
+    x, ids, w, gate, up, down = layer(t, n, inner, count, k, seed=n)
+    gate, up, down = (moved(m, packed_by, codes_by) for m in (gate, up, down))
+    dy, _ = rows(t, n, 16, torch.Generator().manual_seed(8), 0.1)
+    dx, dw = backward(dy, x, ids, w, gate, up, down, 0)
+    want_dx, tol_dx, want_dw, tol_dw = experts_backward(dy.cpu(), x.cpu(), ids.cpu(), clean(w), gate, up, down, 0)
+    assert ((dx.cpu().double() - want_dx).abs() <= tol_dx).all()
+    assert ((dw.cpu().double() - want_dw).abs() <= tol_dw).all()
+    # An accumulator of fp32 that is cut off toward zero at each step of 16: half a unit of 2^-23 on average, 0.72 of it relative
+    # to the sum (a mantissa's mean reciprocal), and the partial sums of random products grow as a square root: of m steps
+    # 0.36 2^-23 sum_j sqrt(j / m) = 0.48 m 2^-24.  Parts of at most 1408 columns of g and u and of 2048 of dh: m = 88, 88 and
+    # 128, together 146 2^-24, however long the rows are.  The roundings of the parts' sums, of the activation, of the
+    # products and of their sum over inner, each random: less than 14 2^-24.
+    assert (dw.cpu().double() - want_dw).norm() <= want_dw.norm() * 160 * 2.0 ** -24
+    again = backward(dy, x, ids, w, gate, up, down, 0)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+    assert hs.hscale_device_error_flags() == 0
+
+
 @pytest.mark.parametrize("t", [1, 20, 200])
 def test_tokens_do_not_meet(t):
     """Inf and NaN in some rows, some weights and the factors of an expert that few tokens are on stay with them."""
