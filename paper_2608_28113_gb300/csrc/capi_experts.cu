@@ -3,6 +3,7 @@
 // Every entry point validates its arguments on the host before enqueueing anything.  No exception crosses the ABI.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -42,12 +43,21 @@ inline int check_rows(const void* x, int64_t rows, int64_t cols, int64_t ld) {
   return aligned(x, 16) && ld % 8 == 0 ? HSCALE_OK : HSCALE_ERR_ALIGN;
 }
 
+// Whether an int64 holds every product of these sizes and an int32 the number of tiles' blocks (128 x 128, four products of
+// them at most); beyond it the operands are terabytes.
+inline bool experts_fit(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
+  constexpr int64_t kMost = (int64_t)1 << 40;
+  if (tokens > INT32_MAX / 32 || k > 32 || experts > hscale::kRouteExperts || n > INT32_MAX || inner > INT32_MAX / 2) return false;
+  const int64_t slots = tokens * k, blocks = ((n + 127) / 128) * ((inner + 127) / 128);
+  const int64_t chunks = hscale::plan_chunks(slots, experts, hscale::experts_width(slots, experts));
+  return slots <= kMost / std::max(n, inner) && n <= (kMost << 10) / inner / experts && blocks <= INT32_MAX / 8 / chunks;
+}
+
 inline int check_experts(int64_t tokens, int64_t n, int64_t k, const int32_t* ids, const float* weights,
                          const hscale::Experts& w, int32_t activation) {
   if (activation != HSCALE_ACT_SILU && activation != HSCALE_ACT_GELU_TANH) return HSCALE_ERR_ARG;
   if (n < 0 || w.inner < 0 || n % 16 != 0 || w.inner % 16 != 0 || n > INT32_MAX || w.inner > INT32_MAX / 2) return HSCALE_ERR_SHAPE;
-  // sizes whose product, with the slots or the experts, an int64 holds
-  if (tokens > 0 && n > 0 && n > INT64_MAX / 16 / 32 / tokens) return HSCALE_ERR_SHAPE;
+  if (tokens > 0 && n > 0 && w.inner > 0 && !experts_fit(tokens, k, n, w.inner, w.count)) return HSCALE_ERR_SHAPE;
   if (tokens == 0 || n == 0 || w.inner == 0) return HSCALE_OK;
   if (ids == nullptr || weights == nullptr) return HSCALE_ERR_NULL;
   if (!aligned(ids, 4) || !aligned(weights, 4)) return HSCALE_ERR_ALIGN;
@@ -113,6 +123,7 @@ int hscale_route_backward(const void* logits, int32_t type, int64_t tokens, int6
 
 size_t hscale_experts_workspace_bytes(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
   if (tokens <= 0 || k <= 0 || n <= 0 || inner <= 0 || experts <= 0) return 0;
+  if (!experts_fit(tokens, k, n, inner, experts)) return SIZE_MAX;  // which no call takes
   return (size_t)hscale::experts_workspace(tokens, k, n, inner, experts);
 }
 
@@ -138,6 +149,7 @@ int hscale_experts(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, 
 
 size_t hscale_experts_backward_workspace_bytes(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
   if (tokens <= 0 || k <= 0 || n <= 0 || inner <= 0 || experts <= 0) return 0;
+  if (!experts_fit(tokens, k, n, inner, experts)) return SIZE_MAX;  // which no call takes
   return (size_t)hscale::experts_backward_workspace(tokens, k, n, inner, experts);
 }
 

@@ -53,6 +53,10 @@ LAYER = [(dict(tokens=-1), ERR_SHAPE), (dict(n=72, ld_x=72, ld_y=72, ld_dy=72, l
          (dict(weights=None), ERR_NULL), (dict(ids=P + 1), ERR_ALIGN), (dict(weights=P + 2), ERR_ALIGN), (dict(x=None), ERR_NULL),
          (dict(x=P + 8), ERR_ALIGN), (dict(ld_x=56), ERR_SHAPE), (dict(ld_x=68), ERR_ALIGN), (dict(ws=None), ERR_WS),
          (dict(ws_bytes=255), ERR_WS), (dict(ws=P + 16), ERR_WS), (dict(tokens=1 << 26, n=1 << 30, ld_x=1 << 30), ERR_SHAPE)]
+# slots times inner, the weights, and the tiles' blocks past what the kernels count
+WIDE = dict(ld_x=1 << 24, ld_y=1 << 24, ld_dy=1 << 24, ld_dx=1 << 24, ws_bytes=(1 << 64) - 1)
+LAYER += [(dict(tokens=(1 << 26) - 1, k=32, inner=1 << 30, **WIDE), ERR_SHAPE), (dict(n=1 << 24, inner=1 << 24, experts=1024, **WIDE), ERR_SHAPE),
+          (dict(tokens=1 << 16, k=1, n=1 << 20, inner=1 << 20, experts=1, **WIDE), ERR_SHAPE)]
 LAYER += [({name: None}, ERR_NULL) for name in WEIGHTS]
 LAYER += [({f"{m}_packed": P + 4}, ERR_ALIGN) for m in ("gate", "up", "down")]
 LAYER += [({f"{m}_scale": P + 2}, ERR_ALIGN) for m in ("gate", "up", "down")]
@@ -83,6 +87,7 @@ def test_workspace_queries(lib):
         assert f(4, 2, 64, 32, 4) > 0
         assert f(4096, 8, 4096, 2048, 64) >= f(4096, 8, 4096, 2048, 1) - 4096 * 8
         assert f(1 << 26, 32, 1 << 14, 1 << 14, 64) > 1 << 46  # no overflow into a small number
+        assert f((1 << 26) - 1, 32, 16, 1 << 30, 64) > 1 << 46 and f(1 << 62, 32, 64, 64, 4) > 1 << 46
     # what a call of fewer tokens needs is no more
     sizes = [hs.hscale_experts_workspace_bytes(t, 8, 512, 256, 64) for t in range(1, 300)]
     assert all(a <= b for a, b in zip(sizes, sizes[1:]))
