@@ -613,7 +613,7 @@ typedef enum hscale_activation { HSCALE_ACT_SILU = 0, HSCALE_ACT_GELU_TANH = 1 }
  * not depend on the batch that it is in.
  *
  * n and inner are multiples of 16, experts at most 1024, k at most 32.  x and y are 16-byte aligned, ld_x and ld_y
- * multiples of 8, packed weights 8-byte aligned.  With inner == 0, y is zero.  The workspace is 256-byte aligned; calls
+ * multiples of 8, packed weights 8-byte aligned; y may be x itself.  With inner == 0, y is zero.  The workspace is 256-byte aligned; calls
  * that may overlap need their own.
  */
 size_t hscale_experts_workspace_bytes(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts);
@@ -629,7 +629,7 @@ int hscale_experts(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, 
  *   dx_t = sum_j w_tj (G_e^T (dh * u * act'(g)) + U_e^T (dh * act(g)))  (bf16, rows ld_dx elements apart)
  * with g = G_e x_t, u = U_e x_t and h = act(g) * u made again from x.  The weights are frozen, and have no gradient.
  * dx or dweights may be NULL: it is then not computed.  dh and the factors beside it are fp32, their products are rounded to bf16
- * before G_e^T and U_e^T.  The rest is as in hscale_experts.
+ * before G_e^T and U_e^T.  dx may be dy or x itself.  The rest is as in hscale_experts.
  */
 size_t hscale_experts_backward_workspace_bytes(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts);
 int hscale_experts_backward(const void* dy_bf16, int64_t tokens, int64_t n, int64_t ld_dy, const void* x_bf16, int64_t ld_x,
@@ -645,7 +645,7 @@ int hscale_experts_backward(const void* dy_bf16, int64_t tokens, int64_t n, int6
  *   out_i = tensors_i * min(1, max_norm / norm)
  * tensors, out, sizes (elements) and types (hscale_type) are HOST arrays of `count`; what tensors and out point to is on
  * the device, contiguous and aligned to its type (to 16 bytes: faster).  out == NULL scales in place; out_i has the type of
- * tensors_i.  Where the norm is not finite nothing is scaled (out_i = tensors_i): the caller sees it in *norm.  Squares that
+ * tensors_i, and is tensors_i itself or overlaps none of them.  Where the norm is not finite nothing is scaled (out_i = tensors_i): the caller sees it in *norm.  Squares that
  * leave fp32's range are not lost; the sum is fp64 across CTAs, and equal calls give equal bits.  count == 0: the norm
  * is 0.  The arrays are read before the call returns, so a captured call keeps what they held.
  */

@@ -229,7 +229,7 @@ cudaError_t run(const void* const* in, void* const* out, const int64_t* sizes, c
       for (; i < count && n < kTensors; ++i) {
         const int64_t p = (sizes[i] + kPiece - 1) / kPiece;
         if (p == 0) continue;
-        if (pieces + p > INT32_MAX) {
+        if (pieces + p > ((int64_t)1 << 30)) {  // a piece's number and a grid's step stay within 32 bits
           if (n == 0) return cudaErrorInvalidValue;
           break;
         }

@@ -260,6 +260,22 @@ def test_weights_at_any_address(t, n, inner, packed_by, codes_by):
     assert torch.equal(dx, want_dx) and torch.equal(dw, want_dw)
 
 
+@pytest.mark.parametrize("t", [3, 40, 300])
+def test_in_place(t):
+    """y over x, and dx over dy and over x."""
+    x, ids, w, gate, up, down = layer(t, 272, 144, 4, 2, seed=31)
+    dy, _ = rows(t, 272, 0, torch.Generator().manual_seed(2))
+    want, (want_dx, want_dw) = run(x, ids, w, gate, up, down, 0), backward(dy, x, ids, w, gate, up, down, 0)
+    y = x.clone()
+    hs.hscale_experts(y, ids, w, gate, up, down, 0, y)
+    assert torch.equal(y, want)
+    for onto_x in (False, True):
+        dw, a, b = torch.zeros_like(w), dy.clone(), x.clone()
+        dx = b if onto_x else a
+        hs.hscale_experts_backward(a, b, ids, w, gate, up, down, 0, dx, dw)
+        assert torch.equal(dx, want_dx) and torch.equal(dw, want_dw)
+
+
 def test_two_calls_at_once():
     """Calls on two streams, each with its own workspace."""
     sets = [layer(t, 512, 256, 8, 2, seed=t) for t in (8, 8, 200, 200)]
