@@ -242,13 +242,26 @@ __global__ void __launch_bounds__(256) spread_kernel(Spread first, Spread second
   }
 }
 
-// h, bf16, to fp16 in place (experts.cuh), 16 bytes a thread.
-__global__ void __launch_bounds__(256) convert_kernel(uint4* h, int64_t pieces, Plan plan, const uint32_t* amax) {
-  pdl_launch_dependents();  // the second product's weights may come; it waits for this kernel before it reads h
+// Rows of fp16 from their groups' powers of two to the row's, in place, 16 bytes a thread: exact but where a number is below
+// 2^-14 then.  A row is `pieces` of 16 bytes in parts of `part`, which have the same groups.  What is there already (a third to a
+// half of the groups) is neither read nor written.
+__global__ void __launch_bounds__(256) level_kernel(uint4* h, int64_t pieces, int64_t part, Plan plan, const uint32_t* amax, const int8_t* groups) {
+  pdl_launch_dependents();  // the next product's weights may come; it waits for this kernel before it reads h
   pdl_wait_primary();
-  const int64_t total = plan.header[1] * pieces;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256)
-    h[i] = bf16_to_f16(h[i], exp2_int(-row_exponent(amax[i / pieces])));
+  const int64_t total = plan.header[1] * pieces, per = (part + 3) / 4;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / pieces;
+    const uint32_t at = (uint32_t)(i - row * pieces);
+    const int e = (int)groups[row * per + at % (uint32_t)part / 4] - row_exponent(amax[row]);
+    if (e == 0) continue;
+    const float f = exp2_int(max(e, -126));
+    const uint4 v = h[i];
+    const auto move = [&](uint32_t w) {
+      const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&w));
+      return pack_f16(x.x * f, x.y * f);
+    };
+    h[i] = make_uint4(move(v.x), move(v.y), move(v.z), move(v.w));
+  }
 }
 
 // out_t = the sum of the token's slots' rows (part, and more where it is not nullptr) times their weights (nullptr: 1), in order;
@@ -340,6 +353,7 @@ struct GemmArgs {
   Plan plan;
   const uint32_t* amax;  // of each position's row of the slots' tile
   uint32_t* h_amax;      // of each position's h
+  int8_t* h_groups;      // [positions, level_groups(rows)] powers of two of h
   void* out;
 };
 
@@ -470,41 +484,49 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       // the warp's last columns: the next tile's MMAs need not wait for what is done with them
       if (j0 + 16 * kWorkers >= c.count) release(acc);
       if constexpr (kMode == kModeHidden) {
-        // rounded and turned, so that a lane stores 8 outputs of a slot at once
-        __syncwarp();
+        // rounded (lane j: slot j's power of two) and turned, so that a lane stores 8 outputs of a slot at once
         const float my_a = have ? my_up * scale_a : nan, my_b = my_up * scale_b;
         const auto hidden = [&](auto kind) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float h[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              h[e] = activate_fast<decltype(kind)::value>(__uint_as_float(a[2 * j + e]) * __shfl_sync(0xFFFFFFFFu, my_a, 2 * j + e)) *
-                     (__uint_as_float(b[2 * j + e]) * __shfl_sync(0xFFFFFFFFu, my_b, 2 * j + e));
-            turn[j * 32 + lane] = pack_bf16(h[0], h[1]);
-          }
+          for (int j = 0; j < 16; ++j)
+            a[j] = __float_as_uint(activate_fast<decltype(kind)::value>(__uint_as_float(a[j]) * __shfl_sync(0xFFFFFFFFu, my_a, j)) *
+                                   (__uint_as_float(b[j]) * __shfl_sync(0xFFFFFFFFu, my_b, j)));
         };
         if (p.activation == kActSilu)
           hidden(std::integral_constant<int, kActSilu>{});
         else
           hidden(std::integral_constant<int, kActGeluTanh>{});
+        uint32_t most = 0u;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, o < p.rows ? a[j] & 0x7FFFFFFFu : 0u);
+          if (lane == j) most = m >> 16;
+        }
+        const int e = row_exponent(most);
+        const float down = exp2_int(-e);
+        const int64_t at32 = o0 + quarter * 32;
+        if (lane < left && at32 < p.rows) {
+          const int64_t pos = c.first + j0 + lane;
+          p.h_groups[pos * level_groups(p.rows) + at32 / kLevel] = (int8_t)e;
+          atomicMax(&p.h_amax[pos], most);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          turn[j * 32 + lane] = pack_f16(__uint_as_float(a[2 * j]) * __shfl_sync(0xFFFFFFFFu, down, 2 * j),
+                                         __uint_as_float(a[2 * j + 1]) * __shfl_sync(0xFFFFFFFFu, down, 2 * j + 1));
         __syncwarp();
         const int pair = lane >> 2;
         const uint4 q0 = reinterpret_cast<const uint4*>(turn)[2 * lane], q1 = reinterpret_cast<const uint4*>(turn)[2 * lane + 1];
-        const int64_t at = o0 + quarter * 32 + (lane & 3) * 8;
+        const int64_t at = at32 + (lane & 3) * 8;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const uint32_t pick = e ? 0x7632u : 0x5410u;
           const uint4 r = make_uint4(__byte_perm(q0.x, q0.y, pick), __byte_perm(q0.z, q0.w, pick), __byte_perm(q1.x, q1.y, pick),
                                      __byte_perm(q1.z, q1.w, pick));
           // rows are a multiple of 16: 8 outputs are all there or none is
-          const bool on = 2 * pair + e < left && at < p.rows;
           const int64_t pos = c.first + j0 + 2 * pair + e;
-          if (on) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + pos * p.rows + at) = r;
-          uint32_t m = on ? amax_bf16(r) : 0u;
-          m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-          m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-          if (on && (lane & 3) == 0) atomicMax(&p.h_amax[pos], m);
+          if (2 * pair + e < left && at < p.rows) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + pos * p.rows + at) = r;
         }
       } else if constexpr (kMode == kModeRaw) {
         // 32 outputs of a slot side by side, g with u
@@ -938,6 +960,16 @@ cudaError_t launch_experts_spread(const void* x, int64_t ld, void* out, uint32_t
                         h_amax);
 }
 
+// h: [positions, parts, cols] of fp16, groups: [positions, level_groups(cols)]
+cudaError_t launch_experts_level(void* h, int64_t slots, int64_t cols, int parts, const Plan& plan, const uint32_t* amax, const int8_t* groups,
+                                 cudaStream_t stream) {
+  DeviceInfo info;
+  const cudaError_t err = current_device_info(&info);
+  if (err != cudaSuccess) return err;
+  const int64_t pieces = parts * (cols / 8), blocks = std::min<int64_t>(8 * info.sm_count, (slots * pieces + 255) / 256);
+  return launch_chained(level_kernel, dim3((unsigned)blocks), 256, 0, stream, static_cast<uint4*>(h), pieces, cols / 8, plan, amax, groups);
+}
+
 cudaError_t launch_experts_combine(const float* part, const float* more, const Routing& r, const float* weights, const Plan& plan, int64_t n,
                                    void* out, int64_t ld, const float* dots, int parts, float* dweights, cudaStream_t stream) {
   const Combine c = {part, more, weights, static_cast<__nv_bfloat16*>(out), n, ld, r.tokens, r.k, dots, parts, dweights};
@@ -958,7 +990,7 @@ cudaError_t launch_experts_raw(const void* xs, const uint32_t* amax, int64_t slo
 int64_t experts_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
   const int64_t slots = tokens * k;
   return experts_plan_bytes(slots, experts) + 2 * round256(slots * 4) + round256(slots * n * 2) + round256(slots * inner * 2) +
-         round256(slots * n * 4);
+         round256(slots * n * 4) + round256(slots * level_groups(inner));
 }
 
 cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const Experts& w, void* y, int64_t ld_y, void* workspace,
@@ -975,16 +1007,15 @@ cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const 
   uint8_t* xs = at + 2 * round256(slots * 4);
   uint8_t* h = xs + round256(slots * w.n * 2);
   float* part = reinterpret_cast<float*>(h + round256(slots * w.inner * 2));
+  int8_t* groups = reinterpret_cast<int8_t*>(part) + round256(slots * w.n * 4);
   const int64_t chunks = plan_chunks(slots, w.count, width);
   if ((err = launch_experts_plan(r, w.count, width, plan, width, nullptr, stream)) != cudaSuccess) return err;
   if ((err = launch_experts_spread(x, ld_x, xs, amax, nullptr, 0, nullptr, nullptr, w.n, r, plan, h_amax, stream)) != cudaSuccess) return err;
   GemmArgs p = {};
   p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan;
-  p.amax = amax, p.h_amax = h_amax, p.out = h;
+  p.amax = amax, p.h_amax = h_amax, p.h_groups = groups, p.out = h;
   if ((err = launch_gemm<kModeHidden>(width, xs, slots, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
-  const int64_t blocks = std::min<int64_t>(8 * info.sm_count, (slots * (w.inner / 8) + 255) / 256);
-  err = launch_chained(convert_kernel, dim3((unsigned)blocks), 256, 0, stream, reinterpret_cast<uint4*>(h), w.inner / 8, plan, h_amax);
-  if (err != cudaSuccess) return err;
+  if ((err = launch_experts_level(h, slots, w.inner, 1, plan, h_amax, groups, stream)) != cudaSuccess) return err;
   p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.amax = h_amax, p.out = part;
   if ((err = launch_gemm<kModeDown>(width, h, slots, w.count, p, chunks, info.sm_count, stream)) != cudaSuccess) return err;
   return launch_experts_combine(part, nullptr, r, r.weights, plan, w.n, y, ld_y, nullptr, 0, nullptr, stream);

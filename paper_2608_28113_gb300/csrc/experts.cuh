@@ -228,6 +228,15 @@ __device__ __forceinline__ uint32_t bf16_to_f16(uint32_t v, float down) {
 __device__ __forceinline__ uint4 bf16_to_f16(const uint4& v, float down) {
   return make_uint4(bf16_to_f16(v.x, down), bf16_to_f16(v.y, down), bf16_to_f16(v.z, down), bf16_to_f16(v.w, down));
 }
+// h and the factors of dx, made in fp32, are rounded to fp16 as they are made, 32 outputs of a slot under their own power of
+// two E (a row's largest is not known yet), and moved under the row's afterwards (launch_experts_level): 11 bits, and as
+// above a number loses more only below 2^-29 of its row's largest.  (As bf16 they were half of y's and dx's error.)
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+constexpr int kLevel = 32;  // outputs under one power of two
+inline __host__ __device__ int64_t level_groups(int64_t cols) { return (cols + kLevel - 1) / kLevel; }
 // the largest magnitude of eight bf16 numbers, as bits
 __device__ __forceinline__ uint32_t amax_bf16(const uint4& v) {
   const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));

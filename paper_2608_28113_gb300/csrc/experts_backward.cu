@@ -70,24 +70,16 @@ struct BackArgs {
   int32_t activation;
   Plan plan;
   const float* weights;
-  const uint32_t* amax;      // of each position's dy
+  const uint32_t* amax;      // of each position's dy, or of its factors
   const float2* raw;         // g and u, [positions, cols]
   const float *gate_scale, *up_scale;
-  __nv_bfloat16* factors;    // [positions, 2, cols], or nullptr
+  uint16_t* factors;         // fp16 [positions, 2, cols], or nullptr
+  int8_t* groups;            // [positions, level_groups(cols)] powers of two of the factors, and the rows' amax
+  uint32_t* factor_amax;
   float* dots;               // [8 tiles_o, slots] partial sums of h . dh, or nullptr
   int64_t slots;
   float *part, *more;        // [slots, cols]
 };
-
-__device__ __forceinline__ void unpack8(uint32_t w, uint32_t scale, uint32_t (&r)[4]) {
-  constexpr uint32_t kSign = 0x80008000u, kMag = 0x01C001C0u;
-  const uint32_t up = w << 4;
-  const uint32_t a = __byte_perm(up, w, 0x5410), b = __byte_perm(up, w, 0x7632);
-  r[0] = mul_bf16x2(((a << 8) & kSign) | ((a << 2) & kMag), scale);
-  r[1] = mul_bf16x2((a & kSign) | ((a >> 6) & kMag), scale);
-  r[2] = mul_bf16x2(((b << 8) & kSign) | ((b << 2) & kMag), scale);
-  r[3] = mul_bf16x2((b & kSign) | ((b >> 6) & kMag), scale);
-}
 
 // Eight columns' sums over a warp's lanes: every lane has that of column_of(lane).
 __device__ __forceinline__ float sum_columns(float (&v)[8], int lane) {
@@ -105,12 +97,14 @@ __device__ __forceinline__ float sum_columns(float (&v)[8], int lane) {
 }
 __device__ __forceinline__ int column_of(int lane) { return lane >> 2; }
 
-// Eight slots of 32 outputs (a slot's in neighbouring lanes) rounded and stored, 8 outputs of a slot a lane.
-__device__ __forceinline__ void store_rows(const float (&v)[8], uint32_t* turn, __nv_bfloat16* out, int64_t stride, int64_t at0,
+// Eight slots of 32 outputs (a slot's in neighbouring lanes) times the power of two in lane j, rounded to fp16 and stored,
+// 8 outputs of a slot a lane.
+__device__ __forceinline__ void store_rows(const float (&v)[8], float down, uint32_t* turn, uint16_t* out, int64_t stride, int64_t at0,
                                            int64_t cols, int left, int lane) {
   __syncwarp();
 #pragma unroll
-  for (int j = 0; j < 4; ++j) turn[j * 32 + lane] = pack_bf16(v[2 * j], v[2 * j + 1]);
+  for (int j = 0; j < 4; ++j)
+    turn[j * 32 + lane] = pack_f16(v[2 * j] * __shfl_sync(0xFFFFFFFFu, down, 2 * j), v[2 * j + 1] * __shfl_sync(0xFFFFFFFFu, down, 2 * j + 1));
   __syncwarp();
   const int odd = lane >> 4, j = 2 * ((lane >> 2) & 3) + odd;
   const uint4 q0 = reinterpret_cast<const uint4*>(turn)[2 * (lane & 15)], q1 = reinterpret_cast<const uint4*>(turn)[2 * (lane & 15) + 1];
@@ -119,7 +113,7 @@ __device__ __forceinline__ void store_rows(const float (&v)[8], uint32_t* turn, 
                              __byte_perm(q1.z, q1.w, pick));
   const int64_t at = at0 + (lane & 3) * 8;
   // cols is a multiple of 16: 8 outputs are all there or none is
-  if (j < left && at < cols) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(out) + j * stride + at) = r;
+  if (j < left && at < cols) *reinterpret_cast<uint4*>(out + j * stride + at) = r;
 }
 
 __device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[8]) {
@@ -215,7 +209,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     const int to = at.to;
     const Chunk c = p.plan.chunks[at.chunk];
     const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc + lane_base;
-    const float scale = kMode == kModeHidden ? p.a.scale[c.expert] : kWeightUnit;
+    const float scale = kMode == kModeHidden ? p.a.scale[c.expert] : 1.0f;
     const float sg = kMode == kModeHidden ? p.gate_scale[c.expert] : 0.0f, su = kMode == kModeHidden ? p.up_scale[c.expert] : 0.0f;
     const float nan = __int_as_float(0x7FC00000);
     const int each = (c.count + 7) / 8, pieces = kHalves * each;
@@ -290,9 +284,21 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           factors(std::integral_constant<int, kActGeluTanh>{});
         fetch(piece + kWorkers);
         if (p.factors != nullptr) {
-          __nv_bfloat16* out = p.factors + pos * 2 * p.cols;
-          store_rows(dg, turn, out, 2 * p.cols, at0, p.cols, left, lane);
-          store_rows(du, turn, out + p.cols, 2 * p.cols, at0, p.cols, left, lane);
+          uint32_t most = 0u;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t m = max(__float_as_uint(dg[j]) & 0x7FFFFFFFu, __float_as_uint(du[j]) & 0x7FFFFFFFu);
+            const uint32_t all = __reduce_max_sync(0xFFFFFFFFu, on ? m : 0u);
+            if (lane == j) most = all >> 16;
+          }
+          const int e = row_exponent(most);
+          if (lane < left && at0 < p.cols) {
+            p.groups[(pos + lane) * level_groups(p.cols) + at0 / kLevel] = (int8_t)e;
+            atomicMax(&p.factor_amax[pos + lane], most);
+          }
+          uint16_t* out = p.factors + pos * 2 * p.cols;
+          store_rows(dg, exp2_int(-e), turn, out, 2 * p.cols, at0, p.cols, left, lane);
+          store_rows(du, exp2_int(-e), turn, out + p.cols, 2 * p.cols, at0, p.cols, left, lane);
         }
         if (p.dots != nullptr) {
           const float s = sum_columns(dot, lane);
@@ -300,12 +306,14 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           if ((lane & 3) == 0 && j < left) p.dots[((int64_t)(to * kHalves + half) * 4 + quarter) * p.slots + pos + j] = s;
         }
       } else {
+        const float my_up = !have ? nan : lane < left ? exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
         tmem_ld_wait();
         if (piece + kWorkers >= pieces) release(acc);
         float* out = (at.split ? p.more : p.part) + pos * p.cols + o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          if (j < left && on) *out = have ? __uint_as_float(a[j]) * scale : nan;
+          const float up = __shfl_sync(0xFFFFFFFFu, my_up, j);
+          if (j < left && on) *out = __uint_as_float(a[j]) * up;
           out += p.cols;
         }
       }
@@ -348,7 +356,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       const Chunk c = p.plan.chunks[where(i).chunk];
       const int kbs = kb_count(i);
       const uint32_t slots = (uint32_t)((c.count + 15) & ~15);
-      const uint32_t idesc = warp_uniform((kMode == kModeHidden ? idesc_f16_f32(kBM, slots) : idesc_bf16_f32(kBM, slots)) | 1u << 15);
+      const uint32_t idesc = warp_uniform(idesc_f16_f32(kBM, slots) | 1u << 15);
       const uint32_t acc = (uint32_t)i % kAccs, d = tmem + acc * T::kAcc;
       if (i >= kAccs && !mbar_wait_warp(&acc_empty[acc], (uint32_t)(i / kAccs - 1) & 1u)) {
         ok = false;
@@ -442,18 +450,12 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
         uint8_t* dst = tile_a + s * T::kABytes + part64 * kGroupBytes + row * 128;
         uint32_t ca, cb;
-        if constexpr (kMode == kModeHidden)
-          codes_f16(code, ca, cb);
-        else
-          ca = unpack_codes(code & 0xFFFFu), cb = unpack_codes(code >> 16);
+        codes_f16(code, ca, cb);
 #pragma unroll
         for (int h = 0; h < 8; ++h) {
           uint32_t r[4];
           const uint32_t scale = __byte_perm(h < 4 ? ca : cb, 0u, (h & 2) ? 0x3232 : 0x1010);
-          if constexpr (kMode == kModeHidden)
-            unpack_f16(q[h], scale, r);
-          else
-            unpack8(q[h], scale, r);
+          unpack_f16(q[h], scale, r);
           *reinterpret_cast<uint4*>(dst + (((uint32_t)h ^ swizzle) << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
         }
         fence_proxy_async_smem();
@@ -609,9 +611,10 @@ inline int64_t dot_parts(int64_t inner) { return (inner + kHalves * kBM - 1) / (
 int64_t experts_backward_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
   const int64_t slots = tokens * k;
   // x and dy in order, whose place the slots' parts of dx take afterwards; g and u, whose place a second sum of them takes;
-  // the factors; the dots; dh of K's segments before the last
+  // the factors; the dots; dh of K's segments before the last; the factors' amax and powers of two
   return experts_plan_bytes(slots, experts) + 2 * round256(slots * 4) + 2 * round256(slots * n * 2) + raw_bytes(slots, n, inner) + round256(slots * inner * 4) +
-         round256(dot_parts(inner) * slots * 4) + held_bytes(slots, n, inner);
+         round256(dot_parts(inner) * slots * 4) + held_bytes(slots, n, inner) + round256(slots * 4) +
+         round256(slots * level_groups(inner));
 }
 
 cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const Routing& r, const Experts& w,
@@ -629,21 +632,27 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   uint8_t* raw = dys + round256(slots * w.n * 2);
   uint8_t* factors = raw + raw_bytes(slots, w.n, w.inner);
   uint8_t* dots = factors + round256(slots * w.inner * 4);
+  uint8_t* held = dots + round256(dot_parts(w.inner) * slots * 4);
+  uint32_t* factor_amax = reinterpret_cast<uint32_t*>(held + held_bytes(slots, w.n, w.inner));
+  int8_t* groups = reinterpret_cast<int8_t*>(factor_amax) + round256(slots * 4);
   const Plan wide = experts_wide_plan(plan, slots, w.count);
   const int64_t chunks = plan_chunks(slots, w.count, wide_width);
   const int64_t expected = slots / wide_width + std::min<int64_t>(slots, w.count) / 2;  // half a chunk an expert is not full
   if ((err = launch_experts_plan(r, w.count, width, plan, wide_width, &wide, stream)) != cudaSuccess) return err;
-  err = launch_experts_spread(x, ld_x, xs, amax, dy, ld_dy, dys, dy_amax, w.n, r, plan, nullptr, stream);
+  err = launch_experts_spread(x, ld_x, xs, amax, dy, ld_dy, dys, dy_amax, w.n, r, plan, factor_amax, stream);
   if (err != cudaSuccess) return err;
   if ((err = launch_experts_raw(xs, amax, slots, w, plan, width, reinterpret_cast<float*>(raw), stream)) != cudaSuccess) return err;
   BackArgs p = {};
   p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.activation = w.activation, p.plan = wide, p.weights = r.weights, p.amax = dy_amax;
   p.raw = reinterpret_cast<const float2*>(raw), p.gate_scale = w.gate.scale, p.up_scale = w.up.scale, p.slots = slots;
-  p.factors = dx != nullptr ? reinterpret_cast<__nv_bfloat16*>(factors) : nullptr;
+  p.factors = dx != nullptr ? reinterpret_cast<uint16_t*>(factors) : nullptr;
+  p.groups = groups, p.factor_amax = factor_amax;
   p.dots = dweights != nullptr ? reinterpret_cast<float*>(dots) : nullptr;
-  p.held = reinterpret_cast<float*>(dots + round256(dot_parts(w.inner) * slots * 4));
+  p.held = reinterpret_cast<float*>(held);
   if ((err = launch_back<kModeHidden>(wide_width, dys, 1, w.count, p, chunks, expected, info.sm_count, stream)) != cudaSuccess) return err;
   if (dx != nullptr) {
+    if ((err = launch_experts_level(factors, slots, w.inner, 2, plan, factor_amax, groups, stream)) != cudaSuccess) return err;
+    p.amax = factor_amax;
     p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.part = reinterpret_cast<float*>(xs), p.more = reinterpret_cast<float*>(raw);
     if ((err = launch_back<kModeInput>(wide_width, factors, 2, w.count, p, chunks, expected, info.sm_count, stream)) != cudaSuccess) return err;
   }

@@ -193,6 +193,8 @@ cudaError_t launch_experts_spread(const void* x, int64_t ld, void* out, uint32_t
                                   uint32_t* h_amax, cudaStream_t stream);
 cudaError_t launch_experts_raw(const void* xs, const uint32_t* amax, int64_t slots, const Experts& w, const Plan& plan,
                                int width, float* raw, cudaStream_t stream);
+cudaError_t launch_experts_level(void* h, int64_t slots, int64_t cols, int parts, const Plan& plan, const uint32_t* amax,
+                                 const int8_t* groups, cudaStream_t stream);
 cudaError_t launch_experts_combine(const float* part, const float* more, const Routing& r, const float* weights,
                                    const Plan& plan, int64_t n, void* out, int64_t ld, const float* dots, int parts,
                                    float* dweights, cudaStream_t stream);
