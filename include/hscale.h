@@ -606,15 +606,15 @@ typedef enum hscale_activation { HSCALE_ACT_SILU = 0, HSCALE_ACT_GELU_TANH = 1 }
  * are bf16 with rows ld_x and ld_y elements apart; ids and weights [tokens, k] are contiguous.  An id outside
  * [0, experts) has no term, whatever its weight; a token without experts gets zeros.
  *
- * Sums are fp32 and y is rounded once; act(G x) * (U x) is rounded to bf16 before the second product.  The products' operands are
- * held in fp16 under a power of two of each row: an element loses bits only where it is below 2^-31 of its row's largest,
- * and 2^-40 of that at most.  A token's value depends on its own row and experts only, an Inf or NaN elsewhere does not
- * reach it.  Where its own values are not finite, NaN may stand for an Inf.  Equal calls give equal bits, and a token's do
- * not depend on the batch that it is in.
+ * Sums are fp32 and y is rounded once.  The products' operands are held in fp16 under a power of two of each row: an
+ * element of x loses bits only where it is below 2^-31 of its row's largest, and 2^-39 of that at most; act(G x) * (U x) is
+ * rounded to fp16's 11 bits, or by 2^-38 of its row's largest.  A token's value depends on its own row and experts only, an
+ * Inf or NaN elsewhere does not reach it.  Where its own values are not finite, NaN may stand for an Inf.  Equal calls
+ * give equal bits, and a token's do not depend on the batch that it is in.
  *
  * n and inner are multiples of 16, experts at most 1024, k at most 32.  x and y are 16-byte aligned, ld_x and ld_y
- * multiples of 8, packed weights 8-byte aligned; y may be x itself.  With inner == 0, y is zero.  The workspace is 256-byte aligned; calls
- * that may overlap need their own.
+ * multiples of 8, packed weights 8-byte aligned; y may be x itself.  With inner == 0, y is zero.  The workspace is 256-byte
+ * aligned; calls that may overlap need their own.
  */
 size_t hscale_experts_workspace_bytes(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts);
 int hscale_experts(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, const int32_t* ids, const float* weights,
@@ -628,8 +628,8 @@ int hscale_experts(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, 
  *   dh = D_e^T dy_t,  dweights_tj = h . dh  (fp32 [tokens, k]; 0 for an id that is none),
  *   dx_t = sum_j w_tj (G_e^T (dh * u * act'(g)) + U_e^T (dh * act(g)))  (bf16, rows ld_dx elements apart)
  * with g = G_e x_t, u = U_e x_t and h = act(g) * u made again from x.  The weights are frozen, and have no gradient.
- * dx or dweights may be NULL: it is then not computed.  dh and the factors beside it are fp32, their products are rounded to bf16
- * before G_e^T and U_e^T.  dx may be dy or x itself.  The rest is as in hscale_experts.
+ * dx or dweights may be NULL: it is then not computed.  dh and the factors beside it are fp32; their products are rounded as
+ * act(G x) * (U x) is before G_e^T and U_e^T.  dx may be dy or x itself.  The rest is as in hscale_experts.
  */
 size_t hscale_experts_backward_workspace_bytes(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts);
 int hscale_experts_backward(const void* dy_bf16, int64_t tokens, int64_t n, int64_t ld_dy, const void* x_bf16, int64_t ld_x,

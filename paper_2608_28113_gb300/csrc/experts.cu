@@ -1,9 +1,9 @@
 // experts.cu -- a layer of experts with packed NVFP4 weights on the tcgen05 tensor cores:
 //   y_t = sum_j w_tj D_e (act(G_e x_t) * (U_e x_t)),  e = ids[t, j]
 // Steps, each launched while the one before it runs: the slots (token, j) are grouped by expert; their x is laid out in that
-// order, in fp16 (experts.cuh); the first product makes h = act(G x) * (U x), rounded to bf16 (its error is of the size
-// of y's own rounding); h becomes fp16 under a power of two of its row, exactly; the second product makes D h of each
-// slot in fp32; a token's slots are weighted and added up in order, and rounded once.
+// order, in fp16 (experts.cuh); the first product makes h = act(G x) * (U x) in fp16 under powers of two of 32 outputs; h is
+// moved under a power of two of its row; the second product makes D h of each slot in fp32; a token's slots are
+// weighted and added up in order, and rounded once.
 //
 // The products.  Tile: 256 rows of weights as two halves of 128 (128 rows of G and the same 128 of U, or 256 rows of
 // D) x up to kN slots of one expert, K in blocks of 64.  24 warps:

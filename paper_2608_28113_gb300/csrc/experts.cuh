@@ -69,13 +69,13 @@ __device__ __forceinline__ float2 activate(float g) {
 }
 
 // Segments of K that the sums behind dweights (fp32) are formed in, each from zero.  The tensor cores cut off a sum's low bits
-// at each step of 16, always toward zero: of sums of random numbers 5e-7 is lost over 2048 columns, 1.0e-6 over 4096, 2e-6
-// over 8192 (of positive ones five times that), where fp32 sums that round are off by 3e-7 to 7e-7.  dweights takes the
-// losses of g, of u and of dh: with these segments 1.2e-6 at 4096 columns as at 8192 (whole sums: 2.9e-6 and 4.6e-6; fp32
-// sums 1.0e-6).  A step of 2048 tokens takes 2340 us with them and 2024 without.  Results in bf16 do not feel the loss, and
-// hscale_experts has no segments.
-inline int gate_up_segments(int64_t cols) { return (int)((cols + 1407) / 1408); }
-inline int hidden_segments(int64_t cols) { return (int)((cols + 2047) / 2048); }
+// at each step of 16, always toward zero: of sums of random numbers 2.5e-7 is lost over 1024 columns and 2e-6 over 8192 (of
+// positive ones five times that), where fp32 sums that round are off by 3e-7 to 7e-7.  dweights takes the losses of g, of
+// u and of dh: with these segments 8e-7 at 4096 columns as at 8192 (whole sums: 2.9e-6 and 4.6e-6; 1408 and 2048 columns:
+// 1.2e-6; fp32 sums 0.6e-6 to 1.9e-6).  A step of 2048 tokens takes 2540 us with them, some 2080 without, 2390 with those
+// longer ones.  Results in bf16 do not feel the loss, and hscale_experts has no segments.
+inline int gate_up_segments(int64_t cols) { return (int)((cols + 1023) / 1024); }
+inline int hidden_segments(int64_t cols) { return (int)((cols + 1407) / 1408); }
 
 // Asynchronous copies of 4 or 8 bytes, of which `bytes` are read and the rest zeros.
 __device__ __forceinline__ void copy_4_async(uint32_t dst, const void* src, uint32_t bytes) {
@@ -214,7 +214,7 @@ __device__ __forceinline__ void unpack_f16(uint32_t w, uint32_t scale, uint32_t*
 // The slots' operand is fp16 too, under a power of two of its row: with amax (the bits of the row's largest bf16
 // magnitude, 2^p <= amax < 2^(p + 1)) elements are held as v 2^-E, E = p - 14, so the largest is below 2^15.  fp16 has
 // 24 binades below 2^0 and bf16's 8 bits fit its 11: an element loses bits only where it is below 2^-31 of the largest, and
-// 2^-40 of the largest at most.  E >= -112: bf16's smallest numbers are still exact then.  A row with an Inf or NaN is taken as
+// 2^-39 of the largest at most.  E >= -112: bf16's smallest numbers are still exact then.  A row with an Inf or NaN is taken as
 // it is.
 __device__ __forceinline__ int row_exponent(uint32_t amax) {
   return amax >= 0x7F80u ? 0 : max((int)(amax >> 7) - 127 - 14, -112);

@@ -1,9 +1,9 @@
 // experts_backward.cu -- the gradients of a layer of experts with packed NVFP4 weights:
 //   dh = D_e^T dy_t,  dw = h . dh,  dx_t = sum_j w_tj (G_e^T (dh u act'(g)) + U_e^T (dh act(g)))
 // The slots are grouped as in the forward pass (experts.cu), x and dy laid out in that order in fp16, and g and u made again
-// in fp32.  Two products by transposed weights follow: the first (K = n) makes dh and, as it leaves tensor memory, dw's partial sums
-// and the two factors of dx, rounded to bf16 with G's and U's global scales in them; the second (K = G's rows, then U's)
-// makes each slot's part of dx in fp32; a token's slots are added up in order and rounded once.
+// in fp32.  Two products by transposed weights follow: the first (K = n) makes dh and, as it leaves tensor memory, dw's
+// partial sums and the two factors of dx, with G's and U's global scales in them, in fp16 (experts.cuh); the second (K =
+// G's rows, then U's) makes each slot's part of dx in fp32; a token's slots are added up in order and rounded once.
 //
 // The transposed products.  Tile: 256 outputs (columns of the weights) as two halves of 128 x up to kN slots, K in blocks
 // of 64 rows.  The packed rows, unpacked as they are stored, make the weights' tile MN-major in shared memory
@@ -13,9 +13,10 @@
 // Bound by shared memory, which carries both operands, the packed blocks and the unpacking: of 128 bytes a
 // cycle, a K block takes some 1010 cycles at 128 slots against 512 of MMAs, and 1416 at 256 against 1024; so an expert
 // with enough slots takes 256 a tile, and the unpacking warps then take part in its epilogue.  4096 slots of 8 experts,
-// 4096 x 14336: first product 737 us (550 without segments of K, 28 % of it the epilogue, whose 65536 numbers a tile are
-// some 45 instructions each; a segment more writes and reads dh in L2, with no second accumulator to go on with), second
-// 868 us (1.1 PFLOP/s), g and u 735 us (600 without segments).
+// 4096 x 14336: g and u 816 us, first product 790, second 770 (1.25 PFLOP/s).  Segments of K (experts.cuh) are 200 us
+// of the first and 200 of g and u: a segment more is an epilogue more, of 65536 numbers a tile at some 45 instructions
+// each in the last one, and at this width there is no second accumulator to go on with.  The factors under their row's power
+// of two: 50 us.
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>

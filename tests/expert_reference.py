@@ -41,9 +41,10 @@ def experts(x, ids, weights, gate, up, down, kind, w=None):
         a, _ = activation(kind, g)
         h, s = a * u, wt[rows, slot][:, None]
         # n products summed in fp32: n 2^-24 of the sum of magnitudes at most; |act'| < 1.13; the fast activation 2^-18;
-        # h rounded to bf16, 2^-8 at most
+        # h rounded to fp16 under a power of two of its 32 outputs, then of its row (the largest above 2^14): 2^-11 of it, or
+        # twice half of fp16's least step, 2^-25 2^-14 of the row's largest
         dg, du = (x[rows].abs() @ m.abs().T * (x.shape[1] + 8) * 2.0 ** -24 for m in (gm, um))
-        dh = (1.13 * dg + 2.0 ** -18 * a.abs()) * u.abs() + a.abs() * du + 2.0 ** -8 * h.abs()
+        dh = (1.13 * dg + 2.0 ** -18 * a.abs()) * u.abs() + a.abs() * du + 2.0 ** -11 * h.abs() + 2.0 ** -38 * h.abs().amax(1, True)
         mag = (h.abs() + dh) @ dm.abs().T
         y.index_add_(0, rows, s * (h @ dm.T))
         tol.index_add_(0, rows, s.abs() * (dh @ dm.abs().T + mag * (dm.shape[1] + 8) * 2.0 ** -24))
@@ -74,9 +75,10 @@ def experts_backward(dy, x, ids, weights, gate, up, down, kind):
         tw[rows, slot] = ((ea * u.abs() + a.abs() * du_) * dh.abs() + (a * u).abs() * ddh).sum(1) * 1.01 + \
             mags.sum(1) * (inner / 32 + 40) * eps
         fg, fu = s * dh * u * slope, s * dh * a
-        # the factors are rounded to bf16
-        eg = s.abs() * (ddh * (u * slope).abs() + dh.abs() * (du_ * slope.abs() + u.abs() * es)) * 1.01 + 2.0 ** -8 * fg.abs()
-        eu = s.abs() * (ddh * a.abs() + dh.abs() * ea) * 1.01 + 2.0 ** -8 * fu.abs()
+        # the factors are rounded as h is, both under one power of two
+        most = 2.0 ** -38 * torch.maximum(fg.abs(), fu.abs()).amax(1, True)
+        eg = s.abs() * (ddh * (u * slope).abs() + dh.abs() * (du_ * slope.abs() + u.abs() * es)) * 1.01 + 2.0 ** -11 * fg.abs() + most
+        eu = s.abs() * (ddh * a.abs() + dh.abs() * ea) * 1.01 + 2.0 ** -11 * fu.abs() + most
         dx.index_add_(0, rows, fg @ gm + fu @ um)
         err = eg @ gm.abs() + eu @ um.abs() + (fg.abs() @ gm.abs() + fu.abs() @ um.abs()) * (2 * inner + 8) * eps
         tx.index_add_(0, rows, err)

@@ -78,8 +78,8 @@ def test_experts(t, n, inner, count, k, kind):
     got = y.cpu().double()
     assert ((got - want).abs() <= tol).all()
     norm = want.norm()
-    if norm > 0:  # h and y each off by at most 2^-8
-        assert (got - want).norm() <= norm * 2.0 ** -7
+    if norm > 0:  # y off by at most 2^-8, h by 2^-11, which sums of many leave the same
+        assert (got - want).norm() <= norm * 1.5 * 2.0 ** -8
     assert torch.equal(run(*args, kind), y)
     assert hs.hscale_device_error_flags() == 0
 
@@ -105,7 +105,7 @@ def test_experts_backward(t, n, inner, count, k, kind):
     assert ((dx.cpu().double() - want_dx).abs() <= tol_dx).all()
     assert ((dw.cpu().double() - want_dw).abs() <= tol_dw).all()
     if want_dx.norm() > 0:
-        assert (dx.cpu().double() - want_dx).norm() <= want_dx.norm() * 2.0 ** -7
+        assert (dx.cpu().double() - want_dx).norm() <= want_dx.norm() * 1.5 * 2.0 ** -8
     again = backward(dy, *args, kind)
     assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
     alone_dx, _ = backward(dy, *args, kind, want_dw=False)
@@ -128,7 +128,7 @@ def test_backward_of_long_rows(t, n, inner, count, k, packed_by, codes_by):
     # An accumulator of fp32 that is cut off toward zero at each step of 16: half a unit of 2^-23 on average, 0.72 of it relative
     # to the sum (a mantissa's mean reciprocal), and the partial sums of random products grow as a square root: of m steps
     # 0.36 2^-23 sum_j sqrt(j / m) = 0.48 m 2^-24.  Parts of at most 1408 columns of g and u and of 2048 of dh: m = 88, 88 and
-    # 128, together 146 2^-24, however long the rows are.  The roundings of the parts' sums, of the activation, of the
+    # 128, together 146 2^-24, however long the rows are (shorter parts lose less).  The roundings of the parts' sums, of the activation, of the
     # products and of their sum over inner, each random: less than 14 2^-24.
     assert (dw.cpu().double() - want_dw).norm() <= want_dw.norm() * 160 * 2.0 ** -24
     again = backward(dy, x, ids, w, gate, up, down, 0)
