@@ -195,6 +195,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int32_t* ids, 
 }
 
 // A token's row in fp16 (experts.cuh) to the positions of its slots, with the row's amax; a row of h begins with none.
+// Where weight_of is not nullptr, the slots' weights too.
 // gridDim.y of them: of x, and of the backward pass's dy.
 struct Spread {
   const uint4* x;
@@ -202,7 +203,8 @@ struct Spread {
   uint4* out;
   uint32_t* amax;
 };
-__global__ void __launch_bounds__(256) spread_kernel(Spread first, Spread second, int64_t pieces, int k, Plan plan, uint32_t* h_amax) {
+__global__ void __launch_bounds__(256) spread_kernel(Spread first, Spread second, int64_t pieces, int k, Plan plan, uint32_t* h_amax,
+                                                     const float* weights, float* weight_of) {
   __shared__ uint32_t warp_max[8];
   pdl_wait_primary();
   pdl_launch_dependents();
@@ -233,6 +235,7 @@ __global__ void __launch_bounds__(256) spread_kernel(Spread first, Spread second
     if (threadIdx.x == 0) {
       amax[pos] = m;
       if (h_amax != nullptr) h_amax[pos] = 0u;
+      if (weight_of != nullptr) weight_of[pos] = weights[t * k + j];
     }
     uint4* to = out + pos * pieces;
 #pragma unroll
@@ -953,11 +956,12 @@ cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, co
 }
 
 cudaError_t launch_experts_spread(const void* x, int64_t ld, void* out, uint32_t* amax, const void* dy, int64_t ld_dy, void* dy_out,
-                                  uint32_t* dy_amax, int64_t n, const Routing& r, const Plan& plan, uint32_t* h_amax, cudaStream_t stream) {
+                                  uint32_t* dy_amax, int64_t n, const Routing& r, const Plan& plan, uint32_t* h_amax, float* weight_of,
+                                  cudaStream_t stream) {
   const Spread first = {static_cast<const uint4*>(x), ld / 8, static_cast<uint4*>(out), amax};
   const Spread second = {static_cast<const uint4*>(dy), ld_dy / 8, static_cast<uint4*>(dy_out), dy_amax};
   return launch_chained(spread_kernel, dim3((unsigned)r.tokens, dy != nullptr ? 2 : 1), 256, 0, stream, first, second, n / 8, r.k, plan,
-                        h_amax);
+                        h_amax, r.weights, weight_of);
 }
 
 // h: [positions, parts, cols] of fp16, groups: [positions, level_groups(cols)]
@@ -1010,7 +1014,7 @@ cudaError_t launch_experts(const void* x, int64_t ld_x, const Routing& r, const 
   int8_t* groups = reinterpret_cast<int8_t*>(part) + round256(slots * w.n * 4);
   const int64_t chunks = plan_chunks(slots, w.count, width);
   if ((err = launch_experts_plan(r, w.count, width, plan, width, nullptr, stream)) != cudaSuccess) return err;
-  if ((err = launch_experts_spread(x, ld_x, xs, amax, nullptr, 0, nullptr, nullptr, w.n, r, plan, h_amax, stream)) != cudaSuccess) return err;
+  if ((err = launch_experts_spread(x, ld_x, xs, amax, nullptr, 0, nullptr, nullptr, w.n, r, plan, h_amax, nullptr, stream)) != cudaSuccess) return err;
   GemmArgs p = {};
   p.a = w.gate, p.b = w.up, p.rows = w.inner, p.cols = w.n, p.activation = w.activation, p.plan = plan;
   p.amax = amax, p.h_amax = h_amax, p.h_groups = groups, p.out = h;

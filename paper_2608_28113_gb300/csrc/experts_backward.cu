@@ -70,7 +70,7 @@ struct BackArgs {
   int64_t all_rows;  // of all experts
   int32_t activation;
   Plan plan;
-  const float* weights;
+  const float* weight_of;    // of each position
   const uint32_t* amax;      // of each position's dy, or of its factors
   const float2* raw;         // g and u, [positions, cols]
   const float *gate_scale, *up_scale;
@@ -260,7 +260,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       }
       if constexpr (kMode == kModeHidden) {
         // lane j: slot j's weight times G's and U's scales, and the power of two of its row of dy times D's
-        const float my_w = lane < left ? p.weights[p.plan.slot_of[pos + lane]] : 0.0f, my_g = my_w * sg, my_u = my_w * su;
+        const float my_w = lane < left ? p.weight_of[pos + lane] : 0.0f, my_g = my_w * sg, my_u = my_w * su;
         float my_up = 1.0f;
         if (segments == 1) {
           my_up = !have ? nan : lane < left ? scale * exp2_int(row_exponent(p.amax[pos + lane])) : 0.0f;
@@ -612,9 +612,10 @@ inline int64_t dot_parts(int64_t inner) { return (inner + kHalves * kBM - 1) / (
 int64_t experts_backward_workspace(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts) {
   const int64_t slots = tokens * k;
   // x and dy in order, whose place the slots' parts of dx take afterwards; g and u, whose place a second sum of them takes;
-  // the factors; the dots; dh of K's segments before the last; the factors' amax and powers of two
+  // the factors; the dots; dh of K's segments before the last; the factors' amax, the slots' weights and
+  // the factors' powers of two
   return experts_plan_bytes(slots, experts) + 2 * round256(slots * 4) + 2 * round256(slots * n * 2) + raw_bytes(slots, n, inner) + round256(slots * inner * 4) +
-         round256(dot_parts(inner) * slots * 4) + held_bytes(slots, n, inner) + round256(slots * 4) +
+         round256(dot_parts(inner) * slots * 4) + held_bytes(slots, n, inner) + 2 * round256(slots * 4) +
          round256(slots * level_groups(inner));
 }
 
@@ -635,16 +636,17 @@ cudaError_t launch_experts_backward(const void* dy, int64_t ld_dy, const void* x
   uint8_t* dots = factors + round256(slots * w.inner * 4);
   uint8_t* held = dots + round256(dot_parts(w.inner) * slots * 4);
   uint32_t* factor_amax = reinterpret_cast<uint32_t*>(held + held_bytes(slots, w.n, w.inner));
-  int8_t* groups = reinterpret_cast<int8_t*>(factor_amax) + round256(slots * 4);
+  float* weight_of = reinterpret_cast<float*>(factor_amax) + round256(slots * 4) / 4;
+  int8_t* groups = reinterpret_cast<int8_t*>(weight_of) + round256(slots * 4);
   const Plan wide = experts_wide_plan(plan, slots, w.count);
   const int64_t chunks = plan_chunks(slots, w.count, wide_width);
   const int64_t expected = slots / wide_width + std::min<int64_t>(slots, w.count) / 2;  // half a chunk an expert is not full
   if ((err = launch_experts_plan(r, w.count, width, plan, wide_width, &wide, stream)) != cudaSuccess) return err;
-  err = launch_experts_spread(x, ld_x, xs, amax, dy, ld_dy, dys, dy_amax, w.n, r, plan, factor_amax, stream);
+  err = launch_experts_spread(x, ld_x, xs, amax, dy, ld_dy, dys, dy_amax, w.n, r, plan, factor_amax, weight_of, stream);
   if (err != cudaSuccess) return err;
   if ((err = launch_experts_raw(xs, amax, slots, w, plan, width, reinterpret_cast<float*>(raw), stream)) != cudaSuccess) return err;
   BackArgs p = {};
-  p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.activation = w.activation, p.plan = wide, p.weights = r.weights, p.amax = dy_amax;
+  p.a = p.b = w.down, p.rows = w.n, p.cols = w.inner, p.activation = w.activation, p.plan = wide, p.weight_of = weight_of, p.amax = dy_amax;
   p.raw = reinterpret_cast<const float2*>(raw), p.gate_scale = w.gate.scale, p.up_scale = w.up.scale, p.slots = slots;
   p.factors = dx != nullptr ? reinterpret_cast<uint16_t*>(factors) : nullptr;
   p.groups = groups, p.factor_amax = factor_amax;

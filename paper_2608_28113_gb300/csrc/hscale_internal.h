@@ -190,7 +190,7 @@ cudaError_t launch_experts_plan(const Routing& r, int64_t experts, int width, co
                                 const Plan* wide, cudaStream_t stream);
 cudaError_t launch_experts_spread(const void* x, int64_t ld, void* out, uint32_t* amax, const void* dy, int64_t ld_dy,
                                   void* dy_out, uint32_t* dy_amax, int64_t n, const Routing& r, const Plan& plan,
-                                  uint32_t* h_amax, cudaStream_t stream);
+                                  uint32_t* h_amax, float* weight_of, cudaStream_t stream);
 cudaError_t launch_experts_raw(const void* xs, const uint32_t* amax, int64_t slots, const Experts& w, const Plan& plan,
                                int width, float* raw, cudaStream_t stream);
 cudaError_t launch_experts_level(void* h, int64_t slots, int64_t cols, int parts, const Plan& plan, const uint32_t* amax,
