@@ -72,7 +72,7 @@ __device__ __forceinline__ float2 activate(float g) {
 // at each step of 16, always toward zero: of sums of random numbers 2.5e-7 is lost over 1024 columns and 2e-6 over 8192 (of
 // positive ones five times that), where fp32 sums that round are off by 3e-7 to 7e-7.  dweights takes the losses of g, of
 // u and of dh: with these segments 8e-7 at 4096 columns as at 8192 (whole sums: 2.9e-6 and 4.6e-6; 1408 and 2048 columns:
-// 1.2e-6; fp32 sums 0.6e-6 to 1.9e-6).  A step of 2048 tokens takes 2540 us with them, some 2080 without, 2390 with those
+// 1.2e-6; fp32 sums 0.6e-6 to 1.9e-6).  A step of 2048 tokens takes 2530 us with them, some 2080 without, 2390 with those
 // longer ones.  Results in bf16 do not feel the loss, and hscale_experts has no segments.
 inline int gate_up_segments(int64_t cols) { return (int)((cols + 1023) / 1024); }
 inline int hidden_segments(int64_t cols) { return (int)((cols + 1407) / 1408); }

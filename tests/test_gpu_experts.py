@@ -260,6 +260,21 @@ def test_weights_at_any_address(t, n, inner, packed_by, codes_by):
     assert torch.equal(dx, want_dx) and torch.equal(dw, want_dw)
 
 
+@pytest.mark.parametrize("t, n, inner, count, k", [(3, 8208, 32, 3, 2), (70, 16400, 48, 2, 2), (40, 64, 9232, 3, 2), (300, 80, 8200 // 16 * 16, 2, 1)])
+def test_rows_longer_than_registers_hold(t, n, inner, count, k):
+    """x and dy past the 8192 columns that a CTA keeps, h and the factors past them."""
+    args = layer(t, n, inner, count, k, seed=t)
+    x, ids, w, gate, up, down = args
+    want, tol = experts(x.cpu(), ids.cpu(), clean(w), gate, up, down, 1)
+    assert ((run(*args, 1).cpu().double() - want).abs() <= tol).all()
+    dy, _ = rows(t, n, 16, torch.Generator().manual_seed(8), 0.1)
+    dx, dw = backward(dy, *args, 1)
+    want_dx, tol_dx, want_dw, tol_dw = experts_backward(dy.cpu(), x.cpu(), ids.cpu(), clean(w), gate, up, down, 1)
+    assert ((dx.cpu().double() - want_dx).abs() <= tol_dx).all()
+    assert ((dw.cpu().double() - want_dw).abs() <= tol_dw).all()
+    assert hs.hscale_device_error_flags() == 0
+
+
 @pytest.mark.parametrize("t", [3, 40, 300])
 def test_in_place(t):
     """y over x, and dx over dy and over x."""
