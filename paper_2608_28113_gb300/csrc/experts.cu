@@ -246,8 +246,8 @@ __global__ void __launch_bounds__(256) spread_kernel(Spread first, Spread second
 }
 
 // Rows of fp16 from their groups' powers of two to the row's, in place, 16 bytes a thread: exact but where a number is below
-// 2^-14 then.  A row is `pieces` of 16 bytes in parts of `part`, which have the same groups.  What is there already (a third to a
-// half of the groups) is neither read nor written.
+// 2^-14 then.  A row is `pieces` of 16 bytes in parts of `part`, which have the same groups; those under the row's power
+// already are neither read nor written.
 __global__ void __launch_bounds__(256) level_kernel(uint4* h, int64_t pieces, int64_t part, Plan plan, const uint32_t* amax, const int8_t* groups) {
   pdl_launch_dependents();  // the next product's weights may come; it waits for this kernel before it reads h
   pdl_wait_primary();
