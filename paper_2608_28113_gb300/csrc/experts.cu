@@ -648,6 +648,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     const uint32_t code_src = smem_addr(packed_codes + half * kHalfCodes);
     uint32_t* turn = turn_at(T::kHelp ? 4 + warp - kUnpackWarp0 : 0);
     bool go = true;
+    int owed = 0;  // the first tile whose epilogue these warps still owe
     // the packed stage that is read next; the stage of unpacked blocks that this group writes next
     uint32_t stage = 0, parity_p = 0, slot = (uint32_t)odd, parity = 1;
     const uint32_t tmem_a = tmem + T::kA0 + (uint32_t)half * (kBK / 2) + lane_base;
@@ -675,7 +676,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         uint32_t code[2] = {0u, 0u};
         const uint32_t from = src + stage * (kHalves * kHalfBytes);
         if constexpr (kPath != kDirect) {
-          if (!mbar_wait_warp(&packed_full[stage], parity_p)) {
+          if (!mbar_wait_unpack(&packed_full[stage], parity_p)) {
             go = false;
             break;
           }
@@ -710,7 +711,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
             }
             code[u] = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
           }
-          if (!mbar_wait_warp(&empty[slot], parity)) {
+          if (!mbar_wait_unpack(&empty[slot], parity)) {
             go = false;
             break;
           }
@@ -743,15 +744,20 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           if (++stage == kPackedStages) stage = 0, parity_p ^= 1u;
         }
         // the tile before, once this one's first blocks are there for the MMAs
-        if (T::kHelp && quad == 0 && i > 0) finish(i - 1, 1 + group, turn, f);
+        if (T::kHelp && quad == 0 && i > 0) finish(owed++, 1 + group, turn, f);
       }
       if (odd >= kbs) {  // a tile of one block has none for the odd groups
         slot += (uint32_t)kbs;
         while (slot >= kStages) slot -= kStages, parity ^= 1u;
       }
     }
-    if (T::kHelp && ntiles == 1) pdl_wait_primary();
-    if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + group, turn, prepare(ntiles - 1, 1 + group));
+    if constexpr (T::kHelp) {
+      // the last tile; after a wait that ran out every tile that is left, as NaN
+      have = have && go;
+      pdl_wait_primary();
+#pragma unroll 1
+      for (; owed < ntiles; ++owed) finish(owed, 1 + group, turn, prepare(owed, 1 + group));
+    }
     if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
   } else if (p.path != kDirect && (warp == kWeightsWarp0 || p.path != kBulk)) {
     // the packed weights.  In small tiles an expert's only chunk reads them, once; in large ones others read them again,

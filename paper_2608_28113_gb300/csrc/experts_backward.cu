@@ -404,7 +404,8 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     // blocks of all tiles, one after another: this group's are group, group + 2, ...
     int kb = group;
     uint32_t block = (uint32_t)group;
-    for (int i = 0; i < ntiles && go; kb -= kb_count(i), ++i) {
+    int i = 0;
+    for (; i < ntiles && go; kb -= kb_count(i), ++i) {
       const int kbs = kb_count(i), kb0 = kb_first(i);
       const Where at = where(i);
       const int64_t e = p.plan.chunks[at.chunk].expert, o0 = (int64_t)at.to * (kHalves * kBM) + part64 * 64;
@@ -416,7 +417,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         const uint32_t ps = block % kPackedStages, parity_p = (block / kPackedStages) & 1u;
         uint32_t q[8], code;
         if (p.path != kDirect) {
-          if (!mbar_wait_warp(&packed_full[ps], parity_p)) {
+          if (!mbar_wait_unpack(&packed_full[ps], parity_p)) {
             go = false;
             break;
           }
@@ -445,7 +446,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
           code = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
         }
         const uint32_t s = block % kStages;
-        if (!mbar_wait_warp(&empty[s], ((block / kStages) & 1u) ^ 1u)) {
+        if (!mbar_wait_unpack(&empty[s], ((block / kStages) & 1u) ^ 1u)) {
           go = false;
           break;
         }
@@ -473,8 +474,14 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       if (T::kHelp && done == 0 && i == 1) pdl_wait_primary();
       if (T::kHelp && done == 0 && i > 0 && go) finish(i - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
     }
-    if (T::kHelp && ntiles == 1) pdl_wait_primary();
-    if (T::kHelp && ntiles > 0 && go) finish(ntiles - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
+    if constexpr (T::kHelp) {
+      // the last tile; after a wait that ran out (in tile i - 1) the one before it, which may not be done, and all that are
+      // left, as NaN
+      have = have && go;
+      pdl_wait_primary();
+#pragma unroll 1
+      for (int j = max(0, go ? ntiles - 1 : i - 2); j < ntiles; ++j) finish(j, 1 + ((warp - kUnpackWarp0) >> 2), turn);
+    }
     if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
   } else if (p.path != kDirect && (warp == kWeightsWarp0 || p.path != kBulk)) {
     const int who = warp - kWeightsWarp0;  // whose copies are 32 of the 64 rows

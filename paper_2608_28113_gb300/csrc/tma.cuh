@@ -11,11 +11,15 @@ namespace hscale {
 // error instead of hanging the GPU.
 //
 // A build with HSCALE_STARVED_BLOCK = b (the failure tests') has a limit of a few milliseconds, and in
-// it mbar_wait_acc, the epilogues' wait for an accumulator, runs out at once in block b.
+// it mbar_wait_acc, the epilogues' wait for an accumulator, runs out at once in block b; with
+// HSCALE_STARVED_WAIT = 1 it is mbar_wait_unpack, the wait of the experts' unpacking warps, instead.
 #ifndef HSCALE_STARVED_BLOCK
 #define HSCALE_STARVED_BLOCK -1
 #endif
-constexpr int kStarvedBlock = HSCALE_STARVED_BLOCK;
+#ifndef HSCALE_STARVED_WAIT
+#define HSCALE_STARVED_WAIT 0
+#endif
+constexpr int kStarvedBlock = HSCALE_STARVED_BLOCK, kStarvedWait = HSCALE_STARVED_WAIT;
 constexpr uint32_t kMbarPollLimit = kStarvedBlock < 0 ? 1u << 24 : 1u << 10;
 
 // Device-wide error word of this library (bit flags, sticky until read by the host).
@@ -67,7 +71,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
 }
 
 __device__ __forceinline__ bool mbar_wait_acc(uint64_t* bar, uint32_t parity) {
-  return (kStarvedBlock < 0 || (int)blockIdx.x != kStarvedBlock) && mbar_wait(bar, parity);
+  return (kStarvedBlock < 0 || kStarvedWait != 0 || (int)blockIdx.x != kStarvedBlock) && mbar_wait(bar, parity);
 }
 
 // The loads that a ring's producer has issued land before the CTA's shared memory may go away; after a
@@ -91,6 +95,9 @@ __device__ __forceinline__ bool elect_one() {
 // A whole warp waits; the same answer in every lane.
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity));
+}
+__device__ __forceinline__ bool mbar_wait_unpack(uint64_t* bar, uint32_t parity) {
+  return (kStarvedBlock < 0 || kStarvedWait != 1 || (int)blockIdx.x != kStarvedBlock) && mbar_wait_warp(bar, parity);
 }
 // The value of lane 0, which the compiler then knows to be uniform.
 __device__ __forceinline__ uint32_t warp_uniform(uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
