@@ -577,8 +577,8 @@ typedef enum hscale_type { HSCALE_BF16 = 0, HSCALE_F32 = 1, HSCALE_F16 = 2 } hsc
  * The router of a mixture of experts: of each token's logits [tokens, experts] (bf16 or fp32, rows ld_logits elements
  * apart) the k largest, in descending order and the lowest index first among equal ones: ids [tokens, k], and
  *   weights_j = p_j with p = softmax(logits), or (renormalize) p_j / sum of the chosen p     (fp32 [tokens, k]).
- * A logit of -Inf or NaN is an expert that is off: never chosen, p = 0; +Inf counts as the largest finite number, and
- * the type's lowest number as any other.  Where fewer than k experts are on, the rest of ids is -1 and of weights 0.
+ * A logit of -Inf or NaN is an expert that is off: never chosen, p = 0; +Inf counts as the type's largest finite
+ * number, and its lowest number as any other.  Where fewer than k experts are on, the rest of ids is -1 and of weights 0.
  * experts at most 1024, k at most 32.  Logits may have any alignment of their type.
  */
 int hscale_route(const void* logits, int32_t type, int64_t tokens, int64_t experts, int64_t ld_logits, int64_t k,

@@ -3,7 +3,7 @@
 //   w_j = p_j, or p_j / sum of the chosen p (renormalized);
 //   backward, over all experts:    dl_e = p_e ([e chosen] dw_e - sum_j w_j dw_j)
 //             over the chosen ones: dl_j = w_j (dw_j - sum_i w_i dw_i), 0 elsewhere.
-// -Inf and NaN are experts that are switched off: never chosen, p = 0.  +Inf counts as the largest finite number.
+// -Inf and NaN are experts that are switched off: never chosen, p = 0.  +Inf counts as the type's largest finite number.
 //
 // One warp a token, its logits in registers (up to 1024).  A choice is two warp-wide integer reductions: the largest key
 // (a float's bits, ordered as integers) and the lowest index that has it.  Up to 256 bf16 logits go another way: a
@@ -38,9 +38,12 @@ template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
 // A logit's key: larger floats have larger keys, -0 is 0, and 0 stands for an expert that is off.
-__device__ __forceinline__ uint32_t key_of(float v) {
+template <typename T>
+__device__ __forceinline__ uint32_t key_of(T logit) {
+  const float v = as_float<T>(logit);
   if (!(v > -INFINITY)) return 0u;
-  const uint32_t b = __float_as_uint(fminf(v, FLT_MAX) + 0.0f);
+  constexpr float kLargest = sizeof(T) == 2 ? 0x1.FEp127f : FLT_MAX;  // bf16's, fp32's
+  const uint32_t b = __float_as_uint(fminf(v, kLargest) + 0.0f);
   return (b >> 31) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t key) {
@@ -57,7 +60,7 @@ __device__ __forceinline__ void load_keys(const T* row, int experts, int lane, u
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int e = lane + 32 * i;
-    key[i] = e < experts ? key_of(as_float<T>(row[e])) : 0u;
+    key[i] = e < experts ? key_of<T>(row[e]) : 0u;
   }
 }
 
