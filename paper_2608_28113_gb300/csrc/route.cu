@@ -249,20 +249,16 @@ cudaError_t launch(const void* logits, int64_t tokens, int64_t experts, int64_t 
                    const float* dweights, int64_t k, bool renormalize, int32_t* ids, float* weights, void* dlogits,
                    int64_t ld_out, cudaStream_t stream) {
   const unsigned grid = (unsigned)((tokens + kWarps - 1) / kWarps);
-  if constexpr (kPer <= 8 && sizeof(T) == 2) {
-    if (dlogits == nullptr) {
-      route_words_kernel<kPer><<<grid, kThreads, 0, stream>>>(static_cast<const uint16_t*>(logits), tokens, (int)experts, ld, (int)k,
-                                                              renormalize, ids, weights);
-      return cudaGetLastError();
-    }
-  }
-  if (dlogits == nullptr)
-    route_kernel<T, kPer><<<grid, kThreads, 0, stream>>>(static_cast<const T*>(logits), tokens, (int)experts, ld, (int)k,
-                                                         renormalize, ids, weights);
-  else
+  if (dlogits != nullptr)
     route_backward_kernel<T, kPer><<<grid, kThreads, 0, stream>>>(static_cast<const T*>(logits), tokens, (int)experts, ld,
                                                                   ids_in, w_in, dweights, (int)k, renormalize,
                                                                   static_cast<T*>(dlogits), ld_out);
+  else if constexpr (kPer <= 8 && sizeof(T) == 2)
+    route_words_kernel<kPer><<<grid, kThreads, 0, stream>>>(static_cast<const uint16_t*>(logits), tokens, (int)experts, ld, (int)k,
+                                                            renormalize, ids, weights);
+  else
+    route_kernel<T, kPer><<<grid, kThreads, 0, stream>>>(static_cast<const T*>(logits), tokens, (int)experts, ld, (int)k,
+                                                         renormalize, ids, weights);
   return cudaGetLastError();
 }
 
