@@ -629,7 +629,10 @@ int hscale_experts(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, 
  *   dx_t = sum_j w_tj (G_e^T (dh * u * act'(g)) + U_e^T (dh * act(g)))  (bf16, rows ld_dx elements apart)
  * with g = G_e x_t, u = U_e x_t and h = act(g) * u made again from x.  The weights are frozen, and have no gradient.
  * dx or dweights may be NULL: it is then not computed.  dh and the factors beside it are fp32; their products are rounded as
- * act(G x) * (U x) is before G_e^T and U_e^T.  dx may be dy or x itself.  The rest is as in hscale_experts.
+ * act(G x) * (U x) is before G_e^T and U_e^T.  dx may be dy or x itself.  Equal calls give equal bits.  A token's dweights have
+ * the same bits in any batch; its dx in any batch of as many tokens on the same GPU, whatever the others are: whether its
+ * terms in G and in U are one fp32 sum or two that are added goes by tokens, k, n, experts and the number of SMs.  The
+ * rest is as in hscale_experts.
  */
 size_t hscale_experts_backward_workspace_bytes(int64_t tokens, int64_t k, int64_t n, int64_t inner, int64_t experts);
 int hscale_experts_backward(const void* dy_bf16, int64_t tokens, int64_t n, int64_t ld_dy, const void* x_bf16, int64_t ld_x,

@@ -589,7 +589,9 @@ cudaError_t launch_back(int width, const void* v, int parts, int64_t experts, Ba
   p.tiles_o = (int32_t)((p.cols + kHalves * kBM - 1) / (kHalves * kBM));
   int64_t tiles = chunks * p.tiles_o;
   // G's and U's rows as tiles of their own where that fills the last round of tiles better (by more than the second
-  // sum costs): 320 tiles of 256 x 256 x 28672 on 152 SMs, 973 us in three rounds
+  // sum costs): 320 tiles of 256 x 256 x 28672 on 152 SMs, 973 us in three rounds, 770 as 640.  dx's bits go by the choice, since one
+  // accumulator cuts its sums off elsewhere than two; tiles of their own always would cost up to a quarter of a call where inner
+  // is short (4096 tokens on 8 of 64 experts, 8192 x 256: 1450 us, 1820), the two added in the tile's epilogue 1 to 9%
   if (parts == 2) {
     const int64_t likely = std::max<int64_t>(1, expected * p.tiles_o);
     const int64_t whole = 2 * ((likely + sms - 1) / sms), halves = (2 * likely + sms - 1) / sms;
