@@ -207,6 +207,9 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ 
   if (t.first && blockIdx.x == 0 && threadIdx.x == 0) *norm = v;
   const bool scaled = v > t.max_norm && v < INFINITY;
   const float factor = scaled ? t.max_norm / v : 1.0f;
+  // below fp32's normal numbers the factor has few bits or none, although the scaled elements may be among them
+  const bool tiny = factor < 0x1p-126f && t.max_norm > 0.0f;
+  const double wide = tiny ? (double)t.max_norm / (double)v : 0.0;
   const int pieces = t.end[t.count - 1];
   int i = 0;
   // the last pieces first: the norm's pass read them last, so they may still be in L2
@@ -216,7 +219,10 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ 
     const int64_t first = (int64_t)(piece - (i ? t.end[i - 1] : 0)) * kPiece;
     float x[kPer];
     load(t.in[i], t.type[i], first, t.size[i], x);
-    if (scaled) {
+    if (tiny) {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) x[j] = (float)((double)x[j] * wide);
+    } else if (scaled) {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) x[j] *= factor;
     }
