@@ -969,8 +969,8 @@ def hscale_grad_norm(tensors, norm: torch.Tensor, workspace: torch.Tensor | None
 
 def hscale_grad_clip(tensors, max_norm: float, norm: torch.Tensor, out=None, workspace: torch.Tensor | None = None,
                      stream=None) -> None:
-    """norm as hscale_grad_norm, and out_i = tensors_i * min(1, max_norm / norm) (out None: in place).  Where the norm is not
-    finite nothing is scaled."""
+    """norm as hscale_grad_norm, and out_i = tensors_i * min(1, max_norm / norm) (out None: in place).  What is written
+    overlaps no other tensor (out_i may be tensors_i).  Where the norm is not finite nothing is scaled."""
     lib, tensors, workspace, nbytes = _grad_arguments(tensors, norm, workspace, stream)
     into = tensors if out is None else hscale_tensors(out)
     if into.shape != tensors.shape or into.device != tensors.device:

@@ -6,6 +6,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <memory>
+#include <new>
 
 #include "../../include/hscale.h"
 #include "experts.cuh"
@@ -73,6 +75,41 @@ inline cudaError_t zero_rows(void* x, int64_t rows, int64_t cols, int64_t ld, cu
   return cudaMemset2DAsync(x, (size_t)ld * 2, 0, (size_t)cols * 2, (size_t)rows, stream);
 }
 
+// Whether no tensor that is written (out; nullptr: in) overlaps another one, written or read: out_i may be in_i itself.
+// HSCALE_OK, HSCALE_ERR_ARG, or HSCALE_ERR_CUDA where the host has no memory for the list.
+int written_apart(const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, int64_t count) {
+  struct Span {
+    uintptr_t first, end;
+    int64_t at;
+  };
+  const std::unique_ptr<Span[]> spans(new (std::nothrow) Span[(size_t)std::max<int64_t>(count, 1)]);
+  if (spans == nullptr) return HSCALE_ERR_CUDA;
+  const auto span = [&](const void* p, int64_t i) {
+    const uintptr_t first = reinterpret_cast<uintptr_t>(p);
+    return Span{first, first + (uintptr_t)sizes[i] * (types[i] == HSCALE_F32 ? 4 : 2), i};
+  };
+  Span *const begin = spans.get(), *end = begin;
+  bool ascending = true;  // as the parts of one buffer are
+  for (int64_t i = 0; i < count; ++i) {
+    if (sizes[i] == 0) continue;
+    *end = span(out != nullptr ? out[i] : in[i], i);
+    ascending = ascending && (end == begin || end[-1].first < end->first);
+    ++end;
+  }
+  if (!ascending) std::sort(begin, end, [](const Span& a, const Span& b) { return a.first < b.first; });
+  for (Span* s = begin; s + 1 < end; ++s)
+    if (s->end > s[1].first) return HSCALE_ERR_ARG;
+  if (out == nullptr) return HSCALE_OK;
+  for (int64_t i = 0; i < count; ++i) {
+    if (sizes[i] == 0) continue;
+    const Span read = span(in[i], i);
+    // the first one written that ends behind this one's beginning: if it is its own place, the next one begins behind it
+    const Span* s = std::upper_bound(begin, end, read.first, [](uintptr_t p, const Span& v) { return p < v.end; });
+    if (s != end && s->first < read.end && !(s->at == i && s->first == read.first)) return HSCALE_ERR_ARG;
+  }
+  return HSCALE_OK;
+}
+
 int grads(const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, int64_t count, bool clip,
           float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
   if (count < 0) return HSCALE_ERR_SHAPE;
@@ -89,6 +126,8 @@ int grads(const void* const* in, void* const* out, const int64_t* sizes, const i
     if (!aligned(in[i], size) || (out != nullptr && !aligned(out[i], size))) return HSCALE_ERR_ALIGN;
   }
   if (workspace == nullptr || workspace_bytes < hscale_grad_norm_workspace_bytes() || !aligned(workspace, 256)) return HSCALE_ERR_WORKSPACE;
+  if (clip)
+    if (const int st = written_apart(in, out, sizes, types, count); st != HSCALE_OK) return st;
   return from_cuda(hscale::launch_grad_norm(in, out, sizes, types, count, clip, max_norm, norm, static_cast<double*>(workspace),
                                             as_stream(stream)));
 }
