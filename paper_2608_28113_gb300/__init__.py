@@ -163,10 +163,11 @@ def hscale_device_error_flags() -> int:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream_ptr(stream) -> int:
+def _stream_ptr(stream, device: int | None = None) -> int:
+    """device: the current one, where the caller knows it."""
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(torch.cuda.current_device() if device is None else device)
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -776,13 +777,23 @@ HSCALE_ACT_SILU, HSCALE_ACT_GELU_TANH = 0, 1
 _TYPES = {torch.bfloat16: 0, torch.float32: 1, torch.float16: 2}
 
 
-def _here(t: torch.Tensor, name: str) -> None:
-    if t.get_device() != torch.cuda.current_device():
+def _here(t: torch.Tensor, name: str) -> int:
+    """The current device, which t is on."""
+    device = torch.cuda.current_device()
+    if t.get_device() != device:
         raise ValueError(f"{name} must be on the current device")
+    return device
+
+
+def _beside(device: int, *others) -> None:
+    """The other tensors of a call (None: not given) are on the device too."""
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise ValueError("the tensors of a call must be on one device, the current one")
 
 
 def _logits(t: torch.Tensor, name: str) -> tuple:
-    """(tokens, experts, row stride, type) of a bf16 or fp32 [tokens, experts] view with contiguous rows."""
+    """(tokens, experts, row stride, type, device) of a bf16 or fp32 [tokens, experts] view with contiguous rows."""
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D view")
     if t.dtype not in (torch.bfloat16, torch.float32) or not t.is_cuda:
@@ -790,8 +801,8 @@ def _logits(t: torch.Tensor, name: str) -> tuple:
     tokens, experts = t.shape
     if experts > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must be a 2-D view with contiguous rows")
-    _here(t, name)
-    return tokens, experts, t.stride(0) if tokens > 1 else max(experts, t.stride(0)), _TYPES[t.dtype]
+    device = _here(t, name)
+    return tokens, experts, t.stride(0) if tokens > 1 else max(experts, t.stride(0)), _TYPES[t.dtype], device
 
 
 def _routing(ids: torch.Tensor, weights: torch.Tensor, tokens: int) -> int:
@@ -808,30 +819,33 @@ def hscale_route(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor,
     """The k largest of each token's logits (bf16 or fp32 [tokens, experts]), ties to the lowest index: ids (int32
     [tokens, k]) and weights (fp32 [tokens, k]), softmax(logits) there, or that divided by its sum over the chosen
     ones (renormalize).  -Inf and NaN are experts that are off; where too few are on, ids are -1 and weights 0."""
-    tokens, experts, ld, kind = _logits(logits, "logits")
+    tokens, experts, ld, kind, device = _logits(logits, "logits")
     k = _routing(ids, weights, tokens)
-    _check("hscale_route", load().hscale_route(logits.data_ptr(), kind, tokens, experts, ld, k, int(bool(renormalize)),
-                                               ids.data_ptr(), weights.data_ptr(), _stream_ptr(stream)))
+    _beside(device, ids, weights)
+    _check("hscale_route",
+           (_lib or load()).hscale_route(logits.data_ptr(), kind, tokens, experts, ld, k, int(bool(renormalize)), ids.data_ptr(),
+                                         weights.data_ptr(), _stream_ptr(stream, device)))
 
 
 def hscale_route_backward(logits: torch.Tensor | None, ids: torch.Tensor, weights: torch.Tensor, dweights: torch.Tensor,
                           renormalize: bool, dlogits: torch.Tensor, stream=None) -> None:
     """dlogits (like logits) of dweights (fp32 [tokens, k]), with the ids and weights that hscale_route gave.  logits may
     be None where the weights are renormalized."""
-    tokens, experts, ld_out, kind = _logits(dlogits, "dlogits")
+    tokens, experts, ld_out, kind, device = _logits(dlogits, "dlogits")
     ld = experts
     if logits is not None:
-        rows, cols, ld, logits_kind = _logits(logits, "logits")
+        rows, cols, ld, logits_kind, _ = _logits(logits, "logits")
         if (rows, cols, logits_kind) != (tokens, experts, kind):
             raise ValueError("logits and dlogits must have the same shape and dtype")
     elif not renormalize:
         raise ValueError("logits are needed where the weights are not renormalized")
     k = _routing(ids, weights, tokens)
     _whole(dweights, "dweights", torch.float32, (tokens, k))
+    _beside(device, ids, weights, dweights)
     _check("hscale_route_backward",
-           load().hscale_route_backward(_ptr(logits), kind, tokens, experts, ld, ids.data_ptr(), weights.data_ptr(),
-                                        dweights.data_ptr(), k, int(bool(renormalize)), dlogits.data_ptr(), ld_out,
-                                        _stream_ptr(stream)))
+           (_lib or load()).hscale_route_backward(_ptr(logits), kind, tokens, experts, ld, ids.data_ptr(), weights.data_ptr(),
+                                                  dweights.data_ptr(), k, int(bool(renormalize)), dlogits.data_ptr(), ld_out,
+                                                  _stream_ptr(stream, device)))
 
 
 def _expert_matrices(gate: tuple, up: tuple, down: tuple, n: int) -> tuple:
@@ -865,15 +879,16 @@ def hscale_experts(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, ga
     y_rows, y_cols, ld_y = _rows(y, "y")
     if (y_rows, y_cols) != (tokens, n):
         raise ValueError("x and y must have the same shape")
-    _here(x, "x")
+    device = _here(x, "x")
     k = _routing(ids, weights, tokens)
     experts, inner, pointers = _expert_matrices(gate, up, down, n)
     lib = _lib or load()
     workspace, nbytes = _project_workspace(
         workspace, lib.hscale_experts_workspace_bytes(tokens, k, n, inner, experts) if workspace is None else 0, x.device, stream)
+    _beside(device, y, ids, weights, *gate, *up, *down, workspace)
     _check("hscale_experts",
            lib.hscale_experts(x.data_ptr(), tokens, n, ld_x, ids.data_ptr(), weights.data_ptr(), k, *pointers, experts, inner,
-                              int(activation), y.data_ptr(), ld_y, _ptr(workspace), nbytes, _stream_ptr(stream)))
+                              int(activation), y.data_ptr(), ld_y, _ptr(workspace), nbytes, _stream_ptr(stream, device)))
 
 
 def hscale_experts_backward_workspace_bytes(tokens: int, k: int, n: int, inner: int, experts: int) -> int:
@@ -894,7 +909,7 @@ def hscale_experts_backward(dy: torch.Tensor, x: torch.Tensor, ids: torch.Tensor
         dx_rows, dx_cols, ld_dx = _rows(dx, "dx")
         if (dx_rows, dx_cols) != (tokens, n):
             raise ValueError(f"dx must be a [{tokens}, {n}] view")
-    _here(dy, "dy")
+    device = _here(dy, "dy")
     k = _routing(ids, weights, tokens)
     if dweights is not None:
         _whole(dweights, "dweights", torch.float32, (tokens, k))
@@ -903,10 +918,11 @@ def hscale_experts_backward(dy: torch.Tensor, x: torch.Tensor, ids: torch.Tensor
     workspace, nbytes = _project_workspace(
         workspace, lib.hscale_experts_backward_workspace_bytes(tokens, k, n, inner, experts) if workspace is None else 0,
         dy.device, stream)
+    _beside(device, x, ids, weights, *gate, *up, *down, dx, dweights, workspace)
     _check("hscale_experts_backward",
            lib.hscale_experts_backward(dy.data_ptr(), tokens, n, ld_dy, x.data_ptr(), ld_x, ids.data_ptr(), weights.data_ptr(), k,
                                        *pointers, experts, inner, int(activation), _ptr(dx), ld_dx, _ptr(dweights),
-                                       _ptr(workspace), nbytes, _stream_ptr(stream)))
+                                       _ptr(workspace), nbytes, _stream_ptr(stream, device)))
 
 
 # ---------------------------------------------------------------- gradients
@@ -947,13 +963,14 @@ def _grad_arguments(tensors, norm, workspace, stream) -> tuple:
     _need(norm, torch.float32, "norm")
     if norm.numel() < 1:
         raise ValueError("norm must hold one float32")
-    _here(norm, "norm")
-    if len(tensors) and tensors.device != norm.get_device():
+    device = _here(norm, "norm")
+    if len(tensors) and tensors.device != device:
         raise ValueError("tensors and norm must be on one device")
     lib = _lib or load()
     workspace, nbytes = _project_workspace(workspace, lib.hscale_grad_norm_workspace_bytes() if workspace is None else 0,
                                            norm.device, stream)
-    return lib, tensors, workspace, nbytes
+    _beside(device, workspace)
+    return lib, tensors, workspace, nbytes, device
 
 
 def hscale_grad_norm_workspace_bytes() -> int:
@@ -962,16 +979,16 @@ def hscale_grad_norm_workspace_bytes() -> int:
 
 def hscale_grad_norm(tensors, norm: torch.Tensor, workspace: torch.Tensor | None = None, stream=None) -> None:
     """norm (fp32 [1]) = the 2-norm over all elements of the tensors (bf16, fp16 and fp32; a list or a TensorList)."""
-    lib, tensors, workspace, nbytes = _grad_arguments(tensors, norm, workspace, stream)
+    lib, tensors, workspace, nbytes, device = _grad_arguments(tensors, norm, workspace, stream)
     _check("hscale_grad_norm", lib.hscale_grad_norm(tensors.pointers, tensors.sizes, tensors.types, len(tensors),
-                                                    norm.data_ptr(), _ptr(workspace), nbytes, _stream_ptr(stream)))
+                                                    norm.data_ptr(), _ptr(workspace), nbytes, _stream_ptr(stream, device)))
 
 
 def hscale_grad_clip(tensors, max_norm: float, norm: torch.Tensor, out=None, workspace: torch.Tensor | None = None,
                      stream=None) -> None:
     """norm as hscale_grad_norm, and out_i = tensors_i * min(1, max_norm / norm) (out None: in place).  What is written
     overlaps no other tensor (out_i may be tensors_i).  Where the norm is not finite nothing is scaled."""
-    lib, tensors, workspace, nbytes = _grad_arguments(tensors, norm, workspace, stream)
+    lib, tensors, workspace, nbytes, device = _grad_arguments(tensors, norm, workspace, stream)
     into = tensors if out is None else hscale_tensors(out)
     if into.shape != tensors.shape or into.device != tensors.device:
         raise ValueError("out must have the tensors' sizes, dtypes and device")
@@ -979,4 +996,4 @@ def hscale_grad_clip(tensors, max_norm: float, norm: torch.Tensor, out=None, wor
         raise ValueError("tensors that are written must not overlap")
     _check("hscale_grad_clip", lib.hscale_grad_clip(tensors.pointers, tensors.sizes, tensors.types, len(tensors),
                                                     float(max_norm), norm.data_ptr(), None if out is None else into.pointers,
-                                                    _ptr(workspace), nbytes, _stream_ptr(stream)))
+                                                    _ptr(workspace), nbytes, _stream_ptr(stream, device)))
