@@ -606,9 +606,11 @@ typedef enum hscale_activation { HSCALE_ACT_SILU = 0, HSCALE_ACT_GELU_TANH = 1 }
  * are bf16 with rows ld_x and ld_y elements apart; ids and weights [tokens, k] are contiguous.  An id outside
  * [0, experts) has no term, whatever its weight; a token without experts gets zeros.
  *
- * Sums are fp32 and y is rounded once.  The products' operands are held in fp16 under a power of two of each row: an
+ * Sums are fp32 and y is rounded once.  The tensor cores' sums lose low bits toward zero as they go, 2^-22 of a sum of random
+ * numbers over 1024 columns and 2^-19 over 8192.  The products' operands are held in fp16 under a power of two of each row: an
  * element of x loses bits only where it is below 2^-31 of its row's largest, and 2^-39 of that at most; act(G x) * (U x) is
- * rounded to fp16's 11 bits, or by 2^-38 of its row's largest.  A token's value depends on its own row and experts only, an
+ * rounded to fp16's 11 bits, or by 2^-38 of its row's largest.  act is made with an approximate exponential and quotient: off by
+ * 2^-18 of itself, or by 2^-55 |G x|.  A token's value depends on its own row and experts only, an
  * Inf or NaN elsewhere does not reach it.  Where its own values are not finite, NaN may stand for an Inf.  Equal calls
  * give equal bits, and a token's do not depend on the batch that it is in.
  *
@@ -628,8 +630,10 @@ int hscale_experts(const void* x_bf16, int64_t tokens, int64_t n, int64_t ld_x, 
  *   dh = D_e^T dy_t,  dweights_tj = h . dh  (fp32 [tokens, k]; 0 for an id that is none),
  *   dx_t = sum_j w_tj (G_e^T (dh * u * act'(g)) + U_e^T (dh * act(g)))  (bf16, rows ld_dx elements apart)
  * with g = G_e x_t, u = U_e x_t and h = act(g) * u made again from x.  The weights are frozen, and have no gradient.
- * dx or dweights may be NULL: it is then not computed.  dh and the factors beside it are fp32; their products are rounded as
- * act(G x) * (U x) is before G_e^T and U_e^T.  dx may be dy or x itself.  Equal calls give equal bits.  A token's dweights have
+ * dx or dweights may be NULL: it is then not computed.  g, u and dh are fp32, summed in parts of at most 1408 columns, and
+ * act and act' are off by 2^-21 of max(1, |g|) and of 1; the products of dh are rounded as act(G x) * (U x) is before
+ * G_e^T and U_e^T.  The workspace holds g, u, dh and those products of every slot, some 16 inner + 4 n bytes each (65536 slots of
+ * 4096 x 14336: 16 GB); a program that has less gives the tokens in parts.  dx may be dy or x itself.  Equal calls give equal bits.  A token's dweights have
  * the same bits in any batch; its dx in any batch of as many tokens on the same GPU, whatever the others are: whether its
  * terms in G and in U are one fp32 sum or two that are added goes by tokens, k, n, experts and the number of SMs.  The
  * rest is as in hscale_experts.

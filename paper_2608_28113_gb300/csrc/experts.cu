@@ -16,7 +16,7 @@
 //   22-23  the packed rows, 256 columns a stage, as many stages ahead as fit (experts.cuh: how they come)
 // A block's 16384 weights cost the unpacking warps some 1200 instructions, 300 cycles at best; its bytes take 390 cycles at the
 // card's bandwidth, its MMAs 512 at 128 slots.  So few slots are bound by memory (16 tokens of 64 experts, 4096 x 2048, k 8:
-// 164 us, 4.8 TB/s of weights; 5.4 TB/s is what the loads alone reach), many by the tensor cores (32768 slots: 1.65 PFLOP/s
+// 147 us, 5.4 TB/s of weights, the launches around the products among them), many by the tensor cores (32768 slots: 1.65 PFLOP/s
 // in the first product, 1.45 in the second, whose K is half as long; the rest is the epilogue, for which tensor memory has
 // no second accumulator at 128 slots: the unpacking warps take part in it).  One token: latency, of six launches one
 // behind another and of each product's first loads.
@@ -910,7 +910,15 @@ cudaError_t bytes_map(CUtensorMap* map, const void* v, int64_t bytes, int64_t ro
              : cudaErrorInvalidValue;
 }
 
-// Slots a tile: as many as an expert has on average, so that a tile's weights serve them all.
+// Slots a tile: as many as an expert has on average, so that a tile's weights serve them all.  Measured on both sides, 32 experts
+// of 4096 x 2048, as many slots each (and, behind the stroke, uneven ones as routers give), us:
+//   slots    16 wide     32 wide     64 wide    128 wide
+//     10    118 / 118   120 / 118   122 / 123   126 / 129
+//     16    132 / 134   120 / 120   122 / 124   128 / 129
+//     24    173 / 172   124 / 137   128 / 126   131 / 134
+//     32    211 / 209   139 / 137   134 / 128   136 / 140
+//     56                183 / 201   138 / 153   147 / 151
+//     72                247 / 244   183 / 182   159 / 157
 int experts_width(int64_t slots, int64_t experts) {
   const int64_t each = (slots + experts - 1) / experts;
   return each <= 10 ? 16 : each <= 24 ? 32 : each <= 56 ? 64 : 128;

@@ -13,10 +13,10 @@
 // Bound by shared memory, which carries both operands, the packed blocks and the unpacking: of 128 bytes a
 // cycle, a K block takes some 1010 cycles at 128 slots against 512 of MMAs, and 1416 at 256 against 1024; so an expert
 // with enough slots takes 256 a tile, and the unpacking warps then take part in its epilogue.  4096 slots of 8 experts,
-// 4096 x 14336: g and u 816 us, first product 790, second 770 (1.25 PFLOP/s).  Segments of K (experts.cuh) are 200 us
+// 4096 x 14336: g and u 803 us, first product 745, second 797 (1.21 PFLOP/s).  Segments of K (experts.cuh) are 200 us
 // of the first and 200 of g and u: a segment more is an epilogue more, of 65536 numbers a tile at some 45 instructions
 // each in the last one, and at this width there is no second accumulator to go on with.  The factors under their row's power
-// of two: 50 us.
+// of two: 74 us.
 //
 // Every wait is bounded; a CTA in which one ran out writes NaN for what it owed and sets the error flag.
 #include <algorithm>
@@ -589,7 +589,7 @@ cudaError_t launch_back(int width, const void* v, int parts, int64_t experts, Ba
   p.tiles_o = (int32_t)((p.cols + kHalves * kBM - 1) / (kHalves * kBM));
   int64_t tiles = chunks * p.tiles_o;
   // G's and U's rows as tiles of their own where that fills the last round of tiles better (by more than the second
-  // sum costs): 320 tiles of 256 x 256 x 28672 on 152 SMs, 973 us in three rounds, 770 as 640.  dx's bits go by the choice, since one
+  // sum costs): 320 tiles of 256 x 256 x 28672 on 152 SMs, 973 us in three rounds, 797 as 640.  dx's bits go by the choice, since one
   // accumulator cuts its sums off elsewhere than two; tiles of their own always would cost up to a quarter of a call where inner
   // is short (4096 tokens on 8 of 64 experts, 8192 x 256: 1450 us, 1820), the two added in the tile's epilogue 1 to 9%
   if (parts == 2) {
@@ -607,7 +607,16 @@ cudaError_t launch_back(int width, const void* v, int parts, int64_t experts, Ba
 }
 
 inline int64_t round256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
-// Slots a tile of the transposed products.
+// Slots a tile of the transposed products.  Measured as in experts_width, whole backward pass, us:
+//   slots    32 wide     64 wide    128 wide    256 wide
+//     24    251 / 295   259 / 278   261 / 303   326 / 350
+//     32    326 / 323   280 / 295   295 / 324   336 / 347
+//     56    416 / 443   341 / 402   351 / 385   379 / 396
+//     72    528 / 525   444 / 445   400 / 420   423 / 446
+//     96                517 / 536   465 / 517   465 / 538
+//    144                759 / 753   696 / 665   587 / 628
+//    176                821 / 829   767 / 747   647 / 646
+// (At 128 to 144 slots 256 wide would be 6 to 16 % faster already.)
 inline int back_width(int64_t slots, int64_t experts) {
   const int64_t each = (slots + experts - 1) / experts;
   return each <= 24 ? 32 : each <= 56 ? 64 : each <= 144 ? 128 : 256;

@@ -2,7 +2,7 @@
 //   norm = sqrt(sum of all squares);  out = g * min(1, max_norm / norm), as they are where the norm is not finite.
 //
 // Bound by bandwidth: every gradient is read for the norm and once more to be scaled, by then from L2 if it is among the
-// last ones read (1120 tensors of fp32, 1.8 GB: 857 us, 6.3 TB/s over the 5.4 GB of both reads and the write; 14 small ones: 9 us,
+// last ones read (1120 tensors of fp32, 1.8 GB: 860 us, 6.3 TB/s over the 5.4 GB of both reads and the write; 14 small ones: 10 us,
 // the call and its two launches).  The tensors' addresses and sizes are kernel parameters (no copy to the GPU, and a graph keeps its own);
 // a call of more tensors than a table holds goes in several launches.  A CTA takes pieces of kPiece elements, whichever tensors
 // they are in, found by bisection of the table's running counts.

@@ -8,7 +8,7 @@ from expert_reference import activation, dequantized, experts, experts_backward
 from test_gpu_experts import backward, layer, matrices, rows, run
 
 pytestmark = pytest.mark.gpu
-BF16, F64, U8, I32 = torch.bfloat16, torch.float64, torch.uint8, torch.int32
+BF16, U8, I32 = torch.bfloat16, torch.uint8, torch.int32
 DEV = "cuda"
 
 
