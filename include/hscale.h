@@ -652,8 +652,8 @@ int hscale_experts_backward(const void* dy_bf16, int64_t tokens, int64_t n, int6
  *   out_i = tensors_i * min(1, max_norm / norm)
  * tensors, out, sizes (elements) and types (hscale_type) are HOST arrays of `count`; what tensors and out point to is on
  * the device, contiguous and aligned to its type (to 16 bytes: faster).  out == NULL scales in place; out_i has the type of
- * tensors_i.  What is written overlaps no other tensor, written or read (out_i may be tensors_i itself; the norm alone may read a tensor
- * twice): HSCALE_ERR_ARG.  Where the norm is not finite nothing is scaled (out_i = tensors_i): the caller sees it in *norm.
+ * tensors_i.  What is written, the norm among it, overlaps no other tensor, written or read (out_i may be tensors_i itself;
+ * hscale_grad_norm may be given a tensor twice): HSCALE_ERR_ARG.  Where the norm is not finite nothing is scaled (out_i = tensors_i): the caller sees it in *norm.
  * Squares that leave fp32's range are not lost; a thread adds up 64 pieces of 16 elements in fp32, the rest is fp64, and
  * equal calls give equal bits.  count == 0: the norm is 0.  The arrays are read before the call returns, so a captured
  * call keeps what they held.

@@ -75,9 +75,11 @@ inline cudaError_t zero_rows(void* x, int64_t rows, int64_t cols, int64_t ld, cu
   return cudaMemset2DAsync(x, (size_t)ld * 2, 0, (size_t)cols * 2, (size_t)rows, stream);
 }
 
-// Whether no tensor that is written (out; nullptr: in) overlaps another one, written or read: out_i may be in_i itself.
+// Whether no tensor that is written (out; nullptr: in) overlaps another one, written or read, and the norm none of them: out_i may
+// be in_i itself.
 // HSCALE_OK, HSCALE_ERR_ARG, or HSCALE_ERR_CUDA where the host has no memory for the list.
-int written_apart(const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, int64_t count) {
+int written_apart(const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, int64_t count,
+                  const float* norm) {
   struct Span {
     uintptr_t first, end;
     int64_t at;
@@ -99,12 +101,17 @@ int written_apart(const void* const* in, void* const* out, const int64_t* sizes,
   if (!ascending) std::sort(begin, end, [](const Span& a, const Span& b) { return a.first < b.first; });
   for (Span* s = begin; s + 1 < end; ++s)
     if (s->end > s[1].first) return HSCALE_ERR_ARG;
+  // the first one written that ends behind an address
+  const auto behind = [&](uintptr_t p) { return std::upper_bound(begin, end, p, [](uintptr_t p, const Span& v) { return p < v.end; }); };
+  const uintptr_t norm_at = reinterpret_cast<uintptr_t>(norm);
+  if (const Span* s = behind(norm_at); s != end && s->first < norm_at + 4) return HSCALE_ERR_ARG;
   if (out == nullptr) return HSCALE_OK;
   for (int64_t i = 0; i < count; ++i) {
     if (sizes[i] == 0) continue;
     const Span read = span(in[i], i);
-    // the first one written that ends behind this one's beginning: if it is its own place, the next one begins behind it
-    const Span* s = std::upper_bound(begin, end, read.first, [](uintptr_t p, const Span& v) { return p < v.end; });
+    if (read.first < norm_at + 4 && norm_at < read.end) return HSCALE_ERR_ARG;
+    // if the first one behind this one's beginning is its own place, the next one begins behind it
+    const Span* s = behind(read.first);
     if (s != end && s->first < read.end && !(s->at == i && s->first == read.first)) return HSCALE_ERR_ARG;
   }
   return HSCALE_OK;
@@ -127,7 +134,7 @@ int grads(const void* const* in, void* const* out, const int64_t* sizes, const i
   }
   if (workspace == nullptr || workspace_bytes < hscale_grad_norm_workspace_bytes() || !aligned(workspace, 256)) return HSCALE_ERR_WORKSPACE;
   if (clip)
-    if (const int st = written_apart(in, out, sizes, types, count); st != HSCALE_OK) return st;
+    if (const int st = written_apart(in, out, sizes, types, count, norm); st != HSCALE_OK) return st;
   return from_cuda(hscale::launch_grad_norm(in, out, sizes, types, count, clip, max_norm, norm, static_cast<double*>(workspace),
                                             as_stream(stream)));
 }

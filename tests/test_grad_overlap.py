@@ -16,12 +16,12 @@ def clip():
     build.build()
     lib = hs.load()
 
-    def call(tensors, out, types=None, ws=P):
+    def call(tensors, out, types=None, ws=P, norm=P // 2):
         """tensors: (address, elements) of each; out: addresses, or None."""
         def array(kind, v):
             return None if v is None else (kind * len(v))(*v)
         return lib.hscale_grad_clip(array(ctypes.c_void_p, [p for p, _ in tensors]), array(ctypes.c_int64, [n for _, n in tensors]),
-                                    array(ctypes.c_int32, types or [F32] * len(tensors)), len(tensors), 1.0, P,
+                                    array(ctypes.c_int32, types or [F32] * len(tensors)), len(tensors), 1.0, norm,
                                     array(ctypes.c_void_p, out), ws, 1 << 20, None)
     return call
 
@@ -50,6 +50,13 @@ A, B, C = P, P + 1024, P + 2048
 def test_overlaps_are_refused(clip, tensors, out):
     assert clip(tensors, out) == ERR_ARG
     assert clip(tensors[::-1], out[::-1] if out else None) == ERR_ARG
+
+
+@pytest.mark.parametrize("norm", [A, A + 512, A + 1020, B + 1020, P + 8192, P + 8192 + 2044])
+def test_the_norm_is_written_too(clip, norm):
+    assert clip([(A, 256), (B, 256)], [P + 8192, P + 8192 + 1024], norm=norm) == ERR_ARG
+    if norm < P + 8192:
+        assert clip([(A, 256), (B, 256)], None, norm=norm) == ERR_ARG
 
 
 def test_sizes_go_by_the_type(clip):
