@@ -464,7 +464,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   const auto release = [&](uint32_t acc) {
     tc_fence_before_sync();
     __syncwarp();
-    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+    // a warp that writes NaN runs ahead of the others: its arrivals would stand for theirs, and the next tile's MMAs overwrite
+    // what they still read
+    if (lane == 0 && have) mbar_arrive(&acc_empty[acc]);
   };
   // The epilogue: 16 slots a time, those of this warp (one of kWorkers of its quarter).
   const auto finish = [&](int i, int who, uint32_t* turn, const Finish& f) {
@@ -676,7 +678,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         uint32_t code[2] = {0u, 0u};
         const uint32_t from = src + stage * (kHalves * kHalfBytes);
         if constexpr (kPath != kDirect) {
-          if (!mbar_wait_unpack(&packed_full[stage], parity_p)) {
+          if (!mbar_wait_unpack(&packed_full[stage], parity_p, parity_p != 0)) {
             go = false;
             break;
           }

@@ -201,7 +201,9 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
   const auto release = [&](uint32_t acc) {
     tc_fence_before_sync();
     __syncwarp();
-    if (lane == 0) mbar_arrive(&acc_empty[acc]);
+    // a warp that writes NaN runs ahead of the others: its arrivals would stand for theirs, and the next tile's MMAs overwrite
+    // what they still read
+    if (lane == 0 && have) mbar_arrive(&acc_empty[acc]);
   };
   // The epilogue of the CTA's tile i: eight slots of a half a time, those of this warp.
   const auto finish = [&](int i, int who, uint32_t* turn) {
@@ -400,12 +402,13 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
     const int64_t cols = p.cols, half_cols = cols >> 1, code_cols = cols >> 4;
     const uint32_t swizzle = (uint32_t)row & 7u;  // of the unpacked tile
     uint32_t* turn = turn_at(T::kHelp ? 4 + warp - kUnpackWarp0 : 0);
-    bool go = true;
+    // after a wait that ran out: how far before the next tile the first one lies whose epilogue is owed
+    int back = 0;
     // blocks of all tiles, one after another: this group's are group, group + 2, ...
     int kb = group;
     uint32_t block = (uint32_t)group;
     int i = 0;
-    for (; i < ntiles && go; kb -= kb_count(i), ++i) {
+    for (; i < ntiles && back == 0; kb -= kb_count(i), ++i) {
       const int kbs = kb_count(i), kb0 = kb_first(i);
       const Where at = where(i);
       const int64_t e = p.plan.chunks[at.chunk].expert, o0 = (int64_t)at.to * (kHalves * kBM) + part64 * 64;
@@ -413,12 +416,12 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       // bits that a row's codes begin into a word: the same for rows 64 apart
       const uint32_t shift = p.path != kDirect && p.path != kBulk ? (uint32_t)(row0 * code_cols & 3) * 8 : 0u;
       int done = 0;
-      for (; kb < kbs && go; kb += 2, block += 2) {
+      for (; kb < kbs && back == 0; kb += 2, block += 2) {
         const uint32_t ps = block % kPackedStages, parity_p = (block / kPackedStages) & 1u;
         uint32_t q[8], code;
         if (p.path != kDirect) {
-          if (!mbar_wait_unpack(&packed_full[ps], parity_p)) {
-            go = false;
+          if (!mbar_wait_unpack(&packed_full[ps], parity_p, parity_p != 0)) {
+            back = done == 0 ? 2 : 1;
             break;
           }
           read_packed(q, smem_addr(packed + ps * kPackedBytes), row, kBK, 2 * part64, kPairRows);
@@ -447,7 +450,7 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
         }
         const uint32_t s = block % kStages;
         if (!mbar_wait_unpack(&empty[s], ((block / kStages) & 1u) ^ 1u)) {
-          go = false;
+          back = done == 0 ? 2 : 1;
           break;
         }
         uint8_t* dst = tile_a + s * T::kABytes + part64 * kGroupBytes + row * 128;
@@ -472,17 +475,16 @@ back_kernel(const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CU
       }
       // (a tile of one K block has none of this group's)
       if (T::kHelp && done == 0 && i == 1) pdl_wait_primary();
-      if (T::kHelp && done == 0 && i > 0 && go) finish(i - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
+      if (T::kHelp && done == 0 && i > 0 && back == 0) finish(i - 1, 1 + ((warp - kUnpackWarp0) >> 2), turn);
     }
     if constexpr (T::kHelp) {
-      // the last tile; after a wait that ran out (in tile i - 1) the one before it, which may not be done, and all that are
-      // left, as NaN
-      have = have && go;
+      // the last tile; after a wait that ran out all that are owed, as NaN
+      have = have && back == 0;
       pdl_wait_primary();
 #pragma unroll 1
-      for (int j = max(0, go ? ntiles - 1 : i - 2); j < ntiles; ++j) finish(j, 1 + ((warp - kUnpackWarp0) >> 2), turn);
+      for (int j = max(0, back == 0 ? ntiles - 1 : i - back); j < ntiles; ++j) finish(j, 1 + ((warp - kUnpackWarp0) >> 2), turn);
     }
-    if ((!go || !have) && lane == 0) atomicOr(failed, 1u);
+    if ((back != 0 || !have) && lane == 0) atomicOr(failed, 1u);
   } else if (p.path != kDirect && (warp == kWeightsWarp0 || p.path != kBulk)) {
     const int who = warp - kWeightsWarp0;  // whose copies are 32 of the 64 rows
     const bool loads = p.path >= kMixed && who == 0, copies = p.path != kBulk;

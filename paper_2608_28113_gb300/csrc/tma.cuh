@@ -12,7 +12,8 @@ namespace hscale {
 //
 // A build with HSCALE_STARVED_BLOCK = b (the failure tests') has a limit of a few milliseconds, and in
 // it mbar_wait_acc, the epilogues' wait for an accumulator, runs out at once in block b; with
-// HSCALE_STARVED_WAIT = 1 it is mbar_wait_unpack, the wait of the experts' unpacking warps, instead.
+// HSCALE_STARVED_WAIT = 1 it is mbar_wait_unpack, the wait of the experts' unpacking warps, instead; with 2 only
+// those that are for a later turn of the ring of packed blocks, which other tiles go before.
 #ifndef HSCALE_STARVED_BLOCK
 #define HSCALE_STARVED_BLOCK -1
 #endif
@@ -96,8 +97,9 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity));
 }
-__device__ __forceinline__ bool mbar_wait_unpack(uint64_t* bar, uint32_t parity) {
-  return (kStarvedBlock < 0 || kStarvedWait != 1 || (int)blockIdx.x != kStarvedBlock) && mbar_wait_warp(bar, parity);
+__device__ __forceinline__ bool mbar_wait_unpack(uint64_t* bar, uint32_t parity, bool later = false) {
+  const bool starved = kStarvedBlock >= 0 && (kStarvedWait == 1 || (kStarvedWait == 2 && later)) && (int)blockIdx.x == kStarvedBlock;
+  return !starved && mbar_wait_warp(bar, parity);
 }
 // The value of lane 0, which the compiler then knows to be uniform.
 __device__ __forceinline__ uint32_t warp_uniform(uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }

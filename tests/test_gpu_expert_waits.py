@@ -1,8 +1,10 @@
-"""The waits of the experts' unpacking warps running out.  In wide tiles (128 slots, 256 in the backward pass) these warps
-take part in the epilogue, and what they owe has to be NaN too, not what an earlier call left in the workspace.
+"""Waits of the experts' kernels running out in a block that has several tiles.  In wide tiles (128 slots, 256 in the backward
+pass) the unpacking warps take part in the epilogue, and what they owe has to be NaN too, not what an earlier call left in the
+workspace; and a warp that gives up must not let the next tile's MMAs overwrite what the others still read.
 
-The library is built once more with one block in which these waits run out at once; every other wait of the block
-then runs out as well, after some milliseconds, and the kernels end normally."""
+The library is built once more with one block in which some waits run out at once: of the four epilogue warps for an accumulator (0),
+of the unpacking warps (1), or those of a later turn of the ring that these read (2).  Every other wait of the block then
+runs out as well, after some milliseconds, and the kernels end normally."""
 import concurrent.futures as cf
 import ctypes
 import subprocess
@@ -20,25 +22,25 @@ BF16, U8 = torch.bfloat16, torch.uint8
 DEV = "cuda"
 
 
-@pytest.fixture(scope="module", params=[0, 1])
+@pytest.fixture(scope="module", params=[(1, 0), (0, 1), (0, 2), (1, 2)])
 def starved_unpacking(request, tmp_path_factory):
     """(block, library): the library with that block's unpacking warps starved."""
     if not torch.cuda.is_available():
         pytest.skip("no CUDA device")
     hs.load()
-    block, out = request.param, tmp_path_factory.mktemp("starved_unpacking")
+    (block, waits), out = request.param, tmp_path_factory.mktemp("starved_unpacking")
 
     def obj_of(src):
         if src.stem not in ("experts", "experts_backward"):
             return str(cuda_build.BUILD / (src.stem + ".o"))
         obj = out / (src.stem + ".o")
         subprocess.run([cuda_build.nvcc_path(), *cuda_build.ARCH, *cuda_build.NVCC_FLAGS, f"-DHSCALE_STARVED_BLOCK={block}",
-                        "-DHSCALE_STARVED_WAIT=1", "-c", str(src), "-o", str(obj)], check=True, capture_output=True)
+                        f"-DHSCALE_STARVED_WAIT={waits}", "-c", str(src), "-o", str(obj)], check=True, capture_output=True)
         return str(obj)
 
     with cf.ThreadPoolExecutor(2) as ex:
         objs = list(ex.map(obj_of, cuda_build.sources()))
-    so = out / f"libhscale_unpacking{block}.so"
+    so = out / f"libhscale_unpacking{block}{waits}.so"
     subprocess.run([cuda_build.nvcc_path(), *cuda_build.ARCH, "-shared", "-o", str(so), *objs], check=True)
     lib = ctypes.CDLL(str(so))
     for name, (res, args) in hs._SIGNATURES.items():
@@ -47,10 +49,11 @@ def starved_unpacking(request, tmp_path_factory):
     return block, lib
 
 
-# tokens: narrow tiles; wide ones, one a block; wide ones, several a block
-@pytest.mark.parametrize("t", [6, 1500, 9000])
-def test_starved_unpacking(starved_unpacking, monkeypatch, t):
-    n, inner, count, k = 512, 1024, 8, 2
+# tokens: narrow tiles; wide ones, one a block; wide ones, several a block, of as many K blocks that the waits run out
+# at the beginning of a tile and inside one
+@pytest.mark.parametrize("t, n, inner", [(6, 2048, 2048), (1500, 512, 1024), (9000, 512, 1024), (30000, 256, 384)])
+def test_starved_unpacking(starved_unpacking, monkeypatch, t, n, inner):
+    count, k = 8, 2
     args = layer(t, n, inner, count, k, seed=12, none=0.0)
     x, ids, w, gate, up, down = args
     dy, _ = rows(t, n, 0, torch.Generator().manual_seed(3))
