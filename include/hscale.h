@@ -88,7 +88,7 @@ typedef enum hscale_status {
   HSCALE_ERR_NULL = 1,      /* a required pointer is NULL                            */
   HSCALE_ERR_SHAPE = 2,     /* negative size, n not a multiple of 16, ld < n, ...    */
   HSCALE_ERR_ALIGN = 3,     /* a pointer or leading dimension breaks the alignment   */
-  HSCALE_ERR_ARG = 4,       /* an out-of-range scalar argument (window half-widths)  */
+  HSCALE_ERR_ARG = 4,       /* an out-of-range scalar argument, overlapping tensors   */
   HSCALE_ERR_CUDA = 5,      /* the CUDA runtime reported an error for a launch       */
   HSCALE_ERR_WORKSPACE = 6  /* workspace missing or smaller than the query says      */
 } hscale_status;
