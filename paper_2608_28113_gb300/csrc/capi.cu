@@ -126,7 +126,7 @@ const char* hscale_status_string(int status) {
     case HSCALE_ERR_NULL: return "a required pointer is NULL";
     case HSCALE_ERR_SHAPE: return "invalid shape (negative size, n not a multiple of 16/8, ld < n, or too large)";
     case HSCALE_ERR_ALIGN: return "misaligned pointer or leading dimension";
-    case HSCALE_ERR_ARG: return "scalar argument out of range";
+    case HSCALE_ERR_ARG: return "scalar argument out of range, or tensors that overlap";
     case HSCALE_ERR_CUDA: return "CUDA runtime error";
     case HSCALE_ERR_WORKSPACE: return "workspace missing or too small";
     default: return "unknown status";

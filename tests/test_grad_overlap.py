@@ -66,3 +66,8 @@ def test_sizes_go_by_the_type(clip):
     assert clip([(A, 256), (A, 256)], None, ws=None) == ERR_WS
     assert clip([(A, 256), (A, 256)], [C, None]) == ERR_NULL
     assert clip([(A, 256), (A, -1)], [C, C]) == ERR_SHAPE
+
+
+def test_the_refusal_says_so(clip):
+    with pytest.raises(hs.HScaleError, match="overlap"):
+        hs._check("hscale_grad_clip", clip([(A, 256), (A, 256)], None))
